@@ -259,6 +259,81 @@ int sk_get_timing(sk_state* state, double* ms, uint64_t* launches);
 #define SK_STATIC_MAX_D 262144u
 int sk_select_static(sk_state* state, uint32_t* idx_out);
 
+/* ---- Operators of language models --------------------------------------------------------------------------------
+ * What stands before and beside the optimiser step when a language model is trained: layer norm, the loss of a linear
+ * head over a large vocabulary, and the orthogonalised update that matrix parameters take instead of a coordinate-wise
+ * one.  (The paper has no counterpart for them.)  They need no handle.  Conventions, beyond those above:
+ *   - All array arguments are DEVICE pointers, element-aligned; matrices have contiguous rows, ld (in elements) apart,
+ *     ld >= the row's length.  Outputs do not overlap inputs unless said.
+ *   - type arguments are SK_F32, SK_BF16 or SK_F16.  Statistics and sums are fp32 (or wider) whatever the type.
+ *   - workspace: device memory of at least the size that the matching ..._workspace function returns for the same sizes
+ *     and pointers, 256-byte aligned, the caller's; contents do not matter before or after, and it must not be used by
+ *     anything else until the call's kernels are done.  A size of 0 allows NULL.
+ *   - stream: a cudaStream_t cast to void* (NULL = default stream).  Asynchronous; nothing allocates or synchronises.
+ *   - Extents of zero are valid: outputs that remain (sums over no rows) are zeroed.
+ *   - Infinities and NaN in an input row spread as the formulas say (into that row and into sums over rows), no further. */
+#define SK_F32  0
+#define SK_BF16 1
+#define SK_F16  2
+
+/* y = (x - mean) rstd weight + bias per row, mean and rstd = 1/sqrt(variance + eps) over the row's cols entries.
+ * x, y: rows x cols of `type`.  weight, bias: cols of `weight_type`, either may be NULL (1 and 0).  mean, rstd: rows
+ * fp32 out, what the backward pass needs; either may be NULL.  y may be x if ld_y == ld_x. */
+int sk_layer_norm(const void* x, uint64_t ld_x, void* y, uint64_t ld_y, int type, uint64_t rows, uint64_t cols,
+                  const void* weight, const void* bias, int weight_type, float eps, float* mean, float* rstd,
+                  void* stream);
+
+/* With h = (x - mean) rstd and g = dy weight: dx = rstd (g - mean(g) - h mean(g h)) per row, dweight = sum over rows of
+ * dy h, dbias = sum over rows of dy.  dx: rows x cols of `type`; dweight, dbias: cols of `dweight_type`; each may be NULL
+ * and is then not computed.  The sums over rows are formed in a fixed order (same bits every time).
+ * dx may be dy or x, with the same ld. */
+uint64_t sk_layer_norm_backward_workspace(uint64_t rows, uint64_t cols);
+int sk_layer_norm_backward(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, void* dx, uint64_t ld_dx, int type,
+                           uint64_t rows, uint64_t cols, const void* weight, int weight_type, const float* mean,
+                           const float* rstd, void* dweight, void* dbias, int dweight_type, void* workspace,
+                           uint64_t workspace_bytes, void* stream);
+
+/* Softmax cross entropy of a linear head, the logits z = hidden weight^T never stored:
+ *   lse_i = log sum_v exp z_iv;  loss_i = lse_i - z_i,targets[i].
+ * hidden: tokens x width, weight: vocab x width, both of `type` (SK_BF16 or SK_F16); targets: tokens int64; loss, lse: tokens
+ * fp32, either may be NULL.  A negative target takes no part (loss 0); a target >= vocab gives a loss of NaN.
+ * vocab >= 1; tokens, vocab, width < 2^31. */
+uint64_t sk_linear_cross_entropy_workspace(const void* hidden, uint64_t ld_hidden, const void* weight, uint64_t ld_weight,
+                                           uint64_t tokens, uint64_t vocab, uint64_t width);
+int sk_linear_cross_entropy(const void* hidden, uint64_t ld_hidden, const void* weight, uint64_t ld_weight, int type,
+                            uint64_t tokens, uint64_t vocab, uint64_t width, const int64_t* targets, float* loss,
+                            float* lse, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Its gradient: G_iv = dloss_i (exp(z_iv - lse_i) - [v = targets[i]]) (0 for rows whose target is outside 0..vocab-1),
+ * dhidden = G weight, dweight = G^T hidden.  lse: the forward pass's; dloss: tokens fp32, the gradient of the whole with respect to
+ * loss_i (1/tokens for a mean).  The vocabulary is taken in pieces whose G (in `type`; the rounding of an operand) stays below half a
+ * GiB; sums are fp32.  dhidden: tokens x width of `dhidden_type`; dweight: vocab x width of `dweight_type`; types `type` or
+ * SK_F32; either may be NULL.  dweight may be a slice of the gradient array of sk_step (element-aligned is enough). */
+uint64_t sk_linear_cross_entropy_backward_workspace(const void* hidden, uint64_t ld_hidden, const void* weight,
+                                                    uint64_t ld_weight, uint64_t tokens, uint64_t vocab, uint64_t width);
+int sk_linear_cross_entropy_backward(const float* dloss, const void* hidden, uint64_t ld_hidden, const void* weight,
+                                     uint64_t ld_weight, int type, uint64_t tokens, uint64_t vocab, uint64_t width,
+                                     const int64_t* targets, const float* lse, void* dhidden, uint64_t ld_dhidden,
+                                     int dhidden_type, void* dweight, uint64_t ld_dweight, int dweight_type,
+                                     void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Orthogonalised updates of `batch` matrices of rows x cols by `steps` Newton-Schulz products:
+ *   U = update, or with momentum M (fp32, updated in place): M = beta M + update, U = update + beta M (nesterov) or M;
+ *   X = U / (|U|_F + eps);  steps times: A = X X^T, X = (a I + b A + c A^2) X   (on the shorter side)
+ * with coefficients = {a, b, c} (HOST).  update: `type`; out: `out_type`, SK_BF16 or SK_F16.  ..._stride: elements from
+ * one matrix to the next (>= rows*ld for outputs).  Inside, matrices are fp16 times 2^12 with fp32 sums, X as a pair of them until the last two
+ * steps; the coefficients must keep singular values from [0,1] below 2 in every step, and |a| + |b| + |c| < 15.
+ * momentum may be NULL.  1 <= steps <= 32; rows, cols <= 65536; batch <= 65535. */
+uint64_t sk_orthogonalize_workspace(uint64_t batch, uint64_t rows, uint64_t cols);
+int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_update, int type, float* momentum,
+                     uint64_t ld_momentum, uint64_t stride_momentum, float beta, int nesterov, void* out, uint64_t ld_out,
+                     uint64_t stride_out, int out_type, uint64_t batch, uint64_t rows, uint64_t cols, int steps,
+                     const float* coefficients, float eps, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Waits for the stream and reports the operators' device status word of the current device (SK_EDEVICE with a message if
+ * it is not zero, after which it is cleared): bit 0, a product kernel gave up a wait and its outputs are invalid. */
+int sk_operators_sync(void* stream);
+
 const char* sk_last_error(void);
 const char* sk_version(void);
 

@@ -2,4 +2,4 @@
 
 Nothing is loaded at import time; `binding.lib()` loads the built shared library and raises if it is missing.
 """
-__all__ = ["binding", "build", "synthetic"]
+__all__ = ["binding", "build", "operators", "synthetic"]

@@ -17,7 +17,10 @@ LIB_PATH = os.environ.get("SKETCHED_AMSGRAD_LIB") or os.path.join(_HERE, "libske
 EXPORTS = ["sk_create", "sk_step", "sk_set_lr", "sk_step_host", "sk_step_host_sparse", "sk_destroy", "sk_set_stream", "sk_sync", "sk_set_option",
            "sk_get_option", "sk_hash", "sk_get", "sk_set", "sk_algorithmic_bytes", "sk_get_timing", "sk_select_static",
            "sk_exchange_floats", "sk_step_local", "sk_step_select", "sk_step_finish", "sk_last_error", "sk_version",
-           "sk_get_stats", "sk_test_fail_allocation", "sk_debug_check"]
+           "sk_get_stats", "sk_test_fail_allocation", "sk_debug_check", "sk_layer_norm", "sk_layer_norm_backward",
+           "sk_layer_norm_backward_workspace", "sk_linear_cross_entropy", "sk_linear_cross_entropy_workspace",
+           "sk_linear_cross_entropy_backward", "sk_linear_cross_entropy_backward_workspace", "sk_orthogonalize",
+           "sk_orthogonalize_workspace", "sk_operators_sync"]
 NUM_STATS = 6
 STAT_NAMES = ["threshold", "threshold_bin_count", "tie_group_count", "emitted", "floats_on_the_wire", "status"]
 STATIC_MAX_D = 262144
@@ -65,6 +68,22 @@ def lib() -> C.CDLL:
         L.sk_step_local.restype = C.c_int; L.sk_step_local.argtypes = [vp, vp, vp]
         L.sk_step_select.restype = C.c_int; L.sk_step_select.argtypes = [vp, vp, vp]
         L.sk_step_finish.restype = C.c_int; L.sk_step_finish.argtypes = [vp, vp, vp]
+        ci = C.c_int
+        L.sk_layer_norm.restype = ci
+        L.sk_layer_norm.argtypes = [vp, u64, vp, u64, ci, u64, u64, vp, vp, ci, f32, vp, vp, vp]
+        L.sk_layer_norm_backward_workspace.restype = u64; L.sk_layer_norm_backward_workspace.argtypes = [u64, u64]
+        L.sk_layer_norm_backward.restype = ci
+        L.sk_layer_norm_backward.argtypes = [vp, u64, vp, u64, vp, u64, ci, u64, u64, vp, ci, vp, vp, vp, vp, ci, vp, u64, vp]
+        for name in ("sk_linear_cross_entropy_workspace", "sk_linear_cross_entropy_backward_workspace"):
+            getattr(L, name).restype = u64; getattr(L, name).argtypes = [vp, u64, vp, u64, u64, u64, u64]
+        L.sk_linear_cross_entropy.restype = ci
+        L.sk_linear_cross_entropy.argtypes = [vp, u64, vp, u64, ci, u64, u64, u64, vp, vp, vp, vp, u64, vp]
+        L.sk_linear_cross_entropy_backward.restype = ci
+        L.sk_linear_cross_entropy_backward.argtypes = [vp, vp, u64, vp, u64, ci, u64, u64, u64, vp, vp, vp, u64, ci, vp, u64, ci, vp, u64, vp]
+        L.sk_orthogonalize_workspace.restype = u64; L.sk_orthogonalize_workspace.argtypes = [u64, u64, u64]
+        L.sk_orthogonalize.restype = ci
+        L.sk_orthogonalize.argtypes = [vp, u64, u64, ci, vp, u64, u64, f32, ci, vp, u64, u64, ci, u64, u64, u64, ci, vp, f32, vp, u64, vp]
+        L.sk_operators_sync.restype = ci; L.sk_operators_sync.argtypes = [vp]
         L.sk_last_error.restype = C.c_char_p; L.sk_last_error.argtypes = []
         L.sk_version.restype = C.c_char_p; L.sk_version.argtypes = []
         _lib = L

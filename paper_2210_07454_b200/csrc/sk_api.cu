@@ -40,6 +40,18 @@ int fail(int code, const char* fmt, ...) {
 
 }  // namespace
 
+namespace sk {
+int set_error(int code, const char* fmt, ...) {       // for the operators' entry points (sk_operators.cu)
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    g_err = buf;
+    return code;
+}
+}  // namespace sk
+
 namespace {
 
 void refresh_hash(sk_state* s) {

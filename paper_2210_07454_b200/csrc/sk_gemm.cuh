@@ -1,0 +1,423 @@
+// Matrix products on the tensor cores (tcgen05), for the operators whose epilogues differ: one kernel, templated on the
+// tile and on what happens to a finished tile.
+//
+//   D[b][i][j] = sum_p sum_k  A_p[b](i, k) * B_p[b](j, k)      p = 0 .. passes-1, 16-bit operands, 32-bit sums
+//
+// Each operand may be stored with k contiguous ("K-major") or with its row index contiguous ("MN-major"); no operand is
+// ever transposed in memory.  Two passes add a second pair of operands into the same accumulator (a matrix held as the
+// sum of two 16-bit matrices).
+//
+// A block (CG = 1) or a pair of blocks on two SMs (CG = 2) works on one output tile of 128*CG rows by BN columns at a
+// time and walks over tiles until none is left.  One warp feeds a ring of kStages shared-memory stages by TMA (64 values of k a
+// stage, 128-byte swizzle), one thread issues the matrix instructions, eight warps empty the accumulators.  Two
+// accumulators in tensor memory take turns, so the next tile's products run while this tile's epilogue does.
+//
+// Every wait has a limit.  A role whose wait runs out records kOpWait in the status word and leaves its loop; the others
+// follow when their own waits run out, so the kernel ends and the host reads an error instead of hanging.
+#pragma once
+#include <cuda.h>
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <atomic>
+#include <cstdint>
+
+#include "sk_chain.cuh"
+
+namespace sk {
+
+constexpr uint32_t kOpWait = 1u;              // status word of the operators: a wait inside a product kernel ran out
+
+constexpr int kGemmK = 64;                    // values of k per stage: 128 bytes, the width of the swizzle
+constexpr int kEpiWarps = 8;
+constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
+
+struct GemmShape {
+    uint32_t M, N;                            // output extents
+    uint32_t k_blocks;                        // stages per pass (the last one zero-filled beyond K)
+    uint32_t passes;                          // 1 or 2
+    uint32_t batch;
+    uint32_t tiles_m, tiles_n;
+    uint32_t group_m;                         // tiles are walked in bands of this many tile rows, row index fastest
+    uint32_t symmetric;                       // 1: only tiles on and below the diagonal; the epilogue mirrors them
+    uint32_t tiles;                           // total over the batch
+    uint32_t a_mn, b_mn;                      // 1: MN-major
+    uint32_t bf16;                            // operand type: 1 bf16, 0 fp16
+    uint32_t* status;
+};
+
+// ---- instruction wrappers -------------------------------------------------------------------------------------------
+__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+
+__device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
+    asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory");
+}
+__device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
+    asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// bar: a shared::cluster address (a block's own shared::cta addresses are valid ones)
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+constexpr uint32_t kWaitTries = 1u << 22;     // a try takes tens of ns at least: far beyond any product, still bounded
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t* status) {
+    for (uint32_t i = 0; i < kWaitTries; ++i)
+        if (mbar_try(bar, parity)) return true;
+    atomicOr(status, kOpWait);
+    return false;
+}
+__device__ __forceinline__ uint32_t map_to_leader(uint32_t addr) {      // the same address in block 0 of the cluster
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
+    return r;
+}
+__device__ __forceinline__ uint32_t cluster_rank() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
+    return r;
+}
+__device__ __forceinline__ void cluster_sync_all() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+
+template <int CG>
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int z) {
+    if constexpr (CG == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%3, %4, %5}], [%2];"
+            ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+            ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y), "r"(z) : "memory");
+}
+
+template <int CG>
+__device__ __forceinline__ void tmem_alloc(uint32_t smem_dst, uint32_t cols) {
+    if constexpr (CG == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_dst), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void tmem_free(uint32_t addr, uint32_t cols) {
+    if constexpr (CG == 2) {
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+    } else {
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(addr), "r"(cols));
+    }
+}
+template <int CG>
+__device__ __forceinline__ void mma_f16(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (CG == 2)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+// arrives on the barrier at this address of every block of the pair once all products issued so far are done
+template <int CG>
+__device__ __forceinline__ void mma_commit(uint32_t bar) {
+    if constexpr (CG == 2)
+        asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                     ::"r"(bar), "h"((uint16_t)3) : "memory");
+    else
+        asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
+    uint32_t r[32];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
+        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]),
+          "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
+}
+
+// Shared-memory descriptor, 128-byte swizzle.  K-major: rows of 128 bytes, groups of eight rows 1024 bytes apart.
+// MN-major: blocks of 64 row indices, 64 k deep (8192 bytes) one after the other, groups of eight k 1024 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn) {
+    const uint64_t lead = mn ? (8192u >> 4) : 1u;
+    return (uint64_t)((addr & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
+}
+
+// ---- which tile ------------------------------------------------------------------------------------------------------
+struct TileAt { uint32_t b, m, n; };
+__device__ __forceinline__ TileAt tile_at(const GemmShape& g, uint32_t t) {
+    TileAt r;
+    if (g.symmetric) {
+        const uint32_t per = g.tiles_m * (g.tiles_m + 1) / 2;
+        r.b = t / per;
+        const uint32_t q = t - r.b * per;
+        uint32_t i = (uint32_t)((sqrtf(8.0f * (float)q + 1.0f) - 1.0f) * 0.5f);
+        while (i * (i + 1) / 2 > q) --i;
+        while ((i + 1) * (i + 2) / 2 <= q) ++i;
+        r.m = i;
+        r.n = q - i * (i + 1) / 2;
+        return r;
+    }
+    const uint32_t per = g.tiles_m * g.tiles_n;
+    r.b = t / per;
+    uint32_t q = t - r.b * per;
+    const uint32_t band = q / (g.group_m * g.tiles_n);
+    q -= band * g.group_m * g.tiles_n;
+    const uint32_t rows = min(g.group_m, g.tiles_m - band * g.group_m);
+    r.n = q / rows;
+    r.m = band * g.group_m + (q - r.n * rows);
+    return r;
+}
+
+template <int CG, int BN>
+struct GemmTile {
+    static constexpr int kStageBytes = 128 * 128 + (BN / CG) * 128;      // both operands, 64 values of k
+    static constexpr int kStages = BN / CG >= 128 ? 6 : 8;               // as many as fit
+    static constexpr int kSmem = kStages * kStageBytes + 1024;           // + alignment of the swizzle
+};
+
+// Epi: struct Args; __device__ Epi(const Args&, batch, row, tile column); chunk(col, v[32]); end().  A thread holds one row of
+// the tile and gets its columns 32 at a time; the two warps that share a row take half the columns each.
+// Rows >= M are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
+template <int CG, int BN, class Epi>
+__global__ void __launch_bounds__(kGemmThreads, 1)
+k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
+       const __grid_constant__ CUtensorMap map_a2, const __grid_constant__ CUtensorMap map_b2,
+       const __grid_constant__ GemmShape g, const __grid_constant__ typename Epi::Args ea) {
+    constexpr int kStages = GemmTile<CG, BN>::kStages;
+    constexpr int kRowsB = BN / CG;
+    constexpr int kBytesA = 128 * 128, kBytesB = kRowsB * 128;
+    constexpr uint32_t kTmemCols = 2 * BN;                       // a power of two >= 32
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bars[2 * kStages + 4];
+    __shared__ uint32_t tmem_slot;
+
+    const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = CG == 2 ? cluster_rank() : 0;
+    const uint32_t stages = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t bar0 = smem_u32(bars);
+    auto full = [&](uint32_t s) { return bar0 + 8 * s; };
+    auto empty = [&](uint32_t s) { return bar0 + 8 * (kStages + s); };
+    auto acc_full = [&](uint32_t a) { return bar0 + 8 * (2 * kStages + a); };
+    auto acc_empty = [&](uint32_t a) { return bar0 + 8 * (2 * kStages + 2 + a); };
+
+    if (threadIdx.x == 0) {
+        for (uint32_t s = 0; s < (uint32_t)kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
+        for (uint32_t a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), CG * kEpiWarps); }
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 1) tmem_alloc<CG>(smem_u32(&tmem_slot), kTmemCols);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync_all();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *(volatile uint32_t*)&tmem_slot;
+
+    chain_acquire();
+
+    const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
+    const uint32_t kb = g.k_blocks * g.passes;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t it = 0;
+            bool ok = true;
+            for (uint32_t t = first; t < g.tiles && ok; t += step) {
+                const TileAt at = tile_at(g, t);
+                const int row_a = (int)(at.m * (128 * CG) + rank * 128);
+                const int row_b = (int)(at.n * BN + rank * kRowsB);
+                for (uint32_t k = 0; k < kb; ++k, ++it) {
+                    const uint32_t s = it % kStages;
+                    if (it >= (uint32_t)kStages && !(ok = mbar_wait(empty(s), ((it / kStages) - 1) & 1, g.status))) break;
+                    const bool second = k >= g.k_blocks;
+                    const CUtensorMap* ma = second ? &map_a2 : &map_a;
+                    const CUtensorMap* mb = second ? &map_b2 : &map_b;
+                    const int k0 = (int)((second ? k - g.k_blocks : k) * kGemmK);
+                    const uint32_t sa = stages + s * (kBytesA + kBytesB), sb = sa + kBytesA;
+                    uint32_t bar = full(s);
+                    if (rank == 0) mbar_expect(bar, CG * (kBytesA + kBytesB));
+                    if constexpr (CG == 2) bar = map_to_leader(bar);
+                    if (g.a_mn) {
+                        tma_load<CG>(sa, ma, bar, row_a, k0, (int)at.b);
+                        tma_load<CG>(sa + 8192, ma, bar, row_a + 64, k0, (int)at.b);
+                    } else {
+                        tma_load<CG>(sa, ma, bar, k0, row_a, (int)at.b);
+                    }
+                    if (g.b_mn) {
+#pragma unroll
+                        for (int q = 0; q < kRowsB / 64; ++q) tma_load<CG>(sb + q * 8192, mb, bar, row_b + q * 64, k0, (int)at.b);
+                    } else {
+                        tma_load<CG>(sb, mb, bar, k0, row_b, (int)at.b);
+                    }
+                }
+            }
+            // this block's own copies land in its shared memory: the last ones are waited for before the block may end
+            if (it) {
+                const uint32_t from = it > (uint32_t)kStages ? it - kStages : 0;
+                for (uint32_t q = from; q < it; ++q)
+                    if (!mbar_wait(empty(q % kStages), (q / kStages) & 1, g.status)) break;
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            // D fp32; A, B bf16 or fp16; majors; N / 8; M / 16
+            const uint32_t idesc = (1u << 4) | (g.bf16 << 7) | (g.bf16 << 10) | (g.a_mn << 15) | (g.b_mn << 16) |
+                                   ((uint32_t)(BN / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
+            const uint64_t step_a = (g.a_mn ? 2048u : 32u) >> 4, step_b = (g.b_mn ? 2048u : 32u) >> 4;
+            uint32_t it = 0, n = 0;
+            bool ok = true;
+            for (uint32_t t = first; t < g.tiles && ok; t += step, ++n) {
+                const uint32_t a = n & 1;
+                if (n >= 2 && !(ok = mbar_wait(acc_empty(a), ((n >> 1) - 1) & 1, g.status))) break;
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                for (uint32_t k = 0; k < kb; ++k, ++it) {
+                    const uint32_t s = it % kStages;
+                    if (!(ok = mbar_wait(full(s), (it / kStages) & 1, g.status))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    const uint32_t sa = stages + s * (kBytesA + kBytesB);
+                    const uint64_t da = smem_desc(sa, g.a_mn), db = smem_desc(sa + kBytesA, g.b_mn);
+#pragma unroll
+                    for (uint32_t q = 0; q < kGemmK / 16; ++q)
+                        mma_f16<CG>(tmem + a * BN, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
+                    mma_commit<CG>(empty(s));
+                }
+                mma_commit<CG>(acc_full(a));
+            }
+        }
+    } else {
+        const uint32_t w = warp - 2, quarter = warp & 3, half = w >> 2;
+        uint32_t n = 0;
+        for (uint32_t t = first; t < g.tiles; t += step, ++n) {
+            const TileAt at = tile_at(g, t);
+            const uint32_t a = n & 1;
+            if (!mbar_wait(acc_full(a), (n >> 1) & 1, g.status)) break;
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            const uint32_t row = at.m * (128 * CG) + rank * 128 + quarter * 32 + lane;
+            const uint32_t col0 = at.n * BN + half * (BN / 2);
+            Epi epi(ea, g, at, row, col0, half);
+#pragma unroll 1
+            for (uint32_t c = 0; c < BN / 2; c += 32) {
+                float v[32];
+                __syncwarp();                                    // the load needs the whole warp
+                tmem_load32(tmem + a * BN + half * (BN / 2) + c + ((quarter * 32) << 16), v);
+                if (c + 32 == BN / 2) {                          // everything is in registers: the accumulator is free
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_leader(acc_empty(a)) : acc_empty(a));
+                }
+                if (col0 + c < g.N) epi.chunk(col0 + c, v);
+            }
+            epi.end();
+        }
+    }
+
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    if constexpr (CG == 2) cluster_sync_all();                   // the other block may still signal this one's barriers
+    if (warp == 1) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        tmem_free<CG>(tmem, kTmemCols);
+    }
+}
+
+// ---- host side -------------------------------------------------------------------------------------------------------
+// A matrix of `rows` x `cols` 16-bit values, cols contiguous, ld and the batch stride in elements (multiples of 8), as the tile
+// source of a product: K-major when its columns are k, MN-major when its rows are.
+struct Operand {
+    const void* p;
+    uint64_t rows, cols, ld, batch_stride;
+    uint32_t batch;
+    bool mn;
+};
+
+bool encode_operand(CUtensorMap* map, const Operand& o, bool bf16, uint32_t box_rows);
+
+template <int CG, int BN, class Epi>
+cudaError_t launch_gemm(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, GemmShape g,
+                        const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
+    g.a_mn = a.mn;
+    g.b_mn = b.mn;
+    const uint64_t K = a.mn ? a.rows : a.cols;
+    g.k_blocks = (uint32_t)((K + kGemmK - 1) / kGemmK);
+    g.passes = a2 ? 2 : 1;
+    g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
+    g.tiles_n = (g.N + BN - 1) / BN;
+    g.tiles = g.batch * (g.symmetric ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n);
+    g.group_m = g.tiles_m < 16 ? g.tiles_m : 16;
+    if (!g.tiles) return cudaSuccess;
+    CUtensorMap ma, mb, ma2, mb2;
+    bool ok = encode_operand(&ma, a, g.bf16, 128) && encode_operand(&mb, b, g.bf16, BN / CG);
+    if (a2) ok = ok && encode_operand(&ma2, *a2, g.bf16, 128) && encode_operand(&mb2, *b2, g.bf16, BN / CG);
+    else { ma2 = ma; mb2 = mb; }
+    if (!ok) return cudaErrorInvalidValue;
+    auto kernel = k_gemm<CG, BN, Epi>;
+    static std::atomic<bool> prepared[64];                       // the attribute is a property of the kernel on a device
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    if (device >= 64 || !prepared[device]) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmTile<CG, BN>::kSmem);
+        if (e != cudaSuccess) return e;
+        if (device < 64) prepared[device] = true;
+    }
+    const uint32_t slots = (uint32_t)sm_count / CG;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((g.tiles < slots ? g.tiles : slots) * CG);
+    cfg.blockDim = dim3(kGemmThreads);
+    cfg.dynamicSmemBytes = GemmTile<CG, BN>::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    uint32_t n = 0;
+    if (CG > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = CG;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (chain) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kernel, ma, mb, ma2, mb2, g, ea);
+}
+
+// Which tile: pairs of blocks on 256 x 256, or single blocks on 128 x 128.  A large tile reads each operand half as often and is
+// what keeps the tensor cores fed (512 cycles of products against 64 KB of operands per stage, both at a pair); small
+// ones spread a small product over more SMs.  The one whose last wave ends first wins.
+inline bool wide_tiles(uint32_t M, uint32_t N, uint32_t batch, bool symmetric, int sm_count) {
+    auto count = [&](uint32_t t) {
+        const uint64_t m = (M + t - 1) / t, n = (N + t - 1) / t;
+        return batch * (symmetric ? m * (m + 1) / 2 : m * n);
+    };
+    const uint64_t slots = (uint64_t)sm_count;
+    const uint64_t wide = (count(256) + slots / 2 - 1) / (slots / 2) * 512, small = (count(128) + slots - 1) / slots * 330;
+    return wide <= small;
+}
+
+template <class Epi>
+cudaError_t launch_product(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, const GemmShape& g,
+                           const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
+    if (wide_tiles(g.M, g.N, g.batch, g.symmetric, sm_count)) return launch_gemm<2, 256, Epi>(chain, a, b, a2, b2, g, ea, sm_count, st);
+    return launch_gemm<1, 128, Epi>(chain, a, b, a2, b2, g, ea, sm_count, st);
+}
+
+}  // namespace sk

@@ -1,0 +1,348 @@
+// Softmax cross entropy of a linear head over a large vocabulary, without keeping the logits.
+//
+//   z = hidden W^T;  lse_i = log sum_v exp z_iv;  loss_i = lse_i - z_i,target(i)
+//   G_iv = dloss_i (exp(z_iv - lse_i) - [v = target(i)]);  dhidden = G W,  dW = G^T hidden
+//
+// Forward: one product whose epilogue keeps, per row and half tile, the maximum and the sum of exponentials relative to
+// it (32 bits), and the target's logit; a small kernel joins the pieces.  The logits never leave the SM.
+// Backward: the vocabulary is taken in pieces.  A product recomputes a piece's logits and its epilogue writes the piece of G (in the
+// inputs' 16-bit type, the operand type of the two products that follow); then dW's rows of the piece and the piece's share
+// of dhidden, which is added up in 32 bits over the pieces.  Bound by the tensor cores (2 T V D multiply-add flops forward, 6 backward plus 2 for
+// the recomputation); for few tokens by reading W.
+//
+// A row whose target is negative takes no part: loss 0, gradient 0.  A target >= vocab gives a loss of NaN and no gradient.
+#include "sk_gemm.cuh"
+#include "sk_operators.h"
+
+namespace sk {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f;
+__device__ __forceinline__ float exp2_fast(float x) {          // 2^x, 2 ulp
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// per (half tile, row): maximum of the logits and the sum of exp(z - maximum)
+struct StatsEpi {
+    struct Args { float2* part; float* at_target; const int64_t* targets; };
+    const Args& a;
+    const GemmShape& g;
+    uint32_t row, slot;
+    int64_t target;
+    float top = -INFINITY, sum = 0;
+    __device__ StatsEpi(const Args& a_, const GemmShape& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t half)
+        : a(a_), g(g_), row(row_), slot(at.n * 2 + half) { target = row < g.M ? a.targets[row] : -1; }
+    __device__ void chunk(uint32_t col, float (&v)[32]) {
+        const uint32_t valid = g.N - col;
+        const uint64_t d = (uint64_t)(target - (int64_t)col);
+        if (d < 32 && d < valid) {
+            float z = v[0];
+#pragma unroll
+            for (int i = 1; i < 32; ++i) z = d == (uint64_t)i ? v[i] : z;
+            a.at_target[row] = z;
+        }
+        if (valid < 32) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = (uint32_t)i < valid ? v[i] : -INFINITY;
+        }
+        float m = v[0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) m = fmaxf(m, v[i]);
+        if (m > top) {
+            sum *= exp2_fast((top - m) * kLog2e);
+            top = m;
+        }
+        // the difference first: it is exact near the maximum, whatever the logits' size
+        const float off = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sum += exp2_fast((v[i] - off) * kLog2e);
+    }
+    __device__ void end() {
+        if (row < g.M) a.part[(uint64_t)slot * g.M + row] = make_float2(top, sum);
+    }
+};
+
+// joins the pieces: a block takes 32 rows, eight threads a row
+__global__ void __launch_bounds__(256) k_head_join(const float2* part, const float* at_target, const int64_t* targets, uint32_t tokens, uint64_t vocab,
+                                                   uint32_t slots, float* loss, float* lse) {
+    __shared__ float2 s[8][33];
+    chain_acquire();
+    const uint32_t x = threadIdx.x & 31, y = threadIdx.x >> 5, row = blockIdx.x * 32 + x;
+    float top = -INFINITY, sum = 0;
+    auto add = [&](float2 p) {
+        const float m = fmaxf(top, p.x);
+        if (p.y == 0.0f) return;                               // an empty half tile
+        sum = sum * (top == m ? 1.0f : expf(top - m)) + p.y * (p.x == m ? 1.0f : expf(p.x - m));
+        top = m;
+    };
+    if (row < tokens)
+        for (uint32_t q = y; q < slots; q += 8) add(part[(uint64_t)q * tokens + row]);
+    s[y][x] = make_float2(top, sum);
+    __syncthreads();
+    if (y == 0 && row < tokens) {
+        for (int i = 1; i < 8; ++i) add(s[i][x]);
+        const float l = top + logf(sum);
+        const int64_t t = targets[row];
+        if (lse) lse[row] = l;
+        if (loss) loss[row] = t < 0 ? 0.0f : t >= (int64_t)vocab ? NAN : l - at_target[row];
+    }
+}
+
+// G's piece
+struct GradEpi {
+    struct Args { uint16_t* out; uint64_t ld; const float *lse, *dloss, *factor; const int64_t* targets; uint64_t vocab; uint32_t first; };
+    const Args& a;
+    const GemmShape& g;
+    uint32_t row;
+    float off = 0, scale = 0;
+    int64_t target = -1;
+    __device__ GradEpi(const Args& a_, const GemmShape& g_, const TileAt&, uint32_t row_, uint32_t, uint32_t) : a(a_), g(g_), row(row_) {
+        if (row < g.M) {
+            const int64_t t = a.targets[row];
+            if (t >= 0 && t < (int64_t)a.vocab) {
+                target = t - (int64_t)a.first;
+                scale = a.dloss[row] * (a.factor ? *a.factor : 1.0f);
+                off = a.lse[row];
+            }
+        }
+    }
+    __device__ void chunk(uint32_t col, float (&v)[32]) {
+        if (row >= g.M) return;
+        const uint64_t d = (uint64_t)(target - (int64_t)col);
+        if (scale != 0.0f) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = exp2_fast((v[i] - off) * kLog2e);
+            if (d < 32) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] -= d == (uint64_t)i ? 1.0f : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= scale;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = 0.0f;
+        }
+        store_row32(a.out, g.bf16 ? SK_BF16 : SK_F16, (uint64_t)row * a.ld + col, v, 32, true);
+    }
+    __device__ void end() {}
+};
+
+// a share of dhidden (`sum` carries it from piece to piece), or rows of dW
+struct OutEpi {
+    struct Args { void* out; float* sum; uint64_t ld, ld_sum; const float* factor; int type; uint32_t vec, first, last; };
+    const Args& a;
+    const GemmShape& g;
+    uint32_t row;
+    float scale;
+    __device__ OutEpi(const Args& a_, const GemmShape& g_, const TileAt&, uint32_t row_, uint32_t, uint32_t)
+        : a(a_), g(g_), row(row_), scale(a_.factor ? 1.0f / *a_.factor : 1.0f) {}
+    __device__ void chunk(uint32_t col, float (&v)[32]) {
+        if (row >= g.M) return;
+        if (!a.first) {
+            const float* s = a.sum + (uint64_t)row * a.ld_sum + col;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint32_t r[8];
+                load32b(s + 8 * q, r);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[8 * q + i] += __uint_as_float(r[i]);
+            }
+        }
+        if (!a.last) {
+            store_row32(a.sum, SK_F32, (uint64_t)row * a.ld_sum + col, v, 32, true);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] *= scale;
+        store_row32(a.out, a.type, (uint64_t)row * a.ld + col, v, g.N - col, a.vec);
+    }
+    __device__ void end() {}
+};
+
+// fp16 only: a power of two that brings the largest |dloss| to about 2^14, so that small probabilities stay above fp16's
+// smallest values; the products divide by it again
+__global__ void __launch_bounds__(1024) k_head_factor(const float* dloss, const int64_t* targets, uint32_t tokens, uint64_t vocab, float* factor) {
+    __shared__ float s[32];
+    chain_acquire();
+    float m = 0;
+    for (uint32_t i = threadIdx.x; i < tokens; i += 1024)
+        if (targets[i] >= 0 && targets[i] < (int64_t)vocab) m = fmaxf(m, fabsf(dloss[i]));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 32; ++i) m = fmaxf(m, s[i]);
+        int e = 0;
+        if (m > 0 && isfinite(m)) frexpf(m, &e);
+        e = 14 - e;
+        *factor = m > 0 && isfinite(m) ? exp2f((float)(e < -100 ? -100 : e > 100 ? 100 : e)) : 1.0f;
+    }
+}
+
+// Rows copied to a leading dimension that TMA can address; with targets, the rows that take no part become zero.  The
+// backward pass always takes the hidden states through this: in dW a token without a target is multiplied by zeros, and
+// whatever its row holds (padding may hold infinities or NaN) must not survive that.
+__global__ void __launch_bounds__(256) k_head_pack(const uint16_t* src, uint64_t ld, uint16_t* dst, uint32_t ld_dst, uint64_t rows, uint32_t cols,
+                                                   const int64_t* targets, uint64_t vocab, uint32_t vec) {
+    chain_acquire();
+    const uint32_t lane = threadIdx.x & 31;
+    for (uint64_t r = blockIdx.x * 8ull + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8ull) {
+        const bool live = !targets || (targets[r] >= 0 && targets[r] < (int64_t)vocab);
+        const uint16_t* s = src + r * ld;
+        uint16_t* d = dst + r * ld_dst;
+        if (vec)
+            for (uint32_t c = lane * 8; c < cols; c += 256) *(uint4*)(d + c) = live ? *(const uint4*)(s + c) : make_uint4(0, 0, 0, 0);
+        else
+            for (uint32_t c = lane; c < cols; c += 32) d[c] = live ? s[c] : (uint16_t)0;
+    }
+}
+
+bool addressable(const void* p, uint64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
+
+struct HeadLayout {
+    bool pack_h, pack_w;
+    uint64_t ld_pack, off_h, off_w, off_part, off_target, off_factor, off_g, ld_g, off_sum, ld_sum, piece, total;
+};
+// columns of the vocabulary per piece: G's piece is to stay below this size
+constexpr uint64_t kPieceBytes = 512ull << 20;
+
+HeadLayout layout_of(const HeadArgs& a, bool backward) {
+    HeadLayout l{};
+    uint64_t at = 0;
+    auto take = [&](uint64_t bytes) { const uint64_t r = at; at += round_up(bytes, 256); return r; };
+    l.pack_h = backward || !addressable(a.hidden, a.ld_hidden);
+    l.pack_w = !addressable(a.weight, a.ld_weight);
+    l.ld_pack = round_up(a.width, 8);
+    if (l.pack_h) l.off_h = take(a.tokens * l.ld_pack * 2);
+    if (l.pack_w) l.off_w = take(a.vocab * l.ld_pack * 2);
+    if (!backward) {
+        l.off_part = take(2 * ((a.vocab + 127) / 128) * a.tokens * sizeof(float2));
+        l.off_target = take(a.tokens * 4);
+    } else {
+        l.off_factor = take(4);
+        uint64_t pieces = (a.tokens * a.vocab * 2 + kPieceBytes - 1) / kPieceBytes;
+        l.piece = round_up((a.vocab + pieces - 1) / pieces, 256);
+        l.ld_g = l.piece < round_up(a.vocab, 32) ? l.piece : round_up(a.vocab, 32);
+        l.off_g = take(a.tokens * l.ld_g * 2);
+        l.ld_sum = round_up(a.width, 32);
+        if (l.piece < a.vocab && a.dhidden) l.off_sum = take(a.tokens * l.ld_sum * 4);
+    }
+    l.total = at;
+    return l;
+}
+
+// the operands as TMA can address them: packed copies where the caller's are not
+int pack_operands(const HeadArgs& a, bool backward, const HeadLayout& l, const OpDevice& dev, const void** h, const void** w, uint64_t* ld_h, uint64_t* ld_w,
+                  cudaStream_t st) {
+    uint8_t* ws = (uint8_t*)a.workspace;
+    *h = a.hidden; *w = a.weight; *ld_h = a.ld_hidden; *ld_w = a.ld_weight;
+    auto pack = [&](const void* src, uint64_t ld, uint64_t off, uint64_t rows, const int64_t* targets) {
+        const bool vec = a.width % 8 == 0 && addressable(src, ld);
+        const uint64_t want = (rows + 7) / 8, most = (uint64_t)dev.sm_count * 8;
+        return launch_kernel(true, k_head_pack, dim3((uint32_t)(want < most ? want : most)), 256, 0, st, (const uint16_t*)src, ld,
+                             (uint16_t*)(ws + off), (uint32_t)l.ld_pack, rows, (uint32_t)a.width, targets, a.vocab, (uint32_t)vec);
+    };
+    if (l.pack_h) {
+        SK_OP_CUDA(pack(a.hidden, a.ld_hidden, l.off_h, a.tokens, backward ? a.targets : nullptr));
+        *h = ws + l.off_h; *ld_h = l.ld_pack;
+    }
+    if (l.pack_w) {
+        SK_OP_CUDA(pack(a.weight, a.ld_weight, l.off_w, a.vocab, nullptr));
+        *w = ws + l.off_w; *ld_w = l.ld_pack;
+    }
+    return SK_OK;
+}
+
+}  // namespace
+
+uint64_t head_workspace(const HeadArgs& a) { return layout_of(a, false).total; }
+uint64_t head_backward_workspace(const HeadArgs& a) { return layout_of(a, true).total; }
+
+int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
+    const HeadLayout l = layout_of(a, false);
+    uint8_t* ws = (uint8_t*)a.workspace;
+    const void *h, *w;
+    uint64_t ld_h, ld_w;
+    int rc = pack_operands(a, false, l, dev, &h, &w, &ld_h, &ld_w, st);
+    if (rc) return rc;
+    GemmShape g{};
+    g.M = (uint32_t)a.tokens;
+    g.N = (uint32_t)a.vocab;
+    g.batch = 1;
+    g.bf16 = a.type == SK_BF16;
+    g.status = dev.status;
+    const StatsEpi::Args ea{(float2*)(ws + l.off_part), (float*)(ws + l.off_target), a.targets};
+    const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{w, a.vocab, a.width, ld_w, 0, 1, false};
+    const bool wide = wide_tiles(g.M, g.N, 1, false, dev.sm_count);
+    if (wide) SK_OP_CUDA((launch_gemm<2, 256, StatsEpi>(true, oh, ow, nullptr, nullptr, g, ea, dev.sm_count, st)));
+    else SK_OP_CUDA((launch_gemm<1, 128, StatsEpi>(true, oh, ow, nullptr, nullptr, g, ea, dev.sm_count, st)));
+    const uint32_t tile = wide ? 256 : 128, slots = 2 * ((g.N + tile - 1) / tile);
+    SK_OP_CUDA(launch_kernel(true, k_head_join, dim3((g.M + 31) / 32), 256, 0, st, (const float2*)ea.part, (const float*)ea.at_target, a.targets, g.M,
+                             a.vocab, slots, a.loss, a.lse));
+    return SK_OK;
+}
+
+int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
+    const HeadLayout l = layout_of(a, true);
+    uint8_t* ws = (uint8_t*)a.workspace;
+    const void *h, *w;
+    uint64_t ld_h, ld_w;
+    int rc = pack_operands(a, true, l, dev, &h, &w, &ld_h, &ld_w, st);
+    if (rc) return rc;
+    const uint32_t tokens = (uint32_t)a.tokens, width = (uint32_t)a.width;
+    float* factor = nullptr;
+    if (a.type == SK_F16) {
+        factor = (float*)(ws + l.off_factor);
+        SK_OP_CUDA(launch_kernel(true, k_head_factor, dim3(1), 1024, 0, st, a.dloss, a.targets, tokens, a.vocab, factor));
+    }
+    uint16_t* gbuf = (uint16_t*)(ws + l.off_g);
+    auto vec_ok = [&](const void* p, uint64_t ld, int type) { return (uintptr_t)p % 32 == 0 && ld * type_size(type) % 32 == 0; };
+    for (uint64_t v0 = 0; v0 < a.vocab; v0 += l.piece) {
+        const uint32_t n = (uint32_t)(a.vocab - v0 < l.piece ? a.vocab - v0 : l.piece);
+        const uint16_t* wp = (const uint16_t*)w + v0 * ld_w;
+        const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{wp, n, a.width, ld_w, 0, 1, false};
+        GemmShape g{};
+        g.batch = 1;
+        g.bf16 = a.type == SK_BF16;
+        g.status = dev.status;
+        g.M = tokens;
+        g.N = n;
+        const GradEpi::Args ga{gbuf, l.ld_g, a.lse, a.dloss, factor, a.targets, a.vocab, (uint32_t)v0};
+        SK_OP_CUDA(launch_product<GradEpi>(true, oh, ow, nullptr, nullptr, g, ga, dev.sm_count, st));
+        if (a.dweight) {                      // dW[v] = sum over tokens of G[t][v] hidden[t]: both factors with their rows contiguous
+            const Operand gt{gbuf, a.tokens, n, l.ld_g, 0, 1, true}, ht{h, a.tokens, a.width, ld_h, 0, 1, true};
+            g.M = n;
+            g.N = width;
+            OutEpi::Args ea{};
+            ea.out = (uint8_t*)a.dweight + v0 * a.ld_dweight * type_size(a.dweight_type);
+            ea.ld = a.ld_dweight;
+            ea.factor = factor;
+            ea.type = a.dweight_type;
+            ea.vec = vec_ok(ea.out, ea.ld, ea.type);
+            ea.first = ea.last = 1;
+            SK_OP_CUDA(launch_product<OutEpi>(true, gt, ht, nullptr, nullptr, g, ea, dev.sm_count, st));
+        }
+        if (a.dhidden) {                      // dhidden[t] += sum over the piece of G[t][v] W[v]
+            const Operand og{gbuf, a.tokens, n, l.ld_g, 0, 1, false}, wt{wp, n, a.width, ld_w, 0, 1, true};
+            g.M = tokens;
+            g.N = width;
+            OutEpi::Args ea{};
+            ea.out = a.dhidden;
+            ea.sum = (float*)(ws + l.off_sum);
+            ea.ld = a.ld_dhidden;
+            ea.ld_sum = l.ld_sum;
+            ea.factor = factor;
+            ea.type = a.dhidden_type;
+            ea.vec = vec_ok(ea.out, ea.ld, ea.type);
+            ea.first = v0 == 0;
+            ea.last = v0 + l.piece >= a.vocab;
+            SK_OP_CUDA(launch_product<OutEpi>(true, og, wt, nullptr, nullptr, g, ea, dev.sm_count, st));
+        }
+    }
+    return SK_OK;
+}
+
+}  // namespace sk

@@ -1,0 +1,152 @@
+// Declarations shared by the operators' files (layer norm, linear cross entropy, orthogonalised updates).  Not installed.
+#pragma once
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_runtime.h>
+#include <cstdint>
+
+#include "../../include/sketched_amsgrad.h"
+
+namespace sk {
+
+// records a message for sk_last_error() and returns `code` (defined with the handle's entry points)
+int set_error(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+
+#define SK_OP_CUDA(...)                                                                                        \
+    do {                                                                                                       \
+        cudaError_t err__ = (__VA_ARGS__);                                                                     \
+        if (err__ != cudaSuccess)                                                                              \
+            return sk::set_error(SK_ECUDA, "%s:%d: %s", __func__, __LINE__, cudaGetErrorString(err__));        \
+    } while (0)
+
+// What the operators know about the current device; resolved once per device.
+struct OpDevice {
+    int sm_count = 0;
+    uint32_t* status = nullptr;      // the operators' status word (a static of the library)
+};
+int op_device(OpDevice* out);        // SK_OK or an error with its message
+
+inline uint64_t round_up(uint64_t v, uint64_t to) { return (v + to - 1) / to * to; }
+inline bool type_ok(int t) { return t == SK_F32 || t == SK_BF16 || t == SK_F16; }
+inline uint32_t type_size(int t) { return t == SK_F32 ? 4 : 2; }
+
+// ---- element types on the device ------------------------------------------------------------------------------------
+__device__ __forceinline__ float to_float(float v) { return v; }
+__device__ __forceinline__ float to_float(__nv_bfloat16 v) { return __bfloat162float(v); }
+__device__ __forceinline__ float to_float(__half v) { return __half2float(v); }
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+
+// element i of an array whose type is known at run time only
+__device__ __forceinline__ float load_as(const void* p, int type, uint64_t i) {
+    if (type == SK_F32) return ((const float*)p)[i];
+    if (type == SK_BF16) return __bfloat162float(((const __nv_bfloat16*)p)[i]);
+    return __half2float(((const __half*)p)[i]);
+}
+__device__ __forceinline__ void store_as(void* p, int type, uint64_t i, float v) {
+    if (type == SK_F32) ((float*)p)[i] = v;
+    else if (type == SK_BF16) ((__nv_bfloat16*)p)[i] = __float2bfloat16_rn(v);
+    else ((__half*)p)[i] = __float2half_rn(v);
+}
+// two values rounded to 16 bits each, the first in the low half
+__device__ __forceinline__ uint32_t pack16(float a, float b, bool bf16) {
+    if (bf16) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+        return *(const uint32_t*)&h;
+    }
+    const __half2 h = __floats2half2_rn(a, b);
+    return *(const uint32_t*)&h;
+}
+__device__ __forceinline__ void store32b(void* p, const uint32_t* r) {       // 32 bytes at a 32-byte boundary
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]),
+                 "r"(r[5]), "r"(r[6]), "r"(r[7]) : "memory");
+}
+__device__ __forceinline__ void load32b(const void* p, uint32_t* r) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];" : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]),
+                 "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
+}
+
+// 32 neighbouring values of one row, rounded to the output's type; valid = how many of them exist.  vec: the row address
+// is 32-byte aligned whenever the column is a multiple of 32.
+__device__ __forceinline__ void store_row32(void* out, int type, uint64_t at, const float (&v)[32], uint32_t valid, bool vec) {
+    if (vec && valid >= 32) {
+        uint32_t r[8];
+        if (type == SK_F32) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[8 * q + i]);
+                store32b((float*)out + at + 8 * q, r);
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < 2; ++q) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) r[i] = pack16(v[16 * q + 2 * i], v[16 * q + 2 * i + 1], type == SK_BF16);
+                store32b((uint16_t*)out + at + 16 * q, r);
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 32; ++i)
+        if ((uint32_t)i < valid) store_as(out, type, at + i, v[i]);
+}
+
+// ---- launchers ---------------------------------------------------------------------------------------------------------
+struct NormArgs {
+    const void *x, *weight, *bias;
+    void* y;
+    float *mean, *rstd;
+    uint64_t rows, cols, ld_x, ld_y;
+    int type, w_type;
+    float eps;
+};
+struct NormBackwardArgs {
+    const void *dy, *x, *weight;
+    const float *mean, *rstd;
+    void *dx, *dweight, *dbias;
+    float* partial;                  // [blocks][2][cols]
+    uint64_t rows, cols, ld_dy, ld_x, ld_dx;
+    int type, w_type, dw_type;
+};
+int launch_norm(const NormArgs& a, int sm_count, cudaStream_t st);
+int launch_norm_backward(const NormBackwardArgs& a, int sm_count, cudaStream_t st);
+uint64_t norm_backward_workspace(uint64_t rows, uint64_t cols, int sm_count);
+
+// hidden (tokens x width) times vocabulary matrix (vocab x width), both of one 16-bit type
+struct HeadArgs {
+    const void *hidden, *weight;
+    const int64_t* targets;
+    uint64_t tokens, vocab, width, ld_hidden, ld_weight;
+    int type;
+    float *loss, *lse;               // forward: out; backward: lse in
+    const float* dloss;              // backward only, from here on
+    void *dhidden, *dweight;         // either may be null
+    uint64_t ld_dhidden, ld_dweight;
+    int dhidden_type, dweight_type;
+    void* workspace;
+};
+int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st);
+int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st);
+uint64_t head_workspace(const HeadArgs& a);
+uint64_t head_backward_workspace(const HeadArgs& a);
+
+struct OrthoArgs {
+    const void* update;              // batch x rows x cols
+    float* momentum;                 // same shape, or null
+    void* out;
+    uint64_t batch, rows, cols;
+    uint64_t ld_update, stride_update, ld_momentum, stride_momentum, ld_out, stride_out;
+    int type, out_type;
+    int nesterov, steps;
+    float beta, eps;
+    float coefficient[3];
+    void* workspace;
+};
+int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t st);
+uint64_t orthogonalize_workspace(const OrthoArgs& a);
+
+}  // namespace sk
