@@ -64,25 +64,43 @@ struct StatsEpi {
     }
 };
 
-// joins the pieces: a block takes 32 rows, eight threads a row
-__global__ void __launch_bounds__(256) k_head_join(const float2* part, const float* at_target, const int64_t* targets, uint32_t tokens, uint64_t vocab,
-                                                   uint32_t slots, float* loss, float* lse) {
-    __shared__ float2 s[8][33];
+// Joins the pieces: eight rows to a block, 64 threads a row; first the maximum over the pieces, then the sum relative to it.
+constexpr int kJoinThreads = 512;
+__global__ void __launch_bounds__(kJoinThreads) k_head_join(const float2* part, const float* at_target, const int64_t* targets, uint32_t tokens,
+                                                            uint64_t vocab, uint32_t slots, float* loss, float* lse) {
+    __shared__ float s[kJoinThreads / 32][8];
     chain_acquire();
-    const uint32_t x = threadIdx.x & 31, y = threadIdx.x >> 5, row = blockIdx.x * 32 + x;
-    float top = -INFINITY, sum = 0;
-    auto add = [&](float2 p) {
-        const float m = fmaxf(top, p.x);
-        if (p.y == 0.0f) return;                               // an empty half tile
-        sum = sum * (top == m ? 1.0f : expf(top - m)) + p.y * (p.x == m ? 1.0f : expf(p.x - m));
-        top = m;
-    };
-    if (row < tokens)
-        for (uint32_t q = y; q < slots; q += 8) add(part[(uint64_t)q * tokens + row]);
-    s[y][x] = make_float2(top, sum);
+    const uint32_t x = threadIdx.x & 7, y = threadIdx.x >> 3, warp = threadIdx.x >> 5, row = blockIdx.x * 8 + x;
+    const bool live = row < tokens;
+    const float2* p = part + row;
+    float top = -INFINITY;
+    if (live) {
+#pragma unroll 4
+        for (uint32_t q = y; q < slots; q += kJoinThreads / 8) top = fmaxf(top, p[(uint64_t)q * tokens].x);
+    }
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 8));
+    top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 16));
+    if ((threadIdx.x & 31) < 8) s[warp][x] = top;
     __syncthreads();
-    if (y == 0 && row < tokens) {
-        for (int i = 1; i < 8; ++i) add(s[i][x]);
+#pragma unroll
+    for (int i = 0; i < kJoinThreads / 32; ++i) top = fmaxf(top, s[i][x]);
+    float sum = 0;
+    if (live) {
+#pragma unroll 4
+        for (uint32_t q = y; q < slots; q += kJoinThreads / 8) {
+            const float2 f = p[(uint64_t)q * tokens];
+            if (f.y != 0.0f) sum += f.y * (f.x == top ? 1.0f : expf(f.x - top));      // 0: nothing above minus infinity
+        }
+    }
+    sum += __shfl_xor_sync(0xffffffffu, sum, 8);
+    sum += __shfl_xor_sync(0xffffffffu, sum, 16);
+    __syncthreads();
+    if ((threadIdx.x & 31) < 8) s[warp][x] = sum;
+    __syncthreads();
+    if (y == 0 && live) {
+        sum = 0;
+#pragma unroll
+        for (int i = 0; i < kJoinThreads / 32; ++i) sum += s[i][x];
         const float l = top + logf(sum);
         const int64_t t = targets[row];
         if (lse) lse[row] = l;
@@ -280,7 +298,7 @@ int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
     if (wide) SK_OP_CUDA((launch_gemm<2, 256, StatsEpi>(true, oh, ow, nullptr, nullptr, g, ea, dev.sm_count, st)));
     else SK_OP_CUDA((launch_gemm<1, 128, StatsEpi>(true, oh, ow, nullptr, nullptr, g, ea, dev.sm_count, st)));
     const uint32_t tile = wide ? 256 : 128, slots = 2 * ((g.N + tile - 1) / tile);
-    SK_OP_CUDA(launch_kernel(true, k_head_join, dim3((g.M + 31) / 32), 256, 0, st, (const float2*)ea.part, (const float*)ea.at_target, a.targets, g.M,
+    SK_OP_CUDA(launch_kernel(true, k_head_join, dim3((g.M + 7) / 8), kJoinThreads, 0, st, (const float2*)ea.part, (const float*)ea.at_target, a.targets, g.M,
                              a.vocab, slots, a.loss, a.lse));
     return SK_OK;
 }

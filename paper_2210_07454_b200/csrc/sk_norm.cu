@@ -3,133 +3,332 @@
 //   mu = mean(x), r = 1 / sqrt(mean((x - mu)^2) + eps), y = (x - mu) r w + b
 //   h = (x - mu) r, g = dy w:  dx = r (g - mean(g) - h mean(g h)),  dw = sum over rows of dy h,  db = sum over rows of dy
 //
-// Bound by memory: forward reads x and writes y once, backward reads x and dy and writes dx once.  A group of threads
-// (a warp for short rows, up to a block of 512 for long ones) holds a row in registers, so the second and third looks
-// at it (variance around the computed mean; dx after the two means) cost no memory traffic.  Groups walk over the rows
-// of a fixed grid; the weights stay in registers, and in the backward pass so do the sums of dw and db, of
-// which every block writes one partial row that a second, column-parallel kernel adds up in a fixed order: no atomics,
-// the same bits every time.  All statistics and sums are 32-bit.
+// Bound by memory: forward reads x and writes y once, backward reads x and dy and writes dx once.  A row belongs to 8 or 32
+// lanes of a warp or to a block, every thread to fixed columns.  What keeps the memory busy is a ring of rows in
+// shared memory that each thread fills for itself with asynchronous copies (its own columns only, so no barrier guards it): the next
+// rows travel while one is worked on, without holding registers.  Rows whose elements cannot be copied in 4 bytes or more
+// (16-bit rows of odd length) come through registers, one row ahead.  The arithmetic is two values to an instruction
+// (f32x2): with one the kernels are bound by issue (bf16 rows then take as long as fp32 ones).
+//
+// Statistics: a warp computes the mean of its part and the squares around that, and the parts are joined by the formula for
+// the variance of a union: nothing cancels whatever the mean, and warps meet once per row.  In the backward pass the sums of
+// dw and db stay in registers, and every block writes one partial row of them that a second, column-parallel kernel adds
+// up in a fixed order: no atomics, the same bits every time.  All statistics and sums are 32-bit.
 #include "sk_chain.cuh"
 #include "sk_operators.h"
+
+#include <type_traits>
 
 namespace sk {
 namespace {
 
+constexpr int kDepth = 3;                        // rows of the ring
+constexpr int kWarpThreads = 128;                // block of the kernels with several groups of lanes to a block
+
+// ---- pairs of 32-bit values ---------------------------------------------------------------------------------------------
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 f2(float x, float y) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 parts(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
+// ---- a thread's elements of a row: NV accesses of V neighbours, in NV * V / 2 pairs (of accesses where V is 1) ---------------
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Pack { T v[V]; };
 
-template <int TPR>
-__device__ __forceinline__ float group_sum(float v, float* scratch) {
+template <typename T, int V, int NV>
+__device__ __forceinline__ void unpack(const Pack<T, V> (&p)[NV], F2 (&o)[NV * V / 2]) {
+    if constexpr (V == 1) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-    if constexpr (TPR > 32) {
-        constexpr int kWarps = TPR / 32;
-        __syncthreads();                                  // the previous sum has been read by everybody
-        if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = 0;
+        for (int q = 0; q < NV / 2; ++q) o[q] = f2(to_float(p[2 * q].v[0]), to_float(p[2 * q + 1].v[0]));
+    } else {
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) v += scratch[i];
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < V / 2; ++j) {
+                F2& d = o[i * V / 2 + j];
+                if constexpr (sizeof(T) == 4) {
+                    d = f2(to_float(p[i].v[2 * j]), to_float(p[i].v[2 * j + 1]));
+                } else {
+                    const uint32_t w = ((const uint32_t*)&p[i])[j];
+                    if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+                        d = f2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+                    } else {
+                        const float2 f = __half22float2(*(const __half2*)&w);
+                        d = f2(f.x, f.y);
+                    }
+                }
+            }
     }
-    return v;
 }
-template <int TPR>
-__device__ __forceinline__ float2 group_sum2(float2 v, float2* scratch) {
-#pragma unroll
-    for (int o = 16; o; o >>= 1) {
-        v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-        v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+// where a thread's accesses lie in the row
+template <int V>
+struct Place {
+    uint32_t t, tpr, cols;
+    __device__ __forceinline__ uint32_t col(int i) const { return (i * tpr + t) * V; }
+    __device__ __forceinline__ bool in(int i) const { return col(i) < cols; }
+    // the pair with its elements beyond the row set to zero
+    __device__ __forceinline__ F2 only(int q, F2 d) const {
+        if constexpr (V == 1) {
+            const float2 f = parts(d);
+            return f2(in(2 * q) ? f.x : 0.0f, in(2 * q + 1) ? f.y : 0.0f);
+        } else {
+            return in(q / (V / 2)) ? d : f2(0, 0);
+        }
     }
-    if constexpr (TPR > 32) {
-        constexpr int kWarps = TPR / 32;
-        __syncthreads();
-        if ((threadIdx.x & 31) == 0) scratch[threadIdx.x >> 5] = v;
-        __syncthreads();
-        v = make_float2(0, 0);
+};
+template <typename T, int V, int NV>
+__device__ __forceinline__ void store(T* row, const F2 (&o)[NV * V / 2], const Place<V>& at) {
+    if constexpr (V == 1) {
 #pragma unroll
-        for (int i = 0; i < kWarps; ++i) { v.x += scratch[i].x; v.y += scratch[i].y; }
+        for (int q = 0; q < NV / 2; ++q) {
+            const float2 f = parts(o[q]);
+            if (at.in(2 * q)) row[at.col(2 * q)] = from_float<T>(f.x);
+            if (at.in(2 * q + 1)) row[at.col(2 * q + 1)] = from_float<T>(f.y);
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            Pack<T, V> p;
+#pragma unroll
+            for (int j = 0; j < V / 2; ++j) {
+                const float2 f = parts(o[i * V / 2 + j]);
+                if constexpr (sizeof(T) == 4) {
+                    p.v[2 * j] = from_float<T>(f.x);
+                    p.v[2 * j + 1] = from_float<T>(f.y);
+                } else {
+                    ((uint32_t*)&p)[j] = pack16(f.x, f.y, std::is_same<T, __nv_bfloat16>::value);
+                }
+            }
+            if (at.in(i)) *(Pack<T, V>*)(row + at.col(i)) = p;
+        }
     }
+}
+// The weights of pair q (`none` without a weight vector or beyond the row).
+template <int V>
+__device__ __forceinline__ F2 weights_of(const void* p, int type, float none, int q, const Place<V>& at) {
+    if constexpr (V == 1) {
+        return f2(p && at.in(2 * q) ? load_as(p, type, at.col(2 * q)) : none, p && at.in(2 * q + 1) ? load_as(p, type, at.col(2 * q + 1)) : none);
+    } else {
+        const int i = q / (V / 2);
+        const uint32_t c = at.col(i) + 2 * (q - i * (V / 2));
+        if (!p || !at.in(i)) return f2(none, none);
+        if (type == SK_F32 && (uintptr_t)p % 8 == 0) {
+            const float2 f = *(const float2*)((const float*)p + c);
+            return f2(f.x, f.y);
+        }
+        return f2(load_as(p, type, c), load_as(p, type, c + 1));
+    }
+}
+
+// ---- the rows on their way -------------------------------------------------------------------------------------------------
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* dst, const void* src, bool live) {            // zeroes without a source
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst), n = live ? BYTES : 0;
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(n) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(d), "l"(src), "n"(BYTES), "r"(n) : "memory");
+}
+
+// A thread's columns of N matrices' rows.
+template <typename T, int V, int NV, int N>
+struct Rows {
+    static constexpr bool kAsync = sizeof(T) * V >= 4;
+    using P = Pack<T, V>;
+    static constexpr uint32_t smem(uint32_t threads) { return kAsync ? kDepth * N * NV * threads * (uint32_t)sizeof(P) : 0; }
+    const T* src[N];
+    uint64_t ld[N], rows;
+    Place<V> at;
+    P* ring;                                     // [kDepth][N][NV][blockDim.x]
+    P ahead[kAsync ? 1 : N][kAsync ? 1 : NV];
+
+    const T* next[N];                            // the thread's first column of the row to ask for next
+    uint64_t next_row;
+
+    __device__ __forceinline__ P* slot(uint32_t s, int n, int i) const { return ring + ((s * N + n) * NV + i) * blockDim.x + threadIdx.x; }
+    __device__ __forceinline__ void issue(uint64_t step, uint32_t s) {
+        const bool live = next_row < rows;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const bool in = live && at.in(i);
+                const T* p = next[n] + i * at.tpr * V;
+                if constexpr (kAsync) {
+                    copy_async<(int)sizeof(P)>(slot(s, n, i), in ? p : src[n], in);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) ahead[n][i].v[j] = from_float<T>(0.0f);
+                    if (in) ahead[n][i] = *(const P*)p;
+                }
+            }
+            next[n] += step * ld[n];
+        }
+        next_row += step;
+        if constexpr (kAsync) asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    __device__ __forceinline__ void start(uint64_t row, uint64_t step) {
+        next_row = row;
+#pragma unroll
+        for (int n = 0; n < N; ++n) next[n] = src[n] + row * ld[n] + at.col(0);
+        issue(step, 0);
+        if constexpr (kAsync)
+#pragma unroll
+            for (int d = 1; d < kDepth - 1; ++d) issue(step, d);
+    }
+    // the row asked for longest ago, and the one kDepth - 1 (through registers: one) rows on asked for
+    __device__ __forceinline__ void take(uint64_t step, uint32_t& s, P (&out)[N][NV]) {
+        if constexpr (kAsync) {
+            const uint32_t to = s == 0 ? kDepth - 1 : s - 1;
+            issue(step, to);
+            asm volatile("cp.async.wait_group %0;" ::"n"(kDepth - 1) : "memory");
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) out[n][i] = *slot(s, n, i);
+            s = s + 1 == kDepth ? 0 : s + 1;
+        } else {
+#pragma unroll
+            for (int n = 0; n < N; ++n)
+#pragma unroll
+                for (int i = 0; i < NV; ++i) out[n][i] = ahead[n][i];
+            issue(step, 0);
+        }
+    }
+};
+
+template <int G>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+    for (int o = (G ? G : 32) / 2; o; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
 }
 
-// TPR threads per row (32, or the whole block), NV accesses of V elements per thread; TPR * NV * V >= cols.
-template <typename T, int V, int NV, int TPR>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) k_norm(const NormArgs a) {
-    __shared__ float scratch[TPR / 32];
-    constexpr int kGroups = TPR < 128 ? 128 / TPR : 1;
-    const uint32_t t = threadIdx.x % TPR, group = threadIdx.x / TPR;
-    const uint32_t cols = (uint32_t)a.cols;
+// G lanes of a warp per row, or (G = 0) the block; threads per row * NV * V >= cols
+template <typename T, int V, int NV, int G, int MAXT, int BLOCKS>
+__global__ void __launch_bounds__(MAXT, BLOCKS) k_norm(const NormArgs a) {
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ float2 warp_stats[2][32];
+    constexpr int kQ = NV * V / 2;
+    const uint32_t tpr = G ? G : blockDim.x, groups = blockDim.x / tpr, warps = blockDim.x >> 5;
+    const Place<V> at{threadIdx.x % tpr, tpr, (uint32_t)a.cols};
+    const uint64_t step = (uint64_t)gridDim.x * groups;
+    uint64_t base = (uint64_t)blockIdx.x * groups, row = base + threadIdx.x / tpr;
+    // columns of the row that the row's lanes, or warp `w` of the block, hold
+    auto count_of = [&](uint32_t w) {
+        uint32_t n = 0;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const uint32_t from = (i * tpr + w * 32) * V, to = from + (G ? G : 32) * V;
+            n += from < at.cols ? (to < at.cols ? to : at.cols) - from : 0;
+        }
+        return (float)n;
+    };
+    const uint32_t lane = threadIdx.x & 31;
+    const float part = count_of(G ? 0 : threadIdx.x >> 5), part_inv = part > 0 ? 1.0f / part : 0.0f, inv = 1.0f / (float)at.cols;
+    const float lane_n = G == 0 && lane < warps ? count_of(lane) : 0.0f, lane_inv = lane_n > 0 ? 1.0f / lane_n : 0.0f;   // of warp `lane`
     chain_acquire();
-    float w[NV * V], b[NV * V];
+    F2 w[kQ], b[kQ];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int q = 0; q < kQ; ++q) {
+        w[q] = weights_of<V>(a.weight, a.w_type, 1.0f, q, at);
+        b[q] = weights_of<V>(a.bias, a.w_type, 0.0f, q, at);
+    }
+    Rows<T, V, NV, 1> in{{(const T*)a.x}, {a.ld_x}, a.rows, at, (Pack<T, V>*)ring};
+    in.start(row, step);
+    uint32_t slot = 0, turn = 0;
+    for (; base < a.rows; base += step, row += step, turn ^= 1) {             // every lane stays in the loop
+        Pack<T, V> x[1][NV];
+        F2 v[kQ];
+        in.take(step, slot, x);
+        unpack<T, V, NV>(x[0], v);
+        F2 s = f2(0, 0);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const uint32_t c = (i * TPR + t) * V + j;
-            w[i * V + j] = c < cols && a.weight ? load_as(a.weight, a.w_type, c) : 1.0f;
-            b[i * V + j] = c < cols && a.bias ? load_as(a.bias, a.w_type, c) : 0.0f;
+        for (int q = 0; q < kQ; ++q) s = s + v[q];
+        float2 f = parts(s);
+        float mean = lanes_sum<G>(f.x + f.y) * part_inv;
+        s = f2(0, 0);
+        F2 minus = f2(-mean, -mean);
+#pragma unroll
+        for (int q = 0; q < kQ; ++q) {
+            const F2 d = at.only(q, v[q] + minus);
+            s = fma2(d, d, s);
         }
-    const float inv = 1.0f / (float)cols;
-    for (uint64_t row = (uint64_t)blockIdx.x * kGroups + group; row < a.rows; row += (uint64_t)gridDim.x * kGroups) {
-        const T* x = (const T*)a.x + row * a.ld_x;
-        Pack<T, V> p[NV];
-        float sum = 0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t c = (i * TPR + t) * V;
-            if (c < cols) p[i] = *(const Pack<T, V>*)(x + c);
-            else
-#pragma unroll
-                for (int j = 0; j < V; ++j) p[i].v[j] = from_float<T>(0.0f);
+        f = parts(s);
+        float squares = lanes_sum<G>(f.x + f.y);
+        if constexpr (G == 0) {
+            if ((threadIdx.x & 31) == 0) warp_stats[turn][threadIdx.x >> 5] = make_float2(mean * part, squares);
+            __syncthreads();                              // two sets in turn: nobody is a whole row ahead of a reader
+            const float2 q = lane < warps ? warp_stats[turn][lane] : make_float2(0, 0);       // a lane for every warp
+            mean = lanes_sum<32>(q.x) * inv;
+            const float d = q.x * lane_inv - mean;
+            squares = lanes_sum<32>(q.y + d * d * lane_n);
         }
+        const float rstd = rsqrtf(squares * inv + a.eps);
+        if (G && row >= a.rows) continue;
+        minus = f2(-mean, -mean);
+        const F2 scale = f2(rstd, rstd);
 #pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) sum += to_float(p[i].v[j]);
-        const float mean = group_sum<TPR>(sum, scratch) * inv;
-        float sq = 0;
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float d = to_float(p[i].v[j]) - mean;
-                if ((i * TPR + t) * V < cols) sq += d * d;
-            }
-        const float rstd = rsqrtf(group_sum<TPR>(sq, scratch) * inv + a.eps);
-        T* y = (T*)a.y + row * a.ld_y;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t c = (i * TPR + t) * V;
-            Pack<T, V> o;
-#pragma unroll
-            for (int j = 0; j < V; ++j) o.v[j] = from_float<T>((to_float(p[i].v[j]) - mean) * rstd * w[i * V + j] + b[i * V + j]);
-            if (c < cols) *(Pack<T, V>*)(y + c) = o;
-        }
-        if (t == 0) {
+        for (int q = 0; q < kQ; ++q) v[q] = fma2((v[q] + minus) * scale, w[q], b[q]);
+        store<T, V, NV>((T*)a.y + row * a.ld_y, v, at);
+        if (at.t == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
     }
+    if constexpr (Rows<T, V, NV, 1>::kAsync) asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+// Sums of a row over a block's threads (the long-row kernels)
+template <int N>
+__device__ __forceinline__ void block_sum(float (&v)[N], float (*scratch)[N]) {
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = lanes_sum<32>(v[k]);
+    const uint32_t warps = blockDim.x >> 5;
+    __syncthreads();                                      // the previous sums have been read by everybody
+    if ((threadIdx.x & 31) == 0)
+#pragma unroll
+        for (int k = 0; k < N; ++k) scratch[threadIdx.x >> 5][k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < N; ++k) v[k] = scratch[0][k];
+    for (uint32_t i = 1; i < warps; ++i)
+#pragma unroll
+        for (int k = 0; k < N; ++k) v[k] += scratch[i][k];
 }
 
 // Rows longer than the register kernels hold: the block looks at the row three times, the later looks from L2.
 constexpr int kLongThreads = 512;
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) k_norm_long(const NormArgs a) {
-    __shared__ float scratch[kLongThreads / 32];
+    __shared__ float scratch[32][1];
     chain_acquire();
     const float inv = 1.0f / (float)a.cols;
     for (uint64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
         const T* x = (const T*)a.x + row * a.ld_x;
         T* y = (T*)a.y + row * a.ld_y;
-        float sum = 0, sq = 0;
-        for (uint64_t c = threadIdx.x; c < a.cols; c += kLongThreads) sum += to_float(x[c]);
-        const float mean = group_sum<kLongThreads>(sum, scratch) * inv;
+        float sum[1] = {0}, sq[1] = {0};
+        for (uint64_t c = threadIdx.x; c < a.cols; c += kLongThreads) sum[0] += to_float(x[c]);
+        block_sum<1>(sum, scratch);
+        const float mean = sum[0] * inv;
         for (uint64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
             const float d = to_float(x[c]) - mean;
-            sq += d * d;
+            sq[0] += d * d;
         }
-        const float rstd = rsqrtf(group_sum<kLongThreads>(sq, scratch) * inv + a.eps);
+        block_sum<1>(sq, scratch);
+        const float rstd = rsqrtf(sq[0] * inv + a.eps);
         for (uint64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
             const float w = a.weight ? load_as(a.weight, a.w_type, c) : 1.0f, b = a.bias ? load_as(a.bias, a.w_type, c) : 0.0f;
             y[c] = from_float<T>((to_float(x[c]) - mean) * rstd * w + b);
@@ -141,101 +340,102 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_long(const NormArgs a) {
     }
 }
 
-template <typename T, int V, int NV, int TPR>
-__global__ void __launch_bounds__(TPR < 128 ? 128 : TPR) k_norm_backward(const NormBackwardArgs a) {
-    constexpr int kGroups = TPR < 128 ? 128 / TPR : 1;
-    constexpr int kPer = NV * V;
-    __shared__ float2 scratch[TPR / 32];
-    __shared__ float gather[kGroups > 1 ? kGroups : 1][kGroups > 1 ? TPR * V : 1];
-    const uint32_t t = threadIdx.x % TPR, group = threadIdx.x / TPR;
-    const uint32_t cols = (uint32_t)a.cols;
+template <typename T, int V, int NV, int G, int MAXT, int BLOCKS>
+__global__ void __launch_bounds__(MAXT, BLOCKS) k_norm_backward(const NormBackwardArgs a) {
+    extern __shared__ __align__(16) uint8_t ring[];
+    __shared__ float2 warp_sums[2][32];
+    __shared__ float gather[G ? kWarpThreads * NV * V : 1];
+    constexpr int kQ = NV * V / 2;
+    const uint32_t tpr = G ? G : blockDim.x, groups = blockDim.x / tpr, warps = blockDim.x >> 5;
+    const Place<V> at{threadIdx.x % tpr, tpr, (uint32_t)a.cols};
+    const float inv = 1.0f / (float)at.cols;
+    const uint64_t step = (uint64_t)gridDim.x * groups;
+    uint64_t base = (uint64_t)blockIdx.x * groups, row = base + threadIdx.x / tpr;
     chain_acquire();
-    float w[kPer], dw[kPer], db[kPer];
+    F2 w[kQ], dw[kQ], db[kQ];
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
+    for (int q = 0; q < kQ; ++q) {
+        w[q] = weights_of<V>(a.weight, a.w_type, 1.0f, q, at);
+        dw[q] = db[q] = f2(0, 0);
+    }
+    Rows<T, V, NV, 2> in{{(const T*)a.x, (const T*)a.dy}, {a.ld_x, a.ld_dy}, a.rows, at, (Pack<T, V>*)ring};
+    in.start(row, step);
+    uint32_t slot = 0, turn = 0;
+    float next_mean = row < a.rows ? a.mean[row] : 0.0f, next_rstd = row < a.rows ? a.rstd[row] : 0.0f;
+    for (; base < a.rows; base += step, row += step, turn ^= 1) {             // every lane stays in the loop
+        Pack<T, V> v[2][NV];
+        in.take(step, slot, v);
+        const float mean = next_mean, rstd = next_rstd;
+        const bool more = row + step < a.rows;
+        next_mean = more ? a.mean[row + step] : 0.0f;
+        next_rstd = more ? a.rstd[row + step] : 0.0f;
+        const F2 minus = f2(-mean, -mean), scale = f2(rstd, rstd);
+        F2 h[kQ], g[kQ], s1 = f2(0, 0), s2 = f2(0, 0);
+        unpack<T, V, NV>(v[0], h);
+        unpack<T, V, NV>(v[1], g);
 #pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const uint32_t c = (i * TPR + t) * V + j;
-            w[i * V + j] = c < cols && a.weight ? load_as(a.weight, a.w_type, c) : 1.0f;
-            dw[i * V + j] = db[i * V + j] = 0.0f;
+        for (int q = 0; q < kQ; ++q) {                    // beyond the row dy is zero, and so is every term
+            h[q] = (h[q] + minus) * scale;
+            dw[q] = fma2(g[q], h[q], dw[q]);
+            db[q] = db[q] + g[q];
+            g[q] = g[q] * w[q];
+            s1 = s1 + g[q];
+            s2 = fma2(g[q], h[q], s2);
         }
-    const float inv = 1.0f / (float)cols;
-    for (uint64_t row = (uint64_t)blockIdx.x * kGroups + group; row < a.rows; row += (uint64_t)gridDim.x * kGroups) {
-        const T* x = (const T*)a.x + row * a.ld_x;
-        const T* dy = (const T*)a.dy + row * a.ld_dy;
-        Pack<T, V> px[NV], pd[NV];
-        const float mean = a.mean[row], rstd = a.rstd[row];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t c = (i * TPR + t) * V;
-            if (c < cols) {
-                px[i] = *(const Pack<T, V>*)(x + c);
-                pd[i] = *(const Pack<T, V>*)(dy + c);
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) { px[i].v[j] = from_float<T>(mean); pd[i].v[j] = from_float<T>(0.0f); }
-            }
-        }
-        float2 s = make_float2(0, 0);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const int q = i * V + j;
-                const float h = (to_float(px[i].v[j]) - mean) * rstd, d = to_float(pd[i].v[j]), g = d * w[q];
-                s.x += g;
-                s.y += g * h;
-                dw[q] += d * h;
-                db[q] += d;
-            }
         if (!a.dx) continue;
-        s = group_sum2<TPR>(s, scratch);
-        const float m1 = s.x * inv, m2 = s.y * inv;
-        T* dx = (T*)a.dx + row * a.ld_dx;
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const uint32_t c = (i * TPR + t) * V;
-            Pack<T, V> o;
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float h = (to_float(px[i].v[j]) - mean) * rstd, g = to_float(pd[i].v[j]) * w[i * V + j];
-                o.v[j] = from_float<T>(rstd * (g - m1 - h * m2));
+        const float2 p1 = parts(s1), p2 = parts(s2);
+        float m1 = lanes_sum<G>(p1.x + p1.y), m2 = lanes_sum<G>(p2.x + p2.y);
+        if constexpr (G == 0) {
+            if ((threadIdx.x & 31) == 0) warp_sums[turn][threadIdx.x >> 5] = make_float2(m1, m2);
+            __syncthreads();                              // two sets in turn: nobody is a whole row ahead of a reader
+            m1 = m2 = 0;
+            for (uint32_t k = 0; k < warps; ++k) {
+                m1 += warp_sums[turn][k].x;
+                m2 += warp_sums[turn][k].y;
             }
-            if (c < cols) *(Pack<T, V>*)(dx + c) = o;
+        }
+        if (G && row >= a.rows) continue;
+        m1 *= -inv * rstd;
+        m2 *= -inv * rstd;
+#pragma unroll
+        for (int q = 0; q < kQ; ++q) g[q] = fma2(g[q], scale, fma2(h[q], f2(m2, m2), f2(m1, m1)));
+        store<T, V, NV>((T*)a.dx + row * a.ld_dx, g, at);
+    }
+    if constexpr (Rows<T, V, NV, 2>::kAsync) asm volatile("cp.async.wait_all;" ::: "memory");
+    if (!a.partial) return;
+    float* out = a.partial + (uint64_t)blockIdx.x * 2 * at.cols;
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float mine[NV * V];
+#pragma unroll
+        for (int q = 0; q < kQ; ++q) {
+            const float2 f = parts(which ? db[q] : dw[q]);
+            mine[2 * q] = f.x;
+            mine[2 * q + 1] = f.y;
+        }
+        if constexpr (G != 0) {                           // the block's rows share their columns: one sum of them
+            const uint32_t width = G * NV * V;
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < NV * V; ++k) gather[(threadIdx.x / G) * width + at.col(k / V) + k % V] = mine[k];
+            __syncthreads();
+            for (uint32_t c = threadIdx.x; c < at.cols; c += blockDim.x) {
+                float sum = 0;
+                for (uint32_t k = 0; k < groups; ++k) sum += gather[k * width + c];
+                out[(uint64_t)which * at.cols + c] = sum;
+            }
+        } else {
+#pragma unroll
+            for (int k = 0; k < NV * V; ++k)
+                if (at.in(k / V)) out[(uint64_t)which * at.cols + at.col(k / V) + k % V] = mine[k];
         }
     }
-    if (!a.partial) return;
-    float* out = a.partial + (uint64_t)blockIdx.x * 2 * cols;
-#pragma unroll
-    for (int which = 0; which < 2; ++which)
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if constexpr (kGroups > 1) {
-                __syncthreads();
-#pragma unroll
-                for (int j = 0; j < V; ++j) gather[group][t * V + j] = which ? db[i * V + j] : dw[i * V + j];
-                __syncthreads();
-                for (uint32_t q = threadIdx.x; q < TPR * V; q += blockDim.x) {
-                    const uint32_t c = i * TPR * V + q;
-                    float v = 0;
-#pragma unroll
-                    for (int k = 0; k < kGroups; ++k) v += gather[k][q];
-                    if (c < cols) out[(uint64_t)which * cols + c] = v;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const uint32_t c = (i * TPR + t) * V + j;
-                    if (c < cols) out[(uint64_t)which * cols + c] = which ? db[i * V + j] : dw[i * V + j];
-                }
-            }
-        }
 }
 
 // Long rows, backward: the sums of a block are kept in its partial row in memory (own columns only, so no races).
 template <typename T>
 __global__ void __launch_bounds__(kLongThreads) k_norm_backward_long(const NormBackwardArgs a) {
-    __shared__ float2 scratch[kLongThreads / 32];
+    __shared__ float scratch[32][2];
     chain_acquire();
     const float inv = 1.0f / (float)a.cols;
     float* part = a.partial ? a.partial + (uint64_t)blockIdx.x * 2 * a.cols : nullptr;
@@ -244,125 +444,169 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_backward_long(const NormB
         const T* x = (const T*)a.x + row * a.ld_x;
         const T* dy = (const T*)a.dy + row * a.ld_dy;
         const float mean = a.mean[row], rstd = a.rstd[row];
-        float2 s = make_float2(0, 0);
+        float s[2] = {0, 0};
         for (uint64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
             const float h = (to_float(x[c]) - mean) * rstd, d = to_float(dy[c]);
             const float g = a.weight ? d * load_as(a.weight, a.w_type, c) : d;
-            s.x += g;
-            s.y += g * h;
+            s[0] += g;
+            s[1] += g * h;
             if (part) {
                 part[c] = (fresh ? 0.0f : part[c]) + d * h;
                 part[a.cols + c] = (fresh ? 0.0f : part[a.cols + c]) + d;
             }
         }
-        s = group_sum2<kLongThreads>(s, scratch);
+        block_sum<2>(s, scratch);
         if (!a.dx) continue;
         T* dx = (T*)a.dx + row * a.ld_dx;
         for (uint64_t c = threadIdx.x; c < a.cols; c += kLongThreads) {
             const float h = (to_float(x[c]) - mean) * rstd;
             const float g = to_float(dy[c]) * (a.weight ? load_as(a.weight, a.w_type, c) : 1.0f);
-            dx[c] = from_float<T>(rstd * (g - s.x * inv - h * (s.y * inv)));
+            dx[c] = from_float<T>(rstd * (g - s[0] * inv - h * (s[1] * inv)));
         }
     }
 }
 
-// Adds the blocks' partial rows, in block order within each of the eight rows of threads, these in order.
+// Adds the blocks' partial rows: eight columns to a block, 32 threads a column, in a fixed order.
 __global__ void __launch_bounds__(256) k_norm_sum(const float* partial, uint32_t blocks, uint32_t cols, void* dweight, void* dbias, int type) {
-    __shared__ float s[8][33];
-    const uint32_t x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const uint64_t c = (uint64_t)blockIdx.x * 32 + x;            // over both sums: 2 * cols columns
+    __shared__ float s[8][8];
+    const uint32_t x = threadIdx.x & 7, y = threadIdx.x >> 3;
+    const uint64_t c = (uint64_t)blockIdx.x * 8 + x, width = 2ull * cols;    // over both sums
     chain_acquire();
     float v = 0;
-    if (c < 2ull * cols)
-        for (uint32_t b = y; b < blocks; b += 8) v += partial[(uint64_t)b * 2 * cols + c];
-    s[y][x] = v;
+    if (c < width) {
+#pragma unroll 8
+        for (uint32_t b = y; b < blocks; b += 32) v += partial[b * width + c];
+    }
+    v += __shfl_xor_sync(0xffffffffu, v, 8);
+    v += __shfl_xor_sync(0xffffffffu, v, 16);
+    if ((threadIdx.x & 31) < 8) s[threadIdx.x >> 5][x] = v;
     __syncthreads();
-    if (y == 0 && c < 2ull * cols) {
+    if (threadIdx.x < 8 && c < width) {
+        v = 0;
 #pragma unroll
-        for (int i = 1; i < 8; ++i) v += s[i][x];
+        for (int i = 0; i < 8; ++i) v += s[i][x];
         void* out = c < cols ? dweight : dbias;
         if (out) store_as(out, type, c < cols ? c : c - cols, v);
     }
 }
 
-// threads per row and values per thread by the row's length; cap = values a thread may hold
-struct NormPlan { uint32_t tpr, per; };
-NormPlan plan_norm(uint64_t cols) {
-    if (cols <= 256) return {32, 8};
-    if (cols <= 1024) return {32, 32};
-    if (cols <= 4096) return {128, 32};
-    if (cols <= 16384) return {512, 32};
-    return {0, 0};
+// Lanes per row (0: the block), threads of the block, values per thread.  More values a thread spread what a row costs each
+// thread whatever its share (sums over lanes, addresses) over more of them.
+struct NormPlan { uint32_t lanes, threads, per; };
+NormPlan plan_lanes(uint64_t cols, uint32_t most) {          // a row to 8 or 32 lanes of a warp
+    if (cols <= 64) return {8, kWarpThreads, 8};
+    for (uint32_t per = 8; per <= most; per *= 2)
+        if (cols <= 32 * per) return {32, kWarpThreads, per};
+    return {0, 0, 0};
 }
+NormPlan plan_block(uint64_t cols, uint32_t per, uint32_t most) {
+    const uint64_t threads = round_up((cols + per - 1) / per, 32);
+    return threads <= most ? NormPlan{0, (uint32_t)threads, per} : NormPlan{0, 0, 0};
+}
+// Blocks: as many as stay resident, rows dealt out evenly over them.
+uint32_t norm_blocks(uint64_t rows, const NormPlan& p, int sm_count, uint32_t threads_per_sm) {
+    const uint64_t threads = p.threads ? p.threads : kLongThreads, groups = p.lanes ? threads / p.lanes : 1;
+    const uint64_t want = (rows + groups - 1) / groups;
+    const uint64_t per_sm = threads_per_sm / threads < 1 ? 1 : threads_per_sm / threads < 24 ? threads_per_sm / threads : 24;
+    const uint64_t most = (uint64_t)sm_count * per_sm;
+    if (want <= most) return (uint32_t)(want ? want : 1);
+    const uint64_t rounds = (want + most - 1) / most;
+    return (uint32_t)((want + rounds - 1) / rounds);
+}
+
+template <auto kernel, typename Args>
+cudaError_t launch_rows(dim3 grid, uint32_t threads, uint32_t smem, cudaStream_t st, const Args& a) {
+    if (smem > 40 * 1024) {                      // with the kernel's own arrays, beyond what needs no permission
+        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+    }
+    return launch_kernel(true, kernel, grid, threads, smem, st, a);
+}
+
+template <typename T, int V, int PER, int G, int MAXT, int BLOCKS>
+cudaError_t run_norm(const NormArgs& a, const NormPlan& p, int sm_count, cudaStream_t st) {
+    return launch_rows<k_norm<T, V, PER / V, G, MAXT, BLOCKS>>(dim3(norm_blocks(a.rows, p, sm_count, MAXT * BLOCKS)), p.threads,
+                                                               Rows<T, V, PER / V, 1>::smem(p.threads), st, a);
+}
+template <typename T, int V>
+int norm_typed(const NormArgs& a, int sm_count, cudaStream_t st) {
+    cudaError_t e;
+    NormPlan p = plan_lanes(a.cols, V > 1 ? 32 : 8);
+    if (p.lanes == 8) e = run_norm<T, V, 8, 8, kWarpThreads, 8>(a, p, sm_count, st);
+    else if (p.per == 8) e = run_norm<T, V, 8, 32, kWarpThreads, 8>(a, p, sm_count, st);
+    else if (V > 1 && p.per == 16) e = run_norm<T, V, 16, 32, kWarpThreads, 6>(a, p, sm_count, st);
+    else if (V > 1 && p.per == 32) e = run_norm<T, V, 32, 32, kWarpThreads, 4>(a, p, sm_count, st);
+    else if (V > 1 && (p = plan_block(a.cols, 32, 256)).threads) e = run_norm<T, V, 32, 0, 256, 2>(a, p, sm_count, st);
+    else if ((p = plan_block(a.cols, 16, 256)).threads) e = run_norm<T, V, 16, 0, 256, 3>(a, p, sm_count, st);
+    else if ((p = plan_block(a.cols, 16, 1024)).threads) e = run_norm<T, V, 16, 0, 1024, 1>(a, p, sm_count, st);
+    else e = launch_rows<k_norm_long<T>>(dim3(norm_blocks(a.rows, p, sm_count, 2048)), kLongThreads, 0, st, a);
+    SK_OP_CUDA(e);
+    return SK_OK;
+}
+
+// The plan decides how many partial rows there are, so the workspace's size needs it too.
 NormPlan plan_backward(uint64_t cols) {
-    if (cols <= 256) return {32, 8};
-    if (cols <= 1024) return {128, 8};
-    if (cols <= 2048) return {128, 16};
-    if (cols <= 8192) return {512, 16};
-    return {0, 0};
+    NormPlan p = plan_lanes(cols, 16);
+    if (!p.threads) p = plan_block(cols, 16, 512);
+    return p;
 }
 uint32_t backward_blocks(uint64_t rows, uint64_t cols, int sm_count) {
     const NormPlan p = plan_backward(cols);
-    const uint64_t groups = p.tpr == 32 ? 4 : 1;
-    const uint64_t want = (rows + groups - 1) / groups, most = (uint64_t)sm_count * (p.tpr == 512 || !p.tpr ? 2 : 4);
-    return (uint32_t)(want < most ? (want ? want : 1) : most);
+    return norm_blocks(rows, p, sm_count, p.threads && p.per == 8 ? 768 : 512);
 }
-
-template <typename T, int V>
-int norm_typed(const NormArgs& a, int sm_count, cudaStream_t st) {
-    const NormPlan p = plan_norm(a.cols);
-    const uint64_t groups = p.tpr == 32 ? 4 : 1;
-    const uint64_t want = (a.rows + groups - 1) / groups, most = (uint64_t)sm_count * (p.tpr == 512 || !p.tpr ? 4 : 12);
-    const dim3 grid((uint32_t)(want < most ? want : most));
-    cudaError_t e;
-    if (p.tpr == 32 && p.per == 8) e = launch_kernel(true, k_norm<T, V, 8 / V, 32>, grid, 128, 0, st, a);
-    else if (p.tpr == 32) e = launch_kernel(true, k_norm<T, V, 32 / V, 32>, grid, 128, 0, st, a);
-    else if (p.tpr == 128) e = launch_kernel(true, k_norm<T, V, 32 / V, 128>, grid, 128, 0, st, a);
-    else if (p.tpr == 512) e = launch_kernel(true, k_norm<T, V, 32 / V, 512>, grid, 512, 0, st, a);
-    else e = launch_kernel(true, k_norm_long<T>, grid, kLongThreads, 0, st, a);
-    SK_OP_CUDA(e);
-    return SK_OK;
+template <typename T, int V, int PER, int G, int MAXT, int BLOCKS>
+cudaError_t run_backward(const NormBackwardArgs& a, const NormPlan& p, uint32_t blocks, cudaStream_t st) {
+    return launch_rows<k_norm_backward<T, V, PER / V, G, MAXT, BLOCKS>>(dim3(blocks), p.threads, Rows<T, V, PER / V, 2>::smem(p.threads), st, a);
 }
 template <typename T, int V>
 int norm_backward_typed(const NormBackwardArgs& a, int sm_count, cudaStream_t st) {
     const NormPlan p = plan_backward(a.cols);
     const uint32_t blocks = backward_blocks(a.rows, a.cols, sm_count);
-    const dim3 grid(blocks);
     cudaError_t e;
-    if (p.tpr == 32) e = launch_kernel(true, k_norm_backward<T, V, 8 / V, 32>, grid, 128, 0, st, a);
-    else if (p.tpr == 128 && p.per == 8) e = launch_kernel(true, k_norm_backward<T, V, 8 / V, 128>, grid, 128, 0, st, a);
-    else if (p.tpr == 128) e = launch_kernel(true, k_norm_backward<T, V, 16 / V, 128>, grid, 128, 0, st, a);
-    else if (p.tpr == 512) e = launch_kernel(true, k_norm_backward<T, V, 16 / V, 512>, grid, 512, 0, st, a);
-    else e = launch_kernel(true, k_norm_backward_long<T>, grid, kLongThreads, 0, st, a);
+    if (p.lanes == 8) e = run_backward<T, V, 8, 8, kWarpThreads, 6>(a, p, blocks, st);
+    else if (p.lanes == 32 && p.per == 8) e = run_backward<T, V, 8, 32, kWarpThreads, 6>(a, p, blocks, st);
+    else if (p.lanes == 32) e = run_backward<T, V, 16, 32, kWarpThreads, 4>(a, p, blocks, st);
+    else if (p.threads) e = run_backward<T, V, 16, 0, 512, 1>(a, p, blocks, st);
+    else e = launch_rows<k_norm_backward_long<T>>(dim3(blocks), kLongThreads, 0, st, a);
     SK_OP_CUDA(e);
     if (a.partial) {
-        e = launch_kernel(true, k_norm_sum, dim3((uint32_t)((2 * a.cols + 31) / 32)), 256, 0, st, a.partial, blocks, (uint32_t)a.cols,
-                          a.dweight, a.dbias, a.dw_type);
+        e = launch_kernel(true, k_norm_sum, dim3((uint32_t)((2 * a.cols + 7) / 8)), 256, 0, st, a.partial, blocks, (uint32_t)a.cols, a.dweight, a.dbias,
+                          a.dw_type);
         SK_OP_CUDA(e);
     }
     return SK_OK;
 }
-bool aligned16(const void* p, uint64_t ld, uint32_t size) { return (uintptr_t)p % 16 == 0 && ld * size % 16 == 0; }
+
+// The widest access, in elements, that starts and ends every row of a matrix on its boundary
+int widest(const void* p, uint64_t ld, uint64_t cols, uint32_t size) {
+    int v = (int)(16 / size);
+    while (v > 1 && (cols % v || ld % v || (uintptr_t)p % (v * size))) v /= 2;
+    return v;
+}
 
 }  // namespace
 
 int launch_norm(const NormArgs& a, int sm_count, cudaStream_t st) {
     const uint32_t size = type_size(a.type);
-    // 128-bit accesses where every row of x and y starts and ends on a 16-byte boundary, single elements elsewhere
-    const bool vec = a.cols * size % 16 == 0 && aligned16(a.x, a.ld_x, size) && aligned16(a.y, a.ld_y, size);
-    if (a.type == SK_F32) return vec ? norm_typed<float, 4>(a, sm_count, st) : norm_typed<float, 1>(a, sm_count, st);
-    if (a.type == SK_BF16) return vec ? norm_typed<__nv_bfloat16, 8>(a, sm_count, st) : norm_typed<__nv_bfloat16, 1>(a, sm_count, st);
-    return vec ? norm_typed<__half, 8>(a, sm_count, st) : norm_typed<__half, 1>(a, sm_count, st);
+    const int vx = widest(a.x, a.ld_x, a.cols, size), vy = widest(a.y, a.ld_y, a.cols, size), v = vx < vy ? vx : vy;
+    if (a.type == SK_F32) return v == 4 ? norm_typed<float, 4>(a, sm_count, st) : norm_typed<float, 1>(a, sm_count, st);
+    if (a.type == SK_BF16)
+        return v == 8 ? norm_typed<__nv_bfloat16, 8>(a, sm_count, st) : v >= 2 ? norm_typed<__nv_bfloat16, 2>(a, sm_count, st)
+                                                                              : norm_typed<__nv_bfloat16, 1>(a, sm_count, st);
+    return v == 8 ? norm_typed<__half, 8>(a, sm_count, st) : v >= 2 ? norm_typed<__half, 2>(a, sm_count, st) : norm_typed<__half, 1>(a, sm_count, st);
 }
 
 int launch_norm_backward(const NormBackwardArgs& a, int sm_count, cudaStream_t st) {
     const uint32_t size = type_size(a.type);
-    const bool vec = a.cols * size % 16 == 0 && aligned16(a.x, a.ld_x, size) && aligned16(a.dy, a.ld_dy, size) &&
-                     (!a.dx || aligned16(a.dx, a.ld_dx, size));
-    if (a.type == SK_F32) return vec ? norm_backward_typed<float, 4>(a, sm_count, st) : norm_backward_typed<float, 1>(a, sm_count, st);
+    const int vx = widest(a.x, a.ld_x, a.cols, size), vd = widest(a.dy, a.ld_dy, a.cols, size);
+    int v = vx < vd ? vx : vd;
+    if (a.dx) v = min(v, widest(a.dx, a.ld_dx, a.cols, size));
+    if (a.type == SK_F32) return v == 4 ? norm_backward_typed<float, 4>(a, sm_count, st) : norm_backward_typed<float, 1>(a, sm_count, st);
     if (a.type == SK_BF16)
-        return vec ? norm_backward_typed<__nv_bfloat16, 8>(a, sm_count, st) : norm_backward_typed<__nv_bfloat16, 1>(a, sm_count, st);
-    return vec ? norm_backward_typed<__half, 8>(a, sm_count, st) : norm_backward_typed<__half, 1>(a, sm_count, st);
+        return v == 8 ? norm_backward_typed<__nv_bfloat16, 8>(a, sm_count, st) : v >= 2 ? norm_backward_typed<__nv_bfloat16, 2>(a, sm_count, st)
+                                                                                       : norm_backward_typed<__nv_bfloat16, 1>(a, sm_count, st);
+    return v == 8 ? norm_backward_typed<__half, 8>(a, sm_count, st) : v >= 2 ? norm_backward_typed<__half, 2>(a, sm_count, st)
+                                                                            : norm_backward_typed<__half, 1>(a, sm_count, st);
 }
 
 uint64_t norm_backward_workspace(uint64_t rows, uint64_t cols, int sm_count) {

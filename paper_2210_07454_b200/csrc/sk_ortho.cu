@@ -28,14 +28,17 @@ constexpr uint32_t kPadCols = 32;                                // leading dime
 
 // A = X X^T, tiles on and below the diagonal, mirrored
 struct GramEpi {
-    struct Args { __half* out; uint64_t stride; uint32_t ld; };
+    struct Args { __half* out; uint64_t stride; uint32_t ld; const float* factor; };
     const Args& a;
     const GemmShape& g;
     __half* out;
     uint32_t row;
     bool mirror;
+    float scale = kUnscale;
     __device__ GramEpi(const Args& a_, const GemmShape& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t)
-        : a(a_), g(g_), out(a_.out + at.b * a_.stride), row(row_), mirror(at.m != at.n) {}
+        : a(a_), g(g_), out(a_.out + at.b * a_.stride), row(row_), mirror(at.m != at.n) {
+        if (a.factor) scale *= a.factor[at.b] * a.factor[at.b];
+    }
     __device__ void put(uint32_t col, float (&v)[32]) {
         if (row >= g.M) return;
         store_row32(out, SK_F16, (uint64_t)row * a.ld + col, v, 32, true);
@@ -47,7 +50,7 @@ struct GramEpi {
     }
     __device__ void chunk(uint32_t col, float (&v)[32]) {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= kUnscale;
+        for (int i = 0; i < 32; ++i) v[i] *= scale;
         put(col, v);
     }
     __device__ void end() {}
@@ -84,23 +87,25 @@ struct PolyEpi {
 
 // X <- P X: one fp16 matrix, or two whose sum it is; the last step writes the result in the caller's type and layout
 struct ApplyEpi {
-    struct Args { __half *hi, *lo; void* out; uint64_t stride; uint64_t ld; int type; uint32_t vec; };
+    struct Args { __half *hi, *lo; void* out; uint64_t stride; uint64_t ld; int type; uint32_t vec; const float* factor; };
     const Args& a;
     const GemmShape& g;
     uint64_t at0;
     uint32_t row;
+    float scale = kUnscale;
     __device__ ApplyEpi(const Args& a_, const GemmShape& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t)
-        : a(a_), g(g_), at0(at.b * a_.stride + (uint64_t)row_ * a_.ld), row(row_) {}
+        : a(a_), g(g_), at0(at.b * a_.stride + (uint64_t)row_ * a_.ld), row(row_) {
+        if (a.factor) scale *= a.factor[at.b];
+        if (a.out) scale *= kUnscale;
+    }
     __device__ void chunk(uint32_t col, float (&v)[32]) {
         if (row >= g.M) return;
-        if (a.out) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= kUnscale * kUnscale;
+        for (int i = 0; i < 32; ++i) v[i] *= scale;
+        if (a.out) {
             store_row32(a.out, a.type, at0 + col, v, g.N - col, a.vec);
             return;
         }
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= kUnscale;
         store_row32(a.hi, SK_F16, at0 + col, v, 32, true);
         if (a.lo) {
 #pragma unroll
@@ -112,76 +117,151 @@ struct ApplyEpi {
 };
 
 // ---- the normalised matrix ------------------------------------------------------------------------------------------
-constexpr uint32_t kNormBlocks = 64;             // most partial sums of squares per matrix
+constexpr uint32_t kNormBlocks = 1024;           // most partial sums of squares per matrix
+
+// eight neighbouring values of a row (vec: on a 16-byte boundary and all of them there), zero beyond the row's end
+__device__ __forceinline__ void load8(const void* p, int type, uint64_t at, uint32_t valid, bool vec, float (&v)[8]) {
+    if (vec) {
+        if (type == SK_F32) {
+            const float4 a = *(const float4*)((const float*)p + at), b = *(const float4*)((const float*)p + at + 4);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            return;
+        }
+        const uint4 r = *(const uint4*)((const uint16_t*)p + at);
+        const uint32_t q[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = type == SK_BF16 ? __bfloat1622float2(*(const __nv_bfloat162*)&q[i]) : __half22float2(*(const __half2*)&q[i]);
+            v[2 * i] = f.x;
+            v[2 * i + 1] = f.y;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = (uint32_t)i < valid ? load_as(p, type, at + i) : 0.0f;
+}
+
+struct SquareArgs {
+    OrthoArgs a;
+    double* partial;                             // [batch][kNormBlocks]
+    float* factor;                               // [batch]: X = factor * (the matrix that is stored)
+    uint32_t blocks, vec_u, vec_m;
+    __half *hi, *lo;
+    uint32_t ld;
+    uint64_t stride;
+    uint32_t exact;                              // U is the 16-bit update itself: stored exactly, times a power of two
+};
 
 // Sums of squares of U per block, in 64 bits (an update in fp32 may have squares beyond its range); updates the momentum.
-__global__ void __launch_bounds__(256) k_ortho_square(const OrthoArgs a, double* partial) {
-    __shared__ double s[8];
+__global__ void __launch_bounds__(256) k_ortho_square(const __grid_constant__ SquareArgs s) {
+    __shared__ double sums[8];
+    const OrthoArgs& a = s.a;
     chain_acquire();
     const uint32_t b = blockIdx.y, groups = ((uint32_t)a.cols + 7) / 8;
-    const uint64_t total = a.rows * groups;
+    const uint32_t total = (uint32_t)a.rows * groups;
     double sum = 0;
-    for (uint64_t q = (uint64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (uint64_t)gridDim.x * 256) {
-        const uint32_t row = (uint32_t)q / groups, col = ((uint32_t)q - row * groups) * 8;
+#pragma unroll 2
+    for (uint32_t q = blockIdx.x * 256 + threadIdx.x; q < total; q += gridDim.x * 256) {
+        const uint32_t row = q / groups, col = (q - row * groups) * 8, valid = (uint32_t)a.cols - col;
+        float u[8];
+        load8(a.update, a.type, b * a.stride_update + row * a.ld_update + col, valid, s.vec_u, u);
+        if (a.momentum) {
+            float m[8];
+            const uint64_t at = b * a.stride_momentum + row * a.ld_momentum + col;
+            load8(a.momentum, SK_F32, at, valid, s.vec_m, m);
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-            if (col + i >= a.cols) break;
-            float u = load_as(a.update, a.type, b * a.stride_update + row * a.ld_update + col + i);
-            if (a.momentum) {
-                float* m = a.momentum + b * a.stride_momentum + row * a.ld_momentum + col + i;
-                const float next = a.beta * *m + u;
-                *m = next;
-                u = a.nesterov ? u + a.beta * next : next;
+            for (int i = 0; i < 8; ++i) {
+                m[i] = a.beta * m[i] + u[i];
+                u[i] = a.nesterov ? u[i] + a.beta * m[i] : m[i];
             }
-            sum += (double)u * (double)u;
+            if (s.vec_m) {
+                *(float4*)(a.momentum + at) = make_float4(m[0], m[1], m[2], m[3]);
+                *(float4*)(a.momentum + at + 4) = make_float4(m[4], m[5], m[6], m[7]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if ((uint32_t)i < valid) a.momentum[at + i] = m[i];
+            }
         }
+        float part = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) part += u[i] * u[i];
+        if (part > 1e-30f && part < 1e30f) sum += (double)part;       // the eight squares are well inside the 32-bit range
+        else
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += (double)u[i] * (double)u[i];
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = sum;
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = sum;
     __syncthreads();
     if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) sum += s[i];
-        partial[(uint64_t)b * kNormBlocks + blockIdx.x] = sum;
+        for (int i = 1; i < 8; ++i) sum += sums[i];
+        s.partial[(uint64_t)b * kNormBlocks + blockIdx.x] = sum;
     }
 }
 
-__global__ void __launch_bounds__(256) k_ortho_scale(const OrthoArgs a, const double* partial, uint32_t blocks, __half* hi, __half* lo,
-                                                     uint32_t ld, uint64_t stride) {
-    __shared__ float s_factor;
+// The matrix the products start from.  16-bit updates without a momentum are stored exactly, times the power of two next to
+// 2^12 / |U| (their significands fit fp16's); the rest of the normalisation is a factor that the first step's epilogues apply, and the
+// first product needs no second matrix.  Otherwise X itself, as the sum of two fp16 matrices.
+__global__ void __launch_bounds__(256) k_ortho_scale(const __grid_constant__ SquareArgs s) {
+    __shared__ double sums[8];
+    __shared__ float s_scale;
+    const OrthoArgs& a = s.a;
     chain_acquire();
     const uint32_t b = blockIdx.y, groups = ((uint32_t)a.cols + 7) / 8;
+    double sum = 0;
+    for (uint32_t i = threadIdx.x; i < s.blocks; i += 256) sum += s.partial[(uint64_t)b * kNormBlocks + i];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if ((threadIdx.x & 31) == 0) sums[threadIdx.x >> 5] = sum;
+    __syncthreads();
     if (threadIdx.x == 0) {
-        double sum = 0;
-        for (uint32_t i = 0; i < blocks; ++i) sum += partial[(uint64_t)b * kNormBlocks + i];
-        s_factor = (float)(1.0 / (sqrt(sum) + (double)a.eps));
+        for (int i = 1; i < 8; ++i) sum += sums[i];
+        const double scale = (double)kScale / (sqrt(sum) + (double)a.eps);
+        int e = 0;
+        double rest = 1.0;
+        if (s.exact && scale > 1e-30 && scale < 1e30) {
+            rest = frexp(scale, &e) * 2.0;                           // scale = rest * 2^(e-1), rest in [1, 2)
+            s_scale = (float)ldexp(1.0, e - 1);
+        } else {
+            s_scale = (float)scale;
+        }
+        if (blockIdx.x == 0) s.factor[b] = (float)rest;
     }
     __syncthreads();
-    const float factor = s_factor;
-    const uint64_t total = a.rows * groups;
-    for (uint64_t q = (uint64_t)blockIdx.x * 256 + threadIdx.x; q < total; q += (uint64_t)gridDim.x * 256) {
-        const uint32_t row = (uint32_t)q / groups, col = ((uint32_t)q - row * groups) * 8;
+    const float scale = s_scale;
+    const uint32_t total = (uint32_t)a.rows * groups;
+#pragma unroll 2
+    for (uint32_t q = blockIdx.x * 256 + threadIdx.x; q < total; q += gridDim.x * 256) {
+        const uint32_t row = q / groups, col = (q - row * groups) * 8, valid = (uint32_t)a.cols - col;
+        float u[8];
+        load8(a.update, a.type, b * a.stride_update + row * a.ld_update + col, valid, s.vec_u, u);
+        if (a.momentum) {
+            float m[8];
+            load8(a.momentum, SK_F32, b * a.stride_momentum + row * a.ld_momentum + col, valid, s.vec_m, m);
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) {
-            if (col + i >= a.cols) break;
-            float u = load_as(a.update, a.type, b * a.stride_update + row * a.ld_update + col + i);
-            if (a.momentum) {
-                const float m = a.momentum[b * a.stride_momentum + row * a.ld_momentum + col + i];
-                u = a.nesterov ? u + a.beta * m : m;
-            }
-            const float x = u * factor * kScale;
-            const __half h = __float2half_rn(x);
-            const uint64_t at = b * stride + (uint64_t)row * ld + col + i;
-            hi[at] = h;
-            if (lo) lo[at] = __float2half_rn(x - __half2float(h));
+            for (int i = 0; i < 8; ++i) u[i] = a.nesterov ? u[i] + a.beta * m[i] : m[i];
         }
+        uint32_t h[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float x = u[2 * i] * scale, y = u[2 * i + 1] * scale;
+            const __half2 p = __floats2half2_rn(x, y);
+            const float2 f = __half22float2(p);
+            h[i] = *(const uint32_t*)&p;
+            l[i] = pack16(x - f.x, y - f.y, false);
+        }
+        const uint64_t at = b * s.stride + (uint64_t)row * s.ld + col;   // ld is a multiple of 32: whole groups fit
+        *(uint4*)(s.hi + at) = make_uint4(h[0], h[1], h[2], h[3]);
+        if (s.lo) *(uint4*)(s.lo + at) = make_uint4(l[0], l[1], l[2], l[3]);
     }
 }
 
 struct OrthoLayout {
     uint32_t ld_x, ld_a, m;
     uint64_t x_elems, a_elems;                   // per matrix
-    uint64_t off_partial, off_x[2], off_lo, off_a, off_p, total;
+    uint64_t off_partial, off_factor, off_x[2], off_lo, off_a, off_p, total;
 };
 OrthoLayout layout_of(const OrthoArgs& a) {
     OrthoLayout l;
@@ -193,6 +273,7 @@ OrthoLayout layout_of(const OrthoArgs& a) {
     uint64_t at = 0;
     auto take = [&](uint64_t bytes) { const uint64_t r = at; at += round_up(bytes, 256); return r; };
     l.off_partial = take(a.batch * kNormBlocks * 8);
+    l.off_factor = take(a.batch * 4);
     l.off_x[0] = take(a.batch * l.x_elems * 2);
     l.off_x[1] = take(a.batch * l.x_elems * 2);
     l.off_lo = take(2 * round_up(a.batch * l.x_elems * 2, 256));
@@ -216,16 +297,25 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     __half* poly = (__half*)(ws + l.off_p);
     const bool tall = a.rows > a.cols;
     const uint32_t batch = (uint32_t)a.batch, m = l.m;
-    // two 16-bit matrices for X in all but the last two steps
-    auto split = [&](int step) { return step < a.steps - 2; };
+    // two 16-bit matrices for X in all but the last two steps, and one where that is exact
+    const bool exact = a.type != SK_F32 && !a.momentum;
+    auto split = [&](int step) { return step < a.steps - 2 && !(step == 0 && exact); };
 
-    const uint64_t groups = a.rows * ((a.cols + 7) / 8);
-    uint32_t blocks = (uint32_t)((groups + 255) / 256);
-    uint32_t few = blocks < kNormBlocks ? blocks : kNormBlocks;
-    SK_OP_CUDA(launch_kernel(true, k_ortho_square, dim3(few, batch), 256, 0, st, a, partial));
-    const uint32_t most = (uint32_t)dev.sm_count * 8;
-    SK_OP_CUDA(launch_kernel(true, k_ortho_scale, dim3(blocks < most ? blocks : most, batch), 256, 0, st, a, partial, few, x[0],
-                             split(0) ? lo[0] : nullptr, l.ld_x, l.x_elems));
+    const uint32_t blocks = (uint32_t)((a.rows * ((a.cols + 7) / 8) + 255) / 256);
+    const uint32_t most = (uint32_t)(round_up((uint64_t)dev.sm_count * 8, batch) / batch), limit = most < kNormBlocks ? most : kNormBlocks;
+    SquareArgs sq{a, partial, (float*)(ws + l.off_factor), blocks < limit ? blocks : limit};
+    auto vec8 = [&](const void* p, uint64_t ld, uint64_t stride, uint32_t size) {
+        return a.cols % 8 == 0 && (uintptr_t)p % 16 == 0 && ld * size % 16 == 0 && (batch == 1 || stride * size % 16 == 0);
+    };
+    sq.vec_u = vec8(a.update, a.ld_update, a.stride_update, type_size(a.type));
+    sq.vec_m = a.momentum && vec8(a.momentum, a.ld_momentum, a.stride_momentum, 4);
+    sq.hi = x[0];
+    sq.lo = split(0) ? lo[0] : nullptr;
+    sq.ld = l.ld_x;
+    sq.stride = l.x_elems;
+    sq.exact = exact;
+    SK_OP_CUDA(launch_kernel(true, k_ortho_square, dim3(sq.blocks, batch), 256, 0, st, sq));
+    SK_OP_CUDA(launch_kernel(true, k_ortho_scale, dim3(sq.blocks, batch), 256, 0, st, sq));
 
     GemmShape square{};
     square.M = square.N = m;
@@ -241,10 +331,11 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     for (int s = 0; s < a.steps; ++s) {
         const int from = s & 1, to = from ^ 1;
         const Operand ox{x[from], a.rows, a.cols, l.ld_x, l.x_elems, batch, tall};
-        SK_OP_CUDA(launch_product<GramEpi>(true, ox, ox, nullptr, nullptr, square, {gram, l.a_elems, l.ld_a}, dev.sm_count, st));
-        PolyEpi::Args pa{{poly, l.a_elems, l.ld_a}, gram, a.coefficient[0], a.coefficient[1], a.coefficient[2]};
+        SK_OP_CUDA(launch_product<GramEpi>(true, ox, ox, nullptr, nullptr, square, {gram, l.a_elems, l.ld_a, s == 0 ? sq.factor : nullptr}, dev.sm_count, st));
+        PolyEpi::Args pa{{poly, l.a_elems, l.ld_a, nullptr}, gram, a.coefficient[0], a.coefficient[1], a.coefficient[2]};
         SK_OP_CUDA(launch_product<PolyEpi>(true, oa, oa, nullptr, nullptr, square, pa, dev.sm_count, st));
         ApplyEpi::Args ea{};
+        ea.factor = s == 0 ? sq.factor : nullptr;
         if (s + 1 < a.steps) {
             ea.hi = x[to];
             ea.lo = split(s + 1) ? lo[to] : nullptr;
