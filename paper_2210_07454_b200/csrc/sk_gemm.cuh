@@ -31,18 +31,30 @@ constexpr uint32_t kOpWait = 1u;              // status word of the operators: a
 constexpr int kGemmK = 64;                    // values of k per stage: 128 bytes, the width of the swizzle
 constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
+constexpr int kStageRow = 20;                 // words from one row of a warp's 32 x 32 sixteen-bit values to the next: whole, odd 16-byte steps
+constexpr int kStageWords = 32 * kStageRow;   // of shared memory for each epilogue warp
 
-struct GemmShape {
+// One product of a launch.
+struct GemmGroup {
     uint32_t M, N;                            // output extents
-    uint32_t k_blocks;                        // stages per pass (the last one zero-filled beyond K)
+    uint32_t k_blocks;                        // stages per tile and pass (the last one zero-filled beyond K)
+    uint32_t k_total;                         // stages along K: more than k_blocks where K is split
     uint32_t passes;                          // 1 or 2
-    uint32_t batch;
+    uint32_t batch;                           // matrices, or slices of K
+    uint32_t sliced;                          // 1: `batch` counts slices of K of one matrix
     uint32_t tiles_m, tiles_n;
-    uint32_t group_m;                         // tiles are walked in bands of this many tile rows, row index fastest
+    uint32_t band;                            // tiles are walked in bands of this many tile rows, row index fastest
     uint32_t symmetric;                       // 1: only tiles on and below the diagonal; the epilogue mirrors them
     uint32_t tiles;                           // total over the batch
     uint32_t a_mn, b_mn;                      // 1: MN-major
     uint32_t bf16;                            // operand type: 1 bf16, 0 fp16
+};
+// A launch: one product, or two that do not depend on each other (the second with map_a2, map_b2 as its operands), the one with
+// the longer tiles first.  Each of the `units` (blocks or pairs) takes the first's tiles in turn; `early` is how many rounds of
+// the second's tiles the units that got one tile less of the first are ahead.
+struct GemmShape {
+    GemmGroup g[2];
+    uint32_t groups, early;
     uint32_t* status;
 };
 
@@ -160,9 +172,10 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn) {
 }
 
 // ---- which tile ------------------------------------------------------------------------------------------------------
-struct TileAt { uint32_t b, m, n; };
-__device__ __forceinline__ TileAt tile_at(const GemmShape& g, uint32_t t) {
+struct TileAt { uint32_t group, b, m, n; };
+__device__ __forceinline__ TileAt tile_at(const GemmGroup& g, uint32_t group, uint32_t t) {
     TileAt r;
+    r.group = group;
     if (g.symmetric) {
         const uint32_t per = g.tiles_m * (g.tiles_m + 1) / 2;
         r.b = t / per;
@@ -177,29 +190,49 @@ __device__ __forceinline__ TileAt tile_at(const GemmShape& g, uint32_t t) {
     const uint32_t per = g.tiles_m * g.tiles_n;
     r.b = t / per;
     uint32_t q = t - r.b * per;
-    const uint32_t band = q / (g.group_m * g.tiles_n);
-    q -= band * g.group_m * g.tiles_n;
-    const uint32_t rows = min(g.group_m, g.tiles_m - band * g.group_m);
+    const uint32_t band = q / (g.band * g.tiles_n);
+    q -= band * g.band * g.tiles_n;
+    const uint32_t rows = min(g.band, g.tiles_m - band * g.band);
     r.n = q / rows;
-    r.m = band * g.group_m + (q - r.n * rows);
+    r.m = band * g.band + (q - r.n * rows);
     return r;
+}
+// The i-th tile of unit p of `units`; false when it has no more.
+__device__ __forceinline__ bool tile_of(const GemmShape& s, uint32_t p, uint32_t units, uint32_t i, TileAt& at) {
+    uint32_t t = p + i * units;
+    if (t < s.g[0].tiles) {
+        at = tile_at(s.g[0], 0, t);
+        return true;
+    }
+    if (s.groups < 2) return false;
+    const uint32_t q = s.g[0].tiles / units, r = s.g[0].tiles - q * units;       // units below r had q + 1 tiles, the others q
+    const uint32_t j = i - (q + (p < r));
+    const uint32_t head = s.early * (units - r);
+    if (p >= r) t = j < s.early ? j * (units - r) + (p - r) : head + (j - s.early) * units + p;
+    else t = head + j * units + p;
+    if (t >= s.g[1].tiles) return false;
+    at = tile_at(s.g[1], 1, t);
+    return true;
+}
+__device__ __forceinline__ uint32_t stages_of(const GemmGroup& g, const TileAt& at) {
+    return g.sliced ? min(g.k_blocks, g.k_total - at.b * g.k_blocks) : g.k_blocks * g.passes;
 }
 
 template <int CG, int BN>
 struct GemmTile {
     static constexpr int kStageBytes = 128 * 128 + (BN / CG) * 128;      // both operands, 64 values of k
     static constexpr int kStages = BN / CG >= 128 ? 6 : 8;               // as many as fit
-    static constexpr int kSmem = kStages * kStageBytes + 1024;           // + alignment of the swizzle
+    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStageWords * 4 + 1024;      // + the epilogue's, + alignment
 };
 
-// Epi: struct Args; __device__ Epi(const Args&, batch, row, tile column); chunk(col, v[32]); end().  A thread holds one row of
-// the tile and gets its columns 32 at a time; the two warps that share a row take half the columns each.
-// Rows >= M are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
+// Epi: struct Args; __device__ Epi(const Args&, group, tile, row, first column, half, the warp's shared memory);
+// chunk(col, v[32]); end().  A thread holds one row of the tile and gets its columns 32 at a time; the two warps that share a row take half
+// the columns each.  Rows >= M are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
 template <int CG, int BN, class Epi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
 k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
        const __grid_constant__ CUtensorMap map_a2, const __grid_constant__ CUtensorMap map_b2,
-       const __grid_constant__ GemmShape g, const __grid_constant__ typename Epi::Args ea) {
+       const __grid_constant__ GemmShape shape, const __grid_constant__ typename Epi::Args ea) {
     constexpr int kStages = GemmTile<CG, BN>::kStages;
     constexpr int kRowsB = BN / CG;
     constexpr int kBytesA = 128 * 128, kBytesB = kRowsB * 128;
@@ -231,39 +264,41 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
 
     chain_acquire();
 
-    const uint32_t first = blockIdx.x / CG, step = gridDim.x / CG;
-    const uint32_t kb = g.k_blocks * g.passes;
+    const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG;
+    TileAt at;
 
     if (warp == 0) {
         if (lane == 0) {
             uint32_t it = 0;
             bool ok = true;
-            for (uint32_t t = first; t < g.tiles && ok; t += step) {
-                const TileAt at = tile_at(g, t);
+            for (uint32_t i = 0; ok && tile_of(shape, unit, units, i, at); ++i) {
+                const GemmGroup& g = shape.g[at.group];
+                const uint32_t kb = stages_of(g, at), k_first = g.sliced ? at.b * g.k_blocks : 0;
+                const int z = g.sliced ? 0 : (int)at.b;
                 const int row_a = (int)(at.m * (128 * CG) + rank * 128);
                 const int row_b = (int)(at.n * BN + rank * kRowsB);
                 for (uint32_t k = 0; k < kb; ++k, ++it) {
                     const uint32_t s = it % kStages;
-                    if (it >= (uint32_t)kStages && !(ok = mbar_wait(empty(s), ((it / kStages) - 1) & 1, g.status))) break;
-                    const bool second = k >= g.k_blocks;
+                    if (it >= (uint32_t)kStages && !(ok = mbar_wait(empty(s), ((it / kStages) - 1) & 1, shape.status))) break;
+                    const bool pass2 = k >= g.k_blocks, second = pass2 || at.group;
                     const CUtensorMap* ma = second ? &map_a2 : &map_a;
                     const CUtensorMap* mb = second ? &map_b2 : &map_b;
-                    const int k0 = (int)((second ? k - g.k_blocks : k) * kGemmK);
+                    const int k0 = (int)((k_first + (pass2 ? k - g.k_blocks : k)) * kGemmK);
                     const uint32_t sa = stages + s * (kBytesA + kBytesB), sb = sa + kBytesA;
                     uint32_t bar = full(s);
                     if (rank == 0) mbar_expect(bar, CG * (kBytesA + kBytesB));
                     if constexpr (CG == 2) bar = map_to_leader(bar);
                     if (g.a_mn) {
-                        tma_load<CG>(sa, ma, bar, row_a, k0, (int)at.b);
-                        tma_load<CG>(sa + 8192, ma, bar, row_a + 64, k0, (int)at.b);
+                        tma_load<CG>(sa, ma, bar, row_a, k0, z);
+                        tma_load<CG>(sa + 8192, ma, bar, row_a + 64, k0, z);
                     } else {
-                        tma_load<CG>(sa, ma, bar, k0, row_a, (int)at.b);
+                        tma_load<CG>(sa, ma, bar, k0, row_a, z);
                     }
                     if (g.b_mn) {
 #pragma unroll
-                        for (int q = 0; q < kRowsB / 64; ++q) tma_load<CG>(sb + q * 8192, mb, bar, row_b + q * 64, k0, (int)at.b);
+                        for (int q = 0; q < kRowsB / 64; ++q) tma_load<CG>(sb + q * 8192, mb, bar, row_b + q * 64, k0, z);
                     } else {
-                        tma_load<CG>(sb, mb, bar, k0, row_b, (int)at.b);
+                        tma_load<CG>(sb, mb, bar, k0, row_b, z);
                     }
                 }
             }
@@ -271,24 +306,25 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
             if (it) {
                 const uint32_t from = it > (uint32_t)kStages ? it - kStages : 0;
                 for (uint32_t q = from; q < it; ++q)
-                    if (!mbar_wait(empty(q % kStages), (q / kStages) & 1, g.status)) break;
+                    if (!mbar_wait(empty(q % kStages), (q / kStages) & 1, shape.status)) break;
             }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            // D fp32; A, B bf16 or fp16; majors; N / 8; M / 16
-            const uint32_t idesc = (1u << 4) | (g.bf16 << 7) | (g.bf16 << 10) | (g.a_mn << 15) | (g.b_mn << 16) |
-                                   ((uint32_t)(BN / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
-            const uint64_t step_a = (g.a_mn ? 2048u : 32u) >> 4, step_b = (g.b_mn ? 2048u : 32u) >> 4;
-            uint32_t it = 0, n = 0;
+            uint32_t it = 0;
             bool ok = true;
-            for (uint32_t t = first; t < g.tiles && ok; t += step, ++n) {
-                const uint32_t a = n & 1;
-                if (n >= 2 && !(ok = mbar_wait(acc_empty(a), ((n >> 1) - 1) & 1, g.status))) break;
+            for (uint32_t n = 0; ok && tile_of(shape, unit, units, n, at); ++n) {
+                const GemmGroup& g = shape.g[at.group];
+                const uint32_t kb = stages_of(g, at), a = n & 1;
+                // D fp32; A, B bf16 or fp16; majors; N / 8; M / 16
+                const uint32_t idesc = (1u << 4) | (g.bf16 << 7) | (g.bf16 << 10) | (g.a_mn << 15) | (g.b_mn << 16) |
+                                       ((uint32_t)(BN / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
+                const uint64_t step_a = (g.a_mn ? 2048u : 32u) >> 4, step_b = (g.b_mn ? 2048u : 32u) >> 4;
+                if (n >= 2 && !(ok = mbar_wait(acc_empty(a), ((n >> 1) - 1) & 1, shape.status))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 for (uint32_t k = 0; k < kb; ++k, ++it) {
                     const uint32_t s = it % kStages;
-                    if (!(ok = mbar_wait(full(s), (it / kStages) & 1, g.status))) break;
+                    if (!(ok = mbar_wait(full(s), (it / kStages) & 1, shape.status))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint32_t sa = stages + s * (kBytesA + kBytesB);
                     const uint64_t da = smem_desc(sa, g.a_mn), db = smem_desc(sa + kBytesA, g.b_mn);
@@ -302,15 +338,15 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
         }
     } else {
         const uint32_t w = warp - 2, quarter = warp & 3, half = w >> 2;
-        uint32_t n = 0;
-        for (uint32_t t = first; t < g.tiles; t += step, ++n) {
-            const TileAt at = tile_at(g, t);
+        uint32_t* stage = (uint32_t*)(smem_raw + (stages - smem_u32(smem_raw)) + kStages * (kBytesA + kBytesB)) + w * kStageWords;
+        for (uint32_t n = 0; tile_of(shape, unit, units, n, at); ++n) {
+            const GemmGroup& g = shape.g[at.group];
             const uint32_t a = n & 1;
-            if (!mbar_wait(acc_full(a), (n >> 1) & 1, g.status)) break;
+            if (!mbar_wait(acc_full(a), (n >> 1) & 1, shape.status)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             const uint32_t row = at.m * (128 * CG) + rank * 128 + quarter * 32 + lane;
             const uint32_t col0 = at.n * BN + half * (BN / 2);
-            Epi epi(ea, g, at, row, col0, half);
+            Epi epi(ea, g, at, row, col0, half, stage);
 #pragma unroll 1
             for (uint32_t c = 0; c < BN / 2; c += 32) {
                 float v[32];
@@ -348,22 +384,33 @@ struct Operand {
 
 bool encode_operand(CUtensorMap* map, const Operand& o, bool bf16, uint32_t box_rows);
 
-template <int CG, int BN, class Epi>
-cudaError_t launch_gemm(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, GemmShape g,
-                        const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
+// The tile-dependent part of a group.  slices > 1 splits K.
+template <int CG, int BN>
+void set_tiles(GemmGroup& g, const Operand& a, const Operand& b, uint32_t slices) {
     g.a_mn = a.mn;
     g.b_mn = b.mn;
-    const uint64_t K = a.mn ? a.rows : a.cols;
-    g.k_blocks = (uint32_t)((K + kGemmK - 1) / kGemmK);
-    g.passes = a2 ? 2 : 1;
+    g.k_total = (uint32_t)(((a.mn ? a.rows : a.cols) + kGemmK - 1) / kGemmK);
+    g.k_blocks = g.k_total;
+    if (slices > 1) {
+        g.k_blocks = (g.k_total + slices - 1) / slices;
+        g.batch = (g.k_total + g.k_blocks - 1) / g.k_blocks;          // no empty slice, and never more than asked for
+        g.sliced = 1;
+    }
     g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
     g.tiles_n = (g.N + BN - 1) / BN;
     g.tiles = g.batch * (g.symmetric ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n);
-    g.group_m = g.tiles_m < 16 ? g.tiles_m : 16;
-    if (!g.tiles) return cudaSuccess;
+    g.band = g.tiles_m < 16 ? g.tiles_m : 16;
+}
+
+// a2, b2: the second pass's operands, or with groups = 2 the second product's.
+template <int CG, int BN, class Epi>
+cudaError_t launch_gemm(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, const GemmShape& g,
+                        const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
+    const uint32_t tiles = g.g[0].tiles + (g.groups == 2 ? g.g[1].tiles : 0);
+    if (!tiles) return cudaSuccess;
     CUtensorMap ma, mb, ma2, mb2;
-    bool ok = encode_operand(&ma, a, g.bf16, 128) && encode_operand(&mb, b, g.bf16, BN / CG);
-    if (a2) ok = ok && encode_operand(&ma2, *a2, g.bf16, 128) && encode_operand(&mb2, *b2, g.bf16, BN / CG);
+    bool ok = encode_operand(&ma, a, g.g[0].bf16, 128) && encode_operand(&mb, b, g.g[0].bf16, BN / CG);
+    if (a2) ok = ok && encode_operand(&ma2, *a2, g.g[0].bf16, 128) && encode_operand(&mb2, *b2, g.g[0].bf16, BN / CG);
     else { ma2 = ma; mb2 = mb; }
     if (!ok) return cudaErrorInvalidValue;
     auto kernel = k_gemm<CG, BN, Epi>;
@@ -378,7 +425,7 @@ cudaError_t launch_gemm(bool chain, const Operand& a, const Operand& b, const Op
     }
     const uint32_t slots = (uint32_t)sm_count / CG;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((g.tiles < slots ? g.tiles : slots) * CG);
+    cfg.gridDim = dim3((tiles < slots ? tiles : slots) * CG);
     cfg.blockDim = dim3(kGemmThreads);
     cfg.dynamicSmemBytes = GemmTile<CG, BN>::kSmem;
     cfg.stream = st;
@@ -400,6 +447,9 @@ cudaError_t launch_gemm(bool chain, const Operand& a, const Operand& b, const Op
     return cudaLaunchKernelEx(&cfg, kernel, ma, mb, ma2, mb2, g, ea);
 }
 
+// What a tile costs beside its stages, in stages (its epilogue where nothing hides it)
+constexpr uint32_t kTileCost = 6;
+
 // Which tile: pairs of blocks on 256 x 256, or single blocks on 128 x 128.  A large tile reads each operand half as often and is
 // what keeps the tensor cores fed (512 cycles of products against 64 KB of operands per stage, both at a pair); small
 // ones spread a small product over more SMs.  The one whose last wave ends first wins.
@@ -413,11 +463,40 @@ inline bool wide_tiles(uint32_t M, uint32_t N, uint32_t batch, bool symmetric, i
     return wide <= small;
 }
 
+// One product; a2, b2: the operands of a second pass into the same sums; slices: K is split into so many.
+template <int CG, int BN, class Epi>
+cudaError_t launch_one(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, GemmGroup g, uint32_t slices,
+                       uint32_t* status, const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
+    GemmShape s{};
+    g.passes = a2 ? 2 : 1;
+    set_tiles<CG, BN>(g, a, b, slices);
+    s.g[0] = g;
+    s.groups = 1;
+    s.status = status;
+    return launch_gemm<CG, BN, Epi>(chain, a, b, a2, b2, s, ea, sm_count, st);
+}
 template <class Epi>
-cudaError_t launch_product(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, const GemmShape& g,
+cudaError_t launch_product(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, const GemmGroup& g, uint32_t* status,
                            const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
-    if (wide_tiles(g.M, g.N, g.batch, g.symmetric, sm_count)) return launch_gemm<2, 256, Epi>(chain, a, b, a2, b2, g, ea, sm_count, st);
-    return launch_gemm<1, 128, Epi>(chain, a, b, a2, b2, g, ea, sm_count, st);
+    if (wide_tiles(g.M, g.N, g.batch, g.symmetric, sm_count)) return launch_one<2, 256, Epi>(chain, a, b, a2, b2, g, 1, status, ea, sm_count, st);
+    return launch_one<1, 128, Epi>(chain, a, b, a2, b2, g, 1, status, ea, sm_count, st);
+}
+
+// Two products in one launch, the longer tiles first; slices: K of the first is split into so many.
+template <int CG, int BN, class Epi>
+cudaError_t launch_two(bool chain, const Operand& a, const Operand& b, GemmGroup g0, uint32_t slices, const Operand& a2, const Operand& b2, GemmGroup g1,
+                       uint32_t* status, const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
+    GemmShape s{};
+    g0.passes = g1.passes = 1;
+    set_tiles<CG, BN>(g0, a, b, slices);
+    set_tiles<CG, BN>(g1, a2, b2, 1);
+    s.g[0] = g0;
+    s.g[1] = g1;
+    s.groups = 2;
+    s.status = status;
+    const uint32_t c0 = g0.k_blocks + kTileCost, c1 = g1.k_blocks + kTileCost;
+    s.early = (c0 + c1 / 2) / c1;
+    return launch_gemm<CG, BN, Epi>(chain, a, b, &a2, &b2, s, ea, sm_count, st);
 }
 
 }  // namespace sk

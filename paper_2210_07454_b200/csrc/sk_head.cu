@@ -28,11 +28,11 @@ __device__ __forceinline__ float exp2_fast(float x) {          // 2^x, 2 ulp
 struct StatsEpi {
     struct Args { float2* part; float* at_target; const int64_t* targets; };
     const Args& a;
-    const GemmShape& g;
+    const GemmGroup& g;
     uint32_t row, slot;
     int64_t target;
     float top = -INFINITY, sum = 0;
-    __device__ StatsEpi(const Args& a_, const GemmShape& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t half)
+    __device__ StatsEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t half, uint32_t*)
         : a(a_), g(g_), row(row_), slot(at.n * 2 + half) { target = row < g.M ? a.targets[row] : -1; }
     __device__ void chunk(uint32_t col, float (&v)[32]) {
         const uint32_t valid = g.N - col;
@@ -112,11 +112,14 @@ __global__ void __launch_bounds__(kJoinThreads) k_head_join(const float2* part, 
 struct GradEpi {
     struct Args { uint16_t* out; uint64_t ld; const float *lse, *dloss, *factor; const int64_t* targets; uint64_t vocab; uint32_t first; };
     const Args& a;
-    const GemmShape& g;
-    uint32_t row;
+    const GemmGroup& g;
+    uint32_t row0, rows;
+    uint32_t* stage;
     float off = 0, scale = 0;
     int64_t target = -1;
-    __device__ GradEpi(const Args& a_, const GemmShape& g_, const TileAt&, uint32_t row_, uint32_t, uint32_t) : a(a_), g(g_), row(row_) {
+    __device__ GradEpi(const Args& a_, const GemmGroup& g_, const TileAt&, uint32_t row, uint32_t, uint32_t, uint32_t* stage_)
+        : a(a_), g(g_), row0(row - (threadIdx.x & 31)), stage(stage_) {
+        rows = row0 >= g.M ? 0 : g.M - row0 < 32 ? g.M - row0 : 32;
         if (row < g.M) {
             const int64_t t = a.targets[row];
             if (t >= 0 && t < (int64_t)a.vocab) {
@@ -127,7 +130,7 @@ struct GradEpi {
         }
     }
     __device__ void chunk(uint32_t col, float (&v)[32]) {
-        if (row >= g.M) return;
+        if (!rows) return;
         const uint64_t d = (uint64_t)(target - (int64_t)col);
         if (scale != 0.0f) {
 #pragma unroll
@@ -142,24 +145,39 @@ struct GradEpi {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0.0f;
         }
-        store_row32(a.out, g.bf16 ? SK_BF16 : SK_F16, (uint64_t)row * a.ld + col, v, 32, true);
+        __syncwarp();
+        store_block32(a.out, g.bf16 ? SK_BF16 : SK_F16, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
     }
     __device__ void end() {}
 };
 
-// a share of dhidden (`sum` carries it from piece to piece), or rows of dW
+// One of two products, by the group: rows of dW, or a share of dhidden.  Shares of more than one piece or slice are added up in 32
+// bits, a slice of K in a matrix of its own (`sum`, one after the other), and joined by k_head_sum.
 struct OutEpi {
-    struct Args { void* out; float* sum; uint64_t ld, ld_sum; const float* factor; int type; uint32_t vec, first, last; };
-    const Args& a;
-    const GemmShape& g;
-    uint32_t row;
+    struct One { void* out; float* sum; uint64_t ld, sum_stride; int type; uint32_t align, add; };
+    struct Args { One o[2]; const float* factor; };
+    const One& a;
+    const GemmGroup& g;
+    float* sum;
+    uint32_t row0, rows;
+    uint32_t* stage;
     float scale;
-    __device__ OutEpi(const Args& a_, const GemmShape& g_, const TileAt&, uint32_t row_, uint32_t, uint32_t)
-        : a(a_), g(g_), row(row_), scale(a_.factor ? 1.0f / *a_.factor : 1.0f) {}
+    __device__ OutEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row, uint32_t, uint32_t, uint32_t* stage_)
+        : a(a_.o[at.group]), g(g_), sum(a.sum ? a.sum + at.b * a.sum_stride : nullptr), row0(row - (threadIdx.x & 31)), stage(stage_),
+          scale(a_.factor ? 1.0f / *a_.factor : 1.0f) {
+        rows = row0 >= g.M ? 0 : g.M - row0 < 32 ? g.M - row0 : 32;
+    }
     __device__ void chunk(uint32_t col, float (&v)[32]) {
-        if (row >= g.M) return;
-        if (!a.first) {
-            const float* s = a.sum + (uint64_t)row * a.ld_sum + col;
+        if (!rows) return;
+        if (!sum) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= scale;
+            store_block32(a.out, a.type, a.ld, row0, rows, col, g.N - col, v, a.align, stage, kStageRow);
+            return;
+        }
+        const uint32_t lane = threadIdx.x & 31;
+        if (a.add && lane < rows) {
+            const float* s = sum + (uint64_t)(row0 + lane) * a.ld + col;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 uint32_t r[8];
@@ -168,16 +186,33 @@ struct OutEpi {
                 for (int i = 0; i < 8; ++i) v[8 * q + i] += __uint_as_float(r[i]);
             }
         }
-        if (!a.last) {
-            store_row32(a.sum, SK_F32, (uint64_t)row * a.ld_sum + col, v, 32, true);
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= scale;
-        store_row32(a.out, a.type, (uint64_t)row * a.ld + col, v, g.N - col, a.vec);
+        store_block32(sum, SK_F32, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
     }
     __device__ void end() {}
 };
+
+// dhidden from its shares, slices in order
+__global__ void __launch_bounds__(256) k_head_sum(const float* sum, uint32_t slices, uint64_t stride, uint64_t ld_sum, uint64_t rows, uint32_t cols,
+                                                  const float* factor, void* out, uint64_t ld, int type) {
+    chain_acquire();
+    const float scale = factor ? 1.0f / *factor : 1.0f;
+    const uint32_t groups = (cols + 3) / 4;
+    const uint64_t total = rows * groups;
+    for (uint64_t q = blockIdx.x * 256ull + threadIdx.x; q < total; q += gridDim.x * 256ull) {
+        const uint64_t row = q / groups;
+        const uint32_t col = (uint32_t)(q - row * groups) * 4;
+        const float* p = sum + row * ld_sum + col;               // ld_sum is a multiple of 32
+        float4 v = *(const float4*)p;
+        for (uint32_t s = 1; s < slices; ++s) {
+            const float4 w = *(const float4*)(p + s * stride);
+            v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+        }
+        const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
+#pragma unroll
+        for (uint32_t i = 0; i < 4; ++i)
+            if (col + i < cols) store_as(out, type, row * ld + col + i, f[i]);
+    }
+}
 
 // fp16 only: a power of two that brings the largest |dloss| to about 2^14, so that small probabilities stay above fp16's
 // smallest values; the products divide by it again
@@ -222,10 +257,30 @@ bool addressable(const void* p, uint64_t ld) { return (uintptr_t)p % 16 == 0 && 
 
 struct HeadLayout {
     bool pack_h, pack_w;
-    uint64_t ld_pack, off_h, off_w, off_part, off_target, off_factor, off_g, ld_g, off_sum, ld_sum, piece, total;
+    uint64_t ld_pack, off_h, off_w, off_part, off_target, off_factor, off_g, ld_g, off_sum, ld_sum, sum_stride, piece, total;
+    uint32_t slices;                             // of the vocabulary's pieces in the product that gives dhidden
+    bool wide;                                   // tiles of the two gradient products
 };
 // columns of the vocabulary per piece: G's piece is to stay below this size
 constexpr uint64_t kPieceBytes = 512ull << 20;
+
+// The product that gives dhidden has few tiles and a long K (a piece of the vocabulary), the one that gives dW many short ones; they run
+// in one launch.  K is split where one tile of the first would last longer than about half of an even share of all the work.
+// (n: columns of a whole piece.)
+constexpr uint32_t kPlanSms = 148;               // the plan, and with it the workspace, is made for a B200
+uint32_t slices_of(uint64_t tokens, uint64_t n, uint64_t width, bool wide) {
+    if (n < tokens) return 1;
+    const uint64_t tile = wide ? 256 : 128, units = kPlanSms / (wide ? 2 : 1);
+    const uint64_t rows = (tokens + tile - 1) / tile, cols = (width + tile - 1) / tile, vocab = (n + tile - 1) / tile;
+    const uint64_t k0 = (n + kGemmK - 1) / kGemmK, k1 = (tokens + kGemmK - 1) / kGemmK;
+    const uint64_t work = rows * cols * (k0 + kTileCost) + vocab * cols * (k1 + kTileCost);
+    uint64_t s = 2 * k0 * units / work;
+    if (s > k0 / 8) s = k0 / 8;                  // a slice is worth its epilogue
+    if (s > 32) s = 32;
+    if (s < 2) return 1;
+    const uint64_t each = (k0 + s - 1) / s;
+    return (uint32_t)((k0 + each - 1) / each);   // as many as the first piece really has: every one is written there
+}
 
 HeadLayout layout_of(const HeadArgs& a, bool backward) {
     HeadLayout l{};
@@ -246,7 +301,10 @@ HeadLayout layout_of(const HeadArgs& a, bool backward) {
         l.ld_g = l.piece < round_up(a.vocab, 32) ? l.piece : round_up(a.vocab, 32);
         l.off_g = take(a.tokens * l.ld_g * 2);
         l.ld_sum = round_up(a.width, 32);
-        if (l.piece < a.vocab && a.dhidden) l.off_sum = take(a.tokens * l.ld_sum * 4);
+        l.sum_stride = a.tokens * l.ld_sum;
+        l.wide = a.tokens > 128;
+        l.slices = slices_of(a.tokens, l.piece < a.vocab ? l.piece : a.vocab, a.width, l.wide);
+        if (a.dhidden && (l.piece < a.vocab || l.slices > 1)) l.off_sum = take(l.slices * l.sum_stride * 4);
     }
     l.total = at;
     return l;
@@ -286,17 +344,16 @@ int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
     uint64_t ld_h, ld_w;
     int rc = pack_operands(a, false, l, dev, &h, &w, &ld_h, &ld_w, st);
     if (rc) return rc;
-    GemmShape g{};
+    GemmGroup g{};
     g.M = (uint32_t)a.tokens;
     g.N = (uint32_t)a.vocab;
     g.batch = 1;
     g.bf16 = a.type == SK_BF16;
-    g.status = dev.status;
     const StatsEpi::Args ea{(float2*)(ws + l.off_part), (float*)(ws + l.off_target), a.targets};
     const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{w, a.vocab, a.width, ld_w, 0, 1, false};
     const bool wide = wide_tiles(g.M, g.N, 1, false, dev.sm_count);
-    if (wide) SK_OP_CUDA((launch_gemm<2, 256, StatsEpi>(true, oh, ow, nullptr, nullptr, g, ea, dev.sm_count, st)));
-    else SK_OP_CUDA((launch_gemm<1, 128, StatsEpi>(true, oh, ow, nullptr, nullptr, g, ea, dev.sm_count, st)));
+    if (wide) SK_OP_CUDA((launch_one<2, 256, StatsEpi>(true, oh, ow, nullptr, nullptr, g, 1, dev.status, ea, dev.sm_count, st)));
+    else SK_OP_CUDA((launch_one<1, 128, StatsEpi>(true, oh, ow, nullptr, nullptr, g, 1, dev.status, ea, dev.sm_count, st)));
     const uint32_t tile = wide ? 256 : 128, slots = 2 * ((g.N + tile - 1) / tile);
     SK_OP_CUDA(launch_kernel(true, k_head_join, dim3((g.M + 7) / 8), kJoinThreads, 0, st, (const float2*)ea.part, (const float*)ea.at_target, a.targets, g.M,
                              a.vocab, slots, a.loss, a.lse));
@@ -317,48 +374,59 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
         SK_OP_CUDA(launch_kernel(true, k_head_factor, dim3(1), 1024, 0, st, a.dloss, a.targets, tokens, a.vocab, factor));
     }
     uint16_t* gbuf = (uint16_t*)(ws + l.off_g);
-    auto vec_ok = [&](const void* p, uint64_t ld, int type) { return (uintptr_t)p % 32 == 0 && ld * type_size(type) % 32 == 0; };
+    float* sum = l.off_sum ? (float*)(ws + l.off_sum) : nullptr;
     for (uint64_t v0 = 0; v0 < a.vocab; v0 += l.piece) {
         const uint32_t n = (uint32_t)(a.vocab - v0 < l.piece ? a.vocab - v0 : l.piece);
         const uint16_t* wp = (const uint16_t*)w + v0 * ld_w;
         const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{wp, n, a.width, ld_w, 0, 1, false};
-        GemmShape g{};
+        GemmGroup g{};
         g.batch = 1;
         g.bf16 = a.type == SK_BF16;
-        g.status = dev.status;
         g.M = tokens;
         g.N = n;
         const GradEpi::Args ga{gbuf, l.ld_g, a.lse, a.dloss, factor, a.targets, a.vocab, (uint32_t)v0};
-        SK_OP_CUDA(launch_product<GradEpi>(true, oh, ow, nullptr, nullptr, g, ga, dev.sm_count, st));
-        if (a.dweight) {                      // dW[v] = sum over tokens of G[t][v] hidden[t]: both factors with their rows contiguous
-            const Operand gt{gbuf, a.tokens, n, l.ld_g, 0, 1, true}, ht{h, a.tokens, a.width, ld_h, 0, 1, true};
-            g.M = n;
-            g.N = width;
-            OutEpi::Args ea{};
-            ea.out = (uint8_t*)a.dweight + v0 * a.ld_dweight * type_size(a.dweight_type);
-            ea.ld = a.ld_dweight;
-            ea.factor = factor;
-            ea.type = a.dweight_type;
-            ea.vec = vec_ok(ea.out, ea.ld, ea.type);
-            ea.first = ea.last = 1;
-            SK_OP_CUDA(launch_product<OutEpi>(true, gt, ht, nullptr, nullptr, g, ea, dev.sm_count, st));
+        SK_OP_CUDA(launch_product<GradEpi>(true, oh, ow, nullptr, nullptr, g, dev.status, ga, dev.sm_count, st));
+        // dW[v] = sum over tokens of G[t][v] hidden[t]: both factors with their rows contiguous;
+        // dhidden[t] += sum over the piece of G[t][v] W[v]
+        const Operand gt{gbuf, a.tokens, n, l.ld_g, 0, 1, true}, ht{h, a.tokens, a.width, ld_h, 0, 1, true};
+        const Operand og{gbuf, a.tokens, n, l.ld_g, 0, 1, false}, wt{wp, n, a.width, ld_w, 0, 1, true};
+        GemmGroup gw = g, gh = g;
+        gw.M = n;
+        gw.N = gh.N = width;
+        gh.M = tokens;
+        OutEpi::One one_w{}, one_h{};
+        one_w.out = (uint8_t*)a.dweight + v0 * a.ld_dweight * type_size(a.dweight_type);
+        one_w.ld = a.ld_dweight;
+        one_w.type = a.dweight_type;
+        one_w.align = row_alignment(one_w.out, one_w.ld, one_w.type);
+        one_h.out = a.dhidden;
+        one_h.type = a.dhidden_type;
+        one_h.ld = sum ? l.ld_sum : a.ld_dhidden;
+        one_h.sum = sum;
+        one_h.sum_stride = l.sum_stride;
+        one_h.add = v0 != 0;
+        one_h.align = row_alignment(one_h.out, one_h.ld, one_h.type);
+        const bool h_first = n >= tokens;                // the one with the longer K is the first
+        const uint32_t split = h_first ? l.slices : 1;   // of dhidden's product, when it is the first
+        OutEpi::Args ea{{h_first ? one_h : one_w, h_first ? one_w : one_h}, factor};
+        if (a.dweight && a.dhidden) {
+            const Operand &a0 = h_first ? og : gt, &b0 = h_first ? wt : ht, &a1 = h_first ? gt : og, &b1 = h_first ? ht : wt;
+            const GemmGroup &g0 = h_first ? gh : gw, &g1 = h_first ? gw : gh;
+            SK_OP_CUDA(l.wide ? launch_two<2, 256, OutEpi>(true, a0, b0, g0, split, a1, b1, g1, dev.status, ea, dev.sm_count, st)
+                              : launch_two<1, 128, OutEpi>(true, a0, b0, g0, split, a1, b1, g1, dev.status, ea, dev.sm_count, st));
+        } else {
+            const Operand &a0 = a.dhidden ? og : gt, &b0 = a.dhidden ? wt : ht;
+            const GemmGroup& g0 = a.dhidden ? gh : gw;
+            const uint32_t parts = a.dhidden ? split : 1;
+            ea.o[0] = a.dhidden ? one_h : one_w;
+            SK_OP_CUDA(l.wide ? launch_one<2, 256, OutEpi>(true, a0, b0, nullptr, nullptr, g0, parts, dev.status, ea, dev.sm_count, st)
+                              : launch_one<1, 128, OutEpi>(true, a0, b0, nullptr, nullptr, g0, parts, dev.status, ea, dev.sm_count, st));
         }
-        if (a.dhidden) {                      // dhidden[t] += sum over the piece of G[t][v] W[v]
-            const Operand og{gbuf, a.tokens, n, l.ld_g, 0, 1, false}, wt{wp, n, a.width, ld_w, 0, 1, true};
-            g.M = tokens;
-            g.N = width;
-            OutEpi::Args ea{};
-            ea.out = a.dhidden;
-            ea.sum = (float*)(ws + l.off_sum);
-            ea.ld = a.ld_dhidden;
-            ea.ld_sum = l.ld_sum;
-            ea.factor = factor;
-            ea.type = a.dhidden_type;
-            ea.vec = vec_ok(ea.out, ea.ld, ea.type);
-            ea.first = v0 == 0;
-            ea.last = v0 + l.piece >= a.vocab;
-            SK_OP_CUDA(launch_product<OutEpi>(true, og, wt, nullptr, nullptr, g, ea, dev.sm_count, st));
-        }
+    }
+    if (sum) {
+        const uint64_t want = (a.tokens * ((width + 3) / 4) + 255) / 256, most = (uint64_t)dev.sm_count * 8;
+        SK_OP_CUDA(launch_kernel(true, k_head_sum, dim3((uint32_t)(want < most ? want : most)), 256, 0, st, (const float*)sum, l.slices, l.sum_stride, l.ld_sum,
+                                 a.tokens, width, (const float*)factor, a.dhidden, a.ld_dhidden, a.dhidden_type));
     }
     return SK_OK;
 }

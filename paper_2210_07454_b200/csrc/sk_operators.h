@@ -68,11 +68,22 @@ __device__ __forceinline__ void load32b(const void* p, uint32_t* r) {
                  "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
 }
 
-// 32 neighbouring values of one row, rounded to the output's type; valid = how many of them exist.  vec: the row address
-// is 32-byte aligned whenever the column is a multiple of 32.
-__device__ __forceinline__ void store_row32(void* out, int type, uint64_t at, const float (&v)[32], uint32_t valid, bool vec) {
-    if (vec && valid >= 32) {
+// What is known of an output's rows: 32 when every row starts on a 32-byte boundary, else the largest of 16, 4 and the element
+inline uint32_t row_alignment(const void* p, uint64_t ld, int type) {
+    const uint64_t bits = (uintptr_t)p | ld * type_size(type);
+    return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
+}
+
+// A warp's 32 x 32 block of an output: lane = row (row0 + lane, rows of them exist), v = its columns col .. col + 31 (cols of them
+// exist; col is a multiple of 32).  Rows on 32-byte boundaries are written by their lanes; others go through the warp's shared memory, so that
+// neighbouring lanes write neighbouring addresses.  All lanes take part.
+__device__ __forceinline__ void store_block32(void* out, int type, uint64_t ld, uint64_t row0, uint32_t rows, uint64_t col, uint32_t cols,
+                                              const float (&v)[32], uint32_t align, uint32_t* stage, uint32_t stage_row) {
+    const uint32_t lane = threadIdx.x & 31;
+    if (align == 32 && cols >= 32) {
+        if (lane >= rows) return;
         uint32_t r[8];
+        const uint64_t at = (row0 + lane) * ld + col;
         if (type == SK_F32) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
@@ -90,9 +101,50 @@ __device__ __forceinline__ void store_row32(void* out, int type, uint64_t at, co
         }
         return;
     }
+    if (type == SK_F32) {                        // two halves of 16 columns through the same space
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-        if ((uint32_t)i < valid) store_as(out, type, at + i, v[i]);
+        for (int half = 0; half < 2; ++half) {
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                *(float4*)(stage + lane * stage_row + 4 * i) =
+                    make_float4(v[16 * half + 4 * i], v[16 * half + 4 * i + 1], v[16 * half + 4 * i + 2], v[16 * half + 4 * i + 3]);
+            __syncwarp();
+            const uint32_t c = lane & 15;
+            for (uint32_t r = lane >> 4; r < rows; r += 2)
+                if (16 * half + c < cols) ((float*)out)[(row0 + r) * ld + col + 16 * half + c] = __uint_as_float(stage[r * stage_row + c]);
+        }
+        return;
+    }
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint4 q;
+        q.x = pack16(v[8 * i], v[8 * i + 1], type == SK_BF16);
+        q.y = pack16(v[8 * i + 2], v[8 * i + 3], type == SK_BF16);
+        q.z = pack16(v[8 * i + 4], v[8 * i + 5], type == SK_BF16);
+        q.w = pack16(v[8 * i + 6], v[8 * i + 7], type == SK_BF16);
+        *(uint4*)(stage + lane * stage_row + 4 * i) = q;
+    }
+    __syncwarp();
+    uint16_t* o = (uint16_t*)out + row0 * ld + col;
+    if (align >= 16 && cols >= 32) {             // four lanes a row
+        const uint32_t c = lane & 3;
+#pragma unroll
+        for (uint32_t r = lane >> 2; r < 32; r += 8)
+            if (r < rows) *(uint4*)(o + r * ld + 8 * c) = *(const uint4*)(stage + r * stage_row + 4 * c);
+    } else if (align >= 4) {                     // sixteen lanes a row
+        const uint32_t c = lane & 15;
+#pragma unroll 4
+        for (uint32_t r = lane >> 4; r < rows; r += 2) {
+            const uint32_t w = stage[r * stage_row + c];
+            if (2 * c + 1 < cols) *(uint32_t*)(o + r * ld + 2 * c) = w;
+            else if (2 * c < cols) o[r * ld + 2 * c] = (uint16_t)w;
+        }
+    } else if (lane < cols) {
+#pragma unroll 4
+        for (uint32_t r = 0; r < rows; ++r) o[r * ld + lane] = ((const uint16_t*)(stage + r * stage_row))[lane];
+    }
 }
 
 // ---- launchers ---------------------------------------------------------------------------------------------------------

@@ -30,23 +30,30 @@ constexpr uint32_t kPadCols = 32;                                // leading dime
 struct GramEpi {
     struct Args { __half* out; uint64_t stride; uint32_t ld; const float* factor; };
     const Args& a;
-    const GemmShape& g;
+    const GemmGroup& g;
     __half* out;
-    uint32_t row;
+    uint32_t row, row0;                          // the lane's, the warp's first
+    uint32_t* stage;
     bool mirror;
     float scale = kUnscale;
-    __device__ GramEpi(const Args& a_, const GemmShape& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t)
-        : a(a_), g(g_), out(a_.out + at.b * a_.stride), row(row_), mirror(at.m != at.n) {
+    __device__ GramEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t, uint32_t* stage_)
+        : a(a_), g(g_), out(a_.out + at.b * a_.stride), row(row_), row0(row_ - (threadIdx.x & 31)), stage(stage_), mirror(at.m != at.n) {
         if (a.factor) scale *= a.factor[at.b] * a.factor[at.b];
     }
     __device__ void put(uint32_t col, float (&v)[32]) {
-        if (row >= g.M) return;
-        store_row32(out, SK_F16, (uint64_t)row * a.ld + col, v, 32, true);
-        if (mirror) {
+        if (row0 >= g.M) return;
+        const uint32_t rows = g.M - row0 < 32 ? g.M - row0 : 32;
+        store_block32(out, SK_F16, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
+        if (!mirror) return;
+        // the block transposed: a lane's values are a column of it; four lanes write a row of the mirror image
+        const uint32_t lane = threadIdx.x & 31, c = lane & 3;
+        __syncwarp();
 #pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (col + i < g.N) out[(uint64_t)(col + i) * a.ld + row] = __float2half_rn(v[i]);
-        }
+        for (int i = 0; i < 32; ++i) ((__half*)(stage + i * kStageRow))[lane] = __float2half_rn(v[i]);
+        __syncwarp();
+#pragma unroll
+        for (uint32_t r = lane >> 2; r < 32; r += 8)
+            if (col + r < g.N) *(uint4*)(out + (uint64_t)(col + r) * a.ld + row0 + 8 * c) = *(const uint4*)(stage + r * kStageRow + 4 * c);
     }
     __device__ void chunk(uint32_t col, float (&v)[32]) {
 #pragma unroll
@@ -62,8 +69,8 @@ struct PolyEpi {
     const Args& p;
     GramEpi e;
     const __half* gram;
-    __device__ PolyEpi(const Args& a_, const GemmShape& g_, const TileAt& at, uint32_t row_, uint32_t c0, uint32_t half)
-        : p(a_), e(a_.o, g_, at, row_, c0, half), gram(a_.gram + at.b * a_.o.stride) {}
+    __device__ PolyEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t c0, uint32_t half, uint32_t* stage_)
+        : p(a_), e(a_.o, g_, at, row_, c0, half, stage_), gram(a_.gram + at.b * a_.o.stride) {}
     __device__ void chunk(uint32_t col, float (&v)[32]) {
         if (e.row < e.g.M) {
             uint32_t r[16];
@@ -87,30 +94,32 @@ struct PolyEpi {
 
 // X <- P X: one fp16 matrix, or two whose sum it is; the last step writes the result in the caller's type and layout
 struct ApplyEpi {
-    struct Args { __half *hi, *lo; void* out; uint64_t stride; uint64_t ld; int type; uint32_t vec; const float* factor; };
+    struct Args { __half *hi, *lo; void* out; uint64_t stride; uint64_t ld; int type; uint32_t align; const float* factor; };
     const Args& a;
-    const GemmShape& g;
-    uint64_t at0;
-    uint32_t row;
+    const GemmGroup& g;
+    uint64_t first;
+    uint32_t row0, rows;
+    uint32_t* stage;
     float scale = kUnscale;
-    __device__ ApplyEpi(const Args& a_, const GemmShape& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t)
-        : a(a_), g(g_), at0(at.b * a_.stride + (uint64_t)row_ * a_.ld), row(row_) {
+    __device__ ApplyEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t, uint32_t* stage_)
+        : a(a_), g(g_), first(at.b * a_.stride), row0(row_ - (threadIdx.x & 31)), stage(stage_) {
+        rows = row0 >= g.M ? 0 : g.M - row0 < 32 ? g.M - row0 : 32;
         if (a.factor) scale *= a.factor[at.b];
         if (a.out) scale *= kUnscale;
     }
     __device__ void chunk(uint32_t col, float (&v)[32]) {
-        if (row >= g.M) return;
+        if (!rows) return;
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= scale;
         if (a.out) {
-            store_row32(a.out, a.type, at0 + col, v, g.N - col, a.vec);
+            store_block32((uint16_t*)a.out + first, a.type, a.ld, row0, rows, col, g.N - col, v, a.align, stage, kStageRow);
             return;
         }
-        store_row32(a.hi, SK_F16, at0 + col, v, 32, true);
+        store_block32(a.hi + first, SK_F16, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
         if (a.lo) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
-            store_row32(a.lo, SK_F16, at0 + col, v, 32, true);
+            store_block32(a.lo + first, SK_F16, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
         }
     }
     __device__ void end() {}
@@ -317,23 +326,23 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     SK_OP_CUDA(launch_kernel(true, k_ortho_square, dim3(sq.blocks, batch), 256, 0, st, sq));
     SK_OP_CUDA(launch_kernel(true, k_ortho_scale, dim3(sq.blocks, batch), 256, 0, st, sq));
 
-    GemmShape square{};
+    GemmGroup square{};
     square.M = square.N = m;
     square.batch = batch;
     square.symmetric = 1;
-    square.status = dev.status;
-    GemmShape apply = square;
+    GemmGroup apply = square;
     apply.symmetric = 0;
     apply.M = (uint32_t)a.rows;
     apply.N = (uint32_t)a.cols;
     const Operand oa{gram, m, m, l.ld_a, l.a_elems, batch, false}, op{poly, m, m, l.ld_a, l.a_elems, batch, false};
-    const bool vec = (uintptr_t)a.out % 32 == 0 && a.ld_out * type_size(a.out_type) % 32 == 0 && a.stride_out * type_size(a.out_type) % 32 == 0;
+    const uint32_t align_rows = row_alignment(a.out, a.ld_out, a.out_type), align_batch = row_alignment(a.out, a.stride_out, a.out_type);
+    const uint32_t align = batch > 1 && align_batch < align_rows ? align_batch : align_rows;
     for (int s = 0; s < a.steps; ++s) {
         const int from = s & 1, to = from ^ 1;
         const Operand ox{x[from], a.rows, a.cols, l.ld_x, l.x_elems, batch, tall};
-        SK_OP_CUDA(launch_product<GramEpi>(true, ox, ox, nullptr, nullptr, square, {gram, l.a_elems, l.ld_a, s == 0 ? sq.factor : nullptr}, dev.sm_count, st));
+        SK_OP_CUDA(launch_product<GramEpi>(true, ox, ox, nullptr, nullptr, square, dev.status, {gram, l.a_elems, l.ld_a, s == 0 ? sq.factor : nullptr}, dev.sm_count, st));
         PolyEpi::Args pa{{poly, l.a_elems, l.ld_a, nullptr}, gram, a.coefficient[0], a.coefficient[1], a.coefficient[2]};
-        SK_OP_CUDA(launch_product<PolyEpi>(true, oa, oa, nullptr, nullptr, square, pa, dev.sm_count, st));
+        SK_OP_CUDA(launch_product<PolyEpi>(true, oa, oa, nullptr, nullptr, square, dev.status, pa, dev.sm_count, st));
         ApplyEpi::Args ea{};
         ea.factor = s == 0 ? sq.factor : nullptr;
         if (s + 1 < a.steps) {
@@ -346,13 +355,13 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
             ea.stride = a.stride_out;
             ea.ld = a.ld_out;
             ea.type = a.out_type;
-            ea.vec = vec;
+            ea.align = align;
         }
         // X stored with its columns contiguous is the K-major first factor of X P, and the MN-major second factor of P X
         const Operand xh{x[from], a.rows, a.cols, l.ld_x, l.x_elems, batch, !tall}, xl{lo[from], a.rows, a.cols, l.ld_x, l.x_elems, batch, !tall};
         const bool two = split(s);
-        if (tall) SK_OP_CUDA(launch_product<ApplyEpi>(true, xh, op, two ? &xl : nullptr, two ? &op : nullptr, apply, ea, dev.sm_count, st));
-        else SK_OP_CUDA(launch_product<ApplyEpi>(true, op, xh, two ? &op : nullptr, two ? &xl : nullptr, apply, ea, dev.sm_count, st));
+        if (tall) SK_OP_CUDA(launch_product<ApplyEpi>(true, xh, op, two ? &xl : nullptr, two ? &op : nullptr, apply, dev.status, ea, dev.sm_count, st));
+        else SK_OP_CUDA(launch_product<ApplyEpi>(true, op, xh, two ? &op : nullptr, two ? &xl : nullptr, apply, dev.status, ea, dev.sm_count, st));
     }
     return SK_OK;
 }
