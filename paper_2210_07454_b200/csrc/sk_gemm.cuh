@@ -165,9 +165,9 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
 }
 
 // Shared-memory descriptor, 128-byte swizzle.  K-major: rows of 128 bytes, groups of eight rows 1024 bytes apart.
-// MN-major: blocks of 64 row indices, 64 k deep (8192 bytes) one after the other, groups of eight k 1024 bytes apart.
-__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn) {
-    const uint64_t lead = mn ? (8192u >> 4) : 1u;
+// MN-major: blocks of 64 row indices (block_bytes from one to the next: 8192 if they are 64 k deep), groups of eight k 1024 bytes apart.
+__device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t block_bytes = 8192) {
+    const uint64_t lead = mn ? (block_bytes >> 4) : 1u;
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
@@ -261,8 +261,14 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
     if constexpr (CG == 2) cluster_sync_all();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *(volatile uint32_t*)&tmem_slot;
+    if (threadIdx.x < 4) {                                       // the descriptors depend on no other kernel
+        const CUtensorMap* m = threadIdx.x == 0 ? &map_a : threadIdx.x == 1 ? &map_b : threadIdx.x == 2 ? &map_a2 : &map_b2;
+        asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+    }
 
     chain_acquire();
+    // the grid fits the SMs, so it is resident as a whole: the next kernel's blocks may take the slots that are free
+    chain_release();
 
     const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG;
     TileAt at;
@@ -450,16 +456,18 @@ cudaError_t launch_gemm(bool chain, const Operand& a, const Operand& b, const Op
 // What a tile costs beside its stages, in stages (its epilogue where nothing hides it)
 constexpr uint32_t kTileCost = 6;
 
-// Which tile: pairs of blocks on 256 x 256, or single blocks on 128 x 128.  A large tile reads each operand half as often and is
-// what keeps the tensor cores fed (512 cycles of products against 64 KB of operands per stage, both at a pair); small
-// ones spread a small product over more SMs.  The one whose last wave ends first wins.
-inline bool wide_tiles(uint32_t M, uint32_t N, uint32_t batch, bool symmetric, int sm_count) {
+// Which tile: pairs of blocks on 256 x 256, or single blocks on 128 x 128.  Both take about 620 cycles a stage at an SM, because 32 KB
+// of operands a stage come from L2 at 50 bytes a cycle: measured 617 (pair; its products alone take 512) and 636.  The pair does
+// twice the work per SM in that time; the small tile ends sooner (its epilogue and start take about 7000 cycles, the pair's 12,000, measured
+// with K = 64) and spreads a small product over more SMs.  The one whose last wave ends first wins.
+inline bool wide_tiles(uint32_t M, uint32_t N, uint64_t stages, uint32_t batch, bool symmetric, int sm_count) {
     auto count = [&](uint32_t t) {
         const uint64_t m = (M + t - 1) / t, n = (N + t - 1) / t;
         return batch * (symmetric ? m * (m + 1) / 2 : m * n);
     };
     const uint64_t slots = (uint64_t)sm_count;
-    const uint64_t wide = (count(256) + slots / 2 - 1) / (slots / 2) * 512, small = (count(128) + slots - 1) / slots * 330;
+    const uint64_t wide = (count(256) + slots / 2 - 1) / (slots / 2) * stages * 620 + 12000;
+    const uint64_t small = (count(128) + slots - 1) / slots * stages * 620 + 7000;
     return wide <= small;
 }
 
@@ -478,7 +486,8 @@ cudaError_t launch_one(bool chain, const Operand& a, const Operand& b, const Ope
 template <class Epi>
 cudaError_t launch_product(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, const GemmGroup& g, uint32_t* status,
                            const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
-    if (wide_tiles(g.M, g.N, g.batch, g.symmetric, sm_count)) return launch_one<2, 256, Epi>(chain, a, b, a2, b2, g, 1, status, ea, sm_count, st);
+    const uint64_t stages = ((a.mn ? a.rows : a.cols) + kGemmK - 1) / kGemmK * (a2 ? 2 : 1);
+    if (wide_tiles(g.M, g.N, stages, g.batch, g.symmetric, sm_count)) return launch_one<2, 256, Epi>(chain, a, b, a2, b2, g, 1, status, ea, sm_count, st);
     return launch_one<1, 128, Epi>(chain, a, b, a2, b2, g, 1, status, ea, sm_count, st);
 }
 

@@ -351,7 +351,7 @@ int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
     g.bf16 = a.type == SK_BF16;
     const StatsEpi::Args ea{(float2*)(ws + l.off_part), (float*)(ws + l.off_target), a.targets};
     const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{w, a.vocab, a.width, ld_w, 0, 1, false};
-    const bool wide = wide_tiles(g.M, g.N, 1, false, dev.sm_count);
+    const bool wide = wide_tiles(g.M, g.N, (a.width + kGemmK - 1) / kGemmK, 1, false, dev.sm_count);
     if (wide) SK_OP_CUDA((launch_one<2, 256, StatsEpi>(true, oh, ow, nullptr, nullptr, g, 1, dev.status, ea, dev.sm_count, st)));
     else SK_OP_CUDA((launch_one<1, 128, StatsEpi>(true, oh, ow, nullptr, nullptr, g, 1, dev.status, ea, dev.sm_count, st)));
     const uint32_t tile = wide ? 256 : 128, slots = 2 * ((g.N + tile - 1) / tile);

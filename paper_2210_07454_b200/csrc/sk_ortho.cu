@@ -292,11 +292,374 @@ OrthoLayout layout_of(const OrthoArgs& a) {
     return l;
 }
 
+// ---- the whole iteration in one launch --------------------------------------------------------------------------------
+// Matrices whose shorter side is at most 128 (Y: m x n, m <= 128, the update or its transpose) and whose longer one is at most 8 * 256: fifteen
+// dependent products of microseconds each are all launch latency one by one, so a cluster of blocks keeps the matrix in shared
+// memory and does everything.  Block c holds 256 columns of Y as fp16 pairs; its layout (blocks of 64 columns, rows of 128 bytes,
+// swizzled) is at once the K-major operand of Y Y^T and the MN-major second factor of P Y.  The blocks' shares of the gram matrix are added
+// up in block order, a slice of rows to each block, over distributed shared memory; A^2 and P are small and formed by every block.
+// Measured against the launches: 100 x 130, 5 steps: see DESIGN's table of times.
+constexpr int kSmallThreads = 512;
+constexpr uint32_t kSmallSide = 128, kSmallCols = 256, kSmallCluster = 8;
+constexpr uint32_t kSmallGroups = kSmallSide * kSmallCols / 8 / kSmallThreads;
+constexpr uint32_t kSmallHi = 0, kSmallLo = 65536, kSmallGram = 131072, kSmallPoly = kSmallGram + 32768, kSmallBytes = 196608;
+
+struct SmallArgs {
+    OrthoArgs a;
+    uint32_t m, n, tall, blocks;                 // blocks of the cluster
+    uint32_t align, vec_u, vec_m;
+    uint32_t* status;
+};
+
+// where 16-byte chunk `chunk` of row r of a 64-column block lies
+__device__ __forceinline__ uint32_t swizzled(uint32_t r, uint32_t chunk) { return r * 128 + ((chunk ^ (r & 7)) << 4); }
+__device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank) {
+    uint32_t r;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
+// 32 values of a row as fp16 into a swizzled matrix of 64-column blocks of 128 rows
+__device__ __forceinline__ void put32(uint8_t* base, uint32_t r, uint32_t col, const float (&v)[32]) {
+    uint8_t* block = base + (col >> 6) * 16384;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        uint4 q;
+        q.x = pack16(v[8 * i], v[8 * i + 1], false);
+        q.y = pack16(v[8 * i + 2], v[8 * i + 3], false);
+        q.z = pack16(v[8 * i + 4], v[8 * i + 5], false);
+        q.w = pack16(v[8 * i + 6], v[8 * i + 7], false);
+        *(uint4*)(block + swizzled(r, ((col & 63) >> 3) + i)) = q;
+    }
+}
+
+__global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_constant__ SmallArgs s) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ __align__(8) uint64_t bar_mem;
+    __shared__ uint32_t tmem_slot;
+    __shared__ double sums[kSmallThreads / 32], shares[kSmallCluster];
+    const OrthoArgs& a = s.a;
+    const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, S = s.blocks;
+    const uint32_t rank = S > 1 ? cluster_rank() : 0, batch = blockIdx.x / S;
+    const uint32_t base32 = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* base = smem_raw + (base32 - smem_u32(smem_raw));
+    const uint32_t bar = smem_u32(&bar_mem);
+    if (tid == 0) {
+        mbar_init(bar, 1);
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) tmem_alloc<1>(smem_u32(&tmem_slot), 512);
+    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+    __syncthreads();
+    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+    const uint32_t tmem = *(volatile uint32_t*)&tmem_slot, tmem_sq = tmem + 128, tmem_x = tmem + 256;
+    chain_acquire();
+
+    // columns first .. first + width of Y are this block's; in memory they are columns (wide) or rows (tall) of the update
+    const uint32_t first = rank * kSmallCols, width = s.n > first ? min(s.n - first, kSmallCols) : 0;
+    // what the products go over, in whole steps of 16 (the same in every block of the cluster): beyond Y's rows and columns up to there is
+    // zero, what lies further out is never read
+    const uint32_t m16 = (s.m + 15) / 16 * 16, w16 = (min(s.n, kSmallCols) + 15) / 16 * 16, blocks64 = (w16 + 63) / 64;
+    const uint64_t at_u = batch * a.stride_update, at_m = batch * a.stride_momentum;
+    // element (i, j) of this block's part: i along the shorter side
+    auto offset = [&](uint64_t ld, uint32_t i, uint32_t j) { return s.tall ? (uint64_t)(first + j) * ld + i : (uint64_t)i * ld + first + j; };
+    // groups of eight neighbours of a row in memory, at most eight groups a thread, held in registers from the norm to the matrix
+    const uint32_t fast = s.tall ? s.m : width, slow = s.tall ? width : s.m, per = (fast + 7) / 8, groups = per * slow;
+    float u[kSmallGroups][8];
+    double sum = 0;
+    auto place = [&](uint32_t g, uint32_t& y, uint32_t& x) {
+        const uint32_t q = g * kSmallThreads + tid;
+        y = q / per;
+        x = (q - y * per) * 8;
+        return q < groups;
+    };
+#pragma unroll
+    for (uint32_t g = 0; g < kSmallGroups; ++g) {
+        uint32_t y, x;
+        const bool live = place(g, y, x);
+        if (live) load8(a.update, a.type, at_u + (s.tall ? offset(a.ld_update, x, y) : offset(a.ld_update, y, x)), fast - x, s.vec_u, u[g]);
+        else
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[g][k] = 0.0f;
+    }
+    if (a.momentum) {
+#pragma unroll
+        for (uint32_t g = 0; g < kSmallGroups; ++g) {
+            uint32_t y, x;
+            if (!place(g, y, x)) continue;
+            const uint64_t at = at_m + (s.tall ? offset(a.ld_momentum, x, y) : offset(a.ld_momentum, y, x));
+            float m[8];
+            load8(a.momentum, SK_F32, at, fast - x, s.vec_m, m);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                m[k] = a.beta * m[k] + u[g][k];
+                u[g][k] = a.nesterov ? u[g][k] + a.beta * m[k] : m[k];
+            }
+            if (s.vec_m) {
+                *(float4*)(a.momentum + at) = make_float4(m[0], m[1], m[2], m[3]);
+                *(float4*)(a.momentum + at + 4) = make_float4(m[4], m[5], m[6], m[7]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (x + k < fast) a.momentum[at + k] = m[k];
+            }
+        }
+    }
+#pragma unroll
+    for (uint32_t g = 0; g < kSmallGroups; ++g) {
+        float part = 0;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) part += u[g][k] * u[g][k];
+        if (part > 1e-30f && part < 1e30f) sum += (double)part;      // the eight squares are well inside the 32-bit range
+        else
+#pragma unroll
+            for (int k = 0; k < 8; ++k) sum += (double)u[g][k] * (double)u[g][k];
+    }
+#pragma unroll
+    for (int o = 16; o; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
+    if (lane == 0) sums[warp] = sum;
+    for (uint32_t q = tid; q < blocks64 * 1024; q += kSmallThreads) {
+        ((uint4*)(base + kSmallHi))[q] = make_uint4(0, 0, 0, 0);
+        ((uint4*)(base + kSmallLo))[q] = make_uint4(0, 0, 0, 0);
+    }
+    if (S > 1) cluster_sync_all();               // every block of the cluster has started
+    __syncthreads();
+    if (tid < S) {                               // this block's share into slot `rank` of every block
+        double t = 0;
+        for (int i = 0; i < kSmallThreads / 32; ++i) t += sums[i];
+        asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(S > 1 ? map_to(smem_u32(&shares[rank]), tid) : smem_u32(&shares[0])), "d"(t) : "memory");
+    }
+    if (S > 1) cluster_sync_all();
+    __syncthreads();
+    sum = 0;
+    for (uint32_t i = 0; i < S; ++i) sum += shares[i];
+    const float scale = (float)((double)kScale / (sqrt(sum) + (double)a.eps));
+    const bool pair = a.steps > 2;
+#pragma unroll
+    for (uint32_t g = 0; g < kSmallGroups; ++g) {
+        uint32_t y, x;
+        if (!place(g, y, x)) continue;
+        if (!s.tall) {                           // eight columns of a row: one 16-byte chunk
+            uint32_t h[4], l[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float p = u[g][2 * k] * scale, r = u[g][2 * k + 1] * scale;
+                const __half2 both = __floats2half2_rn(p, r);
+                const float2 f = __half22float2(both);
+                h[k] = *(const uint32_t*)&both;
+                l[k] = pack16(p - f.x, r - f.y, false);
+            }
+            const uint32_t at = (x >> 6) * 16384 + swizzled(y, (x & 63) >> 3);
+            *(uint4*)(base + kSmallHi + at) = make_uint4(h[0], h[1], h[2], h[3]);
+            if (pair) *(uint4*)(base + kSmallLo + at) = make_uint4(l[0], l[1], l[2], l[3]);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (x + k >= fast) break;
+                const float p = u[g][k] * scale;
+                const __half h = __float2half_rn(p);
+                const uint32_t at = (y >> 6) * 16384 + swizzled(x + k, (y & 63) >> 3) + (y & 7) * 2;
+                *(__half*)(base + kSmallHi + at) = h;
+                if (pair) *(__half*)(base + kSmallLo + at) = __float2half_rn(p - __half2float(h));
+            }
+        }
+    }
+
+    // fp32 sums, fp16 operands, M = 128
+    const uint32_t idesc = (1u << 4) | (8u << 24), idesc_m = idesc | (m16 / 8 << 17), idesc_x = idesc | (1u << 16) | (w16 / 8 << 17);
+    const uint32_t quarter = warp & 3, part = warp >> 2, row = quarter * 32 + lane, lanes = (quarter * 32) << 16;     // part: of the columns
+    uint32_t phase = 0;
+    // the products of one phase issued by one thread, waited for by all
+    auto run = [&](auto issue) {
+        fence_async();
+        __syncthreads();
+        if (tid == 0) {
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            issue();
+            mma_commit<1>(bar);
+        }
+        mbar_wait(bar, phase, s.status);
+        phase ^= 1;
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        __syncwarp();
+    };
+    // every thread has read what it needs of the accumulators before the next products overwrite them
+    auto read_done = [&] { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); };
+
+    for (int step = 0; step < a.steps; ++step) {
+        const bool two = step < a.steps - 2;
+        run([&] {                                // Y Y^T, this block's columns
+            for (uint32_t k = 0; k < w16 / 16; ++k) {
+                const uint64_t d = smem_desc(base32 + kSmallHi + (k >> 2) * 16384, false) + 2 * (k & 3);
+                mma_f16<1>(tmem, d, d, idesc_m, k != 0);
+            }
+        });
+        const uint32_t col = part * 32;
+        const bool mine = quarter * 32 < s.m && col < m16;       // this warp's rows and columns of the square matrices
+        float v[32];
+        if (mine) tmem_load32(tmem + col + lanes, v);
+        if (S == 1) {
+            if (mine) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] *= kUnscale;
+                put32(base + kSmallGram, row, col, v);
+            }
+        } else {
+            if (mine) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    *(float4*)(base + kSmallGram + row * 512 + (((col >> 2) + i) ^ (row & 7)) * 16) =
+                        make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+            }
+            read_done();
+            cluster_sync_all();                  // everybody's share is there
+            const uint32_t each = 128 / S, items = each * 32 / kSmallThreads;        // rows of this block; float4s per thread: 4, 2, 1
+            float4 t[4];
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                t[q] = make_float4(0, 0, 0, 0);
+                if (q >= items) continue;
+                const uint32_t item = q * kSmallThreads + tid, r = rank * each + (item >> 5), c4 = item & 31;
+                const uint32_t local = base32 + kSmallGram + r * 512 + (c4 ^ (r & 7)) * 16;
+                for (uint32_t k = 0; k < S; ++k) {
+                    float4 f;
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(map_to(local, k)) : "memory");
+                    t[q].x += f.x; t[q].y += f.y; t[q].z += f.z; t[q].w += f.w;
+                }
+            }
+            cluster_sync_all();                  // everybody has read: the space becomes A and P
+#pragma unroll
+            for (uint32_t q = 0; q < 4; ++q) {
+                if (q >= items) continue;
+                const uint32_t item = q * kSmallThreads + tid, r = rank * each + (item >> 5), c4 = item & 31;
+                const uint32_t local = base32 + kSmallGram + (c4 >> 4) * 16384 + swizzled(r, (c4 & 15) >> 1) + (c4 & 1) * 8;
+                const uint32_t lo = pack16(t[q].x * kUnscale, t[q].y * kUnscale, false), hi = pack16(t[q].z * kUnscale, t[q].w * kUnscale, false);
+                for (uint32_t k = 0; k < S; ++k) asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(map_to(local, k)), "r"(lo), "r"(hi) : "memory");
+            }
+            fence_async();
+            cluster_sync_all();
+        }
+        read_done();
+        run([&] {                                // A^2
+            for (uint32_t k = 0; k < m16 / 16; ++k) {
+                const uint64_t d = smem_desc(base32 + kSmallGram + (k >> 2) * 16384, false) + 2 * (k & 3);
+                mma_f16<1>(tmem_sq, d, d, idesc_m, k != 0);
+            }
+        });
+        if (mine) {
+            tmem_load32(tmem_sq + col + lanes, v);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint4 w = *(const uint4*)(base + kSmallGram + (col >> 6) * 16384 + swizzled(row, ((col & 63) >> 3) + i));
+                const uint32_t g[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const float2 f = __half22float2(*(const __half2*)&g[k]);
+                    v[8 * i + 2 * k] = a.coefficient[1] * f.x + a.coefficient[2] * kUnscale * v[8 * i + 2 * k];
+                    v[8 * i + 2 * k + 1] = a.coefficient[1] * f.y + a.coefficient[2] * kUnscale * v[8 * i + 2 * k + 1];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (col + i == row) v[i] += a.coefficient[0] * kScale;
+            put32(base + kSmallPoly, row, col, v);
+        }
+        read_done();
+        run([&] {                                // P Y, with both matrices of the pair while there are two
+            for (uint32_t which = 0; which < (two ? 2u : 1u); ++which)
+                for (uint32_t k = 0; k < m16 / 16; ++k)
+                    mma_f16<1>(tmem_x, smem_desc(base32 + kSmallPoly + (k >> 2) * 16384, false) + 2 * (k & 3),
+                               smem_desc(base32 + (which ? kSmallLo : kSmallHi), true, 16384) + 128 * k, idesc_x, (which | k) != 0);
+        });
+        const bool last = step + 1 == a.steps, next_two = step + 1 < a.steps - 2;
+#pragma unroll 1
+        for (uint32_t col = quarter * 32 < s.m ? part * 32 : w16; col < w16; col += 32 * (kSmallThreads / 128)) {
+            __syncwarp();
+            tmem_load32(tmem_x + col + lanes, v);
+            if (!last) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] *= kUnscale;
+                put32(base + kSmallHi, row, col, v);
+                if (next_two) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
+                    put32(base + kSmallLo, row, col, v);
+                }
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= kUnscale * kUnscale;
+            const uint32_t row0 = quarter * 32;
+            if (col >= width) continue;
+            uint16_t* out = (uint16_t*)a.out + batch * a.stride_out;
+            if (!s.tall) {
+                store_block32(out + first, a.out_type, a.ld_out, row0, min(s.m - row0, 32u), col, width - col, v, s.align,
+                              (uint32_t*)(base + kSmallGram) + warp * kStageWords, kStageRow);
+            } else if (row < s.m) {              // the lanes' rows are the output's neighbouring columns
+#pragma unroll
+                for (int i = 0; i < 32; ++i)
+                    if (col + i < width) store_as(out, a.out_type, (uint64_t)(first + col + i) * a.ld_out + row, v[i]);
+            }
+        }
+        read_done();
+    }
+    __syncthreads();
+    if (S > 1) cluster_sync_all();               // nobody leaves while its shared memory may be read
+    if (warp == 0) {
+        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        tmem_free<1>(tmem, 512);
+    }
+}
+
+bool is_small(const OrthoArgs& a) {
+    const uint64_t m = a.rows < a.cols ? a.rows : a.cols, n = a.rows < a.cols ? a.cols : a.rows;
+    return m <= kSmallSide && n <= kSmallCluster * kSmallCols;
+}
+cudaError_t launch_small(const OrthoArgs& a, uint32_t align, const OpDevice& dev, cudaStream_t st) {
+    SmallArgs s{a};
+    s.tall = a.rows > a.cols;
+    s.m = (uint32_t)(s.tall ? a.cols : a.rows);
+    s.n = (uint32_t)(s.tall ? a.rows : a.cols);
+    s.blocks = 1;
+    while (s.blocks * kSmallCols < s.n) s.blocks *= 2;
+    s.align = align;
+    const uint64_t fast = a.cols;
+    auto vec8 = [&](const void* p, uint64_t ld, uint64_t stride, uint32_t size) {
+        return fast % 8 == 0 && (uintptr_t)p % 16 == 0 && ld * size % 16 == 0 && (a.batch == 1 || stride * size % 16 == 0);
+    };
+    s.vec_u = vec8(a.update, a.ld_update, a.stride_update, type_size(a.type));
+    s.vec_m = a.momentum && vec8(a.momentum, a.ld_momentum, a.stride_momentum, 4);
+    s.status = dev.status;
+    constexpr int kSmem = (int)kSmallBytes + 1024;
+    cudaError_t e = cudaFuncSetAttribute(k_ortho_small, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((uint32_t)a.batch * s.blocks);
+    cfg.blockDim = dim3(kSmallThreads);
+    cfg.dynamicSmemBytes = kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = s.blocks;
+    attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = s.blocks > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, k_ortho_small, s);
+}
+
 }  // namespace
 
-uint64_t orthogonalize_workspace(const OrthoArgs& a) { return layout_of(a).total; }
+uint64_t orthogonalize_workspace(const OrthoArgs& a) { return is_small(a) ? 0 : layout_of(a).total; }
 
 int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t st) {
+    const uint32_t align_rows = row_alignment(a.out, a.ld_out, a.out_type), align_batch = row_alignment(a.out, a.stride_out, a.out_type);
+    const uint32_t align = a.batch > 1 && align_batch < align_rows ? align_batch : align_rows;
+    if (is_small(a)) {
+        SK_OP_CUDA(launch_small(a, align, dev, st));
+        return SK_OK;
+    }
     const OrthoLayout l = layout_of(a);
     uint8_t* ws = (uint8_t*)a.workspace;
     double* partial = (double*)(ws + l.off_partial);
@@ -335,8 +698,6 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     apply.M = (uint32_t)a.rows;
     apply.N = (uint32_t)a.cols;
     const Operand oa{gram, m, m, l.ld_a, l.a_elems, batch, false}, op{poly, m, m, l.ld_a, l.a_elems, batch, false};
-    const uint32_t align_rows = row_alignment(a.out, a.ld_out, a.out_type), align_batch = row_alignment(a.out, a.stride_out, a.out_type);
-    const uint32_t align = batch > 1 && align_batch < align_rows ? align_batch : align_rows;
     for (int s = 0; s < a.steps; ++s) {
         const int from = s & 1, to = from ^ 1;
         const Operand ox{x[from], a.rows, a.cols, l.ld_x, l.x_elems, batch, tall};

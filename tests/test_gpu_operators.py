@@ -528,14 +528,15 @@ def test_workspaces_are_checked():
     import ctypes
     from paper_2210_07454_b200 import binding
     L = binding.lib()
-    u = randn(1, 64, 64)
-    out = torch.empty(64, 64, dtype=torch.bfloat16, device="cuda")
-    need = L.sk_orthogonalize_workspace(1, 64, 64)
+    n = 160
+    u = randn(1, n, n)
+    out = torch.empty(n, n, dtype=torch.bfloat16, device="cuda")
+    need = L.sk_orthogonalize_workspace(1, n, n)
     ws = torch.empty(need + 256, dtype=torch.uint8, device="cuda")
     coef = (ctypes.c_float * 3)(*COEF)
 
     def call(ptr, size):
-        return L.sk_orthogonalize(u.data_ptr(), 64, 4096, 0, None, 0, 0, 0.0, 0, out.data_ptr(), 64, 4096, 1, 1, 64, 64, 5, coef, 1e-7, ptr, size, None)
+        return L.sk_orthogonalize(u.data_ptr(), n, n * n, 0, None, 0, 0, 0.0, 0, out.data_ptr(), n, n * n, 1, 1, n, n, 5, coef, 1e-7, ptr, size, None)
 
     assert call(ws.data_ptr(), need) == 0
     assert call(ws.data_ptr(), need - 1) == -1 and b"workspace" in L.sk_last_error()

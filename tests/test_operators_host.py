@@ -24,11 +24,11 @@ def test_c_entries_check_before_they_launch():
     coef = (ctypes.c_float * 3)(3.4445, -4.7750, 2.0315)
     p = 4096                                                       # an aligned address that is never read
 
-    def ortho(batch=1, rows=8, cols=8, steps=5, c=coef, ld=8, out_type=1, eps=1e-7, ws=0):
+    def ortho(batch=1, rows=200, cols=200, steps=5, c=coef, ld=200, out_type=1, eps=1e-7, ws=0):
         return L.sk_orthogonalize(p, ld, 64, 0, None, 0, 0, 0.0, 0, p, ld, 64, out_type, batch, rows, cols, steps, c, eps, None, ws, None)
 
     assert ortho(rows=0) == 0 and ortho(cols=0) == 0 and ortho(batch=0) == 0
-    for kw, word in ((dict(steps=0), b"steps"), (dict(c=None), b"coefficients"), (dict(ld=7), b"leading"), (dict(out_type=0), b"out_type"),
+    for kw, word in ((dict(steps=0), b"steps"), (dict(c=None), b"coefficients"), (dict(ld=199), b"leading"), (dict(out_type=0), b"out_type"),
                      (dict(rows=70000), b"rows"), (dict(eps=-1.0), b"eps"), ({}, b"workspace")):
         assert ortho(**kw) == -1 and word in L.sk_last_error(), kw
 
