@@ -31,8 +31,7 @@ constexpr uint32_t kOpWait = 1u;              // status word of the operators: a
 constexpr int kGemmK = 64;                    // values of k per stage: 128 bytes, the width of the swizzle
 constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
-constexpr int kStageRow = 20;                 // words from one row of a warp's 32 x 32 sixteen-bit values to the next: whole, odd 16-byte steps
-constexpr int kStageWords = 32 * kStageRow;   // of shared memory for each epilogue warp
+constexpr int kStageWords = 1024;             // of shared memory for each epilogue warp (store_tile32)
 
 // One product of a launch.
 struct GemmGroup {
@@ -47,6 +46,8 @@ struct GemmGroup {
     uint32_t symmetric;                       // 1: only tiles on and below the diagonal; the epilogue mirrors them
     uint32_t tiles;                           // total over the batch
     uint32_t a_mn, b_mn;                      // 1: MN-major
+    uint32_t a_rows;                          // rows of A a block loads: 128, or fewer where a single tile row has no more
+    uint32_t k_rows;                          // values of k in a stage: 64, or fewer where K has no more (in steps of 16)
     uint32_t bf16;                            // operand type: 1 bf16, 0 fp16
 };
 // A launch: one product, or two that do not depend on each other (the second with map_a2, map_b2 as its operands), the one with
@@ -67,15 +68,16 @@ __device__ __forceinline__ void mbar_init(uint32_t bar, uint32_t count) {
 __device__ __forceinline__ void mbar_expect(uint32_t bar, uint32_t bytes) {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// bar: a shared::cluster address (a block's own shared::cta addresses are valid ones)
+// bar: a shared::cluster address (a block's own shared::cta addresses are valid ones).  What it orders is the reading of tensor memory, which
+// the tcgen05 fences around it do; a release to the whole cluster would wait for the epilogue's global stores as well.
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     uint32_t ok;
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
@@ -221,12 +223,12 @@ __device__ __forceinline__ uint32_t stages_of(const GemmGroup& g, const TileAt& 
 template <int CG, int BN>
 struct GemmTile {
     static constexpr int kStageBytes = 128 * 128 + (BN / CG) * 128;      // both operands, 64 values of k
-    static constexpr int kStages = BN / CG >= 128 ? 6 : 8;               // as many as fit
+    static constexpr int kStages = BN / CG >= 256 ? 4 : 6;                            // as many as fit
     static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStageWords * 4 + 1024;      // + the epilogue's, + alignment
 };
 
 // Epi: struct Args; __device__ Epi(const Args&, group, tile, row, first column, half, the warp's shared memory);
-// chunk(col, v[32]); end().  A thread holds one row of the tile and gets its columns 32 at a time; the two warps that share a row take half
+// chunk(col, v[32], last); end().  A thread holds one row of the tile and gets its columns 32 at a time; the two warps that share a row take half
 // the columns each.  Rows >= M are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
 template <int CG, int BN, class Epi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
@@ -273,71 +275,84 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
     const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG;
     TileAt at;
 
+    // The two single threads that feed the tensor cores have a stage's time, some 600 cycles, for each trip of their loops: what is constant
+    // over a tile is in registers, and the ring's slot and its parity go round without divisions.
+    constexpr uint32_t kBytes = kBytesA + kBytesB;
     if (warp == 0) {
         if (lane == 0) {
-            uint32_t it = 0;
-            bool ok = true;
+            uint32_t s = 0, parity = 1;                          // a fresh barrier counts as having completed its previous phase
+            bool ok = true, any = false;
             for (uint32_t i = 0; ok && tile_of(shape, unit, units, i, at); ++i) {
                 const GemmGroup& g = shape.g[at.group];
-                const uint32_t kb = stages_of(g, at), k_first = g.sliced ? at.b * g.k_blocks : 0;
-                const int z = g.sliced ? 0 : (int)at.b;
+                const uint32_t kb = stages_of(g, at), pass = g.k_blocks;
+                const bool a_mn = g.a_mn, b_mn = g.b_mn, grouped = at.group != 0;
+                const int z = g.sliced ? 0 : (int)at.b, k_first = g.sliced ? (int)(at.b * g.k_blocks * kGemmK) : 0;
                 const int row_a = (int)(at.m * (128 * CG) + rank * 128);
                 const int row_b = (int)(at.n * BN + rank * kRowsB);
-                for (uint32_t k = 0; k < kb; ++k, ++it) {
-                    const uint32_t s = it % kStages;
-                    if (it >= (uint32_t)kStages && !(ok = mbar_wait(empty(s), ((it / kStages) - 1) & 1, shape.status))) break;
-                    const bool pass2 = k >= g.k_blocks, second = pass2 || at.group;
-                    const CUtensorMap* ma = second ? &map_a2 : &map_a;
-                    const CUtensorMap* mb = second ? &map_b2 : &map_b;
-                    const int k0 = (int)((k_first + (pass2 ? k - g.k_blocks : k)) * kGemmK);
-                    const uint32_t sa = stages + s * (kBytesA + kBytesB), sb = sa + kBytesA;
+                const uint32_t bytes = CG * 128 * ((a_mn ? 2 * g.k_rows : g.a_rows) + (b_mn ? kRowsB / 64 * g.k_rows : kRowsB));
+                const CUtensorMap* ma = grouped ? &map_a2 : &map_a;
+                const CUtensorMap* mb = grouped ? &map_b2 : &map_b;
+                int k0 = k_first;
+                any = true;
+                for (uint32_t k = 0; k < kb; ++k, k0 += kGemmK) {
+                    if (k == pass) {                             // the second pass: the other operands from the start of K
+                        ma = &map_a2;
+                        mb = &map_b2;
+                        k0 = 0;
+                    }
+                    if (!(ok = mbar_wait(empty(s), parity, shape.status))) break;
+                    const uint32_t sa = stages + s * kBytes, sb = sa + kBytesA;
                     uint32_t bar = full(s);
-                    if (rank == 0) mbar_expect(bar, CG * (kBytesA + kBytesB));
+                    if (rank == 0) mbar_expect(bar, bytes);
                     if constexpr (CG == 2) bar = map_to_leader(bar);
-                    if (g.a_mn) {
+                    if (a_mn) {
                         tma_load<CG>(sa, ma, bar, row_a, k0, z);
                         tma_load<CG>(sa + 8192, ma, bar, row_a + 64, k0, z);
                     } else {
                         tma_load<CG>(sa, ma, bar, k0, row_a, z);
                     }
-                    if (g.b_mn) {
+                    if (b_mn) {
 #pragma unroll
                         for (int q = 0; q < kRowsB / 64; ++q) tma_load<CG>(sb + q * 8192, mb, bar, row_b + q * 64, k0, z);
                     } else {
                         tma_load<CG>(sb, mb, bar, k0, row_b, z);
                     }
+                    if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
                 }
             }
-            // this block's own copies land in its shared memory: the last ones are waited for before the block may end
-            if (it) {
-                const uint32_t from = it > (uint32_t)kStages ? it - kStages : 0;
-                for (uint32_t q = from; q < it; ++q)
-                    if (!mbar_wait(empty(q % kStages), (q / kStages) & 1, shape.status)) break;
-            }
+            // this block's own copies land in its shared memory: all of them are waited for before the block may end
+            if (any)
+                for (uint32_t q = 0; q < (uint32_t)kStages; ++q) {
+                    if (!mbar_wait(empty(s), parity, shape.status)) break;
+                    if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
+                }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            uint32_t it = 0;
+            uint32_t s = 0, parity = 0;
             bool ok = true;
             for (uint32_t n = 0; ok && tile_of(shape, unit, units, n, at); ++n) {
                 const GemmGroup& g = shape.g[at.group];
-                const uint32_t kb = stages_of(g, at), a = n & 1;
+                const uint32_t kb = stages_of(g, at), a = n & 1, steps = g.k_rows / 16, d = tmem + a * BN;
                 // D fp32; A, B bf16 or fp16; majors; N / 8; M / 16
                 const uint32_t idesc = (1u << 4) | (g.bf16 << 7) | (g.bf16 << 10) | (g.a_mn << 15) | (g.b_mn << 16) |
                                        ((uint32_t)(BN / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
                 const uint64_t step_a = (g.a_mn ? 2048u : 32u) >> 4, step_b = (g.b_mn ? 2048u : 32u) >> 4;
+                const uint64_t desc_a = smem_desc(stages, g.a_mn), desc_b = smem_desc(stages + kBytesA, g.b_mn);
                 if (n >= 2 && !(ok = mbar_wait(acc_empty(a), ((n >> 1) - 1) & 1, shape.status))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (uint32_t k = 0; k < kb; ++k, ++it) {
-                    const uint32_t s = it % kStages;
-                    if (!(ok = mbar_wait(full(s), (it / kStages) & 1, shape.status))) break;
+                for (uint32_t k = 0; k < kb; ++k) {
+                    if (!(ok = mbar_wait(full(s), parity, shape.status))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint32_t sa = stages + s * (kBytesA + kBytesB);
-                    const uint64_t da = smem_desc(sa, g.a_mn), db = smem_desc(sa + kBytesA, g.b_mn);
+                    const uint64_t da = desc_a + s * (kBytes >> 4), db = desc_b + s * (kBytes >> 4);
+                    if (steps == kGemmK / 16) {
 #pragma unroll
-                    for (uint32_t q = 0; q < kGemmK / 16; ++q)
-                        mma_f16<CG>(tmem + a * BN, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
+                        for (uint32_t q = 0; q < kGemmK / 16; ++q) mma_f16<CG>(d, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
+                    } else {
+                        for (uint32_t q = 0; q < steps; ++q) mma_f16<CG>(d, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
+                    }
                     mma_commit<CG>(empty(s));
+                    if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
                 }
                 mma_commit<CG>(acc_full(a));
             }
@@ -363,7 +378,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_leader(acc_empty(a)) : acc_empty(a));
                 }
-                if (col0 + c < g.N) epi.chunk(col0 + c, v);
+                if (col0 + c < g.N) epi.chunk(col0 + c, v, c + 32 == BN / 2 || col0 + c + 32 >= g.N);
             }
             epi.end();
         }
@@ -395,7 +410,9 @@ template <int CG, int BN>
 void set_tiles(GemmGroup& g, const Operand& a, const Operand& b, uint32_t slices) {
     g.a_mn = a.mn;
     g.b_mn = b.mn;
-    g.k_total = (uint32_t)(((a.mn ? a.rows : a.cols) + kGemmK - 1) / kGemmK);
+    const uint64_t K = a.mn ? a.rows : a.cols;
+    g.k_total = (uint32_t)((K + kGemmK - 1) / kGemmK);
+    g.k_rows = K < kGemmK ? (uint32_t)((K + 15) / 16 * 16) : kGemmK;
     g.k_blocks = g.k_total;
     if (slices > 1) {
         g.k_blocks = (g.k_total + slices - 1) / slices;
@@ -404,8 +421,18 @@ void set_tiles(GemmGroup& g, const Operand& a, const Operand& b, uint32_t slices
     }
     g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
     g.tiles_n = (g.N + BN - 1) / BN;
+    // The rest of the stage's rows stay what they were and give sums that nobody reads.  Loading them as zeros is not free: 8 tokens
+    // against 128,000 x 4096 took 285 us so, and takes 186 us without (reading the matrix alone 172).
+    g.a_rows = CG == 1 && !g.a_mn && g.M < 128 ? (g.M + 7) / 8 * 8 : 128;
     g.tiles = g.batch * (g.symmetric ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n);
-    g.band = g.tiles_m < 16 ? g.tiles_m : 16;
+    // Tiles that run at the same time share operands through L2.  Where A is the smaller operand and fits, its whole height is walked
+    // first, so that B is read once; where B is, a band is just high enough for the SMs to span the width: A is read
+    // once and whole rows of D are written together.
+    const uint64_t a_bytes = g.M * K * 2, b_bytes = g.N * K * 2;
+    uint32_t band = 16;
+    if (a_bytes <= b_bytes && a_bytes <= (32u << 20)) band = g.tiles_m;
+    if (a_bytes > b_bytes) band = g.tiles_n >= 74 ? 1 : 74 / g.tiles_n < 8 ? 74 / g.tiles_n : 8;
+    g.band = band < g.tiles_m ? band : g.tiles_m;
 }
 
 // a2, b2: the second pass's operands, or with groups = 2 the second product's.
@@ -415,8 +442,9 @@ cudaError_t launch_gemm(bool chain, const Operand& a, const Operand& b, const Op
     const uint32_t tiles = g.g[0].tiles + (g.groups == 2 ? g.g[1].tiles : 0);
     if (!tiles) return cudaSuccess;
     CUtensorMap ma, mb, ma2, mb2;
-    bool ok = encode_operand(&ma, a, g.g[0].bf16, 128) && encode_operand(&mb, b, g.g[0].bf16, BN / CG);
-    if (a2) ok = ok && encode_operand(&ma2, *a2, g.g[0].bf16, 128) && encode_operand(&mb2, *b2, g.g[0].bf16, BN / CG);
+    const GemmGroup &g0 = g.g[0], &g1 = g.groups == 2 ? g.g[1] : g.g[0];
+    bool ok = encode_operand(&ma, a, g0.bf16, a.mn ? g0.k_rows : g0.a_rows) && encode_operand(&mb, b, g0.bf16, b.mn ? g0.k_rows : BN / CG);
+    if (a2) ok = ok && encode_operand(&ma2, *a2, g1.bf16, a2->mn ? g1.k_rows : g1.a_rows) && encode_operand(&mb2, *b2, g1.bf16, b2->mn ? g1.k_rows : BN / CG);
     else { ma2 = ma; mb2 = mb; }
     if (!ok) return cudaErrorInvalidValue;
     auto kernel = k_gemm<CG, BN, Epi>;

@@ -34,7 +34,7 @@ struct StatsEpi {
     float top = -INFINITY, sum = 0;
     __device__ StatsEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t half, uint32_t*)
         : a(a_), g(g_), row(row_), slot(at.n * 2 + half) { target = row < g.M ? a.targets[row] : -1; }
-    __device__ void chunk(uint32_t col, float (&v)[32]) {
+    __device__ void chunk(uint32_t col, float (&v)[32], bool) {
         const uint32_t valid = g.N - col;
         const uint64_t d = (uint64_t)(target - (int64_t)col);
         if (d < 32 && d < valid) {
@@ -129,7 +129,7 @@ struct GradEpi {
             }
         }
     }
-    __device__ void chunk(uint32_t col, float (&v)[32]) {
+    __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (!rows) return;
         const uint64_t d = (uint64_t)(target - (int64_t)col);
         if (scale != 0.0f) {
@@ -146,7 +146,7 @@ struct GradEpi {
             for (int i = 0; i < 32; ++i) v[i] = 0.0f;
         }
         __syncwarp();
-        store_block32(a.out, g.bf16 ? SK_BF16 : SK_F16, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
+        store_tile32(a.out, g.bf16 ? SK_BF16 : SK_F16, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage, true, last);
     }
     __device__ void end() {}
 };
@@ -167,12 +167,12 @@ struct OutEpi {
           scale(a_.factor ? 1.0f / *a_.factor : 1.0f) {
         rows = row0 >= g.M ? 0 : g.M - row0 < 32 ? g.M - row0 : 32;
     }
-    __device__ void chunk(uint32_t col, float (&v)[32]) {
+    __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (!rows) return;
         if (!sum) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] *= scale;
-            store_block32(a.out, a.type, a.ld, row0, rows, col, g.N - col, v, a.align, stage, kStageRow);
+            store_tile32(a.out, a.type, a.ld, row0, rows, col, g.N, v, a.align, stage, true, last);
             return;
         }
         const uint32_t lane = threadIdx.x & 31;
@@ -186,7 +186,8 @@ struct OutEpi {
                 for (int i = 0; i < 8; ++i) v[8 * q + i] += __uint_as_float(r[i]);
             }
         }
-        store_block32(sum, SK_F32, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
+        __syncwarp();
+        store_tile32(sum, SK_F32, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage, false, last);
     }
     __device__ void end() {}
 };
@@ -235,21 +236,40 @@ __global__ void __launch_bounds__(1024) k_head_factor(const float* dloss, const 
     }
 }
 
-// Rows copied to a leading dimension that TMA can address; with targets, the rows that take no part become zero.  The
-// backward pass always takes the hidden states through this: in dW a token without a target is multiplied by zeros, and
-// whatever its row holds (padding may hold infinities or NaN) must not survive that.
-__global__ void __launch_bounds__(256) k_head_pack(const uint16_t* src, uint64_t ld, uint16_t* dst, uint32_t ld_dst, uint64_t rows, uint32_t cols,
-                                                   const int64_t* targets, uint64_t vocab, uint32_t vec) {
+// Rows copied to a leading dimension that TMA can address, up to two matrices in one launch; with targets, the rows that
+// take no part become zero.  The backward pass always takes the hidden states through this: in dW a token without a target is multiplied
+// by zeros, and whatever its row holds (padding may hold infinities or NaN) must not survive that.
+struct PackArgs {
+    struct One { const uint16_t* src; uint16_t* dst; uint64_t ld, rows; const int64_t* targets; } m[2];
+    uint64_t vocab;
+    uint32_t ld_dst, cols, first_blocks;         // blocks of the first matrix
+};
+// A thread copies eight neighbours: eight loads on their way at once whatever the alignment, one 16-byte store.
+__global__ void __launch_bounds__(256) k_head_pack(const __grid_constant__ PackArgs a) {
     chain_acquire();
-    const uint32_t lane = threadIdx.x & 31;
-    for (uint64_t r = blockIdx.x * 8ull + (threadIdx.x >> 5); r < rows; r += gridDim.x * 8ull) {
-        const bool live = !targets || (targets[r] >= 0 && targets[r] < (int64_t)vocab);
-        const uint16_t* s = src + r * ld;
-        uint16_t* d = dst + r * ld_dst;
-        if (vec)
-            for (uint32_t c = lane * 8; c < cols; c += 256) *(uint4*)(d + c) = live ? *(const uint4*)(s + c) : make_uint4(0, 0, 0, 0);
-        else
-            for (uint32_t c = lane; c < cols; c += 32) d[c] = live ? s[c] : (uint16_t)0;
+    const uint32_t which = blockIdx.x >= a.first_blocks;
+    const PackArgs::One& m = a.m[which];
+    const uint32_t groups = a.ld_dst / 8, block = which ? blockIdx.x - a.first_blocks : blockIdx.x;
+    const uint64_t total = m.rows * groups, step = (uint64_t)(which ? gridDim.x - a.first_blocks : a.first_blocks) * 256;
+    const bool vec = (uintptr_t)m.src % 16 == 0 && m.ld % 8 == 0, half = (uintptr_t)m.src % 8 == 0 && m.ld % 4 == 0;
+    for (uint64_t q = block * 256ull + threadIdx.x; q < total; q += step) {
+        const uint64_t r = q / groups;
+        const uint32_t c = (uint32_t)(q - r * groups) * 8;
+        const bool live = !m.targets || (m.targets[r] >= 0 && m.targets[r] < (int64_t)a.vocab);
+        const uint16_t* s = m.src + r * m.ld + c;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (live && c + 8 <= a.cols && vec) {
+            v = *(const uint4*)s;
+        } else if (live && c + 8 <= a.cols && half) {
+            const uint2 x = *(const uint2*)s, y = *(const uint2*)(s + 4);
+            v = make_uint4(x.x, x.y, y.x, y.y);
+        } else if (live) {
+            uint32_t e[8];
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) e[i] = c + i < a.cols ? s[i] : 0;
+            v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+        }
+        *(uint4*)(m.dst + r * a.ld_dst + c) = v;
     }
 }
 
@@ -271,7 +291,7 @@ constexpr uint32_t kPlanSms = 148;               // the plan, and with it the wo
 uint32_t slices_of(uint64_t tokens, uint64_t n, uint64_t width, bool wide) {
     if (n < tokens) return 1;
     const uint64_t tile = wide ? 256 : 128, units = kPlanSms / (wide ? 2 : 1);
-    const uint64_t rows = (tokens + tile - 1) / tile, cols = (width + tile - 1) / tile, vocab = (n + tile - 1) / tile;
+    const uint64_t rows = (tokens + tile - 1) / tile, cols = (width + 255) / 256, vocab = (n + tile - 1) / tile;
     const uint64_t k0 = (n + kGemmK - 1) / kGemmK, k1 = (tokens + kGemmK - 1) / kGemmK;
     const uint64_t work = rows * cols * (k0 + kTileCost) + vocab * cols * (k1 + kTileCost);
     uint64_t s = 2 * k0 * units / work;
@@ -315,20 +335,27 @@ int pack_operands(const HeadArgs& a, bool backward, const HeadLayout& l, const O
                   cudaStream_t st) {
     uint8_t* ws = (uint8_t*)a.workspace;
     *h = a.hidden; *w = a.weight; *ld_h = a.ld_hidden; *ld_w = a.ld_weight;
-    auto pack = [&](const void* src, uint64_t ld, uint64_t off, uint64_t rows, const int64_t* targets) {
-        const bool vec = a.width % 8 == 0 && addressable(src, ld);
-        const uint64_t want = (rows + 7) / 8, most = (uint64_t)dev.sm_count * 8;
-        return launch_kernel(true, k_head_pack, dim3((uint32_t)(want < most ? want : most)), 256, 0, st, (const uint16_t*)src, ld,
-                             (uint16_t*)(ws + off), (uint32_t)l.ld_pack, rows, (uint32_t)a.width, targets, a.vocab, (uint32_t)vec);
+    PackArgs p{};
+    uint32_t n = 0, blocks[2] = {0, 0};
+    auto add = [&](const void* src, uint64_t ld, uint64_t off, uint64_t rows, const int64_t* targets) {
+        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, rows, targets};
+        const uint64_t want = (rows * (l.ld_pack / 8) + 255) / 256, most = (uint64_t)dev.sm_count * 16;
+        blocks[n++] = (uint32_t)(want < most ? want : most);
     };
     if (l.pack_h) {
-        SK_OP_CUDA(pack(a.hidden, a.ld_hidden, l.off_h, a.tokens, backward ? a.targets : nullptr));
+        add(a.hidden, a.ld_hidden, l.off_h, a.tokens, backward ? a.targets : nullptr);
         *h = ws + l.off_h; *ld_h = l.ld_pack;
     }
     if (l.pack_w) {
-        SK_OP_CUDA(pack(a.weight, a.ld_weight, l.off_w, a.vocab, nullptr));
+        add(a.weight, a.ld_weight, l.off_w, a.vocab, nullptr);
         *w = ws + l.off_w; *ld_w = l.ld_pack;
     }
+    if (!n) return SK_OK;
+    p.vocab = a.vocab;
+    p.ld_dst = (uint32_t)l.ld_pack;
+    p.cols = (uint32_t)a.width;
+    p.first_blocks = blocks[0];
+    SK_OP_CUDA(launch_kernel(true, k_head_pack, dim3(blocks[0] + blocks[1]), 256, 0, st, p));
     return SK_OK;
 }
 
@@ -413,14 +440,14 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
             const Operand &a0 = h_first ? og : gt, &b0 = h_first ? wt : ht, &a1 = h_first ? gt : og, &b1 = h_first ? ht : wt;
             const GemmGroup &g0 = h_first ? gh : gw, &g1 = h_first ? gw : gh;
             SK_OP_CUDA(l.wide ? launch_two<2, 256, OutEpi>(true, a0, b0, g0, split, a1, b1, g1, dev.status, ea, dev.sm_count, st)
-                              : launch_two<1, 128, OutEpi>(true, a0, b0, g0, split, a1, b1, g1, dev.status, ea, dev.sm_count, st));
+                              : launch_two<1, 256, OutEpi>(true, a0, b0, g0, split, a1, b1, g1, dev.status, ea, dev.sm_count, st));
         } else {
             const Operand &a0 = a.dhidden ? og : gt, &b0 = a.dhidden ? wt : ht;
             const GemmGroup& g0 = a.dhidden ? gh : gw;
             const uint32_t parts = a.dhidden ? split : 1;
             ea.o[0] = a.dhidden ? one_h : one_w;
             SK_OP_CUDA(l.wide ? launch_one<2, 256, OutEpi>(true, a0, b0, nullptr, nullptr, g0, parts, dev.status, ea, dev.sm_count, st)
-                              : launch_one<1, 128, OutEpi>(true, a0, b0, nullptr, nullptr, g0, parts, dev.status, ea, dev.sm_count, st));
+                              : launch_one<1, 256, OutEpi>(true, a0, b0, nullptr, nullptr, g0, parts, dev.status, ea, dev.sm_count, st));
         }
     }
     if (sum) {

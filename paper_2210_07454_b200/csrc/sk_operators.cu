@@ -43,7 +43,7 @@ int op_device(OpDevice* out) {
 bool encode_operand(CUtensorMap* map, const Operand& o, bool bf16, uint32_t box_rows) {
     const cuuint64_t dims[3] = {o.cols, o.rows, o.batch};
     const cuuint64_t strides[2] = {o.ld * 2, (o.batch > 1 ? o.batch_stride : round_up(o.rows * o.ld, 8)) * 2};
-    const cuuint32_t box[3] = {64, o.mn ? 64u : box_rows, 1}, elem[3] = {1, 1, 1};
+    const cuuint32_t box[3] = {64, box_rows, 1}, elem[3] = {1, 1, 1};
     return g_encode.load()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<void*>(o.p), dims, strides, box,
                     elem, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;

@@ -68,82 +68,63 @@ __device__ __forceinline__ void load32b(const void* p, uint32_t* r) {
                  "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
 }
 
-// What is known of an output's rows: 32 when every row starts on a 32-byte boundary, else the largest of 16, 4 and the element
+// What is known of an output's rows: the largest of 16, 4 and 2 bytes that every row starts on
 inline uint32_t row_alignment(const void* p, uint64_t ld, int type) {
     const uint64_t bits = (uintptr_t)p | ld * type_size(type);
-    return bits % 32 == 0 ? 32 : bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
+    return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
 }
 
-// A warp's 32 x 32 block of an output: lane = row (row0 + lane, rows of them exist), v = its columns col .. col + 31 (cols of them
-// exist; col is a multiple of 32).  Rows on 32-byte boundaries are written by their lanes; others go through the warp's shared memory, so that
-// neighbouring lanes write neighbouring addresses.  All lanes take part.
-__device__ __forceinline__ void store_block32(void* out, int type, uint64_t ld, uint64_t row0, uint32_t rows, uint64_t col, uint32_t cols,
-                                              const float (&v)[32], uint32_t align, uint32_t* stage, uint32_t stage_row) {
-    const uint32_t lane = threadIdx.x & 31;
-    if (align == 32 && cols >= 32) {
-        if (lane >= rows) return;
-        uint32_t r[8];
-        const uint64_t at = (row0 + lane) * ld + col;
-        if (type == SK_F32) {
+// A warp's rows of an output tile, 32 columns at a time: the lane's row (row0 + lane; rows of the 32 exist), v = its columns
+// col .. col + 31 (those below limit exist; col is a multiple of 32).  The values pass through 4 KB of the warp's shared memory (32 rows of 128 bytes, 16-byte
+// chunks swizzled), so that neighbouring lanes write neighbouring addresses: whole 128-byte lines, two calls of 16-bit values
+// together (pair; last: no second one follows).  Lanes writing 32 bytes of a row each took 5900 cycles for 128 x 256, about as much as a
+// product over 600 values of k.  All lanes take part.
+__device__ __forceinline__ uint8_t* staged(uint32_t* stage, uint32_t r, uint32_t chunk) { return (uint8_t*)stage + r * 128 + ((chunk ^ (r & 7)) << 4); }
+__device__ __forceinline__ void store_tile32(void* out, int type, uint64_t ld, uint64_t row0, uint32_t rows, uint32_t col, uint32_t limit,
+                                             const float (&v)[32], uint32_t align, uint32_t* stage, bool pair, bool last) {
+    const bool wide = type == SK_F32;            // 32 columns are whole lines already
+    const uint32_t lane = threadIdx.x & 31, second = pair && !wide ? (col >> 5) & 1 : 0;
+    if (!second) __syncwarp();                   // what was staged before has been read
+    if (wide) {
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+        for (int i = 0; i < 8; ++i) *(float4*)staged(stage, lane, i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+    } else {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) r[i] = __float_as_uint(v[8 * q + i]);
-                store32b((float*)out + at + 8 * q, r);
-            }
-        } else {
-#pragma unroll
-            for (int q = 0; q < 2; ++q) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) r[i] = pack16(v[16 * q + 2 * i], v[16 * q + 2 * i + 1], type == SK_BF16);
-                store32b((uint16_t*)out + at + 16 * q, r);
-            }
+        for (int i = 0; i < 4; ++i) {
+            uint4 q;
+            q.x = pack16(v[8 * i], v[8 * i + 1], type == SK_BF16);
+            q.y = pack16(v[8 * i + 2], v[8 * i + 3], type == SK_BF16);
+            q.z = pack16(v[8 * i + 4], v[8 * i + 5], type == SK_BF16);
+            q.w = pack16(v[8 * i + 6], v[8 * i + 7], type == SK_BF16);
+            *(uint4*)staged(stage, lane, 4 * second + i) = q;
         }
-        return;
-    }
-    if (type == SK_F32) {                        // two halves of 16 columns through the same space
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                *(float4*)(stage + lane * stage_row + 4 * i) =
-                    make_float4(v[16 * half + 4 * i], v[16 * half + 4 * i + 1], v[16 * half + 4 * i + 2], v[16 * half + 4 * i + 3]);
-            __syncwarp();
-            const uint32_t c = lane & 15;
-            for (uint32_t r = lane >> 4; r < rows; r += 2)
-                if (16 * half + c < cols) ((float*)out)[(row0 + r) * ld + col + 16 * half + c] = __uint_as_float(stage[r * stage_row + c]);
-        }
-        return;
+        if (pair && !second && !last) return;    // the other half of the lines follows
     }
     __syncwarp();
+    const uint32_t size = wide ? 4 : 2, first = col - 32 * second;
+    const uint32_t bytes = min(wide ? 128u : 64u * (second + 1), (limit - first) * size);            // of every row
+    uint8_t* o = (uint8_t*)out + (row0 * ld + first) * size;
+    const uint64_t step = ld * size;
+    if (align >= 16 && bytes % 16 == 0) {        // eight lanes a row
+        const uint32_t c = lane & 7;
+        if (c * 16 < bytes)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        uint4 q;
-        q.x = pack16(v[8 * i], v[8 * i + 1], type == SK_BF16);
-        q.y = pack16(v[8 * i + 2], v[8 * i + 3], type == SK_BF16);
-        q.z = pack16(v[8 * i + 4], v[8 * i + 5], type == SK_BF16);
-        q.w = pack16(v[8 * i + 6], v[8 * i + 7], type == SK_BF16);
-        *(uint4*)(stage + lane * stage_row + 4 * i) = q;
-    }
-    __syncwarp();
-    uint16_t* o = (uint16_t*)out + row0 * ld + col;
-    if (align >= 16 && cols >= 32) {             // four lanes a row
-        const uint32_t c = lane & 3;
+            for (uint32_t r = lane >> 3; r < 32; r += 4)
+                if (r < rows) *(uint4*)(o + r * step + c * 16) = *(const uint4*)staged(stage, r, c);
+    } else if (align >= 4) {                     // a row after the other
+        if (lane * 4 < bytes)
+#pragma unroll 4
+            for (uint32_t r = 0; r < rows; ++r) {
+                const uint32_t w = *(const uint32_t*)(staged(stage, r, lane >> 2) + (lane & 3) * 4);
+                if (lane * 4 + 4 <= bytes) *(uint32_t*)(o + r * step + lane * 4) = w;
+                else *(uint16_t*)(o + r * step + lane * 4) = (uint16_t)w;
+            }
+    } else {
+#pragma unroll 4
+        for (uint32_t r = 0; r < rows; ++r)
 #pragma unroll
-        for (uint32_t r = lane >> 2; r < 32; r += 8)
-            if (r < rows) *(uint4*)(o + r * ld + 8 * c) = *(const uint4*)(stage + r * stage_row + 4 * c);
-    } else if (align >= 4) {                     // sixteen lanes a row
-        const uint32_t c = lane & 15;
-#pragma unroll 4
-        for (uint32_t r = lane >> 4; r < rows; r += 2) {
-            const uint32_t w = stage[r * stage_row + c];
-            if (2 * c + 1 < cols) *(uint32_t*)(o + r * ld + 2 * c) = w;
-            else if (2 * c < cols) o[r * ld + 2 * c] = (uint16_t)w;
-        }
-    } else if (lane < cols) {
-#pragma unroll 4
-        for (uint32_t r = 0; r < rows; ++r) o[r * ld + lane] = ((const uint16_t*)(stage + r * stage_row))[lane];
+            for (uint32_t c = lane; c < 64; c += 32)
+                if (c * 2 < bytes) *(uint16_t*)(o + r * step + c * 2) = *(const uint16_t*)(staged(stage, r, c >> 3) + (c & 7) * 2);
     }
 }
 

@@ -40,25 +40,25 @@ struct GramEpi {
         : a(a_), g(g_), out(a_.out + at.b * a_.stride), row(row_), row0(row_ - (threadIdx.x & 31)), stage(stage_), mirror(at.m != at.n) {
         if (a.factor) scale *= a.factor[at.b] * a.factor[at.b];
     }
-    __device__ void put(uint32_t col, float (&v)[32]) {
+    __device__ void put(uint32_t col, float (&v)[32], bool last) {
         if (row0 >= g.M) return;
         const uint32_t rows = g.M - row0 < 32 ? g.M - row0 : 32;
-        store_block32(out, SK_F16, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
+        store_tile32(out, SK_F16, a.ld, row0, rows, col, a.ld, v, 16, stage, !mirror, last);
         if (!mirror) return;
         // the block transposed: a lane's values are a column of it; four lanes write a row of the mirror image
         const uint32_t lane = threadIdx.x & 31, c = lane & 3;
         __syncwarp();
 #pragma unroll
-        for (int i = 0; i < 32; ++i) ((__half*)(stage + i * kStageRow))[lane] = __float2half_rn(v[i]);
+        for (int i = 0; i < 32; ++i) ((__half*)stage)[i * 32 + lane] = __float2half_rn(v[i]);
         __syncwarp();
 #pragma unroll
         for (uint32_t r = lane >> 2; r < 32; r += 8)
-            if (col + r < g.N) *(uint4*)(out + (uint64_t)(col + r) * a.ld + row0 + 8 * c) = *(const uint4*)(stage + r * kStageRow + 4 * c);
+            if (col + r < g.N) *(uint4*)(out + (uint64_t)(col + r) * a.ld + row0 + 8 * c) = ((const uint4*)stage)[r * 4 + c];
     }
-    __device__ void chunk(uint32_t col, float (&v)[32]) {
+    __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= scale;
-        put(col, v);
+        put(col, v, last);
     }
     __device__ void end() {}
 };
@@ -71,7 +71,7 @@ struct PolyEpi {
     const __half* gram;
     __device__ PolyEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t c0, uint32_t half, uint32_t* stage_)
         : p(a_), e(a_.o, g_, at, row_, c0, half, stage_), gram(a_.gram + at.b * a_.o.stride) {}
-    __device__ void chunk(uint32_t col, float (&v)[32]) {
+    __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (e.row < e.g.M) {
             uint32_t r[16];
             const __half* src = gram + (uint64_t)e.row * p.o.ld + col;
@@ -87,7 +87,8 @@ struct PolyEpi {
             for (int i = 0; i < 32; ++i)
                 if (col + i == e.row) v[i] += p.a * kScale;
         }
-        e.put(col, v);
+        __syncwarp();
+        e.put(col, v, last);
     }
     __device__ void end() {}
 };
@@ -107,19 +108,19 @@ struct ApplyEpi {
         if (a.factor) scale *= a.factor[at.b];
         if (a.out) scale *= kUnscale;
     }
-    __device__ void chunk(uint32_t col, float (&v)[32]) {
+    __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (!rows) return;
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= scale;
         if (a.out) {
-            store_block32((uint16_t*)a.out + first, a.type, a.ld, row0, rows, col, g.N - col, v, a.align, stage, kStageRow);
+            store_tile32((uint16_t*)a.out + first, a.type, a.ld, row0, rows, col, g.N, v, a.align, stage, true, last);
             return;
         }
-        store_block32(a.hi + first, SK_F16, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
-        if (a.lo) {
+        store_tile32(a.hi + first, SK_F16, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage, !a.lo, last);
+        if (a.lo) {                              // the two share the space, so neither waits for its lines' second half
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
-            store_block32(a.lo + first, SK_F16, a.ld, row0, rows, col, 32, v, 32, stage, kStageRow);
+            store_tile32(a.lo + first, SK_F16, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage, false, last);
         }
     }
     __device__ void end() {}
@@ -593,8 +594,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
             if (col >= width) continue;
             uint16_t* out = (uint16_t*)a.out + batch * a.stride_out;
             if (!s.tall) {
-                store_block32(out + first, a.out_type, a.ld_out, row0, min(s.m - row0, 32u), col, width - col, v, s.align,
-                              (uint32_t*)(base + kSmallGram) + warp * kStageWords, kStageRow);
+                store_tile32(out + first, a.out_type, a.ld_out, row0, min(s.m - row0, 32u), col, width, v, s.align,
+                             (uint32_t*)(base + kSmallGram) + warp * kStageWords, false, true);
             } else if (row < s.m) {              // the lanes' rows are the output's neighbouring columns
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
