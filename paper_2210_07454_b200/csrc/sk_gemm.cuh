@@ -1,11 +1,10 @@
-// Matrix products on the tensor cores (tcgen05), for the operators whose epilogues differ: one kernel, templated on the
-// tile and on what happens to a finished tile.
+// Matrix products on the tensor cores (tcgen05), for the operators whose epilogues and schedules differ: one kernel, templated on
+// the tile, on the plan that says which tiles there are, and on what happens to a finished tile.
 //
-//   D[b][i][j] = sum_p sum_k  A_p[b](i, k) * B_p[b](j, k)      p = 0 .. passes-1, 16-bit operands, 32-bit sums
+//   D(i, j) = sum_k A(i, k) * B(j, k)      16-bit operands, 32-bit sums
 //
 // Each operand may be stored with k contiguous ("K-major") or with its row index contiguous ("MN-major"); no operand is
-// ever transposed in memory.  Two passes add a second pair of operands into the same accumulator (a matrix held as the
-// sum of two 16-bit matrices).
+// ever transposed in memory.  A tile may go over two pairs of operands (a matrix held as the sum of two 16-bit matrices).
 //
 // A block (CG = 1) or a pair of blocks on two SMs (CG = 2) works on one output tile of 128*CG rows by BN columns at a
 // time and walks over tiles until none is left.  One warp feeds a ring of kStages shared-memory stages by TMA (64 values of k a
@@ -31,32 +30,20 @@ constexpr uint32_t kOpWait = 1u;              // status word of the operators: a
 constexpr int kGemmK = 64;                    // values of k per stage: 128 bytes, the width of the swizzle
 constexpr int kEpiWarps = 8;
 constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
-constexpr int kStageWords = 1024;             // of shared memory for each epilogue warp (store_tile32)
+constexpr int kStageWords = 1024;             // of shared memory that store_tile32 needs, for each epilogue warp
 
-// One product of a launch.
-struct GemmGroup {
-    uint32_t M, N;                            // output extents
-    uint32_t k_blocks;                        // stages per tile and pass (the last one zero-filled beyond K)
-    uint32_t k_total;                         // stages along K: more than k_blocks where K is split
-    uint32_t passes;                          // 1 or 2
-    uint32_t batch;                           // matrices, or slices of K
-    uint32_t sliced;                          // 1: `batch` counts slices of K of one matrix
-    uint32_t tiles_m, tiles_n;
-    uint32_t band;                            // tiles are walked in bands of this many tile rows, row index fastest
-    uint32_t symmetric;                       // 1: only tiles on and below the diagonal; the epilogue mirrors them
-    uint32_t tiles;                           // total over the batch
+// What the kernel's roles have to know of a tile.
+struct TileJob {
+    uint32_t M, N;                            // extents of the output
+    uint32_t m, n, b;                         // the tile: row, column, matrix (or slice of K)
+    uint32_t kind, step;                      // which product: for the epilogue
+    uint32_t k_stages, pass;                  // stages; the first `pass` of them over a and b, the others over a2 and b2
+    int k_first, z;                           // first k, matrix of the operands
     uint32_t a_mn, b_mn;                      // 1: MN-major
     uint32_t a_rows;                          // rows of A a block loads: 128, or fewer where a single tile row has no more
     uint32_t k_rows;                          // values of k in a stage: 64, or fewer where K has no more (in steps of 16)
     uint32_t bf16;                            // operand type: 1 bf16, 0 fp16
-};
-// A launch: one product, or two that do not depend on each other (the second with map_a2, map_b2 as its operands), the one with
-// the longer tiles first.  Each of the `units` (blocks or pairs) takes the first's tiles in turn; `early` is how many rounds of
-// the second's tiles the units that got one tile less of the first are ahead.
-struct GemmShape {
-    GemmGroup g[2];
-    uint32_t groups, early;
-    uint32_t* status;
+    const CUtensorMap *map_a, *map_b, *map_a2, *map_b2;
 };
 
 // ---- instruction wrappers -------------------------------------------------------------------------------------------
@@ -173,69 +160,85 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t b
     return (uint64_t)((addr & 0x3FFFFu) >> 4) | (lead << 16) | ((uint64_t)(1024u >> 4) << 32) | (1ull << 46) | (2ull << 61);
 }
 
-// ---- which tile ------------------------------------------------------------------------------------------------------
-struct TileAt { uint32_t group, b, m, n; };
-__device__ __forceinline__ TileAt tile_at(const GemmGroup& g, uint32_t group, uint32_t t) {
-    TileAt r;
-    r.group = group;
-    if (g.symmetric) {
-        const uint32_t per = g.tiles_m * (g.tiles_m + 1) / 2;
-        r.b = t / per;
-        const uint32_t q = t - r.b * per;
-        uint32_t i = (uint32_t)((sqrtf(8.0f * (float)q + 1.0f) - 1.0f) * 0.5f);
-        while (i * (i + 1) / 2 > q) --i;
-        while ((i + 1) * (i + 2) / 2 <= q) ++i;
-        r.m = i;
-        r.n = q - i * (i + 1) / 2;
-        return r;
-    }
-    const uint32_t per = g.tiles_m * g.tiles_n;
-    r.b = t / per;
-    uint32_t q = t - r.b * per;
-    const uint32_t band = q / (g.band * g.tiles_n);
-    q -= band * g.band * g.tiles_n;
-    const uint32_t rows = min(g.band, g.tiles_m - band * g.band);
-    r.n = q / rows;
-    r.m = band * g.band + (q - r.n * rows);
-    return r;
-}
-// The i-th tile of unit p of `units`; false when it has no more.
-__device__ __forceinline__ bool tile_of(const GemmShape& s, uint32_t p, uint32_t units, uint32_t i, TileAt& at) {
-    uint32_t t = p + i * units;
-    if (t < s.g[0].tiles) {
-        at = tile_at(s.g[0], 0, t);
+// ---- one product, or two that do not depend on each other ---------------------------------------------------------------
+struct GemmGroup {
+    uint32_t M, N;                            // output extents
+    uint32_t k_blocks, k_total;               // stages per tile, and along K: more where K is split
+    uint32_t slices;                          // of K: slice s writes a result of its own
+    uint32_t tiles_m, tiles_n, tiles;
+    uint32_t band;                            // tiles are walked in bands of this many tile rows, row index fastest
+    uint32_t a_mn, b_mn, a_rows, k_rows, bf16;
+};
+// The product with the longer tiles is the first.  Each of the `units` (blocks or pairs) takes the first's tiles in turn; `early` is how
+// many rounds of the second's tiles the units that got one tile less of the first are ahead.
+struct GemmPlan {
+    CUtensorMap map[4];                       // A and B of the first, of the second
+    GemmGroup g[2];
+    uint32_t groups, early;
+    uint32_t* status;
+    static constexpr bool kCooperative = false;
+
+    __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, TileJob& j) const {
+        uint32_t t = p + i * units, group = 0;
+        if (t >= g[0].tiles) {
+            if (groups < 2) return false;
+            group = 1;
+            const uint32_t q = g[0].tiles / units, r = g[0].tiles - q * units;   // units below r had q + 1 tiles, the others q
+            const uint32_t k = i - (q + (p < r)), head = early * (units - r);
+            if (p >= r) t = k < early ? k * (units - r) + (p - r) : head + (k - early) * units + p;
+            else t = head + k * units + p;
+            if (t >= g[1].tiles) return false;
+        }
+        const GemmGroup& s = g[group];
+        const uint32_t per = s.tiles_m * s.tiles_n;
+        j.b = t / per;
+        uint32_t q = t - j.b * per;
+        const uint32_t band = q / (s.band * s.tiles_n);
+        q -= band * s.band * s.tiles_n;
+        const uint32_t rows = min(s.band, s.tiles_m - band * s.band);
+        j.n = q / rows;
+        j.m = band * s.band + (q - j.n * rows);
+        j.M = s.M;
+        j.N = s.N;
+        j.kind = group;
+        j.step = 0;
+        j.k_stages = j.pass = min(s.k_blocks, s.k_total - j.b * s.k_blocks);
+        j.k_first = (int)(j.b * s.k_blocks * kGemmK);
+        j.z = 0;
+        j.a_mn = s.a_mn;
+        j.b_mn = s.b_mn;
+        j.a_rows = s.a_rows;
+        j.k_rows = s.k_rows;
+        j.bf16 = s.bf16;
+        j.map_a = j.map_a2 = &map[2 * group];
+        j.map_b = j.map_b2 = &map[2 * group + 1];
         return true;
     }
-    if (s.groups < 2) return false;
-    const uint32_t q = s.g[0].tiles / units, r = s.g[0].tiles - q * units;       // units below r had q + 1 tiles, the others q
-    const uint32_t j = i - (q + (p < r));
-    const uint32_t head = s.early * (units - r);
-    if (p >= r) t = j < s.early ? j * (units - r) + (p - r) : head + (j - s.early) * units + p;
-    else t = head + j * units + p;
-    if (t >= s.g[1].tiles) return false;
-    at = tile_at(s.g[1], 1, t);
-    return true;
-}
-__device__ __forceinline__ uint32_t stages_of(const GemmGroup& g, const TileAt& at) {
-    return g.sliced ? min(g.k_blocks, g.k_total - at.b * g.k_blocks) : g.k_blocks * g.passes;
-}
-
-template <int CG, int BN>
-struct GemmTile {
-    static constexpr int kStageBytes = 128 * 128 + (BN / CG) * 128;      // both operands, 64 values of k
-    static constexpr int kStages = BN / CG >= 256 ? 4 : 6;                            // as many as fit
-    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * kStageWords * 4 + 1024;      // + the epilogue's, + alignment
+    __device__ __forceinline__ bool wait(const TileJob&) const { return true; }
+    __device__ __forceinline__ void done(const TileJob&) const {}
+    __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i < 2 * groups ? &map[i] : nullptr; }
 };
 
-// Epi: struct Args; __device__ Epi(const Args&, group, tile, row, first column, half, the warp's shared memory);
-// chunk(col, v[32], last); end().  A thread holds one row of the tile and gets its columns 32 at a time; the two warps that share a row take half
-// the columns each.  Rows >= M are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
-template <int CG, int BN, class Epi>
+// words: of shared memory for each epilogue warp.  The ring takes what is left of the 227 KB, six stages of 32 KB beside 4 KB a warp: two would cover
+// the 1600 cycles from a copy's issue to its arrival, more even out the waits.
+template <int CG, int BN, int words>
+struct GemmTile {
+    static constexpr int kStageBytes = 128 * 128 + (BN / CG) * 128;      // both operands, 64 values of k
+    static constexpr int kFixed = kEpiWarps * words * 4 + 1024 + 512;    // the epilogue's, alignment of the swizzle, barriers
+    static constexpr int kStages = (232448 - kFixed) / kStageBytes;
+    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * words * 4 + 1024;
+};
+
+// Plan: job(unit, units, i, job): the unit's i-th tile; wait(job): until its operands are there; done(job): called by every epilogue warp
+// when its share of the tile is written.
+// Epi: struct Args; __device__ Epi(const Args&, job, row, half, the warp's shared memory); begin(plan, first column) before the
+// accumulator is waited for; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
+// row of the tile and gets its columns 32 at a time; the two warps that share a row take half the columns each.  Rows >= M
+// are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
+template <int CG, int BN, class Plan, class Epi>
 __global__ void __launch_bounds__(kGemmThreads, 1)
-k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-       const __grid_constant__ CUtensorMap map_a2, const __grid_constant__ CUtensorMap map_b2,
-       const __grid_constant__ GemmShape shape, const __grid_constant__ typename Epi::Args ea) {
-    constexpr int kStages = GemmTile<CG, BN>::kStages;
+k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::Args ea) {
+    constexpr int kStages = GemmTile<CG, BN, Epi::kWords>::kStages;
     constexpr int kRowsB = BN / CG;
     constexpr int kBytesA = 128 * 128, kBytesB = kRowsB * 128;
     constexpr uint32_t kTmemCols = 2 * BN;                       // a power of two >= 32
@@ -263,9 +266,9 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
     if constexpr (CG == 2) cluster_sync_all();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *(volatile uint32_t*)&tmem_slot;
-    if (threadIdx.x < 4) {                                       // the descriptors depend on no other kernel
-        const CUtensorMap* m = threadIdx.x == 0 ? &map_a : threadIdx.x == 1 ? &map_b : threadIdx.x == 2 ? &map_a2 : &map_b2;
-        asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
+    if (threadIdx.x < 8) {                                       // the descriptors depend on no other kernel
+        const CUtensorMap* m = plan.descriptor(threadIdx.x);
+        if (m) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
     }
 
     chain_acquire();
@@ -273,7 +276,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
     chain_release();
 
     const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG;
-    TileAt at;
+    TileJob t;
 
     // The two single threads that feed the tensor cores have a stage's time, some 600 cycles, for each trip of their loops: what is constant
     // over a tile is in registers, and the ring's slot and its parity go round without divisions.
@@ -282,25 +285,24 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
         if (lane == 0) {
             uint32_t s = 0, parity = 1;                          // a fresh barrier counts as having completed its previous phase
             bool ok = true, any = false;
-            for (uint32_t i = 0; ok && tile_of(shape, unit, units, i, at); ++i) {
-                const GemmGroup& g = shape.g[at.group];
-                const uint32_t kb = stages_of(g, at), pass = g.k_blocks;
-                const bool a_mn = g.a_mn, b_mn = g.b_mn, grouped = at.group != 0;
-                const int z = g.sliced ? 0 : (int)at.b, k_first = g.sliced ? (int)(at.b * g.k_blocks * kGemmK) : 0;
-                const int row_a = (int)(at.m * (128 * CG) + rank * 128);
-                const int row_b = (int)(at.n * BN + rank * kRowsB);
-                const uint32_t bytes = CG * 128 * ((a_mn ? 2 * g.k_rows : g.a_rows) + (b_mn ? kRowsB / 64 * g.k_rows : kRowsB));
-                const CUtensorMap* ma = grouped ? &map_a2 : &map_a;
-                const CUtensorMap* mb = grouped ? &map_b2 : &map_b;
-                int k0 = k_first;
+            for (uint32_t i = 0; ok && plan.job(unit, units, i, t); ++i) {
+                if (!(ok = plan.wait(t))) break;
+                const uint32_t kb = t.k_stages, pass = t.pass;
+                const bool a_mn = t.a_mn, b_mn = t.b_mn;
+                const int z = t.z;
+                const int row_a = (int)(t.m * (128 * CG) + rank * 128);
+                const int row_b = (int)(t.n * BN + rank * kRowsB);
+                const uint32_t bytes = CG * 128 * ((a_mn ? 2 * t.k_rows : t.a_rows) + (b_mn ? kRowsB / 64 * t.k_rows : kRowsB));
+                const CUtensorMap *ma = t.map_a, *mb = t.map_b;
+                int k0 = t.k_first;
                 any = true;
                 for (uint32_t k = 0; k < kb; ++k, k0 += kGemmK) {
-                    if (k == pass) {                             // the second pass: the other operands from the start of K
-                        ma = &map_a2;
-                        mb = &map_b2;
-                        k0 = 0;
+                    if (k == pass) {                             // the second pair of operands, from the start of K
+                        ma = t.map_a2;
+                        mb = t.map_b2;
+                        k0 = t.k_first;
                     }
-                    if (!(ok = mbar_wait(empty(s), parity, shape.status))) break;
+                    if (!(ok = mbar_wait(empty(s), parity, plan.status))) break;
                     const uint32_t sa = stages + s * kBytes, sb = sa + kBytesA;
                     uint32_t bar = full(s);
                     if (rank == 0) mbar_expect(bar, bytes);
@@ -323,7 +325,7 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
             // this block's own copies land in its shared memory: all of them are waited for before the block may end
             if (any)
                 for (uint32_t q = 0; q < (uint32_t)kStages; ++q) {
-                    if (!mbar_wait(empty(s), parity, shape.status)) break;
+                    if (!mbar_wait(empty(s), parity, plan.status)) break;
                     if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
                 }
         }
@@ -331,18 +333,17 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
         if (lane == 0 && rank == 0) {
             uint32_t s = 0, parity = 0;
             bool ok = true;
-            for (uint32_t n = 0; ok && tile_of(shape, unit, units, n, at); ++n) {
-                const GemmGroup& g = shape.g[at.group];
-                const uint32_t kb = stages_of(g, at), a = n & 1, steps = g.k_rows / 16, d = tmem + a * BN;
+            for (uint32_t n = 0; ok && plan.job(unit, units, n, t); ++n) {
+                const uint32_t kb = t.k_stages, a = n & 1, steps = t.k_rows / 16, d = tmem + a * BN;
                 // D fp32; A, B bf16 or fp16; majors; N / 8; M / 16
-                const uint32_t idesc = (1u << 4) | (g.bf16 << 7) | (g.bf16 << 10) | (g.a_mn << 15) | (g.b_mn << 16) |
+                const uint32_t idesc = (1u << 4) | (t.bf16 << 7) | (t.bf16 << 10) | (t.a_mn << 15) | (t.b_mn << 16) |
                                        ((uint32_t)(BN / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
-                const uint64_t step_a = (g.a_mn ? 2048u : 32u) >> 4, step_b = (g.b_mn ? 2048u : 32u) >> 4;
-                const uint64_t desc_a = smem_desc(stages, g.a_mn), desc_b = smem_desc(stages + kBytesA, g.b_mn);
-                if (n >= 2 && !(ok = mbar_wait(acc_empty(a), ((n >> 1) - 1) & 1, shape.status))) break;
+                const uint64_t step_a = (t.a_mn ? 2048u : 32u) >> 4, step_b = (t.b_mn ? 2048u : 32u) >> 4;
+                const uint64_t desc_a = smem_desc(stages, t.a_mn), desc_b = smem_desc(stages + kBytesA, t.b_mn);
+                if (n >= 2 && !(ok = mbar_wait(acc_empty(a), ((n >> 1) - 1) & 1, plan.status))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 for (uint32_t k = 0; k < kb; ++k) {
-                    if (!(ok = mbar_wait(full(s), parity, shape.status))) break;
+                    if (!(ok = mbar_wait(full(s), parity, plan.status))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t da = desc_a + s * (kBytes >> 4), db = desc_b + s * (kBytes >> 4);
                     if (steps == kGemmK / 16) {
@@ -359,15 +360,15 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
         }
     } else {
         const uint32_t w = warp - 2, quarter = warp & 3, half = w >> 2;
-        uint32_t* stage = (uint32_t*)(smem_raw + (stages - smem_u32(smem_raw)) + kStages * (kBytesA + kBytesB)) + w * kStageWords;
-        for (uint32_t n = 0; tile_of(shape, unit, units, n, at); ++n) {
-            const GemmGroup& g = shape.g[at.group];
+        uint32_t* stage = (uint32_t*)(smem_raw + (stages - smem_u32(smem_raw)) + kStages * (kBytesA + kBytesB)) + w * Epi::kWords;
+        for (uint32_t n = 0; plan.job(unit, units, n, t); ++n) {
             const uint32_t a = n & 1;
-            if (!mbar_wait(acc_full(a), (n >> 1) & 1, shape.status)) break;
+            const uint32_t row = t.m * (128 * CG) + rank * 128 + quarter * 32 + lane;
+            const uint32_t col0 = t.n * BN + half * (BN / 2);
+            Epi epi(ea, t, row, half, stage);
+            epi.begin(plan, col0);                               // what it reads travels while the products run
+            if (!mbar_wait(acc_full(a), (n >> 1) & 1, plan.status)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            const uint32_t row = at.m * (128 * CG) + rank * 128 + quarter * 32 + lane;
-            const uint32_t col0 = at.n * BN + half * (BN / 2);
-            Epi epi(ea, g, at, row, col0, half, stage);
 #pragma unroll 1
             for (uint32_t c = 0; c < BN / 2; c += 32) {
                 float v[32];
@@ -378,9 +379,10 @@ k_gemm(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtens
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_leader(acc_empty(a)) : acc_empty(a));
                 }
-                if (col0 + c < g.N) epi.chunk(col0 + c, v, c + 32 == BN / 2 || col0 + c + 32 >= g.N);
+                if (col0 + c < t.N) epi.chunk(col0 + c, v, c + 32 == BN / 2 || col0 + c + 32 >= t.N);
             }
             epi.end();
+            plan.done(t);
         }
     }
 
@@ -405,7 +407,47 @@ struct Operand {
 
 bool encode_operand(CUtensorMap* map, const Operand& o, bool bf16, uint32_t box_rows);
 
-// The tile-dependent part of a group.  slices > 1 splits K.
+// Launches a plan on at most `units` blocks or pairs.
+template <int CG, int BN, class Plan, class Epi>
+cudaError_t launch_plan(bool chain, const Plan& plan, const typename Epi::Args& ea, uint32_t units, cudaStream_t st) {
+    auto kernel = k_gemm<CG, BN, Plan, Epi>;
+    static std::atomic<bool> prepared[64];                       // the attribute is a property of the kernel on a device
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    if (device >= 64 || !prepared[device]) {
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmTile<CG, BN, Epi::kWords>::kSmem);
+        if (e != cudaSuccess) return e;
+        if (device < 64) prepared[device] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(units * CG);
+    cfg.blockDim = dim3(kGemmThreads);
+    cfg.dynamicSmemBytes = GemmTile<CG, BN, Epi::kWords>::kSmem;
+    cfg.stream = st;
+    cudaLaunchAttribute attr[2];
+    uint32_t n = 0;
+    if (CG > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = CG;
+        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
+    if (Plan::kCooperative) {                                    // its blocks wait for one another: all of them resident, or an error
+        attr[n].id = cudaLaunchAttributeCooperative;
+        attr[n].val.cooperative = 1;
+        ++n;
+    } else if (chain) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n].val.programmaticStreamSerializationAllowed = 1;
+        ++n;
+    }
+    cfg.attrs = attr;
+    cfg.numAttrs = n;
+    return cudaLaunchKernelEx(&cfg, kernel, plan, ea);
+}
+
+// The tile-dependent part of a product.  slices > 1 splits K.
 template <int CG, int BN>
 void set_tiles(GemmGroup& g, const Operand& a, const Operand& b, uint32_t slices) {
     g.a_mn = a.mn;
@@ -413,18 +455,14 @@ void set_tiles(GemmGroup& g, const Operand& a, const Operand& b, uint32_t slices
     const uint64_t K = a.mn ? a.rows : a.cols;
     g.k_total = (uint32_t)((K + kGemmK - 1) / kGemmK);
     g.k_rows = K < kGemmK ? (uint32_t)((K + 15) / 16 * 16) : kGemmK;
-    g.k_blocks = g.k_total;
-    if (slices > 1) {
-        g.k_blocks = (g.k_total + slices - 1) / slices;
-        g.batch = (g.k_total + g.k_blocks - 1) / g.k_blocks;          // no empty slice, and never more than asked for
-        g.sliced = 1;
-    }
+    g.k_blocks = (g.k_total + slices - 1) / slices;
+    g.slices = (g.k_total + g.k_blocks - 1) / g.k_blocks;            // no empty slice, and never more than asked for
     g.tiles_m = (g.M + 128 * CG - 1) / (128 * CG);
     g.tiles_n = (g.N + BN - 1) / BN;
+    g.tiles = g.slices * g.tiles_m * g.tiles_n;
     // The rest of the stage's rows stay what they were and give sums that nobody reads.  Loading them as zeros is not free: 8 tokens
     // against 128,000 x 4096 took 285 us so, and takes 186 us without (reading the matrix alone 172).
     g.a_rows = CG == 1 && !g.a_mn && g.M < 128 ? (g.M + 7) / 8 * 8 : 128;
-    g.tiles = g.batch * (g.symmetric ? g.tiles_m * (g.tiles_m + 1) / 2 : g.tiles_m * g.tiles_n);
     // Tiles that run at the same time share operands through L2.  Where A is the smaller operand and fits, its whole height is walked
     // first, so that B is read once; where B is, a band is just high enough for the SMs to span the width: A is read
     // once and whole rows of D are written together.
@@ -435,105 +473,46 @@ void set_tiles(GemmGroup& g, const Operand& a, const Operand& b, uint32_t slices
     g.band = band < g.tiles_m ? band : g.tiles_m;
 }
 
-// a2, b2: the second pass's operands, or with groups = 2 the second product's.
-template <int CG, int BN, class Epi>
-cudaError_t launch_gemm(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, const GemmShape& g,
-                        const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
-    const uint32_t tiles = g.g[0].tiles + (g.groups == 2 ? g.g[1].tiles : 0);
-    if (!tiles) return cudaSuccess;
-    CUtensorMap ma, mb, ma2, mb2;
-    const GemmGroup &g0 = g.g[0], &g1 = g.groups == 2 ? g.g[1] : g.g[0];
-    bool ok = encode_operand(&ma, a, g0.bf16, a.mn ? g0.k_rows : g0.a_rows) && encode_operand(&mb, b, g0.bf16, b.mn ? g0.k_rows : BN / CG);
-    if (a2) ok = ok && encode_operand(&ma2, *a2, g1.bf16, a2->mn ? g1.k_rows : g1.a_rows) && encode_operand(&mb2, *b2, g1.bf16, b2->mn ? g1.k_rows : BN / CG);
-    else { ma2 = ma; mb2 = mb; }
-    if (!ok) return cudaErrorInvalidValue;
-    auto kernel = k_gemm<CG, BN, Epi>;
-    static std::atomic<bool> prepared[64];                       // the attribute is a property of the kernel on a device
-    int device = 0;
-    cudaError_t e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return e;
-    if (device >= 64 || !prepared[device]) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmTile<CG, BN>::kSmem);
-        if (e != cudaSuccess) return e;
-        if (device < 64) prepared[device] = true;
-    }
-    const uint32_t slots = (uint32_t)sm_count / CG;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((tiles < slots ? tiles : slots) * CG);
-    cfg.blockDim = dim3(kGemmThreads);
-    cfg.dynamicSmemBytes = GemmTile<CG, BN>::kSmem;
-    cfg.stream = st;
-    cudaLaunchAttribute attr[2];
-    uint32_t n = 0;
-    if (CG > 1) {
-        attr[n].id = cudaLaunchAttributeClusterDimension;
-        attr[n].val.clusterDim.x = CG;
-        attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
-        ++n;
-    }
-    if (chain) {
-        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-        attr[n].val.programmaticStreamSerializationAllowed = 1;
-        ++n;
-    }
-    cfg.attrs = attr;
-    cfg.numAttrs = n;
-    return cudaLaunchKernelEx(&cfg, kernel, ma, mb, ma2, mb2, g, ea);
-}
-
 // What a tile costs beside its stages, in stages (its epilogue where nothing hides it)
 constexpr uint32_t kTileCost = 6;
 
-// Which tile: pairs of blocks on 256 x 256, or single blocks on 128 x 128.  Both take about 620 cycles a stage at an SM, because 32 KB
-// of operands a stage come from L2 at 50 bytes a cycle: measured 617 (pair; its products alone take 512) and 636.  The pair does
-// twice the work per SM in that time; the small tile ends sooner (its epilogue and start take about 7000 cycles, the pair's 12,000, measured
-// with K = 64) and spreads a small product over more SMs.  The one whose last wave ends first wins.
-inline bool wide_tiles(uint32_t M, uint32_t N, uint64_t stages, uint32_t batch, bool symmetric, int sm_count) {
-    auto count = [&](uint32_t t) {
-        const uint64_t m = (M + t - 1) / t, n = (N + t - 1) / t;
-        return batch * (symmetric ? m * (m + 1) / 2 : m * n);
+// One product, or two in one launch with the longer tiles first; slices: K of the first is split into so many.
+template <int CG, int BN, class Epi>
+cudaError_t launch_products(bool chain, const Operand& a, const Operand& b, GemmGroup g0, uint32_t slices, const Operand* a2, const Operand* b2,
+                            const GemmGroup* g1, uint32_t* status, const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
+    GemmPlan p{};
+    set_tiles<CG, BN>(g0, a, b, slices);
+    p.g[0] = g0;
+    p.groups = 1;
+    p.status = status;
+    uint32_t tiles = g0.tiles;
+    auto encode = [&](CUtensorMap* map, const GemmGroup& g, const Operand& x, const Operand& y) {
+        return encode_operand(map, x, g.bf16, x.mn ? g.k_rows : g.a_rows) && encode_operand(map + 1, y, g.bf16, y.mn ? g.k_rows : BN / CG);
     };
+    if (!encode(p.map, g0, a, b)) return cudaErrorInvalidValue;
+    if (g1) {
+        p.g[1] = *g1;
+        set_tiles<CG, BN>(p.g[1], *a2, *b2, 1);
+        p.groups = 2;
+        const uint32_t c0 = g0.k_blocks + kTileCost, c1 = p.g[1].k_blocks + kTileCost;
+        p.early = (c0 + c1 / 2) / c1;
+        tiles += p.g[1].tiles;
+        if (!encode(p.map + 2, p.g[1], *a2, *b2)) return cudaErrorInvalidValue;
+    }
+    const uint32_t slots = (uint32_t)sm_count / CG;
+    return launch_plan<CG, BN, GemmPlan, Epi>(chain, p, ea, tiles < slots ? tiles : slots, st);
+}
+
+// Which tile for a product on its own: pairs of blocks on 256 x 256, or single blocks on 128 x 128.  Both take about 620 cycles a stage
+// at an SM, because 32 KB of operands a stage come from L2 at 50 bytes a cycle: measured 617 (pair; its products alone take 512) and 636.  The
+// pair does twice the work per SM in that time; the small tile ends sooner (its epilogue and start take about 7000 cycles, the pair's
+// 12,000, measured with K = 64) and spreads a small product over more SMs.  The one whose last wave ends first wins.
+inline bool wide_tiles(uint64_t M, uint64_t N, uint64_t stages, int sm_count) {
+    auto count = [&](uint64_t t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
     const uint64_t slots = (uint64_t)sm_count;
     const uint64_t wide = (count(256) + slots / 2 - 1) / (slots / 2) * stages * 620 + 12000;
     const uint64_t small = (count(128) + slots - 1) / slots * stages * 620 + 7000;
     return wide <= small;
-}
-
-// One product; a2, b2: the operands of a second pass into the same sums; slices: K is split into so many.
-template <int CG, int BN, class Epi>
-cudaError_t launch_one(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, GemmGroup g, uint32_t slices,
-                       uint32_t* status, const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
-    GemmShape s{};
-    g.passes = a2 ? 2 : 1;
-    set_tiles<CG, BN>(g, a, b, slices);
-    s.g[0] = g;
-    s.groups = 1;
-    s.status = status;
-    return launch_gemm<CG, BN, Epi>(chain, a, b, a2, b2, s, ea, sm_count, st);
-}
-template <class Epi>
-cudaError_t launch_product(bool chain, const Operand& a, const Operand& b, const Operand* a2, const Operand* b2, const GemmGroup& g, uint32_t* status,
-                           const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
-    const uint64_t stages = ((a.mn ? a.rows : a.cols) + kGemmK - 1) / kGemmK * (a2 ? 2 : 1);
-    if (wide_tiles(g.M, g.N, stages, g.batch, g.symmetric, sm_count)) return launch_one<2, 256, Epi>(chain, a, b, a2, b2, g, 1, status, ea, sm_count, st);
-    return launch_one<1, 128, Epi>(chain, a, b, a2, b2, g, 1, status, ea, sm_count, st);
-}
-
-// Two products in one launch, the longer tiles first; slices: K of the first is split into so many.
-template <int CG, int BN, class Epi>
-cudaError_t launch_two(bool chain, const Operand& a, const Operand& b, GemmGroup g0, uint32_t slices, const Operand& a2, const Operand& b2, GemmGroup g1,
-                       uint32_t* status, const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
-    GemmShape s{};
-    g0.passes = g1.passes = 1;
-    set_tiles<CG, BN>(g0, a, b, slices);
-    set_tiles<CG, BN>(g1, a2, b2, 1);
-    s.g[0] = g0;
-    s.g[1] = g1;
-    s.groups = 2;
-    s.status = status;
-    const uint32_t c0 = g0.k_blocks + kTileCost, c1 = g1.k_blocks + kTileCost;
-    s.early = (c0 + c1 / 2) / c1;
-    return launch_gemm<CG, BN, Epi>(chain, a, b, &a2, &b2, s, ea, sm_count, st);
 }
 
 }  // namespace sk

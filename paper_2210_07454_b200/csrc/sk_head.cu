@@ -26,16 +26,18 @@ __device__ __forceinline__ float exp2_fast(float x) {          // 2^x, 2 ulp
 
 // per (half tile, row): maximum of the logits and the sum of exp(z - maximum)
 struct StatsEpi {
+    static constexpr int kWords = kStageWords;
+    template <class Plan> __device__ void begin(const Plan&, uint32_t) {}
     struct Args { float2* part; float* at_target; const int64_t* targets; };
     const Args& a;
-    const GemmGroup& g;
+    const TileJob& t;
     uint32_t row, slot;
     int64_t target;
     float top = -INFINITY, sum = 0;
-    __device__ StatsEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t half, uint32_t*)
-        : a(a_), g(g_), row(row_), slot(at.n * 2 + half) { target = row < g.M ? a.targets[row] : -1; }
+    __device__ StatsEpi(const Args& a_, const TileJob& t_, uint32_t row_, uint32_t half, uint32_t*)
+        : a(a_), t(t_), row(row_), slot(t_.n * 2 + half) { target = row < t.M ? a.targets[row] : -1; }
     __device__ void chunk(uint32_t col, float (&v)[32], bool) {
-        const uint32_t valid = g.N - col;
+        const uint32_t valid = t.N - col;
         const uint64_t d = (uint64_t)(target - (int64_t)col);
         if (d < 32 && d < valid) {
             float z = v[0];
@@ -60,7 +62,7 @@ struct StatsEpi {
         for (int i = 0; i < 32; ++i) sum += exp2_fast((v[i] - off) * kLog2e);
     }
     __device__ void end() {
-        if (row < g.M) a.part[(uint64_t)slot * g.M + row] = make_float2(top, sum);
+        if (row < t.M) a.part[(uint64_t)slot * t.M + row] = make_float2(top, sum);
     }
 };
 
@@ -110,20 +112,22 @@ __global__ void __launch_bounds__(kJoinThreads) k_head_join(const float2* part, 
 
 // G's piece
 struct GradEpi {
+    static constexpr int kWords = kStageWords;
+    template <class Plan> __device__ void begin(const Plan&, uint32_t) {}
     struct Args { uint16_t* out; uint64_t ld; const float *lse, *dloss, *factor; const int64_t* targets; uint64_t vocab; uint32_t first; };
     const Args& a;
-    const GemmGroup& g;
+    const TileJob& t;
     uint32_t row0, rows;
     uint32_t* stage;
     float off = 0, scale = 0;
     int64_t target = -1;
-    __device__ GradEpi(const Args& a_, const GemmGroup& g_, const TileAt&, uint32_t row, uint32_t, uint32_t, uint32_t* stage_)
-        : a(a_), g(g_), row0(row - (threadIdx.x & 31)), stage(stage_) {
-        rows = row0 >= g.M ? 0 : g.M - row0 < 32 ? g.M - row0 : 32;
-        if (row < g.M) {
-            const int64_t t = a.targets[row];
-            if (t >= 0 && t < (int64_t)a.vocab) {
-                target = t - (int64_t)a.first;
+    __device__ GradEpi(const Args& a_, const TileJob& t_, uint32_t row, uint32_t, uint32_t* stage_)
+        : a(a_), t(t_), row0(row - (threadIdx.x & 31)), stage(stage_) {
+        rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32;
+        if (row < t.M) {
+            const int64_t v = a.targets[row];
+            if (v >= 0 && v < (int64_t)a.vocab) {
+                target = v - (int64_t)a.first;
                 scale = a.dloss[row] * (a.factor ? *a.factor : 1.0f);
                 off = a.lse[row];
             }
@@ -146,7 +150,7 @@ struct GradEpi {
             for (int i = 0; i < 32; ++i) v[i] = 0.0f;
         }
         __syncwarp();
-        store_tile32(a.out, g.bf16 ? SK_BF16 : SK_F16, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage, true, last);
+        store_tile32(a.out, t.bf16 ? SK_BF16 : SK_F16, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage, true, last);
     }
     __device__ void end() {}
 };
@@ -154,25 +158,27 @@ struct GradEpi {
 // One of two products, by the group: rows of dW, or a share of dhidden.  Shares of more than one piece or slice are added up in 32
 // bits, a slice of K in a matrix of its own (`sum`, one after the other), and joined by k_head_sum.
 struct OutEpi {
+    static constexpr int kWords = kStageWords;
+    template <class Plan> __device__ void begin(const Plan&, uint32_t) {}
     struct One { void* out; float* sum; uint64_t ld, sum_stride; int type; uint32_t align, add; };
     struct Args { One o[2]; const float* factor; };
     const One& a;
-    const GemmGroup& g;
+    const TileJob& t;
     float* sum;
     uint32_t row0, rows;
     uint32_t* stage;
     float scale;
-    __device__ OutEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row, uint32_t, uint32_t, uint32_t* stage_)
-        : a(a_.o[at.group]), g(g_), sum(a.sum ? a.sum + at.b * a.sum_stride : nullptr), row0(row - (threadIdx.x & 31)), stage(stage_),
+    __device__ OutEpi(const Args& a_, const TileJob& t_, uint32_t row, uint32_t, uint32_t* stage_)
+        : a(a_.o[t_.kind]), t(t_), sum(a.sum ? a.sum + t_.b * a.sum_stride : nullptr), row0(row - (threadIdx.x & 31)), stage(stage_),
           scale(a_.factor ? 1.0f / *a_.factor : 1.0f) {
-        rows = row0 >= g.M ? 0 : g.M - row0 < 32 ? g.M - row0 : 32;
+        rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32;
     }
     __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (!rows) return;
         if (!sum) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] *= scale;
-            store_tile32(a.out, a.type, a.ld, row0, rows, col, g.N, v, a.align, stage, true, last);
+            store_tile32(a.out, a.type, a.ld, row0, rows, col, t.N, v, a.align, stage, true, last);
             return;
         }
         const uint32_t lane = threadIdx.x & 31;
@@ -374,13 +380,12 @@ int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
     GemmGroup g{};
     g.M = (uint32_t)a.tokens;
     g.N = (uint32_t)a.vocab;
-    g.batch = 1;
     g.bf16 = a.type == SK_BF16;
     const StatsEpi::Args ea{(float2*)(ws + l.off_part), (float*)(ws + l.off_target), a.targets};
     const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{w, a.vocab, a.width, ld_w, 0, 1, false};
-    const bool wide = wide_tiles(g.M, g.N, (a.width + kGemmK - 1) / kGemmK, 1, false, dev.sm_count);
-    if (wide) SK_OP_CUDA((launch_one<2, 256, StatsEpi>(true, oh, ow, nullptr, nullptr, g, 1, dev.status, ea, dev.sm_count, st)));
-    else SK_OP_CUDA((launch_one<1, 128, StatsEpi>(true, oh, ow, nullptr, nullptr, g, 1, dev.status, ea, dev.sm_count, st)));
+    const bool wide = wide_tiles(g.M, g.N, (a.width + kGemmK - 1) / kGemmK, dev.sm_count);
+    auto launch = wide ? launch_products<2, 256, StatsEpi> : launch_products<1, 128, StatsEpi>;
+    SK_OP_CUDA(launch(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.status, ea, dev.sm_count, st));
     const uint32_t tile = wide ? 256 : 128, slots = 2 * ((g.N + tile - 1) / tile);
     SK_OP_CUDA(launch_kernel(true, k_head_join, dim3((g.M + 7) / 8), kJoinThreads, 0, st, (const float2*)ea.part, (const float*)ea.at_target, a.targets, g.M,
                              a.vocab, slots, a.loss, a.lse));
@@ -407,12 +412,12 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
         const uint16_t* wp = (const uint16_t*)w + v0 * ld_w;
         const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{wp, n, a.width, ld_w, 0, 1, false};
         GemmGroup g{};
-        g.batch = 1;
-        g.bf16 = a.type == SK_BF16;
+            g.bf16 = a.type == SK_BF16;
         g.M = tokens;
         g.N = n;
         const GradEpi::Args ga{gbuf, l.ld_g, a.lse, a.dloss, factor, a.targets, a.vocab, (uint32_t)v0};
-        SK_OP_CUDA(launch_product<GradEpi>(true, oh, ow, nullptr, nullptr, g, dev.status, ga, dev.sm_count, st));
+        auto launch_g = wide_tiles(tokens, n, (a.width + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_products<2, 256, GradEpi> : launch_products<1, 128, GradEpi>;
+        SK_OP_CUDA(launch_g(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.status, ga, dev.sm_count, st));
         // dW[v] = sum over tokens of G[t][v] hidden[t]: both factors with their rows contiguous;
         // dhidden[t] += sum over the piece of G[t][v] W[v]
         const Operand gt{gbuf, a.tokens, n, l.ld_g, 0, 1, true}, ht{h, a.tokens, a.width, ld_h, 0, 1, true};
@@ -436,19 +441,11 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
         const bool h_first = n >= tokens;                // the one with the longer K is the first
         const uint32_t split = h_first ? l.slices : 1;   // of dhidden's product, when it is the first
         OutEpi::Args ea{{h_first ? one_h : one_w, h_first ? one_w : one_h}, factor};
-        if (a.dweight && a.dhidden) {
-            const Operand &a0 = h_first ? og : gt, &b0 = h_first ? wt : ht, &a1 = h_first ? gt : og, &b1 = h_first ? ht : wt;
-            const GemmGroup &g0 = h_first ? gh : gw, &g1 = h_first ? gw : gh;
-            SK_OP_CUDA(l.wide ? launch_two<2, 256, OutEpi>(true, a0, b0, g0, split, a1, b1, g1, dev.status, ea, dev.sm_count, st)
-                              : launch_two<1, 256, OutEpi>(true, a0, b0, g0, split, a1, b1, g1, dev.status, ea, dev.sm_count, st));
-        } else {
-            const Operand &a0 = a.dhidden ? og : gt, &b0 = a.dhidden ? wt : ht;
-            const GemmGroup& g0 = a.dhidden ? gh : gw;
-            const uint32_t parts = a.dhidden ? split : 1;
-            ea.o[0] = a.dhidden ? one_h : one_w;
-            SK_OP_CUDA(l.wide ? launch_one<2, 256, OutEpi>(true, a0, b0, nullptr, nullptr, g0, parts, dev.status, ea, dev.sm_count, st)
-                              : launch_one<1, 256, OutEpi>(true, a0, b0, nullptr, nullptr, g0, parts, dev.status, ea, dev.sm_count, st));
-        }
+        auto launch = l.wide ? launch_products<2, 256, OutEpi> : launch_products<1, 256, OutEpi>;
+        const bool both = a.dweight && a.dhidden, h_is_0 = both ? h_first : a.dhidden != nullptr;
+        if (!both) ea.o[0] = h_is_0 ? one_h : one_w;
+        SK_OP_CUDA(launch(true, h_is_0 ? og : gt, h_is_0 ? wt : ht, h_is_0 ? gh : gw, h_is_0 ? split : 1, h_is_0 ? &gt : &og, h_is_0 ? &ht : &wt,
+                          both ? (h_is_0 ? &gw : &gh) : nullptr, dev.status, ea, dev.sm_count, st));
     }
     if (sum) {
         const uint64_t want = (a.tokens * ((width + 3) / 4) + 255) / 256, most = (uint64_t)dev.sm_count * 8;

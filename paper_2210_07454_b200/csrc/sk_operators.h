@@ -79,7 +79,10 @@ inline uint32_t row_alignment(const void* p, uint64_t ld, int type) {
 // chunks swizzled), so that neighbouring lanes write neighbouring addresses: whole 128-byte lines, two calls of 16-bit values
 // together (pair; last: no second one follows).  Lanes writing 32 bytes of a row each took 5900 cycles for 128 x 256, about as much as a
 // product over 600 values of k.  All lanes take part.
-__device__ __forceinline__ uint8_t* staged(uint32_t* stage, uint32_t r, uint32_t chunk) { return (uint8_t*)stage + r * 128 + ((chunk ^ (r & 7)) << 4); }
+// (The swizzle's key differs within any eight neighbouring rows, and within four rows eight apart, which a reader of columns takes.)
+__device__ __forceinline__ uint8_t* staged(uint32_t* stage, uint32_t r, uint32_t chunk) {
+    return (uint8_t*)stage + r * 128 + ((chunk ^ ((r ^ (r >> 3)) & 7)) << 4);
+}
 __device__ __forceinline__ void store_tile32(void* out, int type, uint64_t ld, uint64_t row0, uint32_t rows, uint32_t col, uint32_t limit,
                                              const float (&v)[32], uint32_t align, uint32_t* stage, bool pair, bool last) {
     const bool wide = type == SK_F32;            // 32 columns are whole lines already

@@ -26,101 +26,205 @@ namespace {
 constexpr float kScale = 4096.0f, kUnscale = 1.0f / 4096.0f;     // 2^12
 constexpr uint32_t kPadCols = 32;                                // leading dimensions: whole 32-column chunks
 
-// A = X X^T, tiles on and below the diagonal, mirrored
-struct GramEpi {
-    struct Args { __half* out; uint64_t stride; uint32_t ld; const float* factor; };
-    const Args& a;
-    const GemmGroup& g;
-    __half* out;
-    uint32_t row, row0;                          // the lane's, the warp's first
-    uint32_t* stage;
-    bool mirror;
-    float scale = kUnscale;
-    __device__ GramEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t, uint32_t* stage_)
-        : a(a_), g(g_), out(a_.out + at.b * a_.stride), row(row_), row0(row_ - (threadIdx.x & 31)), stage(stage_), mirror(at.m != at.n) {
-        if (a.factor) scale *= a.factor[at.b] * a.factor[at.b];
-    }
-    __device__ void put(uint32_t col, float (&v)[32], bool last) {
-        if (row0 >= g.M) return;
-        const uint32_t rows = g.M - row0 < 32 ? g.M - row0 : 32;
-        store_tile32(out, SK_F16, a.ld, row0, rows, col, a.ld, v, 16, stage, !mirror, last);
-        if (!mirror) return;
-        // the block transposed: a lane's values are a column of it; four lanes write a row of the mirror image
-        const uint32_t lane = threadIdx.x & 31, c = lane & 3;
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 32; ++i) ((__half*)stage)[i * 32 + lane] = __float2half_rn(v[i]);
-        __syncwarp();
-#pragma unroll
-        for (uint32_t r = lane >> 2; r < 32; r += 8)
-            if (col + r < g.N) *(uint4*)(out + (uint64_t)(col + r) * a.ld + row0 + 8 * c) = ((const uint4*)stage)[r * 4 + c];
-    }
-    __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
-#pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= scale;
-        put(col, v, last);
-    }
-    __device__ void end() {}
-};
+// ---- all products of the iteration in one launch --------------------------------------------------------------------------
+// The tiles of A = X X^T (0), P = a I + b A + c A^2 (1) and X <- P X (2) of all steps and matrices, in this order, dealt out to the units in
+// turn.  A tile may start when all tiles of the products before it of ITS matrix are written: a counter per matrix says how many epilogue
+// warps have written theirs.  Waiting for a matrix instead of for everything keeps the units busy across the products' ends: with a
+// launch per product 12 matrices of 768 x 768 took 282 us (108 tiles of X on 74 pairs are two waves, and every launch costs some 4 us).
+// A unit takes its tiles in order, every tile waits for earlier ones only, and the blocks are all resident (a cooperative launch): so the waits
+// end; they have a limit all the same.
+struct ChainPlan {
+    CUtensorMap gram_x[2], apply_hi[2], apply_lo[2], gram, poly;     // [2]: the two buffers that X alternates between
+    uint32_t steps, exact, tall, batch;
+    uint32_t m, rows, cols;                      // shorter side; X's extents
+    uint32_t side, square;                       // tile rows of A, its tiles on and below the diagonal
+    uint32_t tiles_m, tiles_n, apply;            // of X
+    uint32_t k_gram, k_poly;                     // stages along the longer and the shorter side
+    uint32_t signals;                            // of every tile: its epilogue warps
+    uint32_t* count;                             // per matrix, zero before the launch
+    uint32_t* status;
+    static constexpr bool kCooperative = true;
 
-// P = a I + b A + c A^2, likewise
-struct PolyEpi {
-    struct Args { GramEpi::Args o; const __half* gram; float a, b, c; };
-    const Args& p;
-    GramEpi e;
-    const __half* gram;
-    __device__ PolyEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t c0, uint32_t half, uint32_t* stage_)
-        : p(a_), e(a_.o, g_, at, row_, c0, half, stage_), gram(a_.gram + at.b * a_.o.stride) {}
-    __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
-        if (e.row < e.g.M) {
-            uint32_t r[16];
-            const __half* src = gram + (uint64_t)e.row * p.o.ld + col;
-            load32b(src, r);
-            load32b(src + 16, r + 8);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const float2 f = __half22float2(*(const __half2*)&r[i]);
-                v[2 * i] = p.b * f.x + p.c * kUnscale * v[2 * i];
-                v[2 * i + 1] = p.b * f.y + p.c * kUnscale * v[2 * i + 1];
-            }
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (col + i == e.row) v[i] += p.a * kScale;
+    // X is the sum of two matrices in all but the last two steps, and in the first where one is exact
+    __host__ __device__ bool pair(uint32_t step) const { return step + 2 < steps && !(step == 0 && exact); }
+    __device__ __forceinline__ uint32_t before(const TileJob& j) const {
+        return (j.step * (2 * square + apply) + j.kind * square) * signals;
+    }
+    __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, TileJob& j) const {
+        const uint32_t per = batch * (2 * square + apply), t = p + i * units;
+        j.step = t / per;
+        if (j.step >= steps) return false;
+        uint32_t q = t - j.step * per;
+        const uint32_t from = j.step & 1;
+        j.kind = q < batch * square ? 0 : q < 2 * batch * square ? 1 : 2;
+        q -= j.kind * batch * square;
+        j.k_first = 0;
+        j.a_rows = 128;
+        j.k_rows = kGemmK;
+        j.bf16 = 0;
+        if (j.kind < 2) {
+            j.b = q / square;
+            q -= j.b * square;
+            uint32_t r = (uint32_t)((sqrtf(8.0f * (float)q + 1.0f) - 1.0f) * 0.5f);
+            while (r * (r + 1) / 2 > q) --r;
+            while ((r + 1) * (r + 2) / 2 <= q) ++r;
+            j.m = r;
+            j.n = q - r * (r + 1) / 2;
+            j.M = j.N = m;
+            j.a_mn = j.b_mn = j.kind == 0 && tall;
+            j.k_stages = j.pass = j.kind == 0 ? k_gram : k_poly;
+            j.map_a = j.map_b = j.map_a2 = j.map_b2 = j.kind == 0 ? &gram_x[from] : &gram;
+        } else {
+            j.b = q / apply;
+            q -= j.b * apply;
+            const uint32_t band = q / (8 * tiles_n), high = min(8u, tiles_m - band * 8);
+            q -= band * 8 * tiles_n;
+            j.n = q / high;
+            j.m = band * 8 + (q - j.n * high);
+            j.M = rows;
+            j.N = cols;
+            // X with its columns contiguous is the K-major first factor of X P, and the MN-major second one of P X
+            j.a_mn = 0;
+            j.b_mn = !tall;
+            j.pass = k_poly;
+            j.k_stages = pair(j.step) ? 2 * k_poly : k_poly;
+            j.map_a = tall ? &apply_hi[from] : &poly;
+            j.map_b = tall ? &poly : &apply_hi[from];
+            j.map_a2 = tall ? &apply_lo[from] : &poly;
+            j.map_b2 = tall ? &poly : &apply_lo[from];
         }
-        __syncwarp();
-        e.put(col, v, last);
+        j.z = (int)j.b;
+        return true;
     }
-    __device__ void end() {}
+    __device__ __forceinline__ bool wait(const TileJob& j) const {
+        const uint32_t need = before(j);
+        if (!need) return true;
+        for (uint32_t i = 0; i < kWaitTries; ++i) {
+            uint32_t have;
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(have) : "l"(count + j.b) : "memory");
+            if (have >= need) {
+                asm volatile("fence.proxy.async;" ::: "memory");     // what was written by stores is read by TMA
+                return true;
+            }
+        }
+        atomicOr(status, kOpWait);
+        return false;
+    }
+    __device__ __forceinline__ void done(const TileJob& j) const {
+        __syncwarp();
+        if ((threadIdx.x & 31) == 0) {
+            __threadfence();
+            atomicAdd(count + j.b, 1u);
+        }
+    }
+    __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return &gram_x[0] + i; }
 };
 
-// X <- P X: one fp16 matrix, or two whose sum it is; the last step writes the result in the caller's type and layout
-struct ApplyEpi {
-    struct Args { __half *hi, *lo; void* out; uint64_t stride; uint64_t ld; int type; uint32_t align; const float* factor; };
-    const Args& a;
-    const GemmGroup& g;
-    uint64_t first;
-    uint32_t row0, rows;
+// The epilogues of the three products.  A warp has two areas of staging memory: one for the lines of the matrix it writes, one for those of the second
+// matrix of a pair, or for A's lines on their way to P, which are fetched while the products run.
+struct ChainEpi {
+    static constexpr int kWords = 2 * kStageWords;
+    struct Args {
+        __half *gram, *poly, *hi[2], *lo[2];     // [2]: as the plan's
+        uint64_t a_stride, x_stride;
+        uint32_t ld_a, ld_x;
+        float a, b, c;
+        const float* factor;                     // per matrix: the first step's X = factor * (the matrix that is stored)
+        void* out;                               // the last step's, in the caller's type and layout
+        uint64_t out_stride, ld_out;
+        int out_type;
+        uint32_t align, steps;
+    };
+    const Args& e;
+    const TileJob& t;
+    uint32_t row, row0, rows;                    // the lane's row, the warp's first, how many of the warp's exist
     uint32_t* stage;
     float scale = kUnscale;
-    __device__ ApplyEpi(const Args& a_, const GemmGroup& g_, const TileAt& at, uint32_t row_, uint32_t, uint32_t, uint32_t* stage_)
-        : a(a_), g(g_), first(at.b * a_.stride), row0(row_ - (threadIdx.x & 31)), stage(stage_) {
-        rows = row0 >= g.M ? 0 : g.M - row0 < 32 ? g.M - row0 : 32;
-        if (a.factor) scale *= a.factor[at.b];
-        if (a.out) scale *= kUnscale;
+    __device__ ChainEpi(const Args& a, const TileJob& t_, uint32_t row_, uint32_t, uint32_t* stage_)
+        : e(a), t(t_), row(row_), row0(row_ - (threadIdx.x & 31)), stage(stage_) {
+        rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32;
+        if (t.step == 0 && t.kind != 1) {
+            const float f = a.factor[t.b];
+            scale *= t.kind == 0 ? f * f : f;
+        }
+        if (t.kind == 2 && t.step + 1 == e.steps) scale *= kUnscale;
+    }
+    // A's 64 columns from `col` of the warp's rows into the second area
+    __device__ void fetch(uint32_t col) {
+        const uint32_t lane = threadIdx.x & 31, c = lane & 7;
+        const __half* src = e.gram + t.b * e.a_stride + (uint64_t)row0 * e.ld_a + col + 8 * c;
+        if (col + 8 * c < e.ld_a) {
+#pragma unroll
+            for (uint32_t r = lane >> 3; r < 32; r += 4)
+                if (r < rows)
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(staged(stage + kStageWords, r, c))), "l"(src + (uint64_t)r * e.ld_a) : "memory");
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    }
+    template <class Plan>
+    __device__ void begin(const Plan& plan, uint32_t col0) {
+        if (t.kind != 1 || !rows) return;
+        plan.wait(t);
+        fetch(col0);
+    }
+    __device__ void square(__half* out, uint32_t col, float (&v)[32], bool last) {
+        store_tile32(out, SK_F16, e.ld_a, row0, rows, col, e.ld_a, v, 16, stage, true, last);
+        const bool second = col & 32;
+        if (t.m == t.n || !(second || last)) return;
+        // the mirror image, from the staged lines: four lanes write a row of it, eight of the warp's rows each
+        const uint32_t lane = threadIdx.x & 31, s = lane & 3, first = col & ~63u, count = second ? 64 : 32;
+#pragma unroll 2
+        for (uint32_t c = lane >> 2; c < count; c += 8) {
+            uint32_t h[8];
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) h[k] = *(const uint16_t*)(staged(stage, 8 * s + k, c >> 3) + (c & 7) * 2);
+            if (first + c < t.N)
+                *(uint4*)(out + (uint64_t)(first + c) * e.ld_a + row0 + 8 * s) =
+                    make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        }
     }
     __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (!rows) return;
+        if (t.kind == 1) {
+            if (!(col & 32)) {
+                asm volatile("cp.async.wait_all;" ::: "memory");
+                __syncwarp();
+            }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] *= scale;
-        if (a.out) {
-            store_tile32((uint16_t*)a.out + first, a.type, a.ld, row0, rows, col, g.N, v, a.align, stage, true, last);
+            for (int q = 0; q < 4; ++q) {
+                const uint4 w = *(const uint4*)staged(stage + kStageWords, row - row0, ((col & 32) >> 3) + q);
+                const uint32_t r[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = __half22float2(*(const __half2*)&r[i]);
+                    v[8 * q + 2 * i] = e.b * f.x + e.c * kUnscale * v[8 * q + 2 * i];
+                    v[8 * q + 2 * i + 1] = e.b * f.y + e.c * kUnscale * v[8 * q + 2 * i + 1];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 32; ++i)
+                if (col + i == row) v[i] += e.a * kScale;
+            __syncwarp();
+            if ((col & 32) && !last) fetch(col + 32);                // while this pair is written
+            square(e.poly + t.b * e.a_stride, col, v, last);
             return;
         }
-        store_tile32(a.hi + first, SK_F16, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage, !a.lo, last);
-        if (a.lo) {                              // the two share the space, so neither waits for its lines' second half
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] *= scale;
+        if (t.kind == 0) {
+            square(e.gram + t.b * e.a_stride, col, v, last);
+            return;
+        }
+        if (t.step + 1 == e.steps) {
+            store_tile32((uint16_t*)e.out + t.b * e.out_stride, e.out_type, e.ld_out, row0, rows, col, t.N, v, e.align, stage, true, last);
+            return;
+        }
+        const uint32_t to = (t.step + 1) & 1;
+        store_tile32(e.hi[to] + t.b * e.x_stride, SK_F16, e.ld_x, row0, rows, col, e.ld_x, v, 16, stage, true, last);
+        if (t.step + 3 < e.steps) {              // the next step's X is a pair
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
-            store_tile32(a.lo + first, SK_F16, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage, false, last);
+            store_tile32(e.lo[to] + t.b * e.x_stride, SK_F16, e.ld_x, row0, rows, col, e.ld_x, v, 16, stage + kStageWords, true, last);
         }
     }
     __device__ void end() {}
@@ -160,6 +264,7 @@ struct SquareArgs {
     uint32_t ld;
     uint64_t stride;
     uint32_t exact;                              // U is the 16-bit update itself: stored exactly, times a power of two
+    uint32_t* count;                             // [batch], set to zero
 };
 
 // Sums of squares of U per block, in 64 bits (an update in fp32 may have squares beyond its range); updates the momentum.
@@ -237,7 +342,10 @@ __global__ void __launch_bounds__(256) k_ortho_scale(const __grid_constant__ Squ
         } else {
             s_scale = (float)scale;
         }
-        if (blockIdx.x == 0) s.factor[b] = (float)rest;
+        if (blockIdx.x == 0) {
+            s.factor[b] = (float)rest;
+            s.count[b] = 0;
+        }
     }
     __syncthreads();
     const float scale = s_scale;
@@ -271,7 +379,7 @@ __global__ void __launch_bounds__(256) k_ortho_scale(const __grid_constant__ Squ
 struct OrthoLayout {
     uint32_t ld_x, ld_a, m;
     uint64_t x_elems, a_elems;                   // per matrix
-    uint64_t off_partial, off_factor, off_x[2], off_lo, off_a, off_p, total;
+    uint64_t off_partial, off_factor, off_count, off_x[2], off_lo, off_a, off_p, total;
 };
 OrthoLayout layout_of(const OrthoArgs& a) {
     OrthoLayout l;
@@ -284,6 +392,7 @@ OrthoLayout layout_of(const OrthoArgs& a) {
     auto take = [&](uint64_t bytes) { const uint64_t r = at; at += round_up(bytes, 256); return r; };
     l.off_partial = take(a.batch * kNormBlocks * 8);
     l.off_factor = take(a.batch * 4);
+    l.off_count = take(a.batch * 4);
     l.off_x[0] = take(a.batch * l.x_elems * 2);
     l.off_x[1] = take(a.batch * l.x_elems * 2);
     l.off_lo = take(2 * round_up(a.batch * l.x_elems * 2, 256));
@@ -687,44 +796,74 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     sq.ld = l.ld_x;
     sq.stride = l.x_elems;
     sq.exact = exact;
+    sq.count = (uint32_t*)(ws + l.off_count);
     SK_OP_CUDA(launch_kernel(true, k_ortho_square, dim3(sq.blocks, batch), 256, 0, st, sq));
     SK_OP_CUDA(launch_kernel(true, k_ortho_scale, dim3(sq.blocks, batch), 256, 0, st, sq));
 
-    GemmGroup square{};
-    square.M = square.N = m;
-    square.batch = batch;
-    square.symmetric = 1;
-    GemmGroup apply = square;
-    apply.symmetric = 0;
-    apply.M = (uint32_t)a.rows;
-    apply.N = (uint32_t)a.cols;
-    const Operand oa{gram, m, m, l.ld_a, l.a_elems, batch, false}, op{poly, m, m, l.ld_a, l.a_elems, batch, false};
-    for (int s = 0; s < a.steps; ++s) {
-        const int from = s & 1, to = from ^ 1;
-        const Operand ox{x[from], a.rows, a.cols, l.ld_x, l.x_elems, batch, tall};
-        SK_OP_CUDA(launch_product<GramEpi>(true, ox, ox, nullptr, nullptr, square, dev.status, {gram, l.a_elems, l.ld_a, s == 0 ? sq.factor : nullptr}, dev.sm_count, st));
-        PolyEpi::Args pa{{poly, l.a_elems, l.ld_a, nullptr}, gram, a.coefficient[0], a.coefficient[1], a.coefficient[2]};
-        SK_OP_CUDA(launch_product<PolyEpi>(true, oa, oa, nullptr, nullptr, square, dev.status, pa, dev.sm_count, st));
-        ApplyEpi::Args ea{};
-        ea.factor = s == 0 ? sq.factor : nullptr;
-        if (s + 1 < a.steps) {
-            ea.hi = x[to];
-            ea.lo = split(s + 1) ? lo[to] : nullptr;
-            ea.stride = l.x_elems;
-            ea.ld = l.ld_x;
-        } else {
-            ea.out = a.out;
-            ea.stride = a.stride_out;
-            ea.ld = a.ld_out;
-            ea.type = a.out_type;
-            ea.align = align;
-        }
-        // X stored with its columns contiguous is the K-major first factor of X P, and the MN-major second factor of P X
-        const Operand xh{x[from], a.rows, a.cols, l.ld_x, l.x_elems, batch, !tall}, xl{lo[from], a.rows, a.cols, l.ld_x, l.x_elems, batch, !tall};
-        const bool two = split(s);
-        if (tall) SK_OP_CUDA(launch_product<ApplyEpi>(true, xh, op, two ? &xl : nullptr, two ? &op : nullptr, apply, dev.status, ea, dev.sm_count, st));
-        else SK_OP_CUDA(launch_product<ApplyEpi>(true, op, xh, two ? &op : nullptr, two ? &xl : nullptr, apply, dev.status, ea, dev.sm_count, st));
+    ChainEpi::Args ea{};
+    ea.gram = gram;
+    ea.poly = poly;
+    for (int i = 0; i < 2; ++i) { ea.hi[i] = x[i]; ea.lo[i] = lo[i]; }
+    ea.a_stride = l.a_elems;
+    ea.x_stride = l.x_elems;
+    ea.ld_a = l.ld_a;
+    ea.ld_x = l.ld_x;
+    ea.a = a.coefficient[0];
+    ea.b = a.coefficient[1];
+    ea.c = a.coefficient[2];
+    ea.factor = sq.factor;
+    ea.out = a.out;
+    ea.out_stride = a.stride_out;
+    ea.ld_out = a.ld_out;
+    ea.out_type = a.out_type;
+    ea.align = align;
+    ea.steps = (uint32_t)a.steps;
+
+    ChainPlan p{};
+    bool ok = true;
+    for (int i = 0; i < 2; ++i) {
+        const Operand g{x[i], a.rows, a.cols, l.ld_x, l.x_elems, batch, tall}, h{x[i], a.rows, a.cols, l.ld_x, l.x_elems, batch, !tall},
+            o{lo[i], a.rows, a.cols, l.ld_x, l.x_elems, batch, !tall};
+        ok = ok && encode_operand(&p.gram_x[i], g, false, g.mn ? 64 : 128) && encode_operand(&p.apply_hi[i], h, false, h.mn ? 64 : 128) &&
+             encode_operand(&p.apply_lo[i], o, false, o.mn ? 64 : 128);
     }
+    const Operand oa{gram, m, m, l.ld_a, l.a_elems, batch, false}, op{poly, m, m, l.ld_a, l.a_elems, batch, false};
+    ok = ok && encode_operand(&p.gram, oa, false, 128) && encode_operand(&p.poly, op, false, 128);
+    if (!ok) return set_error(SK_ECUDA, "sk_orthogonalize: a tensor map was refused");
+    p.steps = (uint32_t)a.steps;
+    p.exact = exact;
+    p.tall = tall;
+    p.batch = batch;
+    p.m = m;
+    p.rows = (uint32_t)a.rows;
+    p.cols = (uint32_t)a.cols;
+    p.k_poly = (m + kGemmK - 1) / kGemmK;
+    p.k_gram = (uint32_t)(((tall ? a.rows : a.cols) + kGemmK - 1) / kGemmK);
+    p.count = sq.count;
+    p.status = dev.status;
+    // Pairs of blocks on 256 x 256 or single ones on 128 x 128: a stage takes both the same time (some 620 cycles, see launch_products), the
+    // pair does twice the work per SM in it.  The time is about that of the work on all units, but at least that of one matrix's dependent
+    // products, whose starts and epilogues are shorter with the small tile (7000 cycles, 12,000).
+    auto cost = [&](uint64_t tile, uint64_t units, uint64_t start) {
+        const uint64_t side = (m + tile - 1) / tile, sq_tiles = side * (side + 1) / 2, ap = ((a.rows + tile - 1) / tile) * ((a.cols + tile - 1) / tile);
+        const uint64_t stages = p.k_gram + p.k_poly, work = batch * (sq_tiles * stages + ap * 2 * p.k_poly + (2 * sq_tiles + ap) * kTileCost);
+        auto rounds = [&](uint64_t tiles) { return (tiles + units - 1) / units; };
+        const uint64_t path = (rounds(sq_tiles) * stages + rounds(ap) * 2 * p.k_poly) * 620 + 3 * start, even = work * 620 / units;
+        return path > even ? path : even;
+    };
+    const bool wide = cost(256, (uint64_t)dev.sm_count / 2, 12000) <= cost(128, (uint64_t)dev.sm_count, 7000);
+    const uint32_t tile = wide ? 256 : 128, slots = (uint32_t)dev.sm_count / (wide ? 2 : 1);
+    p.side = (m + tile - 1) / tile;
+    p.square = p.side * (p.side + 1) / 2;
+    p.tiles_m = (p.rows + tile - 1) / tile;
+    p.tiles_n = (p.cols + tile - 1) / tile;
+    p.apply = p.tiles_m * p.tiles_n;
+    p.signals = (wide ? 2 : 1) * kEpiWarps;
+    if ((uint64_t)a.steps * batch * (2ull * p.square + p.apply) * p.signals >= (1ull << 32))
+        return set_error(SK_EINVAL, "sk_orthogonalize: batch * rows * cols is too large for one call");
+    const uint32_t most_tiles = batch * (p.square > p.apply ? p.square : p.apply), units = most_tiles < slots ? most_tiles : slots;
+    auto launch = wide ? launch_plan<2, 256, ChainPlan, ChainEpi> : launch_plan<1, 128, ChainPlan, ChainEpi>;
+    SK_OP_CUDA(launch(false, p, ea, units, st));
     return SK_OK;
 }
 
