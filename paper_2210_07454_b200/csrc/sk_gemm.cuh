@@ -231,7 +231,7 @@ struct GemmTile {
 
 // Plan: job(unit, units, i, job): the unit's i-th tile; wait(job): until its operands are there; done(job): called by every epilogue warp
 // when its share of the tile is written.
-// Epi: struct Args; __device__ Epi(const Args&, job, row, half, the warp's shared memory); begin(plan, first column) before the
+// Epi: struct Args; __device__ Epi(const Args&, job, row, half, shared address of the warp's memory); begin(plan, first column) before the
 // accumulator is waited for; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
 // row of the tile and gets its columns 32 at a time; the two warps that share a row take half the columns each.  Rows >= M
 // are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
@@ -360,7 +360,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
         }
     } else {
         const uint32_t w = warp - 2, quarter = warp & 3, half = w >> 2;
-        uint32_t* stage = (uint32_t*)(smem_raw + (stages - smem_u32(smem_raw)) + kStages * (kBytesA + kBytesB)) + w * Epi::kWords;
+        const uint32_t stage = stages + kStages * kBytes + w * Epi::kWords * 4;
         for (uint32_t n = 0; plan.job(unit, units, n, t); ++n) {
             const uint32_t a = n & 1;
             const uint32_t row = t.m * (128 * CG) + rank * 128 + quarter * 32 + lane;

@@ -34,7 +34,7 @@ struct StatsEpi {
     uint32_t row, slot;
     int64_t target;
     float top = -INFINITY, sum = 0;
-    __device__ StatsEpi(const Args& a_, const TileJob& t_, uint32_t row_, uint32_t half, uint32_t*)
+    __device__ StatsEpi(const Args& a_, const TileJob& t_, uint32_t row_, uint32_t half, uint32_t)
         : a(a_), t(t_), row(row_), slot(t_.n * 2 + half) { target = row < t.M ? a.targets[row] : -1; }
     __device__ void chunk(uint32_t col, float (&v)[32], bool) {
         const uint32_t valid = t.N - col;
@@ -118,10 +118,10 @@ struct GradEpi {
     const Args& a;
     const TileJob& t;
     uint32_t row0, rows;
-    uint32_t* stage;
+    uint32_t stage;
     float off = 0, scale = 0;
     int64_t target = -1;
-    __device__ GradEpi(const Args& a_, const TileJob& t_, uint32_t row, uint32_t, uint32_t* stage_)
+    __device__ GradEpi(const Args& a_, const TileJob& t_, uint32_t row, uint32_t, uint32_t stage_)
         : a(a_), t(t_), row0(row - (threadIdx.x & 31)), stage(stage_) {
         rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32;
         if (row < t.M) {
@@ -166,9 +166,9 @@ struct OutEpi {
     const TileJob& t;
     float* sum;
     uint32_t row0, rows;
-    uint32_t* stage;
+    uint32_t stage;
     float scale;
-    __device__ OutEpi(const Args& a_, const TileJob& t_, uint32_t row, uint32_t, uint32_t* stage_)
+    __device__ OutEpi(const Args& a_, const TileJob& t_, uint32_t row, uint32_t, uint32_t stage_)
         : a(a_.o[t_.kind]), t(t_), sum(a.sum ? a.sum + t_.b * a.sum_stride : nullptr), row0(row - (threadIdx.x & 31)), stage(stage_),
           scale(a_.factor ? 1.0f / *a_.factor : 1.0f) {
         rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32;

@@ -74,33 +74,45 @@ inline uint32_t row_alignment(const void* p, uint64_t ld, int type) {
     return bits % 16 == 0 ? 16 : bits % 4 == 0 ? 4 : 2;
 }
 
-// A warp's rows of an output tile, 32 columns at a time: the lane's row (row0 + lane; rows of the 32 exist), v = its columns
-// col .. col + 31 (those below limit exist; col is a multiple of 32).  The values pass through 4 KB of the warp's shared memory (32 rows of 128 bytes, 16-byte
-// chunks swizzled), so that neighbouring lanes write neighbouring addresses: whole 128-byte lines, two calls of 16-bit values
-// together (pair; last: no second one follows).  Lanes writing 32 bytes of a row each took 5900 cycles for 128 x 256, about as much as a
-// product over 600 values of k.  All lanes take part.
-// (The swizzle's key differs within any eight neighbouring rows, and within four rows eight apart, which a reader of columns takes.)
-__device__ __forceinline__ uint8_t* staged(uint32_t* stage, uint32_t r, uint32_t chunk) {
-    return (uint8_t*)stage + r * 128 + ((chunk ^ ((r ^ (r >> 3)) & 7)) << 4);
+__device__ __forceinline__ void store_shared16(uint32_t at, uint4 q) {
+    asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
 }
+__device__ __forceinline__ uint4 load_shared16(uint32_t at) {
+    uint4 q;
+    asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(at) : "memory");
+    return q;
+}
+// A warp's staging area: 32 rows of 128 bytes, 16-byte chunks swizzled.  The key differs within any eight neighbouring rows, and within
+// the four pairs of rows (2 i, 2 i + 1) + 0, 8, 16, 24 that a reader of columns takes.
+__device__ __forceinline__ uint32_t staged(uint32_t stage, uint32_t r, uint32_t chunk) {
+    return stage + r * 128 + ((chunk ^ ((r ^ ((r >> 3) << 1)) & 7)) << 4);
+}
+
+// A warp's rows of an output tile, 32 columns at a time: the lane's row (row0 + lane; rows of the 32 exist), v = its columns
+// col .. col + 31 (those below limit exist; col is a multiple of 32).  The values pass through 4 KB of the warp's shared memory (stage, its shared
+// address), so that neighbouring lanes write neighbouring addresses: whole 128-byte lines, two calls of 16-bit values
+// together (pair; last: no second one follows).  All lanes take part.
 __device__ __forceinline__ void store_tile32(void* out, int type, uint64_t ld, uint64_t row0, uint32_t rows, uint32_t col, uint32_t limit,
-                                             const float (&v)[32], uint32_t align, uint32_t* stage, bool pair, bool last) {
+                                             const float (&v)[32], uint32_t align, uint32_t stage, bool pair, bool last) {
     const bool wide = type == SK_F32;            // 32 columns are whole lines already
     const uint32_t lane = threadIdx.x & 31, second = pair && !wide ? (col >> 5) & 1 : 0;
     if (!second) __syncwarp();                   // what was staged before has been read
     if (wide) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) *(float4*)staged(stage, lane, i) = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+        for (int i = 0; i < 8; ++i)
+            store_shared16(staged(stage, lane, i), make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i + 2]),
+                                                              __float_as_uint(v[4 * i + 3])));
     } else {
+        uint32_t h[16];
+        if (type == SK_BF16) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            uint4 q;
-            q.x = pack16(v[8 * i], v[8 * i + 1], type == SK_BF16);
-            q.y = pack16(v[8 * i + 2], v[8 * i + 3], type == SK_BF16);
-            q.z = pack16(v[8 * i + 4], v[8 * i + 5], type == SK_BF16);
-            q.w = pack16(v[8 * i + 6], v[8 * i + 7], type == SK_BF16);
-            *(uint4*)staged(stage, lane, 4 * second + i) = q;
+            for (int i = 0; i < 16; ++i) h[i] = pack16(v[2 * i], v[2 * i + 1], true);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) h[i] = pack16(v[2 * i], v[2 * i + 1], false);
         }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store_shared16(staged(stage, lane, 4 * second + i), make_uint4(h[4 * i], h[4 * i + 1], h[4 * i + 2], h[4 * i + 3]));
         if (pair && !second && !last) return;    // the other half of the lines follows
     }
     __syncwarp();
@@ -108,26 +120,45 @@ __device__ __forceinline__ void store_tile32(void* out, int type, uint64_t ld, u
     const uint32_t bytes = min(wide ? 128u : 64u * (second + 1), (limit - first) * size);            // of every row
     uint8_t* o = (uint8_t*)out + (row0 * ld + first) * size;
     const uint64_t step = ld * size;
-    if (align >= 16 && bytes % 16 == 0) {        // eight lanes a row
-        const uint32_t c = lane & 7;
-        if (c * 16 < bytes)
+    if (align >= 16 && bytes % 16 == 0) {        // eight lanes a row, all eight loads before the stores
+        const uint32_t c = lane & 7, r0 = lane >> 3;
+        if (c * 16 < bytes) {
+            uint4 q[8];
 #pragma unroll
-            for (uint32_t r = lane >> 3; r < 32; r += 4)
-                if (r < rows) *(uint4*)(o + r * step + c * 16) = *(const uint4*)staged(stage, r, c);
-    } else if (align >= 4) {                     // a row after the other
-        if (lane * 4 < bytes)
-#pragma unroll 4
-            for (uint32_t r = 0; r < rows; ++r) {
-                const uint32_t w = *(const uint32_t*)(staged(stage, r, lane >> 2) + (lane & 3) * 4);
-                if (lane * 4 + 4 <= bytes) *(uint32_t*)(o + r * step + lane * 4) = w;
-                else *(uint16_t*)(o + r * step + lane * 4) = (uint16_t)w;
+            for (uint32_t i = 0; i < 8; ++i) q[i] = load_shared16(staged(stage, r0 + 4 * i, c));
+            uint8_t* p = o + r0 * step + c * 16;
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i)
+                if (r0 + 4 * i < rows) *(uint4*)(p + 4 * i * step) = q[i];
+        }
+    } else if (align >= 4) {                     // a row after the other, eight at a time
+        if (lane * 4 < bytes) {
+            const bool whole = lane * 4 + 4 <= bytes;
+            for (uint32_t r = 0; r < rows; r += 8) {
+                uint32_t w[8];
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w[i]) : "r"(staged(stage, r + i, lane >> 2) + (lane & 3) * 4) : "memory");
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i)
+                    if (r + i < rows) {
+                        if (whole) *(uint32_t*)(o + (r + i) * step + lane * 4) = w[i];
+                        else *(uint16_t*)(o + (r + i) * step + lane * 4) = (uint16_t)w[i];
+                    }
             }
+        }
     } else {
-#pragma unroll 4
-        for (uint32_t r = 0; r < rows; ++r)
+        for (uint32_t r = 0; r < rows; r += 8) {
 #pragma unroll
-            for (uint32_t c = lane; c < 64; c += 32)
-                if (c * 2 < bytes) *(uint16_t*)(o + r * step + c * 2) = *(const uint16_t*)(staged(stage, r, c >> 3) + (c & 7) * 2);
+            for (uint32_t c = lane; c < 64; c += 32) {
+                if (c * 2 >= bytes) break;
+                uint16_t w[8];
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i) asm volatile("ld.shared.b16 %0, [%1];" : "=h"(w[i]) : "r"(staged(stage, r + i, c >> 3) + (c & 7) * 2) : "memory");
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i)
+                    if (r + i < rows) *(uint16_t*)(o + (r + i) * step + c * 2) = w[i];
+            }
+        }
     }
 }
 

@@ -138,9 +138,9 @@ struct ChainEpi {
     const Args& e;
     const TileJob& t;
     uint32_t row, row0, rows;                    // the lane's row, the warp's first, how many of the warp's exist
-    uint32_t* stage;
+    uint32_t stage;
     float scale = kUnscale;
-    __device__ ChainEpi(const Args& a, const TileJob& t_, uint32_t row_, uint32_t, uint32_t* stage_)
+    __device__ ChainEpi(const Args& a, const TileJob& t_, uint32_t row_, uint32_t, uint32_t stage_)
         : e(a), t(t_), row(row_), row0(row_ - (threadIdx.x & 31)), stage(stage_) {
         rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32;
         if (t.step == 0 && t.kind != 1) {
@@ -157,7 +157,7 @@ struct ChainEpi {
 #pragma unroll
             for (uint32_t r = lane >> 3; r < 32; r += 4)
                 if (r < rows)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(staged(stage + kStageWords, r, c))), "l"(src + (uint64_t)r * e.ld_a) : "memory");
+                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(staged(stage + kStageWords * 4, r, c)), "l"(src + (uint64_t)r * e.ld_a) : "memory");
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
@@ -171,16 +171,19 @@ struct ChainEpi {
         store_tile32(out, SK_F16, e.ld_a, row0, rows, col, e.ld_a, v, 16, stage, true, last);
         const bool second = col & 32;
         if (t.m == t.n || !(second || last)) return;
-        // the mirror image, from the staged lines: four lanes write a row of it, eight of the warp's rows each
-        const uint32_t lane = threadIdx.x & 31, s = lane & 3, first = col & ~63u, count = second ? 64 : 32;
-#pragma unroll 2
-        for (uint32_t c = lane >> 2; c < count; c += 8) {
-            uint32_t h[8];
+        // The mirror image, from the staged lines.  A transposing load of four 8 x 8 matrices gives a lane two neighbouring rows of one column from each;
+        // with rows 8 s + 2 i, 8 s + 2 i + 1 (s = 0..3) in matrix i they are eight neighbours: four lanes write a row of the image.
+        const uint32_t lane = threadIdx.x & 31, first = col & ~63u, count = second ? 64 : 32;
+        const uint32_t from = 8 * ((lane & 7) >> 1) + 2 * (lane >> 3) + (lane & 1);
+        uint4 q[8];
 #pragma unroll
-            for (uint32_t k = 0; k < 8; ++k) h[k] = *(const uint16_t*)(staged(stage, 8 * s + k, c >> 3) + (c & 7) * 2);
-            if (first + c < t.N)
-                *(uint4*)(out + (uint64_t)(first + c) * e.ld_a + row0 + 8 * s) =
-                    make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+        for (uint32_t i = 0; i < 8; ++i)
+            asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                         : "=r"(q[i].x), "=r"(q[i].y), "=r"(q[i].z), "=r"(q[i].w) : "r"(staged(stage, from, i)) : "memory");
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) {
+            const uint32_t c = 8 * i + (lane >> 2);
+            if (c < count && first + c < t.N) *(uint4*)(out + (uint64_t)(first + c) * e.ld_a + row0 + 8 * (lane & 3)) = q[i];
         }
     }
     __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
@@ -192,7 +195,7 @@ struct ChainEpi {
             }
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint4 w = *(const uint4*)staged(stage + kStageWords, row - row0, ((col & 32) >> 3) + q);
+                const uint4 w = load_shared16(staged(stage + kStageWords * 4, row - row0, ((col & 32) >> 3) + q));
                 const uint32_t r[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
@@ -224,7 +227,7 @@ struct ChainEpi {
         if (t.step + 3 < e.steps) {              // the next step's X is a pair
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
-            store_tile32(e.lo[to] + t.b * e.x_stride, SK_F16, e.ld_x, row0, rows, col, e.ld_x, v, 16, stage + kStageWords, true, last);
+            store_tile32(e.lo[to] + t.b * e.x_stride, SK_F16, e.ld_x, row0, rows, col, e.ld_x, v, 16, stage + kStageWords * 4, true, last);
         }
     }
     __device__ void end() {}
@@ -704,7 +707,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
             uint16_t* out = (uint16_t*)a.out + batch * a.stride_out;
             if (!s.tall) {
                 store_tile32(out + first, a.out_type, a.ld_out, row0, min(s.m - row0, 32u), col, width, v, s.align,
-                             (uint32_t*)(base + kSmallGram) + warp * kStageWords, false, true);
+                             base32 + kSmallGram + warp * kStageWords * 4, false, true);
             } else if (row < s.m) {              // the lanes' rows are the output's neighbouring columns
 #pragma unroll
                 for (int i = 0; i < 32; ++i)
