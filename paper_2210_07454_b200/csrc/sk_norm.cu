@@ -6,8 +6,8 @@
 // Bound by memory: forward reads x and writes y once, backward reads x and dy and writes dx once.  A row belongs to 8 or 32
 // lanes of a warp or to a block, every thread to fixed columns.  What keeps the memory busy is a ring of rows in
 // shared memory that each thread fills for itself with asynchronous copies (its own columns only, so no barrier guards it): the next
-// rows travel while one is worked on, without holding registers.  Rows whose elements cannot be copied in 4 bytes or more
-// (16-bit rows of odd length) come through registers, one row ahead.  The arithmetic is two values to an instruction
+// rows travel while one is worked on, without holding registers.  Rows of odd lengths do so too, with accesses that
+// begin before the row (Place); only matrices whose rows lie differently to the 16-byte boundary come element by element, through registers.  The arithmetic is two values to an instruction
 // (f32x2): with one the kernels are bound by issue (bf16 rows then take as long as fp32 ones).
 //
 // Statistics: a warp computes the mean of its part and the squares around that, and the parts are joined by the formula for
@@ -74,24 +74,25 @@ __device__ __forceinline__ void unpack(const Pack<T, V> (&p)[NV], F2 (&o)[NV * V
             }
     }
 }
-// where a thread's accesses lie in the row
-template <int V>
+// Where a thread's accesses lie in the row.  SHIFT: the rows start off the 16-byte boundary; accesses stay on it and begin `shift` elements
+// before the row, so the row's first and last one hold elements that are not the row's.  The shift is the same for all rows of a
+// thread (they are a multiple of 16 bytes apart), and so its columns are.
+template <int V, bool SHIFT>
 struct Place {
-    uint32_t t, tpr, cols;
-    __device__ __forceinline__ uint32_t col(int i) const { return (i * tpr + t) * V; }
-    __device__ __forceinline__ bool in(int i) const { return col(i) < cols; }
-    // the pair with its elements beyond the row set to zero
-    __device__ __forceinline__ F2 only(int q, F2 d) const {
-        if constexpr (V == 1) {
-            const float2 f = parts(d);
-            return f2(in(2 * q) ? f.x : 0.0f, in(2 * q + 1) ? f.y : 0.0f);
-        } else {
-            return in(q / (V / 2)) ? d : f2(0, 0);
-        }
+    uint32_t t, tpr, cols, shift;
+    __device__ __forceinline__ int col(int i) const { return (int)((i * tpr + t) * V) - (SHIFT ? (int)shift : 0); }
+    __device__ __forceinline__ bool in(int i) const { return col(i) < (int)cols; }                       // any of it
+    __device__ __forceinline__ bool whole(int i) const { return !SHIFT || (col(i) >= 0 && col(i) + V <= (int)cols); }
+    __device__ __forceinline__ bool valid(int i, int j) const { return col(i) + j < (int)cols && (!SHIFT || col(i) + j >= 0); }
+    // pair q with its elements beyond the row set to zero
+    __device__ __forceinline__ F2 pair_only(int q, F2 d) const {
+        const int i = V == 1 ? 2 * q : q / (V > 1 ? V / 2 : 1), j = V == 1 ? 0 : 2 * (q - i * (V / 2));
+        const float2 f = parts(d);
+        return f2(valid(i, j) ? f.x : 0.0f, (V == 1 ? valid(i + 1, 0) : valid(i, j + 1)) ? f.y : 0.0f);
     }
 };
-template <typename T, int V, int NV>
-__device__ __forceinline__ void store(T* row, const F2 (&o)[NV * V / 2], const Place<V>& at) {
+template <typename T, int V, int NV, bool SHIFT>
+__device__ __forceinline__ void store(T* row, const F2 (&o)[NV * V / 2], const Place<V, SHIFT>& at) {
     if constexpr (V == 1) {
 #pragma unroll
         for (int q = 0; q < NV / 2; ++q) {
@@ -113,47 +114,50 @@ __device__ __forceinline__ void store(T* row, const F2 (&o)[NV * V / 2], const P
                     ((uint32_t*)&p)[j] = pack16(f.x, f.y, std::is_same<T, __nv_bfloat16>::value);
                 }
             }
-            if (at.in(i)) *(Pack<T, V>*)(row + at.col(i)) = p;
+            if (!at.in(i)) continue;
+            if (at.whole(i)) {
+                *(Pack<T, V>*)(row + at.col(i)) = p;
+            } else {
+#pragma unroll
+                for (int j = 0; j < V; ++j)
+                    if (at.valid(i, j)) row[at.col(i) + j] = p.v[j];
+            }
         }
     }
 }
 // The weights of pair q (`none` without a weight vector or beyond the row).
-template <int V>
-__device__ __forceinline__ F2 weights_of(const void* p, int type, float none, int q, const Place<V>& at) {
-    if constexpr (V == 1) {
-        return f2(p && at.in(2 * q) ? load_as(p, type, at.col(2 * q)) : none, p && at.in(2 * q + 1) ? load_as(p, type, at.col(2 * q + 1)) : none);
-    } else {
-        const int i = q / (V / 2);
-        const uint32_t c = at.col(i) + 2 * (q - i * (V / 2));
-        if (!p || !at.in(i)) return f2(none, none);
-        if (type == SK_F32 && (uintptr_t)p % 8 == 0) {
-            const float2 f = *(const float2*)((const float*)p + c);
-            return f2(f.x, f.y);
-        }
-        return f2(load_as(p, type, c), load_as(p, type, c + 1));
+template <int V, bool SHIFT>
+__device__ __forceinline__ F2 weights_of(const void* p, int type, float none, int q, const Place<V, SHIFT>& at) {
+    const int i = V == 1 ? 2 * q : q / (V > 1 ? V / 2 : 1), j = V == 1 ? 0 : 2 * (q - i * (V / 2));
+    if (!p) return f2(none, none);
+    if (V > 1 && !SHIFT && type == SK_F32 && (uintptr_t)p % 8 == 0) {
+        if (!at.in(i)) return f2(none, none);
+        const float2 f = *(const float2*)((const float*)p + at.col(i) + j);
+        return f2(f.x, f.y);
     }
+    const int i2 = V == 1 ? i + 1 : i, j2 = V == 1 ? 0 : j + 1;
+    return f2(at.valid(i, j) ? load_as(p, type, at.col(i) + j) : none, at.valid(i2, j2) ? load_as(p, type, at.col(i2) + j2) : none);
 }
 
 // ---- the rows on their way -------------------------------------------------------------------------------------------------
 template <int BYTES>
-__device__ __forceinline__ void copy_async(void* dst, const void* src, bool live) {            // zeroes without a source
-    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst), n = live ? BYTES : 0;
-    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(n) : "memory");
-    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(d), "l"(src), "n"(BYTES), "r"(n) : "memory");
+__device__ __forceinline__ void copy_async(void* dst, const void* src, uint32_t bytes) {       // zeroes beyond `bytes`
+    const uint32_t d = (uint32_t)__cvta_generic_to_shared(dst);
+    if constexpr (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(d), "l"(src), "r"(bytes) : "memory");
+    else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(d), "l"(src), "n"(BYTES), "r"(bytes) : "memory");
 }
 
 // A thread's columns of N matrices' rows.
-template <typename T, int V, int NV, int N>
+template <typename T, int V, int NV, int N, bool SHIFT>
 struct Rows {
     static constexpr bool kAsync = sizeof(T) * V >= 4;
     using P = Pack<T, V>;
     static constexpr uint32_t smem(uint32_t threads) { return kAsync ? kDepth * N * NV * threads * (uint32_t)sizeof(P) : 0; }
     const T* src[N];
     uint64_t ld[N], rows;
-    Place<V> at;
+    Place<V, SHIFT> at;
     P* ring;                                     // [kDepth][N][NV][blockDim.x]
     P ahead[kAsync ? 1 : N][kAsync ? 1 : NV];
-
     const T* next[N];                            // the thread's first column of the row to ask for next
     uint64_t next_row;
 
@@ -167,7 +171,19 @@ struct Rows {
                 const bool in = live && at.in(i);
                 const T* p = next[n] + i * at.tpr * V;
                 if constexpr (kAsync) {
-                    copy_async<(int)sizeof(P)>(slot(s, n, i), in ? p : src[n], in);
+                    uint32_t bytes = in ? (uint32_t)sizeof(P) : 0;
+                    if constexpr (SHIFT) {
+                        const int left = (int)at.cols - at.col(i);               // the row's end: no further
+                        if (in && left < V) bytes = (uint32_t)left * sizeof(T);
+                        if (i == 0 && in && p < src[n]) {                        // the matrix' start: the row's own elements one by one
+                            P one;
+#pragma unroll
+                            for (int j = 0; j < V; ++j) one.v[j] = at.valid(0, j) ? p[j] : from_float<T>(0.0f);
+                            *slot(s, n, 0) = one;
+                            continue;
+                        }
+                    }
+                    copy_async<(int)sizeof(P)>(slot(s, n, i), in ? p : (const T*)((uintptr_t)src[n] & ~(uintptr_t)15), bytes);
                 } else {
 #pragma unroll
                     for (int j = 0; j < V; ++j) ahead[n][i].v[j] = from_float<T>(0.0f);
@@ -198,6 +214,15 @@ struct Rows {
             for (int n = 0; n < N; ++n)
 #pragma unroll
                 for (int i = 0; i < NV; ++i) out[n][i] = *slot(s, n, i);
+            if constexpr (SHIFT) {
+                if (at.col(0) < 0) {                                             // what stands before the row
+#pragma unroll
+                    for (int n = 0; n < N; ++n)
+#pragma unroll
+                        for (int j = 0; j < V; ++j)
+                            if (!at.valid(0, j)) out[n][0].v[j] = from_float<T>(0.0f);
+                }
+            }
             s = s + 1 == kDepth ? 0 : s + 1;
         } else {
 #pragma unroll
@@ -208,6 +233,11 @@ struct Rows {
         }
     }
 };
+// elements from the 16-byte boundary before a row to the row's start
+template <typename T>
+__device__ __forceinline__ uint32_t shift_of(const void* p, uint64_t ld, uint64_t row) {
+    return (uint32_t)(((uintptr_t)p + row * ld * sizeof(T)) % 16 / sizeof(T));
+}
 
 template <int G>
 __device__ __forceinline__ float lanes_sum(float v) {
@@ -217,22 +247,23 @@ __device__ __forceinline__ float lanes_sum(float v) {
 }
 
 // G lanes of a warp per row, or (G = 0) the block; threads per row * NV * V >= cols
-template <typename T, int V, int NV, int G, int MAXT, int BLOCKS>
+template <typename T, int V, int NV, int G, int MAXT, int BLOCKS, bool SHIFT>
 __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm(const NormArgs a) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 warp_stats[2][32];
     constexpr int kQ = NV * V / 2;
     const uint32_t tpr = G ? G : blockDim.x, groups = blockDim.x / tpr, warps = blockDim.x >> 5;
-    const Place<V> at{threadIdx.x % tpr, tpr, (uint32_t)a.cols};
     const uint64_t step = (uint64_t)gridDim.x * groups;
     uint64_t base = (uint64_t)blockIdx.x * groups, row = base + threadIdx.x / tpr;
+    const Place<V, SHIFT> at{threadIdx.x % tpr, tpr, (uint32_t)a.cols, SHIFT ? shift_of<T>(a.x, a.ld_x, row) : 0};
     // columns of the row that the row's lanes, or warp `w` of the block, hold
     auto count_of = [&](uint32_t w) {
-        uint32_t n = 0;
+        int n = 0;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const uint32_t from = (i * tpr + w * 32) * V, to = from + (G ? G : 32) * V;
-            n += from < at.cols ? (to < at.cols ? to : at.cols) - from : 0;
+            const int start = (int)((i * tpr + w * 32) * V) - (SHIFT ? (int)at.shift : 0), from = max(start, 0);
+            const int to = min(start + (G ? G : 32) * V, (int)at.cols);
+            n += max(to - from, 0);
         }
         return (float)n;
     };
@@ -243,10 +274,10 @@ __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm(const NormArgs a) {
     F2 w[kQ], b[kQ];
 #pragma unroll
     for (int q = 0; q < kQ; ++q) {
-        w[q] = weights_of<V>(a.weight, a.w_type, 1.0f, q, at);
-        b[q] = weights_of<V>(a.bias, a.w_type, 0.0f, q, at);
+        w[q] = weights_of<V, SHIFT>(a.weight, a.w_type, 1.0f, q, at);
+        b[q] = weights_of<V, SHIFT>(a.bias, a.w_type, 0.0f, q, at);
     }
-    Rows<T, V, NV, 1> in{{(const T*)a.x}, {a.ld_x}, a.rows, at, (Pack<T, V>*)ring};
+    Rows<T, V, NV, 1, SHIFT> in{{(const T*)a.x}, {a.ld_x}, a.rows, at, (Pack<T, V>*)ring};
     in.start(row, step);
     uint32_t slot = 0, turn = 0;
     for (; base < a.rows; base += step, row += step, turn ^= 1) {             // every lane stays in the loop
@@ -261,10 +292,30 @@ __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm(const NormArgs a) {
         float mean = lanes_sum<G>(f.x + f.y) * part_inv;
         s = f2(0, 0);
         F2 minus = f2(-mean, -mean);
+        if constexpr (V == 1) {
 #pragma unroll
-        for (int q = 0; q < kQ; ++q) {
-            const F2 d = at.only(q, v[q] + minus);
-            s = fma2(d, d, s);
+            for (int q = 0; q < kQ; ++q) {
+                const F2 d = at.pair_only(q, v[q] + minus);
+                s = fma2(d, d, s);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                if (!at.in(i)) continue;
+                if (at.whole(i)) {
+#pragma unroll
+                    for (int j = 0; j < V / 2; ++j) {
+                        const F2 d = v[i * V / 2 + j] + minus;
+                        s = fma2(d, d, s);
+                    }
+                } else {                                  // a row's first or last access
+#pragma unroll
+                    for (int j = 0; j < V / 2; ++j) {
+                        const F2 d = at.pair_only(i * V / 2 + j, v[i * V / 2 + j] + minus);
+                        s = fma2(d, d, s);
+                    }
+                }
+            }
         }
         f = parts(s);
         float squares = lanes_sum<G>(f.x + f.y);
@@ -282,13 +333,13 @@ __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm(const NormArgs a) {
         const F2 scale = f2(rstd, rstd);
 #pragma unroll
         for (int q = 0; q < kQ; ++q) v[q] = fma2((v[q] + minus) * scale, w[q], b[q]);
-        store<T, V, NV>((T*)a.y + row * a.ld_y, v, at);
+        store<T, V, NV, SHIFT>((T*)a.y + row * a.ld_y, v, at);
         if (at.t == 0) {
             if (a.mean) a.mean[row] = mean;
             if (a.rstd) a.rstd[row] = rstd;
         }
     }
-    if constexpr (Rows<T, V, NV, 1>::kAsync) asm volatile("cp.async.wait_all;" ::: "memory");
+    if constexpr (Rows<T, V, NV, 1, SHIFT>::kAsync) asm volatile("cp.async.wait_all;" ::: "memory");
 }
 
 // Sums of a row over a block's threads (the long-row kernels)
@@ -340,25 +391,25 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_long(const NormArgs a) {
     }
 }
 
-template <typename T, int V, int NV, int G, int MAXT, int BLOCKS>
+template <typename T, int V, int NV, int G, int MAXT, int BLOCKS, bool SHIFT>
 __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm_backward(const NormBackwardArgs a) {
     extern __shared__ __align__(16) uint8_t ring[];
     __shared__ float2 warp_sums[2][32];
     __shared__ float gather[G ? kWarpThreads * NV * V : 1];
     constexpr int kQ = NV * V / 2;
     const uint32_t tpr = G ? G : blockDim.x, groups = blockDim.x / tpr, warps = blockDim.x >> 5;
-    const Place<V> at{threadIdx.x % tpr, tpr, (uint32_t)a.cols};
-    const float inv = 1.0f / (float)at.cols;
     const uint64_t step = (uint64_t)gridDim.x * groups;
     uint64_t base = (uint64_t)blockIdx.x * groups, row = base + threadIdx.x / tpr;
+    const Place<V, SHIFT> at{threadIdx.x % tpr, tpr, (uint32_t)a.cols, SHIFT ? shift_of<T>(a.x, a.ld_x, row) : 0};
+    const float inv = 1.0f / (float)at.cols;
     chain_acquire();
     F2 w[kQ], dw[kQ], db[kQ];
 #pragma unroll
     for (int q = 0; q < kQ; ++q) {
-        w[q] = weights_of<V>(a.weight, a.w_type, 1.0f, q, at);
+        w[q] = weights_of<V, SHIFT>(a.weight, a.w_type, 1.0f, q, at);
         dw[q] = db[q] = f2(0, 0);
     }
-    Rows<T, V, NV, 2> in{{(const T*)a.x, (const T*)a.dy}, {a.ld_x, a.ld_dy}, a.rows, at, (Pack<T, V>*)ring};
+    Rows<T, V, NV, 2, SHIFT> in{{(const T*)a.x, (const T*)a.dy}, {a.ld_x, a.ld_dy}, a.rows, at, (Pack<T, V>*)ring};
     in.start(row, step);
     uint32_t slot = 0, turn = 0;
     float next_mean = row < a.rows ? a.mean[row] : 0.0f, next_rstd = row < a.rows ? a.rstd[row] : 0.0f;
@@ -399,9 +450,9 @@ __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm_backward(const NormBackwa
         m2 *= -inv * rstd;
 #pragma unroll
         for (int q = 0; q < kQ; ++q) g[q] = fma2(g[q], scale, fma2(h[q], f2(m2, m2), f2(m1, m1)));
-        store<T, V, NV>((T*)a.dx + row * a.ld_dx, g, at);
+        store<T, V, NV, SHIFT>((T*)a.dx + row * a.ld_dx, g, at);
     }
-    if constexpr (Rows<T, V, NV, 2>::kAsync) asm volatile("cp.async.wait_all;" ::: "memory");
+    if constexpr (Rows<T, V, NV, 2, SHIFT>::kAsync) asm volatile("cp.async.wait_all;" ::: "memory");
     if (!a.partial) return;
     float* out = a.partial + (uint64_t)blockIdx.x * 2 * at.cols;
 #pragma unroll
@@ -417,7 +468,8 @@ __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm_backward(const NormBackwa
             const uint32_t width = G * NV * V;
             __syncthreads();
 #pragma unroll
-            for (int k = 0; k < NV * V; ++k) gather[(threadIdx.x / G) * width + at.col(k / V) + k % V] = mine[k];
+            for (int k = 0; k < NV * V; ++k)
+                if (at.valid(k / V, k % V)) gather[(threadIdx.x / G) * width + at.col(k / V) + k % V] = mine[k];
             __syncthreads();
             for (uint32_t c = threadIdx.x; c < at.cols; c += blockDim.x) {
                 float sum = 0;
@@ -427,7 +479,7 @@ __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm_backward(const NormBackwa
         } else {
 #pragma unroll
             for (int k = 0; k < NV * V; ++k)
-                if (at.in(k / V)) out[(uint64_t)which * at.cols + at.col(k / V) + k % V] = mine[k];
+                if (at.valid(k / V, k % V)) out[(uint64_t)which * at.cols + at.col(k / V) + k % V] = mine[k];
         }
     }
 }
@@ -510,8 +562,8 @@ uint32_t norm_blocks(uint64_t rows, const NormPlan& p, int sm_count, uint32_t th
     const uint64_t per_sm = threads_per_sm / threads < 1 ? 1 : threads_per_sm / threads < 24 ? threads_per_sm / threads : 24;
     const uint64_t most = (uint64_t)sm_count * per_sm;
     if (want <= most) return (uint32_t)(want ? want : 1);
-    const uint64_t rounds = (want + most - 1) / most;
-    return (uint32_t)((want + rounds - 1) / rounds);
+    const uint64_t rounds = (want + most - 1) / most, even = round_up((want + rounds - 1) / rounds, 8);
+    return (uint32_t)(even <= most ? even : most / 8 * 8);       // a multiple of eight: a thread's rows are whole 16-byte steps apart
 }
 
 template <auto kernel, typename Args>
@@ -523,22 +575,30 @@ cudaError_t launch_rows(dim3 grid, uint32_t threads, uint32_t smem, cudaStream_t
     return launch_kernel(true, kernel, grid, threads, smem, st, a);
 }
 
-template <typename T, int V, int PER, int G, int MAXT, int BLOCKS>
+template <typename T, int V, bool SHIFT, int PER, int G, int MAXT, int BLOCKS>
 cudaError_t run_norm(const NormArgs& a, const NormPlan& p, int sm_count, cudaStream_t st) {
-    return launch_rows<k_norm<T, V, PER / V, G, MAXT, BLOCKS>>(dim3(norm_blocks(a.rows, p, sm_count, MAXT * BLOCKS)), p.threads,
-                                                               Rows<T, V, PER / V, 1>::smem(p.threads), st, a);
+    return launch_rows<k_norm<T, V, PER / V, G, MAXT, BLOCKS, SHIFT>>(dim3(norm_blocks(a.rows, p, sm_count, MAXT * BLOCKS)), p.threads,
+                                                                      Rows<T, V, PER / V, 1, SHIFT>::smem(p.threads), st, a);
 }
-template <typename T, int V>
+template <typename T, int V, bool SHIFT>
 int norm_typed(const NormArgs& a, int sm_count, cudaStream_t st) {
+    constexpr uint32_t kMost = V > 1 ? 32 : 8;                   // values a lane holds; single elements would take too many registers
+    const uint64_t cols = a.cols + (SHIFT ? V - 1 : 0);
     cudaError_t e;
-    NormPlan p = plan_lanes(a.cols, V > 1 ? 32 : 8);
-    if (p.lanes == 8) e = run_norm<T, V, 8, 8, kWarpThreads, 8>(a, p, sm_count, st);
-    else if (p.per == 8) e = run_norm<T, V, 8, 32, kWarpThreads, 8>(a, p, sm_count, st);
-    else if (V > 1 && p.per == 16) e = run_norm<T, V, 16, 32, kWarpThreads, 6>(a, p, sm_count, st);
-    else if (V > 1 && p.per == 32) e = run_norm<T, V, 32, 32, kWarpThreads, 4>(a, p, sm_count, st);
-    else if (V > 1 && (p = plan_block(a.cols, 32, 256)).threads) e = run_norm<T, V, 32, 0, 256, 2>(a, p, sm_count, st);
-    else if ((p = plan_block(a.cols, 16, 256)).threads) e = run_norm<T, V, 16, 0, 256, 3>(a, p, sm_count, st);
-    else if ((p = plan_block(a.cols, 16, 1024)).threads) e = run_norm<T, V, 16, 0, 1024, 1>(a, p, sm_count, st);
+    NormPlan p = plan_lanes(cols, kMost);
+    if constexpr (V > 1) {
+        if (p.per == 16 || p.per == 32 || (!p.threads && (p = plan_block(cols, 32, 256)).threads)) {
+            if (p.per == 16) e = run_norm<T, V, SHIFT, 16, 32, kWarpThreads, 6>(a, p, sm_count, st);
+            else if (p.lanes) e = run_norm<T, V, SHIFT, 32, 32, kWarpThreads, 4>(a, p, sm_count, st);
+            else e = run_norm<T, V, SHIFT, 32, 0, 256, 2>(a, p, sm_count, st);
+            SK_OP_CUDA(e);
+            return SK_OK;
+        }
+    }
+    if (p.lanes == 8) e = run_norm<T, V, SHIFT, 8, 8, kWarpThreads, 8>(a, p, sm_count, st);
+    else if (p.lanes) e = run_norm<T, V, SHIFT, 8, 32, kWarpThreads, 8>(a, p, sm_count, st);
+    else if ((p = plan_block(cols, 16, 256)).threads) e = run_norm<T, V, SHIFT, 16, 0, 256, 3>(a, p, sm_count, st);
+    else if ((p = plan_block(cols, 16, 1024)).threads) e = run_norm<T, V, SHIFT, 16, 0, 1024, 1>(a, p, sm_count, st);
     else e = launch_rows<k_norm_long<T>>(dim3(norm_blocks(a.rows, p, sm_count, 2048)), kLongThreads, 0, st, a);
     SK_OP_CUDA(e);
     return SK_OK;
@@ -550,23 +610,20 @@ NormPlan plan_backward(uint64_t cols) {
     if (!p.threads) p = plan_block(cols, 16, 512);
     return p;
 }
-uint32_t backward_blocks(uint64_t rows, uint64_t cols, int sm_count) {
-    const NormPlan p = plan_backward(cols);
-    return norm_blocks(rows, p, sm_count, p.threads && p.per == 8 ? 768 : 512);
-}
-template <typename T, int V, int PER, int G, int MAXT, int BLOCKS>
+uint32_t backward_blocks(uint64_t rows, const NormPlan& p, int sm_count) { return norm_blocks(rows, p, sm_count, p.threads && p.per == 8 ? 768 : 512); }
+template <typename T, int V, bool SHIFT, int PER, int G, int MAXT, int BLOCKS>
 cudaError_t run_backward(const NormBackwardArgs& a, const NormPlan& p, uint32_t blocks, cudaStream_t st) {
-    return launch_rows<k_norm_backward<T, V, PER / V, G, MAXT, BLOCKS>>(dim3(blocks), p.threads, Rows<T, V, PER / V, 2>::smem(p.threads), st, a);
+    return launch_rows<k_norm_backward<T, V, PER / V, G, MAXT, BLOCKS, SHIFT>>(dim3(blocks), p.threads, Rows<T, V, PER / V, 2, SHIFT>::smem(p.threads), st, a);
 }
-template <typename T, int V>
+template <typename T, int V, bool SHIFT>
 int norm_backward_typed(const NormBackwardArgs& a, int sm_count, cudaStream_t st) {
-    const NormPlan p = plan_backward(a.cols);
-    const uint32_t blocks = backward_blocks(a.rows, a.cols, sm_count);
+    const NormPlan p = plan_backward(a.cols + (SHIFT ? V - 1 : 0));
+    const uint32_t blocks = backward_blocks(a.rows, p, sm_count);
     cudaError_t e;
-    if (p.lanes == 8) e = run_backward<T, V, 8, 8, kWarpThreads, 6>(a, p, blocks, st);
-    else if (p.lanes == 32 && p.per == 8) e = run_backward<T, V, 8, 32, kWarpThreads, 6>(a, p, blocks, st);
-    else if (p.lanes == 32) e = run_backward<T, V, 16, 32, kWarpThreads, 4>(a, p, blocks, st);
-    else if (p.threads) e = run_backward<T, V, 16, 0, 512, 1>(a, p, blocks, st);
+    if (p.lanes == 8) e = run_backward<T, V, SHIFT, 8, 8, kWarpThreads, 6>(a, p, blocks, st);
+    else if (p.lanes == 32 && p.per == 8) e = run_backward<T, V, SHIFT, 8, 32, kWarpThreads, 6>(a, p, blocks, st);
+    else if (p.lanes == 32) e = run_backward<T, V, SHIFT, 16, 32, kWarpThreads, 4>(a, p, blocks, st);
+    else if (p.threads) e = run_backward<T, V, SHIFT, 16, 0, 512, 1>(a, p, blocks, st);
     else e = launch_rows<k_norm_backward_long<T>>(dim3(blocks), kLongThreads, 0, st, a);
     SK_OP_CUDA(e);
     if (a.partial) {
@@ -577,40 +634,55 @@ int norm_backward_typed(const NormBackwardArgs& a, int sm_count, cudaStream_t st
     return SK_OK;
 }
 
-// The widest access, in elements, that starts and ends every row of a matrix on its boundary
-int widest(const void* p, uint64_t ld, uint64_t cols, uint32_t size) {
-    int v = (int)(16 / size);
-    while (v > 1 && (cols % v || ld % v || (uintptr_t)p % (v * size))) v /= 2;
-    return v;
+// How the rows of up to three matrices are accessed together: 2, whole 16-byte accesses; 1, 16-byte accesses that begin before the
+// row (the matrices' rows lie alike to the boundary); 0, single elements.  The first and the last access of a row cost more where they are
+// not whole, which short rows do not win back: 65536 x 221 bf16 took 34 us so and takes 24 us by elements (backward 37, 28), 16384 x 4097
+// 83 and 184 (156, 409).
+struct Placed { const void* p; uint64_t ld; };
+int access_of(uint64_t cols, uint32_t size, Placed x, Placed y, Placed z) {
+    const uint64_t v = 16 / size;
+    bool whole = cols % v == 0, alike = true;
+    for (const Placed& m : {x, y, z}) {
+        if (!m.p) continue;
+        whole = whole && m.ld % v == 0 && (uintptr_t)m.p % 16 == 0;
+        alike = alike && m.ld % v == x.ld % v && (uintptr_t)m.p % 16 == (uintptr_t)x.p % 16;
+    }
+    return whole ? 2 : alike && cols > 256 ? 1 : 0;
+}
+template <typename T>
+int norm_placed(const NormArgs& a, int sm_count, cudaStream_t st) {
+    constexpr int kV = 16 / sizeof(T);
+    const int access = access_of(a.cols, sizeof(T), {a.x, a.ld_x}, {a.y, a.ld_y}, {nullptr, 0});
+    return access == 2 ? norm_typed<T, kV, false>(a, sm_count, st) : access == 1 ? norm_typed<T, kV, true>(a, sm_count, st) : norm_typed<T, 1, false>(a, sm_count, st);
+}
+template <typename T>
+int norm_backward_placed(const NormBackwardArgs& a, int sm_count, cudaStream_t st) {
+    constexpr int kV = 16 / sizeof(T);
+    const int access = access_of(a.cols, sizeof(T), {a.x, a.ld_x}, {a.dy, a.ld_dy}, {a.dx, a.ld_dx});
+    return access == 2   ? norm_backward_typed<T, kV, false>(a, sm_count, st)
+           : access == 1 ? norm_backward_typed<T, kV, true>(a, sm_count, st)
+                         : norm_backward_typed<T, 1, false>(a, sm_count, st);
 }
 
 }  // namespace
 
 int launch_norm(const NormArgs& a, int sm_count, cudaStream_t st) {
-    const uint32_t size = type_size(a.type);
-    const int vx = widest(a.x, a.ld_x, a.cols, size), vy = widest(a.y, a.ld_y, a.cols, size), v = vx < vy ? vx : vy;
-    if (a.type == SK_F32) return v == 4 ? norm_typed<float, 4>(a, sm_count, st) : norm_typed<float, 1>(a, sm_count, st);
-    if (a.type == SK_BF16)
-        return v == 8 ? norm_typed<__nv_bfloat16, 8>(a, sm_count, st) : v >= 2 ? norm_typed<__nv_bfloat16, 2>(a, sm_count, st)
-                                                                              : norm_typed<__nv_bfloat16, 1>(a, sm_count, st);
-    return v == 8 ? norm_typed<__half, 8>(a, sm_count, st) : v >= 2 ? norm_typed<__half, 2>(a, sm_count, st) : norm_typed<__half, 1>(a, sm_count, st);
+    return a.type == SK_F32 ? norm_placed<float>(a, sm_count, st) : a.type == SK_BF16 ? norm_placed<__nv_bfloat16>(a, sm_count, st) : norm_placed<__half>(a, sm_count, st);
 }
 
 int launch_norm_backward(const NormBackwardArgs& a, int sm_count, cudaStream_t st) {
-    const uint32_t size = type_size(a.type);
-    const int vx = widest(a.x, a.ld_x, a.cols, size), vd = widest(a.dy, a.ld_dy, a.cols, size);
-    int v = vx < vd ? vx : vd;
-    if (a.dx) v = min(v, widest(a.dx, a.ld_dx, a.cols, size));
-    if (a.type == SK_F32) return v == 4 ? norm_backward_typed<float, 4>(a, sm_count, st) : norm_backward_typed<float, 1>(a, sm_count, st);
-    if (a.type == SK_BF16)
-        return v == 8 ? norm_backward_typed<__nv_bfloat16, 8>(a, sm_count, st) : v >= 2 ? norm_backward_typed<__nv_bfloat16, 2>(a, sm_count, st)
-                                                                                       : norm_backward_typed<__nv_bfloat16, 1>(a, sm_count, st);
-    return v == 8 ? norm_backward_typed<__half, 8>(a, sm_count, st) : v >= 2 ? norm_backward_typed<__half, 2>(a, sm_count, st)
-                                                                            : norm_backward_typed<__half, 1>(a, sm_count, st);
+    return a.type == SK_F32    ? norm_backward_placed<float>(a, sm_count, st)
+           : a.type == SK_BF16 ? norm_backward_placed<__nv_bfloat16>(a, sm_count, st)
+                               : norm_backward_placed<__half>(a, sm_count, st);
 }
 
 uint64_t norm_backward_workspace(uint64_t rows, uint64_t cols, int sm_count) {
-    return (uint64_t)backward_blocks(rows, cols, sm_count) * 2 * cols * sizeof(float);
+    uint32_t most = 0;                           // the rows' alignment decides between the plans: room for any
+    for (uint64_t extra : {0, 3, 7}) {
+        const uint32_t blocks = backward_blocks(rows, plan_backward(cols + extra), sm_count);
+        most = blocks > most ? blocks : most;
+    }
+    return (uint64_t)most * 2 * cols * sizeof(float);
 }
 
 }  // namespace sk

@@ -29,13 +29,16 @@ _raw_stream = torch._C._cuda_getCurrentRawStream
 # ---- checks ---------------------------------------------------------------------------------------------------------------
 def _tensor(t, name, types, device=None):
     """The type's code; the tensor is on `device` (an index) if given, else on any CUDA device."""
-    if not isinstance(t, torch.Tensor) or not t.is_cuda:
+    try:
+        code, where = types[t.dtype], t.get_device()
+    except (AttributeError, KeyError):
+        if not isinstance(t, torch.Tensor):
+            raise SkError(f"{name} must be a CUDA tensor") from None
+        raise SkError(f"{name}: type {t.dtype} is not supported here") from None
+    if where < 0:
         raise SkError(f"{name} must be a CUDA tensor")
-    if device is not None and t.get_device() != device:
-        raise SkError(f"{name} is on device {t.get_device()}, not on {device}")
-    code = types.get(t.dtype)
-    if code is None:
-        raise SkError(f"{name}: type {t.dtype} is not supported here")
+    if device is not None and where != device:
+        raise SkError(f"{name} is on device {where}, not on {device}")
     return code
 
 
@@ -118,17 +121,15 @@ def _norm_weights(weight, bias, cols, device):
     """The weights' common type and their addresses."""
     if cols < 1:
         raise SkError("the last axis must not be empty")
-    code, pw, pb = 0, None, None
+    pw = pb = None
     if weight is not None:
-        code = _tensor(weight, "weight", _TYPES, device)
         pw = _vector(weight, "weight", cols, _TYPES, device)
     if bias is not None:
-        other = _tensor(bias, "bias", _TYPES, device)
-        if weight is not None and other != code:
+        if weight is not None and bias.dtype != weight.dtype:
             raise SkError(f"bias has type {bias.dtype}, weight {weight.dtype}")
-        code = other
         pb = _vector(bias, "bias", cols, _TYPES, device)
-    return code, pw, pb
+    first = weight if weight is not None else bias
+    return (0 if first is None else _TYPES[first.dtype]), pw, pb
 
 
 def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
@@ -148,7 +149,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
             raise SkError(f"out has type {out.dtype}, x {x.dtype}")
         _same_shape(out, x, "out")
         y, ld_y = out, _rows(out, "out")[1]
-    mean, rstd = x.new_empty(shape[:-1], dtype=torch.float32), x.new_empty(shape[:-1], dtype=torch.float32)
+    mean = x.new_empty(shape[:-1], dtype=torch.float32)
+    rstd = torch.empty_like(mean)
     _on(stream, y, mean, rstd)
     _run(device, lib().sk_layer_norm, x.data_ptr(), ld, y.data_ptr(), ld_y, code, rows, shape[-1], pw, pb, wcode, eps, mean.data_ptr(),
          rstd.data_ptr(), _pointer_of(stream, device))
@@ -214,7 +216,8 @@ def linear_cross_entropy(hidden, weight, targets, stream=None):
     """Softmax cross entropy of the logits hidden weight^T, which are never stored.  hidden: (tokens, width), weight: (vocab, width),
     both bf16 or both fp16; targets: (tokens,) int64, negative = the token takes no part.  Returns (loss, lse), fp32 (tokens,)."""
     device, code, tokens, vocab, width, ld_h, ld_w, pt = _head(hidden, weight, targets)
-    loss, lse = hidden.new_empty((tokens,), dtype=torch.float32), hidden.new_empty((tokens,), dtype=torch.float32)
+    loss = hidden.new_empty((tokens,), dtype=torch.float32)
+    lse = torch.empty_like(loss)
     ph, pw = hidden.data_ptr(), weight.data_ptr()
     need = lib().sk_linear_cross_entropy_workspace(ph, ld_h, pw, ld_w, tokens, vocab, width)
     ws = _workspace(hidden, need)
