@@ -605,26 +605,33 @@ int norm_typed(const NormArgs& a, int sm_count, cudaStream_t st) {
 }
 
 // The plan decides how many partial rows there are, so the workspace's size needs it too.
-NormPlan plan_backward(uint64_t cols) {
+// wide16: 16-bit rows by 16-byte accesses, of which a lane holds three before warps share a row (16384 x 768 bf16: 17.5 us, 21.2 with
+// two warps a row; fp32 rows, as many bytes in flight, are at the memory's rate either way).
+NormPlan plan_backward(uint64_t cols, bool wide16) {
     NormPlan p = plan_lanes(cols, 16);
+    if (!p.threads && wide16 && cols <= 768) p = {32, kWarpThreads, 24};
     if (!p.threads) p = plan_block(cols, 16, 512);
     return p;
 }
-uint32_t backward_blocks(uint64_t rows, const NormPlan& p, int sm_count) { return norm_blocks(rows, p, sm_count, p.threads && p.per == 8 ? 768 : 512); }
+uint32_t backward_blocks(uint64_t rows, const NormPlan& p, int sm_count) { return norm_blocks(rows, p, sm_count, p.per == 8 ? 768 : p.per == 24 ? 384 : 512); }
 template <typename T, int V, bool SHIFT, int PER, int G, int MAXT, int BLOCKS>
 cudaError_t run_backward(const NormBackwardArgs& a, const NormPlan& p, uint32_t blocks, cudaStream_t st) {
     return launch_rows<k_norm_backward<T, V, PER / V, G, MAXT, BLOCKS, SHIFT>>(dim3(blocks), p.threads, Rows<T, V, PER / V, 2, SHIFT>::smem(p.threads), st, a);
 }
 template <typename T, int V, bool SHIFT>
 int norm_backward_typed(const NormBackwardArgs& a, int sm_count, cudaStream_t st) {
-    const NormPlan p = plan_backward(a.cols + (SHIFT ? V - 1 : 0));
+    constexpr bool kWide16 = V == 8;
+    const NormPlan p = plan_backward(a.cols + (SHIFT ? V - 1 : 0), kWide16);
     const uint32_t blocks = backward_blocks(a.rows, p, sm_count);
-    cudaError_t e;
+    cudaError_t e = cudaSuccess;
+    if constexpr (kWide16) {
+        if (p.per == 24) e = run_backward<T, V, SHIFT, 24, 32, kWarpThreads, 3>(a, p, blocks, st);
+    }
     if (p.lanes == 8) e = run_backward<T, V, SHIFT, 8, 8, kWarpThreads, 6>(a, p, blocks, st);
     else if (p.lanes == 32 && p.per == 8) e = run_backward<T, V, SHIFT, 8, 32, kWarpThreads, 6>(a, p, blocks, st);
-    else if (p.lanes == 32) e = run_backward<T, V, SHIFT, 16, 32, kWarpThreads, 4>(a, p, blocks, st);
-    else if (p.threads) e = run_backward<T, V, SHIFT, 16, 0, 512, 1>(a, p, blocks, st);
-    else e = launch_rows<k_norm_backward_long<T>>(dim3(blocks), kLongThreads, 0, st, a);
+    else if (p.lanes == 32 && p.per == 16) e = run_backward<T, V, SHIFT, 16, 32, kWarpThreads, 4>(a, p, blocks, st);
+    else if (p.threads && !p.lanes) e = run_backward<T, V, SHIFT, 16, 0, 512, 1>(a, p, blocks, st);
+    else if (!p.threads) e = launch_rows<k_norm_backward_long<T>>(dim3(blocks), kLongThreads, 0, st, a);
     SK_OP_CUDA(e);
     if (a.partial) {
         e = launch_kernel(true, k_norm_sum, dim3((uint32_t)((2 * a.cols + 7) / 8)), 256, 0, st, a.partial, blocks, (uint32_t)a.cols, a.dweight, a.dbias,
@@ -678,10 +685,11 @@ int launch_norm_backward(const NormBackwardArgs& a, int sm_count, cudaStream_t s
 
 uint64_t norm_backward_workspace(uint64_t rows, uint64_t cols, int sm_count) {
     uint32_t most = 0;                           // the rows' alignment decides between the plans: room for any
-    for (uint64_t extra : {0, 3, 7}) {
-        const uint32_t blocks = backward_blocks(rows, plan_backward(cols + extra), sm_count);
-        most = blocks > most ? blocks : most;
-    }
+    for (uint64_t extra : {0, 3, 7})
+        for (bool wide16 : {false, true}) {
+            const uint32_t blocks = backward_blocks(rows, plan_backward(cols + extra, wide16), sm_count);
+            most = blocks > most ? blocks : most;
+        }
     return (uint64_t)most * 2 * cols * sizeof(float);
 }
 

@@ -546,3 +546,17 @@ def test_workspaces_are_checked():
     assert L.sk_layer_norm(u.data_ptr() + 2, 64, u.data_ptr(), 64, 0, 4, 64, None, None, 0, 1e-5, None, None, None) == -1
     assert L.sk_layer_norm(None, 64, u.data_ptr(), 64, 0, 4, 64, None, None, 0, 1e-5, None, None, None) == -1
     torch.cuda.synchronize()
+
+
+# ---- together ----------------------------------------------------------------------------------------------------------------
+def test_the_example_learns():
+    """The example trains with every operator and the compressed step; the loss falls well below that of a uniform guess."""
+    import importlib.util
+    import os
+    from conftest import ROOT
+    spec = importlib.util.spec_from_file_location("language_model", os.path.join(ROOT, "examples", "language_model.py"))
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    losses = example.train(steps=80)
+    assert all(math.isfinite(v) for v in losses)
+    assert losses[-1] < min(losses[0], math.log(1024)) - 1.0
