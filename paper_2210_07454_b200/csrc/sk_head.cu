@@ -58,8 +58,15 @@ struct StatsEpi {
         }
         // the difference first: it is exact near the maximum, whatever the logits' size
         const float off = top == -INFINITY ? 0.0f : top;
+        const F2 minus = f2(-off, -off), log2e = f2(kLog2e, kLog2e);
+        F2 s = f2(0, 0);
 #pragma unroll
-        for (int i = 0; i < 32; ++i) sum += exp2_fast((v[i] - off) * kLog2e);
+        for (int i = 0; i < 16; ++i) {
+            const float2 e = parts((f2(v[2 * i], v[2 * i + 1]) + minus) * log2e);
+            s = s + f2(exp2_fast(e.x), exp2_fast(e.y));
+        }
+        const float2 both = parts(s);
+        sum += both.x + both.y;
     }
     __device__ void end() {
         if (row < t.M) a.part[(uint64_t)slot * t.M + row] = make_float2(top, sum);
@@ -137,14 +144,23 @@ struct GradEpi {
         if (!rows) return;
         const uint64_t d = (uint64_t)(target - (int64_t)col);
         if (scale != 0.0f) {
+            const F2 minus = f2(-off, -off), log2e = f2(kLog2e, kLog2e), by = f2(scale, scale);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = exp2_fast((v[i] - off) * kLog2e);
+            for (int i = 0; i < 16; ++i) {
+                const float2 e = parts((f2(v[2 * i], v[2 * i + 1]) + minus) * log2e);
+                v[2 * i] = exp2_fast(e.x);
+                v[2 * i + 1] = exp2_fast(e.y);
+            }
             if (d < 32) {
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] -= d == (uint64_t)i ? 1.0f : 0.0f;
             }
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= scale;
+            for (int i = 0; i < 16; ++i) {
+                const float2 g = parts(f2(v[2 * i], v[2 * i + 1]) * by);
+                v[2 * i] = g.x;
+                v[2 * i + 1] = g.y;
+            }
         } else {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] = 0.0f;

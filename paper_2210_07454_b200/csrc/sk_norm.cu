@@ -25,26 +25,6 @@ namespace {
 constexpr int kDepth = 3;                        // rows of the ring
 constexpr int kWarpThreads = 128;                // block of the kernels with several groups of lanes to a block
 
-// ---- pairs of 32-bit values ---------------------------------------------------------------------------------------------
-struct F2 { unsigned long long v; };
-__device__ __forceinline__ F2 f2(float x, float y) {
-    F2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ float2 parts(F2 a) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
-    return r;
-}
-__device__ __forceinline__ F2 operator+(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 operator*(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
-__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
-    F2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
-    return r;
-}
-
 // ---- a thread's elements of a row: NV accesses of V neighbours, in NV * V / 2 pairs (of accesses where V is 1) ---------------
 template <typename T, int V>
 struct alignas(sizeof(T) * V) Pack { T v[V]; };

@@ -68,6 +68,26 @@ __device__ __forceinline__ void load32b(const void* p, uint32_t* r) {
                  "=r"(r[6]), "=r"(r[7]) : "l"(p) : "memory");
 }
 
+// ---- pairs of 32-bit values ---------------------------------------------------------------------------------------------
+struct F2 { unsigned long long v; };
+__device__ __forceinline__ F2 f2(float x, float y) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 parts(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a.v));
+    return r;
+}
+__device__ __forceinline__ F2 operator+(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 operator*(F2 a, F2 b) { F2 r; asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v)); return r; }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+
 // What is known of an output's rows: the largest of 16, 4 and 2 bytes that every row starts on
 inline uint32_t row_alignment(const void* p, uint64_t ld, int type) {
     const uint64_t bits = (uintptr_t)p | ld * type_size(type);
