@@ -5,15 +5,18 @@
 //
 // Bound by memory: forward reads x and writes y once, backward reads x and dy and writes dx once.  A row belongs to 8 or 32
 // lanes of a warp or to a block, every thread to fixed columns.  What keeps the memory busy is a ring of rows in
-// shared memory that each thread fills for itself with asynchronous copies (its own columns only, so no barrier guards it): the next
-// rows travel while one is worked on, without holding registers.  Rows of odd lengths do so too, with accesses that
-// begin before the row (Place); only matrices whose rows lie differently to the 16-byte boundary come element by element, through registers.  The arithmetic is two values to an instruction
-// (f32x2): with one the kernels are bound by issue (bf16 rows then take as long as fp32 ones).
+// shared memory that each thread fills for itself with asynchronous copies (its own columns only, so no barrier guards
+// it): the next rows travel while one is worked on, without holding registers.  Rows of odd lengths do so too, with accesses
+// that begin before the row (Place); only matrices whose rows lie differently to the 16-byte boundary come element by element,
+// 16-bit ones through registers.  The arithmetic is two values to an instruction (f32x2): with one the kernels are bound by
+// issue (bf16 rows then take as long as fp32 ones).  Measured: 32768 x 4096 bf16 87 us forward (6.15 TB/s), 141 us backward (5.7);
+// 32768 x 4096 fp32 166 and 244 us (6.5, 6.6 TB/s); weights read for every row from L1 instead of registers cost 274 us in the first.
 //
 // Statistics: a warp computes the mean of its part and the squares around that, and the parts are joined by the formula for
 // the variance of a union: nothing cancels whatever the mean, and warps meet once per row.  In the backward pass the sums of
 // dw and db stay in registers, and every block writes one partial row of them that a second, column-parallel kernel adds
-// up in a fixed order: no atomics, the same bits every time.  All statistics and sums are 32-bit.
+// up in a fixed order (for few rows extra blocks form them instead): no atomics, the same bits every time.  All
+// statistics and sums are 32-bit.
 #include "sk_chain.cuh"
 #include "sk_operators.h"
 
@@ -371,6 +374,40 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_long(const NormArgs a) {
     }
 }
 
+// dw and db of eight columns over all rows, threads / 8 rows at a time: for few rows, as extra blocks of the row kernel's launch.
+// They read x and dy a second time, from L2, and need neither partial rows nor a kernel after them.
+template <typename T>
+__device__ void norm_columns(const NormBackwardArgs& a, uint32_t slab, float2 (*sums)[8]) {
+    const uint32_t x = threadIdx.x & 7, y = threadIdx.x >> 3, groups = blockDim.x >> 3;
+    const uint64_t c = (uint64_t)slab * 8 + x;
+    const bool live = c < a.cols;
+    const T *px = (const T*)a.x + c, *pd = (const T*)a.dy + c;
+    float2 s = make_float2(0, 0);
+    if (live) {
+#pragma unroll 8
+        for (uint32_t r = y; r < (uint32_t)a.rows; r += groups) {
+            const float d = to_float(pd[r * a.ld_dy]), h = (to_float(px[r * a.ld_x]) - a.mean[r]) * a.rstd[r];
+            s.x += d * h;
+            s.y += d;
+        }
+    }
+#pragma unroll
+    for (int o = 8; o < 32; o *= 2) {
+        s.x += __shfl_xor_sync(0xffffffffu, s.x, o);
+        s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
+    }
+    if ((threadIdx.x & 31) < 8) sums[threadIdx.x >> 5][x] = s;
+    __syncthreads();
+    if (threadIdx.x < 8 && live) {
+        for (uint32_t w = 1; w < (blockDim.x >> 5); ++w) {
+            s.x += sums[w][x].x;
+            s.y += sums[w][x].y;
+        }
+        if (a.dweight) store_as(a.dweight, a.dw_type, c, s.x);
+        if (a.dbias) store_as(a.dbias, a.dw_type, c, s.y);
+    }
+}
+
 template <typename T, int V, int NV, int G, int MAXT, int BLOCKS, bool SHIFT>
 __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm_backward(const NormBackwardArgs a) {
     extern __shared__ __align__(16) uint8_t ring[];
@@ -378,11 +415,16 @@ __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm_backward(const NormBackwa
     __shared__ float gather[G ? kWarpThreads * NV * V : 1];
     constexpr int kQ = NV * V / 2;
     const uint32_t tpr = G ? G : blockDim.x, groups = blockDim.x / tpr, warps = blockDim.x >> 5;
-    const uint64_t step = (uint64_t)gridDim.x * groups;
+    const uint64_t step = (uint64_t)(gridDim.x - a.slabs) * groups;
     uint64_t base = (uint64_t)blockIdx.x * groups, row = base + threadIdx.x / tpr;
     const Place<V, SHIFT> at{threadIdx.x % tpr, tpr, (uint32_t)a.cols, SHIFT ? shift_of<T>(a.x, a.ld_x, row) : 0};
     const float inv = 1.0f / (float)at.cols;
     chain_acquire();
+    if (blockIdx.x >= gridDim.x - a.slabs) {
+        __shared__ float2 sums[MAXT / 32][8];
+        norm_columns<T>(a, blockIdx.x - (gridDim.x - a.slabs), sums);
+        return;
+    }
     F2 w[kQ], dw[kQ], db[kQ];
 #pragma unroll
     for (int q = 0; q < kQ; ++q) {
@@ -548,7 +590,7 @@ uint32_t norm_blocks(uint64_t rows, const NormPlan& p, int sm_count, uint32_t th
 
 template <auto kernel, typename Args>
 cudaError_t launch_rows(dim3 grid, uint32_t threads, uint32_t smem, cudaStream_t st, const Args& a) {
-    if (smem > 40 * 1024) {                      // with the kernel's own arrays, beyond what needs no permission
+    if (smem > 24 * 1024) {                      // with the kernel's own arrays, perhaps beyond what needs no permission
         const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
     }
@@ -584,6 +626,10 @@ int norm_typed(const NormArgs& a, int sm_count, cudaStream_t st) {
     return SK_OK;
 }
 
+// Up to so many rows dw and db come from extra blocks of the one launch: 16 x 768 bf16 2.8 us against 6.4 with partial rows and a second kernel,
+// 128 x 4096 7.5 and 11.5, 256 x 768 7.7 and 7.2, 512 x 768 12.1 and 7.8 (beside which the second launch and the
+// workspace cost the host some 5 us).
+constexpr uint64_t kSlabRows = 256;
 // The plan decides how many partial rows there are, so the workspace's size needs it too.
 // wide16: 16-bit rows by 16-byte accesses, of which a lane holds three before warps share a row (16384 x 768 bf16: 17.5 us, 21.2 with
 // two warps a row; fp32 rows, as many bytes in flight, are at the memory's rate either way).
@@ -602,7 +648,7 @@ template <typename T, int V, bool SHIFT>
 int norm_backward_typed(const NormBackwardArgs& a, int sm_count, cudaStream_t st) {
     constexpr bool kWide16 = V == 8;
     const NormPlan p = plan_backward(a.cols + (SHIFT ? V - 1 : 0), kWide16);
-    const uint32_t blocks = backward_blocks(a.rows, p, sm_count);
+    const uint32_t blocks = backward_blocks(a.rows, p, sm_count) + a.slabs;
     cudaError_t e = cudaSuccess;
     if constexpr (kWide16) {
         if (p.per == 24) e = run_backward<T, V, SHIFT, 24, 32, kWarpThreads, 3>(a, p, blocks, st);
@@ -663,7 +709,11 @@ int launch_norm_backward(const NormBackwardArgs& a, int sm_count, cudaStream_t s
                                : norm_backward_placed<__half>(a, sm_count, st);
 }
 
+// Extra blocks for dw and db (norm_columns), where they beat the partial rows and the second kernel: few rows, that L2 holds.
+uint32_t norm_backward_slabs(uint64_t rows, uint64_t cols) { return rows <= kSlabRows && cols <= 8192 ? (uint32_t)((cols + 7) / 8) : 0; }
+
 uint64_t norm_backward_workspace(uint64_t rows, uint64_t cols, int sm_count) {
+    if (norm_backward_slabs(rows, cols)) return 0;
     uint32_t most = 0;                           // the rows' alignment decides between the plans: room for any
     for (uint64_t extra : {0, 3, 7})
         for (bool wide16 : {false, true}) {

@@ -29,8 +29,10 @@ constexpr uint32_t kPadCols = 32;                                // leading dime
 // ---- all products of the iteration in one launch --------------------------------------------------------------------------
 // The tiles of A = X X^T (0), P = a I + b A + c A^2 (1) and X <- P X (2) of all steps and matrices, in this order, dealt out to the units in
 // turn.  A tile may start when all tiles of the products before it of ITS matrix are written: a counter per matrix says how many epilogue
-// warps have written theirs.  Waiting for a matrix instead of for everything keeps the units busy across the products' ends: with a
-// launch per product 12 matrices of 768 x 768 took 282 us (108 tiles of X on 74 pairs are two waves, and every launch costs some 4 us).
+// warps have written theirs.  Waiting for a matrix instead of for everything keeps the units busy across the products' ends: 12 matrices of
+// 768 x 768 take 200 us, with a launch per product 252.  What a product costs beside its stages of some 620 cycles: 1500 cycles from the first
+// copy's issue to its arrival, 600 from the last product to the accumulator, 2000 (128 columns) to 7000 (256, mirrored) in the
+// epilogue, 1100 to 2400 until its stores are seen, and as much again until the counter is read.
 // A unit takes its tiles in order, every tile waits for earlier ones only, and the blocks are all resident (a cooperative launch): so the waits
 // end; they have a limit all the same.
 struct ChainPlan {
@@ -406,14 +408,15 @@ OrthoLayout layout_of(const OrthoArgs& a) {
 }
 
 // ---- the whole iteration in one launch --------------------------------------------------------------------------------
-// Matrices whose shorter side is at most 128 (Y: m x n, m <= 128, the update or its transpose) and whose longer one is at most 8 * 256: fifteen
+// Matrices whose shorter side is at most 128 (Y: m x n, m <= 128, the update or its transpose) and whose longer one is at most 16 * 256: fifteen
 // dependent products of microseconds each are all launch latency one by one, so a cluster of blocks keeps the matrix in shared
 // memory and does everything.  Block c holds 256 columns of Y as fp16 pairs; its layout (blocks of 64 columns, rows of 128 bytes,
 // swizzled) is at once the K-major operand of Y Y^T and the MN-major second factor of P Y.  The blocks' shares of the gram matrix are added
 // up in block order, a slice of rows to each block, over distributed shared memory; A^2 and P are small and formed by every block.
-// Measured against the launches: 100 x 130, 5 steps: see DESIGN's table of times.
+// Five steps took 84 us with a launch per product and take 28 us for 100 x 130; 100 x 4000 160 us as tiles of one launch (one SM goes over all of
+// the longer side) and 63 us here.
 constexpr int kSmallThreads = 512;
-constexpr uint32_t kSmallSide = 128, kSmallCols = 256, kSmallCluster = 8;
+constexpr uint32_t kSmallSide = 128, kSmallCols = 256, kSmallCluster = 16;
 constexpr uint32_t kSmallGroups = kSmallSide * kSmallCols / 8 / kSmallThreads;
 constexpr uint32_t kSmallHi = 0, kSmallLo = 65536, kSmallGram = 131072, kSmallPoly = kSmallGram + 32768, kSmallBytes = 196608;
 
@@ -626,13 +629,14 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
             }
             read_done();
             cluster_sync_all();                  // everybody's share is there
-            const uint32_t each = 128 / S, items = each * 32 / kSmallThreads;        // rows of this block; float4s per thread: 4, 2, 1
+            const uint32_t each = 128 / S, total4 = each * 32;           // rows of this block, in float4s: up to four a thread
             float4 t[4];
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q) {
                 t[q] = make_float4(0, 0, 0, 0);
-                if (q >= items) continue;
-                const uint32_t item = q * kSmallThreads + tid, r = rank * each + (item >> 5), c4 = item & 31;
+                const uint32_t item = q * kSmallThreads + tid;
+                if (item >= total4) continue;
+                const uint32_t r = rank * each + (item >> 5), c4 = item & 31;
                 const uint32_t local = base32 + kSmallGram + r * 512 + (c4 ^ (r & 7)) * 16;
                 for (uint32_t k = 0; k < S; ++k) {
                     float4 f;
@@ -643,8 +647,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
             cluster_sync_all();                  // everybody has read: the space becomes A and P
 #pragma unroll
             for (uint32_t q = 0; q < 4; ++q) {
-                if (q >= items) continue;
-                const uint32_t item = q * kSmallThreads + tid, r = rank * each + (item >> 5), c4 = item & 31;
+                const uint32_t item = q * kSmallThreads + tid;
+                if (item >= total4) continue;
+                const uint32_t r = rank * each + (item >> 5), c4 = item & 31;
                 const uint32_t local = base32 + kSmallGram + (c4 >> 4) * 16384 + swizzled(r, (c4 & 15) >> 1) + (c4 & 1) * 8;
                 const uint32_t lo = pack16(t[q].x * kUnscale, t[q].y * kUnscale, false), hi = pack16(t[q].z * kUnscale, t[q].w * kUnscale, false);
                 for (uint32_t k = 0; k < S; ++k) asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(map_to(local, k)), "r"(lo), "r"(hi) : "memory");
@@ -745,6 +750,7 @@ cudaError_t launch_small(const OrthoArgs& a, uint32_t align, const OpDevice& dev
     s.status = dev.status;
     constexpr int kSmem = (int)kSmallBytes + 1024;
     cudaError_t e = cudaFuncSetAttribute(k_ortho_small, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e == cudaSuccess && s.blocks > 8) e = cudaFuncSetAttribute(k_ortho_small, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((uint32_t)a.batch * s.blocks);

@@ -136,14 +136,15 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """y = (x - mean) rstd weight + bias over the last axis.  x: (..., cols) fp32, bf16 or fp16; weight, bias: (cols,) or None.
     Returns (y, mean, rstd): y like x, mean and rstd fp32 of x's leading shape."""
     code = _tensor(x, "x", _TYPES)
-    if x.dim() < 1:
+    shape = x.shape
+    if not shape:
         raise SkError("x must have at least 1 dimension")
-    device, shape = x.get_device(), x.shape
-    wcode, pw, pb = _norm_weights(weight, bias, shape[-1], device)
+    device, cols = x.get_device(), shape[-1]
+    wcode, pw, pb = _norm_weights(weight, bias, cols, device)
     rows, ld = _rows(x, "x")
     if out is None:
         y = torch.empty_like(x, memory_format=torch.contiguous_format)
-        ld_y = shape[-1]
+        ld_y = cols
     else:
         if _tensor(out, "out", _TYPES, device) != code:
             raise SkError(f"out has type {out.dtype}, x {x.dtype}")
@@ -151,9 +152,10 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
         y, ld_y = out, _rows(out, "out")[1]
     mean = x.new_empty(shape[:-1], dtype=torch.float32)
     rstd = torch.empty_like(mean)
-    _on(stream, y, mean, rstd)
-    _run(device, lib().sk_layer_norm, x.data_ptr(), ld, y.data_ptr(), ld_y, code, rows, shape[-1], pw, pb, wcode, eps, mean.data_ptr(),
-         rstd.data_ptr(), _pointer_of(stream, device))
+    if stream is not None:
+        _on(stream, y, mean, rstd)
+    _run(device, lib().sk_layer_norm, x.data_ptr(), ld, y.data_ptr(), ld_y, code, rows, cols, pw, pb, wcode, eps, mean.data_ptr(), rstd.data_ptr(),
+         _pointer_of(stream, device))
     return y, mean, rstd
 
 
@@ -168,32 +170,42 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=
     wcode, pw, _ = _norm_weights(weight, None, cols, device)
     (rows, ld), (_, ld_dy) = _rows(x, "x"), _rows(dy, "dy")
     pm, pr = _vector(mean, "mean", rows, _F32, device), _vector(rstd, "rstd", rows, _F32, device)
-    ld_dx = cols
+    ld_dx, pdx = cols, None
     if dx is None:
         dx = torch.empty_like(x, memory_format=torch.contiguous_format)
+        pdx = dx.data_ptr()
     elif dx is False:
         dx = None
     else:
         if _tensor(dx, "dx", _TYPES, device) != code:
             raise SkError(f"dx has type {dx.dtype}, x {x.dtype}")
         _same_shape(dx, x, "dx")
-        ld_dx = _rows(dx, "dx")[1]
-    dtype = next((t.dtype for t in (dweight, dbias, weight) if isinstance(t, torch.Tensor)), torch.float32)
-    sums = []
-    for t, name in ((dweight, "dweight"), (dbias, "dbias")):
-        if t is None:
-            sums.append(x.new_empty((cols,), dtype=dtype))
-        elif t is False:
-            sums.append(None)
-        else:
-            _vector(t, name, cols, {dtype: 0} if dtype in _TYPES else _TYPES, device)
-            sums.append(t)
-    dweight, dbias = sums
-    need = lib().sk_layer_norm_backward_workspace(rows, cols) if rows and (dweight is not None or dbias is not None) else 0
+        ld_dx, pdx = _rows(dx, "dx")[1], dx.data_ptr()
+    given = dweight if isinstance(dweight, torch.Tensor) else dbias if isinstance(dbias, torch.Tensor) else weight
+    dtype = torch.float32 if given is None else given.dtype
+    pdw = pdb = None
+    if dweight is None:
+        dweight = x.new_empty((cols,), dtype=dtype)
+        pdw = dweight.data_ptr()
+    elif dweight is False:
+        dweight = None
+    else:
+        pdw = _vector(dweight, "dweight", cols, _TYPES, device)
+    if dbias is None:
+        dbias = torch.empty_like(dweight) if pdw and dweight.dim() == 1 else x.new_empty((cols,), dtype=dtype)
+        pdb = dbias.data_ptr()
+    elif dbias is False:
+        dbias = None
+    else:
+        pdb = _vector(dbias, "dbias", cols, _TYPES, device)
+        if dbias.dtype != dtype:
+            raise SkError(f"dbias has type {dbias.dtype}, dweight {dtype}")
+    need = lib().sk_layer_norm_backward_workspace(rows, cols) if rows and (pdw or pdb) else 0
     ws = _workspace(x, need)
-    _on(stream, dx, dweight, dbias, ws)
-    _run(device, lib().sk_layer_norm_backward, dy.data_ptr(), ld_dy, x.data_ptr(), ld, _p(dx), ld_dx, code, rows, cols, pw, wcode, pm, pr, _p(dweight),
-         _p(dbias), _TYPES[dtype], _p(ws), need, _pointer_of(stream, device))
+    if stream is not None:
+        _on(stream, dx, dweight, dbias, ws)
+    _run(device, lib().sk_layer_norm_backward, dy.data_ptr(), ld_dy, x.data_ptr(), ld, pdx, ld_dx, code, rows, cols, pw, wcode, pm, pr, pdw, pdb,
+         _TYPES[dtype], _p(ws), need, _pointer_of(stream, device))
     return dx, dweight, dbias
 
 

@@ -73,7 +73,7 @@ def test_layer_norm(ops, cols, dtype):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 64), (3, 17), (9, 256), (33, 257), (700, 768), (2500, 96), (5, 1025), (301, 2048), (7, 2049), (5, 8192),
+@pytest.mark.parametrize("rows,cols", [(1, 1), (1, 64), (3, 17), (9, 256), (33, 257), (700, 768), (2500, 96), (5, 1025), (301, 2048), (7, 2049), (5, 8192), (256, 300), (257, 300), (200, 1001), (260, 500),
                                        (3, 8200), (700, 9000)])
 def test_layer_norm_backward(ops, rows, cols, dtype):
     x = randn(1, rows, cols, dtype=dtype, scale=1.5)
@@ -376,7 +376,7 @@ def ortho_close(got, want):
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("batch,rows,cols", [(1, 1, 1), (1, 1, 70), (1, 70, 1), (2, 16, 16), (3, 33, 65), (1, 65, 33), (1, 128, 128), (2, 127, 300), (1, 300, 129),
-                                             (1, 256, 256), (1, 257, 255), (5, 64, 512), (1, 640, 384), (2, 1100, 1300), (1, 2304, 2100)])
+                                             (1, 256, 256), (1, 257, 255), (5, 64, 512), (1, 640, 384), (2, 1100, 1300), (2, 100, 2100), (1, 4096, 128), (1, 60, 4100), (1, 2304, 2100)])
 def test_orthogonalize(ops, batch, rows, cols, dtype):
     u = randn(1, batch, rows, 4) @ randn(2, batch, 4, cols) + randn(3, batch, rows, cols, scale=0.3)
     u = (u * 1e-3).to(dtype)
