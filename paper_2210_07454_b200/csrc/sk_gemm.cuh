@@ -69,12 +69,22 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-constexpr uint32_t kWaitTries = 1u << 22;     // a try takes tens of ns at least: far beyond any product, still bounded
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t* status) {
-    for (uint32_t i = 0; i < kWaitTries; ++i)
-        if (mbar_try(bar, parity)) return true;
+// Tries until `ready` says so: some ten thousand at once, as ordinary waits need, then with pauses of about half a microsecond, some
+// sixteen seconds in all.  The longest wait there is, for a product of the largest matrices to be finished, is below one.
+constexpr uint32_t kQuickTries = 1u << 14, kSlowTries = 1u << 25;
+template <class Ready>
+__device__ __forceinline__ bool wait_until(Ready ready, uint32_t* status) {
+    for (uint32_t i = 0; i < kQuickTries; ++i)
+        if (ready()) return true;
+    for (uint32_t i = 0; i < kSlowTries; ++i) {
+        if (ready()) return true;
+        __nanosleep(500);
+    }
     atomicOr(status, kOpWait);
     return false;
+}
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t* status) {
+    return wait_until([&] { return mbar_try(bar, parity); }, status);
 }
 __device__ __forceinline__ uint32_t map_to_leader(uint32_t addr) {      // the same address in block 0 of the cluster
     uint32_t r;

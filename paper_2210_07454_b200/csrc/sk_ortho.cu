@@ -101,16 +101,13 @@ struct ChainPlan {
     __device__ __forceinline__ bool wait(const TileJob& j) const {
         const uint32_t need = before(j);
         if (!need) return true;
-        for (uint32_t i = 0; i < kWaitTries; ++i) {
+        const bool ok = wait_until([&] {
             uint32_t have;
             asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(have) : "l"(count + j.b) : "memory");
-            if (have >= need) {
-                asm volatile("fence.proxy.async;" ::: "memory");     // what was written by stores is read by TMA
-                return true;
-            }
-        }
-        atomicOr(status, kOpWait);
-        return false;
+            return have >= need;
+        }, status);
+        asm volatile("fence.proxy.async;" ::: "memory");             // what was written by stores is read by TMA
+        return ok;
     }
     __device__ __forceinline__ void done(const TileJob& j) const {
         __syncwarp();

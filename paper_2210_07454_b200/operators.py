@@ -57,8 +57,10 @@ def _ld(t, name):
 def _rows(t, name):
     """(rows, ld) of a tensor of any dimension seen as rows of its last axis, without a copy."""
     cols = t.shape[-1]
-    if t.is_contiguous():
-        return (t.numel() // cols if cols else 0), max(cols, 1)
+    if cols and t.is_contiguous():
+        return t.numel() // cols, cols
+    if not cols:
+        return 0, 1
     try:
         flat = t.view(-1, cols)
     except RuntimeError:
@@ -143,14 +145,14 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     wcode, pw, pb = _norm_weights(weight, bias, cols, device)
     rows, ld = _rows(x, "x")
     if out is None:
-        y = torch.empty_like(x, memory_format=torch.contiguous_format)
+        y = torch.empty_like(x) if ld == cols else torch.empty_like(x, memory_format=torch.contiguous_format)
         ld_y = cols
     else:
         if _tensor(out, "out", _TYPES, device) != code:
             raise SkError(f"out has type {out.dtype}, x {x.dtype}")
         _same_shape(out, x, "out")
         y, ld_y = out, _rows(out, "out")[1]
-    mean = x.new_empty(shape[:-1], dtype=torch.float32)
+    mean = x.new_empty((rows,) if len(shape) == 2 else shape[:-1], dtype=torch.float32)
     rstd = torch.empty_like(mean)
     if stream is not None:
         _on(stream, y, mean, rstd)

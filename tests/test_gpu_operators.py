@@ -548,6 +548,38 @@ def test_workspaces_are_checked():
     torch.cuda.synchronize()
 
 
+def test_offsets_beyond_32_bits(ops):
+    """Rows 2^21 elements apart: the last ones start beyond 2^32 elements."""
+    gap, rows = 2 ** 21, 2100
+    big = torch.empty(gap * rows, dtype=torch.bfloat16, device="cuda").view(rows, gap)
+    for cols in (200, 333):
+        x = big[:, 5:5 + cols]
+        x.copy_(randn(1, rows, cols))
+        w, b = randn(2, cols), randn(3, cols)
+        want = ops.layer_norm(x.contiguous(), w, b)
+        got = ops.layer_norm(x, w, b, out=big[:, 1000:1000 + cols])
+        # not the same grouping of the columns, so not the same bits: some ulp of the output, and of the statistics
+        within(got[0], want[0].double(), 2.0 ** -6 * want[0].double().abs() + 1e-4, "y")
+        within(got[1], want[1].double(), 1e-5 + 1e-5 * want[1].double().abs(), "mean")
+        dy = randn(4, rows, cols, dtype=torch.bfloat16)
+        a = ops.layer_norm_backward(dy, x, w, want[1], want[2], dx=big[:, 1000:1000 + cols])
+        c = ops.layer_norm_backward(dy, x.contiguous(), w, want[1], want[2])
+        within(a[0], c[0].double(), 2.0 ** -6 * c[0].double().abs() + 1e-4, "dx")
+        within(a[1], c[1].double(), 1e-3 + 1e-5 * c[1].double().abs(), "dw")
+        t = torch.randint(0, rows, (300,), generator=gen(5), device="cuda")
+        h = randn(6, 300, cols, dtype=torch.bfloat16)
+        loss, lse = ops.linear_cross_entropy(h, x.contiguous(), t)
+        l2, s2 = ops.linear_cross_entropy(h, x, t)
+        assert torch.equal(loss, l2) and torch.equal(lse, s2)
+        dw = ops.linear_cross_entropy_backward(loss, h, x.contiguous(), t, lse)[1]
+        ops.linear_cross_entropy_backward(loss, h, x, t, lse, dhidden=False, dweight=big[:, 1000:1000 + cols])
+        assert torch.equal(big[:, 1000:1000 + cols], dw)
+        for part in (x, x[:, :100]):
+            out = ops.orthogonalize(part.contiguous())
+            assert torch.equal(ops.orthogonalize(part, out=big[:, 1000:1000 + part.shape[1]]), out)
+    ops.sync()
+
+
 # ---- together ----------------------------------------------------------------------------------------------------------------
 def test_the_example_learns():
     """The example trains with every operator and the compressed step; the loss falls well below that of a uniform guess."""
