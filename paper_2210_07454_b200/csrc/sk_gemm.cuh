@@ -8,7 +8,8 @@
 //
 // A block (CG = 1) or a pair of blocks on two SMs (CG = 2) works on one output tile of 128*CG rows by BN columns at a
 // time and walks over tiles until none is left.  One warp feeds a ring of kStages shared-memory stages by TMA (64 values of k a
-// stage, 128-byte swizzle), one thread issues the matrix instructions, eight warps empty the accumulators.  Two
+// stage, 128-byte swizzle), one thread issues the matrix instructions, eight warps empty the accumulators (sixteen,
+// with less shared memory for the ring: 67 against 63 us for the gradient of 8 x 50257 x 768).  Two
 // accumulators in tensor memory take turns, so the next tile's products run while this tile's epilogue does.
 //
 // Every wait has a limit.  A role whose wait runs out records kOpWait in the status word and leaves its loop; the others
@@ -28,8 +29,6 @@ namespace sk {
 constexpr uint32_t kOpWait = 1u;              // status word of the operators: a wait inside a product kernel ran out
 
 constexpr int kGemmK = 64;                    // values of k per stage: 128 bytes, the width of the swizzle
-constexpr int kEpiWarps = 8;
-constexpr int kGemmThreads = 64 + 32 * kEpiWarps;
 constexpr int kStageWords = 1024;             // of shared memory that store_tile32 needs, for each epilogue warp
 
 // What the kernel's roles have to know of a tile.
@@ -229,26 +228,28 @@ struct GemmPlan {
     __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i < 2 * groups ? &map[i] : nullptr; }
 };
 
-// words: of shared memory for each epilogue warp.  The ring takes what is left of the 227 KB, six stages of 32 KB beside 4 KB a warp: two would cover
+// Epi::kWarps epilogue warps with kWords of shared memory each.  The ring takes what is left of the 227 KB, six stages of 32 KB beside 4 KB a warp: two would cover
 // the 1600 cycles from a copy's issue to its arrival, more even out the waits.
-template <int CG, int BN, int words>
+template <int CG, int BN, class Epi>
 struct GemmTile {
+    static constexpr int kEpiBytes = Epi::kWarps * Epi::kWords * 4;
+    static constexpr int kThreads = 64 + 32 * Epi::kWarps;
     static constexpr int kStageBytes = 128 * 128 + (BN / CG) * 128;      // both operands, 64 values of k
-    static constexpr int kFixed = kEpiWarps * words * 4 + 1024 + 512;    // the epilogue's, alignment of the swizzle, barriers
+    static constexpr int kFixed = kEpiBytes + 1024 + 512;    // the epilogue's, alignment of the swizzle, barriers
     static constexpr int kStages = (232448 - kFixed) / kStageBytes;
-    static constexpr int kSmem = kStages * kStageBytes + kEpiWarps * words * 4 + 1024;
+    static constexpr int kSmem = kStages * kStageBytes + kEpiBytes + 1024;
 };
 
 // Plan: job(unit, units, i, job): the unit's i-th tile; wait(job): until its operands are there; done(job): called by every epilogue warp
 // when its share of the tile is written.
-// Epi: struct Args; __device__ Epi(const Args&, job, row, half, shared address of the warp's memory); begin(plan, first column) before the
+// Epi: struct Args; __device__ Epi(const Args&, job, row, part, shared address of the warp's memory); begin(plan, first column) before the
 // accumulator is waited for; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
-// row of the tile and gets its columns 32 at a time; the two warps that share a row take half the columns each.  Rows >= M
+// row of the tile and gets its columns 32 at a time; the kWarps / 4 warps that share a row take a part of the columns each.  Rows >= M
 // are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
 template <int CG, int BN, class Plan, class Epi>
-__global__ void __launch_bounds__(kGemmThreads, 1)
+__global__ void __launch_bounds__(64 + 32 * Epi::kWarps, 1)
 k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::Args ea) {
-    constexpr int kStages = GemmTile<CG, BN, Epi::kWords>::kStages;
+    constexpr int kStages = GemmTile<CG, BN, Epi>::kStages;
     constexpr int kRowsB = BN / CG;
     constexpr int kBytesA = 128 * 128, kBytesB = kRowsB * 128;
     constexpr uint32_t kTmemCols = 2 * BN;                       // a power of two >= 32
@@ -267,7 +268,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
 
     if (threadIdx.x == 0) {
         for (uint32_t s = 0; s < (uint32_t)kStages; ++s) { mbar_init(full(s), 1); mbar_init(empty(s), 1); }
-        for (uint32_t a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), CG * kEpiWarps); }
+        for (uint32_t a = 0; a < 2; ++a) { mbar_init(acc_full(a), 1); mbar_init(acc_empty(a), CG * Epi::kWarps); }
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 1) tmem_alloc<CG>(smem_u32(&tmem_slot), kTmemCols);
@@ -369,27 +370,28 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
             }
         }
     } else {
-        const uint32_t w = warp - 2, quarter = warp & 3, half = w >> 2;
+        const uint32_t w = warp - 2, quarter = warp & 3, part = w >> 2;
+        constexpr uint32_t kCols = BN / (Epi::kWarps / 4);           // of a warp
         const uint32_t stage = stages + kStages * kBytes + w * Epi::kWords * 4;
         for (uint32_t n = 0; plan.job(unit, units, n, t); ++n) {
             const uint32_t a = n & 1;
             const uint32_t row = t.m * (128 * CG) + rank * 128 + quarter * 32 + lane;
-            const uint32_t col0 = t.n * BN + half * (BN / 2);
-            Epi epi(ea, t, row, half, stage);
+            const uint32_t col0 = t.n * BN + part * kCols;
+            Epi epi(ea, t, row, part, stage);
             epi.begin(plan, col0);                               // what it reads travels while the products run
             if (!mbar_wait(acc_full(a), (n >> 1) & 1, plan.status)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
 #pragma unroll 1
-            for (uint32_t c = 0; c < BN / 2; c += 32) {
+            for (uint32_t c = 0; c < kCols; c += 32) {
                 float v[32];
                 __syncwarp();                                    // the load needs the whole warp
-                tmem_load32(tmem + a * BN + half * (BN / 2) + c + ((quarter * 32) << 16), v);
-                if (c + 32 == BN / 2) {                          // everything is in registers: the accumulator is free
+                tmem_load32(tmem + a * BN + part * kCols + c + ((quarter * 32) << 16), v);
+                if (c + 32 == kCols) {                          // everything is in registers: the accumulator is free
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();
                     if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_leader(acc_empty(a)) : acc_empty(a));
                 }
-                if (col0 + c < t.N) epi.chunk(col0 + c, v, c + 32 == BN / 2 || col0 + c + 32 >= t.N);
+                if (col0 + c < t.N) epi.chunk(col0 + c, v, c + 32 == kCols || col0 + c + 32 >= t.N);
             }
             epi.end();
             plan.done(t);
@@ -426,14 +428,14 @@ cudaError_t launch_plan(bool chain, const Plan& plan, const typename Epi::Args& 
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     if (device >= 64 || !prepared[device]) {
-        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmTile<CG, BN, Epi::kWords>::kSmem);
+        e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, GemmTile<CG, BN, Epi>::kSmem);
         if (e != cudaSuccess) return e;
         if (device < 64) prepared[device] = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(units * CG);
-    cfg.blockDim = dim3(kGemmThreads);
-    cfg.dynamicSmemBytes = GemmTile<CG, BN, Epi::kWords>::kSmem;
+    cfg.blockDim = dim3(GemmTile<CG, BN, Epi>::kThreads);
+    cfg.dynamicSmemBytes = GemmTile<CG, BN, Epi>::kSmem;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
     uint32_t n = 0;

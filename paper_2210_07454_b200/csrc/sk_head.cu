@@ -26,7 +26,7 @@ __device__ __forceinline__ float exp2_fast(float x) {          // 2^x, 2 ulp
 
 // per (half tile, row): maximum of the logits and the sum of exp(z - maximum)
 struct StatsEpi {
-    static constexpr int kWords = kStageWords;
+    static constexpr int kWarps = 8, kWords = kStageWords;
     template <class Plan> __device__ void begin(const Plan&, uint32_t) {}
     struct Args { float2* part; float* at_target; const int64_t* targets; };
     const Args& a;
@@ -119,7 +119,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_head_join(const float2* part, 
 
 // G's piece
 struct GradEpi {
-    static constexpr int kWords = kStageWords;
+    static constexpr int kWarps = 8, kWords = kStageWords;
     template <class Plan> __device__ void begin(const Plan&, uint32_t) {}
     struct Args { uint16_t* out; uint64_t ld; const float *lse, *dloss, *factor; const int64_t* targets; uint64_t vocab; uint32_t first; };
     const Args& a;
@@ -174,7 +174,7 @@ struct GradEpi {
 // One of two products, by the group: rows of dW, or a share of dhidden.  Shares of more than one piece or slice are added up in 32
 // bits, a slice of K in a matrix of its own (`sum`, one after the other), and joined by k_head_sum.
 struct OutEpi {
-    static constexpr int kWords = kStageWords;
+    static constexpr int kWarps = 8, kWords = kStageWords;
     template <class Plan> __device__ void begin(const Plan&, uint32_t) {}
     struct One { void* out; float* sum; uint64_t ld, sum_stride; int type; uint32_t align, add; };
     struct Args { One o[2]; const float* factor; };
@@ -237,27 +237,6 @@ __global__ void __launch_bounds__(256) k_head_sum(const float* sum, uint32_t sli
     }
 }
 
-// fp16 only: a power of two that brings the largest |dloss| to about 2^14, so that small probabilities stay above fp16's
-// smallest values; the products divide by it again
-__global__ void __launch_bounds__(1024) k_head_factor(const float* dloss, const int64_t* targets, uint32_t tokens, uint64_t vocab, float* factor) {
-    __shared__ float s[32];
-    chain_acquire();
-    float m = 0;
-    for (uint32_t i = threadIdx.x; i < tokens; i += 1024)
-        if (targets[i] >= 0 && targets[i] < (int64_t)vocab) m = fmaxf(m, fabsf(dloss[i]));
-#pragma unroll
-    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = m;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 32; ++i) m = fmaxf(m, s[i]);
-        int e = 0;
-        if (m > 0 && isfinite(m)) frexpf(m, &e);
-        e = 14 - e;
-        *factor = m > 0 && isfinite(m) ? exp2f((float)(e < -100 ? -100 : e > 100 ? 100 : e)) : 1.0f;
-    }
-}
-
 // Rows copied to a leading dimension that TMA can address, up to two matrices in one launch; with targets, the rows that
 // take no part become zero.  The backward pass always takes the hidden states through this: in dW a token without a target is multiplied
 // by zeros, and whatever its row holds (padding may hold infinities or NaN) must not survive that.
@@ -265,14 +244,40 @@ struct PackArgs {
     struct One { const uint16_t* src; uint16_t* dst; uint64_t ld, rows; const int64_t* targets; } m[2];
     uint64_t vocab;
     uint32_t ld_dst, cols, first_blocks;         // blocks of the first matrix
+    uint32_t copy_blocks;                        // of all matrices
+    const float* dloss;                          // with a factor: one block more
+    float* factor;
 };
+// fp16 only: a power of two that brings the largest |dloss| to about 2^14, so that small probabilities stay above fp16's
+// smallest values; the products divide by it again
+__device__ void head_factor(const float* dloss, const int64_t* targets, uint64_t tokens, uint64_t vocab, float* factor) {
+    __shared__ float s[8];
+    float m = 0;
+    for (uint64_t i = threadIdx.x; i < tokens; i += 256)
+        if (targets[i] >= 0 && targets[i] < (int64_t)vocab) m = fmaxf(m, fabsf(dloss[i]));
+#pragma unroll
+    for (int o = 16; o; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+    if ((threadIdx.x & 31) == 0) s[threadIdx.x >> 5] = m;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i]);
+        int e = 0;
+        if (m > 0 && isfinite(m)) frexpf(m, &e);
+        e = 14 - e;
+        *factor = m > 0 && isfinite(m) ? exp2f((float)(e < -100 ? -100 : e > 100 ? 100 : e)) : 1.0f;
+    }
+}
 // A thread copies eight neighbours: eight loads on their way at once whatever the alignment, one 16-byte store.
 __global__ void __launch_bounds__(256) k_head_pack(const __grid_constant__ PackArgs a) {
     chain_acquire();
+    if (blockIdx.x >= a.copy_blocks) {
+        head_factor(a.dloss, a.m[0].targets, a.m[0].rows, a.vocab, a.factor);
+        return;
+    }
     const uint32_t which = blockIdx.x >= a.first_blocks;
     const PackArgs::One& m = a.m[which];
     const uint32_t groups = a.ld_dst / 8, block = which ? blockIdx.x - a.first_blocks : blockIdx.x;
-    const uint64_t total = m.rows * groups, step = (uint64_t)(which ? gridDim.x - a.first_blocks : a.first_blocks) * 256;
+    const uint64_t total = m.rows * groups, step = (uint64_t)(which ? a.copy_blocks - a.first_blocks : a.first_blocks) * 256;
     const bool vec = (uintptr_t)m.src % 16 == 0 && m.ld % 8 == 0, half = (uintptr_t)m.src % 8 == 0 && m.ld % 4 == 0;
     for (uint64_t q = block * 256ull + threadIdx.x; q < total; q += step) {
         const uint64_t r = q / groups;
@@ -354,7 +359,7 @@ HeadLayout layout_of(const HeadArgs& a, bool backward) {
 
 // the operands as TMA can address them: packed copies where the caller's are not
 int pack_operands(const HeadArgs& a, bool backward, const HeadLayout& l, const OpDevice& dev, const void** h, const void** w, uint64_t* ld_h, uint64_t* ld_w,
-                  cudaStream_t st) {
+                  float* factor, cudaStream_t st) {
     uint8_t* ws = (uint8_t*)a.workspace;
     *h = a.hidden; *w = a.weight; *ld_h = a.ld_hidden; *ld_w = a.ld_weight;
     PackArgs p{};
@@ -377,7 +382,10 @@ int pack_operands(const HeadArgs& a, bool backward, const HeadLayout& l, const O
     p.ld_dst = (uint32_t)l.ld_pack;
     p.cols = (uint32_t)a.width;
     p.first_blocks = blocks[0];
-    SK_OP_CUDA(launch_kernel(true, k_head_pack, dim3(blocks[0] + blocks[1]), 256, 0, st, p));
+    p.copy_blocks = blocks[0] + blocks[1];
+    p.dloss = a.dloss;
+    p.factor = factor;
+    SK_OP_CUDA(launch_kernel(true, k_head_pack, dim3(p.copy_blocks + (factor ? 1 : 0)), 256, 0, st, p));
     return SK_OK;
 }
 
@@ -391,7 +399,7 @@ int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
     uint8_t* ws = (uint8_t*)a.workspace;
     const void *h, *w;
     uint64_t ld_h, ld_w;
-    int rc = pack_operands(a, false, l, dev, &h, &w, &ld_h, &ld_w, st);
+    int rc = pack_operands(a, false, l, dev, &h, &w, &ld_h, &ld_w, nullptr, st);
     if (rc) return rc;
     GemmGroup g{};
     g.M = (uint32_t)a.tokens;
@@ -413,14 +421,10 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
     uint8_t* ws = (uint8_t*)a.workspace;
     const void *h, *w;
     uint64_t ld_h, ld_w;
-    int rc = pack_operands(a, true, l, dev, &h, &w, &ld_h, &ld_w, st);
+    float* factor = a.type == SK_F16 ? (float*)(ws + l.off_factor) : nullptr;
+    int rc = pack_operands(a, true, l, dev, &h, &w, &ld_h, &ld_w, factor, st);
     if (rc) return rc;
     const uint32_t tokens = (uint32_t)a.tokens, width = (uint32_t)a.width;
-    float* factor = nullptr;
-    if (a.type == SK_F16) {
-        factor = (float*)(ws + l.off_factor);
-        SK_OP_CUDA(launch_kernel(true, k_head_factor, dim3(1), 1024, 0, st, a.dloss, a.targets, tokens, a.vocab, factor));
-    }
     uint16_t* gbuf = (uint16_t*)(ws + l.off_g);
     float* sum = l.off_sum ? (float*)(ws + l.off_sum) : nullptr;
     for (uint64_t v0 = 0; v0 < a.vocab; v0 += l.piece) {

@@ -122,7 +122,7 @@ struct ChainPlan {
 // The epilogues of the three products.  A warp has two areas of staging memory: one for the lines of the matrix it writes, one for those of the second
 // matrix of a pair, or for A's lines on their way to P, which are fetched while the products run.
 struct ChainEpi {
-    static constexpr int kWords = 2 * kStageWords;
+    static constexpr int kWarps = 8, kWords = 2 * kStageWords;
     struct Args {
         __half *gram, *poly, *hi[2], *lo[2];     // [2]: as the plan's
         uint64_t a_stride, x_stride;
@@ -864,7 +864,7 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     p.tiles_m = (p.rows + tile - 1) / tile;
     p.tiles_n = (p.cols + tile - 1) / tile;
     p.apply = p.tiles_m * p.tiles_n;
-    p.signals = (wide ? 2 : 1) * kEpiWarps;
+    p.signals = (wide ? 2 : 1) * ChainEpi::kWarps;
     if ((uint64_t)a.steps * batch * (2ull * p.square + p.apply) * p.signals >= (1ull << 32))
         return set_error(SK_EINVAL, "sk_orthogonalize: batch * rows * cols is too large for one call");
     const uint32_t most_tiles = batch * (p.square > p.apply ? p.square : p.apply), units = most_tiles < slots ? most_tiles : slots;
