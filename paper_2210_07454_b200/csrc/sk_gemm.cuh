@@ -34,9 +34,9 @@ constexpr int kStageWords = 1024;             // of shared memory that store_til
 // What the kernel's roles have to know of a tile.
 struct TileJob {
     uint32_t M, N;                            // extents of the output
-    uint32_t m, n, b;                         // the tile: row, column, matrix (or slice of K)
+    uint32_t m, n, b, slice;                  // the tile: row, column, matrix, slice of K
     uint32_t kind, step;                      // which product: for the epilogue
-    uint32_t k_stages, pass;                  // stages; the first `pass` of them over a and b, the others over a2 and b2
+    uint32_t k_stages, pass;                  // stages (none: begin() does it all); the first `pass` of them over a and b, the others over a2 and b2
     int k_first, z;                           // first k, matrix of the operands
     uint32_t a_mn, b_mn;                      // 1: MN-major
     uint32_t a_rows;                          // rows of A a block loads: 128, or fewer where a single tile row has no more
@@ -185,7 +185,7 @@ struct GemmPlan {
     GemmGroup g[2];
     uint32_t groups, early;
     uint32_t* status;
-    static constexpr bool kCooperative = false;
+    static constexpr bool kCooperative = false, kEmpty = false;
 
     __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, TileJob& j) const {
         uint32_t t = p + i * units, group = 0;
@@ -200,8 +200,9 @@ struct GemmPlan {
         }
         const GemmGroup& s = g[group];
         const uint32_t per = s.tiles_m * s.tiles_n;
-        j.b = t / per;
-        uint32_t q = t - j.b * per;
+        j.b = 0;
+        j.slice = t / per;
+        uint32_t q = t - j.slice * per;
         const uint32_t band = q / (s.band * s.tiles_n);
         q -= band * s.band * s.tiles_n;
         const uint32_t rows = min(s.band, s.tiles_m - band * s.band);
@@ -211,8 +212,8 @@ struct GemmPlan {
         j.N = s.N;
         j.kind = group;
         j.step = 0;
-        j.k_stages = j.pass = min(s.k_blocks, s.k_total - j.b * s.k_blocks);
-        j.k_first = (int)(j.b * s.k_blocks * kGemmK);
+        j.k_stages = j.pass = min(s.k_blocks, s.k_total - j.slice * s.k_blocks);
+        j.k_first = (int)(j.slice * s.k_blocks * kGemmK);
         j.z = 0;
         j.a_mn = s.a_mn;
         j.b_mn = s.b_mn;
@@ -381,6 +382,12 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
             epi.begin(plan, col0);                               // what it reads travels while the products run
             if (!mbar_wait(acc_full(a), (n >> 1) & 1, plan.status)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            if (Plan::kEmpty && !t.k_stages) {                   // no products
+                __syncwarp();
+                if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_leader(acc_empty(a)) : acc_empty(a));
+                plan.done(t);
+                continue;
+            }
 #pragma unroll 1
             for (uint32_t c = 0; c < kCols; c += 32) {
                 float v[32];

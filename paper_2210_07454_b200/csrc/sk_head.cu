@@ -185,7 +185,7 @@ struct OutEpi {
     uint32_t stage;
     float scale;
     __device__ OutEpi(const Args& a_, const TileJob& t_, uint32_t row, uint32_t, uint32_t stage_)
-        : a(a_.o[t_.kind]), t(t_), sum(a.sum ? a.sum + t_.b * a.sum_stride : nullptr), row0(row - (threadIdx.x & 31)), stage(stage_),
+        : a(a_.o[t_.kind]), t(t_), sum(a.sum ? a.sum + t_.slice * a.sum_stride : nullptr), row0(row - (threadIdx.x & 31)), stage(stage_),
           scale(a_.factor ? 1.0f / *a_.factor : 1.0f) {
         rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32;
     }

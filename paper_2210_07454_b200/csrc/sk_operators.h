@@ -97,6 +97,7 @@ inline uint32_t row_alignment(const void* p, uint64_t ld, int type) {
 __device__ __forceinline__ void store_shared16(uint32_t at, uint4 q) {
     asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(q.x), "r"(q.y), "r"(q.z), "r"(q.w) : "memory");
 }
+__device__ __forceinline__ void store_shared2(uint32_t at, uint32_t low) { asm volatile("st.shared.b16 [%0], %1;" ::"r"(at), "h"((uint16_t)low) : "memory"); }
 __device__ __forceinline__ uint4 load_shared16(uint32_t at) {
     uint4 q;
     asm volatile("ld.shared.v4.b32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(at) : "memory");

@@ -27,55 +27,78 @@ constexpr float kScale = 4096.0f, kUnscale = 1.0f / 4096.0f;     // 2^12
 constexpr uint32_t kPadCols = 32;                                // leading dimensions: whole 32-column chunks
 
 // ---- all products of the iteration in one launch --------------------------------------------------------------------------
-// The tiles of A = X X^T (0), P = a I + b A + c A^2 (1) and X <- P X (2) of all steps and matrices, in this order, dealt out to the units in
+// The tiles of A = X X^T, P = a I + b A + c A^2 and X <- P X of all steps and matrices, in this order, dealt out to the units in
 // turn.  A tile may start when all tiles of the products before it of ITS matrix are written: a counter per matrix says how many epilogue
 // warps have written theirs.  Waiting for a matrix instead of for everything keeps the units busy across the products' ends: 12 matrices of
 // 768 x 768 take 200 us, with a launch per product 252.  What a product costs beside its stages of some 620 cycles: 1500 cycles from the first
 // copy's issue to its arrival, 600 from the last product to the accumulator, 2000 (128 columns) to 7000 (256, mirrored) in the
 // epilogue, 1100 to 2400 until its stores are seen, and as much again until the counter is read.
+// Where A has few tiles and a long K, K is split: the slices' sums go to memory in 32 bits, and tiles without products, of kJoinParts to a tile
+// of A, add them up in order (2688 x 256: 150 -> 122 us, 768 x 4096: 252 -> 209).  SLICED has its own kernels, as the longer way to a tile's
+// place costs the others 4 %.
 // A unit takes its tiles in order, every tile waits for earlier ones only, and the blocks are all resident (a cooperative launch): so the waits
 // end; they have a limit all the same.
-struct ChainPlan {
+constexpr uint32_t kJoinParts = 4;               // of 32 rows of each block
+enum ChainKind : uint32_t { kGram, kPoly, kApply, kJoin };   // kGram: A, or with slices a slice of it; kJoin, after it: A from its slices
+struct ChainShape {
     CUtensorMap gram_x[2], apply_hi[2], apply_lo[2], gram, poly;     // [2]: the two buffers that X alternates between
     uint32_t steps, exact, tall, batch;
     uint32_t m, rows, cols;                      // shorter side; X's extents
     uint32_t side, square;                       // tile rows of A, its tiles on and below the diagonal
     uint32_t tiles_m, tiles_n, apply;            // of X
     uint32_t k_gram, k_poly;                     // stages along the longer and the shorter side
+    uint32_t slices, k_slice;                    // of the longer side in A, stages of one
     uint32_t signals;                            // of every tile: its epilogue warps
     uint32_t* count;                             // per matrix, zero before the launch
     uint32_t* status;
-    static constexpr bool kCooperative = true;
 
     // X is the sum of two matrices in all but the last two steps, and in the first where one is exact
     __host__ __device__ bool pair(uint32_t step) const { return step + 2 < steps && !(step == 0 && exact); }
-    __device__ __forceinline__ uint32_t before(const TileJob& j) const {
-        return (j.step * (2 * square + apply) + j.kind * square) * signals;
+};
+template <bool SLICED>
+struct ChainPlan : ChainShape {
+    static constexpr bool kCooperative = true, kEmpty = SLICED;      // kEmpty: has tiles without products
+    // tiles of one matrix and step before those of a kind, and of all kinds
+    __device__ __forceinline__ uint32_t tiles_before(uint32_t kind) const {
+        if (!SLICED) return kind * square;
+        return kind == kGram ? 0 : square * (slices + (kind == kJoin ? 0 : kJoinParts + (kind == kPoly ? 0 : 1)));
     }
+    __device__ __forceinline__ uint32_t tiles_per_step() const { return tiles_before(kApply) + apply; }
     __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, TileJob& j) const {
-        const uint32_t per = batch * (2 * square + apply), t = p + i * units;
+        const uint32_t per = batch * tiles_per_step(), t = p + i * units;
         j.step = t / per;
         if (j.step >= steps) return false;
         uint32_t q = t - j.step * per;
         const uint32_t from = j.step & 1;
-        j.kind = q < batch * square ? 0 : q < 2 * batch * square ? 1 : 2;
-        q -= j.kind * batch * square;
+        j.kind = q < batch * tiles_before(kPoly) ? kGram : q < batch * tiles_before(kApply) ? kPoly : kApply;
+        if (SLICED && j.kind == kGram && q >= batch * tiles_before(kJoin)) j.kind = kJoin;
+        q -= batch * tiles_before(j.kind);
         j.k_first = 0;
         j.a_rows = 128;
         j.k_rows = kGemmK;
         j.bf16 = 0;
-        if (j.kind < 2) {
-            j.b = q / square;
-            q -= j.b * square;
+        if (j.kind != kApply) {
+            const uint32_t each = SLICED && j.kind != kPoly ? square * (j.kind == kGram ? slices : kJoinParts) : square;
+            j.b = q / each;
+            q -= j.b * each;
+            if (SLICED) {
+                j.slice = q / square;
+                q -= j.slice * square;
+            }
             uint32_t r = (uint32_t)((sqrtf(8.0f * (float)q + 1.0f) - 1.0f) * 0.5f);
             while (r * (r + 1) / 2 > q) --r;
             while ((r + 1) * (r + 2) / 2 <= q) ++r;
             j.m = r;
             j.n = q - r * (r + 1) / 2;
             j.M = j.N = m;
-            j.a_mn = j.b_mn = j.kind == 0 && tall;
-            j.k_stages = j.pass = j.kind == 0 ? k_gram : k_poly;
-            j.map_a = j.map_b = j.map_a2 = j.map_b2 = j.kind == 0 ? &gram_x[from] : &gram;
+            j.a_mn = j.b_mn = j.kind == kGram && tall;
+            j.k_stages = j.pass = j.kind == kGram ? k_gram : k_poly;
+            if (SLICED && j.kind == kGram) {
+                j.k_first = (int)(j.slice * k_slice * kGemmK);
+                j.k_stages = j.pass = min(k_slice, k_gram - j.slice * k_slice);
+            }
+            if (SLICED && j.kind == kJoin) j.k_stages = 0;
+            j.map_a = j.map_b = j.map_a2 = j.map_b2 = j.kind == kGram ? &gram_x[from] : &gram;
         } else {
             j.b = q / apply;
             q -= j.b * apply;
@@ -99,7 +122,7 @@ struct ChainPlan {
         return true;
     }
     __device__ __forceinline__ bool wait(const TileJob& j) const {
-        const uint32_t need = before(j);
+        const uint32_t need = (j.step * tiles_per_step() + tiles_before(j.kind)) * signals;
         if (!need) return true;
         const bool ok = wait_until([&] {
             uint32_t have;
@@ -119,21 +142,27 @@ struct ChainPlan {
     __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return &gram_x[0] + i; }
 };
 
+struct ChainArgs {
+    __half *gram, *poly, *hi[2], *lo[2];     // [2]: as the plan's
+    float* slices;                           // A's: slice by slice, like A but in 32 bits
+    uint64_t slice_stride;
+    uint32_t slice_count, join_cols;         // join_cols: a warp's columns when they are added up
+    uint64_t a_stride, x_stride;
+    uint32_t ld_a, ld_x;
+    float a, b, c;
+    const float* factor;                     // per matrix: the first step's X = factor * (the matrix that is stored)
+    void* out;                               // the last step's, in the caller's type and layout
+    uint64_t out_stride, ld_out;
+    int out_type;
+    uint32_t align, steps;
+};
+
 // The epilogues of the three products.  A warp has two areas of staging memory: one for the lines of the matrix it writes, one for those of the second
 // matrix of a pair, or for A's lines on their way to P, which are fetched while the products run.
+template <bool SLICED>
 struct ChainEpi {
     static constexpr int kWarps = 8, kWords = 2 * kStageWords;
-    struct Args {
-        __half *gram, *poly, *hi[2], *lo[2];     // [2]: as the plan's
-        uint64_t a_stride, x_stride;
-        uint32_t ld_a, ld_x;
-        float a, b, c;
-        const float* factor;                     // per matrix: the first step's X = factor * (the matrix that is stored)
-        void* out;                               // the last step's, in the caller's type and layout
-        uint64_t out_stride, ld_out;
-        int out_type;
-        uint32_t align, steps;
-    };
+    using Args = ChainArgs;
     const Args& e;
     const TileJob& t;
     uint32_t row, row0, rows;                    // the lane's row, the warp's first, how many of the warp's exist
@@ -142,11 +171,11 @@ struct ChainEpi {
     __device__ ChainEpi(const Args& a, const TileJob& t_, uint32_t row_, uint32_t, uint32_t stage_)
         : e(a), t(t_), row(row_), row0(row_ - (threadIdx.x & 31)), stage(stage_) {
         rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32;
-        if (t.step == 0 && t.kind != 1) {
+        if (t.step == 0 && t.kind != kPoly) {
             const float f = a.factor[t.b];
-            scale *= t.kind == 0 ? f * f : f;
+            scale *= t.kind == kApply ? f : f * f;
         }
-        if (t.kind == 2 && t.step + 1 == e.steps) scale *= kUnscale;
+        if (t.kind == kApply && t.step + 1 == e.steps) scale *= kUnscale;
     }
     // A's 64 columns from `col` of the warp's rows into the second area
     __device__ void fetch(uint32_t col) {
@@ -160,9 +189,65 @@ struct ChainEpi {
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     }
+    // A's slices added up: of 32 rows of the block, the warp's share of the columns, 16 at a time.  Four lanes have the 64 bytes of a row;
+    // the sums of all slices are on their way at once, four slices to a batch.
+    __device__ void join(uint32_t col0) {
+        const uint32_t lane = threadIdx.x & 31, warp = (threadIdx.x >> 5) - 2, quarter = (threadIdx.x >> 5) & 3;
+        const uint32_t first_row = row0 - quarter * 32 + t.slice * 32, r = lane >> 2, c = 4 * (lane & 3);
+        if (first_row >= t.M) return;
+        __half* out = e.gram + t.b * e.a_stride;
+        for (uint32_t q = 0; q < e.join_cols; q += 16) {
+            const uint32_t col = col0 + (warp & 3) * e.join_cols + q;
+            if (col >= t.N) break;
+            const float* p = e.slices + t.b * e.a_stride + (uint64_t)(first_row + r) * e.ld_a + col + c;
+            float4 sum[4] = {};
+            for (uint32_t k = 0; k < e.slice_count; k += 4) {
+                float4 f[4][4];
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        f[j][i] = make_float4(0, 0, 0, 0);
+                        if (k + j < e.slice_count && first_row + r + 8 * i < t.M)
+                            f[j][i] = __ldcg((const float4*)(p + (k + j) * e.slice_stride + (uint64_t)(8 * i) * e.ld_a));
+                    }
+#pragma unroll
+                for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i) {
+                        sum[i].x += f[j][i].x; sum[i].y += f[j][i].y; sum[i].z += f[j][i].z; sum[i].w += f[j][i].w;
+                    }
+            }
+            __syncwarp();
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint32_t lo = pack16(sum[i].x * scale, sum[i].y * scale, false), hi = pack16(sum[i].z * scale, sum[i].w * scale, false);
+                if (first_row + r + 8 * i < t.M) *(uint2*)(out + (uint64_t)(first_row + r + 8 * i) * e.ld_a + col + c) = make_uint2(lo, hi);
+                if (t.m != t.n) {                // the mirror image: 16 rows of 80 bytes in the staging memory
+                    const uint32_t at = stage + c * 80 + (r + 8 * i) * 2;
+                    store_shared2(at, lo);
+                    store_shared2(at + 80, lo >> 16);
+                    store_shared2(at + 160, hi);
+                    store_shared2(at + 240, hi >> 16);
+                }
+            }
+            if (t.m == t.n) continue;
+            __syncwarp();
+#pragma unroll
+            for (uint32_t i = 0; i < 2; ++i) {
+                const uint32_t y = r + 8 * i;
+                const uint4 w = load_shared16(stage + y * 80 + (lane & 3) * 16);
+                if (col + y < t.N) *(uint4*)(out + (uint64_t)(col + y) * e.ld_a + first_row + 8 * (lane & 3)) = w;
+            }
+        }
+    }
     template <class Plan>
     __device__ void begin(const Plan& plan, uint32_t col0) {
-        if (t.kind != 1 || !rows) return;
+        if (SLICED && t.kind == kJoin) {
+            plan.wait(t);                        // no products wait for the warps that have nothing to add up
+            join(col0);
+        }
+        if (t.kind != kPoly || !rows) return;
         plan.wait(t);
         fetch(col0);
     }
@@ -187,7 +272,11 @@ struct ChainEpi {
     }
     __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (!rows) return;
-        if (t.kind == 1) {
+        if (SLICED && t.kind == kGram) {       // scaled when the slices are joined
+            store_tile32(e.slices + t.slice * e.slice_stride + t.b * e.a_stride, SK_F32, e.ld_a, row0, rows, col, e.ld_a, v, 16, stage, false, last);
+            return;
+        }
+        if (t.kind == kPoly) {
             if (!(col & 32)) {
                 asm volatile("cp.async.wait_all;" ::: "memory");
                 __syncwarp();
@@ -213,7 +302,7 @@ struct ChainEpi {
         }
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= scale;
-        if (t.kind == 0) {
+        if (t.kind == kGram) {
             square(e.gram + t.b * e.a_stride, col, v, last);
             return;
         }
@@ -378,10 +467,41 @@ __global__ void __launch_bounds__(256) k_ortho_scale(const __grid_constant__ Squ
     }
 }
 
+// How the products are cut: pairs of blocks on 256 x 256 or single ones on 128 x 128, and slices of the longer side in A.  A stage takes
+// both tiles the same time (some 620 cycles, see launch_products), the pair does twice the work per SM in it.  The time is about that of
+// the work on all units, but at least that of one matrix's dependent products, whose starts and epilogues are shorter with the
+// small tile (7000 cycles, 12,000).  Slices shorten the path by their stages and add kJoinCost (256 x 1024 is slower with them: 114 us for
+// 107).  Planned for the SMs of a B200, as the workspace's size depends on it.
+constexpr uint64_t kJoinCost = 9000;             // cycles: writing slices, their signal, and adding them up
+struct ChainTiles { bool wide; uint32_t slices; };
+ChainTiles chain_tiles(const OrthoArgs& a) {
+    const uint64_t m = a.rows < a.cols ? a.rows : a.cols, n = a.rows < a.cols ? a.cols : a.rows, sms = 148;
+    const uint64_t k_gram = (n + kGemmK - 1) / kGemmK, k_poly = (m + kGemmK - 1) / kGemmK;
+    ChainTiles best = {false, 1};
+    uint64_t least = ~0ull;
+    for (int wide = 1; wide >= 0; --wide) {
+        const uint64_t tile = wide ? 256 : 128, units = wide ? sms / 2 : sms, start = wide ? 12000 : 7000;
+        const uint64_t side = (m + tile - 1) / tile, square = side * (side + 1) / 2, apply = side * ((n + tile - 1) / tile);
+        for (uint64_t slices = 1; slices <= 8; ++slices) {
+            const uint64_t each = (k_gram + slices - 1) / slices;
+            if (slices > 1 && (a.batch * square * slices > units || (slices - 1) * each >= k_gram)) break;       // no empty slice
+            const uint64_t work = a.batch * (square * (k_gram + k_poly) + apply * 2 * k_poly + ((1 + slices) * square + apply) * kTileCost);
+            auto rounds = [&](uint64_t tiles) { return (tiles + units - 1) / units; };
+            const uint64_t path = (rounds(square * slices) * each + rounds(square) * k_poly + rounds(apply) * 2 * k_poly) * 620 + 3 * start +
+                                  (slices > 1 ? kJoinCost : 0), even = work * 620 / units, cost = path > even ? path : even;
+            if (cost < least) {
+                least = cost;
+                best = {wide != 0, (uint32_t)slices};
+            }
+        }
+    }
+    return best;
+}
+
 struct OrthoLayout {
     uint32_t ld_x, ld_a, m;
     uint64_t x_elems, a_elems;                   // per matrix
-    uint64_t off_partial, off_factor, off_count, off_x[2], off_lo, off_a, off_p, total;
+    uint64_t off_partial, off_factor, off_count, off_x[2], off_lo, off_a, off_p, off_slices, total;
 };
 OrthoLayout layout_of(const OrthoArgs& a) {
     OrthoLayout l;
@@ -400,6 +520,8 @@ OrthoLayout layout_of(const OrthoArgs& a) {
     l.off_lo = take(2 * round_up(a.batch * l.x_elems * 2, 256));
     l.off_a = take(a.batch * l.a_elems * 2);
     l.off_p = take(a.batch * l.a_elems * 2);
+    const uint32_t slices = chain_tiles(a).slices;
+    l.off_slices = take(slices > 1 ? slices * a.batch * l.a_elems * 4 : 0);
     l.total = at;
     return l;
 }
@@ -767,6 +889,12 @@ cudaError_t launch_small(const OrthoArgs& a, uint32_t align, const OpDevice& dev
 
 }  // namespace
 
+template <bool SLICED>
+cudaError_t launch_chain(bool wide, const ChainShape& p, const ChainArgs& ea, uint32_t units, cudaStream_t st) {
+    auto launch = wide ? launch_plan<2, 256, ChainPlan<SLICED>, ChainEpi<SLICED>> : launch_plan<1, 128, ChainPlan<SLICED>, ChainEpi<SLICED>>;
+    return launch(false, ChainPlan<SLICED>{p}, ea, units, st);
+}
+
 uint64_t orthogonalize_workspace(const OrthoArgs& a) { return is_small(a) ? 0 : layout_of(a).total; }
 
 int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t st) {
@@ -806,7 +934,7 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     SK_OP_CUDA(launch_kernel(true, k_ortho_square, dim3(sq.blocks, batch), 256, 0, st, sq));
     SK_OP_CUDA(launch_kernel(true, k_ortho_scale, dim3(sq.blocks, batch), 256, 0, st, sq));
 
-    ChainEpi::Args ea{};
+    ChainArgs ea{};
     ea.gram = gram;
     ea.poly = poly;
     for (int i = 0; i < 2; ++i) { ea.hi[i] = x[i]; ea.lo[i] = lo[i]; }
@@ -825,7 +953,7 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     ea.align = align;
     ea.steps = (uint32_t)a.steps;
 
-    ChainPlan p{};
+    ChainShape p{};
     bool ok = true;
     for (int i = 0; i < 2; ++i) {
         const Operand g{x[i], a.rows, a.cols, l.ld_x, l.x_elems, batch, tall}, h{x[i], a.rows, a.cols, l.ld_x, l.x_elems, batch, !tall},
@@ -847,29 +975,26 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     p.k_gram = (uint32_t)(((tall ? a.rows : a.cols) + kGemmK - 1) / kGemmK);
     p.count = sq.count;
     p.status = dev.status;
-    // Pairs of blocks on 256 x 256 or single ones on 128 x 128: a stage takes both the same time (some 620 cycles, see launch_products), the
-    // pair does twice the work per SM in it.  The time is about that of the work on all units, but at least that of one matrix's dependent
-    // products, whose starts and epilogues are shorter with the small tile (7000 cycles, 12,000).
-    auto cost = [&](uint64_t tile, uint64_t units, uint64_t start) {
-        const uint64_t side = (m + tile - 1) / tile, sq_tiles = side * (side + 1) / 2, ap = ((a.rows + tile - 1) / tile) * ((a.cols + tile - 1) / tile);
-        const uint64_t stages = p.k_gram + p.k_poly, work = batch * (sq_tiles * stages + ap * 2 * p.k_poly + (2 * sq_tiles + ap) * kTileCost);
-        auto rounds = [&](uint64_t tiles) { return (tiles + units - 1) / units; };
-        const uint64_t path = (rounds(sq_tiles) * stages + rounds(ap) * 2 * p.k_poly) * 620 + 3 * start, even = work * 620 / units;
-        return path > even ? path : even;
-    };
-    const bool wide = cost(256, (uint64_t)dev.sm_count / 2, 12000) <= cost(128, (uint64_t)dev.sm_count, 7000);
-    const uint32_t tile = wide ? 256 : 128, slots = (uint32_t)dev.sm_count / (wide ? 2 : 1);
+    const ChainTiles c = chain_tiles(a);
+    const uint32_t tile = c.wide ? 256 : 128, slots = (uint32_t)dev.sm_count / (c.wide ? 2 : 1);
     p.side = (m + tile - 1) / tile;
     p.square = p.side * (p.side + 1) / 2;
     p.tiles_m = (p.rows + tile - 1) / tile;
     p.tiles_n = (p.cols + tile - 1) / tile;
     p.apply = p.tiles_m * p.tiles_n;
-    p.signals = (wide ? 2 : 1) * ChainEpi::kWarps;
-    if ((uint64_t)a.steps * batch * (2ull * p.square + p.apply) * p.signals >= (1ull << 32))
+    p.slices = c.slices;
+    p.k_slice = (p.k_gram + c.slices - 1) / c.slices;
+    if (c.slices > 1) {
+        ea.slices = (float*)(ws + l.off_slices);
+        ea.slice_stride = batch * l.a_elems;
+        ea.slice_count = c.slices;
+        ea.join_cols = tile / ChainEpi<true>::kWarps;
+    }
+    p.signals = (c.wide ? 2 : 1) * ChainEpi<true>::kWarps;
+    if ((uint64_t)a.steps * batch * ((c.slices > 1 ? 1ull + c.slices + kJoinParts : 2ull) * p.square + p.apply) * p.signals >= (1ull << 32))
         return set_error(SK_EINVAL, "sk_orthogonalize: batch * rows * cols is too large for one call");
-    const uint32_t most_tiles = batch * (p.square > p.apply ? p.square : p.apply), units = most_tiles < slots ? most_tiles : slots;
-    auto launch = wide ? launch_plan<2, 256, ChainPlan, ChainEpi> : launch_plan<1, 128, ChainPlan, ChainEpi>;
-    SK_OP_CUDA(launch(false, p, ea, units, st));
+    const uint32_t most_tiles = batch * (p.square * p.slices > p.apply ? p.square * p.slices : p.apply), units = most_tiles < slots ? most_tiles : slots;
+    SK_OP_CUDA(c.slices > 1 ? launch_chain<true>(c.wide, p, ea, units, st) : launch_chain<false>(c.wide, p, ea, units, st));
     return SK_OK;
 }
 

@@ -386,6 +386,18 @@ def test_orthogonalize(ops, batch, rows, cols, dtype):
     ops.sync()
 
 
+# few tiles and a long side: the gram product's sums in slices, of both tile sizes, ragged ones and several matrices
+@pytest.mark.parametrize("batch,rows,cols", [(1, 200, 2100), (1, 2688, 256), (2, 333, 4001), (1, 1000, 4096), (1, 2500, 640), (6, 130, 4100)])
+def test_orthogonalize_long_side(ops, batch, rows, cols):
+    u = randn(1, batch, rows, 4) @ randn(2, batch, 4, cols) + randn(3, batch, rows, cols, scale=0.3)
+    for dtype in (torch.float32, torch.bfloat16):
+        out = ops.orthogonalize(u.to(dtype))
+        ortho_close(out, ortho_ref(u.to(dtype)))
+        for _ in range(3):
+            assert torch.equal(ops.orthogonalize(u.to(dtype)), out)
+    ops.sync()
+
+
 @pytest.mark.parametrize("steps", [1, 2, 3, 4, 6])
 def test_orthogonalize_steps_and_coefficients(ops, steps):
     u = randn(1, 200, 264)
