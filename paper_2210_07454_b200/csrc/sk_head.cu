@@ -241,9 +241,9 @@ __global__ void __launch_bounds__(256) k_head_sum(const float* sum, uint32_t sli
 // take no part become zero.  The backward pass always takes the hidden states through this: in dW a token without a target is multiplied
 // by zeros, and whatever its row holds (padding may hold infinities or NaN) must not survive that.
 struct PackArgs {
-    struct One { const uint16_t* src; uint16_t* dst; uint64_t ld, rows; const int64_t* targets; } m[2];
+    struct One { const uint16_t* src; uint16_t* dst; uint64_t ld, rows; const int64_t* targets; uint32_t ld_dst; } m[2];
     uint64_t vocab;
-    uint32_t ld_dst, cols, first_blocks;         // blocks of the first matrix
+    uint32_t cols, first_blocks;                 // blocks of the first matrix
     uint32_t copy_blocks;                        // of all matrices
     const float* dloss;                          // with a factor: one block more
     float* factor;
@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(256) k_head_pack(const __grid_constant__ PackA
     }
     const uint32_t which = blockIdx.x >= a.first_blocks;
     const PackArgs::One& m = a.m[which];
-    const uint32_t groups = a.ld_dst / 8, block = which ? blockIdx.x - a.first_blocks : blockIdx.x;
+    const uint32_t groups = m.ld_dst / 8, block = which ? blockIdx.x - a.first_blocks : blockIdx.x;
     const uint64_t total = m.rows * groups, step = (uint64_t)(which ? a.copy_blocks - a.first_blocks : a.first_blocks) * 256;
     const bool vec = (uintptr_t)m.src % 16 == 0 && m.ld % 8 == 0, half = (uintptr_t)m.src % 8 == 0 && m.ld % 4 == 0;
     for (uint64_t q = block * 256ull + threadIdx.x; q < total; q += step) {
@@ -296,7 +296,7 @@ __global__ void __launch_bounds__(256) k_head_pack(const __grid_constant__ PackA
             for (uint32_t i = 0; i < 8; ++i) e[i] = c + i < a.cols ? s[i] : 0;
             v = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
         }
-        *(uint4*)(m.dst + r * a.ld_dst + c) = v;
+        *(uint4*)(m.dst + r * m.ld_dst + c) = v;
     }
 }
 
@@ -304,7 +304,7 @@ bool addressable(const void* p, uint64_t ld) { return (uintptr_t)p % 16 == 0 && 
 
 struct HeadLayout {
     bool pack_h, pack_w;
-    uint64_t ld_pack, off_h, off_w, off_part, off_target, off_factor, off_g, ld_g, off_sum, ld_sum, sum_stride, piece, total;
+    uint64_t ld_h, ld_w, off_h, off_w, off_part, off_target, off_factor, off_g, ld_g, off_sum, ld_sum, sum_stride, piece, total;
     uint32_t slices;                             // of the vocabulary's pieces in the product that gives dhidden
     bool wide;                                   // tiles of the two gradient products
 };
@@ -335,9 +335,13 @@ HeadLayout layout_of(const HeadArgs& a, bool backward) {
     auto take = [&](uint64_t bytes) { const uint64_t r = at; at += round_up(bytes, 256); return r; };
     l.pack_h = backward || !addressable(a.hidden, a.ld_hidden);
     l.pack_w = !addressable(a.weight, a.ld_weight);
-    l.ld_pack = round_up(a.width, 8);
-    if (l.pack_h) l.off_h = take(a.tokens * l.ld_pack * 2);
-    if (l.pack_w) l.off_w = take(a.vocab * l.ld_pack * 2);
+    // Rows of whole 128-byte lines, as a tile's rows of 64 values are fetched: for the hidden states and G, which every tile reads (1000 x 32003 x 1000
+    // backward: 186 us with rows that are multiples of 16 bytes, 181 with G in whole lines, 173 with both).  The weights' copy costs
+    // more than that would save.
+    l.ld_h = round_up(a.width, 64);
+    l.ld_w = round_up(a.width, 8);
+    if (l.pack_h) l.off_h = take(a.tokens * l.ld_h * 2);
+    if (l.pack_w) l.off_w = take(a.vocab * l.ld_w * 2);
     if (!backward) {
         l.off_part = take(2 * ((a.vocab + 127) / 128) * a.tokens * sizeof(float2));
         l.off_target = take(a.tokens * 4);
@@ -345,7 +349,7 @@ HeadLayout layout_of(const HeadArgs& a, bool backward) {
         l.off_factor = take(4);
         uint64_t pieces = (a.tokens * a.vocab * 2 + kPieceBytes - 1) / kPieceBytes;
         l.piece = round_up((a.vocab + pieces - 1) / pieces, 256);
-        l.ld_g = l.piece < round_up(a.vocab, 32) ? l.piece : round_up(a.vocab, 32);
+        l.ld_g = l.piece < round_up(a.vocab, 64) ? l.piece : round_up(a.vocab, 64);
         l.off_g = take(a.tokens * l.ld_g * 2);
         l.ld_sum = round_up(a.width, 32);
         l.sum_stride = a.tokens * l.ld_sum;
@@ -364,22 +368,21 @@ int pack_operands(const HeadArgs& a, bool backward, const HeadLayout& l, const O
     *h = a.hidden; *w = a.weight; *ld_h = a.ld_hidden; *ld_w = a.ld_weight;
     PackArgs p{};
     uint32_t n = 0, blocks[2] = {0, 0};
-    auto add = [&](const void* src, uint64_t ld, uint64_t off, uint64_t rows, const int64_t* targets) {
-        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, rows, targets};
-        const uint64_t want = (rows * (l.ld_pack / 8) + 255) / 256, most = (uint64_t)dev.sm_count * 16;
+    auto add = [&](const void* src, uint64_t ld, uint64_t off, uint64_t ld_dst, uint64_t rows, const int64_t* targets) {
+        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, rows, targets, (uint32_t)ld_dst};
+        const uint64_t want = (rows * (ld_dst / 8) + 255) / 256, most = (uint64_t)dev.sm_count * 16;
         blocks[n++] = (uint32_t)(want < most ? want : most);
     };
     if (l.pack_h) {
-        add(a.hidden, a.ld_hidden, l.off_h, a.tokens, backward ? a.targets : nullptr);
-        *h = ws + l.off_h; *ld_h = l.ld_pack;
+        add(a.hidden, a.ld_hidden, l.off_h, l.ld_h, a.tokens, backward ? a.targets : nullptr);
+        *h = ws + l.off_h; *ld_h = l.ld_h;
     }
     if (l.pack_w) {
-        add(a.weight, a.ld_weight, l.off_w, a.vocab, nullptr);
-        *w = ws + l.off_w; *ld_w = l.ld_pack;
+        add(a.weight, a.ld_weight, l.off_w, l.ld_w, a.vocab, nullptr);
+        *w = ws + l.off_w; *ld_w = l.ld_w;
     }
     if (!n) return SK_OK;
     p.vocab = a.vocab;
-    p.ld_dst = (uint32_t)l.ld_pack;
     p.cols = (uint32_t)a.width;
     p.first_blocks = blocks[0];
     p.copy_blocks = blocks[0] + blocks[1];

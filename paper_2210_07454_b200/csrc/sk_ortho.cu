@@ -24,7 +24,7 @@ namespace sk {
 namespace {
 
 constexpr float kScale = 4096.0f, kUnscale = 1.0f / 4096.0f;     // 2^12
-constexpr uint32_t kPadCols = 32;                                // leading dimensions: whole 32-column chunks
+constexpr uint32_t kPadCols = 64;                                // leading dimensions: whole 128-byte lines
 
 // ---- all products of the iteration in one launch --------------------------------------------------------------------------
 // The tiles of A = X X^T, P = a I + b A + c A^2 and X <- P X of all steps and matrices, in this order, dealt out to the units in
