@@ -710,7 +710,8 @@ int launch_norm_backward(const NormBackwardArgs& a, int sm_count, cudaStream_t s
 }
 
 // Extra blocks for dw and db (norm_columns), where they beat the partial rows and the second kernel: few rows, that L2 holds.
-uint32_t norm_backward_slabs(uint64_t rows, uint64_t cols) { return rows <= kSlabRows && cols <= 8192 ? (uint32_t)((cols + 7) / 8) : 0; }
+// (8184 columns: with up to seven values before a row that a block's threads still hold; the kernel for longer rows has none.)
+uint32_t norm_backward_slabs(uint64_t rows, uint64_t cols) { return rows <= kSlabRows && cols <= 8184 ? (uint32_t)((cols + 7) / 8) : 0; }
 
 uint64_t norm_backward_workspace(uint64_t rows, uint64_t cols, int sm_count) {
     if (norm_backward_slabs(rows, cols)) return 0;

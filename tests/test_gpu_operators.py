@@ -76,6 +76,17 @@ def test_layer_norm(ops, cols, dtype):
 @pytest.mark.parametrize("rows,cols", [(1, 1), (1, 64), (3, 17), (9, 256), (33, 257), (700, 768), (2500, 96), (5, 1025), (301, 2048), (7, 2049), (5, 8192), (256, 300), (257, 300), (200, 1001), (260, 500),
                                        (3, 8200), (700, 9000)])
 def test_layer_norm_backward(ops, rows, cols, dtype):
+    backward_close(ops, rows, cols, dtype)
+
+
+# few rows of nearly the most columns that a block's threads hold, off the 16-byte boundary
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols", [(3, 8185), (40, 8190), (256, 8191), (5, 8184), (2, 8180)])
+def test_layer_norm_backward_nearly_long_rows(ops, rows, cols, dtype):
+    backward_close(ops, rows, cols, dtype)
+
+
+def backward_close(ops, rows, cols, dtype):
     x = randn(1, rows, cols, dtype=dtype, scale=1.5)
     dy = randn(2, rows, cols, dtype=dtype)
     w = 1 + randn(3, cols, scale=0.1)
