@@ -374,37 +374,51 @@ __global__ void __launch_bounds__(kLongThreads) k_norm_long(const NormArgs a) {
     }
 }
 
-// dw and db of eight columns over all rows, threads / 8 rows at a time: for few rows, as extra blocks of the row kernel's launch.
-// They read x and dy a second time, from L2, and need neither partial rows nor a kernel after them.
-template <typename T>
-__device__ void norm_columns(const NormBackwardArgs& a, uint32_t slab, float2 (*sums)[8]) {
-    const uint32_t x = threadIdx.x & 7, y = threadIdx.x >> 3, groups = blockDim.x >> 3;
-    const uint64_t c = (uint64_t)slab * 8 + x;
-    const bool live = c < a.cols;
-    const T *px = (const T*)a.x + c, *pd = (const T*)a.dy + c;
-    float2 s = make_float2(0, 0);
-    if (live) {
-#pragma unroll 8
+// dw and db of a slab of columns over all rows: for few rows, as extra blocks of the row kernel's launch.  They read x and dy a second time,
+// from L2, and need neither partial rows nor a kernel after them.  A row of the slab is 32 bytes in two 16-byte accesses, or eight
+// single elements where rows do not lie on 16-byte boundaries.
+template <int V> struct Slab { static constexpr uint32_t kCols = V > 1 ? 2 * V : 8; };
+template <typename T, int V>
+__device__ void norm_columns(const NormBackwardArgs& a, uint32_t slab, float2 (*sums)[Slab<V>::kCols]) {
+    constexpr uint32_t kCols = Slab<V>::kCols, kLanes = kCols / V;           // lanes to a row
+    const uint32_t x = threadIdx.x % kLanes, y = threadIdx.x / kLanes, groups = blockDim.x / kLanes;
+    const uint64_t c = (uint64_t)slab * kCols + x * V;
+    float2 s[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k) s[k] = make_float2(0, 0);
+    if (c < a.cols) {                            // a multiple of V
+        const T *px = (const T*)a.x + c, *pd = (const T*)a.dy + c;
+#pragma unroll(V > 1 ? 4 : 8)
         for (uint32_t r = y; r < (uint32_t)a.rows; r += groups) {
-            const float d = to_float(pd[r * a.ld_dy]), h = (to_float(px[r * a.ld_x]) - a.mean[r]) * a.rstd[r];
-            s.x += d * h;
-            s.y += d;
+            const Pack<T, V> dy = *(const Pack<T, V>*)(pd + r * a.ld_dy), in = *(const Pack<T, V>*)(px + r * a.ld_x);
+            const float mean = a.mean[r], rstd = a.rstd[r];
+#pragma unroll
+            for (int k = 0; k < V; ++k) {
+                const float d = to_float(dy.v[k]);
+                s[k].x += d * ((to_float(in.v[k]) - mean) * rstd);
+                s[k].y += d;
+            }
         }
     }
 #pragma unroll
-    for (int o = 8; o < 32; o *= 2) {
-        s.x += __shfl_xor_sync(0xffffffffu, s.x, o);
-        s.y += __shfl_xor_sync(0xffffffffu, s.y, o);
-    }
-    if ((threadIdx.x & 31) < 8) sums[threadIdx.x >> 5][x] = s;
-    __syncthreads();
-    if (threadIdx.x < 8 && live) {
-        for (uint32_t w = 1; w < (blockDim.x >> 5); ++w) {
-            s.x += sums[w][x].x;
-            s.y += sums[w][x].y;
+    for (int k = 0; k < V; ++k) {
+#pragma unroll
+        for (int o = kLanes; o < 32; o *= 2) {
+            s[k].x += __shfl_xor_sync(0xffffffffu, s[k].x, o);
+            s[k].y += __shfl_xor_sync(0xffffffffu, s[k].y, o);
         }
-        if (a.dweight) store_as(a.dweight, a.dw_type, c, s.x);
-        if (a.dbias) store_as(a.dbias, a.dw_type, c, s.y);
+        if ((threadIdx.x & 31) < kLanes) sums[threadIdx.x >> 5][x * V + k] = s[k];
+    }
+    __syncthreads();
+    const uint64_t col = (uint64_t)slab * kCols + threadIdx.x;
+    if (threadIdx.x < kCols && col < a.cols) {
+        float2 t = sums[0][threadIdx.x];
+        for (uint32_t w = 1; w < (blockDim.x >> 5); ++w) {
+            t.x += sums[w][threadIdx.x].x;
+            t.y += sums[w][threadIdx.x].y;
+        }
+        if (a.dweight) store_as(a.dweight, a.dw_type, col, t.x);
+        if (a.dbias) store_as(a.dbias, a.dw_type, col, t.y);
     }
 }
 
@@ -421,8 +435,9 @@ __global__ void __launch_bounds__(MAXT, BLOCKS) k_norm_backward(const NormBackwa
     const float inv = 1.0f / (float)at.cols;
     chain_acquire();
     if (blockIdx.x >= gridDim.x - a.slabs) {
-        __shared__ float2 sums[MAXT / 32][8];
-        norm_columns<T>(a, blockIdx.x - (gridDim.x - a.slabs), sums);
+        constexpr int kV = SHIFT ? 1 : V;
+        __shared__ float2 sums[MAXT / 32][Slab<kV>::kCols];
+        norm_columns<T, kV>(a, blockIdx.x - (gridDim.x - a.slabs), sums);
         return;
     }
     F2 w[kQ], dw[kQ], db[kQ];
@@ -626,10 +641,13 @@ int norm_typed(const NormArgs& a, int sm_count, cudaStream_t st) {
     return SK_OK;
 }
 
-// Up to so many rows dw and db come from extra blocks of the one launch: 16 x 768 bf16 2.8 us against 6.4 with partial rows and a second kernel,
-// 128 x 4096 7.5 and 11.5, 256 x 768 7.7 and 7.2, 512 x 768 12.1 and 7.8 (beside which the second launch and the
-// workspace cost the host some 5 us).
-constexpr uint64_t kSlabRows = 256;
+// Few rows: dw and db come from extra blocks of the one launch, which saves partial rows, the second kernel, and some 3 us of the host's time.
+// Up to 256 rows always (16 x 768 bf16 2.8 us against 6.4); where rows lie on 16-byte boundaries and have at most 16 KB, up to 1024:
+// 512 x 768 bf16 3.9 us against 6.8, 1024 x 4096 10.4 and 18.7, fp32 512 x 768 5.4 and 5.7, 1024 x 4096 14.6 and 13.8; but 1024 x 8192 32.1 and 24.6,
+// 2048 x 768 16.6 and 8.8.
+// (8184 columns: with up to seven values before a row that a block's threads still hold; the kernel for longer rows has no extra blocks.)
+constexpr uint64_t kSlabRows = 256, kSlabCols = 8184, kSlabRowsWide = 1024, kSlabBytesWide = 16384;
+bool always_slabs(uint64_t rows, uint64_t cols) { return rows <= kSlabRows && cols <= kSlabCols; }
 // The plan decides how many partial rows there are, so the workspace's size needs it too.
 // wide16: 16-bit rows by 16-byte accesses, of which a lane holds three before warps share a row (16384 x 768 bf16: 17.5 us, 21.2 with
 // two warps a row; fp32 rows, as many bytes in flight, are at the memory's rate either way).
@@ -645,8 +663,13 @@ cudaError_t run_backward(const NormBackwardArgs& a, const NormPlan& p, uint32_t 
     return launch_rows<k_norm_backward<T, V, PER / V, G, MAXT, BLOCKS, SHIFT>>(dim3(blocks), p.threads, Rows<T, V, PER / V, 2, SHIFT>::smem(p.threads), st, a);
 }
 template <typename T, int V, bool SHIFT>
-int norm_backward_typed(const NormBackwardArgs& a, int sm_count, cudaStream_t st) {
-    constexpr bool kWide16 = V == 8;
+int norm_backward_typed(NormBackwardArgs a, int sm_count, cudaStream_t st) {
+    constexpr bool kWide16 = V == 8, kWhole = V > 1 && !SHIFT;
+    if ((a.dweight || a.dbias) && (always_slabs(a.rows, a.cols) || (kWhole && a.rows <= kSlabRowsWide && a.cols * sizeof(T) <= kSlabBytesWide))) {
+        constexpr uint32_t kCols = Slab<SHIFT ? 1 : V>::kCols;
+        a.slabs = (uint32_t)((a.cols + kCols - 1) / kCols);
+        a.partial = nullptr;
+    }
     const NormPlan p = plan_backward(a.cols + (SHIFT ? V - 1 : 0), kWide16);
     const uint32_t blocks = backward_blocks(a.rows, p, sm_count) + a.slabs;
     cudaError_t e = cudaSuccess;
@@ -709,12 +732,8 @@ int launch_norm_backward(const NormBackwardArgs& a, int sm_count, cudaStream_t s
                                : norm_backward_placed<__half>(a, sm_count, st);
 }
 
-// Extra blocks for dw and db (norm_columns), where they beat the partial rows and the second kernel: few rows, that L2 holds.
-// (8184 columns: with up to seven values before a row that a block's threads still hold; the kernel for longer rows has none.)
-uint32_t norm_backward_slabs(uint64_t rows, uint64_t cols) { return rows <= kSlabRows && cols <= 8184 ? (uint32_t)((cols + 7) / 8) : 0; }
-
 uint64_t norm_backward_workspace(uint64_t rows, uint64_t cols, int sm_count) {
-    if (norm_backward_slabs(rows, cols)) return 0;
+    if (always_slabs(rows, cols)) return 0;
     uint32_t most = 0;                           // the rows' alignment decides between the plans: room for any
     for (uint64_t extra : {0, 3, 7})
         for (bool wide16 : {false, true}) {

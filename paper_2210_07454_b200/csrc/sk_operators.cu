@@ -112,9 +112,8 @@ int sk_layer_norm_backward(const void* dy, uint64_t ld_dy, const void* x, uint64
     OpDevice dev;
     if (int rc = op_device(&dev)) return rc;
     const bool sums = dweight || dbias;
-    const uint32_t slabs = sums ? norm_backward_slabs(rows, cols) : 0;
     if (int rc = check_workspace(who, workspace, workspace_bytes, sums ? norm_backward_workspace(rows, cols, dev.sm_count) : 0)) return rc;
-    const NormBackwardArgs a{dy, x, weight, mean, rstd, dx, dweight, dbias, sums && !slabs ? (float*)workspace : nullptr, slabs, rows, cols, ld_dy, ld_x, ld_dx,
+    const NormBackwardArgs a{dy, x, weight, mean, rstd, dx, dweight, dbias, sums ? (float*)workspace : nullptr, 0, rows, cols, ld_dy, ld_x, ld_dx,
                              type, weight_type, dweight_type};
     return launch_norm_backward(a, dev.sm_count, (cudaStream_t)stream);
 }

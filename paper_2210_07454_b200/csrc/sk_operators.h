@@ -196,14 +196,13 @@ struct NormBackwardArgs {
     const void *dy, *x, *weight;
     const float *mean, *rstd;
     void *dx, *dweight, *dbias;
-    float* partial;                  // [blocks][2][cols], or null where extra blocks form the sums of the rows
-    uint32_t slabs;                  // such blocks (norm_backward_slabs)
+    float* partial;                  // [blocks][2][cols], or null where extra blocks form the sums over the rows
+    uint32_t slabs;                  // such blocks, set by the launcher
     uint64_t rows, cols, ld_dy, ld_x, ld_dx;
     int type, w_type, dw_type;
 };
 int launch_norm(const NormArgs& a, int sm_count, cudaStream_t st);
 int launch_norm_backward(const NormBackwardArgs& a, int sm_count, cudaStream_t st);
-uint32_t norm_backward_slabs(uint64_t rows, uint64_t cols);
 uint64_t norm_backward_workspace(uint64_t rows, uint64_t cols, int sm_count);
 
 // hidden (tokens x width) times vocabulary matrix (vocab x width), both of one 16-bit type

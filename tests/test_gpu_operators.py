@@ -86,6 +86,13 @@ def test_layer_norm_backward_nearly_long_rows(ops, rows, cols, dtype):
     backward_close(ops, rows, cols, dtype)
 
 
+# the rows' number at which the weights' gradients are formed another way, with whole 16-byte accesses
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols", [(64, 8), (65, 24), (256, 8192), (257, 768), (300, 8184), (1000, 40), (1023, 1008), (1024, 4096), (1024, 4104), (1025, 256)])
+def test_layer_norm_backward_some_hundred_rows(ops, rows, cols, dtype):
+    backward_close(ops, rows, cols, dtype)
+
+
 def backward_close(ops, rows, cols, dtype):
     x = randn(1, rows, cols, dtype=dtype, scale=1.5)
     dy = randn(2, rows, cols, dtype=dtype)
