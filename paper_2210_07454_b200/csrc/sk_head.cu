@@ -7,8 +7,8 @@
 // it (32 bits), and the target's logit; a small kernel joins the pieces.  The logits never leave the SM.
 // Backward: the vocabulary is taken in pieces.  A product recomputes a piece's logits and its epilogue writes the piece of G (in the
 // inputs' 16-bit type, the operand type of the two products that follow); then dW's rows of the piece and the piece's share
-// of dhidden, which is added up in 32 bits over the pieces.  Bound by the tensor cores (2 T V D multiply-add flops forward, 6 backward plus 2 for
-// the recomputation); for few tokens by reading W.
+// of dhidden, which is added up in 32 bits over the pieces.  Bound by the tensor cores (2 T V D flops forward, 4 backward plus 2
+// for the recomputation); for few tokens by reading W.
 //
 // A row whose target is negative takes no part: loss 0, gradient 0.  A target >= vocab gives a loss of NaN and no gradient.
 #include "sk_gemm.cuh"
