@@ -671,19 +671,26 @@ int norm_backward_typed(NormBackwardArgs a, int sm_count, cudaStream_t st) {
         a.partial = nullptr;
     }
     const NormPlan p = plan_backward(a.cols + (SHIFT ? V - 1 : 0), kWide16);
-    const uint32_t blocks = backward_blocks(a.rows, p, sm_count) + a.slabs;
-    cudaError_t e = cudaSuccess;
-    if constexpr (kWide16) {
-        if (p.per == 24) e = run_backward<T, V, SHIFT, 24, 32, kWarpThreads, 3>(a, p, blocks, st);
+    const uint32_t row_blocks = backward_blocks(a.rows, p, sm_count);
+    auto run = [&](uint32_t blocks) {
+        if constexpr (kWide16) {
+            if (p.per == 24) return run_backward<T, V, SHIFT, 24, 32, kWarpThreads, 3>(a, p, blocks, st);
+        }
+        if (p.lanes == 8) return run_backward<T, V, SHIFT, 8, 8, kWarpThreads, 6>(a, p, blocks, st);
+        if (p.lanes == 32 && p.per == 8) return run_backward<T, V, SHIFT, 8, 32, kWarpThreads, 6>(a, p, blocks, st);
+        if (p.lanes == 32) return run_backward<T, V, SHIFT, 16, 32, kWarpThreads, 4>(a, p, blocks, st);
+        if (p.threads) return run_backward<T, V, SHIFT, 16, 0, 512, 1>(a, p, blocks, st);
+        return launch_rows<k_norm_backward_long<T>>(dim3(blocks), kLongThreads, 0, st, a);
+    };
+    if (a.slabs && (!a.dx || a.dx == a.dy || a.dx == a.x)) {         // in place the extra blocks would read what the others write: they go first
+        SK_OP_CUDA(run(a.slabs));
+        if (!a.dx) return SK_OK;
+        a.slabs = 0;
     }
-    if (p.lanes == 8) e = run_backward<T, V, SHIFT, 8, 8, kWarpThreads, 6>(a, p, blocks, st);
-    else if (p.lanes == 32 && p.per == 8) e = run_backward<T, V, SHIFT, 8, 32, kWarpThreads, 6>(a, p, blocks, st);
-    else if (p.lanes == 32 && p.per == 16) e = run_backward<T, V, SHIFT, 16, 32, kWarpThreads, 4>(a, p, blocks, st);
-    else if (p.threads && !p.lanes) e = run_backward<T, V, SHIFT, 16, 0, 512, 1>(a, p, blocks, st);
-    else if (!p.threads) e = launch_rows<k_norm_backward_long<T>>(dim3(blocks), kLongThreads, 0, st, a);
+    cudaError_t e = run(row_blocks + a.slabs);
     SK_OP_CUDA(e);
     if (a.partial) {
-        e = launch_kernel(true, k_norm_sum, dim3((uint32_t)((2 * a.cols + 7) / 8)), 256, 0, st, a.partial, blocks, (uint32_t)a.cols, a.dweight, a.dbias,
+        e = launch_kernel(true, k_norm_sum, dim3((uint32_t)((2 * a.cols + 7) / 8)), 256, 0, st, a.partial, row_blocks, (uint32_t)a.cols, a.dweight, a.dbias,
                           a.dw_type);
         SK_OP_CUDA(e);
     }

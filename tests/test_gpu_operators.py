@@ -115,6 +115,25 @@ def backward_close(ops, rows, cols, dtype):
     within(db, d.sum(0), (rows + 4) * e * d.abs().sum(0), "db")
 
 
+# y over x, and dx over dy or x: the same bits as apart, also where extra blocks read the inputs a second time
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("rows,cols", [(1, 8), (16, 768), (200, 4096), (256, 1001), (256, 8184), (700, 512), (1024, 4096), (1500, 768), (3000, 333), (40, 9000)])
+def test_layer_norm_in_place(ops, rows, cols, dtype):
+    x, dy, w = randn(1, rows, cols, dtype=dtype), randn(2, rows, cols, dtype=dtype), 1 + randn(3, cols, scale=0.1)
+    y, mean, rstd = ops.layer_norm(x, w, None)
+    same = x.clone()
+    assert ops.layer_norm(same, w, None, out=same)[0] is same and torch.equal(same, y)
+    want = ops.layer_norm_backward(dy, x, w, mean, rstd)
+    for over in (0, 1):
+        for _ in range(3):
+            pair = [dy.clone(), x.clone()]
+            got = ops.layer_norm_backward(*pair, w, mean, rstd, dx=pair[over])
+            assert got[0] is pair[over] and all(torch.equal(g, t) for g, t in zip(got, want))
+    only = ops.layer_norm_backward(dy, x, w, mean, rstd, dx=False)
+    assert only[0] is None and torch.equal(only[1], want[1]) and torch.equal(only[2], want[2])
+    ops.sync()
+
+
 def test_layer_norm_gradient_against_differences(ops):
     x, dy, w, b = randn(1, 6, 40), randn(2, 6, 40), 1 + randn(3, 40, scale=0.1), randn(4, 40)
     _, mean, rstd = ops.layer_norm(x, w, b)
