@@ -267,8 +267,8 @@ int sk_select_static(sk_state* state, uint32_t* idx_out);
  *     ld >= the row's length.  Outputs do not overlap inputs unless said.
  *   - type arguments are SK_F32, SK_BF16 or SK_F16.  Statistics and sums are fp32 (or wider) whatever the type.
  *   - workspace: device memory of at least the size that the matching ..._workspace function returns for the same sizes
- *     and pointers (asked with the same device current), 256-byte aligned, the caller's; contents do not matter before or after, and it must not be used by
- *     anything else until the call's kernels are done.  A size of 0 allows NULL.
+ *     and pointers (asked with the same device current), 256-byte aligned, the caller's; contents do not matter before
+ *     or after, and it must not be used by anything else until the call's kernels are done.  A size of 0 allows NULL.
  *   - stream: a cudaStream_t cast to void* (NULL = default stream).  Asynchronous; nothing allocates or synchronises.
  *   - Extents of zero are valid: outputs that remain (sums over no rows) are zeroed.
  *   - Infinities and NaN in an input row spread as the formulas say (into that row and into sums over rows), no further. */
@@ -324,8 +324,8 @@ int sk_linear_cross_entropy_backward(const float* dloss, const void* hidden, uin
  * one matrix to the next (>= rows*ld for outputs).  Inside, matrices are fp16 times 2^12 with fp32 sums, X as a pair of them until the last two
  * steps; the coefficients must keep singular values from [0,1] below 2 in every step, and |a| + |b| + |c| < 15.
  * momentum may be NULL.  1 <= steps <= 32; rows, cols <= 65536; batch <= 65535.  Matrices with a side of at most 128 and no side
- * above 4096 take one launch and no workspace; others one cooperative launch for all products, whose blocks wait for one another (so
- * they need the whole device: do not let such calls of two streams overlap with other kernels that never end). */
+ * above 4096 take one launch and no workspace.  Others take one cooperative launch for all products: it starts when up to one block
+ * per SM fits on the device at once, so it waits for kernels of other streams that hold their SMs. */
 uint64_t sk_orthogonalize_workspace(uint64_t batch, uint64_t rows, uint64_t cols);
 int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_update, int type, float* momentum,
                      uint64_t ld_momentum, uint64_t stride_momentum, float beta, int nesterov, void* out, uint64_t ld_out,
