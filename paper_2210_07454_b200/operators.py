@@ -4,7 +4,8 @@ and orthogonalised updates of matrix parameters.
 Argument marshalling only, like ``binding``: every operator runs in the CUDA library (``sk_layer_norm`` and so on in
 ``include/sketched_amsgrad.h``, which states the formulas).  Tensors are CUDA tensors of one device whose rows are
 contiguous; rows may be any distance apart.  Calls are asynchronous on torch's current stream of that device, or on
-``stream`` (a ``torch.cuda.Stream``); workspaces come from torch's allocator.  Outputs are allocated unless given.
+``stream`` (a ``torch.cuda.Stream``), behind what that stream has been given before: if the inputs are still being written elsewhere, let it wait
+first.  Workspaces come from torch's allocator.  Outputs are allocated unless given; wait for ``stream`` before reading them elsewhere.
 
 A small call costs the host a few microseconds more than its kernels, so the checks below ask cheap questions first.
 """
@@ -91,8 +92,20 @@ def _same_shape(t, like, name):
 
 
 # ---- streams, devices, memory ---------------------------------------------------------------------------------------------
-def _pointer_of(stream, device):
-    return _raw_stream(device) if stream is None else stream.cuda_stream
+def _on(stream, call, *given):
+    """call() with `stream` current: what it allocates then belongs to that stream.  (torch hands freed memory out again in the order of
+    the stream it was allocated for; taken from the caller's stream, it might still be in use by kernels that `stream` does not wait for.)
+    The tensors that are handed back are used on the caller's stream too, and must not be reused before it is done with them."""
+    for t in given:
+        if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != stream.device_index:
+            raise SkError(f"the stream is of device {stream.device_index}, a tensor is on device {t.get_device()}")
+    caller = torch.cuda.current_stream(stream.device)
+    with torch.cuda.stream(stream):
+        out = call()
+    for t in out if isinstance(out, tuple) else (out,):
+        if t is not None and not any(t is g for g in given):
+            t.record_stream(caller)
+    return out
 
 
 def _run(device, fn, *args):
@@ -102,14 +115,6 @@ def _run(device, fn, *args):
     else:
         with torch.cuda.device(device):
             _check(fn(*args))
-
-
-def _on(stream, *tensors):
-    """Tensors allocated here, on the current stream, but used on another."""
-    if stream is not None:
-        for t in tensors:
-            if t is not None:
-                t.record_stream(stream)
 
 
 def _new(shape, stride, dtype, device):
@@ -153,6 +158,8 @@ def _norm_weights(weight, bias, cols, device):
 def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     """y = (x - mean) rstd weight + bias over the last axis.  x: (..., cols) fp32, bf16 or fp16; weight, bias: (cols,) or None.
     Returns (y, mean, rstd): y like x, mean and rstd fp32 of x's leading shape."""
+    if stream is not None:
+        return _on(stream, lambda: layer_norm(x, weight, bias, eps, out), x, weight, bias, out)
     code = _tensor(x, "x", _TYPES)
     shape = x.shape
     if not shape:
@@ -172,16 +179,16 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
     else:
         mean = x.new_empty(shape[:-1], dtype=torch.float32)
         rstd = torch.empty_like(mean)
-    if stream is not None:
-        _on(stream, y, mean, rstd)
     _run(device, lib().sk_layer_norm, x.data_ptr(), ld, y.data_ptr(), ld_y, code, rows, cols, pw, pb, wcode, eps, mean.data_ptr(), rstd.data_ptr(),
-         _pointer_of(stream, device))
+         _raw_stream(device))
     return y, mean, rstd
 
 
 def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=None, stream=None):
     """Gradients of ``layer_norm`` from dy and what it returned.  Returns (dx, dweight, dbias): dx like x; dweight, dbias (cols,) of
     weight's type (fp32 without a weight).  ``dx``, ``dweight``, ``dbias``: tensors to write into, False to leave one out."""
+    if stream is not None:
+        return _on(stream, lambda: layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias), dy, x, weight, mean, rstd, dx, dweight, dbias)
     code = _tensor(x, "x", _TYPES)
     device, cols = x.get_device(), x.shape[-1] if x.dim() else 0
     if _tensor(dy, "dy", _TYPES, device) != code:
@@ -222,10 +229,8 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=
             raise SkError(f"dbias has type {dbias.dtype}, dweight {dtype}")
     need = lib().sk_layer_norm_backward_workspace(rows, cols) if rows and (pdw or pdb) else 0
     ws = _workspace(need, device)
-    if stream is not None:
-        _on(stream, dx, dweight, dbias, ws)
     _run(device, lib().sk_layer_norm_backward, dy.data_ptr(), ld_dy, x.data_ptr(), ld, pdx, ld_dx, code, rows, cols, pw, wcode, pm, pr, pdw, pdb,
-         _TYPES[dtype], _p(ws), need, _pointer_of(stream, device))
+         _TYPES[dtype], _p(ws), need, _raw_stream(device))
     return dx, dweight, dbias
 
 
@@ -247,14 +252,15 @@ def _head(hidden, weight, targets):
 def linear_cross_entropy(hidden, weight, targets, stream=None):
     """Softmax cross entropy of the logits hidden weight^T, which are never stored.  hidden: (tokens, width), weight: (vocab, width),
     both bf16 or both fp16; targets: (tokens,) int64, negative = the token takes no part.  Returns (loss, lse), fp32 (tokens,)."""
+    if stream is not None:
+        return _on(stream, lambda: linear_cross_entropy(hidden, weight, targets), hidden, weight, targets)
     device, code, tokens, vocab, width, ld_h, ld_w, pt = _head(hidden, weight, targets)
     loss, lse = _new((tokens,), (1,), torch.float32, device), _new((tokens,), (1,), torch.float32, device)
     ph, pw = hidden.data_ptr(), weight.data_ptr()
     need = lib().sk_linear_cross_entropy_workspace(ph, ld_h, pw, ld_w, tokens, vocab, width)
     ws = _workspace(need, device)
-    _on(stream, loss, lse, ws)
     _run(device, lib().sk_linear_cross_entropy, ph, ld_h, pw, ld_w, code, tokens, vocab, width, pt, loss.data_ptr(), lse.data_ptr(), _p(ws), need,
-         _pointer_of(stream, device))
+         _raw_stream(device))
     return loss, lse
 
 
@@ -262,6 +268,8 @@ def linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden=N
     """Gradients of ``linear_cross_entropy`` from dloss (fp32, the gradient with respect to every token's loss) and the lse it
     returned.  Returns (dhidden, dweight) of the inputs' type.  ``dhidden``, ``dweight``: tensors to write into (of the inputs' type or
     fp32; views of the gradient array of a step are fine), False to leave one out."""
+    if stream is not None:
+        return _on(stream, lambda: linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden, dweight), dloss, hidden, weight, targets, lse, dhidden, dweight)
     device, code, tokens, vocab, width, ld_h, ld_w, pt = _head(hidden, weight, targets)
     pd, pl = _vector(dloss, "dloss", tokens, _F32, device), _vector(lse, "lse", tokens, _F32, device)
     types = {hidden.dtype: code, torch.float32: 0}
@@ -279,9 +287,8 @@ def linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden=N
     ph, pw = hidden.data_ptr(), weight.data_ptr()
     need = lib().sk_linear_cross_entropy_backward_workspace(ph, ld_h, pw, ld_w, tokens, vocab, width)
     ws = _workspace(need, device)
-    _on(stream, dh, dw, ws)
     _run(device, lib().sk_linear_cross_entropy_backward, pd, ph, ld_h, pw, ld_w, code, tokens, vocab, width, pt, pl, _p(dh), ld_dh, type_dh, _p(dw),
-         ld_dw, type_dw, _p(ws), need, _pointer_of(stream, device))
+         ld_dw, type_dw, _p(ws), need, _raw_stream(device))
     return dh, dw
 
 
@@ -301,6 +308,8 @@ def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coef
     """The orthogonalised update of matrix parameters: ``steps`` Newton-Schulz products on U / (|U| + eps), U = update, or with a
     momentum (fp32, updated in place) momentum = beta momentum + update and U = update + beta momentum (nesterov) or momentum.
     update: (rows, cols) or (batch, rows, cols).  Returns out: the same shape, bf16 (fp16 for an fp16 update) unless given."""
+    if stream is not None:
+        return _on(stream, lambda: orthogonalize(update, momentum, beta, nesterov, steps, coefficients, eps, out), update, momentum, out)
     if not isinstance(update, torch.Tensor) or update.dim() not in (2, 3):
         raise SkError("update must be a CUDA tensor of 2 or 3 dimensions")
     device = update.get_device() if update.is_cuda else None
@@ -310,14 +319,12 @@ def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coef
         raise SkError("coefficients are three numbers (a, b, c)")
     if out is None:
         out = _new_like(update, torch.float16 if update.dtype == torch.float16 else torch.bfloat16, device)
-        _on(stream, out)
     po, ld_o, s_o, out_code = _batch_of(out, "out", update, _HALF, device)
     batch, (rows, cols) = (update.shape[0] if update.dim() == 3 else 1), update.shape[-2:]
     need = lib().sk_orthogonalize_workspace(batch, rows, cols)
     ws = _workspace(need, device)
-    _on(stream, ws)
     _run(device, lib().sk_orthogonalize, pu, ld_u, s_u, code, pm, ld_m, s_m, beta, int(nesterov), po, ld_o, s_o, out_code, batch, rows, cols, steps,
-         (C.c_float * 3)(*coefficients), eps, _p(ws), need, _pointer_of(stream, device))
+         (C.c_float * 3)(*coefficients), eps, _p(ws), need, _raw_stream(device))
     return out
 
 
