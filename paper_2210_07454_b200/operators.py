@@ -95,13 +95,17 @@ def _same_shape(t, like, name):
 def _on(stream, call, *given):
     """call() with `stream` current: what it allocates then belongs to that stream.  (torch hands freed memory out again in the order of
     the stream it was allocated for; taken from the caller's stream, it might still be in use by kernels that `stream` does not wait for.)
-    The tensors that are handed back are used on the caller's stream too, and must not be reused before it is done with them."""
+    The tensors that are handed back are used on the caller's stream too, and those that were given on `stream`: neither's memory must be
+    handed out again before that stream is done with it, whenever the caller drops them."""
     for t in given:
         if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != stream.device_index:
             raise SkError(f"the stream is of device {stream.device_index}, a tensor is on device {t.get_device()}")
     caller = torch.cuda.current_stream(stream.device)
     with torch.cuda.stream(stream):
         out = call()
+    for t in given:
+        if isinstance(t, torch.Tensor):
+            t.record_stream(stream)
     for t in out if isinstance(out, tuple) else (out,):
         if t is not None and not any(t is g for g in given):
             t.record_stream(caller)

@@ -85,12 +85,12 @@ class World:
         x, w, dy, mean, rstd = p(4, 8), p(8), p(4, 8), p(4), p(4)
         h, v, t, d = p(4, 8, dtype=torch.float16), p(6, 8, dtype=torch.float16), p(4, dtype=torch.int64), p(4)
         u, m, y = p(3, 5), p(3, 5), p(4, 8)
-        deep = p(2, 4, 8)
+        deep, dw = p(2, 4, 8), p(6, 8, dtype=torch.float16)
         return [("sk_layer_norm", (x, w), (y,), lambda s: o.layer_norm(x, w, out=y, stream=s)),
                 ("sk_layer_norm", (deep, w), (), lambda s: o.layer_norm(deep, w, w, stream=s)),
                 ("sk_layer_norm_backward", (dy, x, w, mean, rstd), (), lambda s: o.layer_norm_backward(dy, x, w, mean, rstd, stream=s)),
                 ("sk_linear_cross_entropy", (h, v, t), (), lambda s: o.linear_cross_entropy(h, v, t, stream=s)),
-                ("sk_linear_cross_entropy_backward", (d, h, v, t), (), lambda s: o.linear_cross_entropy_backward(d, h, v, t, d, stream=s)),
+                ("sk_linear_cross_entropy_backward", (d, h, v, t), (dw,), lambda s: o.linear_cross_entropy_backward(d, h, v, t, d, dweight=dw, stream=s)),
                 ("sk_orthogonalize", (u,), (m,), lambda s: o.orthogonalize(u, momentum=m, stream=s))]
 
 
@@ -124,6 +124,38 @@ def test_a_stream_of_another_device_is_refused(world):
         with pytest.raises(SkError):
             call(other)
     assert not world.called
+
+
+def test_tensors_given_to_a_stream_are_kept_for_it(world):
+    """A temporary that is dropped right after the call must not be handed out again before the given stream is done with it."""
+    for name, inputs, given, call in world.calls():
+        call(world.side)
+        for t in inputs + given:
+            assert world.side in t.recorded, name
+
+
+@pytest.mark.gpu
+def test_operators_on_a_stream_take_temporaries():
+    """Inputs and outputs that are dropped, and whose memory is written again, while the given stream is still busy."""
+    from paper_2210_07454_b200 import operators as ops
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x, gamma = torch.randn(4096, 512, generator=g, device="cuda"), torch.randn(512, generator=g, device="cuda")
+    u = torch.randn(300, 400, generator=g, device="cuda")
+    want, want_u = ops.layer_norm(x, gamma), ops.orthogonalize(u)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(5):
+        copies = [x.clone(), gamma.clone(), u.clone()]
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            torch.cuda._sleep(20_000_000)
+        got = ops.layer_norm(*copies[:2], stream=side)
+        got_u = ops.orthogonalize(copies[2], stream=side)
+        del copies
+        over = [torch.full_like(t, 7.0) for t in (x, gamma, u, x, gamma, u)]
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(got_u, want_u)
+        assert all(bool((t == 7).all()) for t in over)
 
 
 @pytest.mark.gpu
