@@ -20,6 +20,7 @@
 #include "sk_chain.cuh"
 #include "sk_operators.h"
 
+#include <atomic>
 #include <type_traits>
 
 namespace sk {
@@ -603,19 +604,29 @@ uint32_t norm_blocks(uint64_t rows, const NormPlan& p, int sm_count, uint32_t th
     return (uint32_t)(even <= most ? even : most / 8 * 8);       // a multiple of eight: a thread's rows are whole 16-byte steps apart
 }
 
-template <auto kernel, typename Args>
+// What a kernel may take of shared memory is a property of the kernel on a device, not of a launch, and calls of other row lengths may be
+// on their way in other threads: it is set once, to the most that any of its launches takes.
+template <auto kernel, uint32_t MOST, typename Args>
 cudaError_t launch_rows(dim3 grid, uint32_t threads, uint32_t smem, cudaStream_t st, const Args& a) {
-    if (smem > 24 * 1024) {                      // with the kernel's own arrays, perhaps beyond what needs no permission
-        const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    if constexpr (MOST > 24 * 1024) {            // with the kernel's own arrays, perhaps beyond what needs no permission
+        static std::atomic<bool> prepared[64];
+        int device = 0;
+        cudaError_t e = cudaGetDevice(&device);
         if (e != cudaSuccess) return e;
+        if (device >= 64 || !prepared[device]) {
+            e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST);
+            if (e != cudaSuccess) return e;
+            if (device < 64) prepared[device] = true;
+        }
     }
     return launch_kernel(true, kernel, grid, threads, smem, st, a);
 }
 
 template <typename T, int V, bool SHIFT, int PER, int G, int MAXT, int BLOCKS>
 cudaError_t run_norm(const NormArgs& a, const NormPlan& p, int sm_count, cudaStream_t st) {
-    return launch_rows<k_norm<T, V, PER / V, G, MAXT, BLOCKS, SHIFT>>(dim3(norm_blocks(a.rows, p, sm_count, MAXT * BLOCKS)), p.threads,
-                                                                      Rows<T, V, PER / V, 1, SHIFT>::smem(p.threads), st, a);
+    using In = Rows<T, V, PER / V, 1, SHIFT>;
+    return launch_rows<k_norm<T, V, PER / V, G, MAXT, BLOCKS, SHIFT>, In::smem(MAXT)>(dim3(norm_blocks(a.rows, p, sm_count, MAXT * BLOCKS)), p.threads,
+                                                                                      In::smem(p.threads), st, a);
 }
 template <typename T, int V, bool SHIFT>
 int norm_typed(const NormArgs& a, int sm_count, cudaStream_t st) {
@@ -636,7 +647,7 @@ int norm_typed(const NormArgs& a, int sm_count, cudaStream_t st) {
     else if (p.lanes) e = run_norm<T, V, SHIFT, 8, 32, kWarpThreads, 8>(a, p, sm_count, st);
     else if ((p = plan_block(cols, 16, 256)).threads) e = run_norm<T, V, SHIFT, 16, 0, 256, 3>(a, p, sm_count, st);
     else if ((p = plan_block(cols, 16, 1024)).threads) e = run_norm<T, V, SHIFT, 16, 0, 1024, 1>(a, p, sm_count, st);
-    else e = launch_rows<k_norm_long<T>>(dim3(norm_blocks(a.rows, p, sm_count, 2048)), kLongThreads, 0, st, a);
+    else e = launch_rows<k_norm_long<T>, 0>(dim3(norm_blocks(a.rows, p, sm_count, 2048)), kLongThreads, 0, st, a);
     SK_OP_CUDA(e);
     return SK_OK;
 }
@@ -660,7 +671,8 @@ NormPlan plan_backward(uint64_t cols, bool wide16) {
 uint32_t backward_blocks(uint64_t rows, const NormPlan& p, int sm_count) { return norm_blocks(rows, p, sm_count, p.per == 8 ? 768 : p.per == 24 ? 384 : 512); }
 template <typename T, int V, bool SHIFT, int PER, int G, int MAXT, int BLOCKS>
 cudaError_t run_backward(const NormBackwardArgs& a, const NormPlan& p, uint32_t blocks, cudaStream_t st) {
-    return launch_rows<k_norm_backward<T, V, PER / V, G, MAXT, BLOCKS, SHIFT>>(dim3(blocks), p.threads, Rows<T, V, PER / V, 2, SHIFT>::smem(p.threads), st, a);
+    using In = Rows<T, V, PER / V, 2, SHIFT>;
+    return launch_rows<k_norm_backward<T, V, PER / V, G, MAXT, BLOCKS, SHIFT>, In::smem(MAXT)>(dim3(blocks), p.threads, In::smem(p.threads), st, a);
 }
 template <typename T, int V, bool SHIFT>
 int norm_backward_typed(NormBackwardArgs a, int sm_count, cudaStream_t st) {
@@ -680,7 +692,7 @@ int norm_backward_typed(NormBackwardArgs a, int sm_count, cudaStream_t st) {
         if (p.lanes == 32 && p.per == 8) return run_backward<T, V, SHIFT, 8, 32, kWarpThreads, 6>(a, p, blocks, st);
         if (p.lanes == 32) return run_backward<T, V, SHIFT, 16, 32, kWarpThreads, 4>(a, p, blocks, st);
         if (p.threads) return run_backward<T, V, SHIFT, 16, 0, 512, 1>(a, p, blocks, st);
-        return launch_rows<k_norm_backward_long<T>>(dim3(blocks), kLongThreads, 0, st, a);
+        return launch_rows<k_norm_backward_long<T>, 0>(dim3(blocks), kLongThreads, 0, st, a);
     };
     if (a.slabs && (!a.dx || a.dx == a.dy || a.dx == a.x)) {         // in place the extra blocks would read what the others write: they go first
         SK_OP_CUDA(run(a.slabs));
