@@ -336,6 +336,11 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
  * it is not zero, after which it is cleared): bit 0, a product kernel gave up a wait and its outputs are invalid. */
 int sk_operators_sync(void* stream);
 
+/* Test hook: the products of the calling thread's next sk_orthogonalize, if they are the tiles of one cooperative launch, wait for more
+ * signals than are given, and every wait inside that kernel runs out after limit_ms (1..1000) milliseconds.  The kernel ends by
+ * itself, with out unspecified, and the next sk_operators_sync reports it. */
+int sk_test_operators_wait(uint32_t limit_ms);
+
 const char* sk_last_error(void);
 const char* sk_version(void);
 

@@ -20,7 +20,7 @@ EXPORTS = ["sk_create", "sk_step", "sk_set_lr", "sk_step_host", "sk_step_host_sp
            "sk_get_stats", "sk_test_fail_allocation", "sk_debug_check", "sk_layer_norm", "sk_layer_norm_backward",
            "sk_layer_norm_backward_workspace", "sk_linear_cross_entropy", "sk_linear_cross_entropy_workspace",
            "sk_linear_cross_entropy_backward", "sk_linear_cross_entropy_backward_workspace", "sk_orthogonalize",
-           "sk_orthogonalize_workspace", "sk_operators_sync"]
+           "sk_orthogonalize_workspace", "sk_operators_sync", "sk_test_operators_wait"]
 NUM_STATS = 6
 STAT_NAMES = ["threshold", "threshold_bin_count", "tie_group_count", "emitted", "floats_on_the_wire", "status"]
 STATIC_MAX_D = 262144
@@ -84,6 +84,7 @@ def lib() -> C.CDLL:
         L.sk_orthogonalize.restype = ci
         L.sk_orthogonalize.argtypes = [vp, u64, u64, ci, vp, u64, u64, f32, ci, vp, u64, u64, ci, u64, u64, u64, ci, vp, f32, vp, u64, vp]
         L.sk_operators_sync.restype = ci; L.sk_operators_sync.argtypes = [vp]
+        L.sk_test_operators_wait.restype = ci; L.sk_test_operators_wait.argtypes = [C.c_uint32]
         L.sk_last_error.restype = C.c_char_p; L.sk_last_error.argtypes = []
         L.sk_version.restype = C.c_char_p; L.sk_version.argtypes = []
         _lib = L

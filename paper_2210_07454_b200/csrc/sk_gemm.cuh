@@ -12,8 +12,9 @@
 // with less shared memory for the ring: 67 against 63 us for the gradient of 8 x 50257 x 768).  Two
 // accumulators in tensor memory take turns, so the next tile's products run while this tile's epilogue does.
 //
-// Every wait has a limit.  A role whose wait runs out records kOpWait in the status word and leaves its loop; the others
-// follow when their own waits run out, so the kernel ends and the host reads an error instead of hanging.
+// Every wait has a limit (Waits).  A role whose wait runs out records kOpWait in the status word and leaves its loop: it waits for nothing
+// more but what it has set going itself (copies, matrix instructions), once and with the same limit.  The others follow when their
+// own waits, begun at most a tile later, run out.  So the kernel ends within about two limits, and the host reads an error instead of hanging.
 #pragma once
 #include <cuda.h>
 #include <cuda_bf16.h>
@@ -23,6 +24,7 @@
 #include <cstdint>
 
 #include "sk_chain.cuh"
+#include "sk_operators.h"
 
 namespace sk {
 
@@ -68,23 +70,37 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
 }
-// Tries until `ready` says so: some ten thousand at once, as ordinary waits need, then with pauses of about half a microsecond, some
-// sixteen seconds in all.  The longest wait there is, for a product of the largest matrices to be finished, is below one.
-constexpr uint32_t kQuickTries = 1u << 14, kSlowTries = 1u << 25;
+__device__ __forceinline__ uint64_t clock_ns() {
+    uint64_t t;
+    asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
+    return t;
+}
+// Tries until `ready` says so: some ten thousand at once, as ordinary waits need, then with pauses of about half a microsecond, until the
+// limit has passed on the GPU's clock.  A try may itself take long (mbarrier.try_wait suspends the thread for a time that the hardware
+// chooses), so tries alone do not bound a wait; they do so as the last resort, should the clock stand still.
+constexpr uint32_t kQuickTries = 256, kQuickRounds = 64, kSlowTries = 1u << 28;
 template <class Ready>
-__device__ __forceinline__ bool wait_until(Ready ready, uint32_t* status) {
-    for (uint32_t i = 0; i < kQuickTries; ++i)
-        if (ready()) return true;
-    for (uint32_t i = 0; i < kSlowTries; ++i) {
+__device__ __forceinline__ bool wait_until(Ready ready, const Waits& w) {
+    uint64_t end = 0;
+    for (uint32_t r = 0; r < kQuickRounds; ++r) {
+        for (uint32_t i = 0; i < kQuickTries; ++i)
+            if (ready()) return true;
+        const uint64_t now = clock_ns();
+        if (r == 0) end = now + w.limit_ms * 1000000ull;
+        else if (now > end) break;
+    }
+    for (uint32_t i = 0; i < kSlowTries && clock_ns() <= end; ++i) {
         if (ready()) return true;
         __nanosleep(500);
     }
-    atomicOr(status, kOpWait);
+    atomicOr(w.status, kOpWait);
     return false;
 }
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, uint32_t* status) {
-    return wait_until([&] { return mbar_try(bar, parity); }, status);
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Waits& w) {
+    return wait_until([&] { return mbar_try(bar, parity); }, w);
 }
+// the same for a warp that stays together
+__device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const Waits& w) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, w)); }
 __device__ __forceinline__ uint32_t map_to_leader(uint32_t addr) {      // the same address in block 0 of the cluster
     uint32_t r;
     asm volatile("mapa.shared::cluster.u32 %0, %1, 0;" : "=r"(r) : "r"(addr));
@@ -184,7 +200,7 @@ struct GemmPlan {
     CUtensorMap map[4];                       // A and B of the first, of the second
     GemmGroup g[2];
     uint32_t groups, early;
-    uint32_t* status;
+    Waits waits;
     static constexpr bool kCooperative = false, kEmpty = false;
 
     __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, TileJob& j) const {
@@ -244,7 +260,7 @@ struct GemmTile {
 // Plan: job(unit, units, i, job): the unit's i-th tile; wait(job): until its operands are there; done(job): called by every epilogue warp
 // when its share of the tile is written.
 // Epi: struct Args; __device__ Epi(const Args&, job, row, part, shared address of the warp's memory); begin(plan, first column) before the
-// accumulator is waited for; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
+// accumulator is waited for, false (in the whole warp) if a wait of its own ran out; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
 // row of the tile and gets its columns 32 at a time; the kWarps / 4 warps that share a row take a part of the columns each.  Rows >= M
 // are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
 template <int CG, int BN, class Plan, class Epi>
@@ -314,7 +330,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                         mb = t.map_b2;
                         k0 = t.k_first;
                     }
-                    if (!(ok = mbar_wait(empty(s), parity, plan.status))) break;
+                    if (!(ok = mbar_wait(empty(s), parity, plan.waits))) break;
                     const uint32_t sa = stages + s * kBytes, sb = sa + kBytesA;
                     uint32_t bar = full(s);
                     if (rank == 0) mbar_expect(bar, bytes);
@@ -334,28 +350,29 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                     if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
                 }
             }
-            // this block's own copies land in its shared memory: all of them are waited for before the block may end
+            // this block's own copies land in its shared memory: all of them are waited for before the block may end (where the products
+            // have been given up, for the limit, in which they land)
             if (any)
                 for (uint32_t q = 0; q < (uint32_t)kStages; ++q) {
-                    if (!mbar_wait(empty(s), parity, plan.status)) break;
+                    if (!mbar_wait(empty(s), parity, plan.waits)) break;
                     if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
                 }
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            uint32_t s = 0, parity = 0;
+            uint32_t s = 0, parity = 0, n = 0;
             bool ok = true;
-            for (uint32_t n = 0; ok && plan.job(unit, units, n, t); ++n) {
+            for (; ok && plan.job(unit, units, n, t); ++n) {
                 const uint32_t kb = t.k_stages, a = n & 1, steps = t.k_rows / 16, d = tmem + a * BN;
                 // D fp32; A, B bf16 or fp16; majors; N / 8; M / 16
                 const uint32_t idesc = (1u << 4) | (t.bf16 << 7) | (t.bf16 << 10) | (t.a_mn << 15) | (t.b_mn << 16) |
                                        ((uint32_t)(BN / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
                 const uint64_t step_a = (t.a_mn ? 2048u : 32u) >> 4, step_b = (t.b_mn ? 2048u : 32u) >> 4;
                 const uint64_t desc_a = smem_desc(stages, t.a_mn), desc_b = smem_desc(stages + kBytesA, t.b_mn);
-                if (n >= 2 && !(ok = mbar_wait(acc_empty(a), ((n >> 1) - 1) & 1, plan.status))) break;
+                if (n >= 2 && !(ok = mbar_wait(acc_empty(a), ((n >> 1) - 1) & 1, plan.waits))) break;
                 asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                 for (uint32_t k = 0; k < kb; ++k) {
-                    if (!(ok = mbar_wait(full(s), parity, plan.status))) break;
+                    if (!(ok = mbar_wait(full(s), parity, plan.waits))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     const uint64_t da = desc_a + s * (kBytes >> 4), db = desc_b + s * (kBytes >> 4);
                     if (steps == kGemmK / 16) {
@@ -369,6 +386,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                 }
                 mma_commit<CG>(acc_full(a));
             }
+            if (!ok && n) mbar_wait(acc_full((n - 1) & 1), ((n - 1) >> 1) & 1, plan.waits);      // the products begun, which no epilogue waits for
         }
     } else {
         const uint32_t w = warp - 2, quarter = warp & 3, part = w >> 2;
@@ -379,8 +397,8 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
             const uint32_t row = t.m * (128 * CG) + rank * 128 + quarter * 32 + lane;
             const uint32_t col0 = t.n * BN + part * kCols;
             Epi epi(ea, t, row, part, stage);
-            epi.begin(plan, col0);                               // what it reads travels while the products run
-            if (!mbar_wait(acc_full(a), (n >> 1) & 1, plan.status)) break;
+            if (!epi.begin(plan, col0)) break;                   // what it reads travels while the products run
+            if (!mbar_wait_warp(acc_full(a), (n >> 1) & 1, plan.waits)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (Plan::kEmpty && !t.k_stages) {                   // no products
                 __syncwarp();
@@ -498,12 +516,12 @@ constexpr uint32_t kTileCost = 6;
 // One product, or two in one launch with the longer tiles first; slices: K of the first is split into so many.
 template <int CG, int BN, class Epi>
 cudaError_t launch_products(bool chain, const Operand& a, const Operand& b, GemmGroup g0, uint32_t slices, const Operand* a2, const Operand* b2,
-                            const GemmGroup* g1, uint32_t* status, const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
+                            const GemmGroup* g1, const Waits& waits, const typename Epi::Args& ea, int sm_count, cudaStream_t st) {
     GemmPlan p{};
     set_tiles<CG, BN>(g0, a, b, slices);
     p.g[0] = g0;
     p.groups = 1;
-    p.status = status;
+    p.waits = waits;
     uint32_t tiles = g0.tiles;
     auto encode = [&](CUtensorMap* map, const GemmGroup& g, const Operand& x, const Operand& y) {
         return encode_operand(map, x, g.bf16, x.mn ? g.k_rows : g.a_rows) && encode_operand(map + 1, y, g.bf16, y.mn ? g.k_rows : BN / CG);

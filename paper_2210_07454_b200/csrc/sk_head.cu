@@ -27,7 +27,7 @@ __device__ __forceinline__ float exp2_fast(float x) {          // 2^x, 2 ulp
 // per (half tile, row): maximum of the logits and the sum of exp(z - maximum)
 struct StatsEpi {
     static constexpr int kWarps = 8, kWords = kStageWords;
-    template <class Plan> __device__ void begin(const Plan&, uint32_t) {}
+    template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
     struct Args { float2* part; float* at_target; const int64_t* targets; };
     const Args& a;
     const TileJob& t;
@@ -120,7 +120,7 @@ __global__ void __launch_bounds__(kJoinThreads) k_head_join(const float2* part, 
 // G's piece
 struct GradEpi {
     static constexpr int kWarps = 8, kWords = kStageWords;
-    template <class Plan> __device__ void begin(const Plan&, uint32_t) {}
+    template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
     struct Args { uint16_t* out; uint64_t ld; const float *lse, *dloss, *factor; const int64_t* targets; uint64_t vocab; uint32_t first; };
     const Args& a;
     const TileJob& t;
@@ -175,7 +175,7 @@ struct GradEpi {
 // bits, a slice of K in a matrix of its own (`sum`, one after the other), and joined by k_head_sum.
 struct OutEpi {
     static constexpr int kWarps = 8, kWords = kStageWords;
-    template <class Plan> __device__ void begin(const Plan&, uint32_t) {}
+    template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
     struct One { void* out; float* sum; uint64_t ld, sum_stride; int type; uint32_t align, add; };
     struct Args { One o[2]; const float* factor; };
     const One& a;
@@ -412,7 +412,7 @@ int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
     const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{w, a.vocab, a.width, ld_w, 0, 1, false};
     const bool wide = wide_tiles(g.M, g.N, (a.width + kGemmK - 1) / kGemmK, dev.sm_count);
     auto launch = wide ? launch_products<2, 256, StatsEpi> : launch_products<1, 128, StatsEpi>;
-    SK_OP_CUDA(launch(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.status, ea, dev.sm_count, st));
+    SK_OP_CUDA(launch(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ea, dev.sm_count, st));
     const uint32_t tile = wide ? 256 : 128, slots = 2 * ((g.N + tile - 1) / tile);
     SK_OP_CUDA(launch_kernel(true, k_head_join, dim3((g.M + 7) / 8), kJoinThreads, 0, st, (const float2*)ea.part, (const float*)ea.at_target, a.targets, g.M,
                              a.vocab, slots, a.loss, a.lse));
@@ -440,7 +440,7 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
         g.N = n;
         const GradEpi::Args ga{gbuf, l.ld_g, a.lse, a.dloss, factor, a.targets, a.vocab, (uint32_t)v0};
         auto launch_g = wide_tiles(tokens, n, (a.width + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_products<2, 256, GradEpi> : launch_products<1, 128, GradEpi>;
-        SK_OP_CUDA(launch_g(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.status, ga, dev.sm_count, st));
+        SK_OP_CUDA(launch_g(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ga, dev.sm_count, st));
         // dW[v] = sum over tokens of G[t][v] hidden[t]: both factors with their rows contiguous;
         // dhidden[t] += sum over the piece of G[t][v] W[v]
         const Operand gt{gbuf, a.tokens, n, l.ld_g, 0, 1, true}, ht{h, a.tokens, a.width, ld_h, 0, 1, true};
@@ -468,7 +468,7 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
         const bool both = a.dweight && a.dhidden, h_is_0 = both ? h_first : a.dhidden != nullptr;
         if (!both) ea.o[0] = h_is_0 ? one_h : one_w;
         SK_OP_CUDA(launch(true, h_is_0 ? og : gt, h_is_0 ? wt : ht, h_is_0 ? gh : gw, h_is_0 ? split : 1, h_is_0 ? &gt : &og, h_is_0 ? &ht : &wt,
-                          both ? (h_is_0 ? &gw : &gh) : nullptr, dev.status, ea, dev.sm_count, st));
+                          both ? (h_is_0 ? &gw : &gh) : nullptr, dev.waits(), ea, dev.sm_count, st));
     }
     if (sum) {
         const uint64_t want = (a.tokens * ((width + 3) / 4) + 255) / 256, most = (uint64_t)dev.sm_count * 8;

@@ -11,6 +11,7 @@ namespace {
 __device__ uint32_t g_op_status;                 // see kOpWait
 
 thread_local OpDevice t_devices[64];
+thread_local uint32_t t_withhold_ms;             // of this thread's next call, see sk_test_operators_wait
 
 using EncodeFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                               const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
@@ -233,7 +234,15 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
     if (int rc = check_workspace(who, workspace, workspace_bytes, orthogonalize_workspace(a))) return rc;
     OpDevice dev;
     if (int rc = op_device(&dev)) return rc;
-    return launch_orthogonalize(a, dev, (cudaStream_t)stream);
+    const uint32_t withhold_ms = t_withhold_ms;
+    t_withhold_ms = 0;
+    return launch_orthogonalize(a, dev, withhold_ms, (cudaStream_t)stream);
+}
+
+int sk_test_operators_wait(uint32_t limit_ms) {
+    if (limit_ms < 1 || limit_ms > 1000) return set_error(SK_EINVAL, "sk_test_operators_wait: limit_ms must be in 1..1000");
+    t_withhold_ms = limit_ms;
+    return SK_OK;
 }
 
 int sk_operators_sync(void* stream) {

@@ -19,10 +19,18 @@ int set_error(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3
             return sk::set_error(SK_ECUDA, "%s:%d: %s", __func__, __LINE__, cudaGetErrorString(err__));        \
     } while (0)
 
+// Where a wait inside a kernel that runs out is recorded, and after how long it does.  Thirty seconds: a tile over K = 2^31, the longest
+// wait that any call can mean, takes up to eighteen; of the largest matrices in practice, below one.
+constexpr uint32_t kWaitLimitMs = 30000;
+struct Waits {
+    uint32_t* status;
+    uint32_t limit_ms;
+};
 // What the operators know about the current device; resolved once per device.
 struct OpDevice {
     int sm_count = 0;
     uint32_t* status = nullptr;      // the operators' status word (a static of the library)
+    Waits waits() const { return {status, kWaitLimitMs}; }
 };
 int op_device(OpDevice* out);        // SK_OK or an error with its message
 
@@ -235,7 +243,8 @@ struct OrthoArgs {
     float coefficient[3];
     void* workspace;
 };
-int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t st);
+// withhold_ms: not zero in tests, see sk_test_operators_wait
+int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, uint32_t withhold_ms, cudaStream_t st);
 uint64_t orthogonalize_workspace(const OrthoArgs& a);
 
 }  // namespace sk

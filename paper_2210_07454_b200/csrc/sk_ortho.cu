@@ -50,7 +50,7 @@ struct ChainShape {
     uint32_t slices, k_slice;                    // of the longer side in A, stages of one
     uint32_t signals;                            // of every tile: its epilogue warps
     uint32_t* count;                             // per matrix, zero before the launch
-    uint32_t* status;
+    Waits waits;
 
     // X is the sum of two matrices in all but the last two steps, and in the first where one is exact
     __host__ __device__ bool pair(uint32_t step) const { return step + 2 < steps && !(step == 0 && exact); }
@@ -128,7 +128,7 @@ struct ChainPlan : ChainShape {
             uint32_t have;
             asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(have) : "l"(count + j.b) : "memory");
             return have >= need;
-        }, status);
+        }, waits);
         asm volatile("fence.proxy.async;" ::: "memory");             // what was written by stores is read by TMA
         return ok;
     }
@@ -242,14 +242,15 @@ struct ChainEpi {
         }
     }
     template <class Plan>
-    __device__ void begin(const Plan& plan, uint32_t col0) {
+    __device__ bool begin(const Plan& plan, uint32_t col0) {
         if (SLICED && t.kind == kJoin) {
-            plan.wait(t);                        // no products wait for the warps that have nothing to add up
+            if (!__all_sync(0xffffffffu, plan.wait(t))) return false;            // no products wait for the warps that have nothing to add up
             join(col0);
         }
-        if (t.kind != kPoly || !rows) return;
-        plan.wait(t);
+        if (t.kind != kPoly || !rows) return true;
+        if (!__all_sync(0xffffffffu, plan.wait(t))) return false;
         fetch(col0);
+        return true;
     }
     __device__ void square(__half* out, uint32_t col, float (&v)[32], bool last) {
         store_tile32(out, SK_F16, e.ld_a, row0, rows, col, e.ld_a, v, 16, stage, true, last);
@@ -543,7 +544,7 @@ struct SmallArgs {
     OrthoArgs a;
     uint32_t m, n, tall, blocks;                 // blocks of the cluster
     uint32_t align, vec_u, vec_m;
-    uint32_t* status;
+    Waits waits;
 };
 
 // where 16-byte chunk `chunk` of row r of a 64-column block lies
@@ -571,7 +572,7 @@ __device__ __forceinline__ void put32(uint8_t* base, uint32_t r, uint32_t col, c
 __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_constant__ SmallArgs s) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_mem;
-    __shared__ uint32_t tmem_slot;
+    __shared__ uint32_t tmem_slot, gave_up;
     __shared__ double sums[kSmallThreads / 32], shares[kSmallCluster];
     const OrthoArgs& a = s.a;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, S = s.blocks;
@@ -582,6 +583,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
     if (tid == 0) {
         mbar_init(bar, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        gave_up = 0;
     }
     if (warp == 0) tmem_alloc<1>(smem_u32(&tmem_slot), 512);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -704,16 +706,19 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
     const uint32_t idesc = (1u << 4) | (8u << 24), idesc_m = idesc | (m16 / 8 << 17), idesc_x = idesc | (1u << 16) | (w16 / 8 << 17);
     const uint32_t quarter = warp & 3, part = warp >> 2, row = quarter * 32 + lane, lanes = (quarter * 32) << 16;     // part: of the columns
     uint32_t phase = 0;
-    // the products of one phase issued by one thread, waited for by all
+    // The products of one phase issued by one thread, waited for by all.  Once a wait has run out, nothing more is issued or waited for in this
+    // block; it still takes part in the cluster's barriers.
     auto run = [&](auto issue) {
         fence_async();
         __syncthreads();
-        if (tid == 0) {
-            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-            issue();
-            mma_commit<1>(bar);
+        if (!*(volatile uint32_t*)&gave_up) {
+            if (tid == 0) {
+                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                issue();
+                mma_commit<1>(bar);
+            }
+            if (!mbar_wait(bar, phase, s.waits)) *(volatile uint32_t*)&gave_up = 1;
         }
-        mbar_wait(bar, phase, s.status);
         phase ^= 1;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         __syncwarp();
@@ -866,7 +871,7 @@ cudaError_t launch_small(const OrthoArgs& a, uint32_t align, const OpDevice& dev
     };
     s.vec_u = vec8(a.update, a.ld_update, a.stride_update, type_size(a.type));
     s.vec_m = a.momentum && vec8(a.momentum, a.ld_momentum, a.stride_momentum, 4);
-    s.status = dev.status;
+    s.waits = dev.waits();
     constexpr int kSmem = (int)kSmallBytes + 1024;
     cudaError_t e = cudaFuncSetAttribute(k_ortho_small, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
     if (e == cudaSuccess && s.blocks > 8) e = cudaFuncSetAttribute(k_ortho_small, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
@@ -897,7 +902,7 @@ cudaError_t launch_chain(bool wide, const ChainShape& p, const ChainArgs& ea, ui
 
 uint64_t orthogonalize_workspace(const OrthoArgs& a) { return is_small(a) ? 0 : layout_of(a).total; }
 
-int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t st) {
+int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, uint32_t withhold_ms, cudaStream_t st) {
     const uint32_t align_rows = row_alignment(a.out, a.ld_out, a.out_type), align_batch = row_alignment(a.out, a.stride_out, a.out_type);
     const uint32_t align = a.batch > 1 && align_batch < align_rows ? align_batch : align_rows;
     if (is_small(a)) {
@@ -974,7 +979,7 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     p.k_poly = (m + kGemmK - 1) / kGemmK;
     p.k_gram = (uint32_t)(((tall ? a.rows : a.cols) + kGemmK - 1) / kGemmK);
     p.count = sq.count;
-    p.status = dev.status;
+    p.waits = dev.waits();
     const ChainTiles c = chain_tiles(a);
     const uint32_t tile = c.wide ? 256 : 128, slots = (uint32_t)dev.sm_count / (c.wide ? 2 : 1);
     p.side = (m + tile - 1) / tile;
@@ -993,6 +998,10 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, cudaStream_t s
     p.signals = (c.wide ? 2 : 1) * ChainEpi<true>::kWarps;
     if ((uint64_t)a.steps * batch * ((c.slices > 1 ? 1ull + c.slices + kJoinParts : 2ull) * p.square + p.apply) * p.signals >= (1ull << 32))
         return set_error(SK_EINVAL, "sk_orthogonalize: batch * rows * cols is too large for one call");
+    if (withhold_ms) {                           // every wait asks for more than the tiles' warps ever count
+        ++p.signals;
+        p.waits.limit_ms = withhold_ms;
+    }
     const uint32_t most_tiles = batch * (p.square * p.slices > p.apply ? p.square * p.slices : p.apply), units = most_tiles < slots ? most_tiles : slots;
     SK_OP_CUDA(c.slices > 1 ? launch_chain<true>(c.wide, p, ea, units, st) : launch_chain<false>(c.wide, p, ea, units, st));
     return SK_OK;
