@@ -332,8 +332,8 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
                      uint64_t stride_out, int out_type, uint64_t batch, uint64_t rows, uint64_t cols, int steps,
                      const float* coefficients, float eps, void* workspace, uint64_t workspace_bytes, void* stream);
 
-/* Waits for the stream and reports the operators' device status word of the current device (SK_EDEVICE with a message if
- * it is not zero, after which it is cleared): bit 0, a product kernel gave up a wait and its outputs are invalid. */
+/* Waits for the stream and reports waits inside operators' kernels that have run out on the current device, in any stream, since the
+ * last report (SK_EDEVICE with a message: such a kernel's outputs are invalid).  Each is reported once. */
 int sk_operators_sync(void* stream);
 
 /* Test hook: the products of the calling thread's next sk_orthogonalize, if they are the tiles of one cooperative launch, wait for more

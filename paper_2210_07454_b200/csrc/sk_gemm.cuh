@@ -12,7 +12,7 @@
 // with less shared memory for the ring: 67 against 63 us for the gradient of 8 x 50257 x 768).  Two
 // accumulators in tensor memory take turns, so the next tile's products run while this tile's epilogue does.
 //
-// Every wait has a limit (Waits).  A role whose wait runs out records kOpWait in the status word and leaves its loop: it waits for nothing
+// Every wait has a limit (Waits).  A role whose wait runs out counts it and leaves its loop: it waits for nothing
 // more but what it has set going itself (copies, matrix instructions), once and with the same limit.  The others follow when their
 // own waits, begun at most a tile later, run out.  So the kernel ends within about two limits, and the host reads an error instead of hanging.
 #pragma once
@@ -27,8 +27,6 @@
 #include "sk_operators.h"
 
 namespace sk {
-
-constexpr uint32_t kOpWait = 1u;              // status word of the operators: a wait inside a product kernel ran out
 
 constexpr int kGemmK = 64;                    // values of k per stage: 128 bytes, the width of the swizzle
 constexpr int kStageWords = 1024;             // of shared memory that store_tile32 needs, for each epilogue warp
@@ -93,7 +91,7 @@ __device__ __forceinline__ bool wait_until(Ready ready, const Waits& w) {
         if (ready()) return true;
         __nanosleep(500);
     }
-    atomicOr(w.status, kOpWait);
+    atomicAdd(w.status, 1u);
     return false;
 }
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Waits& w) {

@@ -8,7 +8,10 @@
 namespace sk {
 namespace {
 
-__device__ uint32_t g_op_status;                 // see kOpWait
+// How many waits inside kernels have run out on the device, ever, and how many of them have been reported.  Nothing is set back on the
+// device, so a wait that runs out while another is being reported is not lost.
+__device__ uint32_t g_op_status;
+std::atomic<uint32_t> g_reported[64];
 
 thread_local OpDevice t_devices[64];
 thread_local uint32_t t_withhold_ms;             // of this thread's next call, see sk_test_operators_wait
@@ -248,13 +251,16 @@ int sk_test_operators_wait(uint32_t limit_ms) {
 int sk_operators_sync(void* stream) {
     OpDevice dev;
     if (int rc = op_device(&dev)) return rc;
-    uint32_t word = 0;
-    SK_OP_CUDA(cudaMemcpyAsync(&word, dev.status, 4, cudaMemcpyDeviceToHost, (cudaStream_t)stream));
+    int d = 0;
+    SK_OP_CUDA(cudaGetDevice(&d));
+    uint32_t count = 0;
+    SK_OP_CUDA(cudaMemcpyAsync(&count, dev.status, 4, cudaMemcpyDeviceToHost, (cudaStream_t)stream));
     SK_OP_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
-    if (!word) return SK_OK;
-    SK_OP_CUDA(cudaMemsetAsync(dev.status, 0, 4, (cudaStream_t)stream));
-    SK_OP_CUDA(cudaStreamSynchronize((cudaStream_t)stream));
-    return set_error(SK_EDEVICE, "operators' status word %u: a product kernel gave up a wait, its outputs are invalid", word);
+    uint32_t reported = g_reported[d].load();
+    do {
+        if ((int32_t)(count - reported) <= 0) return SK_OK;          // reported, or overtaken by a thread that read later
+    } while (!g_reported[d].compare_exchange_weak(reported, count));
+    return set_error(SK_EDEVICE, "%u waits inside operators' kernels ran out: their outputs are invalid", count - reported);
 }
 
 }  // extern "C"

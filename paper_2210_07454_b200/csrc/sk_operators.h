@@ -19,7 +19,7 @@ int set_error(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3
             return sk::set_error(SK_ECUDA, "%s:%d: %s", __func__, __LINE__, cudaGetErrorString(err__));        \
     } while (0)
 
-// Where a wait inside a kernel that runs out is recorded, and after how long it does.  Thirty seconds: a tile over K = 2^31, the longest
+// Where a wait inside a kernel that runs out is counted, and after how long it does.  Thirty seconds: a tile over K = 2^31, the longest
 // wait that any call can mean, takes up to eighteen; of the largest matrices in practice, below one.
 constexpr uint32_t kWaitLimitMs = 30000;
 struct Waits {
@@ -29,7 +29,7 @@ struct Waits {
 // What the operators know about the current device; resolved once per device.
 struct OpDevice {
     int sm_count = 0;
-    uint32_t* status = nullptr;      // the operators' status word (a static of the library)
+    uint32_t* status = nullptr;      // count of waits that ran out (a static of the library)
     Waits waits() const { return {status, kWaitLimitMs}; }
 };
 int op_device(OpDevice* out);        // SK_OK or an error with its message

@@ -34,3 +34,26 @@ def test_the_limit_is_checked():
     from paper_2210_07454_b200 import binding
     for bad in (0, 1001):
         assert binding.lib().sk_test_operators_wait(bad) == -1
+
+
+def test_every_wait_is_reported_once_whatever_the_stream():
+    """Waits that run out in one stream while another's are being reported: none is lost, none reported twice."""
+    from paper_2210_07454_b200 import binding, operators as ops
+    u = torch.randn(1, 300, 300, generator=torch.Generator(device="cuda").manual_seed(1), device="cuda")
+    ops.orthogonalize(u)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for sync_on in (None, side):
+        for _ in range(2):
+            binding._check(binding.lib().sk_test_operators_wait(20))
+            ops.orthogonalize(u, stream=side)
+        side.synchronize()
+        with pytest.raises(binding.SkError, match="ran out"):
+            ops.sync(sync_on)                        # the whole device's, from any stream
+        ops.sync()
+        ops.sync(side)
+        binding._check(binding.lib().sk_test_operators_wait(20))
+        ops.orthogonalize(u)                         # after a report another
+        with pytest.raises(binding.SkError, match="ran out"):
+            ops.sync()
+        ops.sync(side)
