@@ -121,6 +121,14 @@ def _run(device, fn, *args):
             _check(fn(*args))
 
 
+def _size(device, fn, *args):
+    """A workspace's size, which may depend on the device."""
+    if _current_device() == device:
+        return fn(*args)
+    with torch.cuda.device(device):
+        return fn(*args)
+
+
 def _new(shape, stride, dtype, device):
     """Uninitialised memory on the device of that index."""
     if _current_device() == device:
@@ -231,7 +239,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=
         pdb = _vector(dbias, "dbias", cols, _TYPES, device)
         if dbias.dtype != dtype:
             raise SkError(f"dbias has type {dbias.dtype}, dweight {dtype}")
-    need = lib().sk_layer_norm_backward_workspace(rows, cols) if rows and (pdw or pdb) else 0
+    need = _size(device, lib().sk_layer_norm_backward_workspace, rows, cols) if rows and (pdw or pdb) else 0
     ws = _workspace(need, device)
     _run(device, lib().sk_layer_norm_backward, dy.data_ptr(), ld_dy, x.data_ptr(), ld, pdx, ld_dx, code, rows, cols, pw, wcode, pm, pr, pdw, pdb,
          _TYPES[dtype], _p(ws), need, _raw_stream(device))
@@ -261,7 +269,7 @@ def linear_cross_entropy(hidden, weight, targets, stream=None):
     device, code, tokens, vocab, width, ld_h, ld_w, pt = _head(hidden, weight, targets)
     loss, lse = _new((tokens,), (1,), torch.float32, device), _new((tokens,), (1,), torch.float32, device)
     ph, pw = hidden.data_ptr(), weight.data_ptr()
-    need = lib().sk_linear_cross_entropy_workspace(ph, ld_h, pw, ld_w, tokens, vocab, width)
+    need = _size(device, lib().sk_linear_cross_entropy_workspace, ph, ld_h, pw, ld_w, tokens, vocab, width)
     ws = _workspace(need, device)
     _run(device, lib().sk_linear_cross_entropy, ph, ld_h, pw, ld_w, code, tokens, vocab, width, pt, loss.data_ptr(), lse.data_ptr(), _p(ws), need,
          _raw_stream(device))
@@ -289,7 +297,7 @@ def linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden=N
             outs.append((t, ld, tcode))
     (dh, ld_dh, type_dh), (dw, ld_dw, type_dw) = outs
     ph, pw = hidden.data_ptr(), weight.data_ptr()
-    need = lib().sk_linear_cross_entropy_backward_workspace(ph, ld_h, pw, ld_w, tokens, vocab, width)
+    need = _size(device, lib().sk_linear_cross_entropy_backward_workspace, ph, ld_h, pw, ld_w, tokens, vocab, width)
     ws = _workspace(need, device)
     _run(device, lib().sk_linear_cross_entropy_backward, pd, ph, ld_h, pw, ld_w, code, tokens, vocab, width, pt, pl, _p(dh), ld_dh, type_dh, _p(dw),
          ld_dw, type_dw, _p(ws), need, _raw_stream(device))
@@ -325,7 +333,7 @@ def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coef
         out = _new_like(update, torch.float16 if update.dtype == torch.float16 else torch.bfloat16, device)
     po, ld_o, s_o, out_code = _batch_of(out, "out", update, _HALF, device)
     batch, (rows, cols) = (update.shape[0] if update.dim() == 3 else 1), update.shape[-2:]
-    need = lib().sk_orthogonalize_workspace(batch, rows, cols)
+    need = _size(device, lib().sk_orthogonalize_workspace, batch, rows, cols)
     ws = _workspace(need, device)
     _run(device, lib().sk_orthogonalize, pu, ld_u, s_u, code, pm, ld_m, s_m, beta, int(nesterov), po, ld_o, s_o, out_code, batch, rows, cols, steps,
          (C.c_float * 3)(*coefficients), eps, _p(ws), need, _raw_stream(device))

@@ -134,6 +134,16 @@ def test_tensors_given_to_a_stream_are_kept_for_it(world):
             assert world.side in t.recorded, name
 
 
+def test_sizes_are_asked_with_the_tensors_device_current(world):
+    """The layer norm's workspace depends on the device's number of SMs."""
+    for _, _, _, call in world.calls(device=1):
+        call(None)
+    assert {"sk_layer_norm_backward_workspace", "sk_linear_cross_entropy_workspace", "sk_linear_cross_entropy_backward_workspace",
+            "sk_orthogonalize_workspace"} == {name for name, _ in world.asked}
+    assert all(device == 1 for _, device in world.asked), world.asked
+    assert all(device == 1 for _, device, _ in world.called) and world.device == 0
+
+
 @pytest.mark.gpu
 def test_operators_on_a_stream_take_temporaries():
     """Inputs and outputs that are dropped, and whose memory is written again, while the given stream is still busy."""
