@@ -146,7 +146,7 @@ __device__ __forceinline__ void store_tile32(void* out, int type, uint64_t ld, u
     }
     __syncwarp();
     const uint32_t size = wide ? 4 : 2, first = col - 32 * second;
-    const uint32_t bytes = min(wide ? 128u : 64u * (second + 1), (limit - first) * size);            // of every row
+    const uint32_t bytes = min(limit - first, 32 * (second + 1)) * size;         // of every row (a whole one may have more than 32 bits can say)
     uint8_t* o = (uint8_t*)out + (row0 * ld + first) * size;
     const uint64_t step = ld * size;
     if (align >= 16 && bytes % 16 == 0) {        // eight lanes a row, all eight loads before the stores
