@@ -24,9 +24,18 @@ _INT64 = {torch.int64: 0}
 
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)         # Newton-Schulz step X <- a X + (b A + c A^2) X, A = X X^T
 
-_raw_stream = torch._C._cuda_getCurrentRawStream
-_current_device = torch._C._cuda_getDevice
-_empty_here = torch._C._dynamo.guards._empty_strided_cuda        # 0.7 us of the host's time; torch.empty_like 1.3, new_empty 1.8
+
+def _shortcut(owner, name, public):
+    """torch's inner function if this torch has it (a microsecond of the host's time each), else what its public interface offers."""
+    for part in name.split("."):
+        owner = getattr(owner, part, None)
+    return owner or public
+
+
+_raw_stream = _shortcut(torch._C, "_cuda_getCurrentRawStream", lambda device: torch.cuda.current_stream(device).cuda_stream)
+_current_device = _shortcut(torch._C, "_cuda_getDevice", lambda: torch.cuda.current_device())
+_empty_here = _shortcut(torch._C, "_dynamo.guards._empty_strided_cuda",                     # 0.7 us; torch.empty_like 1.3, new_empty 1.8
+                        lambda shape, stride, dtype: torch.empty_strided(shape, stride, dtype=dtype, device="cuda"))
 
 
 # ---- checks ---------------------------------------------------------------------------------------------------------------
