@@ -156,6 +156,13 @@ def _workspace(nbytes, device):
     return _new((nbytes,), (1,), torch.uint8, device) if nbytes else None
 
 
+def _wrote(*given):
+    """Tensors of the caller's that a call writes: autograd's check for tensors changed in place learns of it."""
+    for t in given:
+        if isinstance(t, torch.Tensor):
+            torch.autograd.graph.increment_version(t)
+
+
 def _p(t):
     return t.data_ptr() if t is not None else None
 
@@ -202,6 +209,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
         rstd = torch.empty_like(mean)
     _run(device, lib().sk_layer_norm, x.data_ptr(), ld, y.data_ptr(), ld_y, code, rows, cols, pw, pb, wcode, eps, mean.data_ptr(), rstd.data_ptr(),
          _raw_stream(device))
+    _wrote(out)
     return y, mean, rstd
 
 
@@ -210,6 +218,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=
     weight's type (fp32 without a weight).  ``dx``, ``dweight``, ``dbias``: tensors to write into, False to leave one out."""
     if stream is not None:
         return _on(stream, lambda: layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias), dy, x, weight, mean, rstd, dx, dweight, dbias)
+    given_outputs = dx, dweight, dbias
     code = _tensor(x, "x", _TYPES)
     device, cols = x.get_device(), x.shape[-1] if x.dim() else 0
     if _tensor(dy, "dy", _TYPES, device) != code:
@@ -252,6 +261,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=
     ws = _workspace(need, device)
     _run(device, lib().sk_layer_norm_backward, dy.data_ptr(), ld_dy, x.data_ptr(), ld, pdx, ld_dx, code, rows, cols, pw, wcode, pm, pr, pdw, pdb,
          _TYPES[dtype], _p(ws), need, _raw_stream(device))
+    _wrote(*given_outputs)
     return dx, dweight, dbias
 
 
@@ -310,6 +320,7 @@ def linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden=N
     ws = _workspace(need, device)
     _run(device, lib().sk_linear_cross_entropy_backward, pd, ph, ld_h, pw, ld_w, code, tokens, vocab, width, pt, pl, _p(dh), ld_dh, type_dh, _p(dw),
          ld_dw, type_dw, _p(ws), need, _raw_stream(device))
+    _wrote(dhidden, dweight)
     return dh, dw
 
 
@@ -338,6 +349,7 @@ def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coef
     pm, ld_m, s_m, _ = _batch_of(momentum, "momentum", update, _F32, device)
     if len(coefficients) != 3:
         raise SkError("coefficients are three numbers (a, b, c)")
+    given_out = out
     if out is None:
         out = _new_like(update, torch.float16 if update.dtype == torch.float16 else torch.bfloat16, device)
     po, ld_o, s_o, out_code = _batch_of(out, "out", update, _HALF, device)
@@ -346,6 +358,7 @@ def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coef
     ws = _workspace(need, device)
     _run(device, lib().sk_orthogonalize, pu, ld_u, s_u, code, pm, ld_m, s_m, beta, int(nesterov), po, ld_o, s_o, out_code, batch, rows, cols, steps,
          (C.c_float * 3)(*coefficients), eps, _p(ws), need, _raw_stream(device))
+    _wrote(momentum, given_out)
     return out
 
 

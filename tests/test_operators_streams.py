@@ -134,6 +134,25 @@ def test_tensors_given_to_a_stream_are_kept_for_it(world):
             assert world.side in t.recorded, name
 
 
+def test_tensors_written_in_place_say_so(world):
+    """What a call writes into given tensors raises their version, as torch's own functions do: autograd's check for tensors that were
+    changed after they were saved sees it."""
+    o, p = world.ops, lambda *shape, dtype=torch.float32: world.place(torch.zeros(*shape, dtype=dtype))
+    half = torch.bfloat16
+    x, w, s, h, t = p(4, 8), p(8), p(4), p(4, 8, dtype=half), p(4, dtype=torch.int64)
+    y, dx, dw, db, dh, dv, u, m = p(4, 8), p(4, 8), p(8), p(8), p(4, 8, dtype=half), p(4, 8), p(4, 8, dtype=half), p(4, 8)
+    calls = [((y,), lambda **k: o.layer_norm(x, w, out=y, **k)),
+             ((dx, dw, db), lambda **k: o.layer_norm_backward(x, x, w, s, s, dx=dx, dweight=dw, dbias=db, **k)),
+             ((dh, dv), lambda **k: o.linear_cross_entropy_backward(s, h, h, t, s, dhidden=dh, dweight=dv, **k)),
+             ((u, m), lambda **k: o.orthogonalize(x, momentum=m, out=u, **k))]
+    inputs = (x, w, s, h, t)
+    for written, call in calls:
+        for kw in ({}, dict(stream=world.side)):
+            before, kept = [v._version for v in written], [v._version for v in inputs]
+            call(**kw)
+            assert all(v._version > b for v, b in zip(written, before)) and [v._version for v in inputs] == kept
+
+
 def test_sizes_are_asked_with_the_tensors_device_current(world):
     """The layer norm's workspace depends on the device's number of SMs."""
     for _, _, _, call in world.calls(device=1):
