@@ -7,6 +7,9 @@ contiguous; rows may be any distance apart.  Calls are asynchronous on torch's c
 ``stream`` (a ``torch.cuda.Stream``), behind what that stream has been given before: if the inputs are still being written elsewhere, let it wait
 first.  Workspaces come from torch's allocator.  Outputs are allocated unless given; wait for ``stream`` before reading them elsewhere.
 
+The calls are not part of torch's autograd: results carry no history, whether or not the inputs require gradients.  A backward pass is a call of its own, with
+the tensors that it needs; inside a torch graph, wrap the pair in a ``torch.autograd.Function``.
+
 A small call costs the host a few microseconds more than its kernels, so the checks below ask cheap questions first.
 """
 from __future__ import annotations
@@ -22,7 +25,8 @@ _HALF = {torch.bfloat16: 1, torch.float16: 2}
 _F32 = {torch.float32: 0}
 _INT64 = {torch.int64: 0}
 
-COEFFICIENTS = (3.4445, -4.7750, 2.0315)         # Newton-Schulz step X <- a X + (b A + c A^2) X, A = X X^T
+# Newton-Schulz step X <- a X + (b A + c A^2) X, A = X X^T: the coefficients published with the Muon optimiser (K. Jordan and others, 2024)
+COEFFICIENTS = (3.4445, -4.7750, 2.0315)
 
 
 def _shortcut(owner, name, public):
@@ -298,7 +302,8 @@ def linear_cross_entropy(hidden, weight, targets, stream=None):
 def linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden=None, dweight=None, stream=None):
     """Gradients of ``linear_cross_entropy`` from dloss (fp32, the gradient with respect to every token's loss) and the lse it
     returned.  Returns (dhidden, dweight) of the inputs' type.  ``dhidden``, ``dweight``: tensors to write into (of the inputs' type or
-    fp32; views of the gradient array of a step are fine), False to leave one out."""
+    fp32; views of the gradient array of a step are fine), False to leave one out.  The gradient of the logits is rounded to the inputs' type before
+    the two products that take it, whatever the type of the outputs; sums are fp32."""
     if stream is not None:
         return _on(stream, lambda: linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden, dweight), dloss, hidden, weight, targets, lse, dhidden, dweight)
     device, code, tokens, vocab, width, ld_h, ld_w, pt = _head(hidden, weight, targets)
@@ -339,7 +344,9 @@ def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coef
                   stream=None):
     """The orthogonalised update of matrix parameters: ``steps`` Newton-Schulz products on U / (|U| + eps), U = update, or with a
     momentum (fp32, updated in place) momentum = beta momentum + update and U = update + beta momentum (nesterov) or momentum.
-    update: (rows, cols) or (batch, rows, cols).  Returns out: the same shape, bf16 (fp16 for an fp16 update) unless given."""
+    update: (rows, cols) or (batch, rows, cols).  Returns out: the same shape, bf16 (fp16 for an fp16 update) unless given.
+    Inside, matrices are fp16 with a common scale (X a pair of them in the product P X of all but the last two steps) and sums fp32: the result is
+    within some 1.1e-3 (2-norm, relative) of the formulas' before it is rounded to its own type, for fp16 as for bf16."""
     if stream is not None:
         return _on(stream, lambda: orthogonalize(update, momentum, beta, nesterov, steps, coefficients, eps, out), update, momentum, out)
     if not isinstance(update, torch.Tensor) or update.dim() not in (2, 3):
