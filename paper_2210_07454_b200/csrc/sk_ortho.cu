@@ -347,6 +347,20 @@ __device__ __forceinline__ void load8(const void* p, int type, uint64_t at, uint
     for (int i = 0; i < 8; ++i) v[i] = (uint32_t)i < valid ? load_as(p, type, at + i) : 0.0f;
 }
 
+// 2^12 / (norm + eps) as a product of two factors that are ordinary 32-bit values each: by itself it may be beyond their range (a norm
+// below 2^-115).  exact: both are powers of two, and `rest` in [1, 2) what is left.
+struct Scale { float first, second, rest; };
+__device__ __forceinline__ Scale scale_of(double squares, float eps, bool exact) {
+    const double scale = (double)kScale / (sqrt(squares) + (double)eps);
+    const bool large = scale > 0x1p100, tiny = scale < 0x1p-100;
+    const float first = large ? 0x1p64f : tiny ? 0x1p-64f : 1.0f;
+    const double other = large ? scale * 0x1p-64 : tiny ? scale * 0x1p64 : scale;
+    if (!exact || !(scale > 0.0 && isfinite(scale))) return {first, (float)other, 1.0f};         // (not: infinities or NaN in the update)
+    int e = 0;
+    const double m = 2.0 * frexp(other, &e);                         // other = m 2^(e-1), m in [1, 2)
+    return {first, (float)ldexp(1.0, e - 1), (float)m};
+}
+
 struct SquareArgs {
     OrthoArgs a;
     double* partial;                             // [batch][kNormBlocks]
@@ -413,7 +427,7 @@ __global__ void __launch_bounds__(256) k_ortho_square(const __grid_constant__ Sq
 // first product needs no second matrix.  Otherwise X itself, as the sum of two fp16 matrices.
 __global__ void __launch_bounds__(256) k_ortho_scale(const __grid_constant__ SquareArgs s) {
     __shared__ double sums[8];
-    __shared__ float s_scale;
+    __shared__ Scale s_scale;
     const OrthoArgs& a = s.a;
     chain_acquire();
     const uint32_t b = blockIdx.y, groups = ((uint32_t)a.cols + 7) / 8;
@@ -425,22 +439,14 @@ __global__ void __launch_bounds__(256) k_ortho_scale(const __grid_constant__ Squ
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < 8; ++i) sum += sums[i];
-        const double scale = (double)kScale / (sqrt(sum) + (double)a.eps);
-        int e = 0;
-        double rest = 1.0;
-        if (s.exact && scale > 1e-30 && scale < 1e30) {
-            rest = frexp(scale, &e) * 2.0;                           // scale = rest * 2^(e-1), rest in [1, 2)
-            s_scale = (float)ldexp(1.0, e - 1);
-        } else {
-            s_scale = (float)scale;
-        }
+        s_scale = scale_of(sum, a.eps, s.exact);
         if (blockIdx.x == 0) {
-            s.factor[b] = (float)rest;
+            s.factor[b] = s_scale.rest;
             s.count[b] = 0;
         }
     }
     __syncthreads();
-    const float scale = s_scale;
+    const float first = s_scale.first, second = s_scale.second;
     const uint32_t total = (uint32_t)a.rows * groups;
 #pragma unroll 2
     for (uint32_t q = blockIdx.x * 256 + threadIdx.x; q < total; q += gridDim.x * 256) {
@@ -456,13 +462,13 @@ __global__ void __launch_bounds__(256) k_ortho_scale(const __grid_constant__ Squ
         uint32_t h[4], l[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float x = u[2 * i] * scale, y = u[2 * i + 1] * scale;
+            const float x = u[2 * i] * first * second, y = u[2 * i + 1] * first * second;
             const __half2 p = __floats2half2_rn(x, y);
             const float2 f = __half22float2(p);
             h[i] = *(const uint32_t*)&p;
             l[i] = pack16(x - f.x, y - f.y, false);
         }
-        const uint64_t at = b * s.stride + (uint64_t)row * s.ld + col;   // ld is a multiple of 32: whole groups fit
+        const uint64_t at = b * s.stride + (uint64_t)row * s.ld + col;   // ld is a multiple of 64: whole groups fit
         *(uint4*)(s.hi + at) = make_uint4(h[0], h[1], h[2], h[3]);
         if (s.lo) *(uint4*)(s.lo + at) = make_uint4(l[0], l[1], l[2], l[3]);
     }
@@ -670,7 +676,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
     __syncthreads();
     sum = 0;
     for (uint32_t i = 0; i < S; ++i) sum += shares[i];
-    const float scale = (float)((double)kScale / (sqrt(sum) + (double)a.eps));
+    const Scale scale = scale_of(sum, a.eps, false);
     const bool pair = a.steps > 2;
 #pragma unroll
     for (uint32_t g = 0; g < kSmallGroups; ++g) {
@@ -680,7 +686,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
             uint32_t h[4], l[4];
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float p = u[g][2 * k] * scale, r = u[g][2 * k + 1] * scale;
+                const float p = u[g][2 * k] * scale.first * scale.second, r = u[g][2 * k + 1] * scale.first * scale.second;
                 const __half2 both = __floats2half2_rn(p, r);
                 const float2 f = __half22float2(both);
                 h[k] = *(const uint32_t*)&both;
@@ -693,7 +699,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
                 if (x + k >= fast) break;
-                const float p = u[g][k] * scale;
+                const float p = u[g][k] * scale.first * scale.second;
                 const __half h = __float2half_rn(p);
                 const uint32_t at = (y >> 6) * 16384 + swizzled(x + k, (y & 63) >> 3) + (y & 7) * 2;
                 *(__half*)(base + kSmallHi + at) = h;
