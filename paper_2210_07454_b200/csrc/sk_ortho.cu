@@ -578,7 +578,7 @@ __device__ __forceinline__ void put32(uint8_t* base, uint32_t r, uint32_t col, c
 __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_constant__ SmallArgs s) {
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_mem;
-    __shared__ uint32_t tmem_slot, gave_up;
+    __shared__ uint32_t tmem_slot;
     __shared__ double sums[kSmallThreads / 32], shares[kSmallCluster];
     const OrthoArgs& a = s.a;
     const uint32_t tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, S = s.blocks;
@@ -589,7 +589,6 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
     if (tid == 0) {
         mbar_init(bar, 1);
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        gave_up = 0;
     }
     if (warp == 0) tmem_alloc<1>(smem_u32(&tmem_slot), 512);
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -712,19 +711,18 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
     const uint32_t idesc = (1u << 4) | (8u << 24), idesc_m = idesc | (m16 / 8 << 17), idesc_x = idesc | (1u << 16) | (w16 / 8 << 17);
     const uint32_t quarter = warp & 3, part = warp >> 2, row = quarter * 32 + lane, lanes = (quarter * 32) << 16;     // part: of the columns
     uint32_t phase = 0;
-    // The products of one phase issued by one thread, waited for by all.  Once a wait has run out, nothing more is issued or waited for in this
-    // block; it still takes part in the cluster's barriers.
+    // The products of one phase issued by one thread, waited for by all.  A thread whose wait has run out issues nothing and waits for no products
+    // any more; it still takes part in the barriers of the block and the cluster.
+    bool ok = true;
     auto run = [&](auto issue) {
         fence_async();
         __syncthreads();
-        if (!*(volatile uint32_t*)&gave_up) {
-            if (tid == 0) {
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                issue();
-                mma_commit<1>(bar);
-            }
-            if (!mbar_wait(bar, phase, s.waits)) *(volatile uint32_t*)&gave_up = 1;
+        if (tid == 0 && ok) {
+            asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+            issue();
+            mma_commit<1>(bar);
         }
+        if (ok) ok = mbar_wait(bar, phase, s.waits);
         phase ^= 1;
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         __syncwarp();
