@@ -78,15 +78,11 @@ __device__ __forceinline__ uint64_t clock_ns() {
 // chooses), so tries alone do not bound a wait; they do so as the last resort, should the clock stand still.
 constexpr uint32_t kQuickTries = 256, kQuickRounds = 64, kSlowTries = 1u << 28;
 template <class Ready>
-__device__ __forceinline__ bool wait_until(Ready ready, const Waits& w) {
-    uint64_t end = 0;
-    for (uint32_t r = 0; r < kQuickRounds; ++r) {
+__device__ __forceinline__ bool wait_longer(Ready ready, const Waits& w) {
+    const uint64_t end = clock_ns() + w.limit_ms * 1000000ull;
+    for (uint32_t r = 1; r < kQuickRounds && clock_ns() <= end; ++r)
         for (uint32_t i = 0; i < kQuickTries; ++i)
             if (ready()) return true;
-        const uint64_t now = clock_ns();
-        if (r == 0) end = now + w.limit_ms * 1000000ull;
-        else if (now > end) break;
-    }
     for (uint32_t i = 0; i < kSlowTries && clock_ns() <= end; ++i) {
         if (ready()) return true;
         __nanosleep(500);
@@ -94,8 +90,14 @@ __device__ __forceinline__ bool wait_until(Ready ready, const Waits& w) {
     atomicAdd(w.status, 1u);
     return false;
 }
+template <class Ready>
+__device__ __forceinline__ bool wait_until(Ready ready, const Waits& w) {
+    for (uint32_t i = 0; i < kQuickTries; ++i)
+        if (ready()) return true;
+    return wait_longer(ready, w);
+}
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, const Waits& w) {
-    return wait_until([&] { return mbar_try(bar, parity); }, w);
+    return wait_until([bar, parity] { return mbar_try(bar, parity); }, w);
 }
 // the same for a warp that stays together
 __device__ __forceinline__ bool mbar_wait_warp(uint32_t bar, uint32_t parity, const Waits& w) { return __all_sync(0xffffffffu, mbar_wait(bar, parity, w)); }

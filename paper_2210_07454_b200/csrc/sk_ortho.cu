@@ -124,9 +124,10 @@ struct ChainPlan : ChainShape {
     __device__ __forceinline__ bool wait(const TileJob& j) const {
         const uint32_t need = (j.step * tiles_per_step() + tiles_before(j.kind)) * signals;
         if (!need) return true;
-        const bool ok = wait_until([&] {
+        const uint32_t* counter = count + j.b;
+        const bool ok = wait_until([counter, need] {
             uint32_t have;
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(have) : "l"(count + j.b) : "memory");
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(have) : "l"(counter) : "memory");
             return have >= need;
         }, waits);
         asm volatile("fence.proxy.async;" ::: "memory");             // what was written by stores is read by TMA
