@@ -607,7 +607,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
     // element (i, j) of this block's part: i along the shorter side
     auto offset = [&](uint64_t ld, uint32_t i, uint32_t j) { return s.tall ? (uint64_t)(first + j) * ld + i : (uint64_t)i * ld + first + j; };
     // groups of eight neighbours of a row in memory, at most eight groups a thread, held in registers from the norm to the matrix
-    const uint32_t fast = s.tall ? s.m : width, slow = s.tall ? width : s.m, per = (fast + 7) / 8, groups = per * slow;
+    const uint32_t fast = s.tall ? s.m : width, slow = s.tall ? width : s.m;
+    const uint32_t per = max((fast + 7) / 8, 1u), groups = fast ? per * slow : 0;         // the cluster's last blocks may have no columns
     float u[kSmallGroups][8];
     double sum = 0;
     auto place = [&](uint32_t g, uint32_t& y, uint32_t& x) {

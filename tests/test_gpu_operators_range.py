@@ -56,3 +56,17 @@ def test_orthogonalize_whatever_the_norm(shape, dtype):
         err = torch.linalg.matrix_norm(got.double() - want) / torch.linalg.matrix_norm(want)
         assert float(err.max()) <= BOUND[got.dtype], (power, float(err.max()))
     ops.sync()
+
+
+@pytest.mark.parametrize("rows,cols", [(20, 600), (600, 20), (128, 1100), (1100, 127), (1, 2100), (3, 2500), (65, 4090)])
+def test_orthogonalize_in_a_cluster_with_blocks_that_hold_nothing(rows, cols):
+    """A cluster has a power of two of blocks of 256 columns each: the last ones may have none."""
+    from paper_2210_07454_b200 import operators as ops
+    u = torch.randn(rows, cols, generator=torch.Generator(device="cuda").manual_seed(rows), device="cuda")
+    got, want = ops.orthogonalize(u, out=torch.empty(rows, cols, dtype=torch.float16, device="cuda")), newton_schulz(u)
+    assert float(torch.linalg.matrix_norm(got.double() - want) / torch.linalg.matrix_norm(want)) <= BOUND[torch.float16]
+    m = torch.zeros_like(u)
+    ops.orthogonalize(u, momentum=m, beta=0.5, nesterov=False, out=got)
+    assert torch.equal(m, u)
+    assert float(torch.linalg.matrix_norm(got.double() - want) / torch.linalg.matrix_norm(want)) <= BOUND[torch.float16]
+    ops.sync()
