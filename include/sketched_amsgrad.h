@@ -321,8 +321,9 @@ int sk_linear_cross_entropy_backward(const float* dloss, const void* hidden, uin
  *   U = update, or with momentum M (fp32, updated in place): M = beta M + update, U = update + beta M (nesterov) or M;
  *   X = U / (|U|_F + eps);  steps times: A = X X^T, X = (a I + b A + c A^2) X   (on the shorter side)
  * with coefficients = {a, b, c} (HOST).  update: `type`; out: `out_type`, SK_BF16 or SK_F16.  ..._stride: elements from
- * one matrix to the next (>= rows*ld for outputs).  Inside, matrices are fp16 times 2^12 with fp32 sums, X as a pair of them until the last two
- * steps; the coefficients must keep singular values from [0,1] below 2 in every step, and |a| + |b| + |c| < 15.
+ * one matrix to the next (>= rows*ld for outputs).  Inside, matrices are fp16 times 2^12 with fp32 sums: for SK_BF16 outputs X as a pair of them
+ * in P X until the last two steps (the result is within 1.1e-3 of the formulas' before its own rounding), for SK_F16 outputs, which would
+ * show that, X, A and P as pairs throughout (about 1e-6, at 1.4 to 2.2 times the time); the coefficients must keep singular values from [0,1] below 2 in every step, and |a| + |b| + |c| < 15.
  * momentum may be NULL.  1 <= steps <= 32; rows, cols <= 65536; batch <= 65535.  Matrices with a side of at most 128 and no side
  * above 4096 take one launch and no workspace.  Others take one cooperative launch for all products: it starts when up to one block
  * per SM fits on the device at once, so it waits for kernels of other streams that hold their SMs. */

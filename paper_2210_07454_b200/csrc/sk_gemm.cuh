@@ -4,7 +4,7 @@
 //   D(i, j) = sum_k A(i, k) * B(j, k)      16-bit operands, 32-bit sums
 //
 // Each operand may be stored with k contiguous ("K-major") or with its row index contiguous ("MN-major"); no operand is
-// ever transposed in memory.  A tile may go over two pairs of operands (a matrix held as the sum of two 16-bit matrices).
+// ever transposed in memory.  A tile may go over two or three pairs of operands (matrices held as the sum of two 16-bit matrices).
 //
 // A block (CG = 1) or a pair of blocks on two SMs (CG = 2) works on one output tile of 128*CG rows by BN columns at a
 // time and walks over tiles until none is left.  One warp feeds a ring of kStages shared-memory stages by TMA (64 values of k a
@@ -36,13 +36,13 @@ struct TileJob {
     uint32_t M, N;                            // extents of the output
     uint32_t m, n, b, slice;                  // the tile: row, column, matrix, slice of K
     uint32_t kind, step;                      // which product: for the epilogue
-    uint32_t k_stages, pass;                  // stages (none: begin() does it all); the first `pass` of them over a and b, the others over a2 and b2
+    uint32_t k_stages, pass;                  // stages (none: begin() does it all); the first `pass` of them over a and b, the next over a2 and b2, a3 and b3
     int k_first, z;                           // first k, matrix of the operands
     uint32_t a_mn, b_mn;                      // 1: MN-major
     uint32_t a_rows;                          // rows of A a block loads: 128, or fewer where a single tile row has no more
     uint32_t k_rows;                          // values of k in a stage: 64, or fewer where K has no more (in steps of 16)
     uint32_t bf16;                            // operand type: 1 bf16, 0 fp16
-    const CUtensorMap *map_a, *map_b, *map_a2, *map_b2;
+    const CUtensorMap *map_a, *map_b, *map_a2, *map_b2, *map_a3, *map_b3;
 };
 
 // ---- instruction wrappers -------------------------------------------------------------------------------------------
@@ -201,7 +201,7 @@ struct GemmPlan {
     GemmGroup g[2];
     uint32_t groups, early;
     Waits waits;
-    static constexpr bool kCooperative = false, kEmpty = false;
+    static constexpr bool kCooperative = false, kEmpty = false, kThree = false;      // kThree: a third pair of operands
 
     __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, TileJob& j) const {
         uint32_t t = p + i * units, group = 0;
@@ -294,7 +294,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
     if constexpr (CG == 2) cluster_sync_all();
     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
     const uint32_t tmem = *(volatile uint32_t*)&tmem_slot;
-    if (threadIdx.x < 8) {                                       // the descriptors depend on no other kernel
+    if (threadIdx.x < 16) {                                      // the descriptors depend on no other kernel
         const CUtensorMap* m = plan.descriptor(threadIdx.x);
         if (m) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
     }
@@ -328,6 +328,11 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                     if (k == pass) {                             // the second pair of operands, from the start of K
                         ma = t.map_a2;
                         mb = t.map_b2;
+                        k0 = t.k_first;
+                    }
+                    if (Plan::kThree && k == 2 * pass) {
+                        ma = t.map_a3;
+                        mb = t.map_b3;
                         k0 = t.k_first;
                     }
                     if (!(ok = mbar_wait(empty(s), parity, plan.waits))) break;

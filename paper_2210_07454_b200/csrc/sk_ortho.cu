@@ -14,11 +14,17 @@
 // steps X is the sum of two fp16 matrices (22 bits) in the product P X, whose errors stay in the direction they arise in;
 // A and P are single.  Errors of the result against 64 bits, before the output's own rounding (2-norm,
 // rank 8 plus 5 % noise / gaussian): bf16 throughout 1.1e-1 / 1.0e-2, single fp16 1.4e-2 / 1.3e-3, this 1.1e-3 / 1.1e-3.
+// That is below a bf16 output's own rounding (1.7e-3), but five times an fp16 output's (2.1e-4).  For those, PRECISE: X, A and P are pairs in every
+// product, which is then the sum of three (high high, high low, low high; what is left out is 2^-22 of it).  Modelled: 5e-7, and any one of the
+// matrices single in any three steps costs 2e-4 to 2e-3.  Three times the products take 1.4 times as long for 100 x 130 (31 -> 42 us), 1.8 for
+// 12 x 768 x 768 (206 -> 373) and 2.2 for 8192 x 4096 (2.52 -> 5.66 ms).
 //
 // No operand is transposed: for a tall matrix (rows > cols) the same kernels take X in the other major
 // (A = X^T X, X <- X P).
 #include "sk_gemm.cuh"
 #include "sk_operators.h"
+
+#include <type_traits>
 
 namespace sk {
 namespace {
@@ -55,9 +61,12 @@ struct ChainShape {
     // X is the sum of two matrices in all but the last two steps, and in the first where one is exact
     __host__ __device__ bool pair(uint32_t step) const { return step + 2 < steps && !(step == 0 && exact); }
 };
-template <bool SLICED>
-struct ChainPlan : ChainShape {
-    static constexpr bool kCooperative = true, kEmpty = SLICED;      // kEmpty: has tiles without products
+struct ChainLow {                                // PRECISE: the second matrices of the pairs, where ChainShape has none
+    CUtensorMap gram_xlo[2], gram_lo, poly_lo;
+};
+template <bool SLICED, bool PRECISE>
+struct ChainPlan : ChainShape, std::conditional<PRECISE, ChainLow, std::false_type>::type {
+    static constexpr bool kCooperative = true, kEmpty = SLICED, kThree = PRECISE;    // kEmpty: has tiles without products
     // tiles of one matrix and step before those of a kind, and of all kinds
     __device__ __forceinline__ uint32_t tiles_before(uint32_t kind) const {
         if (!SLICED) return kind * square;
@@ -99,6 +108,11 @@ struct ChainPlan : ChainShape {
             }
             if (SLICED && j.kind == kJoin) j.k_stages = 0;
             j.map_a = j.map_b = j.map_a2 = j.map_b2 = j.kind == kGram ? &gram_x[from] : &gram;
+            if constexpr (PRECISE) {
+                j.map_b2 = j.map_a3 = j.kind == kGram ? &this->gram_xlo[from] : &this->gram_lo;
+                j.map_b3 = j.map_b;
+                if (j.kind == kPoly || (j.kind == kGram && !(j.step == 0 && exact))) j.k_stages *= 3;
+            }
         } else {
             j.b = q / apply;
             q -= j.b * apply;
@@ -117,6 +131,13 @@ struct ChainPlan : ChainShape {
             j.map_b = tall ? &poly : &apply_hi[from];
             j.map_a2 = tall ? &apply_lo[from] : &poly;
             j.map_b2 = tall ? &poly : &apply_lo[from];
+            if constexpr (PRECISE) {             // P's second matrix goes before X's, which the first step may not have
+                j.k_stages = (j.step == 0 && exact ? 2 : 3) * k_poly;
+                j.map_a3 = j.map_a2;
+                j.map_b3 = j.map_b2;
+                j.map_a2 = tall ? j.map_a : &this->poly_lo;
+                j.map_b2 = tall ? &this->poly_lo : j.map_b;
+            }
         }
         j.z = (int)j.b;
         return true;
@@ -140,11 +161,16 @@ struct ChainPlan : ChainShape {
             atomicAdd(count + j.b, 1u);
         }
     }
-    __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return &gram_x[0] + i; }
+    __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const {
+        if (i < 8) return &gram_x[0] + i;
+        if constexpr (PRECISE) return i < 12 ? &this->gram_xlo[0] + (i - 8) : nullptr;
+        return nullptr;
+    }
 };
 
 struct ChainArgs {
     __half *gram, *poly, *hi[2], *lo[2];     // [2]: as the plan's
+    __half *gram_lo, *poly_lo;               // PRECISE
     float* slices;                           // A's: slice by slice, like A but in 32 bits
     uint64_t slice_stride;
     uint32_t slice_count, join_cols;         // join_cols: a warp's columns when they are added up
@@ -160,7 +186,7 @@ struct ChainArgs {
 
 // The epilogues of the three products.  A warp has two areas of staging memory: one for the lines of the matrix it writes, one for those of the second
 // matrix of a pair, or for A's lines on their way to P, which are fetched while the products run.
-template <bool SLICED>
+template <bool SLICED, bool PRECISE>
 struct ChainEpi {
     static constexpr int kWarps = 8, kWords = 2 * kStageWords;
     using Args = ChainArgs;
@@ -219,27 +245,38 @@ struct ChainEpi {
                         sum[i].x += f[j][i].x; sum[i].y += f[j][i].y; sum[i].z += f[j][i].z; sum[i].w += f[j][i].w;
                     }
             }
-            __syncwarp();
 #pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) {
-                const uint32_t lo = pack16(sum[i].x * scale, sum[i].y * scale, false), hi = pack16(sum[i].z * scale, sum[i].w * scale, false);
-                if (first_row + r + 8 * i < t.M) *(uint2*)(out + (uint64_t)(first_row + r + 8 * i) * e.ld_a + col + c) = make_uint2(lo, hi);
-                if (t.m != t.n) {                // the mirror image: 16 rows of 80 bytes in the staging memory
-                    const uint32_t at = stage + c * 80 + (r + 8 * i) * 2;
-                    store_shared2(at, lo);
-                    store_shared2(at + 80, lo >> 16);
-                    store_shared2(at + 160, hi);
-                    store_shared2(at + 240, hi >> 16);
+            for (uint32_t which = 0; which < (PRECISE ? 2u : 1u); ++which) {
+                if (which) out = e.gram_lo + t.b * e.a_stride;
+                __syncwarp();
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    float4& f = sum[i];
+                    if (!which) f = make_float4(f.x * scale, f.y * scale, f.z * scale, f.w * scale);
+                    const uint32_t lo = pack16(f.x, f.y, false), hi = pack16(f.z, f.w, false);
+                    if (first_row + r + 8 * i < t.M) *(uint2*)(out + (uint64_t)(first_row + r + 8 * i) * e.ld_a + col + c) = make_uint2(lo, hi);
+                    if (t.m != t.n) {            // the mirror image: 16 rows of 80 bytes in the staging memory
+                        const uint32_t at = stage + c * 80 + (r + 8 * i) * 2;
+                        store_shared2(at, lo);
+                        store_shared2(at + 80, lo >> 16);
+                        store_shared2(at + 160, hi);
+                        store_shared2(at + 240, hi >> 16);
+                    }
+                    if (PRECISE && !which) {     // what the first matrix leaves
+                        const float2 a = __half22float2(*(const __half2*)&lo), b = __half22float2(*(const __half2*)&hi);
+                        f = make_float4(f.x - a.x, f.y - a.y, f.z - b.x, f.w - b.y);
+                    }
+                }
+                if (t.m == t.n) continue;
+                __syncwarp();
+#pragma unroll
+                for (uint32_t i = 0; i < 2; ++i) {
+                    const uint32_t y = r + 8 * i;
+                    const uint4 w = load_shared16(stage + y * 80 + (lane & 3) * 16);
+                    if (col + y < t.N) *(uint4*)(out + (uint64_t)(col + y) * e.ld_a + first_row + 8 * (lane & 3)) = w;
                 }
             }
-            if (t.m == t.n) continue;
-            __syncwarp();
-#pragma unroll
-            for (uint32_t i = 0; i < 2; ++i) {
-                const uint32_t y = r + 8 * i;
-                const uint4 w = load_shared16(stage + y * 80 + (lane & 3) * 16);
-                if (col + y < t.N) *(uint4*)(out + (uint64_t)(col + y) * e.ld_a + first_row + 8 * (lane & 3)) = w;
-            }
+            out = e.gram + t.b * e.a_stride;
         }
     }
     template <class Plan>
@@ -272,6 +309,29 @@ struct ChainEpi {
             if (c < count && first + c < t.N) *(uint4*)(out + (uint64_t)(first + c) * e.ld_a + row0 + 8 * (lane & 3)) = q[i];
         }
     }
+    // A pair of matrices and their mirror images, 32 columns at a time, one matrix after the other through the first area: the second holds
+    // what is fetched.
+    __device__ void square_pair(__half* hi, __half* lo, uint32_t col, float (&v)[32]) {
+        const uint32_t lane = threadIdx.x & 31, from = 8 * ((lane & 7) >> 1) + 2 * (lane >> 3) + (lane & 1);
+#pragma unroll 1
+        for (uint32_t which = 0; which < 2; ++which) {
+            __half* out = which ? lo : hi;
+            store_tile32(out, SK_F16, e.ld_a, row0, rows, col, e.ld_a, v, 16, stage, false, true);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
+            if (t.m == t.n) continue;
+            uint4 q[4];
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i)
+                asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                             : "=r"(q[i].x), "=r"(q[i].y), "=r"(q[i].z), "=r"(q[i].w) : "r"(staged(stage, from, i)) : "memory");
+#pragma unroll
+            for (uint32_t i = 0; i < 4; ++i) {
+                const uint32_t c = col + 8 * i + (lane >> 2);
+                if (c < t.N) *(uint4*)(out + (uint64_t)c * e.ld_a + row0 + 8 * (lane & 3)) = q[i];
+            }
+        }
+    }
     __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (!rows) return;
         if (SLICED && t.kind == kGram) {       // scaled when the slices are joined
@@ -294,18 +354,36 @@ struct ChainEpi {
                     v[8 * q + 2 * i + 1] = e.b * f.y + e.c * kUnscale * v[8 * q + 2 * i + 1];
                 }
             }
+            if (PRECISE && row < t.M) {          // A's second matrix straight from L2, where the other SMs have written it
+                const __half* low = e.gram_lo + t.b * e.a_stride + (uint64_t)row * e.ld_a + col;
+                uint4 w[4];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) w[q] = __ldcg((const uint4*)low + q);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t r[4] = {w[q].x, w[q].y, w[q].z, w[q].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 f = __half22float2(*(const __half2*)&r[i]);
+                        v[8 * q + 2 * i] += e.b * f.x;
+                        v[8 * q + 2 * i + 1] += e.b * f.y;
+                    }
+                }
+            }
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 if (col + i == row) v[i] += e.a * kScale;
             __syncwarp();
             if ((col & 32) && !last) fetch(col + 32);                // while this pair is written
-            square(e.poly + t.b * e.a_stride, col, v, last);
+            if constexpr (PRECISE) square_pair(e.poly + t.b * e.a_stride, e.poly_lo + t.b * e.a_stride, col, v);
+            else square(e.poly + t.b * e.a_stride, col, v, last);
             return;
         }
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] *= scale;
         if (t.kind == kGram) {
-            square(e.gram + t.b * e.a_stride, col, v, last);
+            if constexpr (PRECISE) square_pair(e.gram + t.b * e.a_stride, e.gram_lo + t.b * e.a_stride, col, v);
+            else square(e.gram + t.b * e.a_stride, col, v, last);
             return;
         }
         if (t.step + 1 == e.steps) {
@@ -314,7 +392,7 @@ struct ChainEpi {
         }
         const uint32_t to = (t.step + 1) & 1;
         store_tile32(e.hi[to] + t.b * e.x_stride, SK_F16, e.ld_x, row0, rows, col, e.ld_x, v, 16, stage, true, last);
-        if (t.step + 3 < e.steps) {              // the next step's X is a pair
+        if (PRECISE || t.step + 3 < e.steps) {   // the next step's X is a pair
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
             store_tile32(e.lo[to] + t.b * e.x_stride, SK_F16, e.ld_x, row0, rows, col, e.ld_x, v, 16, stage + kStageWords * 4, true, last);
@@ -482,8 +560,9 @@ __global__ void __launch_bounds__(256) k_ortho_scale(const __grid_constant__ Squ
 // 107).  Planned for the SMs of a B200, as the workspace's size depends on it.
 constexpr uint64_t kJoinCost = 9000;             // cycles: writing slices, their signal, and adding them up
 struct ChainTiles { bool wide; uint32_t slices; };
-ChainTiles chain_tiles(const OrthoArgs& a) {
+ChainTiles chain_tiles(const OrthoArgs& a, bool precise) {
     const uint64_t m = a.rows < a.cols ? a.rows : a.cols, n = a.rows < a.cols ? a.cols : a.rows, sms = 148;
+    const uint64_t square_passes = precise ? 3 : 1, apply_passes = precise ? 3 : 2;       // most of a step's
     const uint64_t k_gram = (n + kGemmK - 1) / kGemmK, k_poly = (m + kGemmK - 1) / kGemmK;
     ChainTiles best = {false, 1};
     uint64_t least = ~0ull;
@@ -493,10 +572,11 @@ ChainTiles chain_tiles(const OrthoArgs& a) {
         for (uint64_t slices = 1; slices <= 8; ++slices) {
             const uint64_t each = (k_gram + slices - 1) / slices;
             if (slices > 1 && (a.batch * square * slices > units || (slices - 1) * each >= k_gram)) break;       // no empty slice
-            const uint64_t work = a.batch * (square * (k_gram + k_poly) + apply * 2 * k_poly + ((1 + slices) * square + apply) * kTileCost);
+            const uint64_t work = a.batch * (square * square_passes * (k_gram + k_poly) + apply * apply_passes * k_poly +
+                                             ((1 + slices) * square + apply) * kTileCost);
             auto rounds = [&](uint64_t tiles) { return (tiles + units - 1) / units; };
-            const uint64_t path = (rounds(square * slices) * each + rounds(square) * k_poly + rounds(apply) * 2 * k_poly) * 620 + 3 * start +
-                                  (slices > 1 ? kJoinCost : 0), even = work * 620 / units, cost = path > even ? path : even;
+            const uint64_t path = ((rounds(square * slices) * each + rounds(square) * k_poly) * square_passes + rounds(apply) * apply_passes * k_poly) * 620 +
+                                  3 * start + (slices > 1 ? kJoinCost : 0), even = work * 620 / units, cost = path > even ? path : even;
             if (cost < least) {
                 least = cost;
                 best = {wide != 0, (uint32_t)slices};
@@ -509,8 +589,9 @@ ChainTiles chain_tiles(const OrthoArgs& a) {
 struct OrthoLayout {
     uint32_t ld_x, ld_a, m;
     uint64_t x_elems, a_elems;                   // per matrix
-    uint64_t off_partial, off_factor, off_count, off_x[2], off_lo, off_a, off_p, off_slices, total;
+    uint64_t off_partial, off_factor, off_count, off_x[2], off_lo, off_a, off_p, off_a_lo, off_p_lo, off_slices, total;
 };
+// for either type of output
 OrthoLayout layout_of(const OrthoArgs& a) {
     OrthoLayout l;
     l.m = (uint32_t)(a.rows < a.cols ? a.rows : a.cols);
@@ -528,7 +609,9 @@ OrthoLayout layout_of(const OrthoArgs& a) {
     l.off_lo = take(2 * round_up(a.batch * l.x_elems * 2, 256));
     l.off_a = take(a.batch * l.a_elems * 2);
     l.off_p = take(a.batch * l.a_elems * 2);
-    const uint32_t slices = chain_tiles(a).slices;
+    l.off_a_lo = take(a.batch * l.a_elems * 2);
+    l.off_p_lo = take(a.batch * l.a_elems * 2);
+    const uint32_t plain = chain_tiles(a, false).slices, precise = chain_tiles(a, true).slices, slices = plain > precise ? plain : precise;
     l.off_slices = take(slices > 1 ? slices * a.batch * l.a_elems * 4 : 0);
     l.total = at;
     return l;
@@ -561,6 +644,11 @@ __device__ __forceinline__ uint32_t map_to(uint32_t addr, uint32_t rank) {
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
     return r;
 }
+// what rounding to fp16 leaves of values
+__device__ __forceinline__ void leave_low(float (&v)[32]) {
+#pragma unroll
+    for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
+}
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
 // 32 values of a row as fp16 into a swizzled matrix of 64-column blocks of 128 rows
 __device__ __forceinline__ void put32(uint8_t* base, uint32_t r, uint32_t col, const float (&v)[32]) {
@@ -576,7 +664,10 @@ __device__ __forceinline__ void put32(uint8_t* base, uint32_t r, uint32_t col, c
     }
 }
 
+// PRECISE: A's second matrix lies where P lies otherwise, and P's pair takes the places of A's, element by element.
+template <bool PRECISE>
 __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_constant__ SmallArgs s) {
+    constexpr uint32_t kGramLo = kSmallPoly, kP = PRECISE ? kSmallGram : kSmallPoly, kPLo = kSmallPoly;
     extern __shared__ uint8_t smem_raw[];
     __shared__ __align__(8) uint64_t bar_mem;
     __shared__ uint32_t tmem_slot;
@@ -678,7 +769,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
     sum = 0;
     for (uint32_t i = 0; i < S; ++i) sum += shares[i];
     const Scale scale = scale_of(sum, a.eps, false);
-    const bool pair = a.steps > 2;
+    const bool pair = PRECISE || a.steps > 2;
 #pragma unroll
     for (uint32_t g = 0; g < kSmallGroups; ++g) {
         uint32_t y, x;
@@ -733,11 +824,16 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
     auto read_done = [&] { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); };
 
     for (int step = 0; step < a.steps; ++step) {
-        const bool two = step < a.steps - 2;
+        const bool two = PRECISE || step < a.steps - 2;
         run([&] {                                // Y Y^T, this block's columns
             for (uint32_t k = 0; k < w16 / 16; ++k) {
                 const uint64_t d = smem_desc(base32 + kSmallHi + (k >> 2) * 16384, false) + 2 * (k & 3);
                 mma_f16<1>(tmem, d, d, idesc_m, k != 0);
+                if (PRECISE) {
+                    const uint64_t low = smem_desc(base32 + kSmallLo + (k >> 2) * 16384, false) + 2 * (k & 3);
+                    mma_f16<1>(tmem, d, low, idesc_m, 1);
+                    mma_f16<1>(tmem, low, d, idesc_m, 1);
+                }
             }
         });
         const uint32_t col = part * 32;
@@ -749,6 +845,10 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
 #pragma unroll
                 for (int i = 0; i < 32; ++i) v[i] *= kUnscale;
                 put32(base + kSmallGram, row, col, v);
+                if (PRECISE) {
+                    leave_low(v);
+                    put32(base + kGramLo, row, col, v);
+                }
             }
         } else {
             if (mine) {
@@ -783,6 +883,13 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
                 const uint32_t local = base32 + kSmallGram + (c4 >> 4) * 16384 + swizzled(r, (c4 & 15) >> 1) + (c4 & 1) * 8;
                 const uint32_t lo = pack16(t[q].x * kUnscale, t[q].y * kUnscale, false), hi = pack16(t[q].z * kUnscale, t[q].w * kUnscale, false);
                 for (uint32_t k = 0; k < S; ++k) asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(map_to(local, k)), "r"(lo), "r"(hi) : "memory");
+                if (PRECISE) {
+                    const float2 f = __half22float2(*(const __half2*)&lo), g = __half22float2(*(const __half2*)&hi);
+                    const uint32_t lo2 = pack16(t[q].x * kUnscale - f.x, t[q].y * kUnscale - f.y, false),
+                                   hi2 = pack16(t[q].z * kUnscale - g.x, t[q].w * kUnscale - g.y, false);
+                    for (uint32_t k = 0; k < S; ++k)
+                        asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(map_to(local + kGramLo - kSmallGram, k)), "r"(lo2), "r"(hi2) : "memory");
+                }
             }
             fence_async();
             cluster_sync_all();
@@ -792,6 +899,11 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
             for (uint32_t k = 0; k < m16 / 16; ++k) {
                 const uint64_t d = smem_desc(base32 + kSmallGram + (k >> 2) * 16384, false) + 2 * (k & 3);
                 mma_f16<1>(tmem_sq, d, d, idesc_m, k != 0);
+                if (PRECISE) {
+                    const uint64_t low = smem_desc(base32 + kGramLo + (k >> 2) * 16384, false) + 2 * (k & 3);
+                    mma_f16<1>(tmem_sq, d, low, idesc_m, 1);
+                    mma_f16<1>(tmem_sq, low, d, idesc_m, 1);
+                }
             }
         });
         if (mine) {
@@ -806,20 +918,38 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
                     v[8 * i + 2 * k] = a.coefficient[1] * f.x + a.coefficient[2] * kUnscale * v[8 * i + 2 * k];
                     v[8 * i + 2 * k + 1] = a.coefficient[1] * f.y + a.coefficient[2] * kUnscale * v[8 * i + 2 * k + 1];
                 }
+                if (PRECISE) {
+                    const uint4 x = *(const uint4*)(base + kGramLo + (col >> 6) * 16384 + swizzled(row, ((col & 63) >> 3) + i));
+                    const uint32_t l[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float2 f = __half22float2(*(const __half2*)&l[k]);
+                        v[8 * i + 2 * k] += a.coefficient[1] * f.x;
+                        v[8 * i + 2 * k + 1] += a.coefficient[1] * f.y;
+                    }
+                }
             }
 #pragma unroll
             for (int i = 0; i < 32; ++i)
                 if (col + i == row) v[i] += a.coefficient[0] * kScale;
-            put32(base + kSmallPoly, row, col, v);
+            put32(base + kP, row, col, v);
+            if (PRECISE) {
+                leave_low(v);
+                put32(base + kPLo, row, col, v);
+            }
         }
         read_done();
         run([&] {                                // P Y, with both matrices of the pair while there are two
             for (uint32_t which = 0; which < (two ? 2u : 1u); ++which)
                 for (uint32_t k = 0; k < m16 / 16; ++k)
-                    mma_f16<1>(tmem_x, smem_desc(base32 + kSmallPoly + (k >> 2) * 16384, false) + 2 * (k & 3),
+                    mma_f16<1>(tmem_x, smem_desc(base32 + kP + (k >> 2) * 16384, false) + 2 * (k & 3),
                                smem_desc(base32 + (which ? kSmallLo : kSmallHi), true, 16384) + 128 * k, idesc_x, (which | k) != 0);
+            if (PRECISE)
+                for (uint32_t k = 0; k < m16 / 16; ++k)
+                    mma_f16<1>(tmem_x, smem_desc(base32 + kPLo + (k >> 2) * 16384, false) + 2 * (k & 3), smem_desc(base32 + kSmallHi, true, 16384) + 128 * k,
+                               idesc_x, 1);
         });
-        const bool last = step + 1 == a.steps, next_two = step + 1 < a.steps - 2;
+        const bool last = step + 1 == a.steps, next_two = PRECISE || step + 1 < a.steps - 2;
 #pragma unroll 1
         for (uint32_t col = quarter * 32 < s.m ? part * 32 : w16; col < w16; col += 32 * (kSmallThreads / 128)) {
             __syncwarp();
@@ -829,8 +959,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) k_ortho_small(const __grid_c
                 for (int i = 0; i < 32; ++i) v[i] *= kUnscale;
                 put32(base + kSmallHi, row, col, v);
                 if (next_two) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] -= __half2float(__float2half_rn(v[i]));
+                    leave_low(v);
                     put32(base + kSmallLo, row, col, v);
                 }
                 continue;
@@ -879,8 +1008,9 @@ cudaError_t launch_small(const OrthoArgs& a, uint32_t align, const OpDevice& dev
     s.vec_m = a.momentum && vec8(a.momentum, a.ld_momentum, a.stride_momentum, 4);
     s.waits = dev.waits();
     constexpr int kSmem = (int)kSmallBytes + 1024;
-    cudaError_t e = cudaFuncSetAttribute(k_ortho_small, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
-    if (e == cudaSuccess && s.blocks > 8) e = cudaFuncSetAttribute(k_ortho_small, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    auto kernel = a.out_type == SK_F16 ? k_ortho_small<true> : k_ortho_small<false>;
+    cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e == cudaSuccess && s.blocks > 8) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e != cudaSuccess) return e;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((uint32_t)a.batch * s.blocks);
@@ -895,15 +1025,20 @@ cudaError_t launch_small(const OrthoArgs& a, uint32_t align, const OpDevice& dev
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = s.blocks > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, k_ortho_small, s);
+    return cudaLaunchKernelEx(&cfg, kernel, s);
 }
 
 }  // namespace
 
-template <bool SLICED>
-cudaError_t launch_chain(bool wide, const ChainShape& p, const ChainArgs& ea, uint32_t units, cudaStream_t st) {
-    auto launch = wide ? launch_plan<2, 256, ChainPlan<SLICED>, ChainEpi<SLICED>> : launch_plan<1, 128, ChainPlan<SLICED>, ChainEpi<SLICED>>;
-    return launch(false, ChainPlan<SLICED>{p}, ea, units, st);
+template <bool SLICED, bool PRECISE>
+cudaError_t launch_chain(bool wide, const ChainShape& p, const ChainLow& low, const ChainArgs& ea, uint32_t units, cudaStream_t st) {
+    using Plan = ChainPlan<SLICED, PRECISE>;
+    using Epi = ChainEpi<SLICED, PRECISE>;
+    Plan plan{};
+    static_cast<ChainShape&>(plan) = p;
+    if constexpr (PRECISE) static_cast<ChainLow&>(plan) = low;
+    auto launch = wide ? launch_plan<2, 256, Plan, Epi> : launch_plan<1, 128, Plan, Epi>;
+    return launch(false, plan, ea, units, st);
 }
 
 uint64_t orthogonalize_workspace(const OrthoArgs& a) { return is_small(a) ? 0 : layout_of(a).total; }
@@ -925,8 +1060,8 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, uint32_t withh
     const bool tall = a.rows > a.cols;
     const uint32_t batch = (uint32_t)a.batch, m = l.m;
     // two 16-bit matrices for X in all but the last two steps, and one where that is exact
-    const bool exact = a.type != SK_F32 && !a.momentum;
-    auto split = [&](int step) { return step < a.steps - 2 && !(step == 0 && exact); };
+    const bool exact = a.type != SK_F32 && !a.momentum, precise = a.out_type == SK_F16;
+    auto split = [&](int step) { return (precise || step < a.steps - 2) && !(step == 0 && exact); };
 
     const uint32_t blocks = (uint32_t)((a.rows * ((a.cols + 7) / 8) + 255) / 256);
     const uint32_t most = (uint32_t)(round_up((uint64_t)dev.sm_count * 8, batch) / batch), limit = most < kNormBlocks ? most : kNormBlocks;
@@ -948,6 +1083,8 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, uint32_t withh
     ChainArgs ea{};
     ea.gram = gram;
     ea.poly = poly;
+    ea.gram_lo = (__half*)(ws + l.off_a_lo);
+    ea.poly_lo = (__half*)(ws + l.off_p_lo);
     for (int i = 0; i < 2; ++i) { ea.hi[i] = x[i]; ea.lo[i] = lo[i]; }
     ea.a_stride = l.a_elems;
     ea.x_stride = l.x_elems;
@@ -965,15 +1102,24 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, uint32_t withh
     ea.steps = (uint32_t)a.steps;
 
     ChainShape p{};
+    ChainLow low{};
     bool ok = true;
     for (int i = 0; i < 2; ++i) {
         const Operand g{x[i], a.rows, a.cols, l.ld_x, l.x_elems, batch, tall}, h{x[i], a.rows, a.cols, l.ld_x, l.x_elems, batch, !tall},
             o{lo[i], a.rows, a.cols, l.ld_x, l.x_elems, batch, !tall};
         ok = ok && encode_operand(&p.gram_x[i], g, false, g.mn ? 64 : 128) && encode_operand(&p.apply_hi[i], h, false, h.mn ? 64 : 128) &&
              encode_operand(&p.apply_lo[i], o, false, o.mn ? 64 : 128);
+        if (precise) {
+            const Operand gl{lo[i], a.rows, a.cols, l.ld_x, l.x_elems, batch, tall};
+            ok = ok && encode_operand(&low.gram_xlo[i], gl, false, gl.mn ? 64 : 128);
+        }
     }
     const Operand oa{gram, m, m, l.ld_a, l.a_elems, batch, false}, op{poly, m, m, l.ld_a, l.a_elems, batch, false};
     ok = ok && encode_operand(&p.gram, oa, false, 128) && encode_operand(&p.poly, op, false, 128);
+    if (precise) {
+        const Operand al{ea.gram_lo, m, m, l.ld_a, l.a_elems, batch, false}, pl{ea.poly_lo, m, m, l.ld_a, l.a_elems, batch, false};
+        ok = ok && encode_operand(&low.gram_lo, al, false, 128) && encode_operand(&low.poly_lo, pl, false, 128);
+    }
     if (!ok) return set_error(SK_ECUDA, "sk_orthogonalize: a tensor map was refused");
     p.steps = (uint32_t)a.steps;
     p.exact = exact;
@@ -986,7 +1132,7 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, uint32_t withh
     p.k_gram = (uint32_t)(((tall ? a.rows : a.cols) + kGemmK - 1) / kGemmK);
     p.count = sq.count;
     p.waits = dev.waits();
-    const ChainTiles c = chain_tiles(a);
+    const ChainTiles c = chain_tiles(a, precise);
     const uint32_t tile = c.wide ? 256 : 128, slots = (uint32_t)dev.sm_count / (c.wide ? 2 : 1);
     p.side = (m + tile - 1) / tile;
     p.square = p.side * (p.side + 1) / 2;
@@ -999,9 +1145,9 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, uint32_t withh
         ea.slices = (float*)(ws + l.off_slices);
         ea.slice_stride = batch * l.a_elems;
         ea.slice_count = c.slices;
-        ea.join_cols = tile / ChainEpi<true>::kWarps;
+        ea.join_cols = tile / ChainEpi<true, false>::kWarps;
     }
-    p.signals = (c.wide ? 2 : 1) * ChainEpi<true>::kWarps;
+    p.signals = (c.wide ? 2 : 1) * ChainEpi<true, false>::kWarps;
     if ((uint64_t)a.steps * batch * ((c.slices > 1 ? 1ull + c.slices + kJoinParts : 2ull) * p.square + p.apply) * p.signals >= (1ull << 32))
         return set_error(SK_EINVAL, "sk_orthogonalize: batch * rows * cols is too large for one call");
     if (withhold_ms) {                           // every wait asks for more than the tiles' warps ever count
@@ -1009,7 +1155,8 @@ int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, uint32_t withh
         p.waits.limit_ms = withhold_ms;
     }
     const uint32_t most_tiles = batch * (p.square * p.slices > p.apply ? p.square * p.slices : p.apply), units = most_tiles < slots ? most_tiles : slots;
-    SK_OP_CUDA(c.slices > 1 ? launch_chain<true>(c.wide, p, ea, units, st) : launch_chain<false>(c.wide, p, ea, units, st));
+    auto launch = c.slices > 1 ? precise ? launch_chain<true, true> : launch_chain<true, false> : precise ? launch_chain<false, true> : launch_chain<false, false>;
+    SK_OP_CUDA(launch(c.wide, p, low, ea, units, st));
     return SK_OK;
 }
 
