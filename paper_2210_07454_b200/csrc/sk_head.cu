@@ -10,6 +10,12 @@
 // of dhidden, which is added up in 32 bits over the pieces.  Bound by the tensor cores (2 T V D flops forward, 4 backward plus 2
 // for the recomputation); for few tokens by reading W.
 //
+// For few tokens the rounding of G shows in the gradients: one entry of a row, the target's, is much larger than the others, and its error is not
+// averaged away (1 x 3941 x 1024 bf16: 2.7e-3 for an output whose own rounding is 1.7e-3).  Up to kPairTokens tokens G is therefore the sum of two 16-bit
+// matrices, one below the other, and so are the hidden states twice: dW sums over twice the rows, and the rows of dhidden are added up in
+// pairs.  The rows fit one tile either way, and W is read no more often (8 x 50257 x 768 60 -> 65 us, 64 tokens 64 -> 73).  For more tokens that would double the products; there the rounding of
+// G adds up to 41 % to the error of the output's own.
+//
 // A row whose target is negative takes no part: loss 0, gradient 0.  A target >= vocab gives a loss of NaN and no gradient.
 #include "sk_gemm.cuh"
 #include "sk_operators.h"
@@ -117,11 +123,19 @@ __global__ void __launch_bounds__(kJoinThreads) k_head_join(const float2* part, 
     }
 }
 
-// G's piece
+// G's piece.  PAIR: as the sum of two matrices, the second's lines through an area of their own.
+template <bool PAIR>
 struct GradEpi {
-    static constexpr int kWarps = 8, kWords = kStageWords;
+    static constexpr int kWarps = 8, kWords = (PAIR ? 2 : 1) * kStageWords;
     template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
-    struct Args { uint16_t* out; uint64_t ld; const float *lse, *dloss, *factor; const int64_t* targets; uint64_t vocab; uint32_t first; };
+    struct Args {
+        uint16_t *out, *low;                     // low: the second matrix
+        uint64_t ld;
+        const float *lse, *dloss, *factor;
+        const int64_t* targets;
+        uint64_t vocab;
+        uint32_t first;
+    };
     const Args& a;
     const TileJob& t;
     uint32_t row0, rows;
@@ -167,6 +181,11 @@ struct GradEpi {
         }
         __syncwarp();
         store_tile32(a.out, t.bf16 ? SK_BF16 : SK_F16, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage, true, last);
+        if constexpr (PAIR) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] -= t.bf16 ? __bfloat162float(__float2bfloat16_rn(v[i])) : __half2float(__float2half_rn(v[i]));
+            store_tile32(a.low, t.bf16 ? SK_BF16 : SK_F16, a.ld, row0, rows, col, (uint32_t)a.ld, v, 16, stage + kStageWords * 4, true, last);
+        }
     }
     __device__ void end() {}
 };
@@ -214,9 +233,9 @@ struct OutEpi {
     __device__ void end() {}
 };
 
-// dhidden from its shares, slices in order
-__global__ void __launch_bounds__(256) k_head_sum(const float* sum, uint32_t slices, uint64_t stride, uint64_t ld_sum, uint64_t rows, uint32_t cols,
-                                                  const float* factor, void* out, uint64_t ld, int type) {
+// dhidden from its shares, slices in order, and with `second` the other half of the sum as far behind each
+__global__ void __launch_bounds__(256) k_head_sum(const float* sum, uint32_t slices, uint64_t stride, uint64_t second, uint64_t ld_sum, uint64_t rows,
+                                                  uint32_t cols, const float* factor, void* out, uint64_t ld, int type) {
     chain_acquire();
     const float scale = factor ? 1.0f / *factor : 1.0f;
     const uint32_t groups = (cols + 3) / 4;
@@ -230,6 +249,14 @@ __global__ void __launch_bounds__(256) k_head_sum(const float* sum, uint32_t sli
             const float4 w = *(const float4*)(p + s * stride);
             v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
         }
+        if (second) {                            // small against the first: added last
+            float4 u = *(const float4*)(p + second);
+            for (uint32_t s = 1; s < slices; ++s) {
+                const float4 w = *(const float4*)(p + second + s * stride);
+                u.x += w.x; u.y += w.y; u.z += w.z; u.w += w.w;
+            }
+            v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
+        }
         const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
@@ -241,7 +268,7 @@ __global__ void __launch_bounds__(256) k_head_sum(const float* sum, uint32_t sli
 // take no part become zero.  The backward pass always takes the hidden states through this: in dW a token without a target is multiplied
 // by zeros, and whatever its row holds (padding may hold infinities or NaN) must not survive that.
 struct PackArgs {
-    struct One { const uint16_t* src; uint16_t* dst; uint64_t ld, rows; const int64_t* targets; uint32_t ld_dst; } m[2];
+    struct One { const uint16_t* src; uint16_t* dst; uint64_t ld, rows, distinct; const int64_t* targets; uint32_t ld_dst; } m[2];    // rows: `distinct` ones over again
     uint64_t vocab;
     uint32_t cols, first_blocks;                 // blocks of the first matrix
     uint32_t copy_blocks;                        // of all matrices
@@ -271,7 +298,7 @@ __device__ void head_factor(const float* dloss, const int64_t* targets, uint64_t
 __global__ void __launch_bounds__(256) k_head_pack(const __grid_constant__ PackArgs a) {
     chain_acquire();
     if (blockIdx.x >= a.copy_blocks) {
-        head_factor(a.dloss, a.m[0].targets, a.m[0].rows, a.vocab, a.factor);
+        head_factor(a.dloss, a.m[0].targets, a.m[0].distinct, a.vocab, a.factor);
         return;
     }
     const uint32_t which = blockIdx.x >= a.first_blocks;
@@ -282,8 +309,9 @@ __global__ void __launch_bounds__(256) k_head_pack(const __grid_constant__ PackA
     for (uint64_t q = block * 256ull + threadIdx.x; q < total; q += step) {
         const uint64_t r = q / groups;
         const uint32_t c = (uint32_t)(q - r * groups) * 8;
-        const bool live = !m.targets || (m.targets[r] >= 0 && m.targets[r] < (int64_t)a.vocab);
-        const uint16_t* s = m.src + r * m.ld + c;
+        const uint64_t from = r < m.distinct ? r : r - m.distinct;
+        const bool live = !m.targets || (m.targets[from] >= 0 && m.targets[from] < (int64_t)a.vocab);
+        const uint16_t* s = m.src + from * m.ld + c;
         uint4 v = make_uint4(0, 0, 0, 0);
         if (live && c + 8 <= a.cols && vec) {
             v = *(const uint4*)s;
@@ -306,10 +334,12 @@ struct HeadLayout {
     bool pack_h, pack_w;
     uint64_t ld_h, ld_w, off_h, off_w, off_part, off_target, off_factor, off_g, ld_g, off_sum, ld_sum, sum_stride, piece, total;
     uint32_t slices;                             // of the vocabulary's pieces in the product that gives dhidden
+    uint64_t rows;                               // of G: one or two for a token
     bool wide;                                   // tiles of the two gradient products
 };
 // columns of the vocabulary per piece: G's piece is to stay below this size
 constexpr uint64_t kPieceBytes = 512ull << 20;
+constexpr uint64_t kPairTokens = 64;             // G a pair: both halves' rows fit a tile of 128
 
 // The product that gives dhidden has few tiles and a long K (a piece of the vocabulary), the one that gives dW many short ones; they run
 // in one launch.  K is split where one tile of the first would last longer than about half of an even share of all the work.
@@ -340,22 +370,23 @@ HeadLayout layout_of(const HeadArgs& a, bool backward) {
     // more than that would save.
     l.ld_h = round_up(a.width, 64);
     l.ld_w = round_up(a.width, 8);
-    if (l.pack_h) l.off_h = take(a.tokens * l.ld_h * 2);
+    l.rows = backward && a.tokens <= kPairTokens ? 2 * a.tokens : a.tokens;
+    if (l.pack_h) l.off_h = take(l.rows * l.ld_h * 2);
     if (l.pack_w) l.off_w = take(a.vocab * l.ld_w * 2);
     if (!backward) {
         l.off_part = take(2 * ((a.vocab + 127) / 128) * a.tokens * sizeof(float2));
         l.off_target = take(a.tokens * 4);
     } else {
         l.off_factor = take(4);
-        uint64_t pieces = (a.tokens * a.vocab * 2 + kPieceBytes - 1) / kPieceBytes;
+        uint64_t pieces = (l.rows * a.vocab * 2 + kPieceBytes - 1) / kPieceBytes;
         l.piece = round_up((a.vocab + pieces - 1) / pieces, 256);
         l.ld_g = l.piece < round_up(a.vocab, 64) ? l.piece : round_up(a.vocab, 64);
-        l.off_g = take(a.tokens * l.ld_g * 2);
+        l.off_g = take(l.rows * l.ld_g * 2);
         l.ld_sum = round_up(a.width, 32);
-        l.sum_stride = a.tokens * l.ld_sum;
+        l.sum_stride = l.rows * l.ld_sum;
         l.wide = a.tokens > 128;
         l.slices = slices_of(a.tokens, l.piece < a.vocab ? l.piece : a.vocab, a.width, l.wide);
-        if (a.dhidden && (l.piece < a.vocab || l.slices > 1)) l.off_sum = take(l.slices * l.sum_stride * 4);
+        if (a.dhidden && (l.piece < a.vocab || l.slices > 1 || l.rows > a.tokens)) l.off_sum = take(l.slices * l.sum_stride * 4);
     }
     l.total = at;
     return l;
@@ -368,17 +399,17 @@ int pack_operands(const HeadArgs& a, bool backward, const HeadLayout& l, const O
     *h = a.hidden; *w = a.weight; *ld_h = a.ld_hidden; *ld_w = a.ld_weight;
     PackArgs p{};
     uint32_t n = 0, blocks[2] = {0, 0};
-    auto add = [&](const void* src, uint64_t ld, uint64_t off, uint64_t ld_dst, uint64_t rows, const int64_t* targets) {
-        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, rows, targets, (uint32_t)ld_dst};
+    auto add = [&](const void* src, uint64_t ld, uint64_t off, uint64_t ld_dst, uint64_t rows, uint64_t distinct, const int64_t* targets) {
+        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, rows, distinct, targets, (uint32_t)ld_dst};
         const uint64_t want = (rows * (ld_dst / 8) + 255) / 256, most = (uint64_t)dev.sm_count * 16;
         blocks[n++] = (uint32_t)(want < most ? want : most);
     };
     if (l.pack_h) {
-        add(a.hidden, a.ld_hidden, l.off_h, l.ld_h, a.tokens, backward ? a.targets : nullptr);
+        add(a.hidden, a.ld_hidden, l.off_h, l.ld_h, l.rows, a.tokens, backward ? a.targets : nullptr);
         *h = ws + l.off_h; *ld_h = l.ld_h;
     }
     if (l.pack_w) {
-        add(a.weight, a.ld_weight, l.off_w, l.ld_w, a.vocab, nullptr);
+        add(a.weight, a.ld_weight, l.off_w, l.ld_w, a.vocab, a.vocab, nullptr);
         *w = ws + l.off_w; *ld_w = l.ld_w;
     }
     if (!n) return SK_OK;
@@ -435,20 +466,26 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
         const uint16_t* wp = (const uint16_t*)w + v0 * ld_w;
         const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{wp, n, a.width, ld_w, 0, 1, false};
         GemmGroup g{};
-            g.bf16 = a.type == SK_BF16;
+        g.bf16 = a.type == SK_BF16;
         g.M = tokens;
         g.N = n;
-        const GradEpi::Args ga{gbuf, l.ld_g, a.lse, a.dloss, factor, a.targets, a.vocab, (uint32_t)v0};
-        auto launch_g = wide_tiles(tokens, n, (a.width + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_products<2, 256, GradEpi> : launch_products<1, 128, GradEpi>;
-        SK_OP_CUDA(launch_g(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ga, dev.sm_count, st));
+        if (l.rows > a.tokens) {                         // one tile high
+            const GradEpi<true>::Args ga{gbuf, gbuf + a.tokens * l.ld_g, l.ld_g, a.lse, a.dloss, factor, a.targets, a.vocab, (uint32_t)v0};
+            SK_OP_CUDA((launch_products<1, 128, GradEpi<true>>(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ga, dev.sm_count, st)));
+        } else {
+            const GradEpi<false>::Args ga{gbuf, nullptr, l.ld_g, a.lse, a.dloss, factor, a.targets, a.vocab, (uint32_t)v0};
+            auto launch_g = wide_tiles(tokens, n, (a.width + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_products<2, 256, GradEpi<false>>
+                                                                                                  : launch_products<1, 128, GradEpi<false>>;
+            SK_OP_CUDA(launch_g(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ga, dev.sm_count, st));
+        }
         // dW[v] = sum over tokens of G[t][v] hidden[t]: both factors with their rows contiguous;
         // dhidden[t] += sum over the piece of G[t][v] W[v]
-        const Operand gt{gbuf, a.tokens, n, l.ld_g, 0, 1, true}, ht{h, a.tokens, a.width, ld_h, 0, 1, true};
-        const Operand og{gbuf, a.tokens, n, l.ld_g, 0, 1, false}, wt{wp, n, a.width, ld_w, 0, 1, true};
+        const Operand gt{gbuf, l.rows, n, l.ld_g, 0, 1, true}, ht{h, l.rows, a.width, ld_h, 0, 1, true};
+        const Operand og{gbuf, l.rows, n, l.ld_g, 0, 1, false}, wt{wp, n, a.width, ld_w, 0, 1, true};
         GemmGroup gw = g, gh = g;
         gw.M = n;
         gw.N = gh.N = width;
-        gh.M = tokens;
+        gh.M = (uint32_t)l.rows;
         OutEpi::One one_w{}, one_h{};
         one_w.out = (uint8_t*)a.dweight + v0 * a.ld_dweight * type_size(a.dweight_type);
         one_w.ld = a.ld_dweight;
@@ -472,8 +509,8 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
     }
     if (sum) {
         const uint64_t want = (a.tokens * ((width + 3) / 4) + 255) / 256, most = (uint64_t)dev.sm_count * 8;
-        SK_OP_CUDA(launch_kernel(true, k_head_sum, dim3((uint32_t)(want < most ? want : most)), 256, 0, st, (const float*)sum, l.slices, l.sum_stride, l.ld_sum,
-                                 a.tokens, width, (const float*)factor, a.dhidden, a.ld_dhidden, a.dhidden_type));
+        SK_OP_CUDA(launch_kernel(true, k_head_sum, dim3((uint32_t)(want < most ? want : most)), 256, 0, st, (const float*)sum, l.slices, l.sum_stride,
+                                 l.rows > a.tokens ? a.tokens * l.ld_sum : 0, l.ld_sum, a.tokens, width, (const float*)factor, a.dhidden, a.ld_dhidden, a.dhidden_type));
     }
     return SK_OK;
 }

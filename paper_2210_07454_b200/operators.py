@@ -302,8 +302,8 @@ def linear_cross_entropy(hidden, weight, targets, stream=None):
 def linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden=None, dweight=None, stream=None):
     """Gradients of ``linear_cross_entropy`` from dloss (fp32, the gradient with respect to every token's loss) and the lse it
     returned.  Returns (dhidden, dweight) of the inputs' type.  ``dhidden``, ``dweight``: tensors to write into (of the inputs' type or
-    fp32; views of the gradient array of a step are fine), False to leave one out.  The gradient of the logits is rounded to the inputs' type before
-    the two products that take it, whatever the type of the outputs; sums are fp32."""
+    fp32; views of the gradient array of a step are fine), False to leave one out.  Beyond 64 tokens the gradient of the logits is rounded to the inputs'
+    type before the two products that take it, whatever the type of the outputs; up to 64 it is a pair of such values.  Sums are fp32."""
     if stream is not None:
         return _on(stream, lambda: linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden, dweight), dloss, hidden, weight, targets, lse, dhidden, dweight)
     device, code, tokens, vocab, width, ld_h, ld_w, pt = _head(hidden, weight, targets)

@@ -64,3 +64,40 @@ def test_orthogonalize_keeps_fp16s_bits_whatever_the_steps(rows, cols, steps):
         want = newton_schulz(u, steps, coefficients)
         small = 2.0 ** -25 * math.sqrt(rows * cols) / float(torch.linalg.matrix_norm(want))
         assert error(got, want) <= FP16 + small
+
+
+# Beside the output's own rounding, which is that of the definition's value: the logits' errors (1e-6 of values about ten, in the exponent), the
+# exponentials', 32-bit sums, and the gradient of the logits as a pair of 16-bit values (2^-17): 4e-5.
+HEAD = 4e-5
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("tokens,vocab,width", [(1, 3941, 1024), (1, 300, 64), (2, 7374, 2113), (4, 2048, 204), (5, 50257, 768), (10, 5332, 114), (17, 4288, 1127),
+                                                (31, 1001, 65), (32, 130, 96), (33, 9000, 200), (48, 20001, 100), (63, 4000, 770), (64, 32003, 320)])
+def test_linear_cross_entropy_backward_of_few_tokens_keeps_the_types_bits(tokens, vocab, width, dtype):
+    """Few gradients of logits are large (those of the targets): what rounding them would cost is not averaged away over few tokens."""
+    from paper_2210_07454_b200 import operators as ops
+    w = (randn(1, vocab, width) * (2 / math.sqrt(width))).to(dtype)
+    t = torch.randint(0, vocab, (tokens,), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    sure = torch.arange(tokens, device="cuda") % 2 == 1
+    h = (randn(3, tokens, width) + 2.5 * sure[:, None] * w[t].float()).to(dtype)
+    if tokens > 4:
+        t[3] = -100
+    z = h.double() @ w.double().T
+    lse = torch.logsumexp(z, 1).float()
+    dloss = (0.5 + torch.rand(tokens, generator=torch.Generator(device="cuda").manual_seed(4), device="cuda")) / tokens
+    dh, dw = ops.linear_cross_entropy_backward(dloss, h, w, t, lse)
+    g = torch.exp(z - lse.double()[:, None])
+    g[torch.arange(tokens, device="cuda"), t.clamp(min=0)] -= 1.0
+    g *= torch.where(t >= 0, dloss.double(), 0.0)[:, None]
+    for got, want in ((dh, g @ w.double()), (dw, g.T @ h.double())):
+        rounding = float((want.to(dtype).double() - want).norm())
+        assert float((got.double() - want).norm()) <= rounding + HEAD * float(want.norm())
+    fh, fw = torch.empty_like(h, dtype=torch.float32), torch.empty_like(w, dtype=torch.float32)
+    ops.linear_cross_entropy_backward(dloss, h, w, t, lse, dhidden=fh, dweight=fw)
+    assert torch.equal(fh.to(dtype), dh) and torch.equal(fw.to(dtype), dw)
+    for got, want in ((fh, g @ w.double()), (fw, g.T @ h.double())):
+        assert float((got.double() - want).norm()) <= HEAD * float(want.norm())
+    one = ops.linear_cross_entropy_backward(dloss, h, w, t, lse, dweight=False)[0], ops.linear_cross_entropy_backward(dloss, h, w, t, lse, dhidden=False)[1]
+    assert torch.equal(one[0], dh) and torch.equal(one[1], dw)
+    ops.sync()
