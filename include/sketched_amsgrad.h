@@ -307,7 +307,8 @@ int sk_linear_cross_entropy(const void* hidden, uint64_t ld_hidden, const void* 
 /* Its gradient: G_iv = dloss_i (exp(z_iv - lse_i) - [v = targets[i]]) (0 for rows whose target is outside 0..vocab-1),
  * dhidden = G weight, dweight = G^T hidden.  lse: the forward pass's; dloss: tokens fp32, the gradient of the whole with respect to
  * loss_i (1/tokens for a mean).  The vocabulary is taken in pieces whose G stays below half a GiB.  G is an operand of both products, in `type`:
- * the sum of two such matrices for up to 64 tokens, one for more (its rounding then adds up to 41 % to the error of an output's own); sums
+ * the sum of two such matrices for up to 64 tokens, one for more (its rounding then adds up to 41 % to the error of an output's own), taken
+ * relative to the largest |dloss|, so that the targets' entries of a mean, all about -dloss, are exact; sums
  * are fp32, the tensor cores' (logits of width 2500: 1.5e-6).  dhidden: tokens x width of `dhidden_type`; dweight: vocab x width of `dweight_type`; types `type` or
  * SK_F32; either may be NULL.  dweight may be a slice of the gradient array of sk_step (element-aligned is enough). */
 uint64_t sk_linear_cross_entropy_backward_workspace(const void* hidden, uint64_t ld_hidden, const void* weight,

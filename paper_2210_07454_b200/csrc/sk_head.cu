@@ -14,7 +14,7 @@
 // averaged away (1 x 3941 x 1024 bf16: 2.7e-3 for an output whose own rounding is 1.7e-3).  Up to kPairTokens tokens G is therefore the sum of two 16-bit
 // matrices, one below the other, and so are the hidden states twice: dW sums over twice the rows, and the rows of dhidden are added up in
 // pairs.  The rows fit one tile either way, and W is read no more often (8 x 50257 x 768 60 -> 65 us, 64 tokens 64 -> 73).  For more tokens that would double the products; there the rounding of
-// G adds up to 41 % to the error of the output's own.
+// G adds some 35 % to the error of the output's own (41 % at most, were every entry rounded by itself).
 //
 // A row whose target is negative takes no part: loss 0, gradient 0.  A target >= vocab gives a loss of NaN and no gradient.
 #include "sk_gemm.cuh"
@@ -149,7 +149,7 @@ struct GradEpi {
             const int64_t v = a.targets[row];
             if (v >= 0 && v < (int64_t)a.vocab) {
                 target = v - (int64_t)a.first;
-                scale = a.dloss[row] * (a.factor ? *a.factor : 1.0f);
+                scale = a.dloss[row] * *a.factor;
                 off = a.lse[row];
             }
         }
@@ -205,7 +205,7 @@ struct OutEpi {
     float scale;
     __device__ OutEpi(const Args& a_, const TileJob& t_, uint32_t row, uint32_t, uint32_t stage_)
         : a(a_.o[t_.kind]), t(t_), sum(a.sum ? a.sum + t_.slice * a.sum_stride : nullptr), row0(row - (threadIdx.x & 31)), stage(stage_),
-          scale(a_.factor ? 1.0f / *a_.factor : 1.0f) {
+          scale(1.0f / *a_.factor) {
         rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32;
     }
     __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
@@ -237,7 +237,7 @@ struct OutEpi {
 __global__ void __launch_bounds__(256) k_head_sum(const float* sum, uint32_t slices, uint64_t stride, uint64_t second, uint64_t ld_sum, uint64_t rows,
                                                   uint32_t cols, const float* factor, void* out, uint64_t ld, int type) {
     chain_acquire();
-    const float scale = factor ? 1.0f / *factor : 1.0f;
+    const float scale = 1.0f / *factor;
     const uint32_t groups = (cols + 3) / 4;
     const uint64_t total = rows * groups;
     for (uint64_t q = blockIdx.x * 256ull + threadIdx.x; q < total; q += gridDim.x * 256ull) {
@@ -274,10 +274,12 @@ struct PackArgs {
     uint32_t copy_blocks;                        // of all matrices
     const float* dloss;                          // with a factor: one block more
     float* factor;
+    float most;                                  // of |dloss| times the factor
 };
-// fp16 only: a power of two that brings the largest |dloss| to about 2^14, so that small probabilities stay above fp16's
-// smallest values; the products divide by it again
-__device__ void head_factor(const float* dloss, const int64_t* targets, uint64_t tokens, uint64_t vocab, float* factor) {
+// What G is multiplied by before it is rounded; the products divide by it again.  It brings the largest |dloss| to a power of two: 1, or 2^14 for fp16, so
+// that small probabilities stay above fp16's smallest values.  A target's entry of G is dloss (p - 1), about -dloss, and in a mean it is the same for
+// all tokens: this way its rounding is nothing (-1 is exact), where it would be the same error in all of them, up to 2^-8 of the gradients in bf16.
+__device__ void head_factor(const float* dloss, const int64_t* targets, uint64_t tokens, uint64_t vocab, float most, float* factor) {
     __shared__ float s[8];
     float m = 0;
     for (uint64_t i = threadIdx.x; i < tokens; i += 256)
@@ -288,17 +290,14 @@ __device__ void head_factor(const float* dloss, const int64_t* targets, uint64_t
     __syncthreads();
     if (threadIdx.x == 0) {
         for (int i = 1; i < 8; ++i) m = fmaxf(m, s[i]);
-        int e = 0;
-        if (m > 0 && isfinite(m)) frexpf(m, &e);
-        e = 14 - e;
-        *factor = m > 0 && isfinite(m) ? exp2f((float)(e < -100 ? -100 : e > 100 ? 100 : e)) : 1.0f;
+        *factor = m > 0 && isfinite(m) ? fminf(fmaxf(most / m, 0x1p-100f), 0x1p100f) : 1.0f;
     }
 }
 // A thread copies eight neighbours: eight loads on their way at once whatever the alignment, one 16-byte store.
 __global__ void __launch_bounds__(256) k_head_pack(const __grid_constant__ PackArgs a) {
     chain_acquire();
     if (blockIdx.x >= a.copy_blocks) {
-        head_factor(a.dloss, a.m[0].targets, a.m[0].distinct, a.vocab, a.factor);
+        head_factor(a.dloss, a.m[0].targets, a.m[0].distinct, a.vocab, a.most, a.factor);
         return;
     }
     const uint32_t which = blockIdx.x >= a.first_blocks;
@@ -419,6 +418,7 @@ int pack_operands(const HeadArgs& a, bool backward, const HeadLayout& l, const O
     p.copy_blocks = blocks[0] + blocks[1];
     p.dloss = a.dloss;
     p.factor = factor;
+    p.most = a.type == SK_F16 ? 0x1p14f : 1.0f;
     SK_OP_CUDA(launch_kernel(true, k_head_pack, dim3(p.copy_blocks + (factor ? 1 : 0)), 256, 0, st, p));
     return SK_OK;
 }
@@ -455,7 +455,7 @@ int launch_head_backward(const HeadArgs& a, const OpDevice& dev, cudaStream_t st
     uint8_t* ws = (uint8_t*)a.workspace;
     const void *h, *w;
     uint64_t ld_h, ld_w;
-    float* factor = a.type == SK_F16 ? (float*)(ws + l.off_factor) : nullptr;
+    float* factor = (float*)(ws + l.off_factor);
     int rc = pack_operands(a, true, l, dev, &h, &w, &ld_h, &ld_w, factor, st);
     if (rc) return rc;
     const uint32_t tokens = (uint32_t)a.tokens, width = (uint32_t)a.width;

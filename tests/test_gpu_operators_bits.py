@@ -101,3 +101,31 @@ def test_linear_cross_entropy_backward_of_few_tokens_keeps_the_types_bits(tokens
     one = ops.linear_cross_entropy_backward(dloss, h, w, t, lse, dweight=False)[0], ops.linear_cross_entropy_backward(dloss, h, w, t, lse, dhidden=False)[1]
     assert torch.equal(one[0], dh) and torch.equal(one[1], dw)
     ops.sync()
+
+
+@pytest.mark.parametrize("dtype,bits", [(torch.bfloat16, 8), (torch.float16, 11)], ids=["bfloat16", "float16"])
+@pytest.mark.parametrize("tokens,vocab,width", [(300, 5000, 64), (1100, 20000, 96), (65, 3000, 100)])
+def test_linear_cross_entropy_backward_of_a_mean(tokens, vocab, width, dtype, bits):
+    """The gradient of a mean: every token has the same dloss, here one that the type rounds by half a unit.  The targets' entries of the
+    logits' gradient are all about -dloss: an error that they have in common would scale the gradients as a whole."""
+    from paper_2210_07454_b200 import operators as ops
+    w = (randn(1, vocab, width) * (0.2 / math.sqrt(width))).to(dtype)
+    t = torch.randint(0, vocab, (tokens,), generator=torch.Generator(device="cuda").manual_seed(2), device="cuda")
+    h = randn(3, tokens, width).to(dtype)
+    z = h.double() @ w.double().T
+    lse = torch.logsumexp(z, 1).float()
+    rows = torch.arange(tokens, device="cuda")
+    for c in ((1 + 2.0 ** -bits) * 2.0 ** -9, 1.0 / tokens):
+        dloss = torch.full((tokens,), c, device="cuda")
+        fh, fw = torch.empty_like(h, dtype=torch.float32), torch.empty_like(w, dtype=torch.float32)
+        ops.linear_cross_entropy_backward(dloss, h, w, t, lse, dhidden=fh, dweight=fw)
+        p = torch.exp(z - lse.double()[:, None])
+        g = p.clone()
+        g[rows, t] -= 1.0
+        # -1 is exact: p - 1 is off by at most p, the other entries by half a unit (and by half of 2^-38 of -1 below fp16's range)
+        off = p * 2.0 ** -bits + (2.0 ** -39 if dtype == torch.float16 else 0.0)
+        off[rows, t] = p[rows, t]
+        for got, want, norm in ((fh, g @ w.double(), torch.linalg.matrix_norm(w.double(), 2)), (fw, g.T @ h.double(), torch.linalg.matrix_norm(h.double(), 2))):
+            want = want * float(dloss[0])
+            assert float((got.double() - want).norm()) <= float(off.norm() * norm) * c + HEAD * float(want.norm()), c
+    ops.sync()
