@@ -306,11 +306,12 @@ int sk_linear_cross_entropy(const void* hidden, uint64_t ld_hidden, const void* 
 
 /* Its gradient: G_iv = dloss_i (exp(z_iv - lse_i) - [v = targets[i]]) (0 for rows whose target is outside 0..vocab-1),
  * dhidden = G weight, dweight = G^T hidden.  lse: the forward pass's; dloss: tokens fp32, the gradient of the whole with respect to
- * loss_i (1/tokens for a mean).  The vocabulary is taken in pieces whose G stays below half a GiB.  G is an operand of both products, in `type`:
- * the sum of two such matrices for up to 64 tokens, one for more (its rounding then adds up to 41 % to the error of an output's own), taken
- * relative to the largest |dloss|, so that the targets' entries of a mean, all about -dloss, are exact; sums
- * are fp32, the tensor cores' (logits of width 2500: 1.5e-6).  dhidden: tokens x width of `dhidden_type`; dweight: vocab x width of `dweight_type`; types `type` or
- * SK_F32; either may be NULL.  dweight may be a slice of the gradient array of sk_step (element-aligned is enough). */
+ * loss_i (1/tokens for a mean).  The vocabulary is taken in pieces whose G stays below half a GiB.  G is an operand of both products, in
+ * `type`: the sum of two such matrices for up to 64 tokens, one for more (its rounding then adds up to 41 % to the error of an output's own),
+ * taken relative to the largest |dloss|, so that the targets' entries of a mean, all about -dloss, are exact.  Sums are fp32, the tensor
+ * cores' (relative error of logits of width 2500: 1.5e-6).  dhidden: tokens x width of `dhidden_type`; dweight: vocab x width of
+ * `dweight_type`; types `type` or SK_F32; either may be NULL.  dweight may be a slice of the gradient array of sk_step (element-aligned is
+ * enough); dhidden may be hidden, neither may be weight. */
 uint64_t sk_linear_cross_entropy_backward_workspace(const void* hidden, uint64_t ld_hidden, const void* weight,
                                                     uint64_t ld_weight, uint64_t tokens, uint64_t vocab, uint64_t width);
 int sk_linear_cross_entropy_backward(const float* dloss, const void* hidden, uint64_t ld_hidden, const void* weight,
@@ -323,9 +324,10 @@ int sk_linear_cross_entropy_backward(const float* dloss, const void* hidden, uin
  *   U = update, or with momentum M (fp32, updated in place): M = beta M + update, U = update + beta M (nesterov) or M;
  *   X = U / (|U|_F + eps);  steps times: A = X X^T, X = (a I + b A + c A^2) X   (on the shorter side)
  * with coefficients = {a, b, c} (HOST).  update: `type`; out: `out_type`, SK_BF16 or SK_F16.  ..._stride: elements from
- * one matrix to the next (>= rows*ld for outputs).  Inside, matrices are fp16 times 2^12 with fp32 sums: for SK_BF16 outputs X as a pair of them
- * in P X until the last two steps (the result is within 1.1e-3 of the formulas' before its own rounding), for SK_F16 outputs, which would
- * show that, X, A and P as pairs throughout (about 1e-6, at 1.4 to 2.2 times the time); the coefficients must keep singular values from [0,1] below 2 in every step, and |a| + |b| + |c| < 15.
+ * one matrix to the next (>= rows*ld for outputs).  Inside, matrices are fp16 times 2^12 with fp32 sums: for SK_BF16 outputs X as a pair
+ * of them in P X until the last two steps (the result is within 1.1e-3 of the formulas' before its own rounding), for SK_F16 outputs, which
+ * would show that, X, A and P as pairs throughout (about 1e-6, at 1.4 to 2.2 times the time).  The coefficients must keep singular values
+ * from [0,1] below 2 in every step, and |a| + |b| + |c| < 15.
  * momentum may be NULL.  1 <= steps <= 32; rows, cols <= 65536; batch <= 65535.  Matrices with a side of at most 128 and no side
  * above 4096 take one launch and no workspace.  Others take one cooperative launch for all products: it starts when up to one block
  * per SM fits on the device at once, so it waits for kernels of other streams that hold their SMs. */

@@ -80,6 +80,7 @@ int sk_layer_norm(const void* x, uint64_t ld_x, void* y, uint64_t ld_y, int type
     if (rows == 0) return SK_OK;
     if (!x || !y) return set_error(SK_EINVAL, "%s: null argument", who);
     if (ld_x < cols || ld_y < cols) return set_error(SK_EINVAL, "%s: a leading dimension is below cols", who);
+    if (rows > 1 && y == x && ld_y != ld_x) return set_error(SK_EINVAL, "%s: in place, the leading dimensions must be the same", who);
     if (misaligned(x, type) || misaligned(y, type) || misaligned(weight, weight_type) || misaligned(bias, weight_type) || misaligned(mean, SK_F32) ||
         misaligned(rstd, SK_F32))
         return set_error(SK_EINVAL, "%s: a pointer is not aligned to its element", who);
@@ -112,6 +113,8 @@ int sk_layer_norm_backward(const void* dy, uint64_t ld_dy, const void* x, uint64
     }
     if (!dy || !x || !mean || !rstd) return set_error(SK_EINVAL, "%s: null argument", who);
     if (ld_dy < cols || ld_x < cols || (dx && ld_dx < cols)) return set_error(SK_EINVAL, "%s: a leading dimension is below cols", who);
+    if (rows > 1 && ((dx == x && ld_dx != ld_x) || (dx == dy && ld_dx != ld_dy)))
+        return set_error(SK_EINVAL, "%s: in place, the leading dimensions must be the same", who);
     if (!dx && !dweight && !dbias) return SK_OK;
     OpDevice dev;
     if (int rc = op_device(&dev)) return rc;
@@ -193,6 +196,7 @@ int sk_linear_cross_entropy_backward(const float* dloss, const void* hidden, uin
         return SK_OK;
     }
     if (!dhidden && !dweight) return SK_OK;
+    if (dweight == weight || dhidden == weight) return set_error(SK_EINVAL, "%s: weight's memory cannot take a gradient in place", who);
     if (int rc = check_workspace(who, workspace, workspace_bytes, head_backward_workspace(a))) return rc;
     OpDevice dev;
     if (int rc = op_device(&dev)) return rc;
