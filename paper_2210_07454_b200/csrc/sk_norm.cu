@@ -9,7 +9,7 @@
 // it): the next rows travel while one is worked on, without holding registers.  Rows of odd lengths do so too, with accesses
 // that begin before the row (Place); only matrices whose rows lie differently to the 16-byte boundary come element by element,
 // 16-bit ones through registers.  The arithmetic is two values to an instruction (f32x2): with one the kernels are bound by
-// issue (bf16 rows then take as long as fp32 ones).  Measured: 32768 x 4096 bf16 87 us forward (6.15 TB/s), 141 us backward (5.7);
+// issue (bf16 rows then take as long as fp32 ones).  Measured: 32768 x 4096 bf16 90 us forward (5.9 TB/s), 141 us backward (5.7);
 // 32768 x 4096 fp32 166 and 244 us (6.5, 6.6 TB/s); weights read for every row from L1 instead of registers cost 274 us in the first.
 //
 // Statistics: a warp computes the mean of its part and the squares around that, and the parts are joined by the formula for

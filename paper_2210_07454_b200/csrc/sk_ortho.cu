@@ -554,7 +554,7 @@ __global__ void __launch_bounds__(256) k_ortho_scale(const __grid_constant__ Squ
 }
 
 // How the products are cut: pairs of blocks on 256 x 256 or single ones on 128 x 128, and slices of the longer side in A.  A stage takes
-// both tiles the same time (some 620 cycles, see launch_products), the pair does twice the work per SM in it.  The time is about that of
+// both tiles the same time (some 620 cycles, see wide_tiles), the pair does twice the work per SM in it.  The time is about that of
 // the work on all units, but at least that of one matrix's dependent products, whose starts and epilogues are shorter with the
 // small tile (7000 cycles, 12,000).  Slices shorten the path by their stages and add kJoinCost (256 x 1024 is slower with them: 114 us for
 // 107).  Planned for the SMs of a B200, as the workspace's size depends on it.

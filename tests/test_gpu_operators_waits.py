@@ -57,3 +57,20 @@ def test_every_wait_is_reported_once_whatever_the_stream():
         with pytest.raises(binding.SkError, match="ran out"):
             ops.sync()
         ops.sync(side)
+
+
+@pytest.mark.parametrize("batch,rows,cols", SIZES)
+def test_a_withheld_signal_ends_in_an_error_where_every_matrix_is_a_pair(batch, rows, cols):
+    """fp16 outputs have kernels of their own."""
+    from paper_2210_07454_b200 import binding, operators as ops
+    u = torch.randn(batch, rows, cols, generator=torch.Generator(device="cuda").manual_seed(cols), device="cuda").half()
+    want = ops.orthogonalize(u)
+    ops.sync()
+    binding._check(binding.lib().sk_test_operators_wait(100))
+    start = time.monotonic()
+    ops.orthogonalize(u)
+    with pytest.raises(binding.SkError, match="ran out"):
+        ops.sync()
+    assert 0.1 <= time.monotonic() - start < 2.0
+    assert torch.equal(ops.orthogonalize(u), want)
+    ops.sync()
