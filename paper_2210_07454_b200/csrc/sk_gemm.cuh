@@ -12,6 +12,10 @@
 // with less shared memory for the ring: 67 against 63 us for the gradient of 8 x 50257 x 768).  Two
 // accumulators in tensor memory take turns, so the next tile's products run while this tile's epilogue does.
 //
+// The tensor cores truncate what they add to an accumulator: a sum of 4096 bf16 products of one sign comes out 1.1e-5 too small, one of 256 by 3e-7.
+// Where an epilogue needs its sums to 32 bits (kParts), a tile's products are cut along K and the accumulators take turns part by part: the
+// epilogue adds the parts up in registers, with rounding.
+//
 // Every wait has a limit (Waits).  A role whose wait runs out counts it and leaves its loop: it waits for nothing
 // more but what it has set going itself (copies, matrix instructions), once and with the same limit.  The others follow when their
 // own waits, begun at most a tile later, run out.  So the kernel ends within about two limits, and the host reads an error instead of hanging.
@@ -36,6 +40,7 @@ struct TileJob {
     uint32_t M, N;                            // extents of the output
     uint32_t m, n, b, slice;                  // the tile: row, column, matrix, slice of K
     uint32_t kind, step;                      // which product: for the epilogue
+    uint32_t part;                            // stages to an accumulation, for epilogues with kParts
     uint32_t k_stages, pass;                  // stages (none: begin() does it all); the first `pass` of them over a and b, the next over a2 and b2, a3 and b3
     int k_first, z;                           // first k, matrix of the operands
     uint32_t a_mn, b_mn;                      // 1: MN-major
@@ -64,6 +69,15 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
     asm volatile(
         "{\n\t.reg .pred p;\n\t"
         "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+__device__ __forceinline__ bool mbar_test(uint32_t bar, uint32_t parity) {      // does not suspend the thread: cheaper where it is ready
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
         "selp.u32 %0, 1, 0, p;\n\t}"
         : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
     return ok != 0;
@@ -192,7 +206,7 @@ struct GemmGroup {
     uint32_t slices;                          // of K: slice s writes a result of its own
     uint32_t tiles_m, tiles_n, tiles;
     uint32_t band;                            // tiles are walked in bands of this many tile rows, row index fastest
-    uint32_t a_mn, b_mn, a_rows, k_rows, bf16;
+    uint32_t a_mn, b_mn, a_rows, k_rows, bf16, part;
 };
 // The product with the longer tiles is the first.  Each of the `units` (blocks or pairs) takes the first's tiles in turn; `early` is how
 // many rounds of the second's tiles the units that got one tile less of the first are ahead.
@@ -236,6 +250,7 @@ struct GemmPlan {
         j.a_rows = s.a_rows;
         j.k_rows = s.k_rows;
         j.bf16 = s.bf16;
+        j.part = s.part;
         j.map_a = j.map_a2 = &map[2 * group];
         j.map_b = j.map_b2 = &map[2 * group + 1];
         return true;
@@ -260,7 +275,7 @@ struct GemmTile {
 // Plan: job(unit, units, i, job): the unit's i-th tile; wait(job): until its operands are there; done(job): called by every epilogue warp
 // when its share of the tile is written.
 // Epi: struct Args; __device__ Epi(const Args&, job, row, part, shared address of the warp's memory); begin(plan, first column) before the
-// accumulator is waited for, false (in the whole warp) if a wait of its own ran out; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
+// accumulator is waited for, false (in the whole warp) if a wait of its own ran out; kParts: see above; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
 // row of the tile and gets its columns 32 at a time; the kWarps / 4 warps that share a row take a part of the columns each.  Rows >= M
 // are passed too (the epilogue skips them: all lanes of a warp stay together), columns >= N may be.
 template <int CG, int BN, class Plan, class Epi>
@@ -365,44 +380,81 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
         }
     } else if (warp == 1) {
         if (lane == 0 && rank == 0) {
-            uint32_t s = 0, parity = 0, n = 0;
+            uint32_t s = 0, parity = 0, m = 0;                   // m: accumulations so far
             bool ok = true;
-            for (; ok && plan.job(unit, units, n, t); ++n) {
-                const uint32_t kb = t.k_stages, a = n & 1, steps = t.k_rows / 16, d = tmem + a * BN;
+            for (uint32_t n = 0; ok && plan.job(unit, units, n, t); ++n) {
+                const uint32_t kb = t.k_stages, steps = t.k_rows / 16, most = Epi::kParts ? t.part : kb;
                 // D fp32; A, B bf16 or fp16; majors; N / 8; M / 16
                 const uint32_t idesc = (1u << 4) | (t.bf16 << 7) | (t.bf16 << 10) | (t.a_mn << 15) | (t.b_mn << 16) |
                                        ((uint32_t)(BN / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
                 const uint64_t step_a = (t.a_mn ? 2048u : 32u) >> 4, step_b = (t.b_mn ? 2048u : 32u) >> 4;
                 const uint64_t desc_a = smem_desc(stages, t.a_mn), desc_b = smem_desc(stages + kBytesA, t.b_mn);
-                if (n >= 2 && !(ok = mbar_wait(acc_empty(a), ((n >> 1) - 1) & 1, plan.waits))) break;
-                asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                for (uint32_t k = 0; k < kb; ++k) {
-                    if (!(ok = mbar_wait(full(s), parity, plan.waits))) break;
+                uint32_t from = 0;
+                do {
+                    const uint32_t a = m & 1, d = tmem + a * BN, stages_here = Epi::kParts ? min(kb - from, most) : kb;
+                    if (m >= 2 && !(Epi::kParts && mbar_test(acc_empty(a), ((m >> 1) - 1) & 1)) &&
+                        !(ok = mbar_wait(acc_empty(a), ((m >> 1) - 1) & 1, plan.waits))) break;
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-                    const uint64_t da = desc_a + s * (kBytes >> 4), db = desc_b + s * (kBytes >> 4);
-                    if (steps == kGemmK / 16) {
+                    for (uint32_t k = 0; k < stages_here; ++k) {
+                        if (!(ok = mbar_wait(full(s), parity, plan.waits))) break;
+                        asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                        const uint64_t da = desc_a + s * (kBytes >> 4), db = desc_b + s * (kBytes >> 4);
+                        if (steps == kGemmK / 16) {
 #pragma unroll
-                        for (uint32_t q = 0; q < kGemmK / 16; ++q) mma_f16<CG>(d, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
-                    } else {
-                        for (uint32_t q = 0; q < steps; ++q) mma_f16<CG>(d, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
+                            for (uint32_t q = 0; q < kGemmK / 16; ++q) mma_f16<CG>(d, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
+                        } else {
+                            for (uint32_t q = 0; q < steps; ++q) mma_f16<CG>(d, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
+                        }
+                        mma_commit<CG>(empty(s));
+                        if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
                     }
-                    mma_commit<CG>(empty(s));
-                    if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
-                }
-                mma_commit<CG>(acc_full(a));
+                    mma_commit<CG>(acc_full(a));
+                    ++m;
+                    from += stages_here;
+                } while (Epi::kParts && ok && from < kb);
             }
-            if (!ok && n) mbar_wait(acc_full((n - 1) & 1), ((n - 1) >> 1) & 1, plan.waits);      // the products begun, which no epilogue waits for
+            if (!ok && m) mbar_wait(acc_full((m - 1) & 1), ((m - 1) >> 1) & 1, plan.waits);      // the products begun, which no epilogue waits for
         }
     } else {
         const uint32_t w = warp - 2, quarter = warp & 3, part = w >> 2;
         constexpr uint32_t kCols = BN / (Epi::kWarps / 4);           // of a warp
         const uint32_t stage = stages + kStages * kBytes + w * Epi::kWords * 4;
+        uint32_t m = 0;                                              // accumulations so far
         for (uint32_t n = 0; plan.job(unit, units, n, t); ++n) {
             const uint32_t a = n & 1;
             const uint32_t row = t.m * (128 * CG) + rank * 128 + quarter * 32 + lane;
             const uint32_t col0 = t.n * BN + part * kCols;
             Epi epi(ea, t, row, part, stage);
             if (!epi.begin(plan, col0)) break;                   // what it reads travels while the products run
+            if constexpr (Epi::kParts) {
+                float sum[kCols / 32][32];
+                bool ok = true;
+                const uint32_t kb = t.k_stages, most = t.part;
+#pragma unroll 1
+                for (uint32_t k = 0; k < kb; k += most, ++m) {
+                    const uint32_t b = m & 1;
+                    if (!(ok = mbar_wait_warp(acc_full(b), (m >> 1) & 1, plan.waits))) break;
+                    asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+                    __syncwarp();
+#pragma unroll
+                    for (uint32_t q = 0; q < kCols / 32; ++q) {
+                        float v[32];
+                        tmem_load32(tmem + b * BN + part * kCols + q * 32 + ((quarter * 32) << 16), v);
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) sum[q][i] = k == 0 ? v[i] : sum[q][i] + v[i];
+                    }
+                    asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_leader(acc_empty(b)) : acc_empty(b));
+                }
+                if (!ok) break;
+#pragma unroll
+                for (uint32_t q = 0; q < kCols / 32; ++q)
+                    if (col0 + q * 32 < t.N) epi.chunk(col0 + q * 32, sum[q], q * 32 + 32 == kCols || col0 + q * 32 + 32 >= t.N);
+                epi.end();
+                plan.done(t);
+                continue;
+            }
             if (!mbar_wait_warp(acc_full(a), (n >> 1) & 1, plan.waits)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (Plan::kEmpty && !t.k_stages) {                   // no products

@@ -189,6 +189,7 @@ struct ChainArgs {
 template <bool SLICED, bool PRECISE>
 struct ChainEpi {
     static constexpr int kWarps = 8, kWords = 2 * kStageWords;
+    static constexpr bool kParts = false;
     using Args = ChainArgs;
     const Args& e;
     const TileJob& t;

@@ -129,3 +129,40 @@ def test_linear_cross_entropy_backward_of_a_mean(tokens, vocab, width, dtype, bi
             want = want * float(dloss[0])
             assert float((got.double() - want).norm()) <= float(off.norm() * norm) * c + HEAD * float(want.norm()), c
     ops.sync()
+
+
+# The tensor cores add sixteen products and the accumulator a step, each truncated to at least 24 bits of the largest: 17 times 2^-24 of what has been added up
+# so far, at most.  For few tokens the accumulator is emptied after 256 values and the parts are added with rounding: of a sum of values of one sign,
+# (s + 1) / 2 steps' errors for the s steps of a part and (n + 1) / 2 half ulps for n parts.
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16], ids=str)
+@pytest.mark.parametrize("width", [16, 64, 100, 256, 257, 300, 768, 1000, 2048, 2500, 4096, 8192])
+def test_logits_of_few_tokens_are_sums_of_32_bits(width, dtype):
+    """With a vocabulary of one word, lse is the logit.  (One accumulation of 2500 fp16 values came out 1.6e-5 too small, one of 4096 2.7e-5.)"""
+    from paper_2210_07454_b200 import operators as ops
+    bound = 17 * 2.0 ** -24 * (min(width, 256) / 16 + 1) / 2 + 2.0 ** -24 * (math.ceil(width / 256) + 1) / 2
+    for tokens in (1, 5, 100):
+        h, w = randn(1, tokens, width).abs().to(dtype), randn(2, 1, width).abs().to(dtype)
+        z = (h.double() @ w.double().T)[:, 0]
+        lse = ops.linear_cross_entropy(h, w, torch.zeros(tokens, dtype=torch.int64, device="cuda"))[1]
+        assert float(((lse.double() - z) / z).abs().max()) <= bound
+    ops.sync()
+
+
+def test_the_loss_of_confident_tokens():
+    """Two words, whose logits are exact, large, and apart by d: the loss is log(1 + exp(-d)).  It comes from their difference, which is exact, and the
+    logarithm of a sum just above 1 (half an ulp of it, an ulp of the logarithm), with exp(-d) off by d 2^-23 (its argument's two roundings) and 2^-22.  Formed
+    from a logarithm of sums of 1000 it would be off by half an ulp of that, 3e-5."""
+    from paper_2210_07454_b200 import operators as ops
+    d = torch.arange(0.25, 12.25, 0.25, device="cuda")
+    h = torch.zeros(len(d), 64, dtype=torch.float16, device="cuda")
+    h[:, 0], h[:, 1] = 1000.0, d
+    w = torch.zeros(2, 64, dtype=torch.float16, device="cuda")
+    w[:, 0], w[1, 1] = 1.0, -1.0
+    loss, lse = ops.linear_cross_entropy(h, w, torch.zeros(len(d), dtype=torch.int64, device="cuda"))
+    d = d.double()
+    want = torch.log1p(torch.exp(-d))
+    assert bool(((loss.double() - want).abs() <= 2.0 ** -23 + 2.0 ** -23 + torch.exp(-d) * (d * 2.0 ** -23 + 2.0 ** -22)).all())
+    assert float((lse.double() - 1000 - want).abs().max()) <= 2.0 ** -14
+    second = ops.linear_cross_entropy(h, w, torch.ones(len(d), dtype=torch.int64, device="cuda"))[0]
+    assert bool(((second.double() - want - d).abs() <= 2.0 ** -22 + torch.exp(-d) * (d * 2.0 ** -23 + 2.0 ** -22) + 2.0 ** -24 * (d + want)).all())
+    ops.sync()
