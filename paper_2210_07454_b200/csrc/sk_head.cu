@@ -13,7 +13,7 @@
 // For few tokens the rounding of G shows in the gradients: one entry of a row, the target's, is much larger than the others, and its error is not
 // averaged away (1 x 3941 x 1024 bf16: 2.7e-3 for an output whose own rounding is 1.7e-3).  Up to kPairTokens tokens G is therefore the sum of two 16-bit
 // matrices, one below the other, and so are the hidden states twice: dW sums over twice the rows, and the rows of dhidden are added up in
-// pairs.  The rows fit one tile either way, and W is read no more often (8 x 50257 x 768 60 -> 65 us, 64 tokens 64 -> 73).  For more tokens that would double the products; there the rounding of
+// pairs.  The rows fit one tile either way, and W is read no more often (8 x 50257 x 768 64.3 -> 66.4 us, 64 tokens 68 -> 73).  For more tokens that would double the products; there the rounding of
 // G adds some 35 % to the error of the output's own (41 % at most, were every entry rounded by itself).
 //
 // A row whose target is negative takes no part: loss 0, gradient 0.  A target >= vocab gives a loss of NaN and no gradient.
@@ -249,19 +249,17 @@ __global__ void __launch_bounds__(256) k_head_sum(const float* sum, uint32_t sli
         const uint64_t row = q / groups;
         const uint32_t col = (uint32_t)(q - row * groups) * 4;
         const float* p = sum + row * ld_sum + col;               // ld_sum is a multiple of 32
-        float4 v = *(const float4*)p;
-        for (uint32_t s = 1; s < slices; ++s) {
+        float4 v = *(const float4*)p, u = second ? *(const float4*)(p + second) : make_float4(0, 0, 0, 0);
+#pragma unroll 4
+        for (uint32_t s = 1; s < slices; ++s) {                  // several slices' loads on their way at once
             const float4 w = *(const float4*)(p + s * stride);
             v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-        }
-        if (second) {                            // small against the first: added last
-            float4 u = *(const float4*)(p + second);
-            for (uint32_t s = 1; s < slices; ++s) {
-                const float4 w = *(const float4*)(p + second + s * stride);
-                u.x += w.x; u.y += w.y; u.z += w.z; u.w += w.w;
+            if (second) {
+                const float4 x = *(const float4*)(p + second + s * stride);
+                u.x += x.x; u.y += x.y; u.z += x.z; u.w += x.w;
             }
-            v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;
         }
+        v.x += u.x; v.y += u.y; v.z += u.z; v.w += u.w;          // small against the first: added last
         const float f[4] = {v.x * scale, v.y * scale, v.z * scale, v.w * scale};
 #pragma unroll
         for (uint32_t i = 0; i < 4; ++i)
@@ -333,10 +331,14 @@ __global__ void __launch_bounds__(256) k_head_pack(const __grid_constant__ PackA
 }
 
 // Stages of K to an accumulation of the logits, in the forward pass by single tiles: the loss of a few tokens is the difference of two logits, and
-// nothing averages what they are off.  (1 x 2424 fp16: error of the loss 2.5e-5 in one accumulation, 8e-7 so; 8 x 50257 x 768 takes 25.1 us for 23.1,
-// 27.5 with two stages.)  For batches pairs of tiles keep one accumulation, as the parts' sums do not fit their registers: 4096 x 32000 x 4096 took
-// 1080 us for 807, for an error of the losses of some 3e-7 instead of 1.5e-6 (width 2500).
-constexpr uint32_t kLogitPart = 4;
+// nothing averages what they are off.  (1 x 2424 fp16: error of the loss 2.5e-5 in one accumulation, 8e-7 so; 8 x 50257 x 768 takes 25.9 us for 24.3,
+// 27.5 with two stages.)  More tokens average it below 1e-6 up to a width of 1024 (64 x 50257 x 768 would take 29.6 us for 24.0).  For batches pairs of
+// tiles keep one accumulation at any width, as the parts' sums do not fit their registers: 4096 x 32000 x 4096 took 1080 us for 807, for an error of
+// the losses of some 3e-7 instead of 1.5e-6 (width 2500).
+constexpr uint64_t kLogitPart = 4, kPartTokens = 16, kWholeStages = 16;
+bool logits_in_parts(uint64_t tokens, uint64_t stages, bool wide) {
+    return !wide && stages > kLogitPart && (tokens <= kPartTokens || stages > kWholeStages);
+}
 
 bool addressable(const void* p, uint64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
 
@@ -455,13 +457,13 @@ int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
     const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{w, a.vocab, a.width, ld_w, 0, 1, false};
     const uint64_t stages = (a.width + kGemmK - 1) / kGemmK;
     const bool wide = wide_tiles(g.M, g.N, stages, dev.sm_count);
-    if (wide || stages <= kLogitPart) {
+    if (!logits_in_parts(a.tokens, stages, wide)) {
         const StatsEpi<false>::Args ea{part, at_target, a.targets};
         auto launch = wide ? launch_products<2, 256, StatsEpi<false>> : launch_products<1, 128, StatsEpi<false>>;
         SK_OP_CUDA(launch(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ea, dev.sm_count, st));
     } else {
         const StatsEpi<true>::Args ea{part, at_target, a.targets};
-        g.part = kLogitPart;
+        g.part = (uint32_t)kLogitPart;
         SK_OP_CUDA((launch_products<1, 128, StatsEpi<true>>(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ea, dev.sm_count, st)));
     }
     const uint32_t tile = wide ? 256 : 128, slots = 2 * ((g.N + tile - 1) / tile);
