@@ -297,8 +297,8 @@ int sk_layer_norm_backward(const void* dy, uint64_t ld_dy, const void* x, uint64
  *   lse_i = log sum_v exp z_iv;  loss_i = lse_i - z_i,targets[i].
  * hidden: tokens x width, weight: vocab x width, both of `type` (SK_BF16 or SK_F16); targets: tokens int64; loss, lse: tokens
  * fp32, either may be NULL.  A negative target takes no part (loss 0); a target >= vocab gives a loss of NaN.
- * Logits are 32-bit sums of the tensor cores, which truncate: for up to 16 tokens, and up to 128 of a width above 1024, in parts of 256 values
- * that are added with rounding, otherwise in one (relative error of the losses at width 768 4e-7, at 2500 1.5e-6).
+ * Logits are 32-bit sums of the tensor cores, which truncate, in parts of 256 values (up to 16 tokens) or 1024 that are added with
+ * rounding: the losses of a batch are off by some 5e-7 of their size.
  * vocab >= 1; tokens, vocab, width < 2^31. */
 uint64_t sk_linear_cross_entropy_workspace(const void* hidden, uint64_t ld_hidden, const void* weight, uint64_t ld_weight,
                                            uint64_t tokens, uint64_t vocab, uint64_t width);

@@ -192,6 +192,15 @@ __device__ __forceinline__ void tmem_load32(uint32_t addr, float (&v)[32]) {
     for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(r[i]);
 }
 
+__device__ __forceinline__ void tmem_load8(uint32_t addr, float (&v)[8]) {
+    uint32_t r[8];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]) : "r"(addr));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
+}
 // Shared-memory descriptor, 128-byte swizzle.  K-major: rows of 128 bytes, groups of eight rows 1024 bytes apart.
 // MN-major: blocks of 64 row indices (block_bytes from one to the next: 8192 if they are 64 k deep), groups of eight k 1024 bytes apart.
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t block_bytes = 8192) {
@@ -427,7 +436,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
             Epi epi(ea, t, row, part, stage);
             if (!epi.begin(plan, col0)) break;                   // what it reads travels while the products run
             if constexpr (Epi::kParts) {
-                float sum[kCols / 32][32];
+                float sum[kCols / 32][32] = {};                      // 128 of a thread's 168 registers with the widest tile: loads of eight
                 bool ok = true;
                 const uint32_t kb = t.k_stages, most = t.part;
 #pragma unroll 1
@@ -437,11 +446,11 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                     asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                     __syncwarp();
 #pragma unroll
-                    for (uint32_t q = 0; q < kCols / 32; ++q) {
-                        float v[32];
-                        tmem_load32(tmem + b * BN + part * kCols + q * 32 + ((quarter * 32) << 16), v);
+                    for (uint32_t q = 0; q < kCols / 8; ++q) {
+                        float v[8];
+                        tmem_load8(tmem + b * BN + part * kCols + q * 8 + ((quarter * 32) << 16), v);
 #pragma unroll
-                        for (int i = 0; i < 32; ++i) sum[q][i] = k == 0 ? v[i] : sum[q][i] + v[i];
+                        for (int i = 0; i < 8; ++i) sum[q / 4][8 * (q & 3) + i] += v[i];
                     }
                     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                     __syncwarp();

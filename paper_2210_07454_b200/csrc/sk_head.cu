@@ -330,15 +330,11 @@ __global__ void __launch_bounds__(256) k_head_pack(const __grid_constant__ PackA
     }
 }
 
-// Stages of K to an accumulation of the logits, in the forward pass by single tiles: the loss of a few tokens is the difference of two logits, and
-// nothing averages what they are off.  (1 x 2424 fp16: error of the loss 2.5e-5 in one accumulation, 8e-7 so; 8 x 50257 x 768 takes 25.9 us for 24.3,
-// 27.5 with two stages.)  More tokens average it below 1e-6 up to a width of 1024 (64 x 50257 x 768 would take 29.6 us for 24.0).  For batches pairs of
-// tiles keep one accumulation at any width, as the parts' sums do not fit their registers: 4096 x 32000 x 4096 took 1080 us for 807, for an error of
-// the losses of some 3e-7 instead of 1.5e-6 (width 2500).
-constexpr uint64_t kLogitPart = 4, kPartTokens = 16, kWholeStages = 16;
-bool logits_in_parts(uint64_t tokens, uint64_t stages, bool wide) {
-    return !wide && stages > kLogitPart && (tokens <= kPartTokens || stages > kWholeStages);
-}
+// Stages of K to an accumulation of the logits in the forward pass.  The loss of a few tokens is the difference of two logits, and nothing averages
+// what they are off: up to 16 tokens take 256 values (1 x 2424 fp16: error of the loss 2.5e-5 in one accumulation, 8e-7 so; 8 x 50257 x 768 takes
+// 25.9 us for 24.2, with 128 values 27.5).  Over more tokens 1024 values keep it below 7e-7 (in one accumulation 1e-6 to 2.3e-6 at widths of 1500 to
+// 3800; 4096 x 32000 x 4096 takes 832 us for 797, 2048 x 50257 x 2048 some 2 % more).
+uint32_t logit_part(uint64_t tokens) { return tokens <= 16 ? 4 : 16; }
 
 bool addressable(const void* p, uint64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
 
@@ -457,14 +453,15 @@ int launch_head(const HeadArgs& a, const OpDevice& dev, cudaStream_t st) {
     const Operand oh{h, a.tokens, a.width, ld_h, 0, 1, false}, ow{w, a.vocab, a.width, ld_w, 0, 1, false};
     const uint64_t stages = (a.width + kGemmK - 1) / kGemmK;
     const bool wide = wide_tiles(g.M, g.N, stages, dev.sm_count);
-    if (!logits_in_parts(a.tokens, stages, wide)) {
+    g.part = logit_part(a.tokens);
+    if (stages <= g.part) {
         const StatsEpi<false>::Args ea{part, at_target, a.targets};
         auto launch = wide ? launch_products<2, 256, StatsEpi<false>> : launch_products<1, 128, StatsEpi<false>>;
         SK_OP_CUDA(launch(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ea, dev.sm_count, st));
     } else {
         const StatsEpi<true>::Args ea{part, at_target, a.targets};
-        g.part = (uint32_t)kLogitPart;
-        SK_OP_CUDA((launch_products<1, 128, StatsEpi<true>>(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ea, dev.sm_count, st)));
+        auto launch = wide ? launch_products<2, 256, StatsEpi<true>> : launch_products<1, 128, StatsEpi<true>>;
+        SK_OP_CUDA(launch(true, oh, ow, g, 1, nullptr, nullptr, nullptr, dev.waits(), ea, dev.sm_count, st));
     }
     const uint32_t tile = wide ? 256 : 128, slots = 2 * ((g.N + tile - 1) / tile);
     SK_OP_CUDA(launch_kernel(true, k_head_join, dim3((g.M + 7) / 8), kJoinThreads, 0, st, (const float2*)part, (const float*)at_target, a.targets, g.M,
