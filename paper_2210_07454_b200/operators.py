@@ -134,10 +134,8 @@ def _run(device, fn, *args):
             _check(fn(*args))
 
 
-def _size(device, fn, *args):
-    """A workspace's size, which may depend on the device."""
-    if _current_device() == device:
-        return fn(*args)
+def _elsewhere(device, fn, *args):
+    """What a function of the library (a workspace's size) gives for a device that is not current."""
     with torch.cuda.device(device):
         return fn(*args)
 
@@ -213,7 +211,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5, out=None, stream=None):
         rstd = torch.empty_like(mean)
     _run(device, lib().sk_layer_norm, x.data_ptr(), ld, y.data_ptr(), ld_y, code, rows, cols, pw, pb, wcode, eps, mean.data_ptr(), rstd.data_ptr(),
          _raw_stream(device))
-    _wrote(out)
+    if out is not None:
+        _wrote(out)
     return y, mean, rstd
 
 
@@ -222,7 +221,7 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=
     weight's type (fp32 without a weight).  ``dx``, ``dweight``, ``dbias``: tensors to write into, False to leave one out."""
     if stream is not None:
         return _on(stream, lambda: layer_norm_backward(dy, x, weight, mean, rstd, dx, dweight, dbias), dy, x, weight, mean, rstd, dx, dweight, dbias)
-    given_outputs = dx, dweight, dbias
+    given_outputs = None if dx is None and dweight is None and dbias is None else (dx, dweight, dbias)
     code = _tensor(x, "x", _TYPES)
     device, cols = x.get_device(), x.shape[-1] if x.dim() else 0
     if _tensor(dy, "dy", _TYPES, device) != code:
@@ -261,11 +260,15 @@ def layer_norm_backward(dy, x, weight, mean, rstd, dx=None, dweight=None, dbias=
         pdb = _vector(dbias, "dbias", cols, _TYPES, device)
         if dbias.dtype != dtype:
             raise SkError(f"dbias has type {dbias.dtype}, dweight {dtype}")
-    need = _size(device, lib().sk_layer_norm_backward_workspace, rows, cols) if rows and (pdw or pdb) else 0
+    need = 0
+    if rows and (pdw or pdb):
+        size = lib().sk_layer_norm_backward_workspace
+        need = size(rows, cols) if _current_device() == device else _elsewhere(device, size, rows, cols)
     ws = _workspace(need, device)
     _run(device, lib().sk_layer_norm_backward, dy.data_ptr(), ld_dy, x.data_ptr(), ld, pdx, ld_dx, code, rows, cols, pw, wcode, pm, pr, pdw, pdb,
          _TYPES[dtype], _p(ws), need, _raw_stream(device))
-    _wrote(*given_outputs)
+    if given_outputs:
+        _wrote(*given_outputs)
     return dx, dweight, dbias
 
 
@@ -292,7 +295,8 @@ def linear_cross_entropy(hidden, weight, targets, stream=None):
     device, code, tokens, vocab, width, ld_h, ld_w, pt = _head(hidden, weight, targets)
     loss, lse = _new((tokens,), (1,), torch.float32, device), _new((tokens,), (1,), torch.float32, device)
     ph, pw = hidden.data_ptr(), weight.data_ptr()
-    need = _size(device, lib().sk_linear_cross_entropy_workspace, ph, ld_h, pw, ld_w, tokens, vocab, width)
+    size, sizes = lib().sk_linear_cross_entropy_workspace, (ph, ld_h, pw, ld_w, tokens, vocab, width)
+    need = size(*sizes) if _current_device() == device else _elsewhere(device, size, *sizes)
     ws = _workspace(need, device)
     _run(device, lib().sk_linear_cross_entropy, ph, ld_h, pw, ld_w, code, tokens, vocab, width, pt, loss.data_ptr(), lse.data_ptr(), _p(ws), need,
          _raw_stream(device))
@@ -321,11 +325,13 @@ def linear_cross_entropy_backward(dloss, hidden, weight, targets, lse, dhidden=N
             outs.append((t, ld, tcode))
     (dh, ld_dh, type_dh), (dw, ld_dw, type_dw) = outs
     ph, pw = hidden.data_ptr(), weight.data_ptr()
-    need = _size(device, lib().sk_linear_cross_entropy_backward_workspace, ph, ld_h, pw, ld_w, tokens, vocab, width)
+    size, sizes = lib().sk_linear_cross_entropy_backward_workspace, (ph, ld_h, pw, ld_w, tokens, vocab, width)
+    need = size(*sizes) if _current_device() == device else _elsewhere(device, size, *sizes)
     ws = _workspace(need, device)
     _run(device, lib().sk_linear_cross_entropy_backward, pd, ph, ld_h, pw, ld_w, code, tokens, vocab, width, pt, pl, _p(dh), ld_dh, type_dh, _p(dw),
          ld_dw, type_dw, _p(ws), need, _raw_stream(device))
-    _wrote(dhidden, dweight)
+    if dhidden is not None or dweight is not None:
+        _wrote(dhidden, dweight)
     return dh, dw
 
 
@@ -362,11 +368,13 @@ def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coef
         out = _new_like(update, torch.float16 if update.dtype == torch.float16 else torch.bfloat16, device)
     po, ld_o, s_o, out_code = _batch_of(out, "out", update, _HALF, device)
     batch, (rows, cols) = (update.shape[0] if update.dim() == 3 else 1), update.shape[-2:]
-    need = _size(device, lib().sk_orthogonalize_workspace, batch, rows, cols)
+    size = lib().sk_orthogonalize_workspace
+    need = size(batch, rows, cols) if _current_device() == device else _elsewhere(device, size, batch, rows, cols)
     ws = _workspace(need, device)
     _run(device, lib().sk_orthogonalize, pu, ld_u, s_u, code, pm, ld_m, s_m, beta, int(nesterov), po, ld_o, s_o, out_code, batch, rows, cols, steps,
          (C.c_float * 3)(*coefficients), eps, _p(ws), need, _raw_stream(device))
-    _wrote(momentum, given_out)
+    if momentum is not None or given_out is not None:
+        _wrote(momentum, given_out)
     return out
 
 
