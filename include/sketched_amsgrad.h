@@ -339,6 +339,68 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
                      uint64_t stride_out, int out_type, uint64_t batch, uint64_t rows, uint64_t cols, int steps,
                      const float* coefficients, float eps, void* workspace, uint64_t workspace_bytes, void* stream);
 
+/* The products of a layer of experts.  Group g is the rows offsets[g] .. offsets[g + 1] - 1 of x (a group may be empty), matrix g is weight's g-th:
+ *   y_i = W_g x_i  for the rows i of group g.
+ * x: rows x width, weight: groups matrices of out x width, y: rows x out, all of `type` (SK_BF16 or SK_F16); stride_weight: elements from one matrix
+ * to the next.  offsets: groups + 1 int64 on the DEVICE, not decreasing, within 0..rows (what is not is taken as the nearest that is, never as an
+ * address).  Rows of no group (before offsets[0], from offsets[groups] on): zero if fill, else left as they were.
+ * Sums are the tensor cores' 32-bit ones.  1 <= groups <= 2048; rows <= 2^30; 1 <= width, out <= 2^20.  y may not be x or weight. */
+uint64_t sk_grouped_linear_workspace(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight,
+                                     uint64_t rows, uint64_t groups, uint64_t width, uint64_t out);
+int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight, int type, uint64_t rows,
+                      uint64_t groups, uint64_t width, uint64_t out, const int64_t* offsets, void* y, uint64_t ld_y, int fill, void* workspace,
+                      uint64_t workspace_bytes, void* stream);
+
+/* Its gradients: dx_i = W_g^T dy_i (rows of no group: as for y), dweight_g = sum over the rows of group g of dy_i x_i^T (zero for an empty group).
+ * dy: rows x out, dx: rows x width, of `type`; dweight: groups matrices of out x width, of `type` or SK_F32, stride_dweight apart (it may be a
+ * slice of the gradient array of sk_step); dx and dweight may be NULL.  For SK_F32 and fp16 dweight is added up in parts of 1024 rows with rounding
+ * between them; for bf16 in the tensor cores' accumulators alone, whose truncation stays below its rounding.  No output may be an input. */
+uint64_t sk_grouped_linear_backward_workspace(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight,
+                                              uint64_t ld_weight, uint64_t stride_weight, uint64_t rows, uint64_t groups, uint64_t width,
+                                              uint64_t out);
+int sk_grouped_linear_backward(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight,
+                               uint64_t stride_weight, int type, uint64_t rows, uint64_t groups, uint64_t width, uint64_t out,
+                               const int64_t* offsets, void* dx, uint64_t ld_dx, int fill, void* dweight, uint64_t ld_dweight,
+                               uint64_t stride_dweight, int dweight_type, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* What brings the rows of x into that order: n assignments of something to an expert (experts: int32 or int64, by expert_bits), sorted by
+ * expert, equal ones in the order they have; those outside 0..groups-1 come last.  order[j] is the assignment at place j, places its inverse,
+ * offsets[g] the number of assignments to experts below g (groups + 1 values).  order or places may be NULL.  n < 2^31; 1 <= groups <= 2048. */
+uint64_t sk_sort_by_expert_workspace(uint64_t n, uint64_t groups);
+int sk_sort_by_expert(const void* experts, int expert_bits, uint64_t n, uint64_t groups, int64_t* order, int64_t* places, int64_t* offsets,
+                      void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Dropout whose mask is a function of the seed and of a value's number i = row cols + column, so that it is never stored:
+ *   y_i = residual_i + (f_i >= T ? x_i 65536 / (65536 - T) : 0),  T = 65536 p rounded to a whole number (half to even)
+ * where f_i is bits 16 (i mod 4) to 16 (i mod 4) + 15 of output number (i div 4) + 1 of splitmix64 started at K, and K its first
+ * output when started at the seed.  The seed is *seed_at (DEVICE, read when the kernel runs: a captured call may be replayed with another) or,
+ * where seed_at is NULL, `seed`.  The gradient with respect to x is the same call on dy, without the residual, whose gradient is dy.
+ * x, residual, y: rows x cols of `type`; residual may be NULL (0).  What x holds in a dropped place (infinities and NaN too) does not matter.
+ * y may be x or residual, with the same ld.  0 <= p <= 1. */
+int sk_dropout(const void* x, uint64_t ld_x, const void* residual, uint64_t ld_residual, void* y, uint64_t ld_y, int type, uint64_t rows,
+               uint64_t cols, double p, uint64_t seed, const uint64_t* seed_at, void* stream);
+
+/* The clipped policy loss with a KL term, over the losses that sk_linear_cross_entropy gives (nll: of the policy that is trained, old_nll: of
+ * the one that drew the tokens, reference_nll: of one it is to stay close to; NULL = none).  Per token, with r = exp(old_nll - nll):
+ *   s = A min(r, 1 + clip_high) for A >= 0, A max(r, 1 - clip_low) for A < 0;  e = nll - reference_nll;  k = exp(e) - e - 1;
+ *   token loss = -s + kl k.
+ * tokens fp32 each; advantages A: one for each token or, if advantage_of_sequences, for each sequence.  Tokens with a negative target take no
+ * part (targets may be NULL: all do), whatever their other values are.  offsets: sequences + 1 int64 on the DEVICE, not decreasing; sequence q is
+ * tokens offsets[q] .. offsets[q + 1] - 1, tokens of no sequence take no part; NULL: one sequence of all tokens (sequences = 1).
+ * norm (sequences fp32 out): what a token of the sequence counts: 1 / (tokens that take part), or, if average_sequences, 1 / (sequences with such
+ * a token) / (such tokens of this sequence); 0 where there is none.  result (3 fp32 out): the sums over the tokens of norm times the token
+ * loss (the loss), k, and 1 where the ratio is clipped.  Sums in a fixed order (same bits every time), in 64 bits beyond eight tokens. */
+uint64_t sk_policy_loss_workspace(uint64_t tokens, uint64_t sequences);
+int sk_policy_loss(const float* nll, const float* old_nll, const float* advantages, int advantage_of_sequences, const int64_t* targets,
+                   const int64_t* offsets, uint64_t sequences, const float* reference_nll, uint64_t tokens, double clip_low, double clip_high,
+                   double kl, int average_sequences, float* result, float* norm, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Its gradient, with the norm of the forward pass: dnll = dloss norm ([not clipped] A r + kl (exp(e) - 1)), 0 for tokens that take no part: what
+ * sk_linear_cross_entropy_backward takes as dloss.  dloss: one fp32 on the DEVICE, or NULL (1).  dnll may be any of the tokens' fp32 inputs. */
+int sk_policy_loss_backward(const float* dloss, const float* nll, const float* old_nll, const float* advantages, int advantage_of_sequences,
+                            const int64_t* targets, const int64_t* offsets, uint64_t sequences, const float* reference_nll, uint64_t tokens,
+                            double clip_low, double clip_high, double kl, const float* norm, float* dnll, void* stream);
+
 /* Waits for the stream and reports waits inside operators' kernels that have run out on the current device, in any stream, since the
  * last report (SK_EDEVICE with a message: such a kernel's outputs are invalid).  Each is reported once. */
 int sk_operators_sync(void* stream);

@@ -20,7 +20,9 @@ EXPORTS = ["sk_create", "sk_step", "sk_set_lr", "sk_step_host", "sk_step_host_sp
            "sk_get_stats", "sk_test_fail_allocation", "sk_debug_check", "sk_layer_norm", "sk_layer_norm_backward",
            "sk_layer_norm_backward_workspace", "sk_linear_cross_entropy", "sk_linear_cross_entropy_workspace",
            "sk_linear_cross_entropy_backward", "sk_linear_cross_entropy_backward_workspace", "sk_orthogonalize",
-           "sk_orthogonalize_workspace", "sk_operators_sync", "sk_test_operators_wait"]
+           "sk_orthogonalize_workspace", "sk_grouped_linear", "sk_grouped_linear_workspace", "sk_grouped_linear_backward",
+           "sk_grouped_linear_backward_workspace", "sk_sort_by_expert", "sk_sort_by_expert_workspace", "sk_dropout", "sk_policy_loss",
+           "sk_policy_loss_workspace", "sk_policy_loss_backward", "sk_operators_sync", "sk_test_operators_wait"]
 NUM_STATS = 6
 STAT_NAMES = ["threshold", "threshold_bin_count", "tie_group_count", "emitted", "floats_on_the_wire", "status"]
 STATIC_MAX_D = 262144
@@ -83,6 +85,22 @@ def lib() -> C.CDLL:
         L.sk_orthogonalize_workspace.restype = u64; L.sk_orthogonalize_workspace.argtypes = [u64, u64, u64]
         L.sk_orthogonalize.restype = ci
         L.sk_orthogonalize.argtypes = [vp, u64, u64, ci, vp, u64, u64, f32, ci, vp, u64, u64, ci, u64, u64, u64, ci, vp, f32, vp, u64, vp]
+        f64 = C.c_double
+        L.sk_grouped_linear_workspace.restype = u64; L.sk_grouped_linear_workspace.argtypes = [vp, u64, vp, u64, u64, u64, u64, u64, u64]
+        L.sk_grouped_linear.restype = ci
+        L.sk_grouped_linear.argtypes = [vp, u64, vp, u64, u64, ci, u64, u64, u64, u64, vp, vp, u64, ci, vp, u64, vp]
+        L.sk_grouped_linear_backward_workspace.restype = u64
+        L.sk_grouped_linear_backward_workspace.argtypes = [vp, u64, vp, u64, vp, u64, u64, u64, u64, u64, u64]
+        L.sk_grouped_linear_backward.restype = ci
+        L.sk_grouped_linear_backward.argtypes = [vp, u64, vp, u64, vp, u64, u64, ci, u64, u64, u64, u64, vp, vp, u64, ci, vp, u64, u64, ci, vp, u64, vp]
+        L.sk_sort_by_expert_workspace.restype = u64; L.sk_sort_by_expert_workspace.argtypes = [u64, u64]
+        L.sk_sort_by_expert.restype = ci; L.sk_sort_by_expert.argtypes = [vp, ci, u64, u64, vp, vp, vp, vp, u64, vp]
+        L.sk_dropout.restype = ci; L.sk_dropout.argtypes = [vp, u64, vp, u64, vp, u64, ci, u64, u64, f64, u64, vp, vp]
+        L.sk_policy_loss_workspace.restype = u64; L.sk_policy_loss_workspace.argtypes = [u64, u64]
+        L.sk_policy_loss.restype = ci
+        L.sk_policy_loss.argtypes = [vp, vp, vp, ci, vp, vp, u64, vp, u64, f64, f64, f64, ci, vp, vp, vp, u64, vp]
+        L.sk_policy_loss_backward.restype = ci
+        L.sk_policy_loss_backward.argtypes = [vp, vp, vp, vp, ci, vp, vp, u64, vp, u64, f64, f64, f64, vp, vp, vp]
         L.sk_operators_sync.restype = ci; L.sk_operators_sync.argtypes = [vp]
         L.sk_test_operators_wait.restype = ci; L.sk_test_operators_wait.argtypes = [C.c_uint32]
         L.sk_last_error.restype = C.c_char_p; L.sk_last_error.argtypes = []

@@ -18,7 +18,8 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libsketched_amsgrad.so")
 LIB_DEBUG = os.path.join(HERE, "libsketched_amsgrad_debug.so")    # device-side bounds checks compiled in
 SOURCES = ["sk_api.cu", "sk_sketch.cu", "sk_sketch_own.cu", "sk_select.cu", "sk_static.cu", "sk_shard.cu",
-           "sk_operators.cu", "sk_norm.cu", "sk_head.cu", "sk_ortho.cu"]
+           "sk_operators.cu", "sk_norm.cu", "sk_head.cu", "sk_ortho.cu",
+           "sk_grouped.cu", "sk_sort.cu", "sk_dropout.cu", "sk_policy.cu"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo",
               "-Xcompiler", "-fPIC"]
 

@@ -26,6 +26,7 @@
 #include <cuda_runtime.h>
 #include <atomic>
 #include <cstdint>
+#include <type_traits>
 
 #include "sk_chain.cuh"
 #include "sk_operators.h"
@@ -48,6 +49,14 @@ struct TileJob {
     uint32_t k_rows;                          // values of k in a stage: 64, or fewer where K has no more (in steps of 16)
     uint32_t bf16;                            // operand type: 1 bf16, 0 fp16
     const CUtensorMap *map_a, *map_b, *map_a2, *map_b2, *map_a3, *map_b3;
+};
+
+// Of a ragged plan, whose tiles differ in their columns and in the rows of their last stage
+struct RaggedJob : TileJob {
+    uint32_t cols;                            // columns of the matrix instruction: a multiple of 16, at most BN
+    uint32_t last_rows;                       // values of k in the last stage, rounded up to 16
+    uint32_t last_valid;                      // and those that are the tile's
+    uint32_t first;                           // first row of the ragged side
 };
 
 // ---- instruction wrappers -------------------------------------------------------------------------------------------
@@ -225,6 +234,7 @@ struct GemmPlan {
     uint32_t groups, early;
     Waits waits;
     static constexpr bool kCooperative = false, kEmpty = false, kThree = false;      // kThree: a third pair of operands
+    static constexpr bool kRagged = false;
 
     __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, TileJob& j) const {
         uint32_t t = p + i * units, group = 0;
@@ -282,7 +292,8 @@ struct GemmTile {
 };
 
 // Plan: job(unit, units, i, job): the unit's i-th tile; wait(job): until its operands are there; done(job): called by every epilogue warp
-// when its share of the tile is written.
+// when its share of the tile is written.  kRagged: the tiles depend on data; prepare(shared address of all epilogue warps' memory) is called once by the
+// whole block before the first job(), load(job, k, ...) issues the copies of a stage, stage_bytes(job, k) says what they bring to a block.
 // Epi: struct Args; __device__ Epi(const Args&, job, row, part, shared address of the warp's memory); begin(plan, first column) before the
 // accumulator is waited for, false (in the whole warp) if a wait of its own ran out; kParts: see above; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
 // row of the tile and gets its columns 32 at a time; the kWarps / 4 warps that share a row take a part of the columns each.  Rows >= M
@@ -328,16 +339,33 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
     chain_release();
 
     const uint32_t unit = blockIdx.x / CG, units = gridDim.x / CG;
-    TileJob t;
+    std::conditional_t<Plan::kRagged, RaggedJob, TileJob> t;
+    constexpr uint32_t kBytes = kBytesA + kBytesB;
+    if constexpr (Plan::kRagged) {
+        plan.prepare(smem_raw + (stages - smem_u32(smem_raw)) + kStages * kBytes);
+        __syncthreads();
+    }
 
     // The two single threads that feed the tensor cores have a stage's time, some 600 cycles, for each trip of their loops: what is constant
     // over a tile is in registers, and the ring's slot and its parity go round without divisions.
-    constexpr uint32_t kBytes = kBytesA + kBytesB;
     if (warp == 0) {
         if (lane == 0) {
             uint32_t s = 0, parity = 1;                          // a fresh barrier counts as having completed its previous phase
             bool ok = true, any = false;
             for (uint32_t i = 0; ok && plan.job(unit, units, i, t); ++i) {
+                if constexpr (Plan::kRagged) {
+                    any = true;
+                    for (uint32_t k = 0; k < t.k_stages; ++k) {
+                        if (!(ok = mbar_wait(empty(s), parity, plan.waits))) break;
+                        const uint32_t sa = stages + s * kBytes, bytes = CG * plan.template stage_bytes<kRowsB>(t, k);
+                        uint32_t bar = full(s);
+                        if (rank == 0) mbar_expect(bar, bytes);
+                        if constexpr (CG == 2) bar = map_to_leader(bar);
+                        plan.template load<CG, kRowsB>(t, k, rank, sa, sa + kBytesA, bar);
+                        if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
+                    }
+                    continue;
+                }
                 if (!(ok = plan.wait(t))) break;
                 const uint32_t kb = t.k_stages, pass = t.pass;
                 const bool a_mn = t.a_mn, b_mn = t.b_mn;
@@ -392,10 +420,15 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
             uint32_t s = 0, parity = 0, m = 0;                   // m: accumulations so far
             bool ok = true;
             for (uint32_t n = 0; ok && plan.job(unit, units, n, t); ++n) {
-                const uint32_t kb = t.k_stages, steps = t.k_rows / 16, most = Epi::kParts ? t.part : kb;
+                const uint32_t kb = t.k_stages, most = Epi::kParts ? t.part : kb;
+                uint32_t steps = t.k_rows / 16, columns = BN;
+                if constexpr (Plan::kRagged) {
+                    if (!kb) continue;                           // nothing to add up, no accumulator taken
+                    columns = t.cols;
+                }
                 // D fp32; A, B bf16 or fp16; majors; N / 8; M / 16
                 const uint32_t idesc = (1u << 4) | (t.bf16 << 7) | (t.bf16 << 10) | (t.a_mn << 15) | (t.b_mn << 16) |
-                                       ((uint32_t)(BN / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
+                                       ((columns / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
                 const uint64_t step_a = (t.a_mn ? 2048u : 32u) >> 4, step_b = (t.b_mn ? 2048u : 32u) >> 4;
                 const uint64_t desc_a = smem_desc(stages, t.a_mn), desc_b = smem_desc(stages + kBytesA, t.b_mn);
                 uint32_t from = 0;
@@ -408,6 +441,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                         if (!(ok = mbar_wait(full(s), parity, plan.waits))) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint64_t da = desc_a + s * (kBytes >> 4), db = desc_b + s * (kBytes >> 4);
+                        if constexpr (Plan::kRagged) steps = from + k + 1 == kb ? t.last_rows / 16 : kGemmK / 16;
                         if (steps == kGemmK / 16) {
 #pragma unroll
                             for (uint32_t q = 0; q < kGemmK / 16; ++q) mma_f16<CG>(d, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
@@ -429,12 +463,25 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
         constexpr uint32_t kCols = BN / (Epi::kWarps / 4);           // of a warp
         const uint32_t stage = stages + kStages * kBytes + w * Epi::kWords * 4;
         uint32_t m = 0;                                              // accumulations so far
+        uint32_t taken = 0;                                          // accumulators so far, of a ragged plan
         for (uint32_t n = 0; plan.job(unit, units, n, t); ++n) {
-            const uint32_t a = n & 1;
+            const uint32_t turn = Plan::kRagged ? taken : n, a = turn & 1;
             const uint32_t row = t.m * (128 * CG) + rank * 128 + quarter * 32 + lane;
             const uint32_t col0 = t.n * BN + part * kCols;
             Epi epi(ea, t, row, part, stage);
             if (!epi.begin(plan, col0)) break;                   // what it reads travels while the products run
+            if constexpr (Plan::kRagged) {
+                if (!t.k_stages) {                               // a sum over nothing
+                    float v[32] = {};
+#pragma unroll 1
+                    for (uint32_t c = 0; c < kCols; c += 32) {
+                        const uint32_t col = Epi::column(t, part, c, kCols, BN);
+                        if (col < t.N) epi.chunk(col, v, c + 32 == kCols || Epi::column(t, part, c + 32, kCols, BN) >= t.N);
+                    }
+                    continue;
+                }
+                ++taken;
+            }
             if constexpr (Epi::kParts) {
                 float sum[kCols / 32][32] = {};                      // 128 of a thread's 168 registers with the widest tile: loads of eight
                 bool ok = true;
@@ -457,6 +504,14 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                     if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_leader(acc_empty(b)) : acc_empty(b));
                 }
                 if (!ok) break;
+                if constexpr (Plan::kRagged) {
+#pragma unroll
+                    for (uint32_t q = 0; q < kCols / 32; ++q) {
+                        const uint32_t col = Epi::column(t, part, q * 32, kCols, BN);
+                        if (col < t.N) epi.chunk(col, sum[q], q * 32 + 32 == kCols || Epi::column(t, part, q * 32 + 32, kCols, BN) >= t.N);
+                    }
+                    continue;
+                }
 #pragma unroll
                 for (uint32_t q = 0; q < kCols / 32; ++q)
                     if (col0 + q * 32 < t.N) epi.chunk(col0 + q * 32, sum[q], q * 32 + 32 == kCols || col0 + q * 32 + 32 >= t.N);
@@ -464,12 +519,31 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                 plan.done(t);
                 continue;
             }
-            if (!mbar_wait_warp(acc_full(a), (n >> 1) & 1, plan.waits)) break;
+            if (!mbar_wait_warp(acc_full(a), (turn >> 1) & 1, plan.waits)) break;
             asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
             if (Plan::kEmpty && !t.k_stages) {                   // no products
                 __syncwarp();
                 if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_leader(acc_empty(a)) : acc_empty(a));
                 plan.done(t);
+                continue;
+            }
+            if constexpr (Plan::kRagged) {
+                // interleaved or in halves, as the epilogue has it; the accumulator is free after the last columns that exist
+                bool more = true;
+#pragma unroll 1
+                for (uint32_t c = 0; more; c += 32) {
+                    const uint32_t col = Epi::column(t, part, c, kCols, BN), at = Epi::kInterleaved ? col : part * kCols + c;
+                    more = c + 32 < kCols && Epi::column(t, part, c + 32, kCols, BN) < t.N;
+                    float v[32];
+                    __syncwarp();
+                    if (col < t.N) tmem_load32(tmem + a * BN + at + ((quarter * 32) << 16), v);
+                    if (!more) {
+                        asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive_cluster(CG == 2 ? map_to_leader(acc_empty(a)) : acc_empty(a));
+                    }
+                    if (col < t.N) epi.chunk(col, v, !more);
+                }
                 continue;
             }
 #pragma unroll 1

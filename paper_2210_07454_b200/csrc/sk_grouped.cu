@@ -1,0 +1,446 @@
+// Matrix products grouped by expert: group g's rows of x (offsets[g] .. offsets[g + 1], sizes known on the device only) times matrix g.
+//
+//   y_i = W_g x_i;   dx_i = W_g^T dy_i;   dW_g = sum over the group's rows of dy_i x_i^T
+//
+// Bound by the tensor cores (2 rows width out flops a product) or, with few rows, by reading the matrices that have a row.
+//
+// y and dx: the matrix is the first operand, with 128 or 256 of the output's columns in a tile, and the rows of the group are the second, so that
+// a tile ends within 15 (31) rows of its group's end: the matrix instruction has as many columns as the tile has rows, rounded up to 16 (pairs of
+// blocks: 32), and only those rows are copied.  (With rows of x as the first operand a group of 300 rows takes two tiles of 256, of which 41 % are
+// nobody's.)  A group's rows are shared out evenly among its tiles.  The tile comes out transposed; lanes exchange values in pairs and write two
+// neighbouring columns each, 64 bytes of a row by 16 lanes.  Every block makes the list of tiles for itself, from the offsets, in shared memory.
+//
+// dW: a tile of W_g, K the group's rows.  The last stage of a group is copied in boxes of 32, 16, ... 1 rows, and what is missing to the 16
+// rows of a matrix instruction comes as zeros from behind the last row of the matrix: rows of the next group, which may hold
+// anything, never reach shared memory.
+//
+// Rows that TMA cannot address (a base off the 16-byte boundary, or rows no multiple of 16 bytes apart) are copied first.
+#include "sk_gemm.cuh"
+#include "sk_operators.h"
+
+namespace sk {
+namespace {
+
+constexpr uint32_t kSegments = kMaxGroups + 2;       // the groups, the rows before the first and behind the last
+constexpr uint32_t kTableWords = 2 * (kSegments + 1);
+
+// The group boundaries as the kernels take them: never decreasing, never outside 0..rows, whatever the offsets hold.
+__device__ __forceinline__ uint32_t bounded(int64_t v, uint32_t rows) { return v < 0 ? 0 : v > (int64_t)rows ? rows : (uint32_t)v; }
+
+// y (or dx) by tiles of BN rows of the ragged side and 128 CG columns of the output
+template <int CG, int BN>
+struct RowsPlan {
+    CUtensorMap matrix, rows_map[5];                 // boxes of 128, 64, ... 8 rows
+    const int64_t* offsets;
+    uint32_t groups, rows, features, tiles_m;        // tiles_m: of the features
+    uint32_t k_stages, last_k;                       // K is the same for all tiles
+    uint32_t mn, k_rows, bf16, fill;                 // mn: the matrix is read along its rows; fill: rows of no group become zero
+    Waits waits;
+    static constexpr bool kCooperative = false, kEmpty = false, kThree = false, kRagged = true;
+    static constexpr uint32_t kStep = 16 * CG;       // of a tile's rows: a block's own are whole groups of eight, as the swizzle has them, and more
+
+    // In shared memory: where each segment begins, and the number of tiles before it.  Segment 0 is what lies before the first group.
+    __device__ void prepare(void* memory) const {
+        uint32_t *begin = (uint32_t*)memory, *before = begin + kSegments + 1;
+        for (uint32_t g = threadIdx.x; g <= groups; g += blockDim.x) begin[g + 1] = bounded(offsets[g], rows);
+        if (threadIdx.x == 0) {
+            begin[0] = 0;
+            begin[groups + 2] = rows;
+        }
+        __syncthreads();
+        if (threadIdx.x >= 32) return;
+        const uint32_t lane = threadIdx.x, segments = groups + 2;
+        uint32_t top = 0, tiles = 0;                 // of all before this round
+        for (uint32_t at = 0; at < segments; at += 32) {
+            const uint32_t i = at + lane;
+            // the round's beginnings, made never to decrease, and the next one's first
+            uint32_t b = i <= segments ? begin[i] : rows, e = i < segments ? begin[i + 1] : rows;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t u = __shfl_up_sync(0xffffffffu, b, o), v = __shfl_up_sync(0xffffffffu, e, o);
+                if (lane >= o) { b = max(b, u); e = max(e, v); }
+            }
+            b = max(b, top);
+            e = max(e, b);
+            const bool counts = i < segments && (fill || (i > 0 && i <= groups));
+            const uint32_t mine = counts ? (e - b + BN - 1) / BN * tiles_m : 0;
+            uint32_t sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t u = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += u;
+            }
+            __syncwarp();
+            if (i < segments) {
+                begin[i] = b;
+                before[i] = tiles + sum - mine;
+            }
+            top = __shfl_sync(0xffffffffu, b, 31);
+            tiles += __shfl_sync(0xffffffffu, sum, 31);
+            __syncwarp();
+        }
+        if (lane == 0) before[segments] = tiles;
+    }
+    __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, RaggedJob& j) const {
+        const uint32_t *begin = table(), *before = begin + kSegments + 1, t = p + i * units, segments = groups + 2;
+        if (t >= before[segments]) return false;
+        uint32_t low = 0, high = segments;           // before[low] <= t < before[high]
+        while (high - low > 1) {
+            const uint32_t middle = (low + high) / 2;
+            if (before[middle] <= t) low = middle;
+            else high = middle;
+        }
+        const uint32_t from = begin[low], length = begin[low + 1] - from, q = t - before[low], tile = q / tiles_m;
+        const uint32_t count = (length + BN - 1) / BN, each = ((length + count - 1) / count + kStep - 1) & ~(kStep - 1);
+        const bool real = low > 0 && low <= groups;
+        j.M = features;
+        j.m = q - tile * tiles_m;
+        j.n = 0;
+        j.first = from + tile * each;
+        j.N = min(each, length - tile * each);
+        j.cols = (j.N + kStep - 1) & ~(kStep - 1);
+        j.z = (int)low - 1;
+        j.k_stages = real ? k_stages : 0;
+        j.last_rows = last_k;
+        j.k_rows = k_rows;
+        j.a_mn = mn;
+        j.b_mn = 0;
+        j.bf16 = bf16;
+        j.part = j.k_stages;
+        return true;
+    }
+    __device__ __forceinline__ const uint32_t* table() const {
+        extern __shared__ uint8_t smem_raw[];
+        const uint32_t base = smem_u32(smem_raw), first = ((base + 1023u) & ~1023u) - base;
+        return (const uint32_t*)(smem_raw + first + kTableOffset);
+    }
+    static constexpr uint32_t kTableOffset = (232448 - (kTableWords + 7) / 8 * 8 * 4 - 1536) / (128 * 128 + BN / CG * 128) * (128 * 128 + BN / CG * 128);
+    template <int ROWS>
+    __device__ __forceinline__ uint32_t stage_bytes(const RaggedJob& j, uint32_t) const {
+        return 128 * ((mn ? 2 * k_rows : 128) + j.cols / CG);
+    }
+    template <int G, int ROWS>
+    __device__ __forceinline__ void load(const RaggedJob& j, uint32_t k, uint32_t rank, uint32_t sa, uint32_t sb, uint32_t bar) const {
+        const int k0 = (int)(k * kGemmK), feature = (int)(j.m * (128 * CG) + rank * 128);
+        if (mn) {
+            tma_load<CG>(sa, &matrix, bar, feature, k0, j.z);
+            tma_load<CG>(sa + 8192, &matrix, bar, feature + 64, k0, j.z);
+        } else {
+            tma_load<CG>(sa, &matrix, bar, k0, feature, j.z);
+        }
+        const uint32_t mine = j.cols / CG;           // a multiple of 16: the swizzle's groups of eight rows stay whole
+        uint32_t done = 0;
+#pragma unroll
+        for (uint32_t q = 0; q < 5; ++q) {
+            const uint32_t box = 128 >> q;
+            if (mine & box) {
+                tma_load<CG>(sb + done * 128, &rows_map[q], bar, k0, (int)(j.first + rank * mine + done), 0);
+                done += box;
+            }
+        }
+    }
+    __device__ __forceinline__ bool wait(const TileJob&) const { return true; }
+    __device__ __forceinline__ void done(const TileJob&) const {}
+    __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i == 0 ? &matrix : i < 6 ? &rows_map[i - 1] : nullptr; }
+};
+
+// A thread holds an output column (a row of the transposed tile) and 32 of the group's rows.
+struct RowsEpi {
+    static constexpr int kWarps = 8, kWords = (kTableWords + 7) / 8;         // not the epilogue's: the list of tiles
+    static constexpr bool kParts = false, kInterleaved = true;
+    struct Args { uint16_t* out; uint64_t ld; uint32_t bf16, paired; };      // paired: rows start on 4-byte boundaries
+    const Args& a;
+    const RaggedJob& t;
+    uint32_t feature;
+    __device__ RowsEpi(const Args& a_, const RaggedJob& t_, uint32_t row, uint32_t, uint32_t) : a(a_), t(t_), feature(row) {}
+    template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
+    // the warps that share a column take turns, 32 rows each: of a tile of few rows both have some
+    __device__ static uint32_t column(const RaggedJob&, uint32_t part, uint32_t c, uint32_t, uint32_t) { return 2 * c + 32 * part; }
+    __device__ void chunk(uint32_t col, float (&v)[32], bool) {
+        const uint32_t odd = threadIdx.x & 1, rows = t.N - col;
+        uint16_t* o = a.out + (uint64_t)(t.first + col) * a.ld;
+        if (a.paired) {
+            const bool both = (feature | 1) < t.M, last = !both && (feature & ~1u) < t.M;      // last: the last column of an odd number
+            o += (uint64_t)odd * a.ld + (feature & ~1u);
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) {
+                const uint32_t mine = pack16(v[2 * i], v[2 * i + 1], a.bf16), other = __shfl_xor_sync(0xffffffffu, mine, 1);
+                const uint32_t word = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
+                if (2 * i + odd < rows) {
+                    uint16_t* at = o + 2 * i * a.ld;
+                    if (both) *(uint32_t*)at = word;
+                    else if (last) *at = (uint16_t)word;
+                }
+            }
+        } else if (feature < t.M) {
+#pragma unroll
+            for (uint32_t i = 0; i < 32; ++i)
+                if (i < rows) o[i * a.ld + feature] = (uint16_t)pack16(v[i], 0.0f, a.bf16);
+        }
+        __syncwarp();
+    }
+    __device__ void end() {}
+};
+
+// dW by tiles of 128 CG x BN of every matrix
+template <int CG, int BN>
+struct MatrixPlan {
+    CUtensorMap a[7], b[7];                          // dy and x, boxes of 64, 32, ... 1 rows
+    const int64_t* offsets;
+    uint32_t groups, rows, M, N, tiles_m, tiles_n, bf16, part;
+    Waits waits;
+    static constexpr bool kCooperative = false, kEmpty = false, kThree = false, kRagged = true;
+    __device__ void prepare(void*) const {}
+    __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, RaggedJob& j) const {
+        const uint32_t t = p + i * units, per = tiles_m * tiles_n, g = t / per, q = t - g * per;
+        if (g >= groups) return false;
+        const uint32_t from = bounded(offsets[g], rows), to = bounded(offsets[g + 1], rows), length = to > from ? to - from : 0;
+        j.M = M;
+        j.N = N;
+        j.n = q / tiles_m;
+        j.m = q - j.n * tiles_m;
+        j.b = g;
+        j.first = from;
+        j.cols = BN;
+        j.k_stages = (length + kGemmK - 1) / kGemmK;
+        j.last_valid = length - (j.k_stages ? j.k_stages - 1 : 0) * kGemmK;
+        j.last_rows = (j.last_valid + 15) & ~15u;
+        j.k_rows = kGemmK;
+        j.a_mn = j.b_mn = 1;
+        j.bf16 = bf16;
+        j.part = part;
+        return true;
+    }
+    template <int ROWS>
+    __device__ __forceinline__ uint32_t stage_bytes(const RaggedJob& j, uint32_t k) const {
+        return 128 * (2 + ROWS / 64) * (k + 1 == j.k_stages ? j.last_rows : kGemmK);
+    }
+    // `count` rows from `row` on (a box of 64 >> q) to row `at` of the stage
+    template <int ROWS>
+    __device__ __forceinline__ void box(const RaggedJob& j, uint32_t q, int row, uint32_t at, uint32_t rank, uint32_t sa, uint32_t sb, uint32_t bar) const {
+        const int m = (int)(j.m * (128 * CG) + rank * 128), n = (int)(j.n * BN + rank * ROWS);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) tma_load<CG>(sa + i * 8192 + at * 128, &a[q], bar, m + 64 * i, row, 0);
+#pragma unroll
+        for (int i = 0; i < ROWS / 64; ++i) tma_load<CG>(sb + i * 8192 + at * 128, &b[q], bar, n + 64 * i, row, 0);
+    }
+    template <int G, int ROWS>
+    __device__ __forceinline__ void load(const RaggedJob& j, uint32_t k, uint32_t rank, uint32_t sa, uint32_t sb, uint32_t bar) const {
+        const uint32_t row = j.first + k * kGemmK;
+        if (k + 1 < j.k_stages || j.last_valid == kGemmK) {
+            box<ROWS>(j, 0, (int)row, 0, rank, sa, sb, bar);
+            return;
+        }
+        uint32_t at = 0;
+        for (uint32_t q = 1; q < 7; ++q)             // large boxes first: each begins at a multiple of its size
+            if (j.last_valid & (64u >> q)) {
+                box<ROWS>(j, q, (int)(row + at), at, rank, sa, sb, bar);
+                at += 64u >> q;
+            }
+        for (uint32_t q = 6; at < j.last_rows; --q)  // zeros up to a multiple of 16, small boxes first
+            if (at & (64u >> q)) {
+                box<ROWS>(j, q, (int)rows, at, rank, sa, sb, bar);
+                at += 64u >> q;
+            }
+    }
+    __device__ __forceinline__ bool wait(const TileJob&) const { return true; }
+    __device__ __forceinline__ void done(const TileJob&) const {}
+    __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i < 7 ? &a[i] : i < 14 ? &b[i - 7] : nullptr; }
+};
+
+template <bool PARTS>
+struct MatrixEpi {
+    static constexpr int kWarps = 8, kWords = kStageWords;
+    static constexpr bool kParts = PARTS, kInterleaved = false;
+    struct Args { void* out; uint64_t ld, stride; int type; uint32_t align; };
+    const Args& a;
+    const RaggedJob& t;
+    uint32_t row0, rows, stage;
+    __device__ MatrixEpi(const Args& a_, const RaggedJob& t_, uint32_t row, uint32_t, uint32_t stage_)
+        : a(a_), t(t_), row0(row - (threadIdx.x & 31)), stage(stage_) { rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32; }
+    template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
+    __device__ static uint32_t column(const RaggedJob& t, uint32_t part, uint32_t c, uint32_t cols, uint32_t bn) { return t.n * bn + part * cols + c; }
+    __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
+        if (!rows) return;
+        store_tile32((uint8_t*)a.out + t.b * a.stride * type_bytes(), a.type, a.ld, row0, rows, col, t.N, v, a.align, stage, true, last);
+    }
+    __device__ void end() {}
+    __device__ uint32_t type_bytes() const { return a.type == SK_F32 ? 4 : 2; }
+};
+
+// Rows of up to three batches of matrices copied to where TMA can address them, in one launch.  A thread copies eight neighbours: eight
+// loads on their way at once, one 16-byte store.
+struct PackedOne { const uint16_t* src; uint16_t* dst; uint64_t ld, stride, rows, total; uint32_t cols, ld_dst, blocks; };      // total: rows of all matrices
+struct PackedArgs { PackedOne m[3]; };
+__global__ void __launch_bounds__(256) k_grouped_pack(const __grid_constant__ PackedArgs a) {
+    chain_acquire();
+    uint32_t block = blockIdx.x, which = 0;
+    while (block >= a.m[which].blocks) block -= a.m[which++].blocks;
+    const PackedOne& m = a.m[which];
+    const uint32_t groups = m.ld_dst / 8;
+    const uint64_t total = m.total * groups, step = (uint64_t)m.blocks * 256;
+    for (uint64_t q = block * 256ull + threadIdx.x; q < total; q += step) {
+        const uint64_t r = q / groups, z = r / m.rows;
+        const uint32_t c = (uint32_t)(q - r * groups) * 8;
+        const uint16_t* s = m.src + z * m.stride + (r - z * m.rows) * m.ld + c;
+        uint32_t e[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) e[i] = c + i < m.cols ? s[i] : 0;
+        *(uint4*)(m.dst + r * m.ld_dst + c) = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+    }
+}
+
+bool addressable(const void* p, uint64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
+
+// Copies that a call needs, and where they lie in the workspace.
+struct GroupedLayout {
+    bool pack_x, pack_w, pack_dy;
+    uint64_t ld_x, ld_w, ld_dy, off_x, off_w, off_dy, total;
+};
+GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
+    GroupedLayout l{};
+    auto take = [&](bool pack, uint64_t rows, uint64_t ld) {
+        const uint64_t at = l.total;
+        if (pack) l.total += round_up(rows * ld * 2, 256);
+        return at;
+    };
+    l.pack_x = !addressable(a.x, a.ld_x);
+    l.pack_dy = backward && !addressable(a.dy, a.ld_dy);
+    l.pack_w = !addressable(a.weight, a.ld_weight) || (a.groups > 1 && (a.stride_weight % 8 || !a.stride_weight));
+    l.ld_x = round_up(a.width, 64);                  // whole 128-byte lines for what is read by every tile
+    l.ld_dy = round_up(a.out, 64);
+    l.ld_w = round_up(a.width, 8);
+    l.off_x = take(l.pack_x, a.rows, l.ld_x);
+    l.off_dy = take(l.pack_dy, a.rows, l.ld_dy);
+    l.off_w = take(l.pack_w, a.groups * a.out, l.ld_w);
+    return l;
+}
+
+// the operands as TMA can address them
+int pack_operands(GroupedArgs& a, const GroupedLayout& l, int sm_count, cudaStream_t st) {
+    uint8_t* ws = (uint8_t*)a.workspace;
+    PackedArgs p{};
+    uint32_t n = 0, blocks = 0;
+    auto add = [&](const void*& src, uint64_t& ld, uint64_t stride, uint64_t rows, uint64_t total, uint64_t cols, uint64_t off, uint64_t ld_dst) {
+        const uint64_t want = (total * (ld_dst / 8) + 255) / 256, most = (uint64_t)sm_count * 16;
+        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, stride, rows, total, (uint32_t)cols, (uint32_t)ld_dst, (uint32_t)(want < most ? want : most)};
+        blocks += p.m[n++].blocks;
+        src = ws + off;
+        ld = ld_dst;
+    };
+    if (l.pack_x) add(a.x, a.ld_x, 0, a.rows, a.rows, a.width, l.off_x, l.ld_x);
+    if (l.pack_dy) add(a.dy, a.ld_dy, 0, a.rows, a.rows, a.out, l.off_dy, l.ld_dy);
+    if (l.pack_w) {
+        add(a.weight, a.ld_weight, a.stride_weight, a.out, a.groups * a.out, a.width, l.off_w, l.ld_w);
+        a.stride_weight = a.out * l.ld_w;
+    }
+    if (n) SK_OP_CUDA(launch_kernel(true, k_grouped_pack, dim3(blocks), 256, 0, st, p));
+    return SK_OK;
+}
+
+// Pairs of blocks or single ones for y and dx, from what the host knows: the mean number of rows of the groups that can have one.  A stage costs what
+// it brings to an SM, at 50 bytes a cycle; the constants are those of plain products (see wide_tiles).
+bool wide_rows(const GroupedArgs& a, uint64_t features, uint64_t k_stages, int sm_count) {
+    const uint64_t live = a.groups < a.rows ? a.groups : a.rows, mean = (a.rows + live - 1) / live;
+    auto last = [&](uint64_t high, uint64_t wide, uint64_t blocks, uint64_t units, uint64_t fixed) {
+        const uint64_t count = (mean + wide - 1) / wide, cols = round_up((mean + count - 1) / count, 16);
+        const uint64_t tiles = live * count * ((features + high - 1) / high), stage = (16384 + cols / blocks * 128) / 50;
+        return (tiles + units - 1) / units * k_stages * stage + fixed;
+    };
+    return last(256, 256, 2, sm_count / 2, 12000) <= last(128, 128, 1, sm_count, 7000);
+}
+
+template <int CG, int BN>
+int launch_rows(const GroupedArgs& a, const void* matrix_rows, uint64_t ld_rows, bool transposed, void* out, uint64_t ld_out, int fill, const OpDevice& dev,
+                cudaStream_t st) {
+    using Plan = RowsPlan<CG, BN>;
+    static_assert(Plan::kTableOffset == GemmTile<CG, BN, RowsEpi>::kStages * GemmTile<CG, BN, RowsEpi>::kStageBytes);
+    Plan p{};
+    const uint32_t K = (uint32_t)(transposed ? a.out : a.width);
+    const bool bf16 = a.type == SK_BF16;
+    p.offsets = a.offsets;
+    p.groups = (uint32_t)a.groups;
+    p.rows = (uint32_t)a.rows;
+    p.features = (uint32_t)(transposed ? a.width : a.out);
+    p.tiles_m = (p.features + 128 * CG - 1) / (128 * CG);
+    p.k_stages = (K + kGemmK - 1) / kGemmK;
+    p.last_k = (K - (p.k_stages - 1) * kGemmK + 15) / 16 * 16;
+    p.k_rows = K < kGemmK ? p.last_k : kGemmK;
+    p.mn = transposed;
+    p.bf16 = bf16;
+    p.fill = fill;
+    p.waits = dev.waits();
+    const Operand w{a.weight, a.out, a.width, a.ld_weight, a.stride_weight, (uint32_t)a.groups, transposed};
+    const Operand x{matrix_rows, a.rows, K, ld_rows, 0, 1, false};
+    bool ok = encode_operand(&p.matrix, w, bf16, transposed ? p.k_rows : 128);
+    for (int q = 0; q < 5; ++q) ok = ok && encode_operand(&p.rows_map[q], x, bf16, 128 >> q);
+    if (!ok) return set_error(SK_ECUDA, "%s: the tensors cannot be described to the copy engine", __func__);
+    // rows over BN of each segment, at most one tile more in each
+    const uint64_t live = (a.groups < a.rows ? a.groups : a.rows) + (fill ? 2 : 0), most = (a.rows / BN + live) * p.tiles_m, slots = (uint64_t)dev.sm_count / CG;
+    const RowsEpi::Args ea{(uint16_t*)out, ld_out, bf16, (uintptr_t)out % 4 == 0 && ld_out % 2 == 0};
+    SK_OP_CUDA((launch_plan<CG, BN, Plan, RowsEpi>(true, p, ea, (uint32_t)(most < slots ? most : slots), st)));
+    return SK_OK;
+}
+
+template <int CG, int BN, bool PARTS>
+int launch_matrices(const GroupedArgs& a, const OpDevice& dev, cudaStream_t st) {
+    using Plan = MatrixPlan<CG, BN>;
+    Plan p{};
+    const bool bf16 = a.type == SK_BF16;
+    p.offsets = a.offsets;
+    p.groups = (uint32_t)a.groups;
+    p.rows = (uint32_t)a.rows;
+    p.M = (uint32_t)a.out;
+    p.N = (uint32_t)a.width;
+    p.tiles_m = (p.M + 128 * CG - 1) / (128 * CG);
+    p.tiles_n = (p.N + BN - 1) / BN;
+    p.bf16 = bf16;
+    p.part = 16;
+    p.waits = dev.waits();
+    const Operand dy{a.dy, a.rows, a.out, a.ld_dy, 0, 1, true}, x{a.x, a.rows, a.width, a.ld_x, 0, 1, true};
+    bool ok = true;
+    for (int q = 0; q < 7; ++q) ok = ok && encode_operand(&p.a[q], dy, bf16, 64 >> q) && encode_operand(&p.b[q], x, bf16, 64 >> q);
+    if (!ok) return set_error(SK_ECUDA, "%s: the tensors cannot be described to the copy engine", __func__);
+    typename MatrixEpi<PARTS>::Args ea{a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type, 0};
+    const uint32_t by_row = row_alignment(a.dweight, a.ld_dweight, a.dweight_type), by_matrix = row_alignment(a.dweight, a.stride_dweight, a.dweight_type);
+    ea.align = a.groups > 1 && by_matrix < by_row ? by_matrix : by_row;
+    const uint64_t tiles = a.groups * p.tiles_m * p.tiles_n, slots = (uint64_t)dev.sm_count / CG;
+    SK_OP_CUDA((launch_plan<CG, BN, Plan, MatrixEpi<PARTS>>(true, p, ea, (uint32_t)(tiles < slots ? tiles : slots), st)));
+    return SK_OK;
+}
+
+bool wide_matrices(const GroupedArgs& a, int sm_count) {
+    const uint64_t stages = a.rows / a.groups / kGemmK + 1, slots = (uint64_t)sm_count;
+    auto count = [&](uint64_t t) { return a.groups * ((a.out + t - 1) / t) * ((a.width + t - 1) / t); };
+    const uint64_t wide = (count(256) + slots / 2 - 1) / (slots / 2) * (stages + kTileCost) * 620 + 12000;
+    const uint64_t small = (count(128) + slots - 1) / slots * (stages + kTileCost) * 620 + 7000;
+    return wide <= small;
+}
+
+}  // namespace
+
+uint64_t grouped_workspace(const GroupedArgs& a, bool backward) { return layout_of(a, backward).total; }
+
+int launch_grouped(GroupedArgs a, const OpDevice& dev, cudaStream_t st) {
+    const GroupedLayout l = layout_of(a, false);
+    if (int rc = pack_operands(a, l, dev.sm_count, st)) return rc;
+    auto launch = wide_rows(a, a.out, (a.width + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_rows<2, 256> : launch_rows<1, 128>;
+    return launch(a, a.x, a.ld_x, false, a.y, a.ld_y, a.fill, dev, st);
+}
+
+int launch_grouped_backward(GroupedArgs a, const OpDevice& dev, cudaStream_t st) {
+    const GroupedLayout l = layout_of(a, true);
+    if (int rc = pack_operands(a, l, dev.sm_count, st)) return rc;
+    if (a.dx) {
+        auto launch = wide_rows(a, a.width, (a.out + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_rows<2, 256> : launch_rows<1, 128>;
+        if (int rc = launch(a, a.dy, a.ld_dy, true, a.dx, a.ld_dx, a.fill, dev, st)) return rc;
+    }
+    if (!a.dweight) return SK_OK;
+    // The accumulators' truncation grows with the rows added up: 16-bit gradients of fp16 and 32-bit ones show it, bf16's rounding is coarser.
+    const bool parts = a.dweight_type == SK_F32 || a.type == SK_F16, wide = wide_matrices(a, dev.sm_count);
+    auto launch = parts ? (wide ? launch_matrices<2, 256, true> : launch_matrices<1, 128, true>)
+                        : (wide ? launch_matrices<2, 256, false> : launch_matrices<1, 128, false>);
+    return launch(a, dev, st);
+}
+
+}  // namespace sk

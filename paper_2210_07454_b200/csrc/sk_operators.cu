@@ -246,6 +246,194 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
     return launch_orthogonalize(a, dev, withhold_ms, (cudaStream_t)stream);
 }
 
+static int grouped_checked(const char* who, const GroupedArgs& a, bool backward) {
+    if (a.type != SK_BF16 && a.type != SK_F16) return set_error(SK_EINVAL, "%s: type must be SK_BF16 or SK_F16", who);
+    if (a.groups < 1 || a.groups > kMaxGroups) return set_error(SK_EINVAL, "%s: groups must be in 1..%u", who, kMaxGroups);
+    if (a.rows > (1ull << 30)) return set_error(SK_EINVAL, "%s: rows must be <= 2^30", who);
+    if (a.width < 1 || a.width > (1u << 20) || a.out < 1 || a.out > (1u << 20)) return set_error(SK_EINVAL, "%s: width and out must be in 1..2^20", who);
+    const uint64_t tile_rows = a.rows / 128 + a.groups + 2, tw = a.width / 128 + 1, to = a.out / 128 + 1;
+    if (tile_rows * (tw > to ? tw : to) >= kMaxExtent || a.groups * tw * to >= kMaxExtent) return set_error(SK_EINVAL, "%s: the product is too large", who);
+    if (a.rows && (!a.x || !a.weight || !a.offsets || (backward && !a.dy))) return set_error(SK_EINVAL, "%s: null argument", who);
+    if (a.ld_x < a.width || a.ld_weight < a.width || (backward && a.ld_dy < a.out)) return set_error(SK_EINVAL, "%s: a leading dimension is below the rows' length", who);
+    if (a.ld_x >= (1ull << 36) || a.ld_weight >= (1ull << 36) || a.ld_dy >= (1ull << 36) || a.stride_weight >= (1ull << 38))
+        return set_error(SK_EINVAL, "%s: a leading dimension or stride is too large", who);
+    if (misaligned(a.x, a.type) || misaligned(a.weight, a.type) || misaligned(a.dy, a.type) || (uintptr_t)a.offsets % 8)
+        return set_error(SK_EINVAL, "%s: a pointer is not aligned to its element", who);
+    return SK_OK;
+}
+
+uint64_t sk_grouped_linear_workspace(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight, uint64_t rows,
+                                     uint64_t groups, uint64_t width, uint64_t out) {
+    GroupedArgs a{};
+    a.x = x; a.ld_x = ld_x; a.weight = weight; a.ld_weight = ld_weight; a.stride_weight = stride_weight;
+    a.rows = rows; a.groups = groups; a.width = width; a.out = out;
+    return rows ? grouped_workspace(a, false) : 0;
+}
+
+int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight, int type, uint64_t rows, uint64_t groups,
+                      uint64_t width, uint64_t out, const int64_t* offsets, void* y, uint64_t ld_y, int fill, void* workspace, uint64_t workspace_bytes,
+                      void* stream) {
+    const char* who = "sk_grouped_linear";
+    GroupedArgs a{};
+    a.x = x; a.ld_x = ld_x; a.weight = weight; a.ld_weight = ld_weight; a.stride_weight = stride_weight;
+    a.type = type; a.rows = rows; a.groups = groups; a.width = width; a.out = out; a.offsets = offsets; a.fill = fill;
+    a.y = y; a.ld_y = ld_y; a.workspace = workspace;
+    if (int rc = grouped_checked(who, a, false)) return rc;
+    if (!rows) return SK_OK;
+    if (!y) return set_error(SK_EINVAL, "%s: null argument", who);
+    if (ld_y < out) return set_error(SK_EINVAL, "%s: a leading dimension is below the rows' length", who);
+    if (misaligned(y, type)) return set_error(SK_EINVAL, "%s: a pointer is not aligned to its element", who);
+    if (y == x || y == weight) return set_error(SK_EINVAL, "%s: the product cannot be written in place", who);
+    if (int rc = check_workspace(who, workspace, workspace_bytes, grouped_workspace(a, false))) return rc;
+    OpDevice dev;
+    if (int rc = op_device(&dev)) return rc;
+    return launch_grouped(a, dev, (cudaStream_t)stream);
+}
+
+uint64_t sk_grouped_linear_backward_workspace(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight,
+                                              uint64_t stride_weight, uint64_t rows, uint64_t groups, uint64_t width, uint64_t out) {
+    GroupedArgs a{};
+    a.dy = dy; a.ld_dy = ld_dy; a.x = x; a.ld_x = ld_x; a.weight = weight; a.ld_weight = ld_weight; a.stride_weight = stride_weight;
+    a.rows = rows; a.groups = groups; a.width = width; a.out = out;
+    return rows ? grouped_workspace(a, true) : 0;
+}
+
+int sk_grouped_linear_backward(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight,
+                               int type, uint64_t rows, uint64_t groups, uint64_t width, uint64_t out, const int64_t* offsets, void* dx, uint64_t ld_dx,
+                               int fill, void* dweight, uint64_t ld_dweight, uint64_t stride_dweight, int dweight_type, void* workspace,
+                               uint64_t workspace_bytes, void* stream) {
+    const char* who = "sk_grouped_linear_backward";
+    GroupedArgs a{};
+    a.dy = dy; a.ld_dy = ld_dy; a.x = x; a.ld_x = ld_x; a.weight = weight; a.ld_weight = ld_weight; a.stride_weight = stride_weight;
+    a.type = type; a.rows = rows; a.groups = groups; a.width = width; a.out = out; a.offsets = offsets; a.fill = fill;
+    a.dx = dx; a.ld_dx = ld_dx; a.dweight = dweight; a.ld_dweight = ld_dweight; a.stride_dweight = stride_dweight; a.dweight_type = dweight_type;
+    a.workspace = workspace;
+    if (int rc = grouped_checked(who, a, true)) return rc;
+    if (dweight && dweight_type != type && dweight_type != SK_F32) return set_error(SK_EINVAL, "%s: dweight's type must be the inputs' or SK_F32", who);
+    if ((dx && ld_dx < width) || (dweight && ld_dweight < width)) return set_error(SK_EINVAL, "%s: a leading dimension is below the rows' length", who);
+    if (dweight && groups > 1 && stride_dweight < (out - 1) * ld_dweight + width) return set_error(SK_EINVAL, "%s: the matrices of an output overlap", who);
+    if (misaligned(dx, type) || (dweight && misaligned(dweight, dweight_type))) return set_error(SK_EINVAL, "%s: a pointer is not aligned to its element", who);
+    if (!rows) {                                  // sums over no rows
+        const uint64_t size = dweight ? type_size(dweight_type) : 0;
+        const bool together = groups == 1 || stride_dweight == out * ld_dweight;
+        for (uint64_t g = 0; dweight && g < (together ? 1 : groups); ++g)
+            SK_OP_CUDA(cudaMemset2DAsync((uint8_t*)dweight + g * stride_dweight * size, ld_dweight * size, 0, width * size, together ? groups * out : out,
+                                         (cudaStream_t)stream));
+        return SK_OK;
+    }
+    if (!dx && !dweight) return SK_OK;
+    if ((dx && (dx == dy || dx == x || dx == weight)) || (dweight && (dweight == dy || dweight == x || dweight == weight)))
+        return set_error(SK_EINVAL, "%s: the gradients cannot be written in place", who);
+    if (int rc = check_workspace(who, workspace, workspace_bytes, grouped_workspace(a, true))) return rc;
+    OpDevice dev;
+    if (int rc = op_device(&dev)) return rc;
+    return launch_grouped_backward(a, dev, (cudaStream_t)stream);
+}
+
+uint64_t sk_sort_by_expert_workspace(uint64_t n, uint64_t groups) {
+    OpDevice dev;
+    if (!n || n >= kMaxExtent || groups < 1 || groups > kMaxGroups || op_device(&dev)) return 0;
+    return sort_workspace(n, (uint32_t)groups, dev.sm_count);
+}
+
+int sk_sort_by_expert(const void* experts, int expert_bits, uint64_t n, uint64_t groups, int64_t* order, int64_t* places, int64_t* offsets, void* workspace,
+                      uint64_t workspace_bytes, void* stream) {
+    const char* who = "sk_sort_by_expert";
+    if (expert_bits != 32 && expert_bits != 64) return set_error(SK_EINVAL, "%s: expert_bits must be 32 or 64", who);
+    if (groups < 1 || groups > kMaxGroups) return set_error(SK_EINVAL, "%s: groups must be in 1..%u", who, kMaxGroups);
+    if (n >= kMaxExtent) return set_error(SK_EINVAL, "%s: n must be below 2^31", who);
+    if (!offsets || (n && !experts)) return set_error(SK_EINVAL, "%s: null argument", who);
+    if ((uintptr_t)experts % (expert_bits / 8) || (uintptr_t)order % 8 || (uintptr_t)places % 8 || (uintptr_t)offsets % 8)
+        return set_error(SK_EINVAL, "%s: a pointer is not aligned to its element", who);
+    if (n && (order == experts || places == experts || offsets == experts)) return set_error(SK_EINVAL, "%s: the experts cannot be sorted in place", who);
+    if (!n) {
+        SK_OP_CUDA(cudaMemsetAsync(offsets, 0, (groups + 1) * 8, (cudaStream_t)stream));
+        return SK_OK;
+    }
+    OpDevice dev;
+    if (int rc = op_device(&dev)) return rc;
+    if (int rc = check_workspace(who, workspace, workspace_bytes, sort_workspace(n, (uint32_t)groups, dev.sm_count))) return rc;
+    return launch_sort({experts, n, (uint32_t)groups, expert_bits == 64, order, places, offsets, (uint32_t*)workspace}, dev.sm_count, (cudaStream_t)stream);
+}
+
+int sk_dropout(const void* x, uint64_t ld_x, const void* residual, uint64_t ld_residual, void* y, uint64_t ld_y, int type, uint64_t rows, uint64_t cols,
+               double p, uint64_t seed, const uint64_t* seed_at, void* stream) {
+    const char* who = "sk_dropout";
+    if (!type_ok(type)) return set_error(SK_EINVAL, "%s: unknown type", who);
+    if (!(p >= 0.0 && p <= 1.0)) return set_error(SK_EINVAL, "%s: p must be in 0..1", who);
+    if (cols >= (1ull << 40) || rows >= (1ull << 40) || rows * (cols >> 20) >= (1ull << 30)) return set_error(SK_EINVAL, "%s: too many values", who);
+    if (!rows || !cols) return SK_OK;
+    if (!x || !y) return set_error(SK_EINVAL, "%s: null argument", who);
+    if (ld_x < cols || ld_y < cols || (residual && ld_residual < cols)) return set_error(SK_EINVAL, "%s: a leading dimension is below cols", who);
+    if (rows > 1 && ((y == x && ld_y != ld_x) || (y == residual && ld_y != ld_residual)))
+        return set_error(SK_EINVAL, "%s: in place, the leading dimensions must be the same", who);
+    if (misaligned(x, type) || misaligned(residual, type) || misaligned(y, type) || (uintptr_t)seed_at % 8)
+        return set_error(SK_EINVAL, "%s: a pointer is not aligned to its element", who);
+    OpDevice dev;
+    if (int rc = op_device(&dev)) return rc;
+    const uint32_t below = (uint32_t)std::nearbyint(p * 65536.0);
+    const float scale = below < 65536 ? (float)(65536.0 / (65536.0 - below)) : 0.0f;
+    return launch_dropout({x, residual, y, rows, cols, ld_x, ld_residual, ld_y, type, seed, seed_at, below, scale}, dev.sm_count, (cudaStream_t)stream);
+}
+
+static int policy_checked(const char* who, const PolicyArgs& a, double clip_low, double clip_high) {
+    if (a.tokens >= (1ull << 40) || a.sequences < 1 || a.sequences >= kMaxExtent) return set_error(SK_EINVAL, "%s: tokens must be below 2^40, sequences in 1..2^31-1", who);
+    if (!a.offsets && a.sequences != 1) return set_error(SK_EINVAL, "%s: without offsets there is one sequence", who);
+    if (!(clip_low >= 0 && clip_low <= 1) || !(clip_high >= 0)) return set_error(SK_EINVAL, "%s: clip_low must be in 0..1, clip_high not negative", who);
+    if (!std::isfinite(a.kl)) return set_error(SK_EINVAL, "%s: kl must be finite", who);
+    if (a.tokens && (!a.nll || !a.old_nll || !a.advantages)) return set_error(SK_EINVAL, "%s: null argument", who);
+    if (a.kl != 0 && !a.reference && a.tokens) return set_error(SK_EINVAL, "%s: kl needs reference_nll", who);
+    if (misaligned(a.nll, SK_F32) || misaligned(a.old_nll, SK_F32) || misaligned(a.advantages, SK_F32) || misaligned(a.reference, SK_F32) ||
+        misaligned(a.result, SK_F32) || misaligned(a.norm, SK_F32) || misaligned(a.dloss, SK_F32) || misaligned(a.dnll, SK_F32) ||
+        (uintptr_t)a.targets % 8 || (uintptr_t)a.offsets % 8)
+        return set_error(SK_EINVAL, "%s: a pointer is not aligned to its element", who);
+    return SK_OK;
+}
+
+uint64_t sk_policy_loss_workspace(uint64_t tokens, uint64_t sequences) {
+    return tokens && tokens < (1ull << 40) && sequences < kMaxExtent ? policy_workspace(tokens, sequences) : 0;
+}
+
+static PolicyArgs policy_args(const float* nll, const float* old_nll, const float* advantages, int advantage_of_sequences, const int64_t* targets,
+                              const int64_t* offsets, uint64_t sequences, const float* reference_nll, uint64_t tokens, double clip_low, double clip_high,
+                              double kl) {
+    PolicyArgs a{};
+    a.nll = nll; a.old_nll = old_nll; a.advantages = advantages; a.advantage_of_sequences = advantage_of_sequences;
+    a.targets = targets; a.offsets = offsets; a.sequences = sequences; a.reference = reference_nll; a.tokens = tokens;
+    a.log_low = std::log1p(-clip_low); a.log_high = std::log1p(clip_high);
+    a.low = (float)(1.0 - clip_low); a.high = (float)(1.0 + clip_high); a.kl = (float)kl;
+    return a;
+}
+
+int sk_policy_loss(const float* nll, const float* old_nll, const float* advantages, int advantage_of_sequences, const int64_t* targets,
+                   const int64_t* offsets, uint64_t sequences, const float* reference_nll, uint64_t tokens, double clip_low, double clip_high, double kl,
+                   int average_sequences, float* result, float* norm, void* workspace, uint64_t workspace_bytes, void* stream) {
+    const char* who = "sk_policy_loss";
+    PolicyArgs a = policy_args(nll, old_nll, advantages, advantage_of_sequences, targets, offsets, sequences, reference_nll, tokens, clip_low, clip_high, kl);
+    a.average_sequences = average_sequences; a.result = result; a.norm = norm; a.workspace = (float4*)workspace;
+    if (int rc = policy_checked(who, a, clip_low, clip_high)) return rc;
+    if (!result || !norm) return set_error(SK_EINVAL, "%s: null argument", who);
+    if (!tokens) {
+        SK_OP_CUDA(cudaMemsetAsync(result, 0, 12, (cudaStream_t)stream));
+        SK_OP_CUDA(cudaMemsetAsync(norm, 0, sequences * 4, (cudaStream_t)stream));
+        return SK_OK;
+    }
+    if (int rc = check_workspace(who, workspace, workspace_bytes, policy_workspace(tokens, sequences))) return rc;
+    return launch_policy(a, (cudaStream_t)stream);
+}
+
+int sk_policy_loss_backward(const float* dloss, const float* nll, const float* old_nll, const float* advantages, int advantage_of_sequences,
+                            const int64_t* targets, const int64_t* offsets, uint64_t sequences, const float* reference_nll, uint64_t tokens,
+                            double clip_low, double clip_high, double kl, const float* norm, float* dnll, void* stream) {
+    const char* who = "sk_policy_loss_backward";
+    PolicyArgs a = policy_args(nll, old_nll, advantages, advantage_of_sequences, targets, offsets, sequences, reference_nll, tokens, clip_low, clip_high, kl);
+    a.dloss = dloss; a.norm = const_cast<float*>(norm); a.dnll = dnll;
+    if (int rc = policy_checked(who, a, clip_low, clip_high)) return rc;
+    if (!tokens) return SK_OK;
+    if (!norm || !dnll) return set_error(SK_EINVAL, "%s: null argument", who);
+    return launch_policy_backward(a, (cudaStream_t)stream);
+}
+
 int sk_test_operators_wait(uint32_t limit_ms) {
     if (limit_ms < 1 || limit_ms > 1000) return set_error(SK_EINVAL, "sk_test_operators_wait: limit_ms must be in 1..1000");
     t_withhold_ms = limit_ms;

@@ -243,6 +243,65 @@ struct OrthoArgs {
     float coefficient[3];
     void* workspace;
 };
+// Products grouped by expert: rows offsets[g] .. offsets[g + 1] of x with matrix g (out x width), all of one 16-bit type
+constexpr uint32_t kMaxGroups = 2048;
+struct GroupedArgs {
+    const void *x, *weight;
+    const int64_t* offsets;          // groups + 1
+    uint64_t rows, groups, width, out;
+    uint64_t ld_x, ld_weight, stride_weight;
+    int type, fill;                  // fill: rows of no group become zero in y or dx
+    void* y;                         // forward: rows x out
+    uint64_t ld_y;
+    const void* dy;                  // backward only, from here on
+    void *dx, *dweight;              // either may be null
+    uint64_t ld_dy, ld_dx, ld_dweight, stride_dweight;
+    int dweight_type;
+    void* workspace;
+};
+int launch_grouped(GroupedArgs a, const OpDevice& dev, cudaStream_t st);
+int launch_grouped_backward(GroupedArgs a, const OpDevice& dev, cudaStream_t st);
+uint64_t grouped_workspace(const GroupedArgs& a, bool backward);
+
+struct SortArgs {
+    const void* experts;             // n int64, or int32
+    uint64_t n;
+    uint32_t groups;
+    int wide;                        // 64-bit
+    int64_t *order, *places, *offsets;       // either of the first two may be null
+    uint32_t* workspace;
+};
+int launch_sort(const SortArgs& a, int sm_count, cudaStream_t st);
+uint64_t sort_workspace(uint64_t n, uint32_t groups, int sm_count);
+
+struct DropoutArgs {
+    const void *x, *residual;        // residual may be null
+    void* y;
+    uint64_t rows, cols, ld_x, ld_residual, ld_y;
+    int type;
+    uint64_t seed;
+    const uint64_t* seed_at;         // on the device, or null
+    uint32_t below;                  // a 16-bit number below this drops the value
+    float scale;
+};
+int launch_dropout(const DropoutArgs& a, int sm_count, cudaStream_t st);
+
+struct PolicyArgs {
+    const float *nll, *old_nll, *advantages, *reference;
+    const int64_t *targets, *offsets;        // either may be null
+    uint64_t tokens, sequences;
+    int advantage_of_sequences, average_sequences;
+    double log_high, log_low;        // of the ratio's bounds
+    float high, low, kl;
+    float *result, *norm;            // forward: out
+    const float* dloss;              // backward: may be null
+    float* dnll;
+    float4* workspace;
+};
+int launch_policy(const PolicyArgs& a, cudaStream_t st);
+int launch_policy_backward(const PolicyArgs& a, cudaStream_t st);
+uint64_t policy_workspace(uint64_t tokens, uint64_t sequences);
+
 // withhold_ms: not zero in tests, see sk_test_operators_wait
 int launch_orthogonalize(const OrthoArgs& a, const OpDevice& dev, uint32_t withhold_ms, cudaStream_t st);
 uint64_t orthogonalize_workspace(const OrthoArgs& a);

@@ -67,6 +67,7 @@ struct ChainLow {                                // PRECISE: the second matrices
 template <bool SLICED, bool PRECISE>
 struct ChainPlan : ChainShape, std::conditional<PRECISE, ChainLow, std::false_type>::type {
     static constexpr bool kCooperative = true, kEmpty = SLICED, kThree = PRECISE;    // kEmpty: has tiles without products
+    static constexpr bool kRagged = false;
     // tiles of one matrix and step before those of a kind, and of all kinds
     __device__ __forceinline__ uint32_t tiles_before(uint32_t kind) const {
         if (!SLICED) return kind * square;

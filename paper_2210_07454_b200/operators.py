@@ -1,5 +1,5 @@
 """Operators of language models beside the optimiser step: layer norm, the loss of a linear head over a large vocabulary,
-and orthogonalised updates of matrix parameters.
+orthogonalised updates of matrix parameters, the products of a layer of experts, dropout, and the clipped policy loss.
 
 Argument marshalling only, like ``binding``: every operator runs in the CUDA library (``sk_layer_norm`` and so on in
 ``include/sketched_amsgrad.h``, which states the formulas).  Tensors are CUDA tensors of one device whose rows are
@@ -24,6 +24,7 @@ _TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
 _HALF = {torch.bfloat16: 1, torch.float16: 2}
 _F32 = {torch.float32: 0}
 _INT64 = {torch.int64: 0}
+_INDEX = {torch.int64: 64, torch.int32: 32}
 
 # Newton-Schulz step X <- a X + (b A + c A^2) X, A = X X^T: the coefficients published with the Muon optimiser (K. Jordan and others, 2024)
 COEFFICIENTS = (3.4445, -4.7750, 2.0315)
@@ -138,6 +139,11 @@ def _elsewhere(device, fn, *args):
     """What a function of the library (a workspace's size) gives for a device that is not current."""
     with torch.cuda.device(device):
         return fn(*args)
+
+
+def _need(device, size, *args):
+    """Bytes of workspace, asked with the tensors' device current."""
+    return size(*args) if _current_device() == device else _elsewhere(device, size, *args)
 
 
 def _new(shape, stride, dtype, device):
@@ -375,6 +381,238 @@ def orthogonalize(update, momentum=None, beta=0.95, nesterov=True, steps=5, coef
          (C.c_float * 3)(*coefficients), eps, _p(ws), need, _raw_stream(device))
     if momentum is not None or given_out is not None:
         _wrote(momentum, given_out)
+    return out
+
+
+# ---- products grouped by expert ---------------------------------------------------------------------------------------------
+def sort_by_expert(experts, groups, stream=None):
+    """Brings assignments of rows to experts into the order that ``grouped_linear`` takes.  experts: a contiguous tensor of n values, int64 or
+    int32; what lies outside 0..groups-1 belongs to no expert and comes last.  Returns (order, places, offsets), int64: order (n,), the assignments sorted
+    by expert, equal ones in the order they have; places, like experts, where each one went (order[places[i]] = i); offsets (groups + 1,),
+    the places at which the experts' assignments begin and end.
+
+    With k experts for each token (experts: (tokens, k)) the rows are x[order // k], and a token's results are y[places]: (tokens, k, out)."""
+    if stream is not None:
+        return _on(stream, lambda: sort_by_expert(experts, groups), experts)
+    wide = _tensor(experts, "experts", _INDEX)
+    if not experts.is_contiguous():
+        raise SkError("experts must be contiguous")
+    device, n = experts.get_device(), experts.numel()
+    if groups < 1 or groups > 2048:
+        raise SkError("groups must be in 1..2048")
+    order, offsets = _new((n,), (1,), torch.int64, device), _new((groups + 1,), (1,), torch.int64, device)
+    places = _new_like(experts, torch.int64, device)
+    need = _need(device, lib().sk_sort_by_expert_workspace, n, groups)
+    ws = _workspace(need, device)
+    _run(device, lib().sk_sort_by_expert, experts.data_ptr(), wide, n, groups, order.data_ptr(), places.data_ptr(), offsets.data_ptr(), _p(ws), need,
+         _raw_stream(device))
+    return order, places, offsets
+
+
+def _grouped(x, weight, offsets):
+    """What both directions take: (device, code, rows, groups, width, out, ld_x, ld_w, stride_w, address of the offsets)"""
+    code, ld_x = _matrix(x, "x", _HALF)
+    device = x.get_device()
+    if _tensor(weight, "weight", _HALF, device) != code:
+        raise SkError(f"x has type {x.dtype}, weight {weight.dtype}")
+    if weight.dim() != 3:
+        raise SkError(f"weight must have 3 dimensions, got {weight.dim()}")
+    (rows, width), (groups, out, other) = x.shape, weight.shape
+    if width != other:
+        raise SkError(f"x has width {width}, weight {other}")
+    if groups < 1 or width < 1 or out < 1:
+        raise SkError("the groups, the width and the outputs must not be empty")
+    return device, code, rows, groups, width, out, ld_x, _ld(weight, "weight"), weight.stride(0), _vector(offsets, "offsets", groups + 1, _INT64, device)
+
+
+def grouped_linear(x, weight, offsets, out=None, stream=None):
+    """y[i] = weight[g] x[i] for the rows i of every group g: offsets[g] <= i < offsets[g + 1].  x: (rows, width), weight: (groups, out, width), both
+    bf16 or both fp16; offsets: (groups + 1,) int64 on the same device (see ``sort_by_expert``), which the host never reads.  Returns (rows, out) of
+    x's type.  Rows of no group are zero, or left as they were in an ``out`` that is given."""
+    if stream is not None:
+        return _on(stream, lambda: grouped_linear(x, weight, offsets, out), x, weight, offsets, out)
+    device, code, rows, groups, width, n, ld_x, ld_w, s_w, po = _grouped(x, weight, offsets)
+    if out is None:
+        y, ld_y = _new((rows, n), (n, 1), x.dtype, device), n
+    else:
+        ycode, ld_y = _matrix(out, "out", _HALF, device)
+        if ycode != code:
+            raise SkError(f"out has type {out.dtype}, x {x.dtype}")
+        if out.shape != (rows, n):
+            raise SkError(f"out must have the shape {(rows, n)}, got {tuple(out.shape)}")
+        y = out
+    px, pw = x.data_ptr(), weight.data_ptr()
+    need = _need(device, lib().sk_grouped_linear_workspace, px, ld_x, pw, ld_w, s_w, rows, groups, width, n)
+    ws = _workspace(need, device)
+    _run(device, lib().sk_grouped_linear, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, y.data_ptr(), ld_y, out is None, _p(ws), need,
+         _raw_stream(device))
+    if out is not None:
+        _wrote(out)
+    return y
+
+
+def grouped_linear_backward(dy, x, weight, offsets, dx=None, dweight=None, stream=None):
+    """Gradients of ``grouped_linear``.  Returns (dx, dweight) of the inputs' type: dx like x (rows of no group are zero, or left as they were in a given one),
+    dweight like weight (zero for a group without rows).  ``dx``, ``dweight``: tensors to write into (dweight of the inputs' type or fp32; a view of
+    the gradient array of a step is fine), False to leave one out.  Sums are fp32."""
+    if stream is not None:
+        return _on(stream, lambda: grouped_linear_backward(dy, x, weight, offsets, dx, dweight), dy, x, weight, offsets, dx, dweight)
+    device, code, rows, groups, width, n, ld_x, ld_w, s_w, po = _grouped(x, weight, offsets)
+    dcode, ld_dy = _matrix(dy, "dy", _HALF, device)
+    if dcode != code:
+        raise SkError(f"dy has type {dy.dtype}, x {x.dtype}")
+    if dy.shape != (rows, n):
+        raise SkError(f"dy must have the shape {(rows, n)}, got {tuple(dy.shape)}")
+    given_outputs, fill, ld_dx = (dx, dweight), dx is None, width
+    if dx is None:
+        dx = _new((rows, width), (width, 1), x.dtype, device)
+    elif dx is False:
+        dx = None
+    else:
+        xcode, ld_dx = _matrix(dx, "dx", _HALF, device)
+        if xcode != code:
+            raise SkError(f"dx has type {dx.dtype}, x {x.dtype}")
+        _same_shape(dx, x, "dx")
+    wcode, ld_dw, s_dw = code, width, n * width
+    if dweight is None:
+        dweight = _new((groups, n, width), (n * width, width, 1), weight.dtype, device)
+    elif dweight is False:
+        dweight = None
+    else:
+        wcode = _tensor(dweight, "dweight", {weight.dtype: code, torch.float32: 0}, device)
+        _same_shape(dweight, weight, "dweight")
+        ld_dw, s_dw = _ld(dweight, "dweight"), dweight.stride(0)
+    pd, px, pw = dy.data_ptr(), x.data_ptr(), weight.data_ptr()
+    need = _need(device, lib().sk_grouped_linear_backward_workspace, pd, ld_dy, px, ld_x, pw, ld_w, s_w, rows, groups, width, n)
+    ws = _workspace(need, device)
+    _run(device, lib().sk_grouped_linear_backward, pd, ld_dy, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, _p(dx), ld_dx, fill, _p(dweight),
+         ld_dw, s_dw, wcode, _p(ws), need, _raw_stream(device))
+    _wrote(*given_outputs)
+    return dx, dweight
+
+
+# ---- dropout ------------------------------------------------------------------------------------------------------------------
+def _seed(seed, device):
+    """(value, address) of a seed: a whole number, or one on the device"""
+    if isinstance(seed, torch.Tensor):
+        _vector(seed, "seed", 1, _INT64, device)
+        return 0, seed.data_ptr()
+    try:
+        return int(seed) & 0xFFFFFFFFFFFFFFFF, None
+    except (TypeError, ValueError):
+        raise SkError("seed must be a whole number or a CUDA tensor of one int64") from None
+
+
+def dropout(x, p, seed, residual=None, out=None, stream=None):
+    """residual + x / (1 - p) where a value stays, residual where it is dropped, with probability p.  Which ones stay is a function of the seed and the
+    value's number in x (in row order, whatever its strides): there is no mask to keep.  x: fp32, bf16 or fp16 of any shape; residual: like x, or None
+    (zero).  p is rounded to a multiple of 2^-16.  seed: a whole number (modulo 2^64), another one for every use, or a CUDA tensor of one int64 that is read when
+    the kernel runs (a captured call can then be replayed with another).  Returns a tensor like x; ``out`` may be x or residual."""
+    if stream is not None:
+        return _on(stream, lambda: dropout(x, p, seed, residual, out), x, seed, residual, out)
+    code = _tensor(x, "x", _TYPES)
+    if not x.dim():
+        raise SkError("x must have at least 1 dimension")
+    device, cols = x.get_device(), x.shape[-1]
+    rows, ld = _rows(x, "x")
+    pr, ld_r = None, cols
+    if residual is not None:
+        if _tensor(residual, "residual", _TYPES, device) != code:
+            raise SkError(f"residual has type {residual.dtype}, x {x.dtype}")
+        _same_shape(residual, x, "residual")
+        pr, ld_r = residual.data_ptr(), _rows(residual, "residual")[1]
+    if out is None:
+        y, ld_y = _new_like(x, x.dtype, device), cols
+    else:
+        if _tensor(out, "out", _TYPES, device) != code:
+            raise SkError(f"out has type {out.dtype}, x {x.dtype}")
+        _same_shape(out, x, "out")
+        y, ld_y = out, _rows(out, "out")[1]
+    value, at = _seed(seed, device)
+    _run(device, lib().sk_dropout, x.data_ptr(), ld, pr, ld_r, y.data_ptr(), ld_y, code, rows, cols, p, value, at, _raw_stream(device))
+    if out is not None:
+        _wrote(out)
+    return y
+
+
+def dropout_backward(dy, p, seed, dx=None, stream=None):
+    """Gradient of ``dropout`` with respect to x, from dy with the p and the seed of the forward pass (that of the residual is dy).  Returns dx, which may
+    be given and may be dy."""
+    return dropout(dy, p, seed, None, dx, stream)
+
+
+# ---- policy loss ----------------------------------------------------------------------------------------------------------------
+_OF = {"tokens": 0, "sequences": 1}
+
+
+def _policy(nll, old_nll, advantages, targets, offsets, reference_nll, clip, kl, advantage_of):
+    """The arguments that both directions share, from nll to kl, and (device, tokens, sequences)"""
+    _tensor(nll, "nll", _F32)
+    device, tokens = nll.get_device(), nll.numel()
+    pn, pold = _vector(nll, "nll", tokens, _F32, device), _vector(old_nll, "old_nll", tokens, _F32, device)
+    pt = _vector(targets, "targets", tokens, _INT64, device) if targets is not None else None
+    sequences, po = 1, None
+    if offsets is not None:
+        _tensor(offsets, "offsets", _INT64, device)
+        sequences = offsets.numel() - 1
+        if sequences < 1:
+            raise SkError("offsets must hold at least 2 values")
+        po = _vector(offsets, "offsets", sequences + 1, _INT64, device)
+    of = _OF.get(advantage_of)
+    if of is None:
+        raise SkError(f"advantage_of must be 'tokens' or 'sequences', got {advantage_of!r}")
+    pa = _vector(advantages, "advantages", sequences if of else tokens, _F32, device)
+    pr = _vector(reference_nll, "reference_nll", tokens, _F32, device) if reference_nll is not None else None
+    try:
+        low, high = clip
+    except (TypeError, ValueError):
+        raise SkError("clip is two numbers (low, high)") from None
+    return (pn, pold, pa, of, pt, po, sequences, pr, tokens, low, high, kl), device, tokens, sequences
+
+
+def policy_loss(nll, old_nll, advantages, targets=None, offsets=None, reference_nll=None, clip=(0.2, 0.2), kl=0.0, average="tokens",
+                advantage_of="tokens", stream=None):
+    """The clipped policy loss with a KL term, over losses as ``linear_cross_entropy`` returns them (negative log probabilities of the tokens drawn).
+    With r = exp(old_nll - nll), A the advantage, e = nll - reference_nll, a token's loss is
+    -min(r A, min(max(r, 1 - clip[0]), 1 + clip[1]) A) + kl (exp(e) - e - 1).
+
+    nll, old_nll, reference_nll: fp32, (tokens,); advantages: fp32, one for each token or (advantage_of="sequences") each sequence; targets: (tokens,) int64, tokens
+    with a negative one take no part (the vector that the head takes); offsets: (sequences + 1,) int64, where the sequences begin and end (None: all
+    tokens are one).  average: "tokens" (every token counts the same) or "sequences" (every sequence, and its tokens among one another).
+    Returns (result, norm): result (3,) fp32 is the loss, the mean of exp(e) - e - 1, the share of clipped tokens, all in the same average; norm (sequences,) fp32
+    is what a token counts, for the backward pass."""
+    if stream is not None:
+        return _on(stream, lambda: policy_loss(nll, old_nll, advantages, targets, offsets, reference_nll, clip, kl, average, advantage_of), nll, old_nll,
+                   advantages, targets, offsets, reference_nll)
+    args, device, tokens, sequences = _policy(nll, old_nll, advantages, targets, offsets, reference_nll, clip, kl, advantage_of)
+    if average not in _OF:
+        raise SkError(f"average must be 'tokens' or 'sequences', got {average!r}")
+    result, norm = _new((3,), (1,), torch.float32, device), _new((sequences,), (1,), torch.float32, device)
+    need = _need(device, lib().sk_policy_loss_workspace, tokens, sequences)
+    ws = _workspace(need, device)
+    _run(device, lib().sk_policy_loss, *args, _OF[average], result.data_ptr(), norm.data_ptr(), _p(ws), need, _raw_stream(device))
+    return result, norm
+
+
+def policy_loss_backward(dloss, nll, old_nll, advantages, norm, targets=None, offsets=None, reference_nll=None, clip=(0.2, 0.2), kl=0.0,
+                         advantage_of="tokens", dnll=None, stream=None):
+    """Gradient of ``policy_loss``'s loss with respect to nll, from the norm it returned and its other arguments: what
+    ``linear_cross_entropy_backward`` takes as dloss.  dloss: fp32 of one value, or None (1).  Returns dnll (tokens,) fp32, zero for tokens that take no
+    part; ``dnll``, if given, may be nll."""
+    if stream is not None:
+        return _on(stream, lambda: policy_loss_backward(dloss, nll, old_nll, advantages, norm, targets, offsets, reference_nll, clip, kl, advantage_of, dnll),
+                   dloss, nll, old_nll, advantages, norm, targets, offsets, reference_nll, dnll)
+    args, device, tokens, sequences = _policy(nll, old_nll, advantages, targets, offsets, reference_nll, clip, kl, advantage_of)
+    pl = _vector(dloss, "dloss", 1, _F32, device) if dloss is not None else None
+    pm = _vector(norm, "norm", sequences, _F32, device)
+    if dnll is None:
+        out = _new((tokens,), (1,), torch.float32, device)
+    else:
+        _vector(dnll, "dnll", tokens, _F32, device)
+        out = dnll
+    _run(device, lib().sk_policy_loss_backward, pl, *args, pm, out.data_ptr(), _raw_stream(device))
+    if dnll is not None:
+        _wrote(dnll)
     return out
 
 
