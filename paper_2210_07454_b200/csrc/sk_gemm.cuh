@@ -210,6 +210,18 @@ __device__ __forceinline__ void tmem_load8(uint32_t addr, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(r[i]);
 }
+// 16 of a warp's rows and 32 columns, as fragments of 8 x 8: of the j-th eight columns a lane has row lane / 4 in v[4 j], v[4 j + 1] and row lane / 4 + 8 in
+// the next two, columns 2 (lane mod 4) and the one after it.
+__device__ __forceinline__ void tmem_load_fragments(uint32_t addr, float (&v)[32], int at) {
+    uint32_t r[16];
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]),
+          "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(addr));
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[at + i] = __uint_as_float(r[i]);
+}
 // Shared-memory descriptor, 128-byte swizzle.  K-major: rows of 128 bytes, groups of eight rows 1024 bytes apart.
 // MN-major: blocks of 64 row indices (block_bytes from one to the next: 8192 if they are 64 k deep), groups of eight k 1024 bytes apart.
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, bool mn, uint32_t block_bytes = 8192) {
@@ -293,7 +305,8 @@ struct GemmTile {
 
 // Plan: job(unit, units, i, job): the unit's i-th tile; wait(job): until its operands are there; done(job): called by every epilogue warp
 // when its share of the tile is written.  kRagged: the tiles depend on data; prepare(shared address of all epilogue warps' memory) is called once by the
-// whole block before the first job(), load(job, k, ...) issues the copies of a stage, stage_bytes(job, k) says what they bring to a block.
+// whole block before the first job(); Feed(plan, job, rank) holds what the copies of a tile's stages need: copy(k, ...) issues them, bytes(k) is what they bring to a
+// block.  Epi: load() reads 32 columns of the accumulator, column() says which, finish() is called after the last tile.
 // Epi: struct Args; __device__ Epi(const Args&, job, row, part, shared address of the warp's memory); begin(plan, first column) before the
 // accumulator is waited for, false (in the whole warp) if a wait of its own ran out; kParts: see above; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
 // row of the tile and gets its columns 32 at a time; the kWarps / 4 warps that share a row take a part of the columns each.  Rows >= M
@@ -355,13 +368,15 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
             for (uint32_t i = 0; ok && plan.job(unit, units, i, t); ++i) {
                 if constexpr (Plan::kRagged) {
                     any = true;
-                    for (uint32_t k = 0; k < t.k_stages; ++k) {
+                    const uint32_t kb = t.k_stages;
+                    typename Plan::Feed feed(plan, t, rank);
+                    for (uint32_t k = 0; k < kb; ++k) {
                         if (!(ok = mbar_wait(empty(s), parity, plan.waits))) break;
-                        const uint32_t sa = stages + s * kBytes, bytes = CG * plan.template stage_bytes<kRowsB>(t, k);
+                        const uint32_t sa = stages + s * kBytes;
                         uint32_t bar = full(s);
-                        if (rank == 0) mbar_expect(bar, bytes);
+                        if (rank == 0) mbar_expect(bar, CG * feed.bytes(k));
                         if constexpr (CG == 2) bar = map_to_leader(bar);
-                        plan.template load<CG, kRowsB>(t, k, rank, sa, sa + kBytesA, bar);
+                        feed.copy(k, sa, sa + kBytesA, bar);
                         if (++s == (uint32_t)kStages) { s = 0; parity ^= 1; }
                     }
                     continue;
@@ -423,9 +438,11 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                 const uint32_t kb = t.k_stages, most = Epi::kParts ? t.part : kb;
                 uint32_t steps = t.k_rows / 16, columns = BN;
                 if constexpr (Plan::kRagged) {
-                    if (!kb) continue;                           // nothing to add up, no accumulator taken
+                    steps = t.last_rows / 16;
                     columns = t.cols;
                 }
+                const uint32_t whole = steps == kGemmK / 16 ? kb : kb - 1;       // of a ragged tile: stages of four instructions
+                if (Plan::kRagged && !kb) continue;              // nothing to add up, no accumulator taken
                 // D fp32; A, B bf16 or fp16; majors; N / 8; M / 16
                 const uint32_t idesc = (1u << 4) | (t.bf16 << 7) | (t.bf16 << 10) | (t.a_mn << 15) | (t.b_mn << 16) |
                                        ((columns / 8) << 17) | ((uint32_t)(128 * CG / 16) << 24);
@@ -441,8 +458,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                         if (!(ok = mbar_wait(full(s), parity, plan.waits))) break;
                         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
                         const uint64_t da = desc_a + s * (kBytes >> 4), db = desc_b + s * (kBytes >> 4);
-                        if constexpr (Plan::kRagged) steps = from + k + 1 == kb ? t.last_rows / 16 : kGemmK / 16;
-                        if (steps == kGemmK / 16) {
+                        if (Plan::kRagged ? from + k < whole : steps == kGemmK / 16) {
 #pragma unroll
                             for (uint32_t q = 0; q < kGemmK / 16; ++q) mma_f16<CG>(d, da + q * step_a, db + q * step_b, idesc, (k | q) != 0);
                         } else {
@@ -536,7 +552,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
                     more = c + 32 < kCols && Epi::column(t, part, c + 32, kCols, BN) < t.N;
                     float v[32];
                     __syncwarp();
-                    if (col < t.N) tmem_load32(tmem + a * BN + at + ((quarter * 32) << 16), v);
+                    if (col < t.N) Epi::load(tmem + a * BN + at + ((quarter * 32) << 16), v);
                     if (!more) {
                         asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
                         __syncwarp();
@@ -561,6 +577,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
             epi.end();
             plan.done(t);
         }
+        if constexpr (Plan::kRagged) Epi::finish();
     }
 
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
@@ -583,6 +600,8 @@ struct Operand {
 };
 
 bool encode_operand(CUtensorMap* map, const Operand& o, bool bf16, uint32_t box_rows);
+// an output that is written in boxes of 16 rows and 32 columns, 64-byte swizzle
+bool encode_rows_out(CUtensorMap* map, void* out, uint64_t rows, uint64_t cols, uint64_t ld, bool bf16);
 
 // Launches a plan on at most `units` blocks or pairs.
 template <int CG, int BN, class Plan, class Epi>

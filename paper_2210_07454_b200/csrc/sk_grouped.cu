@@ -27,10 +27,97 @@ constexpr uint32_t kTableWords = 2 * (kSegments + 1);
 // The group boundaries as the kernels take them: never decreasing, never outside 0..rows, whatever the offsets hold.
 __device__ __forceinline__ uint32_t bounded(int64_t v, uint32_t rows) { return v < 0 ? 0 : v > (int64_t)rows ? rows : (uint32_t)v; }
 
+// A warp holds 32 output columns (rows of the transposed tile) and takes 32 of the group's rows at a time, as fragments that the transposing stores to shared
+// memory turn round: 16 rows of 64 bytes are written as one box by the copy engine, or, where it cannot write (the last rows of a group, outputs it cannot address),
+// by the lanes.  Two boxes take turns.
+struct RowsEpi {
+    static constexpr uint32_t kBox = 1024;
+    static constexpr int kWarps = 8, kWords = (kTableWords + 7) / 8 + 2 * kBox / 4 + 32;      // the list of tiles, then the boxes, each on a 512-byte boundary
+    static constexpr bool kParts = false, kInterleaved = true;
+    struct Args { CUtensorMap map; uint16_t* out; uint64_t ld; uint32_t bf16, align, by_box; };
+    const Args& a;
+    const RaggedJob& t;
+    uint32_t first, box, turn = 0;
+    __device__ RowsEpi(const Args& a_, const RaggedJob& t_, uint32_t row, uint32_t, uint32_t stage) : a(a_), t(t_), first(row - (threadIdx.x & 31)) {
+        const uint32_t w = (threadIdx.x >> 5) - 2, memory = stage - w * kWords * 4;            // of all warps
+        box = ((memory + kTableWords * 4 + 511) & ~511u) + w * 2 * kBox;
+    }
+    template <class Plan> __device__ bool begin(const Plan&, uint32_t) {
+        finish();                                    // the boxes are free
+        return true;
+    }
+    __device__ static void finish() {
+        if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+    }
+    // the warps that share a column take turns, 32 rows each: of a tile of few rows both have some
+    __device__ static uint32_t column(const RaggedJob&, uint32_t part, uint32_t c, uint32_t, uint32_t) { return 2 * c + 32 * part; }
+    __device__ static void load(uint32_t addr, float (&v)[32]) {
+        tmem_load_fragments(addr, v, 0);
+        tmem_load_fragments(addr + (16u << 16), v, 16);
+        asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+    }
+    __device__ void chunk(uint32_t col, float (&v)[32], bool) {
+        if (first >= t.M) return;
+        const uint32_t lane = threadIdx.x & 31, rows = t.N - col;
+#pragma unroll
+        for (uint32_t h = 0; h < 2; ++h) {           // 16 rows each
+            if (16 * h >= rows) break;
+            const uint32_t at = box + (turn & 1) * kBox;
+            if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");      // all but the other box' copy
+            __syncwarp();
+            ++turn;
+#pragma unroll
+            for (uint32_t j = 0; j < 2; ++j) {       // eight rows: four blocks of eight columns, one to every eight lanes' addresses
+                const uint32_t row = 8 * j + (lane & 7), to = at + row * 64 + (((lane >> 3) ^ (row >> 1 & 3)) << 4), i = 8 * h + 4 * j;
+                asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1, %2, %3, %4};" ::"r"(to), "r"(pack16(v[i], v[i + 1], a.bf16)),
+                             "r"(pack16(v[i + 2], v[i + 3], a.bf16)), "r"(pack16(v[16 + i], v[17 + i], a.bf16)), "r"(pack16(v[18 + i], v[19 + i], a.bf16)) : "memory");
+            }
+            if (a.by_box && rows >= 16 * h + 16) {
+                asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                __syncwarp();
+                if (lane == 0)
+                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&a.map), "r"(first),
+                                 "r"(t.first + col + 16 * h), "r"(at) : "memory");
+            } else {
+                __syncwarp();
+                by_lanes(at, t.first + col + 16 * h, rows - 16 * h < 16 ? rows - 16 * h : 16);
+            }
+            if (lane == 0) asm volatile("cp.async.bulk.commit_group;" ::: "memory");           // an empty one too: they are counted
+        }
+    }
+    __device__ void end() {}
+    // `rows` rows of the box at `at` to rows from `row` on: four lanes a row, 16 bytes each
+    __device__ __forceinline__ void by_lanes(uint32_t at, uint32_t row, uint32_t rows) {
+        const uint32_t lane = threadIdx.x & 31, c = lane & 3, col = first + 8 * c, there = col < t.M ? min(t.M - col, 8u) : 0;
+#pragma unroll
+        for (uint32_t r = lane >> 2; r < 16; r += 8) {
+            if (r >= rows || !there) continue;
+            const uint4 q = load_shared16(at + r * 64 + ((c ^ (r >> 1 & 3)) << 4));
+            uint16_t* o = a.out + (uint64_t)(row + r) * a.ld + col;
+            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
+            if (a.align == 16 && there == 8) {
+                *(uint4*)o = q;
+            } else if (a.align >= 4) {
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) {
+                    if (2 * i + 1 < there) *(uint32_t*)(o + 2 * i) = w[i];
+                    else if (2 * i < there) o[2 * i] = (uint16_t)w[i];
+                }
+            } else {
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i)
+                    if (i < there) o[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+            }
+        }
+        __syncwarp();
+    }
+};
+
 // y (or dx) by tiles of BN rows of the ragged side and 128 CG columns of the output
 template <int CG, int BN>
 struct RowsPlan {
-    CUtensorMap matrix, rows_map[5];                 // boxes of 128, 64, ... 8 rows
+    CUtensorMap matrix, rows_map[4];                 // boxes of 128, 64, 32 and 16 rows
     const int64_t* offsets;
     uint32_t groups, rows, features, tiles_m;        // tiles_m: of the features
     uint32_t k_stages, last_k;                       // K is the same for all tiles
@@ -114,72 +201,47 @@ struct RowsPlan {
         const uint32_t base = smem_u32(smem_raw), first = ((base + 1023u) & ~1023u) - base;
         return (const uint32_t*)(smem_raw + first + kTableOffset);
     }
-    static constexpr uint32_t kTableOffset = (232448 - (kTableWords + 7) / 8 * 8 * 4 - 1536) / (128 * 128 + BN / CG * 128) * (128 * 128 + BN / CG * 128);
-    template <int ROWS>
-    __device__ __forceinline__ uint32_t stage_bytes(const RaggedJob& j, uint32_t) const {
-        return 128 * ((mn ? 2 * k_rows : 128) + j.cols / CG);
-    }
-    template <int G, int ROWS>
-    __device__ __forceinline__ void load(const RaggedJob& j, uint32_t k, uint32_t rank, uint32_t sa, uint32_t sb, uint32_t bar) const {
-        const int k0 = (int)(k * kGemmK), feature = (int)(j.m * (128 * CG) + rank * 128);
-        if (mn) {
-            tma_load<CG>(sa, &matrix, bar, feature, k0, j.z);
-            tma_load<CG>(sa + 8192, &matrix, bar, feature + 64, k0, j.z);
-        } else {
-            tma_load<CG>(sa, &matrix, bar, k0, feature, j.z);
-        }
-        const uint32_t mine = j.cols / CG;           // a multiple of 16: the swizzle's groups of eight rows stay whole
-        uint32_t done = 0;
-#pragma unroll
-        for (uint32_t q = 0; q < 5; ++q) {
-            const uint32_t box = 128 >> q;
-            if (mine & box) {
-                tma_load<CG>(sb + done * 128, &rows_map[q], bar, k0, (int)(j.first + rank * mine + done), 0);
-                done += box;
+    static constexpr uint32_t kTableOffset = (232448 - RowsEpi::kWarps * RowsEpi::kWords * 4 - 1536) / (128 * 128 + BN / CG * 128) * (128 * 128 + BN / CG * 128);
+    // The rows come in two boxes at most: a thread has a stage's time, some 600 cycles, for all it does, and a third copy costs more of it than 16 rows too
+    // many cost to bring (112 rows are fetched as 128).
+    struct Feed {
+        const CUtensorMap *matrix, *first_map, *second_map;
+        int feature, z, row;
+        uint32_t first, total, mn;
+        __device__ __forceinline__ Feed(const RowsPlan& p, const RaggedJob& j, uint32_t rank) {
+            const uint32_t mine = j.cols / CG;       // a multiple of 16: the swizzle's groups of eight rows stay whole
+            uint32_t q = __clz(mine) - 24;           // the largest power of two in it: 128 >> q
+            uint32_t second = mine - (128 >> q);
+            if (second & (second - 1)) {             // not a power of two: 112 only
+                --q;
+                second = 0;
             }
+            first = 128 >> q;
+            total = 128 * ((p.mn ? 2 * p.k_rows : 128) + first + second);
+            first_map = &p.rows_map[q];
+            second_map = second ? &p.rows_map[__clz(second) - 24] : nullptr;
+            matrix = &p.matrix;
+            mn = p.mn;
+            feature = (int)(j.m * (128 * CG) + rank * 128);
+            z = j.z;
+            row = (int)(j.first + rank * mine);
         }
-    }
+        __device__ __forceinline__ uint32_t bytes(uint32_t) const { return total; }
+        __device__ __forceinline__ void copy(uint32_t k, uint32_t sa, uint32_t sb, uint32_t bar) const {
+            const int k0 = (int)(k * kGemmK);
+            if (mn) {
+                tma_load<CG>(sa, matrix, bar, feature, k0, z);
+                tma_load<CG>(sa + 8192, matrix, bar, feature + 64, k0, z);
+            } else {
+                tma_load<CG>(sa, matrix, bar, k0, feature, z);
+            }
+            tma_load<CG>(sb, first_map, bar, k0, row, 0);
+            if (second_map) tma_load<CG>(sb + first * 128, second_map, bar, k0, row + (int)first, 0);
+        }
+    };
     __device__ __forceinline__ bool wait(const TileJob&) const { return true; }
     __device__ __forceinline__ void done(const TileJob&) const {}
-    __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i == 0 ? &matrix : i < 6 ? &rows_map[i - 1] : nullptr; }
-};
-
-// A thread holds an output column (a row of the transposed tile) and 32 of the group's rows.
-struct RowsEpi {
-    static constexpr int kWarps = 8, kWords = (kTableWords + 7) / 8;         // not the epilogue's: the list of tiles
-    static constexpr bool kParts = false, kInterleaved = true;
-    struct Args { uint16_t* out; uint64_t ld; uint32_t bf16, paired; };      // paired: rows start on 4-byte boundaries
-    const Args& a;
-    const RaggedJob& t;
-    uint32_t feature;
-    __device__ RowsEpi(const Args& a_, const RaggedJob& t_, uint32_t row, uint32_t, uint32_t) : a(a_), t(t_), feature(row) {}
-    template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
-    // the warps that share a column take turns, 32 rows each: of a tile of few rows both have some
-    __device__ static uint32_t column(const RaggedJob&, uint32_t part, uint32_t c, uint32_t, uint32_t) { return 2 * c + 32 * part; }
-    __device__ void chunk(uint32_t col, float (&v)[32], bool) {
-        const uint32_t odd = threadIdx.x & 1, rows = t.N - col;
-        uint16_t* o = a.out + (uint64_t)(t.first + col) * a.ld;
-        if (a.paired) {
-            const bool both = (feature | 1) < t.M, last = !both && (feature & ~1u) < t.M;      // last: the last column of an odd number
-            o += (uint64_t)odd * a.ld + (feature & ~1u);
-#pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) {
-                const uint32_t mine = pack16(v[2 * i], v[2 * i + 1], a.bf16), other = __shfl_xor_sync(0xffffffffu, mine, 1);
-                const uint32_t word = odd ? __byte_perm(other, mine, 0x7632) : __byte_perm(mine, other, 0x5410);
-                if (2 * i + odd < rows) {
-                    uint16_t* at = o + 2 * i * a.ld;
-                    if (both) *(uint32_t*)at = word;
-                    else if (last) *at = (uint16_t)word;
-                }
-            }
-        } else if (feature < t.M) {
-#pragma unroll
-            for (uint32_t i = 0; i < 32; ++i)
-                if (i < rows) o[i * a.ld + feature] = (uint16_t)pack16(v[i], 0.0f, a.bf16);
-        }
-        __syncwarp();
-    }
-    __device__ void end() {}
+    __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i == 0 ? &matrix : i < 5 ? &rows_map[i - 1] : nullptr; }
 };
 
 // dW by tiles of 128 CG x BN of every matrix
@@ -211,38 +273,41 @@ struct MatrixPlan {
         j.part = part;
         return true;
     }
-    template <int ROWS>
-    __device__ __forceinline__ uint32_t stage_bytes(const RaggedJob& j, uint32_t k) const {
-        return 128 * (2 + ROWS / 64) * (k + 1 == j.k_stages ? j.last_rows : kGemmK);
-    }
-    // `count` rows from `row` on (a box of 64 >> q) to row `at` of the stage
-    template <int ROWS>
-    __device__ __forceinline__ void box(const RaggedJob& j, uint32_t q, int row, uint32_t at, uint32_t rank, uint32_t sa, uint32_t sb, uint32_t bar) const {
-        const int m = (int)(j.m * (128 * CG) + rank * 128), n = (int)(j.n * BN + rank * ROWS);
+    struct Feed {
+        const MatrixPlan& p;
+        int m, n, row, rows;
+        uint32_t stages, last_valid, last_rows;
+        static constexpr int kRows = BN / CG;
+        __device__ __forceinline__ Feed(const MatrixPlan& p_, const RaggedJob& j, uint32_t rank)
+            : p(p_), m((int)(j.m * (128 * CG) + rank * 128)), n((int)(j.n * BN + rank * kRows)), row((int)j.first), rows((int)p_.rows), stages(j.k_stages),
+              last_valid(j.last_valid), last_rows(j.last_rows) {}
+        __device__ __forceinline__ uint32_t bytes(uint32_t k) const { return 128 * (2 + kRows / 64) * (k + 1 == stages ? last_rows : kGemmK); }
+        // rows from `from` on (a box of 64 >> q) to row `at` of the stage
+        __device__ __forceinline__ void box(uint32_t q, int from, uint32_t at, uint32_t sa, uint32_t sb, uint32_t bar) const {
 #pragma unroll
-        for (int i = 0; i < 2; ++i) tma_load<CG>(sa + i * 8192 + at * 128, &a[q], bar, m + 64 * i, row, 0);
+            for (int i = 0; i < 2; ++i) tma_load<CG>(sa + i * 8192 + at * 128, &p.a[q], bar, m + 64 * i, from, 0);
 #pragma unroll
-        for (int i = 0; i < ROWS / 64; ++i) tma_load<CG>(sb + i * 8192 + at * 128, &b[q], bar, n + 64 * i, row, 0);
-    }
-    template <int G, int ROWS>
-    __device__ __forceinline__ void load(const RaggedJob& j, uint32_t k, uint32_t rank, uint32_t sa, uint32_t sb, uint32_t bar) const {
-        const uint32_t row = j.first + k * kGemmK;
-        if (k + 1 < j.k_stages || j.last_valid == kGemmK) {
-            box<ROWS>(j, 0, (int)row, 0, rank, sa, sb, bar);
-            return;
+            for (int i = 0; i < kRows / 64; ++i) tma_load<CG>(sb + i * 8192 + at * 128, &p.b[q], bar, n + 64 * i, from, 0);
         }
-        uint32_t at = 0;
-        for (uint32_t q = 1; q < 7; ++q)             // large boxes first: each begins at a multiple of its size
-            if (j.last_valid & (64u >> q)) {
-                box<ROWS>(j, q, (int)(row + at), at, rank, sa, sb, bar);
-                at += 64u >> q;
+        __device__ __forceinline__ void copy(uint32_t k, uint32_t sa, uint32_t sb, uint32_t bar) const {
+            const int from = row + (int)(k * kGemmK);
+            if (k + 1 < stages || last_valid == kGemmK) {
+                box(0, from, 0, sa, sb, bar);
+                return;
             }
-        for (uint32_t q = 6; at < j.last_rows; --q)  // zeros up to a multiple of 16, small boxes first
-            if (at & (64u >> q)) {
-                box<ROWS>(j, q, (int)rows, at, rank, sa, sb, bar);
-                at += 64u >> q;
-            }
-    }
+            uint32_t at = 0;
+            for (uint32_t q = 1; q < 7; ++q)             // large boxes first: each begins at a multiple of its size
+                if (last_valid & (64u >> q)) {
+                    box(q, from + (int)at, at, sa, sb, bar);
+                    at += 64u >> q;
+                }
+            for (uint32_t q = 6; at < last_rows; --q)    // zeros up to a multiple of 16, small boxes first
+                if (at & (64u >> q)) {
+                    box(q, rows, at, sa, sb, bar);
+                    at += 64u >> q;
+                }
+        }
+    };
     __device__ __forceinline__ bool wait(const TileJob&) const { return true; }
     __device__ __forceinline__ void done(const TileJob&) const {}
     __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i < 7 ? &a[i] : i < 14 ? &b[i - 7] : nullptr; }
@@ -265,6 +330,8 @@ struct MatrixEpi {
         store_tile32((uint8_t*)a.out + t.b * a.stride * type_bytes(), a.type, a.ld, row0, rows, col, t.N, v, a.align, stage, true, last);
     }
     __device__ void end() {}
+    __device__ static void finish() {}
+    __device__ static void load(uint32_t addr, float (&v)[32]) { tmem_load32(addr, v); }
     __device__ uint32_t type_bytes() const { return a.type == SK_F32 ? 4 : 2; }
 };
 
@@ -373,11 +440,12 @@ int launch_rows(const GroupedArgs& a, const void* matrix_rows, uint64_t ld_rows,
     const Operand w{a.weight, a.out, a.width, a.ld_weight, a.stride_weight, (uint32_t)a.groups, transposed};
     const Operand x{matrix_rows, a.rows, K, ld_rows, 0, 1, false};
     bool ok = encode_operand(&p.matrix, w, bf16, transposed ? p.k_rows : 128);
-    for (int q = 0; q < 5; ++q) ok = ok && encode_operand(&p.rows_map[q], x, bf16, 128 >> q);
+    for (int q = 0; q < 4; ++q) ok = ok && encode_operand(&p.rows_map[q], x, bf16, 128 >> q);
     if (!ok) return set_error(SK_ECUDA, "%s: the tensors cannot be described to the copy engine", __func__);
     // rows over BN of each segment, at most one tile more in each
     const uint64_t live = (a.groups < a.rows ? a.groups : a.rows) + (fill ? 2 : 0), most = (a.rows / BN + live) * p.tiles_m, slots = (uint64_t)dev.sm_count / CG;
-    const RowsEpi::Args ea{(uint16_t*)out, ld_out, bf16, (uintptr_t)out % 4 == 0 && ld_out % 2 == 0};
+    RowsEpi::Args ea{{}, (uint16_t*)out, ld_out, bf16, row_alignment(out, ld_out, a.type), addressable(out, ld_out)};
+    if (ea.by_box && !encode_rows_out(&ea.map, out, a.rows, p.features, ld_out, bf16)) return set_error(SK_ECUDA, "%s: the output cannot be described to the copy engine", __func__);
     SK_OP_CUDA((launch_plan<CG, BN, Plan, RowsEpi>(true, p, ea, (uint32_t)(most < slots ? most : slots), st)));
     return SK_OK;
 }
