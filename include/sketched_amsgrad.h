@@ -389,7 +389,7 @@ int sk_dropout(const void* x, uint64_t ld_x, const void* residual, uint64_t ld_r
  * tokens offsets[q] .. offsets[q + 1] - 1, tokens of no sequence take no part; NULL: one sequence of all tokens (sequences = 1).
  * norm (sequences fp32 out): what a token of the sequence counts: 1 / (tokens that take part), or, if average_sequences, 1 / (sequences with such
  * a token) / (such tokens of this sequence); 0 where there is none.  result (3 fp32 out): the sums over the tokens of norm times the token
- * loss (the loss), k, and 1 where the ratio is clipped.  Sums in a fixed order (same bits every time), in 64 bits beyond eight tokens. */
+ * loss (the loss), k, and 1 where the ratio is clipped.  Sums in a fixed order (same bits every time), in 64 bits beyond 2048 tokens. */
 uint64_t sk_policy_loss_workspace(uint64_t tokens, uint64_t sequences);
 int sk_policy_loss(const float* nll, const float* old_nll, const float* advantages, int advantage_of_sequences, const int64_t* targets,
                    const int64_t* offsets, uint64_t sequences, const float* reference_nll, uint64_t tokens, double clip_low, double clip_high,

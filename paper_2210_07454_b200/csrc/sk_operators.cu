@@ -408,6 +408,7 @@ static PolicyArgs policy_args(const float* nll, const float* old_nll, const floa
     a.nll = nll; a.old_nll = old_nll; a.advantages = advantages; a.advantage_of_sequences = advantage_of_sequences;
     a.targets = targets; a.offsets = offsets; a.sequences = sequences; a.reference = reference_nll; a.tokens = tokens;
     a.log_low = std::log1p(-clip_low); a.log_high = std::log1p(clip_high);
+    a.border_low = (float)a.log_low; a.border_high = (float)a.log_high;
     a.low = (float)(1.0 - clip_low); a.high = (float)(1.0 + clip_high); a.kl = (float)kl;
     return a;
 }

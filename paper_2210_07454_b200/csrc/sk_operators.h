@@ -292,6 +292,7 @@ struct PolicyArgs {
     uint64_t tokens, sequences;
     int advantage_of_sequences, average_sequences;
     double log_high, log_low;        // of the ratio's bounds
+    float border_high, border_low;   // the same, rounded
     float high, low, kl;
     float *result, *norm;            // forward: out
     const float* dloss;              // backward: may be null

@@ -6,8 +6,8 @@
 //   any and over their number in the sequence
 //   d loss / d nll = norm ([not clipped] A r + kl (exp e - 1))
 //
-// What is clipped is decided on d in 64 bits, where the difference of two 32-bit numbers is exact enough, so that the loss and its gradient, which are two
-// calls, and anyone who computes the formula decide alike.  A min(r, ...) instead of min(A r, ...): an infinite r with A = 0 is 0.
+// What is clipped is decided as on d in 64 bits, where the difference of two 32-bit numbers is exact enough, so that the loss and its gradient, which are
+// two calls, and anyone who computes the formula decide alike.  A min(r, ...) instead of min(A r, ...): an infinite r with A = 0 is 0.
 //
 // Tokens are taken in chunks of kChunk by a block each.  A chunk adds up what it has of each sequence; a sequence that goes over several chunks has
 // one sum where it begins (unless that is a chunk's first token) and one for each chunk whose first token is its own.  A second launch joins
@@ -28,62 +28,140 @@ __device__ __forceinline__ float k_term(float e) {
 }
 
 struct Token { float ratio, advantage; bool clipped; };
-__device__ __forceinline__ Token token_of(const PolicyArgs& a, uint64_t t, uint64_t sequence) {
-    const double d = (double)a.old_nll[t] - (double)a.nll[t];
+// The difference is rounded once, like the argument of exp; it says by itself what is clipped unless it lies within its rounding of the border.
+__device__ __forceinline__ Token token_of(const PolicyArgs& a, float old_nll, float nll, float advantage) {
+    const float d = old_nll - nll;
     Token v;
-    v.ratio = expf((float)d);
-    v.advantage = a.advantages[a.advantage_of_sequences ? sequence : t];
-    v.clipped = v.advantage >= 0 ? d > a.log_high : d < a.log_low;
+    v.ratio = expf(d);
+    v.advantage = advantage;
+    const bool up = advantage >= 0;
+    const float border = up ? a.border_high : a.border_low;
+    v.clipped = up ? d > border : d < border;
+    if (fabsf(d - border) <= 0x1p-21f * fabsf(border)) {
+        const double exact = (double)old_nll - (double)nll;
+        v.clipped = up ? exact > a.log_high : exact < a.log_low;
+    }
     return v;
 }
-__device__ __forceinline__ float drift_of(const PolicyArgs& a, uint64_t t) { return (float)((double)a.nll[t] - (double)a.reference[t]); }
 
-// The number of sequences that begin at or before token t, of those from `low` on that begin before `high`; less one, the token's own (or, behind the
-// last one's end, the number of sequences).
-__device__ __forceinline__ int64_t sequence_of(const int64_t* offsets, int64_t low, int64_t high, int64_t t) {
-    while (low < high) {                             // offsets[i] <= t for all i < low, > t for all i >= high
-        const int64_t middle = (low + high) >> 1;
-        if (offsets[middle] <= t) low = middle + 1;
-        else high = middle;
+// The number of sequences that begin at or before token t, less one: the token's own (or, behind the last one's end, the number of sequences; before
+// the first, -1).  By a whole warp: 32 probes at a time.
+__device__ __forceinline__ int64_t sequence_of(const int64_t* offsets, int64_t count, int64_t t) {
+    const int64_t lane = threadIdx.x & 31;
+    int64_t low = 0, high = count;                   // offsets[i] <= t for all i < low, > t for all i >= high
+    while (low < high) {
+        const int64_t step = (high - low + 31) / 32, at = low + (lane + 1) * step - 1;       // the ends of 32 pieces
+        const uint32_t under = __popc(__ballot_sync(0xffffffffu, at < high && offsets[at] <= t));
+        const int64_t from = low + under * step;
+        high = min(high, from + step - 1);
+        low = min(from, high);
     }
     return low - 1;
 }
 
-// the sequences of a chunk's first and last token
-struct Range { int64_t first, last; };
+// What a block knows of the sequences of its tokens, from the first token's to the last one's: where up to kHeld of them begin.
+constexpr int kHeld = 256;
+struct Range {
+    int64_t first, last;
+    const int64_t* begins;                           // of sequence first + i, in shared memory, or in the offsets where there are more
+};
 __device__ __forceinline__ Range range_of(const PolicyArgs& a, uint64_t c0, uint64_t c1) {
-    __shared__ int64_t found[2];
-    if (!a.offsets) return {0, 0};
-    if (threadIdx.x < 64 && (threadIdx.x & 31) == 0)
-        found[threadIdx.x >> 5] = sequence_of(a.offsets, 0, (int64_t)a.sequences + 1, (int64_t)(threadIdx.x ? c1 - 1 : c0));
+    __shared__ int64_t found[2], held[kHeld + 1];
+    if (!a.offsets) return {0, 0, nullptr};
+    const uint32_t warp = threadIdx.x >> 5;
+    if (warp < 2) {
+        const int64_t s = sequence_of(a.offsets, (int64_t)a.sequences + 1, (int64_t)(warp ? c1 - 1 : c0));
+        if ((threadIdx.x & 31) == 0) found[warp] = s;
+    }
     __syncthreads();
-    return {found[0], found[1]};
+    const int64_t first = found[0], last = found[1];
+    if (first >= last) return {first, first, nullptr};
+    if (last - first > kHeld) return {first, last, a.offsets + first};
+    for (int64_t i = threadIdx.x; i <= last - first; i += blockDim.x) held[i] = first + i >= 0 ? a.offsets[first + i] : 0;
+    __syncthreads();
+    return {first, last, held};
 }
-__device__ __forceinline__ int64_t own_sequence(const PolicyArgs& a, const Range& r, uint64_t t) {
-    return r.first == r.last ? r.first : sequence_of(a.offsets, r.first + 1, r.last + 1, (int64_t)t);
+__device__ __forceinline__ int64_t own_sequence(const Range& r, uint64_t t) {
+    int64_t low = 1, high = r.last - r.first + 1;    // begins[i] <= t for all i < low, > t for all i >= high
+    while (low < high) {
+        const int64_t middle = (low + high) >> 1;
+        if (r.begins[middle] <= (int64_t)t) low = middle + 1;
+        else high = middle;
+    }
+    return r.first + low - 1;
 }
 
+// kN tokens of a thread, kPolicyThreads apart from `t0` on: everything is loaded before anything is computed, of tokens that take no part too.
+template <uint32_t kN>
+struct Tokens {
+    float nll[kN], old_nll[kN], advantage[kN], reference[kN];
+    uint32_t sequence[kN];
+    bool live[kN];
+    __device__ __forceinline__ Tokens(const PolicyArgs& a, uint64_t t0, uint64_t end) {
+#pragma unroll
+        for (uint32_t i = 0; i < kN; ++i) {
+            const uint64_t t = t0 + i * kPolicyThreads;
+            live[i] = t < end;
+            nll[i] = live[i] ? a.nll[t] : 0;
+            old_nll[i] = live[i] ? a.old_nll[t] : 0;
+        }
+        if (a.reference) {
+#pragma unroll
+            for (uint32_t i = 0; i < kN; ++i) reference[i] = live[i] ? a.reference[t0 + i * kPolicyThreads] : 0;
+        }
+        if (!a.advantage_of_sequences) {
+#pragma unroll
+            for (uint32_t i = 0; i < kN; ++i) advantage[i] = live[i] ? a.advantages[t0 + i * kPolicyThreads] : 0;
+        }
+        if (a.targets) {
+#pragma unroll
+            for (uint32_t i = 0; i < kN; ++i) live[i] = live[i] && a.targets[t0 + i * kPolicyThreads] >= 0;
+        }
+    }
+    __device__ __forceinline__ void place(const PolicyArgs& a, const Range& r, uint64_t t0) {
+#pragma unroll
+        for (uint32_t i = 0; i < kN; ++i) {
+            const int64_t q = own_sequence(r, t0 + i * kPolicyThreads);
+            live[i] = live[i] && q >= 0 && q < (int64_t)a.sequences;
+            sequence[i] = live[i] ? (uint32_t)q : 0;
+        }
+        if (a.advantage_of_sequences) {
+#pragma unroll
+            for (uint32_t i = 0; i < kN; ++i) advantage[i] = live[i] ? a.advantages[sequence[i]] : 0;
+        }
+    }
+};
+
+// sums of a chunk in 32 bits, of chunks in 64
 struct Sums { double loss, k, clipped, count; };
 __device__ __forceinline__ void add(Sums& s, const Sums& o) { s.loss += o.loss; s.k += o.k; s.clipped += o.clipped; s.count += o.count; }
 __device__ __forceinline__ void add(Sums& s, const float4& o) { s.loss += o.x; s.k += o.y; s.clipped += o.z; s.count += o.w; }
-__device__ __forceinline__ void warp_sum(Sums& s) {
+__device__ __forceinline__ void add(float4& s, const float4& o) { s.x += o.x; s.y += o.y; s.z += o.z; s.w += o.w; }
+__device__ __forceinline__ Sums over(const Sums& s, int o) {
+    return {__shfl_xor_sync(0xffffffffu, s.loss, o), __shfl_xor_sync(0xffffffffu, s.k, o), __shfl_xor_sync(0xffffffffu, s.clipped, o),
+            __shfl_xor_sync(0xffffffffu, s.count, o)};
+}
+__device__ __forceinline__ float4 over(const float4& s, int o) {
+    return make_float4(__shfl_xor_sync(0xffffffffu, s.x, o), __shfl_xor_sync(0xffffffffu, s.y, o), __shfl_xor_sync(0xffffffffu, s.z, o),
+                       __shfl_xor_sync(0xffffffffu, s.w, o));
+}
+template <class T>
+__device__ __forceinline__ void warp_sum(T& s) {
 #pragma unroll
-    for (int o = 16; o; o >>= 1)
-        add(s, Sums{__shfl_xor_sync(0xffffffffu, s.loss, o), __shfl_xor_sync(0xffffffffu, s.k, o), __shfl_xor_sync(0xffffffffu, s.clipped, o),
-                    __shfl_xor_sync(0xffffffffu, s.count, o)});
+    for (int o = 16; o; o >>= 1) add(s, over(s, o));
 }
 // over the block, to every thread
-__device__ Sums block_sum(Sums s) {
-    __shared__ Sums parts[kPolicyJoin / 32];
+template <class T>
+__device__ T block_sum(T s) {
+    __shared__ T parts[kPolicyJoin / 32];
     warp_sum(s);
     __syncthreads();                                 // what was read before has been
     if ((threadIdx.x & 31) == 0) parts[threadIdx.x >> 5] = s;
     __syncthreads();
-    Sums r{};
+    T r{};
     for (uint32_t w = 0; w < blockDim.x / 32; ++w) add(r, parts[w]);
     return r;
 }
-__device__ __forceinline__ float4 narrow(const Sums& s) { return make_float4((float)s.loss, (float)s.k, (float)s.clipped, (float)s.count); }
 
 // workspace: chunks' sums (of all their tokens, or of their first token's sequence), then for each sequence the sum where it begins
 __device__ void join(const PolicyArgs& a, uint32_t chunks) {
@@ -144,53 +222,58 @@ __device__ void join(const PolicyArgs& a, uint32_t chunks) {
     }
 }
 
-__global__ void __launch_bounds__(kPolicyThreads) k_policy(const __grid_constant__ PolicyArgs a) {
+__global__ void __launch_bounds__(kPolicyThreads, 4) k_policy(const __grid_constant__ PolicyArgs a) {
     __shared__ float4 of_token[kChunk];
     chain_acquire();
     const uint64_t c0 = (uint64_t)blockIdx.x * kChunk, c1 = min(c0 + kChunk, a.tokens);
+    Tokens<kPerThread> t(a, c0 + threadIdx.x, c1);
     const Range r = range_of(a, c0, c1);
-    Sums s{};
-    {
-        float loss = 0, k = 0, clipped = 0, count = 0;
+    t.place(a, r, c0 + threadIdx.x);
+    float4 s = make_float4(0, 0, 0, 0);
 #pragma unroll
-        for (uint32_t i = 0; i < kPerThread; ++i) {
-            const uint32_t at = i * kPolicyThreads + threadIdx.x;
-            const uint64_t t = c0 + at;
-            float4 v = make_float4(0, 0, 0, 0);
-            if (t < c1) {
-                const int64_t q = own_sequence(a, r, t);
-                if (q >= 0 && q < (int64_t)a.sequences && (!a.targets || a.targets[t] >= 0)) {
-                    const Token p = token_of(a, t, (uint64_t)q);
-                    v.x = -p.advantage * (p.clipped ? (p.advantage >= 0 ? a.high : a.low) : p.ratio);
-                    if (a.reference) {
-                        v.y = k_term(drift_of(a, t));
-                        if (a.kl != 0) v.x += a.kl * v.y;
-                    }
-                    v.z = p.clipped;
-                    v.w = 1;
-                }
+    for (uint32_t i = 0; i < kPerThread; ++i) {
+        float4 v = make_float4(0, 0, 0, 0);
+        if (t.live[i]) {
+            const Token p = token_of(a, t.old_nll[i], t.nll[i], t.advantage[i]);
+            v.x = -p.advantage * (p.clipped ? (p.advantage >= 0 ? a.high : a.low) : p.ratio);
+            if (a.reference) {
+                v.y = k_term(t.nll[i] - t.reference[i]);
+                if (a.kl != 0) v.x += a.kl * v.y;
             }
-            if (a.average_sequences) of_token[at] = v;
-            loss += v.x; k += v.y; clipped += v.z; count += v.w;
+            v.z = p.clipped;
+            v.w = 1;
         }
-        s = Sums{loss, k, clipped, count};
+        if (a.average_sequences) of_token[i * kPolicyThreads + threadIdx.x] = v;
+        add(s, v);
     }
     const uint32_t chunks = gridDim.x;
     if (!a.average_sequences) {
         s = block_sum(s);
-        if (threadIdx.x == 0) a.workspace[blockIdx.x] = narrow(s);
+        if (threadIdx.x == 0) a.workspace[blockIdx.x] = s;
     } else {
         __syncthreads();
         const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-        for (int64_t q = r.first + warp; q <= r.last; q += kPolicyThreads / 32) {
-            if (q < 0 || q >= (int64_t)a.sequences) continue;
-            const int64_t begin = a.offsets ? a.offsets[q] : 0, end = a.offsets ? a.offsets[q + 1] : (int64_t)a.tokens;
-            const int64_t from = max(begin, (int64_t)c0), to = min(end, (int64_t)c1);
-            if (from >= to) continue;
-            Sums p{};
-            for (int64_t t = from + lane; t < to; t += 32) add(p, of_token[t - c0]);
-            warp_sum(p);
-            if (lane == 0) a.workspace[begin <= (int64_t)c0 ? blockIdx.x : chunks + q] = narrow(p);
+        uint32_t turn = warp;
+        for (int64_t q0 = r.first; q0 <= r.last; q0 += 32) {                                     // a lane finds each one's tokens, the warps take turns adding up
+            const int64_t q = q0 + lane;
+            int64_t from = 0, to = 0;
+            bool begins_here = false;
+            if (q >= 0 && q <= r.last && q < (int64_t)a.sequences) {
+                const int64_t begin = a.offsets ? a.offsets[q] : 0, end = a.offsets ? a.offsets[q + 1] : (int64_t)a.tokens;
+                from = max(begin, (int64_t)c0);
+                to = min(end, (int64_t)c1);
+                begins_here = begin > (int64_t)c0;
+            }
+            const uint32_t first = (uint32_t)(from - (int64_t)c0), count = from < to ? (uint32_t)(to - from) : 0;
+            for (uint32_t some = __ballot_sync(0xffffffffu, count > 0); some; some &= some - 1) {
+                if (turn++ % (kPolicyThreads / 32)) continue;
+                const int l = __ffs(some) - 1;
+                const uint32_t f = __shfl_sync(0xffffffffu, first, l), n = __shfl_sync(0xffffffffu, count, l);
+                float4 p = make_float4(0, 0, 0, 0);
+                for (uint32_t i = lane; i < n; i += 32) add(p, of_token[f + i]);
+                warp_sum(p);
+                if ((int)lane == l) a.workspace[begins_here ? chunks + q : blockIdx.x] = p;
+            }
         }
     }
     if (chunks > 1) return;
@@ -207,21 +290,24 @@ constexpr uint32_t kBackEach = 4;
 __global__ void __launch_bounds__(kPolicyThreads) k_policy_backward(const __grid_constant__ PolicyArgs a) {
     chain_acquire();
     const uint64_t c0 = (uint64_t)blockIdx.x * (kPolicyThreads * kBackEach), c1 = min(c0 + kPolicyThreads * kBackEach, a.tokens);
-    const Range r = range_of(a, c0, c1);
+    Tokens<kBackEach> t(a, c0 + threadIdx.x, c1);
     const float dloss = a.dloss ? *a.dloss : 1.0f;
+    const Range r = range_of(a, c0, c1);
+    t.place(a, r, c0 + threadIdx.x);
+    float norm[kBackEach];
+#pragma unroll
+    for (uint32_t i = 0; i < kBackEach; ++i) norm[i] = t.live[i] ? a.norm[t.sequence[i]] : 0;
 #pragma unroll
     for (uint32_t i = 0; i < kBackEach; ++i) {
-        const uint64_t t = c0 + i * kPolicyThreads + threadIdx.x;
-        if (t >= c1) break;
-        const int64_t q = own_sequence(a, r, t);
+        const uint64_t at = c0 + i * kPolicyThreads + threadIdx.x;
         float g = 0;
-        if (q >= 0 && q < (int64_t)a.sequences && (!a.targets || a.targets[t] >= 0)) {
-            const Token p = token_of(a, t, (uint64_t)q);
+        if (t.live[i]) {
+            const Token p = token_of(a, t.old_nll[i], t.nll[i], t.advantage[i]);
             g = p.clipped ? 0.0f : p.advantage * p.ratio;
-            if (a.reference && a.kl != 0) g += a.kl * expm1f(drift_of(a, t));
-            g *= dloss * a.norm[q];
+            if (a.reference && a.kl != 0) g += a.kl * expm1f(t.nll[i] - t.reference[i]);
+            g *= dloss * norm[i];
         }
-        a.dnll[t] = g;
+        if (at < c1) a.dnll[at] = g;
     }
 }
 
