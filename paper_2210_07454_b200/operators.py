@@ -15,6 +15,7 @@ A small call costs the host a few microseconds more than its kernels, so the che
 from __future__ import annotations
 
 import ctypes as C
+import functools
 
 import torch
 
@@ -61,6 +62,8 @@ def _tensor(t, name, types, device=None):
 
 def _ld(t, name):
     """Distance between the rows of a tensor of two or more dimensions, in elements."""
+    if t.is_contiguous():
+        return t.shape[-1] or 1
     rows, cols = t.shape[-2], t.shape[-1]
     if cols > 1 and t.stride(-1) != 1:
         raise SkError(f"{name}: the entries of a row must be contiguous")
@@ -144,6 +147,19 @@ def _elsewhere(device, fn, *args):
 def _need(device, size, *args):
     """Bytes of workspace, asked with the tensors' device current."""
     return size(*args) if _current_device() == device else _elsewhere(device, size, *args)
+
+
+@functools.lru_cache(maxsize=256)
+def _size(name, device, *sizes):
+    """What a workspace function of the library gives that depends on sizes and the device only."""
+    return _need(device, getattr(lib(), name), *sizes)
+
+
+def _new_on(device):
+    """What allocates uninitialised memory on the device of that index: f(shape, stride, dtype)"""
+    if _current_device() == device:
+        return _empty_here
+    return lambda shape, stride, dtype: torch.empty_strided(shape, stride, dtype=dtype, device=f"cuda:{device}")
 
 
 def _new(shape, stride, dtype, device):
@@ -397,13 +413,15 @@ def sort_by_expert(experts, groups, stream=None):
     wide = _tensor(experts, "experts", _INDEX)
     if not experts.is_contiguous():
         raise SkError("experts must be contiguous")
-    device, n = experts.get_device(), experts.numel()
     if groups < 1 or groups > 2048:
         raise SkError("groups must be in 1..2048")
-    order, offsets = _new((n,), (1,), torch.int64, device), _new((groups + 1,), (1,), torch.int64, device)
-    places = _new_like(experts, torch.int64, device)
-    need = _need(device, lib().sk_sort_by_expert_workspace, n, groups)
-    ws = _workspace(need, device)
+    device, shape = experts.get_device(), experts.shape
+    n = shape[0] if len(shape) == 1 else experts.numel()
+    new = _new_on(device)
+    order, offsets = new((n,), (1,), torch.int64), new((groups + 1,), (1,), torch.int64)
+    places = new((n,), (1,), torch.int64) if len(shape) == 1 else _new_like(experts, torch.int64, device)
+    need = _size("sk_sort_by_expert_workspace", device, n, groups)
+    ws = new((need,), (1,), torch.uint8) if need else None
     _run(device, lib().sk_sort_by_expert, experts.data_ptr(), wide, n, groups, order.data_ptr(), places.data_ptr(), offsets.data_ptr(), _p(ws), need,
          _raw_stream(device))
     return order, places, offsets
@@ -411,18 +429,22 @@ def sort_by_expert(experts, groups, stream=None):
 
 def _grouped(x, weight, offsets):
     """What both directions take: (device, code, rows, groups, width, out, ld_x, ld_w, stride_w, address of the offsets)"""
-    code, ld_x = _matrix(x, "x", _HALF)
+    code = _tensor(x, "x", _HALF)
     device = x.get_device()
     if _tensor(weight, "weight", _HALF, device) != code:
         raise SkError(f"x has type {x.dtype}, weight {weight.dtype}")
-    if weight.dim() != 3:
-        raise SkError(f"weight must have 3 dimensions, got {weight.dim()}")
+    if x.dim() != 2 or weight.dim() != 3:
+        raise SkError(f"x must have 2 dimensions and weight 3, got {x.dim()} and {weight.dim()}")
     (rows, width), (groups, out, other) = x.shape, weight.shape
     if width != other:
         raise SkError(f"x has width {width}, weight {other}")
     if groups < 1 or width < 1 or out < 1:
         raise SkError("the groups, the width and the outputs must not be empty")
-    return device, code, rows, groups, width, out, ld_x, _ld(weight, "weight"), weight.stride(0), _vector(offsets, "offsets", groups + 1, _INT64, device)
+    if weight.is_contiguous():
+        ld_w, s_w = width, out * width
+    else:
+        ld_w, s_w = _ld(weight, "weight"), weight.stride(0)
+    return device, code, rows, groups, width, out, width if x.is_contiguous() else _ld(x, "x"), ld_w, s_w, _vector(offsets, "offsets", groups + 1, _INT64, device)
 
 
 def grouped_linear(x, weight, offsets, out=None, stream=None):
@@ -432,8 +454,9 @@ def grouped_linear(x, weight, offsets, out=None, stream=None):
     if stream is not None:
         return _on(stream, lambda: grouped_linear(x, weight, offsets, out), x, weight, offsets, out)
     device, code, rows, groups, width, n, ld_x, ld_w, s_w, po = _grouped(x, weight, offsets)
+    new = _new_on(device)
     if out is None:
-        y, ld_y = _new((rows, n), (n, 1), x.dtype, device), n
+        y, ld_y = new((rows, n), (n, 1), x.dtype), n
     else:
         ycode, ld_y = _matrix(out, "out", _HALF, device)
         if ycode != code:
@@ -442,9 +465,10 @@ def grouped_linear(x, weight, offsets, out=None, stream=None):
             raise SkError(f"out must have the shape {(rows, n)}, got {tuple(out.shape)}")
         y = out
     px, pw = x.data_ptr(), weight.data_ptr()
-    need = _need(device, lib().sk_grouped_linear_workspace, px, ld_x, pw, ld_w, s_w, rows, groups, width, n)
-    ws = _workspace(need, device)
-    _run(device, lib().sk_grouped_linear, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, y.data_ptr(), ld_y, out is None, _p(ws), need,
+    L = lib()
+    need = _need(device, L.sk_grouped_linear_workspace, px, ld_x, pw, ld_w, s_w, rows, groups, width, n)
+    ws = new((need,), (1,), torch.uint8) if need else None
+    _run(device, L.sk_grouped_linear, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, y.data_ptr(), ld_y, out is None, _p(ws), need,
          _raw_stream(device))
     if out is not None:
         _wrote(out)
@@ -458,14 +482,13 @@ def grouped_linear_backward(dy, x, weight, offsets, dx=None, dweight=None, strea
     if stream is not None:
         return _on(stream, lambda: grouped_linear_backward(dy, x, weight, offsets, dx, dweight), dy, x, weight, offsets, dx, dweight)
     device, code, rows, groups, width, n, ld_x, ld_w, s_w, po = _grouped(x, weight, offsets)
-    dcode, ld_dy = _matrix(dy, "dy", _HALF, device)
-    if dcode != code:
+    if _tensor(dy, "dy", _HALF, device) != code:
         raise SkError(f"dy has type {dy.dtype}, x {x.dtype}")
     if dy.shape != (rows, n):
         raise SkError(f"dy must have the shape {(rows, n)}, got {tuple(dy.shape)}")
-    given_outputs, fill, ld_dx = (dx, dweight), dx is None, width
+    ld_dy, given_outputs, fill, ld_dx, new = n if dy.is_contiguous() else _ld(dy, "dy"), (dx, dweight), dx is None, width, _new_on(device)
     if dx is None:
-        dx = _new((rows, width), (width, 1), x.dtype, device)
+        dx = new((rows, width), (width, 1), x.dtype)
     elif dx is False:
         dx = None
     else:
@@ -475,7 +498,7 @@ def grouped_linear_backward(dy, x, weight, offsets, dx=None, dweight=None, strea
         _same_shape(dx, x, "dx")
     wcode, ld_dw, s_dw = code, width, n * width
     if dweight is None:
-        dweight = _new((groups, n, width), (n * width, width, 1), weight.dtype, device)
+        dweight = new((groups, n, width), (n * width, width, 1), x.dtype)
     elif dweight is False:
         dweight = None
     else:
@@ -483,11 +506,13 @@ def grouped_linear_backward(dy, x, weight, offsets, dx=None, dweight=None, strea
         _same_shape(dweight, weight, "dweight")
         ld_dw, s_dw = _ld(dweight, "dweight"), dweight.stride(0)
     pd, px, pw = dy.data_ptr(), x.data_ptr(), weight.data_ptr()
-    need = _need(device, lib().sk_grouped_linear_backward_workspace, pd, ld_dy, px, ld_x, pw, ld_w, s_w, rows, groups, width, n)
-    ws = _workspace(need, device)
-    _run(device, lib().sk_grouped_linear_backward, pd, ld_dy, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, _p(dx), ld_dx, fill, _p(dweight),
+    L = lib()
+    need = _need(device, L.sk_grouped_linear_backward_workspace, pd, ld_dy, px, ld_x, pw, ld_w, s_w, rows, groups, width, n)
+    ws = new((need,), (1,), torch.uint8) if need else None
+    _run(device, L.sk_grouped_linear_backward, pd, ld_dy, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, _p(dx), ld_dx, fill, _p(dweight),
          ld_dw, s_dw, wcode, _p(ws), need, _raw_stream(device))
-    _wrote(*given_outputs)
+    if given_outputs[0] is not None or given_outputs[1] is not None:
+        _wrote(*given_outputs)
     return dx, dweight
 
 
@@ -548,16 +573,18 @@ _OF = {"tokens": 0, "sequences": 1}
 def _policy(nll, old_nll, advantages, targets, offsets, reference_nll, clip, kl, advantage_of):
     """The arguments that both directions share, from nll to kl, and (device, tokens, sequences)"""
     _tensor(nll, "nll", _F32)
+    if not nll.is_contiguous():
+        raise SkError("nll must be contiguous")
     device, tokens = nll.get_device(), nll.numel()
-    pn, pold = _vector(nll, "nll", tokens, _F32, device), _vector(old_nll, "old_nll", tokens, _F32, device)
+    pn, pold = nll.data_ptr(), _vector(old_nll, "old_nll", tokens, _F32, device)
     pt = _vector(targets, "targets", tokens, _INT64, device) if targets is not None else None
     sequences, po = 1, None
     if offsets is not None:
         _tensor(offsets, "offsets", _INT64, device)
         sequences = offsets.numel() - 1
-        if sequences < 1:
-            raise SkError("offsets must hold at least 2 values")
-        po = _vector(offsets, "offsets", sequences + 1, _INT64, device)
+        if sequences < 1 or not offsets.is_contiguous():
+            raise SkError("offsets must be contiguous and hold at least 2 values")
+        po = offsets.data_ptr()
     of = _OF.get(advantage_of)
     if of is None:
         raise SkError(f"advantage_of must be 'tokens' or 'sequences', got {advantage_of!r}")
@@ -587,9 +614,10 @@ def policy_loss(nll, old_nll, advantages, targets=None, offsets=None, reference_
     args, device, tokens, sequences = _policy(nll, old_nll, advantages, targets, offsets, reference_nll, clip, kl, advantage_of)
     if average not in _OF:
         raise SkError(f"average must be 'tokens' or 'sequences', got {average!r}")
-    result, norm = _new((3,), (1,), torch.float32, device), _new((sequences,), (1,), torch.float32, device)
-    need = _need(device, lib().sk_policy_loss_workspace, tokens, sequences)
-    ws = _workspace(need, device)
+    new = _new_on(device)
+    result, norm = new((3,), (1,), torch.float32), new((sequences,), (1,), torch.float32)
+    need = _size("sk_policy_loss_workspace", device, tokens, sequences)
+    ws = new((need,), (1,), torch.uint8) if need else None
     _run(device, lib().sk_policy_loss, *args, _OF[average], result.data_ptr(), norm.data_ptr(), _p(ws), need, _raw_stream(device))
     return result, norm
 
