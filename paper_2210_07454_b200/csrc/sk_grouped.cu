@@ -244,28 +244,119 @@ struct RowsPlan {
     __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i == 0 ? &matrix : i < 5 ? &rows_map[i - 1] : nullptr; }
 };
 
-// dW by tiles of 128 CG x BN of every matrix
+// dW by tiles of 128 CG x BN of every matrix, the longest groups first; units take them up and down in turn, so that what one has too much in one round
+// it has too little in the next (in the groups' own order, 32 groups of 16384 rows kept one pair of blocks busy for 82,000 cycles and another for 55,000).
+// Where there are few tiles, K is split: the longest slice is made as short as it can be with as many slices as there are units, or twice as many. A group
+// in several slices leaves their sums in 32 bits in the workspace, and k_grouped_join adds them up in order.
+constexpr uint32_t kSorted = 256;                    // groups that are put in order, and may be split
+constexpr uint32_t kShortest = 8;                    // stages of a slice: it has to be worth its epilogue and its way through the workspace
 template <int CG, int BN>
 struct MatrixPlan {
     CUtensorMap a[7], b[7];                          // dy and x, boxes of 64, 32, ... 1 rows
     const int64_t* offsets;
     uint32_t groups, rows, M, N, tiles_m, tiles_n, bf16, part;
+    uint32_t most_slices;                            // of all groups together; 0: none is split
+    uint32_t* slices;                                // for each group their number, and that of the first one's sums
     Waits waits;
     static constexpr bool kCooperative = false, kEmpty = false, kThree = false, kRagged = true;
-    __device__ void prepare(void*) const {}
+    struct Table { uint16_t order[kSorted], first[kSorted + 1]; };       // groups by length, slices before each
+    __device__ static Table& table() {
+        __shared__ Table t;
+        return t;
+    }
+    __device__ __forceinline__ uint32_t length(uint32_t g) const {
+        const uint32_t from = bounded(offsets[g], rows), to = bounded(offsets[g + 1], rows);
+        return to > from ? to - from : 0;
+    }
+    __device__ void prepare(void* memory) const {
+        if (groups > kSorted) return;
+        uint32_t *stages = (uint32_t*)memory, *sorted = stages + kSorted;
+        for (uint32_t g = threadIdx.x; g < groups; g += blockDim.x) stages[g] = (length(g) + kGemmK - 1) / kGemmK;
+        __syncthreads();
+        for (uint32_t g = threadIdx.x; g < groups; g += blockDim.x) {
+            uint32_t rank = 0;
+            for (uint32_t h = 0; h < groups; ++h) rank += stages[h] > stages[g] || (stages[h] == stages[g] && h < g);
+            table().order[rank] = (uint16_t)g;
+            sorted[rank] = stages[g];
+        }
+        __syncthreads();
+        if (threadIdx.x >= 32) return;
+        const uint32_t lane = threadIdx.x, most = sorted[0];
+        auto count = [&](uint32_t longest) {         // slices, if none may be longer
+            uint32_t n = 0;
+            for (uint32_t r = lane; r < groups; r += 32) n += (sorted[r] + longest - 1) / longest;
+            return __reduce_add_sync(0xffffffffu, n);
+        };
+        uint32_t longest = max(most, 1u), best = ~0u;
+        if (most_slices) {
+            const uint32_t units = gridDim.x / CG, per = tiles_m * tiles_n;
+            for (uint32_t rounds = 1; rounds <= 2; ++rounds) {
+                const uint32_t fit = min(rounds * units / per, most_slices);
+                uint32_t low = 1, high = max(most, 1u);              // the least length that fits, if any does
+                if (count(high) > fit) continue;
+                while (low < high) {
+                    const uint32_t middle = (low + high) / 2;
+                    if (count(middle) <= fit) high = middle;
+                    else low = middle + 1;
+                }
+                low = max(low, min(kShortest, max(most, 1u)));
+                const uint32_t cost = rounds * (low + kTileCost);
+                if (cost < best) {
+                    best = cost;
+                    longest = low;
+                }
+            }
+        }
+        uint32_t before = 0;
+        for (uint32_t at = 0; at < groups; at += 32) {
+            const uint32_t r = at + lane, mine = r < groups ? max((sorted[r] + longest - 1) / longest, 1u) : 0;
+            uint32_t sum = mine;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const uint32_t u = __shfl_up_sync(0xffffffffu, sum, o);
+                if (lane >= o) sum += u;
+            }
+            if (r < groups) {
+                table().first[r] = (uint16_t)(before + sum - mine);
+                if (most_slices && blockIdx.x == 0) *(uint2*)(slices + 2 * table().order[r]) = make_uint2(mine, before + sum - mine);
+            }
+            before += __shfl_sync(0xffffffffu, sum, 31);
+        }
+        if (lane == 0) table().first[groups] = (uint16_t)before;
+    }
     __device__ __forceinline__ bool job(uint32_t p, uint32_t units, uint32_t i, RaggedJob& j) const {
-        const uint32_t t = p + i * units, per = tiles_m * tiles_n, g = t / per, q = t - g * per;
+        const uint32_t t = i * units + (i & 1 ? units - 1 - p : p), per = tiles_m * tiles_n, c = t / per, q = t - c * per;
+        uint32_t g = c, slice = 0, count = 1;
+        if (groups <= kSorted) {
+            const Table& order = table();
+            if (c >= order.first[groups]) return false;
+            uint32_t low = 0, high = groups;         // first[low] <= c < first[high]
+            if (order.first[groups] == groups) {
+                low = c;
+            } else {
+                while (high - low > 1) {
+                    const uint32_t middle = (low + high) / 2;
+                    if (order.first[middle] <= c) low = middle;
+                    else high = middle;
+                }
+            }
+            g = order.order[low];
+            slice = c - order.first[low];
+            count = order.first[low + 1] - order.first[low];
+        }
         if (g >= groups) return false;
-        const uint32_t from = bounded(offsets[g], rows), to = bounded(offsets[g + 1], rows), length = to > from ? to - from : 0;
+        const uint32_t from = bounded(offsets[g], rows), rest = length(g), stages = (rest + kGemmK - 1) / kGemmK, each = (stages + count - 1) / count;
+        const uint32_t valid = min(rest - slice * each * kGemmK, each * kGemmK);
         j.M = M;
         j.N = N;
         j.n = q / tiles_m;
         j.m = q - j.n * tiles_m;
         j.b = g;
-        j.first = from;
+        j.slice = count > 1 ? c + 1 : 0;             // c: what is split comes first, so this is the number of the slice among those of all groups
+        j.first = from + slice * each * kGemmK;
         j.cols = BN;
-        j.k_stages = (length + kGemmK - 1) / kGemmK;
-        j.last_valid = length - (j.k_stages ? j.k_stages - 1 : 0) * kGemmK;
+        j.k_stages = (valid + kGemmK - 1) / kGemmK;
+        j.last_valid = valid - (j.k_stages ? j.k_stages - 1 : 0) * kGemmK;
         j.last_rows = (j.last_valid + 15) & ~15u;
         j.k_rows = kGemmK;
         j.a_mn = j.b_mn = 1;
@@ -317,7 +408,7 @@ template <bool PARTS>
 struct MatrixEpi {
     static constexpr int kWarps = 8, kWords = kStageWords;
     static constexpr bool kParts = PARTS, kInterleaved = false;
-    struct Args { void* out; uint64_t ld, stride; int type; uint32_t align; };
+    struct Args { void* out; uint64_t ld, stride; int type; uint32_t align; float* sums; uint64_t ld_sums; };
     const Args& a;
     const RaggedJob& t;
     uint32_t row0, rows, stage;
@@ -327,6 +418,10 @@ struct MatrixEpi {
     __device__ static uint32_t column(const RaggedJob& t, uint32_t part, uint32_t c, uint32_t cols, uint32_t bn) { return t.n * bn + part * cols + c; }
     __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (!rows) return;
+        if (t.slice) {
+            store_tile32(a.sums + (uint64_t)(t.slice - 1) * t.M * a.ld_sums, SK_F32, a.ld_sums, row0, rows, col, (uint32_t)a.ld_sums, v, 16, stage, false, last);
+            return;
+        }
         store_tile32((uint8_t*)a.out + t.b * a.stride * type_bytes(), a.type, a.ld, row0, rows, col, t.N, v, a.align, stage, true, last);
     }
     __device__ void end() {}
@@ -334,6 +429,34 @@ struct MatrixEpi {
     __device__ static void load(uint32_t addr, float (&v)[32]) { tmem_load32(addr, v); }
     __device__ uint32_t type_bytes() const { return a.type == SK_F32 ? 4 : 2; }
 };
+
+// dW of the groups whose K was split, from the slices' sums in order
+__global__ void __launch_bounds__(256) k_grouped_join(const uint32_t* slices, const float* sums, uint64_t ld_sums, uint32_t groups, uint32_t M, uint32_t N, void* out,
+                                                      uint64_t ld, uint64_t stride, int type) {
+    chain_acquire();
+    const uint32_t quads = (N + 3) / 4;
+    const uint64_t total = (uint64_t)M * quads, step = (uint64_t)gridDim.x * 256;
+    for (uint32_t g = 0; g < groups; ++g) {
+        const uint2 s = *(const uint2*)(slices + 2 * g);
+        if (s.x < 2) continue;
+        const float* first = sums + (uint64_t)s.y * M * ld_sums;
+        for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < total; i += step) {
+            const uint64_t row = i / quads;
+            const uint32_t col = (uint32_t)(i - row * quads) * 4;
+            const float* p = first + row * ld_sums + col;
+            float4 v = *(const float4*)p;
+#pragma unroll 4
+            for (uint32_t k = 1; k < s.x; ++k) {
+                const float4 w = *(const float4*)(p + (uint64_t)k * M * ld_sums);
+                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+            }
+            const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+            for (uint32_t e = 0; e < 4; ++e)
+                if (col + e < N) store_as(out, type, g * stride + row * ld + col + e, f[e]);
+        }
+    }
+}
 
 // Rows of up to three batches of matrices copied to where TMA can address them, in one launch.  A thread copies eight neighbours: eight
 // loads on their way at once, one 16-byte store.
@@ -363,7 +486,18 @@ bool addressable(const void* p, uint64_t ld) { return (uintptr_t)p % 16 == 0 && 
 struct GroupedLayout {
     bool pack_x, pack_w, pack_dy;
     uint64_t ld_x, ld_w, ld_dy, off_x, off_w, off_dy, total;
+    bool wide;                                       // tiles of dW
+    uint32_t most_slices;                            // of the products that give dW, see MatrixPlan; 0: none is split
+    uint64_t off_slices, off_sums, ld_sums;
 };
+constexpr uint32_t kPlanSms = 148;                   // the slices, and with them the workspace, are planned for a B200
+bool wide_matrices(const GroupedArgs& a) {
+    const uint64_t stages = a.rows / a.groups / kGemmK + 1, slots = kPlanSms;
+    auto count = [&](uint64_t t) { return a.groups * ((a.out + t - 1) / t) * ((a.width + t - 1) / t); };
+    const uint64_t wide = (count(256) + slots / 2 - 1) / (slots / 2) * (stages + kTileCost) * 620 + 12000;
+    const uint64_t small = (count(128) + slots - 1) / slots * (stages + kTileCost) * 620 + 7000;
+    return wide <= small;
+}
 GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
     GroupedLayout l{};
     auto take = [&](bool pack, uint64_t rows, uint64_t ld) {
@@ -380,6 +514,18 @@ GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
     l.off_x = take(l.pack_x, a.rows, l.ld_x);
     l.off_dy = take(l.pack_dy, a.rows, l.ld_dy);
     l.off_w = take(l.pack_w, a.groups * a.out, l.ld_w);
+    if (backward) {
+        l.wide = wide_matrices(a);
+        const uint64_t tile = l.wide ? 256 : 128, tiles = ((a.out + tile - 1) / tile) * ((a.width + tile - 1) / tile), most = 2 * (kPlanSms / (l.wide ? 2 : 1)) / tiles;
+        // few groups of few tiles, and rows enough for two slices
+        if (most >= 2 && most >= a.groups && a.groups <= kSorted && a.rows > 2 * kShortest * kGemmK) {
+            l.most_slices = (uint32_t)most;
+            l.ld_sums = round_up(a.width, 32);
+            l.off_slices = l.total;
+            l.off_sums = l.off_slices + round_up(a.groups * 8, 256);
+            l.total = l.off_sums + round_up(most * a.out * l.ld_sums * 4, 256);
+        }
+    }
     return l;
 }
 
@@ -451,8 +597,9 @@ int launch_rows(const GroupedArgs& a, const void* matrix_rows, uint64_t ld_rows,
 }
 
 template <int CG, int BN, bool PARTS>
-int launch_matrices(const GroupedArgs& a, const OpDevice& dev, cudaStream_t st) {
+int launch_matrices(const GroupedArgs& a, const GroupedLayout& l, const OpDevice& dev, cudaStream_t st) {
     using Plan = MatrixPlan<CG, BN>;
+    static_assert(GemmTile<CG, BN, MatrixEpi<PARTS>>::kSmem + sizeof(typename Plan::Table) + 256 <= 232448);
     Plan p{};
     const bool bf16 = a.type == SK_BF16;
     p.offsets = a.offsets;
@@ -469,20 +616,18 @@ int launch_matrices(const GroupedArgs& a, const OpDevice& dev, cudaStream_t st) 
     bool ok = true;
     for (int q = 0; q < 7; ++q) ok = ok && encode_operand(&p.a[q], dy, bf16, 64 >> q) && encode_operand(&p.b[q], x, bf16, 64 >> q);
     if (!ok) return set_error(SK_ECUDA, "%s: the tensors cannot be described to the copy engine", __func__);
-    typename MatrixEpi<PARTS>::Args ea{a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type, 0};
+    p.most_slices = l.most_slices;
+    p.slices = (uint32_t*)((uint8_t*)a.workspace + l.off_slices);
+    typename MatrixEpi<PARTS>::Args ea{a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type, 0, (float*)((uint8_t*)a.workspace + l.off_sums), l.ld_sums};
     const uint32_t by_row = row_alignment(a.dweight, a.ld_dweight, a.dweight_type), by_matrix = row_alignment(a.dweight, a.stride_dweight, a.dweight_type);
     ea.align = a.groups > 1 && by_matrix < by_row ? by_matrix : by_row;
-    const uint64_t tiles = a.groups * p.tiles_m * p.tiles_n, slots = (uint64_t)dev.sm_count / CG;
+    const uint64_t tiles = (l.most_slices ? l.most_slices : a.groups) * p.tiles_m * p.tiles_n, slots = (uint64_t)dev.sm_count / CG;
     SK_OP_CUDA((launch_plan<CG, BN, Plan, MatrixEpi<PARTS>>(true, p, ea, (uint32_t)(tiles < slots ? tiles : slots), st)));
+    if (!l.most_slices) return SK_OK;
+    const uint64_t want = (a.out * ((a.width + 3) / 4) + 255) / 256, most = (uint64_t)dev.sm_count * 8;
+    SK_OP_CUDA(launch_kernel(true, k_grouped_join, dim3((uint32_t)(want < most ? want : most)), 256, 0, st, (const uint32_t*)p.slices, (const float*)ea.sums, l.ld_sums,
+                             p.groups, p.M, p.N, a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type));
     return SK_OK;
-}
-
-bool wide_matrices(const GroupedArgs& a, int sm_count) {
-    const uint64_t stages = a.rows / a.groups / kGemmK + 1, slots = (uint64_t)sm_count;
-    auto count = [&](uint64_t t) { return a.groups * ((a.out + t - 1) / t) * ((a.width + t - 1) / t); };
-    const uint64_t wide = (count(256) + slots / 2 - 1) / (slots / 2) * (stages + kTileCost) * 620 + 12000;
-    const uint64_t small = (count(128) + slots - 1) / slots * (stages + kTileCost) * 620 + 7000;
-    return wide <= small;
 }
 
 }  // namespace
@@ -505,10 +650,10 @@ int launch_grouped_backward(GroupedArgs a, const OpDevice& dev, cudaStream_t st)
     }
     if (!a.dweight) return SK_OK;
     // The accumulators' truncation grows with the rows added up: 16-bit gradients of fp16 and 32-bit ones show it, bf16's rounding is coarser.
-    const bool parts = a.dweight_type == SK_F32 || a.type == SK_F16, wide = wide_matrices(a, dev.sm_count);
-    auto launch = parts ? (wide ? launch_matrices<2, 256, true> : launch_matrices<1, 128, true>)
-                        : (wide ? launch_matrices<2, 256, false> : launch_matrices<1, 128, false>);
-    return launch(a, dev, st);
+    const bool parts = a.dweight_type == SK_F32 || a.type == SK_F16;
+    auto launch = parts ? (l.wide ? launch_matrices<2, 256, true> : launch_matrices<1, 128, true>)
+                        : (l.wide ? launch_matrices<2, 256, false> : launch_matrices<1, 128, false>);
+    return launch(a, l, dev, st);
 }
 
 }  // namespace sk

@@ -174,6 +174,16 @@ def test_long_groups_in_32_bits(ops, dtype):
     assert float(((dw[0].double() - want).abs() / want).max()) <= bound
 
 
+# few tiles and many rows: a group's rows are shared out among several blocks and the sums joined
+@pytest.mark.parametrize("dtype", HALF, ids=str)
+@pytest.mark.parametrize("sizes", [[1025], [6000], [5000, 0, 130, 2000], [64, 4097, 1, 63, 65, 0], [3000] * 5, [1030] + [7] * 40], ids=str)
+@pytest.mark.parametrize("width,out", [(64, 200), (300, 260), (333, 40), (768, 512)])
+def test_long_groups_of_small_matrices(ops, sizes, width, out, dtype):
+    e = ends(sizes, 5)
+    check(ops, e, e[-1] + 70, width, out, dtype)
+    check(ops, e, e[-1] + 70, width, out, dtype, dweight_type=torch.float32)
+
+
 def views(dtype, rows, cols, pad, offset, seed):
     """A matrix whose rows are cols + pad apart and begin off any boundary, and the same numbers alone"""
     whole = randn(seed, rows * (cols + pad) + offset, dtype=dtype)
