@@ -608,8 +608,8 @@ struct Operand {
 };
 
 bool encode_operand(CUtensorMap* map, const Operand& o, bool bf16, uint32_t box_rows);
-// an output that is written in boxes of 16 rows and 32 columns, 64-byte swizzle
-bool encode_rows_out(CUtensorMap* map, void* out, uint64_t rows, uint64_t cols, uint64_t ld, bool bf16);
+// outputs that are written in boxes of box_rows rows and 32 columns, with a swizzle as wide as that: 64 bytes, or 128 for fp32
+bool encode_out(CUtensorMap* map, void* out, uint64_t batch, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t stride, int type, uint32_t box_rows);
 
 // Launches a plan on at most `units` blocks or pairs.
 template <int CG, int BN, class Plan, class Epi>

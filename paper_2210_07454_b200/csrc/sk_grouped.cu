@@ -77,8 +77,8 @@ struct RowsEpi {
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                 __syncwarp();
                 if (lane == 0)
-                    asm volatile("cp.async.bulk.tensor.2d.global.shared::cta.tile.bulk_group [%0, {%1, %2}], [%3];" ::"l"(&a.map), "r"(first),
-                                 "r"(t.first + col + 16 * h), "r"(at) : "memory");
+                    asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(&a.map), "r"(first),
+                                 "r"(t.first + col + 16 * h), "r"(0), "r"(at) : "memory");
             } else {
                 __syncwarp();
                 by_lanes(at, t.first + col + 16 * h, rows - 16 * h < 16 ? rows - 16 * h : 16);
@@ -87,27 +87,35 @@ struct RowsEpi {
         }
     }
     __device__ void end() {}
-    // `rows` rows of the box at `at` to rows from `row` on: four lanes a row, 16 bytes each
+    // `rows` rows of the box at `at` to rows from `row` on, neighbouring lanes at neighbouring addresses: 16 bytes each, 4 or 2, as the rows are aligned
     __device__ __forceinline__ void by_lanes(uint32_t at, uint32_t row, uint32_t rows) {
-        const uint32_t lane = threadIdx.x & 31, c = lane & 3, col = first + 8 * c, there = col < t.M ? min(t.M - col, 8u) : 0;
+        const uint32_t lane = threadIdx.x & 31;
+        uint16_t* o = a.out + (uint64_t)row * a.ld + first;
+        const uint32_t there = min(t.M - first, 32u);            // columns
+        if (a.align == 16 && there == 32) {
 #pragma unroll
-        for (uint32_t r = lane >> 2; r < 16; r += 8) {
-            if (r >= rows || !there) continue;
-            const uint4 q = load_shared16(at + r * 64 + ((c ^ (r >> 1 & 3)) << 4));
-            uint16_t* o = a.out + (uint64_t)(row + r) * a.ld + col;
-            const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-            if (a.align == 16 && there == 8) {
-                *(uint4*)o = q;
-            } else if (a.align >= 4) {
+            for (uint32_t i = 0; i < 2; ++i) {
+                const uint32_t r = 8 * i + (lane >> 2), c = lane & 3;
+                if (r < rows) *(uint4*)(o + r * a.ld + 8 * c) = load_shared16(at + r * 64 + ((c ^ (r >> 1 & 3)) << 4));
+            }
+        } else if (a.align >= 4) {
+            const uint32_t c = lane & 15;                        // a pair of columns
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) {
-                    if (2 * i + 1 < there) *(uint32_t*)(o + 2 * i) = w[i];
-                    else if (2 * i < there) o[2 * i] = (uint16_t)w[i];
+            for (uint32_t i = 0; i < 8; ++i) {
+                const uint32_t r = 2 * i + (lane >> 4);
+                uint32_t w;
+                asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at + r * 64 + (((c >> 2) ^ (r >> 1 & 3)) << 4) + (c & 3) * 4) : "memory");
+                if (r < rows && 2 * c < there) {
+                    if (2 * c + 1 < there) *(uint32_t*)(o + r * a.ld + 2 * c) = w;
+                    else o[r * a.ld + 2 * c] = (uint16_t)w;
                 }
-            } else {
+            }
+        } else {
 #pragma unroll
-                for (uint32_t i = 0; i < 8; ++i)
-                    if (i < there) o[i] = (uint16_t)(w[i / 2] >> (16 * (i & 1)));
+            for (uint32_t r = 0; r < 16; ++r) {
+                uint16_t w;
+                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(w) : "r"(at + r * 64 + (((lane >> 3) ^ (r >> 1 & 3)) << 4) + (lane & 7) * 2) : "memory");
+                if (r < rows && lane < there) o[r * a.ld + lane] = w;
             }
         }
         __syncwarp();
@@ -404,79 +412,165 @@ struct MatrixPlan {
     __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i < 7 ? &a[i] : i < 14 ? &b[i - 7] : nullptr; }
 };
 
+// A lane holds a row of the output and 32 of its columns. They go out in boxes of 32 rows through the copy engine, 16-bit ones from two boxes in turn, or, where
+// that cannot write and for the sums of slices, by the lanes.
 template <bool PARTS>
 struct MatrixEpi {
     static constexpr int kWarps = 8, kWords = kStageWords;
     static constexpr bool kParts = PARTS, kInterleaved = false;
-    struct Args { void* out; uint64_t ld, stride; int type; uint32_t align; float* sums; uint64_t ld_sums; };
+    struct Args { CUtensorMap map; void* out; uint64_t ld, stride; int type; uint32_t align, by_box; float* sums; uint64_t ld_sums; };
     const Args& a;
     const RaggedJob& t;
-    uint32_t row0, rows, stage;
+    uint32_t row0, rows, stage, turn = 0;
     __device__ MatrixEpi(const Args& a_, const RaggedJob& t_, uint32_t row, uint32_t, uint32_t stage_)
         : a(a_), t(t_), row0(row - (threadIdx.x & 31)), stage(stage_) { rows = row0 >= t.M ? 0 : t.M - row0 < 32 ? t.M - row0 : 32; }
-    template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
+    template <class Plan> __device__ bool begin(const Plan&, uint32_t) {
+        finish();                                    // the boxes are free
+        return true;
+    }
+    __device__ static void finish() {
+        if ((threadIdx.x & 31) == 0) asm volatile("cp.async.bulk.wait_group.read 0;" ::: "memory");
+        __syncwarp();
+    }
     __device__ static uint32_t column(const RaggedJob& t, uint32_t part, uint32_t c, uint32_t cols, uint32_t bn) { return t.n * bn + part * cols + c; }
+    __device__ static void load(uint32_t addr, float (&v)[32]) { tmem_load32(addr, v); }
     __device__ void chunk(uint32_t col, float (&v)[32], bool last) {
         if (!rows) return;
         if (t.slice) {
             store_tile32(a.sums + (uint64_t)(t.slice - 1) * t.M * a.ld_sums, SK_F32, a.ld_sums, row0, rows, col, (uint32_t)a.ld_sums, v, 16, stage, false, last);
-            return;
+        } else if (!a.by_box) {
+            store_tile32((uint8_t*)a.out + t.b * a.stride * (a.type == SK_F32 ? 4 : 2), a.type, a.ld, row0, rows, col, t.N, v, a.align, stage, true, last);
+        } else {
+            const uint32_t lane = threadIdx.x & 31;
+            uint32_t at = stage;
+            if (a.type == SK_F32) {
+                finish();
+#pragma unroll
+                for (uint32_t i = 0; i < 8; ++i)
+                    store_shared16(at + lane * 128 + ((i ^ (lane & 7)) << 4), make_uint4(__float_as_uint(v[4 * i]), __float_as_uint(v[4 * i + 1]),
+                                                                                         __float_as_uint(v[4 * i + 2]), __float_as_uint(v[4 * i + 3])));
+            } else {
+                at += (turn++ & 1) * 2048;
+                if (lane == 0) asm volatile("cp.async.bulk.wait_group.read 1;" ::: "memory");  // all but the other box' copy
+                __syncwarp();
+                const bool bf16 = a.type == SK_BF16;
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i)
+                    store_shared16(at + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4), make_uint4(pack16(v[8 * i], v[8 * i + 1], bf16), pack16(v[8 * i + 2], v[8 * i + 3], bf16),
+                                                                                             pack16(v[8 * i + 4], v[8 * i + 5], bf16), pack16(v[8 * i + 6], v[8 * i + 7], bf16)));
+            }
+            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+            __syncwarp();
+            if (lane == 0) {
+                asm volatile("cp.async.bulk.tensor.3d.global.shared::cta.tile.bulk_group [%0, {%1, %2, %3}], [%4];" ::"l"(&a.map), "r"(col), "r"(row0), "r"(t.b), "r"(at)
+                             : "memory");
+                asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            }
         }
-        store_tile32((uint8_t*)a.out + t.b * a.stride * type_bytes(), a.type, a.ld, row0, rows, col, t.N, v, a.align, stage, true, last);
     }
     __device__ void end() {}
-    __device__ static void finish() {}
-    __device__ static void load(uint32_t addr, float (&v)[32]) { tmem_load32(addr, v); }
-    __device__ uint32_t type_bytes() const { return a.type == SK_F32 ? 4 : 2; }
 };
 
-// dW of the groups whose K was split, from the slices' sums in order
+// dW of the groups whose K was split: the sums of their slices, eight warps every eighth each, then those eight in order.
 __global__ void __launch_bounds__(256) k_grouped_join(const uint32_t* slices, const float* sums, uint64_t ld_sums, uint32_t groups, uint32_t M, uint32_t N, void* out,
                                                       uint64_t ld, uint64_t stride, int type) {
+    __shared__ float4 part[8][32];
     chain_acquire();
-    const uint32_t quads = (N + 3) / 4;
-    const uint64_t total = (uint64_t)M * quads, step = (uint64_t)gridDim.x * 256;
+    const uint32_t quads = (N + 3) / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint64_t total = (uint64_t)M * quads;
     for (uint32_t g = 0; g < groups; ++g) {
         const uint2 s = *(const uint2*)(slices + 2 * g);
         if (s.x < 2) continue;
         const float* first = sums + (uint64_t)s.y * M * ld_sums;
-        for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < total; i += step) {
-            const uint64_t row = i / quads;
+        for (uint64_t i0 = blockIdx.x * 32ull; i0 < total; i0 += gridDim.x * 32ull) {
+            const uint64_t i = i0 + lane, row = i / quads;
             const uint32_t col = (uint32_t)(i - row * quads) * 4;
-            const float* p = first + row * ld_sums + col;
-            float4 v = *(const float4*)p;
+            float4 v = make_float4(0, 0, 0, 0);
+            if (i < total) {
 #pragma unroll 4
-            for (uint32_t k = 1; k < s.x; ++k) {
-                const float4 w = *(const float4*)(p + (uint64_t)k * M * ld_sums);
-                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                for (uint32_t k = warp; k < s.x; k += 8) {
+                    const float4 w = *(const float4*)(first + row * ld_sums + col + (uint64_t)k * M * ld_sums);
+                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                }
             }
-            const float f[4] = {v.x, v.y, v.z, v.w};
+            part[warp][lane] = v;
+            __syncthreads();
+            if (warp < 4) {                          // a value of the four each
+                float f = 0;
 #pragma unroll
-            for (uint32_t e = 0; e < 4; ++e)
-                if (col + e < N) store_as(out, type, g * stride + row * ld + col + e, f[e]);
+                for (uint32_t k = 0; k < 8; ++k) f += ((const float*)&part[k][0])[warp * 32 + lane];
+                const uint64_t j = i0 + (warp * 32 + lane) / 4, r = j / quads;
+                const uint32_t c = (uint32_t)(j - r * quads) * 4 + (lane & 3);
+                if (j < total && c < N) store_as(out, type, g * stride + r * ld + c, f);
+            }
+            __syncthreads();
         }
     }
 }
 
-// Rows of up to three batches of matrices copied to where TMA can address them, in one launch.  A thread copies eight neighbours: eight
-// loads on their way at once, one 16-byte store.
-struct PackedOne { const uint16_t* src; uint16_t* dst; uint64_t ld, stride, rows, total; uint32_t cols, ld_dst, blocks; };      // total: rows of all matrices
+// Rows of up to three batches of matrices copied to where TMA can address them, in one launch. A thread makes 16 bytes of a row out of the two aligned
+// accesses that they lie in, wherever the row begins; at the ends of the tensor, where those would reach outside, and of a row, out of single values.
+struct PackedOne {
+    const uint16_t* src;
+    uint16_t* dst;
+    uint64_t ld, stride, total;                      // total: rows of all matrices
+    uint32_t rows, cols, ld_dst, blocks;
+};
 struct PackedArgs { PackedOne m[3]; };
+constexpr uint32_t kPackEach = 4;                    // of a thread, on their way at once
 __global__ void __launch_bounds__(256) k_grouped_pack(const __grid_constant__ PackedArgs a) {
     chain_acquire();
     uint32_t block = blockIdx.x, which = 0;
     while (block >= a.m[which].blocks) block -= a.m[which++].blocks;
     const PackedOne& m = a.m[which];
-    const uint32_t groups = m.ld_dst / 8;
-    const uint64_t total = m.total * groups, step = (uint64_t)m.blocks * 256;
-    for (uint64_t q = block * 256ull + threadIdx.x; q < total; q += step) {
-        const uint64_t r = q / groups, z = r / m.rows;
-        const uint32_t c = (uint32_t)(q - r * groups) * 8;
-        const uint16_t* s = m.src + z * m.stride + (r - z * m.rows) * m.ld + c;
-        uint32_t e[8];
+    const uint32_t pieces = m.ld_dst / 8;            // of 16 bytes in a row
+    uint32_t lanes = 32;                             // that share a row: so many that its pieces keep them busy
+    while (lanes > 1 && lanes / 2 >= pieces) lanes /= 2;
+    const uint32_t lane = threadIdx.x & (lanes - 1), each = 256 / lanes, total = (uint32_t)m.total;         // below 2^32 rows, by the workspace's size
+    const uint64_t begin = (uint64_t)(uintptr_t)m.src, end = begin + ((m.total / m.rows - 1) * m.stride + (m.rows - 1) * m.ld + m.cols) * 2;
+    for (uint64_t r64 = (uint64_t)block * each + threadIdx.x / lanes; r64 < total; r64 += (uint64_t)m.blocks * each) {
+        const uint32_t r = (uint32_t)r64, z = r / m.rows;
+        const uint16_t* row = m.src + z * m.stride + (r - z * m.rows) * m.ld;
+        uint4* to = (uint4*)(m.dst + (uint64_t)r * m.ld_dst);
+        const uint32_t by = (uint32_t)(uintptr_t)row & 15, more = by ? 1 : 0, shift = (by & 2) * 8;
+        const uint4* p = (const uint4*)((uintptr_t)row - by);
+        // pieces [low, high) lie in whole accesses inside the tensor
+        const uint32_t low = (uint64_t)(uintptr_t)p < begin, inside = (uint32_t)min((end - (uint64_t)(uintptr_t)p) / 16, (uint64_t)m.ld_dst);
+        const uint32_t high = min(m.cols / 8, inside > more ? inside - more : 0);
+        for (uint32_t c0 = lane; c0 < pieces; c0 += lanes * kPackEach) {
+            uint4 x[kPackEach], y[kPackEach];
 #pragma unroll
-        for (uint32_t i = 0; i < 8; ++i) e[i] = c + i < m.cols ? s[i] : 0;
-        *(uint4*)(m.dst + r * m.ld_dst + c) = make_uint4(e[0] | e[1] << 16, e[2] | e[3] << 16, e[4] | e[5] << 16, e[6] | e[7] << 16);
+            for (uint32_t e = 0; e < kPackEach; ++e) {
+                const uint32_t c = c0 + e * lanes;
+                if (c >= low && c < high) {
+                    x[e] = p[c];
+                    y[e] = p[c + more];
+                }
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < kPackEach; ++e) {
+                const uint32_t c = c0 + e * lanes;
+                if (c >= pieces) break;
+                if (c >= low && c < high) {
+                    uint32_t w[8] = {x[e].x, x[e].y, x[e].z, x[e].w, y[e].x, y[e].y, y[e].z, y[e].w};
+                    if (by & 8) {
+#pragma unroll
+                        for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+                    }
+                    if (by & 4) {
+#pragma unroll
+                        for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+                    }
+                    to[c] = make_uint4(__funnelshift_r(w[0], w[1], shift), __funnelshift_r(w[1], w[2], shift), __funnelshift_r(w[2], w[3], shift),
+                                       __funnelshift_r(w[3], w[4], shift));
+                } else {
+                    uint32_t v[8];
+#pragma unroll
+                    for (uint32_t i = 0; i < 8; ++i) v[i] = 8 * c + i < m.cols ? row[8 * c + i] : 0;
+                    to[c] = make_uint4(v[0] | v[1] << 16, v[2] | v[3] << 16, v[4] | v[5] << 16, v[6] | v[7] << 16);
+                }
+            }
+        }
     }
 }
 
@@ -535,15 +629,15 @@ int pack_operands(GroupedArgs& a, const GroupedLayout& l, int sm_count, cudaStre
     PackedArgs p{};
     uint32_t n = 0, blocks = 0;
     auto add = [&](const void*& src, uint64_t& ld, uint64_t stride, uint64_t rows, uint64_t total, uint64_t cols, uint64_t off, uint64_t ld_dst) {
-        const uint64_t want = (total * (ld_dst / 8) + 255) / 256, most = (uint64_t)sm_count * 16;
-        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, stride, rows, total, (uint32_t)cols, (uint32_t)ld_dst, (uint32_t)(want < most ? want : most)};
+        const uint64_t want = (total * (ld_dst / 8) + 255) / 256, most = (uint64_t)sm_count * 8;
+        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, stride, total, (uint32_t)rows, (uint32_t)cols, (uint32_t)ld_dst, (uint32_t)(want < most ? want : most)};
         blocks += p.m[n++].blocks;
         src = ws + off;
         ld = ld_dst;
     };
-    if (l.pack_x) add(a.x, a.ld_x, 0, a.rows, a.rows, a.width, l.off_x, l.ld_x);
+    if (l.pack_x && (a.y || a.dweight)) add(a.x, a.ld_x, 0, a.rows, a.rows, a.width, l.off_x, l.ld_x);
     if (l.pack_dy) add(a.dy, a.ld_dy, 0, a.rows, a.rows, a.out, l.off_dy, l.ld_dy);
-    if (l.pack_w) {
+    if (l.pack_w && (a.y || a.dx)) {
         add(a.weight, a.ld_weight, a.stride_weight, a.out, a.groups * a.out, a.width, l.off_w, l.ld_w);
         a.stride_weight = a.out * l.ld_w;
     }
@@ -591,7 +685,7 @@ int launch_rows(const GroupedArgs& a, const void* matrix_rows, uint64_t ld_rows,
     // rows over BN of each segment, at most one tile more in each
     const uint64_t live = (a.groups < a.rows ? a.groups : a.rows) + (fill ? 2 : 0), most = (a.rows / BN + live) * p.tiles_m, slots = (uint64_t)dev.sm_count / CG;
     RowsEpi::Args ea{{}, (uint16_t*)out, ld_out, bf16, row_alignment(out, ld_out, a.type), addressable(out, ld_out)};
-    if (ea.by_box && !encode_rows_out(&ea.map, out, a.rows, p.features, ld_out, bf16)) return set_error(SK_ECUDA, "%s: the output cannot be described to the copy engine", __func__);
+    if (ea.by_box && !encode_out(&ea.map, out, 1, a.rows, p.features, ld_out, a.rows * ld_out, a.type, 16)) return set_error(SK_ECUDA, "%s: the output cannot be described to the copy engine", __func__);
     SK_OP_CUDA((launch_plan<CG, BN, Plan, RowsEpi>(true, p, ea, (uint32_t)(most < slots ? most : slots), st)));
     return SK_OK;
 }
@@ -618,13 +712,17 @@ int launch_matrices(const GroupedArgs& a, const GroupedLayout& l, const OpDevice
     if (!ok) return set_error(SK_ECUDA, "%s: the tensors cannot be described to the copy engine", __func__);
     p.most_slices = l.most_slices;
     p.slices = (uint32_t*)((uint8_t*)a.workspace + l.off_slices);
-    typename MatrixEpi<PARTS>::Args ea{a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type, 0, (float*)((uint8_t*)a.workspace + l.off_sums), l.ld_sums};
+    typename MatrixEpi<PARTS>::Args ea{{}, a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type, 0, 0, (float*)((uint8_t*)a.workspace + l.off_sums), l.ld_sums};
+    const uint64_t size = type_size(a.dweight_type);
+    ea.by_box = ((uintptr_t)a.dweight | a.ld_dweight * size | (a.groups > 1 ? a.stride_dweight * size : 0)) % 16 == 0;
+    if (ea.by_box && !encode_out(&ea.map, a.dweight, a.groups, a.out, a.width, a.ld_dweight, a.groups > 1 ? a.stride_dweight : a.out * a.ld_dweight, a.dweight_type, 32))
+        return set_error(SK_ECUDA, "%s: the output cannot be described to the copy engine", __func__);
     const uint32_t by_row = row_alignment(a.dweight, a.ld_dweight, a.dweight_type), by_matrix = row_alignment(a.dweight, a.stride_dweight, a.dweight_type);
     ea.align = a.groups > 1 && by_matrix < by_row ? by_matrix : by_row;
     const uint64_t tiles = (l.most_slices ? l.most_slices : a.groups) * p.tiles_m * p.tiles_n, slots = (uint64_t)dev.sm_count / CG;
     SK_OP_CUDA((launch_plan<CG, BN, Plan, MatrixEpi<PARTS>>(true, p, ea, (uint32_t)(tiles < slots ? tiles : slots), st)));
     if (!l.most_slices) return SK_OK;
-    const uint64_t want = (a.out * ((a.width + 3) / 4) + 255) / 256, most = (uint64_t)dev.sm_count * 8;
+    const uint64_t want = (a.out * ((a.width + 3) / 4) + 31) / 32, most = (uint64_t)dev.sm_count * 8;
     SK_OP_CUDA(launch_kernel(true, k_grouped_join, dim3((uint32_t)(want < most ? want : most)), 256, 0, st, (const uint32_t*)p.slices, (const float*)ea.sums, l.ld_sums,
                              p.groups, p.M, p.N, a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type));
     return SK_OK;

@@ -53,11 +53,13 @@ bool encode_operand(CUtensorMap* map, const Operand& o, bool bf16, uint32_t box_
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-bool encode_rows_out(CUtensorMap* map, void* out, uint64_t rows, uint64_t cols, uint64_t ld, bool bf16) {
-    const cuuint64_t dims[2] = {cols, rows}, strides[1] = {ld * 2};
-    const cuuint32_t box[2] = {32, 16}, elem[2] = {1, 1};
-    return g_encode.load()(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 2, out, dims, strides, box, elem,
-                           CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_64B, CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+bool encode_out(CUtensorMap* map, void* out, uint64_t batch, uint64_t rows, uint64_t cols, uint64_t ld, uint64_t stride, int type, uint32_t box_rows) {
+    const uint64_t size = type_size(type);
+    const cuuint64_t dims[3] = {cols, rows, batch}, strides[2] = {ld * size, stride * size};
+    const cuuint32_t box[3] = {32, box_rows, 1}, elem[3] = {1, 1, 1};
+    const CUtensorMapDataType t = type == SK_F32 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : type == SK_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16;
+    return g_encode.load()(map, t, 3, out, dims, strides, box, elem, CU_TENSOR_MAP_INTERLEAVE_NONE, type == SK_F32 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B,
+                           CU_TENSOR_MAP_L2_PROMOTION_NONE, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
 namespace {
