@@ -27,6 +27,28 @@ constexpr uint32_t kTableWords = 2 * (kSegments + 1);
 // The group boundaries as the kernels take them: never decreasing, never outside 0..rows, whatever the offsets hold.
 __device__ __forceinline__ uint32_t bounded(int64_t v, uint32_t rows) { return v < 0 ? 0 : v > (int64_t)rows ? rows : (uint32_t)v; }
 
+// 16 rows of 64 bytes in shared memory (64-byte swizzle) to rows that begin anywhere: every row's aligned words, two rows at a time, then the values before
+// and behind those, of all rows at once. (Single values throughout take twice the stores: dweight of 5001 rows of 1001 x 1500 53 us.)
+__device__ __forceinline__ void store_unaligned(uint32_t at, uint16_t* o, uint64_t ld, uint32_t rows, uint32_t there) {
+    const uint32_t lane = threadIdx.x & 31, c = lane & 15;
+    const uint32_t odd0 = (uint32_t)((uintptr_t)o >> 1) & 1, step = (uint32_t)ld & 1;                  // row r begins off a word if odd0 + r step is odd
+#pragma unroll
+    for (uint32_t i = 0; i < 8; ++i) {
+        const uint32_t r = 2 * i + (lane >> 4), odd = (odd0 + r * step) & 1;
+        uint32_t w;
+        asm volatile("ld.shared.b32 %0, [%1];" : "=r"(w) : "r"(at + r * 64 + (((c >> 2) ^ (r >> 1 & 3)) << 4) + (c & 3) * 4) : "memory");
+        const uint32_t next = __shfl_down_sync(0xffffffffu, w, 1);
+        if (odd) w = __byte_perm(w, next, 0x5432);   // columns 2 c + 1 and 2 c + 2
+        if (r < rows && 2 * c + odd + 1 < there && !(odd && c == 15)) *(uint32_t*)(o + r * ld + 2 * c + odd) = w;
+    }
+    const uint32_t r = c, odd = (odd0 + r * step) & 1, last = there - 1, col = lane < 16 ? 0 : last;
+    if (r < rows && (lane < 16 ? odd : (there - odd) & 1)) {
+        uint16_t w;
+        asm volatile("ld.shared.b16 %0, [%1];" : "=h"(w) : "r"(at + r * 64 + (((col >> 3) ^ (r >> 1 & 3)) << 4) + (col & 7) * 2) : "memory");
+        o[r * ld + col] = w;
+    }
+}
+
 // A warp holds 32 output columns (rows of the transposed tile) and takes 32 of the group's rows at a time, as fragments that the transposing stores to shared
 // memory turn round: 16 rows of 64 bytes are written as one box by the copy engine, or, where it cannot write (the last rows of a group, outputs it cannot address),
 // by the lanes.  Two boxes take turns.
@@ -111,12 +133,7 @@ struct RowsEpi {
                 }
             }
         } else {
-#pragma unroll
-            for (uint32_t r = 0; r < 16; ++r) {
-                uint16_t w;
-                asm volatile("ld.shared.b16 %0, [%1];" : "=h"(w) : "r"(at + r * 64 + (((lane >> 3) ^ (r >> 1 & 3)) << 4) + (lane & 7) * 2) : "memory");
-                if (r < rows && lane < there) o[r * a.ld + lane] = w;
-            }
+            store_unaligned(at, o, a.ld, rows, there);
         }
         __syncwarp();
     }
@@ -438,7 +455,7 @@ struct MatrixEpi {
         if (!rows) return;
         if (t.slice) {
             store_tile32(a.sums + (uint64_t)(t.slice - 1) * t.M * a.ld_sums, SK_F32, a.ld_sums, row0, rows, col, (uint32_t)a.ld_sums, v, 16, stage, false, last);
-        } else if (!a.by_box) {
+        } else if (!a.by_box && (a.type == SK_F32 || a.align >= 4)) {
             store_tile32((uint8_t*)a.out + t.b * a.stride * (a.type == SK_F32 ? 4 : 2), a.type, a.ld, row0, rows, col, t.N, v, a.align, stage, true, last);
         } else {
             const uint32_t lane = threadIdx.x & 31;
@@ -458,6 +475,15 @@ struct MatrixEpi {
                 for (uint32_t i = 0; i < 4; ++i)
                     store_shared16(at + lane * 64 + ((i ^ (lane >> 1 & 3)) << 4), make_uint4(pack16(v[8 * i], v[8 * i + 1], bf16), pack16(v[8 * i + 2], v[8 * i + 3], bf16),
                                                                                              pack16(v[8 * i + 4], v[8 * i + 5], bf16), pack16(v[8 * i + 6], v[8 * i + 7], bf16)));
+            }
+            if (!a.by_box) {
+                __syncwarp();
+                uint16_t* o = (uint16_t*)a.out + t.b * a.stride + (uint64_t)row0 * a.ld + col;
+                const uint32_t there = min(t.N - col, 32u);
+                store_unaligned(at, o, a.ld, min(rows, 16u), there);
+                if (rows > 16) store_unaligned(at + 1024, o + 16 * a.ld, a.ld, rows - 16, there);
+                __syncwarp();
+                return;
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
             __syncwarp();
