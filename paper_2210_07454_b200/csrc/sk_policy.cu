@@ -19,12 +19,24 @@ namespace sk {
 namespace {
 
 constexpr uint32_t kPolicyThreads = 256, kPerThread = 8, kChunk = kPolicyThreads * kPerThread;
-constexpr uint32_t kPolicyJoin = 1024;
+constexpr uint32_t kPolicyJoin = 1024;               // threads of the second launch, at most
 
-// exp(e) - e - 1: near 0 the three cancel, and the series takes over
+// exp(e) - e - 1. Below 1 the series, in which nothing cancels (the next term is 2e-9 of the sum); beyond, exp, whose error is at most three times as large
+// relative to the difference. exp(e) - 1 is this plus e.
 __device__ __forceinline__ float k_term(float e) {
-    const float s = 1.0f + e * (1.0f / 3) * (1.0f + e * 0.25f * (1.0f + e * 0.2f * (1.0f + e * (1.0f / 6) * (1.0f + e * (1.0f / 7) * (1.0f + e * 0.125f)))));
-    return fabsf(e) < 0.35f ? 0.5f * e * e * s : expm1f(e) - e;
+    float s = 1.0f / 39916800;
+    s = fmaf(s, e, 1.0f / 3628800);
+    s = fmaf(s, e, 1.0f / 362880);
+    s = fmaf(s, e, 1.0f / 40320);
+    s = fmaf(s, e, 1.0f / 5040);
+    s = fmaf(s, e, 1.0f / 720);
+    s = fmaf(s, e, 1.0f / 120);
+    s = fmaf(s, e, 1.0f / 24);
+    s = fmaf(s, e, 1.0f / 6);
+    s = fmaf(s, e, 0.5f);
+    s *= e * e;
+    if (!(fabsf(e) < 1.0f)) s = expf(e) - e - 1.0f;
+    return s;
 }
 
 struct Token { float ratio, advantage; bool clipped; };
@@ -59,75 +71,86 @@ __device__ __forceinline__ int64_t sequence_of(const int64_t* offsets, int64_t c
     return low - 1;
 }
 
-// What a block knows of the sequences of its tokens, from the first token's to the last one's: where up to kHeld of them begin.
-constexpr int kHeld = 256;
+// What a block knows of the sequences of its tokens, from the first token's to the last one's: where they begin, counted from its first token, if they
+// are few; else they are looked up in the offsets.
+constexpr uint32_t kHeld = 256;
 struct Range {
     int64_t first, last;
-    const int64_t* begins;                           // of sequence first + i, in shared memory, or in the offsets where there are more
+    uint32_t count;                                  // of those that begin inside
+    const uint32_t* begins;                          // null: too many
 };
 __device__ __forceinline__ Range range_of(const PolicyArgs& a, uint64_t c0, uint64_t c1) {
-    __shared__ int64_t found[2], held[kHeld + 1];
-    if (!a.offsets) return {0, 0, nullptr};
+    __shared__ int64_t found[2];
+    __shared__ uint32_t held[kHeld];
+    if (!a.offsets) return {0, 0, 0, held};
     const uint32_t warp = threadIdx.x >> 5;
     if (warp < 2) {
         const int64_t s = sequence_of(a.offsets, (int64_t)a.sequences + 1, (int64_t)(warp ? c1 - 1 : c0));
         if ((threadIdx.x & 31) == 0) found[warp] = s;
     }
     __syncthreads();
-    const int64_t first = found[0], last = found[1];
-    if (first >= last) return {first, first, nullptr};
-    if (last - first > kHeld) return {first, last, a.offsets + first};
-    for (int64_t i = threadIdx.x; i <= last - first; i += blockDim.x) held[i] = first + i >= 0 ? a.offsets[first + i] : 0;
-    __syncthreads();
-    return {first, last, held};
+    const int64_t first = found[0], last = max(found[1], first);         // offsets that decrease are no reason to look anywhere else
+    if (last - first > (int64_t)kHeld) return {first, last, 0, nullptr};
+    const uint32_t count = (uint32_t)(last - first);
+    if (count) {
+        for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) held[i] = (uint32_t)max(a.offsets[first + 1 + i] - (int64_t)c0, (int64_t)0);
+        __syncthreads();
+    }
+    return {first, last, count, held};
 }
-__device__ __forceinline__ int64_t own_sequence(const Range& r, uint64_t t) {
-    int64_t low = 1, high = r.last - r.first + 1;    // begins[i] <= t for all i < low, > t for all i >= high
+// of token c0 + at
+__device__ __forceinline__ int64_t own_sequence(const PolicyArgs& a, const Range& r, uint64_t c0, uint32_t at) {
+    if (!r.begins) {
+        int64_t low = r.first + 1, high = r.last + 1;        // offsets[i] <= token for all i < low, > for all i >= high
+        while (low < high) {
+            const int64_t middle = (low + high) >> 1;
+            if (a.offsets[middle] <= (int64_t)(c0 + at)) low = middle + 1;
+            else high = middle;
+        }
+        return low - 1;
+    }
+    uint32_t low = 0, high = r.count;
     while (low < high) {
-        const int64_t middle = (low + high) >> 1;
-        if (r.begins[middle] <= (int64_t)t) low = middle + 1;
+        const uint32_t middle = (low + high) >> 1;
+        if (r.begins[middle] <= at) low = middle + 1;
         else high = middle;
     }
-    return r.first + low - 1;
+    return r.first + low;
 }
 
-// kN tokens of a thread, kPolicyThreads apart from `t0` on: everything is loaded before anything is computed, of tokens that take no part too.
+// kN tokens of a thread, kPolicyThreads apart: everything is loaded before anything is computed, of tokens that take no part too.
 template <uint32_t kN>
 struct Tokens {
     float nll[kN], old_nll[kN], advantage[kN], reference[kN];
     uint32_t sequence[kN];
-    bool live[kN];
-    __device__ __forceinline__ Tokens(const PolicyArgs& a, uint64_t t0, uint64_t end) {
+    uint32_t live;                                   // a bit each
+    __device__ __forceinline__ void load(float (&v)[kN], const float* p, uint32_t rest) {
 #pragma unroll
-        for (uint32_t i = 0; i < kN; ++i) {
-            const uint64_t t = t0 + i * kPolicyThreads;
-            live[i] = t < end;
-            nll[i] = live[i] ? a.nll[t] : 0;
-            old_nll[i] = live[i] ? a.old_nll[t] : 0;
-        }
-        if (a.reference) {
-#pragma unroll
-            for (uint32_t i = 0; i < kN; ++i) reference[i] = live[i] ? a.reference[t0 + i * kPolicyThreads] : 0;
-        }
-        if (!a.advantage_of_sequences) {
-#pragma unroll
-            for (uint32_t i = 0; i < kN; ++i) advantage[i] = live[i] ? a.advantages[t0 + i * kPolicyThreads] : 0;
-        }
-        if (a.targets) {
-#pragma unroll
-            for (uint32_t i = 0; i < kN; ++i) live[i] = live[i] && a.targets[t0 + i * kPolicyThreads] >= 0;
-        }
+        for (uint32_t i = 0; i < kN; ++i) v[i] = i * kPolicyThreads < rest ? p[i * kPolicyThreads] : 0.0f;
     }
-    __device__ __forceinline__ void place(const PolicyArgs& a, const Range& r, uint64_t t0) {
+    __device__ __forceinline__ Tokens(const PolicyArgs& a, uint64_t c0, uint64_t c1) {
+        const uint64_t t0 = c0 + threadIdx.x;
+        const uint32_t rest = t0 < c1 ? (uint32_t)(c1 - t0) : 0;
+        load(nll, a.nll + t0, rest);
+        load(old_nll, a.old_nll + t0, rest);
+        if (a.reference) load(reference, a.reference + t0, rest);
+        if (!a.advantage_of_sequences) load(advantage, a.advantages + t0, rest);
+        live = 0;
+        const int64_t* targets = a.targets + (a.targets ? t0 : 0);
+#pragma unroll
+        for (uint32_t i = 0; i < kN; ++i)
+            if (i * kPolicyThreads < rest && (!a.targets || targets[i * kPolicyThreads] >= 0)) live |= 1u << i;
+    }
+    __device__ __forceinline__ void place(const PolicyArgs& a, const Range& r, uint64_t c0) {
 #pragma unroll
         for (uint32_t i = 0; i < kN; ++i) {
-            const int64_t q = own_sequence(r, t0 + i * kPolicyThreads);
-            live[i] = live[i] && q >= 0 && q < (int64_t)a.sequences;
-            sequence[i] = live[i] ? (uint32_t)q : 0;
+            const int64_t q = own_sequence(a, r, c0, i * kPolicyThreads + threadIdx.x);
+            if (q < 0 || q >= (int64_t)a.sequences) live &= ~(1u << i);
+            sequence[i] = live >> i & 1 ? (uint32_t)q : 0;
         }
         if (a.advantage_of_sequences) {
 #pragma unroll
-            for (uint32_t i = 0; i < kN; ++i) advantage[i] = live[i] ? a.advantages[sequence[i]] : 0;
+            for (uint32_t i = 0; i < kN; ++i) advantage[i] = a.advantages[sequence[i]];      // there is at least one sequence
         }
     }
 };
@@ -226,14 +249,14 @@ __global__ void __launch_bounds__(kPolicyThreads, 4) k_policy(const __grid_const
     __shared__ float4 of_token[kChunk];
     chain_acquire();
     const uint64_t c0 = (uint64_t)blockIdx.x * kChunk, c1 = min(c0 + kChunk, a.tokens);
-    Tokens<kPerThread> t(a, c0 + threadIdx.x, c1);
+    Tokens<kPerThread> t(a, c0, c1);
     const Range r = range_of(a, c0, c1);
-    t.place(a, r, c0 + threadIdx.x);
+    t.place(a, r, c0);
     float4 s = make_float4(0, 0, 0, 0);
 #pragma unroll
     for (uint32_t i = 0; i < kPerThread; ++i) {
         float4 v = make_float4(0, 0, 0, 0);
-        if (t.live[i]) {
+        if (t.live >> i & 1) {
             const Token p = token_of(a, t.old_nll[i], t.nll[i], t.advantage[i]);
             v.x = -p.advantage * (p.clipped ? (p.advantage >= 0 ? a.high : a.low) : p.ratio);
             if (a.reference) {
@@ -290,21 +313,24 @@ constexpr uint32_t kBackEach = 4;
 __global__ void __launch_bounds__(kPolicyThreads) k_policy_backward(const __grid_constant__ PolicyArgs a) {
     chain_acquire();
     const uint64_t c0 = (uint64_t)blockIdx.x * (kPolicyThreads * kBackEach), c1 = min(c0 + kPolicyThreads * kBackEach, a.tokens);
-    Tokens<kBackEach> t(a, c0 + threadIdx.x, c1);
+    Tokens<kBackEach> t(a, c0, c1);
     const float dloss = a.dloss ? *a.dloss : 1.0f;
     const Range r = range_of(a, c0, c1);
-    t.place(a, r, c0 + threadIdx.x);
+    t.place(a, r, c0);
     float norm[kBackEach];
 #pragma unroll
-    for (uint32_t i = 0; i < kBackEach; ++i) norm[i] = t.live[i] ? a.norm[t.sequence[i]] : 0;
+    for (uint32_t i = 0; i < kBackEach; ++i) norm[i] = a.norm[t.sequence[i]];
 #pragma unroll
     for (uint32_t i = 0; i < kBackEach; ++i) {
         const uint64_t at = c0 + i * kPolicyThreads + threadIdx.x;
         float g = 0;
-        if (t.live[i]) {
+        if (t.live >> i & 1) {
             const Token p = token_of(a, t.old_nll[i], t.nll[i], t.advantage[i]);
             g = p.clipped ? 0.0f : p.advantage * p.ratio;
-            if (a.reference && a.kl != 0) g += a.kl * expm1f(t.nll[i] - t.reference[i]);
+            if (a.reference && a.kl != 0) {
+                const float e = t.nll[i] - t.reference[i];
+                g += a.kl * (k_term(e) + e);
+            }
             g *= dloss * norm[i];
         }
         if (at < c1) a.dnll[at] = g;
@@ -320,7 +346,9 @@ uint64_t policy_workspace(uint64_t tokens, uint64_t sequences) { return (chunks_
 int launch_policy(const PolicyArgs& a, cudaStream_t st) {
     const uint32_t chunks = (uint32_t)chunks_of(a.tokens);
     SK_OP_CUDA(launch_kernel(true, k_policy, dim3(chunks), kPolicyThreads, 0, st, a));
-    if (chunks > 1) SK_OP_CUDA(launch_kernel(true, k_policy_join, dim3(1), kPolicyJoin, 0, st, a, chunks));
+    // a thread a sequence; sums over the chunks need few
+    const uint32_t threads = a.average_sequences && a.sequences > kPolicyThreads ? kPolicyJoin : kPolicyThreads;
+    if (chunks > 1) SK_OP_CUDA(launch_kernel(true, k_policy_join, dim3(1), threads, 0, st, a, chunks));
     return SK_OK;
 }
 
