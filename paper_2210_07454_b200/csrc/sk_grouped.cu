@@ -497,7 +497,9 @@ struct MatrixEpi {
     __device__ void end() {}
 };
 
-// dW of the groups whose K was split: the sums of their slices, eight warps every eighth each, then those eight in order.
+// dW of the groups whose K was split: the sums of their slices in order, by a thread for four columns where that keeps the GPU busy, else by eight warps every eighth
+// each and then those eight in order (2 groups of 30000 rows of 64 x 200: 30 us by single threads, 18; 16384 rows of 768 x 2048: 55, and 72 by eight warps).
+constexpr uint64_t kManyQuads = 1 << 17;
 __global__ void __launch_bounds__(256) k_grouped_join(const uint32_t* slices, const float* sums, uint64_t ld_sums, uint32_t groups, uint32_t M, uint32_t N, void* out,
                                                       uint64_t ld, uint64_t stride, int type) {
     __shared__ float4 part[8][32];
@@ -508,6 +510,24 @@ __global__ void __launch_bounds__(256) k_grouped_join(const uint32_t* slices, co
         const uint2 s = *(const uint2*)(slices + 2 * g);
         if (s.x < 2) continue;
         const float* first = sums + (uint64_t)s.y * M * ld_sums;
+        if (total >= kManyQuads) {
+            for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < total; i += gridDim.x * 256ull) {
+                const uint64_t row = i / quads;
+                const uint32_t col = (uint32_t)(i - row * quads) * 4;
+                const float* p = first + row * ld_sums + col;
+                float4 v = *(const float4*)p;
+#pragma unroll 4
+                for (uint32_t k = 1; k < s.x; ++k) {
+                    const float4 w = *(const float4*)(p + (uint64_t)k * M * ld_sums);
+                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+                }
+                const float f[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+                for (uint32_t e = 0; e < 4; ++e)
+                    if (col + e < N) store_as(out, type, g * stride + row * ld + col + e, f[e]);
+            }
+            continue;
+        }
         for (uint64_t i0 = blockIdx.x * 32ull; i0 < total; i0 += gridDim.x * 32ull) {
             const uint64_t i = i0 + lane, row = i / quads;
             const uint32_t col = (uint32_t)(i - row * quads) * 4;
@@ -611,12 +631,25 @@ struct GroupedLayout {
     uint64_t off_slices, off_sums, ld_sums;
 };
 constexpr uint32_t kPlanSms = 148;                   // the slices, and with them the workspace, are planned for a B200
+// How many slices all groups of dW may be cut into, 0: K is not split. Few groups of few tiles, and rows enough for two slices.
+uint64_t slices_of(const GroupedArgs& a, bool wide) {
+    const uint64_t tile = wide ? 256 : 128, tiles = ((a.out + tile - 1) / tile) * ((a.width + tile - 1) / tile), most = 2 * (kPlanSms / (wide ? 2 : 1)) / tiles;
+    return most >= 2 && most >= a.groups && a.groups <= kSorted && a.rows > 2 * kShortest * kGemmK ? most : 0;
+}
+// Pairs of blocks or single ones: the one that is through first, at some 600 cycles a stage, if the groups are of one length (see wide_tiles for the constants).
 bool wide_matrices(const GroupedArgs& a) {
-    const uint64_t stages = a.rows / a.groups / kGemmK + 1, slots = kPlanSms;
-    auto count = [&](uint64_t t) { return a.groups * ((a.out + t - 1) / t) * ((a.width + t - 1) / t); };
-    const uint64_t wide = (count(256) + slots / 2 - 1) / (slots / 2) * (stages + kTileCost) * 620 + 12000;
-    const uint64_t small = (count(128) + slots - 1) / slots * (stages + kTileCost) * 620 + 7000;
-    return wide <= small;
+    auto cycles = [&](bool wide) {
+        const uint64_t tile = wide ? 256 : 128, units = kPlanSms / (wide ? 2 : 1), tiles = ((a.out + tile - 1) / tile) * ((a.width + tile - 1) / tile);
+        const uint64_t stages = a.rows / kGemmK + a.groups;
+        uint64_t longest = (a.groups * tiles + units - 1) / units * (stages / a.groups + kTileCost);
+        if (slices_of(a, wide))
+            for (uint64_t rounds = 1; rounds <= 2; ++rounds) {
+                const uint64_t slices = rounds * units / tiles, each = slices >= a.groups ? rounds * (stages / slices + 1 + kTileCost) : longest;
+                if (each < longest) longest = each;
+            }
+        return longest * 620 + (wide ? 12000 : 7000);
+    };
+    return cycles(true) <= cycles(false);
 }
 GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
     GroupedLayout l{};
@@ -636,14 +669,12 @@ GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
     l.off_w = take(l.pack_w, a.groups * a.out, l.ld_w);
     if (backward) {
         l.wide = wide_matrices(a);
-        const uint64_t tile = l.wide ? 256 : 128, tiles = ((a.out + tile - 1) / tile) * ((a.width + tile - 1) / tile), most = 2 * (kPlanSms / (l.wide ? 2 : 1)) / tiles;
-        // few groups of few tiles, and rows enough for two slices
-        if (most >= 2 && most >= a.groups && a.groups <= kSorted && a.rows > 2 * kShortest * kGemmK) {
-            l.most_slices = (uint32_t)most;
+        l.most_slices = (uint32_t)slices_of(a, l.wide);
+        if (l.most_slices) {
             l.ld_sums = round_up(a.width, 32);
             l.off_slices = l.total;
             l.off_sums = l.off_slices + round_up(a.groups * 8, 256);
-            l.total = l.off_sums + round_up(most * a.out * l.ld_sums * 4, 256);
+            l.total = l.off_sums + round_up(l.most_slices * a.out * l.ld_sums * 4, 256);
         }
     }
     return l;
