@@ -355,7 +355,11 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
         if (m) asm volatile("prefetch.tensormap [%0];" ::"l"(m) : "memory");
     }
 
-    chain_acquire();
+    // A ragged product may begin while the one before it in the stream, whose results it does not need, still runs: that one's blocks have all passed their
+    // own chain_acquire() by now, so whatever was launched before it is complete. The wait is made up for at the end.
+    bool waited = true;
+    if constexpr (Plan::kRagged) waited = !plan.beside;
+    if (waited) chain_acquire();
     // the grid fits the SMs, so it is resident as a whole: the next kernel's blocks may take the slots that are free
     chain_release();
 
@@ -587,6 +591,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
         }
         if constexpr (Plan::kRagged) Epi::finish();
     }
+    if (!waited) chain_acquire();
 
     asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
     __syncthreads();

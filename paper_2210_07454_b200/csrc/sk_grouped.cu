@@ -146,6 +146,7 @@ struct RowsPlan {
     const int64_t* offsets;
     uint32_t groups, rows, features, tiles_m;        // tiles_m: of the features
     uint32_t k_stages, last_k;                       // K is the same for all tiles
+    uint32_t beside;                                 // no
     uint32_t mn, k_rows, bf16, fill;                 // mn: the matrix is read along its rows; fill: rows of no group become zero
     Waits waits;
     static constexpr bool kCooperative = false, kEmpty = false, kThree = false, kRagged = true;
@@ -281,6 +282,7 @@ struct MatrixPlan {
     const int64_t* offsets;
     uint32_t groups, rows, M, N, tiles_m, tiles_n, bf16, part;
     uint32_t most_slices;                            // of all groups together; 0: none is split
+    uint32_t beside;                                 // it may run beside the kernel before it, the product that gives dx
     uint32_t* slices;                                // for each group their number, and that of the first one's sums
     Waits waits;
     static constexpr bool kCooperative = false, kEmpty = false, kThree = false, kRagged = true;
@@ -768,6 +770,7 @@ int launch_matrices(const GroupedArgs& a, const GroupedLayout& l, const OpDevice
     for (int q = 0; q < 7; ++q) ok = ok && encode_operand(&p.a[q], dy, bf16, 64 >> q) && encode_operand(&p.b[q], x, bf16, 64 >> q);
     if (!ok) return set_error(SK_ECUDA, "%s: the tensors cannot be described to the copy engine", __func__);
     p.most_slices = l.most_slices;
+    p.beside = a.dx != nullptr;
     p.slices = (uint32_t*)((uint8_t*)a.workspace + l.off_slices);
     typename MatrixEpi<PARTS>::Args ea{{}, a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type, 0, 0, (float*)((uint8_t*)a.workspace + l.off_sums), l.ld_sums};
     const uint64_t size = type_size(a.dweight_type);
