@@ -276,7 +276,7 @@ uint64_t sk_grouped_linear_workspace(const void* x, uint64_t ld_x, const void* w
     GroupedArgs a{};
     a.x = x; a.ld_x = ld_x; a.weight = weight; a.ld_weight = ld_weight; a.stride_weight = stride_weight;
     a.rows = rows; a.groups = groups; a.width = width; a.out = out;
-    return rows ? grouped_workspace(a, false) : 0;
+    return rows && groups && width && out ? grouped_workspace(a, false) : 0;
 }
 
 int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight, int type, uint64_t rows, uint64_t groups,
@@ -304,7 +304,7 @@ uint64_t sk_grouped_linear_backward_workspace(const void* dy, uint64_t ld_dy, co
     GroupedArgs a{};
     a.dy = dy; a.ld_dy = ld_dy; a.x = x; a.ld_x = ld_x; a.weight = weight; a.ld_weight = ld_weight; a.stride_weight = stride_weight;
     a.rows = rows; a.groups = groups; a.width = width; a.out = out;
-    return rows ? grouped_workspace(a, true) : 0;
+    return rows && groups && width && out ? grouped_workspace(a, true) : 0;
 }
 
 int sk_grouped_linear_backward(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight,

@@ -59,6 +59,17 @@ def test_grouped_linear_backward_checks(L):
         assert refused(L, call(**kw), word), kw
 
 
+def test_sizes_of_nothing(L):
+    """Questions about empty extents are answered, whatever the call itself would say."""
+    for rows, groups, width, out in ((0, 2, 8, 8), (4, 0, 8, 8), (4, 2, 0, 8), (4, 2, 8, 0)):
+        assert L.sk_grouped_linear_workspace(P + 2, 9, Q, 9, 64, rows, groups, width, out) == 0
+        assert L.sk_grouped_linear_backward_workspace(P + 2, 9, P, 9, Q, 9, 64, rows, groups, width, out) == 0
+    assert L.sk_sort_by_expert_workspace(0, 4) == 0 and L.sk_sort_by_expert_workspace(10, 0) == 0 and L.sk_sort_by_expert_workspace(10, 5000) == 0
+    # few tiles and many rows: the sums of the slices, below 80 MB whatever the sizes
+    for width, out, groups in ((64, 200, 2), (768, 2048, 1), (256, 64, 30)):
+        assert 0 < L.sk_grouped_linear_backward_workspace(P, out, P, width, Q, width, out * width, 30000, groups, width, out) < (80 << 20)
+
+
 def test_sort_by_expert_checks(L):
     def call(e=P, bits=64, n=10, groups=4, order=Q, places=R, off=2 * R):
         return L.sk_sort_by_expert(e, bits, n, groups, order, places, off, None, 0, None)
