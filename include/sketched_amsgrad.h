@@ -346,7 +346,7 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
  * address).  Rows of no group (before offsets[0], from offsets[groups] on): zero if fill, else left as they were.
  * Sums are the tensor cores' 32-bit ones.  1 <= groups <= 2048; rows <= 2^30; 1 <= width, out <= 2^20.  y may not be x or weight. */
 uint64_t sk_grouped_linear_workspace(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight,
-                                     uint64_t rows, uint64_t groups, uint64_t width, uint64_t out);
+                                     uint64_t rows, uint64_t groups, uint64_t width, uint64_t out, const void* y, uint64_t ld_y);
 int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight, int type, uint64_t rows,
                       uint64_t groups, uint64_t width, uint64_t out, const int64_t* offsets, void* y, uint64_t ld_y, int fill, void* workspace,
                       uint64_t workspace_bytes, void* stream);
@@ -357,7 +357,8 @@ int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t
  * between them; for bf16 in the tensor cores' accumulators alone, whose truncation stays below its rounding.  No output may be an input. */
 uint64_t sk_grouped_linear_backward_workspace(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight,
                                               uint64_t ld_weight, uint64_t stride_weight, uint64_t rows, uint64_t groups, uint64_t width,
-                                              uint64_t out);
+                                              uint64_t out, const void* dx, uint64_t ld_dx, const void* dweight, uint64_t ld_dweight,
+                                              uint64_t stride_dweight, int dweight_type);
 int sk_grouped_linear_backward(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight,
                                uint64_t stride_weight, int type, uint64_t rows, uint64_t groups, uint64_t width, uint64_t out,
                                const int64_t* offsets, void* dx, uint64_t ld_dx, int fill, void* dweight, uint64_t ld_dweight,

@@ -86,11 +86,11 @@ def lib() -> C.CDLL:
         L.sk_orthogonalize.restype = ci
         L.sk_orthogonalize.argtypes = [vp, u64, u64, ci, vp, u64, u64, f32, ci, vp, u64, u64, ci, u64, u64, u64, ci, vp, f32, vp, u64, vp]
         f64 = C.c_double
-        L.sk_grouped_linear_workspace.restype = u64; L.sk_grouped_linear_workspace.argtypes = [vp, u64, vp, u64, u64, u64, u64, u64, u64]
+        L.sk_grouped_linear_workspace.restype = u64; L.sk_grouped_linear_workspace.argtypes = [vp, u64, vp, u64, u64, u64, u64, u64, u64, vp, u64]
         L.sk_grouped_linear.restype = ci
         L.sk_grouped_linear.argtypes = [vp, u64, vp, u64, u64, ci, u64, u64, u64, u64, vp, vp, u64, ci, vp, u64, vp]
         L.sk_grouped_linear_backward_workspace.restype = u64
-        L.sk_grouped_linear_backward_workspace.argtypes = [vp, u64, vp, u64, vp, u64, u64, u64, u64, u64, u64]
+        L.sk_grouped_linear_backward_workspace.argtypes = [vp, u64, vp, u64, vp, u64, u64, u64, u64, u64, u64, vp, u64, vp, u64, u64, ci]
         L.sk_grouped_linear_backward.restype = ci
         L.sk_grouped_linear_backward.argtypes = [vp, u64, vp, u64, vp, u64, u64, ci, u64, u64, u64, u64, vp, vp, u64, ci, vp, u64, u64, ci, vp, u64, vp]
         L.sk_sort_by_expert_workspace.restype = u64; L.sk_sort_by_expert_workspace.argtypes = [u64, u64]

@@ -314,7 +314,7 @@ struct GemmTile {
 // Plan: job(unit, units, i, job): the unit's i-th tile; wait(job): until its operands are there; done(job): called by every epilogue warp
 // when its share of the tile is written.  kRagged: the tiles depend on data; prepare(shared address of all epilogue warps' memory) is called once by the
 // whole block before the first job(); Feed(plan, job, rank) holds what the copies of a tile's stages need: copy(k, ...) issues them, bytes(k) is what they bring to a
-// block.  Epi: load() reads 32 columns of the accumulator, column() says which, finish() is called after the last tile.
+// block.  Epi: load() reads 32 columns of the accumulator, column() says which, nothing() writes a tile without products, finish() is called after the last tile.
 // Epi: struct Args; __device__ Epi(const Args&, job, row, part, shared address of the warp's memory); begin(plan, first column) before the
 // accumulator is waited for, false (in the whole warp) if a wait of its own ran out; kParts: see above; chunk(col, v[32], last); end(); kWords of shared memory for each warp.  A thread holds one
 // row of the tile and gets its columns 32 at a time; the kWarps / 4 warps that share a row take a part of the columns each.  Rows >= M
@@ -500,12 +500,7 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
             if (!epi.begin(plan, col0)) break;                   // what it reads travels while the products run
             if constexpr (Plan::kRagged) {
                 if (!t.k_stages) {                               // a sum over nothing
-                    float v[32] = {};
-#pragma unroll 1
-                    for (uint32_t c = 0; c < kCols; c += 32) {
-                        const uint32_t col = Epi::column(t, part, c, kCols, BN);
-                        if (col < t.N) epi.chunk(col, v, c + 32 == kCols || Epi::column(t, part, c + 32, kCols, BN) >= t.N);
-                    }
+                    epi.nothing(part, kCols, BN, rank);
                     continue;
                 }
                 ++taken;

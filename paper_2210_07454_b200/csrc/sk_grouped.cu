@@ -112,6 +112,11 @@ struct RowsEpi {
         }
     }
     __device__ void end() {}
+    __device__ void nothing(uint32_t part, uint32_t cols, uint32_t bn, uint32_t) {
+        float v[32] = {};
+#pragma unroll 1
+        for (uint32_t c = 0; c < cols && column(t, part, c, cols, bn) < t.N; c += 32) chunk(column(t, part, c, cols, bn), v, false);
+    }
     // `rows` rows of the box at `at` to rows from `row` on, neighbouring lanes at neighbouring addresses: 16 bytes each, 4 or 2, as the rows are aligned
     __device__ __forceinline__ void by_lanes(uint32_t at, uint32_t row, uint32_t rows) {
         const uint32_t lane = threadIdx.x & 31;
@@ -440,7 +445,8 @@ template <bool PARTS>
 struct MatrixEpi {
     static constexpr int kWarps = 8, kWords = kStageWords;
     static constexpr bool kParts = PARTS, kInterleaved = false;
-    struct Args { CUtensorMap map; void* out; uint64_t ld, stride; int type; uint32_t align, by_box; float* sums; uint64_t ld_sums; };
+    // zeros: where a matrix without rows is one run of values, else null
+    struct Args { CUtensorMap map; void* out; uint64_t ld, stride; int type; uint32_t align, by_box; float* sums; uint64_t ld_sums; uint8_t* zeros; uint64_t zeros_stride; };
     const Args& a;
     const RaggedJob& t;
     uint32_t row0, rows, stage, turn = 0;
@@ -500,62 +506,83 @@ struct MatrixEpi {
         }
     }
     __device__ void end() {}
+    // A tile of a matrix without rows: zeros, written as a part of the whole run (in boxes of 64 bytes, rows whose length is no multiple of 32 bytes go out at 2.2 TB/s)
+    __device__ void nothing(uint32_t part, uint32_t cols, uint32_t bn, uint32_t rank) {
+        if (!a.zeros) {
+            float v[32] = {};
+#pragma unroll 1
+            for (uint32_t c = 0; c < cols; c += 32) {
+                const uint32_t col = column(t, part, c, cols, bn);
+                if (col < t.N) chunk(col, v, c + 32 == cols || col + 32 >= t.N);
+            }
+            return;
+        }
+        const uint32_t lane = threadIdx.x & 31, high = bn == 256 ? 256 : 128, tiles_m = (t.M + high - 1) / high, tiles = tiles_m * ((t.N + bn - 1) / bn);
+        const uint32_t units = tiles * (bn == 256 ? 2 : 1) * kWarps, unit = ((t.n * tiles_m + t.m) * (bn == 256 ? 2 : 1) + rank) * kWarps + (threadIdx.x >> 5) - 2;
+        const uint64_t size = a.type == SK_F32 ? 4 : 2, total = (uint64_t)t.M * t.N * size, each = (total / units + 512) / 512 * 512;
+        const uint64_t from = unit * each;
+        if (from >= total) return;
+        uint8_t *p = a.zeros + t.b * a.zeros_stride + from, *end = p + (total - from < each ? total - from : each);
+        uint8_t* whole = (uint8_t*)(((uintptr_t)p + 15) & ~(uintptr_t)15);           // from here on 16 bytes at a time
+        if (p + 2 * lane < whole && p + 2 * lane < end) *(uint16_t*)(p + 2 * lane) = 0;
+        for (whole += 16 * lane; whole + 16 <= end; whole += 512) *(uint4*)whole = make_uint4(0, 0, 0, 0);
+        for (; whole < end && whole + 16 > end; whole += 16)                                // the lane that comes to the last piece
+            for (uint8_t* q = whole; q < end; q += 2) *(uint16_t*)q = 0;
+    }
 };
 
 // dW of the groups whose K was split: the sums of their slices in order, by a thread for four columns where that keeps the GPU busy, else by eight warps every eighth
 // each and then those eight in order (2 groups of 30000 rows of 64 x 200: 30 us by single threads, 18; 16384 rows of 768 x 2048: 55, and 72 by eight warps).
 constexpr uint64_t kManyQuads = 1 << 17;
-__global__ void __launch_bounds__(256) k_grouped_join(const uint32_t* slices, const float* sums, uint64_t ld_sums, uint32_t groups, uint32_t M, uint32_t N, void* out,
-                                                      uint64_t ld, uint64_t stride, int type) {
+__global__ void __launch_bounds__(256) k_grouped_join(const uint32_t* slices, const float* sums, uint64_t ld_sums, uint32_t M, uint32_t N, void* out, uint64_t ld,
+                                                      uint64_t stride, int type) {
     __shared__ float4 part[8][32];
     chain_acquire();
-    const uint32_t quads = (N + 3) / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t quads = (N + 3) / 4, warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = blockIdx.y;
     const uint64_t total = (uint64_t)M * quads;
-    for (uint32_t g = 0; g < groups; ++g) {
-        const uint2 s = *(const uint2*)(slices + 2 * g);
-        if (s.x < 2) continue;
-        const float* first = sums + (uint64_t)s.y * M * ld_sums;
-        if (total >= kManyQuads) {
-            for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < total; i += gridDim.x * 256ull) {
-                const uint64_t row = i / quads;
-                const uint32_t col = (uint32_t)(i - row * quads) * 4;
-                const float* p = first + row * ld_sums + col;
-                float4 v = *(const float4*)p;
-#pragma unroll 4
-                for (uint32_t k = 1; k < s.x; ++k) {
-                    const float4 w = *(const float4*)(p + (uint64_t)k * M * ld_sums);
-                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-                }
-                const float f[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-                for (uint32_t e = 0; e < 4; ++e)
-                    if (col + e < N) store_as(out, type, g * stride + row * ld + col + e, f[e]);
-            }
-            continue;
-        }
-        for (uint64_t i0 = blockIdx.x * 32ull; i0 < total; i0 += gridDim.x * 32ull) {
-            const uint64_t i = i0 + lane, row = i / quads;
+    const uint2 s = *(const uint2*)(slices + 2 * g);
+    if (s.x < 2) return;
+    const float* first = sums + (uint64_t)s.y * M * ld_sums;
+    if (total >= kManyQuads) {
+        for (uint64_t i = blockIdx.x * 256ull + threadIdx.x; i < total; i += gridDim.x * 256ull) {
+            const uint64_t row = i / quads;
             const uint32_t col = (uint32_t)(i - row * quads) * 4;
-            float4 v = make_float4(0, 0, 0, 0);
-            if (i < total) {
+            const float* p = first + row * ld_sums + col;
+            float4 v = *(const float4*)p;
 #pragma unroll 4
-                for (uint32_t k = warp; k < s.x; k += 8) {
-                    const float4 w = *(const float4*)(first + row * ld_sums + col + (uint64_t)k * M * ld_sums);
-                    v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
-                }
+            for (uint32_t k = 1; k < s.x; ++k) {
+                const float4 w = *(const float4*)(p + (uint64_t)k * M * ld_sums);
+                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
             }
-            part[warp][lane] = v;
-            __syncthreads();
-            if (warp < 4) {                          // a value of the four each
-                float f = 0;
+            const float f[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-                for (uint32_t k = 0; k < 8; ++k) f += ((const float*)&part[k][0])[warp * 32 + lane];
-                const uint64_t j = i0 + (warp * 32 + lane) / 4, r = j / quads;
-                const uint32_t c = (uint32_t)(j - r * quads) * 4 + (lane & 3);
-                if (j < total && c < N) store_as(out, type, g * stride + r * ld + c, f);
-            }
-            __syncthreads();
+            for (uint32_t e = 0; e < 4; ++e)
+                if (col + e < N) store_as(out, type, g * stride + row * ld + col + e, f[e]);
         }
+        return;
+    }
+    for (uint64_t i0 = blockIdx.x * 32ull; i0 < total; i0 += gridDim.x * 32ull) {
+        const uint64_t i = i0 + lane, row = i / quads;
+        const uint32_t col = (uint32_t)(i - row * quads) * 4;
+        float4 v = make_float4(0, 0, 0, 0);
+        if (i < total) {
+#pragma unroll 4
+            for (uint32_t k = warp; k < s.x; k += 8) {
+                const float4 w = *(const float4*)(first + row * ld_sums + col + (uint64_t)k * M * ld_sums);
+                v.x += w.x; v.y += w.y; v.z += w.z; v.w += w.w;
+            }
+        }
+        part[warp][lane] = v;
+        __syncthreads();
+        if (warp < 4) {                              // a value of the four each
+            float f = 0;
+#pragma unroll
+            for (uint32_t k = 0; k < 8; ++k) f += ((const float*)&part[k][0])[warp * 32 + lane];
+            const uint64_t j = i0 + (warp * 32 + lane) / 4, r = j / quads;
+            const uint32_t c = (uint32_t)(j - r * quads) * 4 + (lane & 3);
+            if (j < total && c < N) store_as(out, type, g * stride + r * ld + c, f);
+        }
+        __syncthreads();
     }
 }
 
@@ -625,6 +652,74 @@ __global__ void __launch_bounds__(256) k_grouped_pack(const __grid_constant__ Pa
     }
 }
 
+// M x N values from rows that the copy engine wrote, ld_src apart, to rows that begin anywhere, one behind the other: 16 aligned bytes at a time, out of the two
+// accesses in which they lie, and the few values before and behind those one by one. (Written from the tiles, rows that are no multiple of 32 bytes leave at
+// 0.6 to 2 TB/s: most sectors are written in two parts.) matrices: of the groups that have rows; else rows offsets[0] to offsets[groups] of one matrix, or,
+// with fill, all of it.
+struct UnpackArgs {
+    const uint8_t* src;
+    uint8_t* dst;
+    const int64_t* offsets;
+    uint64_t ld_src, M;
+    uint32_t N, groups, rows, matrices, fill;            // matrices: dW; else y or dx
+};
+constexpr uint32_t kUnpackEach = 4;
+template <int SIZE>
+__global__ void __launch_bounds__(256) k_grouped_unpack(const __grid_constant__ UnpackArgs a) {
+    using V = std::conditional_t<SIZE == 2, uint16_t, uint32_t>;
+    constexpr uint32_t kN = 16 / SIZE;
+    chain_acquire();
+    const uint32_t g = blockIdx.y;
+    uint32_t from = 0, to = (uint32_t)a.M;
+    if (a.matrices) {
+        if (bounded(a.offsets[g + 1], a.rows) <= bounded(a.offsets[g], a.rows)) return;
+    } else if (!a.fill) {
+        from = bounded(a.offsets[0], a.rows);
+        to = bounded(a.offsets[a.groups], a.rows);
+    }
+    const uint32_t pieces = a.N / kN + 1;            // of a row, at most
+    uint32_t lanes = 32;                             // that share a row
+    while (lanes > 1 && lanes / 2 >= pieces) lanes /= 2;
+    const uint32_t lane = threadIdx.x & (lanes - 1), each = 256 / lanes;
+    for (uint64_t r = from + (uint64_t)blockIdx.x * each + threadIdx.x / lanes; r < to; r += (uint64_t)gridDim.x * each) {
+        const V* src = (const V*)a.src + ((uint64_t)g * a.M + r) * a.ld_src;             // on a 16-byte boundary
+        V* dst = (V*)a.dst + ((uint64_t)g * a.M + r) * a.N;
+        const uint32_t head = min(((16 - (uint32_t)((uintptr_t)dst & 15)) & 15) / SIZE, a.N), whole = (a.N - head) / kN, by = head * SIZE, more = by ? 1 : 0;
+        const uint4* p = (const uint4*)src;
+        uint4* o = (uint4*)(dst + head);
+        for (uint32_t i = lane; i < head; i += lanes) dst[i] = src[i];
+        for (uint32_t i = head + whole * kN + lane; i < a.N; i += lanes) dst[i] = src[i];
+        for (uint32_t c0 = lane; c0 < whole; c0 += lanes * kUnpackEach) {
+            uint4 x[kUnpackEach], y[kUnpackEach];
+#pragma unroll
+            for (uint32_t e = 0; e < kUnpackEach; ++e) {
+                const uint32_t c = c0 + e * lanes;
+                if (c < whole) {                     // 16 bytes behind the last row may be read
+                    x[e] = p[c];
+                    y[e] = p[c + more];
+                }
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < kUnpackEach; ++e) {
+                const uint32_t c = c0 + e * lanes;
+                if (c >= whole) break;
+                uint32_t w[8] = {x[e].x, x[e].y, x[e].z, x[e].w, y[e].x, y[e].y, y[e].z, y[e].w};
+                if (by & 8) {
+#pragma unroll
+                    for (int i = 0; i < 6; ++i) w[i] = w[i + 2];
+                }
+                if (by & 4) {
+#pragma unroll
+                    for (int i = 0; i < 5; ++i) w[i] = w[i + 1];
+                }
+                const uint32_t shift = (by & 2) * 8;
+                o[c] = make_uint4(__funnelshift_r(w[0], w[1], shift), __funnelshift_r(w[1], w[2], shift), __funnelshift_r(w[2], w[3], shift),
+                                  __funnelshift_r(w[3], w[4], shift));
+            }
+        }
+    }
+}
+
 bool addressable(const void* p, uint64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
 
 // Copies that a call needs, and where they lie in the workspace.
@@ -634,12 +729,18 @@ struct GroupedLayout {
     bool wide;                                       // tiles of dW
     uint32_t most_slices;                            // of the products that give dW, see MatrixPlan; 0: none is split
     uint64_t off_slices, off_sums, ld_sums;
+    bool unpack_rows, unpack_matrices;               // y or dx, dW: through the workspace, where rows are whole lines
+    uint64_t ld_rows, ld_matrices, off_rows, off_matrices;
 };
+// An output goes through the workspace if its rows cannot be written by the copy engine, if it is one run of values, and if it is large enough for another launch.
+constexpr uint64_t kUnpackBytes = 4 << 20;
 constexpr uint32_t kPlanSms = 148;                   // the slices, and with them the workspace, are planned for a B200
-// How many slices all groups of dW may be cut into, 0: K is not split. Few groups of few tiles, and rows enough for two slices.
+// How many slices all groups of dW may be cut into, 0: K is not split. Few groups of few tiles, rows enough to be worth another launch (4096 are some 19 us of one
+// tile), and a slice's worth of them in a group of the mean length.
+constexpr uint64_t kSplitRows = 4096;
 uint64_t slices_of(const GroupedArgs& a, bool wide) {
     const uint64_t tile = wide ? 256 : 128, tiles = ((a.out + tile - 1) / tile) * ((a.width + tile - 1) / tile), most = 2 * (kPlanSms / (wide ? 2 : 1)) / tiles;
-    return most >= 2 && most >= a.groups && a.groups <= kSorted && a.rows > 2 * kShortest * kGemmK ? most : 0;
+    return most >= 2 && most >= a.groups && a.groups <= kSorted && a.rows >= kSplitRows && a.rows >= a.groups * kShortest * kGemmK ? most : 0;
 }
 // Pairs of blocks or single ones: the one that is through first, at some 600 cycles a stage, if the groups are of one length (see wide_tiles for the constants).
 bool wide_matrices(const GroupedArgs& a) {
@@ -681,6 +782,22 @@ GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
             l.off_sums = l.off_slices + round_up(a.groups * 8, 256);
             l.total = l.off_sums + round_up(l.most_slices * a.out * l.ld_sums * 4, 256);
         }
+        const uint64_t size = type_size(a.dweight_type), stride = a.groups > 1 ? a.stride_dweight : a.out * a.ld_dweight;
+        if (a.dweight && a.ld_dweight == a.width && stride == a.out * a.width && ((uintptr_t)a.dweight | a.width * size) % 16 &&
+            a.groups * a.out * a.width * size >= kUnpackBytes) {
+            l.unpack_matrices = true;
+            l.ld_matrices = round_up(a.width, 128 / size);
+            l.off_matrices = l.total;
+            l.total += round_up(a.groups * a.out * l.ld_matrices * size + 32, 256);      // 16 bytes may be read behind the last row
+        }
+    }
+    const void* rows = backward ? a.dx : a.y;
+    const uint64_t cols = backward ? a.width : a.out, ld = backward ? a.ld_dx : a.ld_y;
+    if (rows && ld == cols && !addressable(rows, ld) && a.rows * cols * 2 >= kUnpackBytes) {
+        l.unpack_rows = true;
+        l.ld_rows = round_up(cols, 64);
+        l.off_rows = l.total;
+        l.total += round_up(a.rows * l.ld_rows * 2 + 32, 256);
     }
     return l;
 }
@@ -717,6 +834,15 @@ bool wide_rows(const GroupedArgs& a, uint64_t features, uint64_t k_stages, int s
         return (tiles + units - 1) / units * k_stages * stage + fixed;
     };
     return last(256, 256, 2, sm_count / 2, 12000) <= last(128, 128, 1, sm_count, 7000);
+}
+
+int launch_unpack(const GroupedArgs& a, const void* src, uint64_t ld_src, void* dst, uint64_t M, uint64_t N, int type, bool matrices, int sm_count, cudaStream_t st) {
+    const UnpackArgs u{(const uint8_t*)src, (uint8_t*)dst, a.offsets, ld_src, M, (uint32_t)N, (uint32_t)a.groups, (uint32_t)a.rows, matrices, (uint32_t)a.fill};
+    const uint64_t batch = matrices ? a.groups : 1, each = 256 * kUnpackEach * (16 / type_size(type)), want = (M * N + each - 1) / each;
+    const uint64_t most = ((uint64_t)sm_count * 16 + batch - 1) / batch;
+    const dim3 grid((uint32_t)(want < most ? want : most), (uint32_t)batch);
+    SK_OP_CUDA(type == SK_F32 ? launch_kernel(true, k_grouped_unpack<4>, grid, 256, 0, st, u) : launch_kernel(true, k_grouped_unpack<2>, grid, 256, 0, st, u));
+    return SK_OK;
 }
 
 template <int CG, int BN>
@@ -776,20 +902,31 @@ int launch_matrices(const GroupedArgs& a, const GroupedLayout& l, const OpDevice
     p.most_slices = l.most_slices;
     p.beside = a.dx != nullptr;
     p.slices = (uint32_t*)((uint8_t*)a.workspace + l.off_slices);
-    typename MatrixEpi<PARTS>::Args ea{{}, a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type, 0, 0, (float*)((uint8_t*)a.workspace + l.off_sums), l.ld_sums};
+    typename MatrixEpi<PARTS>::Args ea{{}, a.dweight, a.ld_dweight, a.groups > 1 ? a.stride_dweight : a.out * a.ld_dweight, a.dweight_type, 0, 0,
+                                       (float*)((uint8_t*)a.workspace + l.off_sums), l.ld_sums, nullptr, 0};
     const uint64_t size = type_size(a.dweight_type);
-    ea.by_box = ((uintptr_t)a.dweight | a.ld_dweight * size | (a.groups > 1 ? a.stride_dweight * size : 0)) % 16 == 0;
-    if (ea.by_box && !encode_out(&ea.map, a.dweight, a.groups, a.out, a.width, a.ld_dweight, a.groups > 1 ? a.stride_dweight : a.out * a.ld_dweight, a.dweight_type, 32))
+    if (ea.ld == a.width) {                          // the distance between the matrices is that of the output itself in any case
+        ea.zeros = (uint8_t*)a.dweight;
+        ea.zeros_stride = ea.stride * size;
+    }
+    if (l.unpack_matrices) {
+        ea.out = (uint8_t*)a.workspace + l.off_matrices;
+        ea.ld = l.ld_matrices;
+        ea.stride = a.out * l.ld_matrices;
+    }
+    ea.by_box = ((uintptr_t)ea.out | ea.ld * size | ea.stride * size) % 16 == 0;
+    if (ea.by_box && !encode_out(&ea.map, ea.out, a.groups, a.out, a.width, ea.ld, ea.stride, ea.type, 32))
         return set_error(SK_ECUDA, "%s: the output cannot be described to the copy engine", __func__);
-    const uint32_t by_row = row_alignment(a.dweight, a.ld_dweight, a.dweight_type), by_matrix = row_alignment(a.dweight, a.stride_dweight, a.dweight_type);
-    ea.align = a.groups > 1 && by_matrix < by_row ? by_matrix : by_row;
+    const uint32_t by_row = row_alignment(ea.out, ea.ld, ea.type), by_matrix = row_alignment(ea.out, ea.stride, ea.type);
+    ea.align = by_matrix < by_row ? by_matrix : by_row;
     const uint64_t tiles = (l.most_slices ? l.most_slices : a.groups) * p.tiles_m * p.tiles_n, slots = (uint64_t)dev.sm_count / CG;
     SK_OP_CUDA((launch_plan<CG, BN, Plan, MatrixEpi<PARTS>>(true, p, ea, (uint32_t)(tiles < slots ? tiles : slots), st)));
-    if (!l.most_slices) return SK_OK;
-    const uint64_t want = (a.out * ((a.width + 3) / 4) + 31) / 32, most = (uint64_t)dev.sm_count * 8;
-    SK_OP_CUDA(launch_kernel(true, k_grouped_join, dim3((uint32_t)(want < most ? want : most)), 256, 0, st, (const uint32_t*)p.slices, (const float*)ea.sums, l.ld_sums,
-                             p.groups, p.M, p.N, a.dweight, a.ld_dweight, a.stride_dweight, a.dweight_type));
-    return SK_OK;
+    if (l.most_slices) {
+        const uint64_t want = (a.out * ((a.width + 3) / 4) + 31) / 32, most = (uint64_t)dev.sm_count * 8;
+        SK_OP_CUDA(launch_kernel(true, k_grouped_join, dim3((uint32_t)(want < most ? want : most), p.groups), 256, 0, st, (const uint32_t*)p.slices,
+                                 (const float*)ea.sums, l.ld_sums, p.M, p.N, ea.out, ea.ld, ea.stride, ea.type));
+    }
+    return l.unpack_matrices ? launch_unpack(a, ea.out, ea.ld, a.dweight, a.out, a.width, a.dweight_type, true, dev.sm_count, st) : SK_OK;
 }
 
 }  // namespace
@@ -800,7 +937,10 @@ int launch_grouped(GroupedArgs a, const OpDevice& dev, cudaStream_t st) {
     const GroupedLayout l = layout_of(a, false);
     if (int rc = pack_operands(a, l, dev.sm_count, st)) return rc;
     auto launch = wide_rows(a, a.out, (a.width + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_rows<2, 256> : launch_rows<1, 128>;
-    return launch(a, a.x, a.ld_x, false, a.y, a.ld_y, a.fill, dev, st);
+    if (!l.unpack_rows) return launch(a, a.x, a.ld_x, false, a.y, a.ld_y, a.fill, dev, st);
+    void* rows = (uint8_t*)a.workspace + l.off_rows;
+    if (int rc = launch(a, a.x, a.ld_x, false, rows, l.ld_rows, a.fill, dev, st)) return rc;
+    return launch_unpack(a, rows, l.ld_rows, a.y, a.rows, a.out, a.type, false, dev.sm_count, st);
 }
 
 int launch_grouped_backward(GroupedArgs a, const OpDevice& dev, cudaStream_t st) {
@@ -808,14 +948,19 @@ int launch_grouped_backward(GroupedArgs a, const OpDevice& dev, cudaStream_t st)
     if (int rc = pack_operands(a, l, dev.sm_count, st)) return rc;
     if (a.dx) {
         auto launch = wide_rows(a, a.width, (a.out + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_rows<2, 256> : launch_rows<1, 128>;
-        if (int rc = launch(a, a.dy, a.ld_dy, true, a.dx, a.ld_dx, a.fill, dev, st)) return rc;
+        void* rows = l.unpack_rows ? (uint8_t*)a.workspace + l.off_rows : a.dx;
+        if (int rc = launch(a, a.dy, a.ld_dy, true, rows, l.unpack_rows ? l.ld_rows : a.ld_dx, a.fill, dev, st)) return rc;
     }
-    if (!a.dweight) return SK_OK;
+    auto unpack_dx = [&] {                           // behind both products: the second one begins while the first still runs
+        return l.unpack_rows ? launch_unpack(a, (uint8_t*)a.workspace + l.off_rows, l.ld_rows, a.dx, a.rows, a.width, a.type, false, dev.sm_count, st) : SK_OK;
+    };
+    if (!a.dweight) return unpack_dx();
     // The accumulators' truncation grows with the rows added up: 16-bit gradients of fp16 and 32-bit ones show it, bf16's rounding is coarser.
     const bool parts = a.dweight_type == SK_F32 || a.type == SK_F16;
     auto launch = parts ? (l.wide ? launch_matrices<2, 256, true> : launch_matrices<1, 128, true>)
                         : (l.wide ? launch_matrices<2, 256, false> : launch_matrices<1, 128, false>);
-    return launch(a, l, dev, st);
+    if (int rc = launch(a, l, dev, st)) return rc;
+    return unpack_dx();
 }
 
 }  // namespace sk

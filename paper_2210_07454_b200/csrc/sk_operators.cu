@@ -272,10 +272,11 @@ static int grouped_checked(const char* who, const GroupedArgs& a, bool backward)
 }
 
 uint64_t sk_grouped_linear_workspace(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight, uint64_t rows,
-                                     uint64_t groups, uint64_t width, uint64_t out) {
+                                     uint64_t groups, uint64_t width, uint64_t out, const void* y, uint64_t ld_y) {
     GroupedArgs a{};
     a.x = x; a.ld_x = ld_x; a.weight = weight; a.ld_weight = ld_weight; a.stride_weight = stride_weight;
     a.rows = rows; a.groups = groups; a.width = width; a.out = out;
+    a.y = const_cast<void*>(y); a.ld_y = ld_y;
     return rows && groups && width && out ? grouped_workspace(a, false) : 0;
 }
 
@@ -300,11 +301,14 @@ int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t
 }
 
 uint64_t sk_grouped_linear_backward_workspace(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight,
-                                              uint64_t stride_weight, uint64_t rows, uint64_t groups, uint64_t width, uint64_t out) {
+                                              uint64_t stride_weight, uint64_t rows, uint64_t groups, uint64_t width, uint64_t out, const void* dx,
+                                              uint64_t ld_dx, const void* dweight, uint64_t ld_dweight, uint64_t stride_dweight, int dweight_type) {
     GroupedArgs a{};
     a.dy = dy; a.ld_dy = ld_dy; a.x = x; a.ld_x = ld_x; a.weight = weight; a.ld_weight = ld_weight; a.stride_weight = stride_weight;
     a.rows = rows; a.groups = groups; a.width = width; a.out = out;
-    return rows && groups && width && out ? grouped_workspace(a, true) : 0;
+    a.dx = const_cast<void*>(dx); a.ld_dx = ld_dx;
+    a.dweight = const_cast<void*>(dweight); a.ld_dweight = ld_dweight; a.stride_dweight = stride_dweight; a.dweight_type = dweight_type;
+    return rows && groups && width && out && type_ok(dweight_type) ? grouped_workspace(a, true) : 0;
 }
 
 int sk_grouped_linear_backward(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight,

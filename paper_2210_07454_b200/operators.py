@@ -466,10 +466,10 @@ def grouped_linear(x, weight, offsets, out=None, stream=None):
         y = out
     px, pw = x.data_ptr(), weight.data_ptr()
     L = lib()
-    need = _need(device, L.sk_grouped_linear_workspace, px, ld_x, pw, ld_w, s_w, rows, groups, width, n)
+    py = y.data_ptr()
+    need = _need(device, L.sk_grouped_linear_workspace, px, ld_x, pw, ld_w, s_w, rows, groups, width, n, py, ld_y)
     ws = new((need,), (1,), torch.uint8) if need else None
-    _run(device, L.sk_grouped_linear, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, y.data_ptr(), ld_y, out is None, _p(ws), need,
-         _raw_stream(device))
+    _run(device, L.sk_grouped_linear, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, py, ld_y, out is None, _p(ws), need, _raw_stream(device))
     if out is not None:
         _wrote(out)
     return y
@@ -505,11 +505,11 @@ def grouped_linear_backward(dy, x, weight, offsets, dx=None, dweight=None, strea
         wcode = _tensor(dweight, "dweight", {weight.dtype: code, torch.float32: 0}, device)
         _same_shape(dweight, weight, "dweight")
         ld_dw, s_dw = _ld(dweight, "dweight"), dweight.stride(0)
-    pd, px, pw = dy.data_ptr(), x.data_ptr(), weight.data_ptr()
+    pd, px, pw, pdx, pdw = dy.data_ptr(), x.data_ptr(), weight.data_ptr(), _p(dx), _p(dweight)
     L = lib()
-    need = _need(device, L.sk_grouped_linear_backward_workspace, pd, ld_dy, px, ld_x, pw, ld_w, s_w, rows, groups, width, n)
+    need = _need(device, L.sk_grouped_linear_backward_workspace, pd, ld_dy, px, ld_x, pw, ld_w, s_w, rows, groups, width, n, pdx, ld_dx, pdw, ld_dw, s_dw, wcode)
     ws = new((need,), (1,), torch.uint8) if need else None
-    _run(device, L.sk_grouped_linear_backward, pd, ld_dy, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, _p(dx), ld_dx, fill, _p(dweight),
+    _run(device, L.sk_grouped_linear_backward, pd, ld_dy, px, ld_x, pw, ld_w, s_w, code, rows, groups, width, n, po, pdx, ld_dx, fill, pdw,
          ld_dw, s_dw, wcode, _p(ws), need, _raw_stream(device))
     if given_outputs[0] is not None or given_outputs[1] is not None:
         _wrote(*given_outputs)

@@ -176,12 +176,41 @@ def test_long_groups_in_32_bits(ops, dtype):
 
 # few tiles and many rows: a group's rows are shared out among several blocks and the sums joined
 @pytest.mark.parametrize("dtype", HALF, ids=str)
-@pytest.mark.parametrize("sizes", [[1025], [6000], [5000, 0, 130, 2000], [64, 4097, 1, 63, 65, 0], [3000] * 5, [1030] + [7] * 40], ids=str)
+@pytest.mark.parametrize("sizes", [[1025], [6000], [5000, 0, 130, 2000], [64, 4097, 1, 63, 65, 0], [3000] * 5, [1030] + [7] * 40, [21000] + [7] * 40], ids=str)
 @pytest.mark.parametrize("width,out", [(64, 200), (300, 260), (333, 40), (768, 512)])
 def test_long_groups_of_small_matrices(ops, sizes, width, out, dtype):
     e = ends(sizes, 5)
     check(ops, e, e[-1] + 70, width, out, dtype)
     check(ops, e, e[-1] + 70, width, out, dtype, dweight_type=torch.float32)
+
+
+# outputs of some megabytes whose rows the copy engine cannot write, or that begin off its boundaries
+@pytest.mark.parametrize("dtype", HALF, ids=str)
+@pytest.mark.parametrize("width,out", [(1001, 1333), (1002, 1334), (1004, 1340), (2049, 515), (75, 3001), (1400, 1416)])
+def test_large_outputs_of_odd_rows(ops, width, out, dtype):
+    e = ends([700, 0, 33, 0, 1, 1500, 0], 11)
+    y, dx, dw = check(ops, e, e[-1] + 300, width, out, dtype)
+    check(ops, e, e[-1] + 300, width, out, dtype, dweight_type=torch.float32)
+    x, w, dy, off = randn(1, e[-1] + 300, width, dtype=dtype), randn(2, 7, out, width, dtype=dtype), randn(3, e[-1] + 300, out, dtype=dtype), offsets_of(e)
+    outside = torch.ones(len(x), dtype=torch.bool, device="cuda")
+    outside[e[0]:e[-1]] = False
+    for at in (0, 1, 3, 8):                                          # given, from another boundary, with something around them that stays
+        flat = [torch.full((at + t.numel() + 40,), 6.0, dtype=dtype, device="cuda") for t in (y, dx, dw)]
+        oy, ox, ow = (f[at:at + t.numel()].view(t.shape) for f, t in zip(flat, (y, dx, dw)))
+        ops.grouped_linear(x, w, off, out=oy)
+        ops.grouped_linear_backward(dy, x, w, off, dx=ox, dweight=ow)
+        assert torch.equal(oy[~outside], y[~outside]) and torch.equal(ox[~outside], dx[~outside]) and torch.equal(ow, dw)
+        assert bool((oy[outside] == 6).all()) and bool((ox[outside] == 6).all())
+        assert all(bool((f[:at] == 6).all()) and bool((f[-40:] == 6).all()) for f in flat)
+    ops.sync()
+
+
+@pytest.mark.parametrize("dtype", HALF, ids=str)
+def test_large_gradients_of_few_groups_with_odd_rows(ops, dtype):
+    """K split, the sums joined and the rows put together."""
+    for dweight_type in (None, torch.float32):
+        check(ops, ends([9000]), 9000, 1501, 1777, dtype, dweight_type=dweight_type)
+        check(ops, ends([5000, 0, 100]), 5100, 777, 1503, dtype, dweight_type=dweight_type)
 
 
 def views(dtype, rows, cols, pad, offset, seed):

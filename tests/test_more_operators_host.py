@@ -41,8 +41,8 @@ def test_grouped_linear_checks(L):
                      (dict(rows=1 << 30, out=1 << 20, ld_y=1 << 20), b"large"), (dict(x=P + 2), b"workspace"), (dict(ld_x=9), b"workspace"),
                      (dict(w=Q + 2), b"workspace"), (dict(s_w=65), b"workspace"), (dict(x=P + 2, ws=Q + 16, need=1 << 20), b"workspace")):
         assert refused(L, call(**kw), word), kw
-    assert L.sk_grouped_linear_workspace(P, 8, Q, 8, 64, 4, 2, 8, 8) == 0
-    assert L.sk_grouped_linear_workspace(P + 2, 8, Q, 8, 64, 4, 2, 8, 8) > 0
+    assert L.sk_grouped_linear_workspace(P, 8, Q, 8, 64, 4, 2, 8, 8, R, 8) == 0
+    assert L.sk_grouped_linear_workspace(P + 2, 8, Q, 8, 64, 4, 2, 8, 8, R, 8) > 0
 
 
 def test_grouped_linear_backward_checks(L):
@@ -62,12 +62,12 @@ def test_grouped_linear_backward_checks(L):
 def test_sizes_of_nothing(L):
     """Questions about empty extents are answered, whatever the call itself would say."""
     for rows, groups, width, out in ((0, 2, 8, 8), (4, 0, 8, 8), (4, 2, 0, 8), (4, 2, 8, 0)):
-        assert L.sk_grouped_linear_workspace(P + 2, 9, Q, 9, 64, rows, groups, width, out) == 0
-        assert L.sk_grouped_linear_backward_workspace(P + 2, 9, P, 9, Q, 9, 64, rows, groups, width, out) == 0
+        assert L.sk_grouped_linear_workspace(P + 2, 9, Q, 9, 64, rows, groups, width, out, R, 9) == 0
+        assert L.sk_grouped_linear_backward_workspace(P + 2, 9, P, 9, Q, 9, 64, rows, groups, width, out, R, 9, 2 * R, 9, 72, 1) == 0
     assert L.sk_sort_by_expert_workspace(0, 4) == 0 and L.sk_sort_by_expert_workspace(10, 0) == 0 and L.sk_sort_by_expert_workspace(10, 5000) == 0
     # few tiles and many rows: the sums of the slices, below 80 MB whatever the sizes
     for width, out, groups in ((64, 200, 2), (768, 2048, 1), (256, 64, 30)):
-        assert 0 < L.sk_grouped_linear_backward_workspace(P, out, P, width, Q, width, out * width, 30000, groups, width, out) < (80 << 20)
+        assert 0 < L.sk_grouped_linear_backward_workspace(P, out, P, width, Q, width, out * width, 30000, groups, width, out, R, width, 2 * R, width, out * width, 1) < (80 << 20)
 
 
 def test_sort_by_expert_checks(L):
