@@ -155,6 +155,7 @@ struct RowsPlan {
     uint32_t groups, rows, features, tiles_m;        // tiles_m: of the features
     uint32_t k_stages, last_k;                       // K is the same for all tiles
     uint32_t beside;                                 // no
+    uint32_t slices, each;                           // of K, and their stages
     uint32_t mn, k_rows, bf16, fill;                 // mn: the matrix is read along its rows; fill: rows of no group become zero
     Waits waits;
     static constexpr bool kCooperative = false, kEmpty = false, kThree = false, kRagged = true;
@@ -184,7 +185,7 @@ struct RowsPlan {
             b = max(b, top);
             e = max(e, b);
             const bool counts = i < segments && (fill || (i > 0 && i <= groups));
-            const uint32_t mine = counts ? (e - b + BN - 1) / BN * tiles_m : 0;
+            const uint32_t mine = counts ? (e - b + BN - 1) / BN * tiles_m * slices : 0;
             uint32_t sum = mine;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
@@ -211,7 +212,7 @@ struct RowsPlan {
             if (before[middle] <= t) low = middle;
             else high = middle;
         }
-        const uint32_t from = begin[low], length = begin[low + 1] - from, q = t - before[low], tile = q / tiles_m;
+        const uint32_t from = begin[low], length = begin[low + 1] - from, all = t - before[low], slice = all % slices, q = all / slices, tile = q / tiles_m;
         const uint32_t count = (length + BN - 1) / BN, each = ((length + count - 1) / count + kStep - 1) & ~(kStep - 1);
         const bool real = low > 0 && low <= groups;
         j.M = features;
@@ -221,8 +222,10 @@ struct RowsPlan {
         j.N = min(each, length - tile * each);
         j.cols = (j.N + kStep - 1) & ~(kStep - 1);
         j.z = (int)low - 1;
-        j.k_stages = real ? k_stages : 0;
-        j.last_rows = last_k;
+        j.slice = slice;
+        j.k_first = (int)(slice * this->each * kGemmK);
+        j.k_stages = real ? min(this->each, k_stages - slice * this->each) : 0;
+        j.last_rows = (slice + 1) * this->each >= k_stages ? last_k : kGemmK;
         j.k_rows = k_rows;
         j.a_mn = mn;
         j.b_mn = 0;
@@ -240,7 +243,7 @@ struct RowsPlan {
     // many cost to bring (112 rows are fetched as 128).
     struct Feed {
         const CUtensorMap *matrix, *first_map, *second_map;
-        int feature, z, row;
+        int feature, z, row, k_first;
         uint32_t first, total, mn;
         __device__ __forceinline__ Feed(const RowsPlan& p, const RaggedJob& j, uint32_t rank) {
             const uint32_t mine = j.cols / CG;       // a multiple of 16: the swizzle's groups of eight rows stay whole
@@ -259,10 +262,11 @@ struct RowsPlan {
             feature = (int)(j.m * (128 * CG) + rank * 128);
             z = j.z;
             row = (int)(j.first + rank * mine);
+            k_first = j.k_first;
         }
         __device__ __forceinline__ uint32_t bytes(uint32_t) const { return total; }
         __device__ __forceinline__ void copy(uint32_t k, uint32_t sa, uint32_t sb, uint32_t bar) const {
-            const int k0 = (int)(k * kGemmK);
+            const int k0 = k_first + (int)(k * kGemmK);
             if (mn) {
                 tma_load<CG>(sa, matrix, bar, feature, k0, z);
                 tma_load<CG>(sa + 8192, matrix, bar, feature + 64, k0, z);
@@ -277,6 +281,53 @@ struct RowsPlan {
     __device__ __forceinline__ void done(const TileJob&) const {}
     __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i == 0 ? &matrix : i < 5 ? &rows_map[i - 1] : nullptr; }
 };
+
+// Where there are few tiles and K is long, it is split: slices' sums in 32 bits, rows and columns as in the output, joined by k_grouped_sum. A lane holds an output
+// column, so that a warp writes 32 neighbouring ones of a row.
+struct SumsEpi {
+    static constexpr int kWarps = RowsEpi::kWarps, kWords = RowsEpi::kWords;
+    static constexpr bool kParts = false, kInterleaved = true;
+    struct Args { float* sums; uint64_t ld, stride; };           // stride: from slice to slice
+    const Args& a;
+    const RaggedJob& t;
+    uint32_t feature;
+    __device__ SumsEpi(const Args& a_, const RaggedJob& t_, uint32_t row, uint32_t, uint32_t) : a(a_), t(t_), feature(row) {}
+    template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
+    __device__ static void finish() {}
+    __device__ static uint32_t column(const RaggedJob& t, uint32_t part, uint32_t c, uint32_t cols, uint32_t bn) { return RowsEpi::column(t, part, c, cols, bn); }
+    __device__ static void load(uint32_t addr, float (&v)[32]) { tmem_load32(addr, v); }
+    __device__ void chunk(uint32_t col, float (&v)[32], bool) {
+        float* o = a.sums + t.slice * a.stride + (uint64_t)(t.first + col) * a.ld + feature;
+        const uint32_t rows = t.N - col;
+        if (feature < t.M) {
+#pragma unroll
+            for (uint32_t i = 0; i < 32; ++i)
+                if (i < rows) o[i * a.ld] = v[i];
+        }
+        __syncwarp();
+    }
+    __device__ void end() {}
+    __device__ void nothing(uint32_t, uint32_t, uint32_t, uint32_t) {}           // rows of no group: left to what joins the slices
+};
+// The slices in order, a thread a value. Rows of no group become zero with fill, else stay.
+__global__ void __launch_bounds__(256) k_grouped_sum(const float* sums, uint64_t ld_sums, uint64_t stride, uint32_t slices, const int64_t* offsets, uint32_t groups,
+                                                     uint32_t rows, uint32_t cols, uint16_t* out, uint64_t ld, int bf16, int fill) {
+    chain_acquire();
+    const uint32_t col = blockIdx.x * 256 + threadIdx.x, from = bounded(offsets[0], rows), to = bounded(offsets[groups], rows);
+    if (col >= cols) return;
+    for (uint32_t r = blockIdx.y; r < rows; r += gridDim.y) {
+        float v = 0;
+        if (r >= from && r < to) {
+            const float* p = sums + r * ld_sums + col;
+            v = *p;
+#pragma unroll 8
+            for (uint32_t s = 1; s < slices; ++s) v += p[s * stride];
+        } else if (!fill) {
+            continue;
+        }
+        out[r * ld + col] = (uint16_t)pack16(v, 0.0f, bf16);
+    }
+}
 
 // dW by tiles of 128 CG x BN of every matrix, the longest groups first; units take them up and down in turn, so that what one has too much in one round
 // it has too little in the next (in the groups' own order, 32 groups of 16384 rows kept one pair of blocks busy for 82,000 cycles and another for 55,000).
@@ -591,25 +642,31 @@ __global__ void __launch_bounds__(256) k_grouped_join(const uint32_t* slices, co
 struct PackedOne {
     const uint16_t* src;
     uint16_t* dst;
-    uint64_t ld, stride, total;                      // total: rows of all matrices
-    uint32_t rows, cols, ld_dst, blocks;
+    uint64_t ld, stride;
+    uint32_t rows, matrices, cols, ld_dst, blocks;   // blocks: of each matrix
+    const int64_t* offsets;                          // not null: only matrices whose group has rows
 };
-struct PackedArgs { PackedOne m[3]; };
+struct PackedArgs { PackedOne m[3]; uint32_t rows; };
 constexpr uint32_t kPackEach = 4;                    // of a thread, on their way at once
 __global__ void __launch_bounds__(256) k_grouped_pack(const __grid_constant__ PackedArgs a) {
     chain_acquire();
     uint32_t block = blockIdx.x, which = 0;
-    while (block >= a.m[which].blocks) block -= a.m[which++].blocks;
+    while (block >= a.m[which].blocks * a.m[which].matrices) {
+        block -= a.m[which].blocks * a.m[which].matrices;
+        ++which;
+    }
     const PackedOne& m = a.m[which];
+    const uint32_t z = block / m.blocks;
+    block -= z * m.blocks;
+    if (m.offsets && bounded(m.offsets[z + 1], a.rows) <= bounded(m.offsets[z], a.rows)) return;
     const uint32_t pieces = m.ld_dst / 8;            // of 16 bytes in a row
     uint32_t lanes = 32;                             // that share a row: so many that its pieces keep them busy
     while (lanes > 1 && lanes / 2 >= pieces) lanes /= 2;
-    const uint32_t lane = threadIdx.x & (lanes - 1), each = 256 / lanes, total = (uint32_t)m.total;         // at most 2^31
-    const uint64_t begin = (uint64_t)(uintptr_t)m.src, end = begin + ((m.total / m.rows - 1) * m.stride + (m.rows - 1) * m.ld + m.cols) * 2;
-    for (uint64_t r64 = (uint64_t)block * each + threadIdx.x / lanes; r64 < total; r64 += (uint64_t)m.blocks * each) {
-        const uint32_t r = (uint32_t)r64, z = r / m.rows;
-        const uint16_t* row = m.src + z * m.stride + (r - z * m.rows) * m.ld;
-        uint4* to = (uint4*)(m.dst + (uint64_t)r * m.ld_dst);
+    const uint32_t lane = threadIdx.x & (lanes - 1), each = 256 / lanes;
+    const uint64_t begin = (uint64_t)(uintptr_t)m.src, end = begin + ((m.matrices - 1) * m.stride + (m.rows - 1) * m.ld + m.cols) * 2;
+    for (uint64_t r = (uint64_t)block * each + threadIdx.x / lanes; r < m.rows; r += (uint64_t)m.blocks * each) {
+        const uint16_t* row = m.src + z * m.stride + r * m.ld;
+        uint4* to = (uint4*)(m.dst + ((uint64_t)z * m.rows + r) * m.ld_dst);
         const uint32_t by = (uint32_t)(uintptr_t)row & 15, more = by ? 1 : 0, shift = (by & 2) * 8;
         const uint4* p = (const uint4*)((uintptr_t)row - by);
         // pieces [low, high) lie in whole accesses inside the tensor
@@ -729,6 +786,8 @@ struct GroupedLayout {
     bool wide;                                       // tiles of dW
     uint32_t most_slices;                            // of the products that give dW, see MatrixPlan; 0: none is split
     uint64_t off_slices, off_sums, ld_sums;
+    uint32_t slices;                                 // of K, of the product that gives y or dx
+    uint64_t off_row_sums, ld_row_sums;
     bool unpack_rows, unpack_matrices;               // y or dx, dW: through the workspace, where rows are whole lines
     uint64_t ld_rows, ld_matrices, off_rows, off_matrices;
 };
@@ -756,6 +815,15 @@ bool wide_matrices(const GroupedArgs& a) {
         return longest * 620 + (wide ? 12000 : 7000);
     };
     return cycles(true) <= cycles(false);
+}
+// Slices of K for y or dx. Single blocks with a tile each, if all the tiles there can be leave at least half of the SMs without work; a slice has kShortest stages or more, and what
+// is saved, at some 350 cycles a stage of few rows, has to be worth another launch.
+uint32_t row_slices(const GroupedArgs& a, uint64_t features, uint64_t k_stages) {
+    const uint64_t live = a.groups < a.rows ? a.groups : a.rows, tiles = (a.rows / 128 + live) * ((features + 127) / 128);
+    uint64_t slices = kPlanSms / tiles < k_stages / kShortest ? kPlanSms / tiles : k_stages / kShortest;
+    if (slices < 2 || k_stages < 2 * kShortest) return 1;
+    const uint64_t each = (k_stages + slices - 1) / slices;
+    return (uint32_t)((k_stages + each - 1) / each);
 }
 GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
     GroupedLayout l{};
@@ -793,7 +861,12 @@ GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
     }
     const void* rows = backward ? a.dx : a.y;
     const uint64_t cols = backward ? a.width : a.out, ld = backward ? a.ld_dx : a.ld_y;
-    if (rows && ld == cols && !addressable(rows, ld) && a.rows * cols * 2 >= kUnpackBytes) {
+    l.slices = rows ? row_slices(a, cols, ((backward ? a.out : a.width) + kGemmK - 1) / kGemmK) : 1;
+    if (l.slices > 1) {
+        l.ld_row_sums = round_up(cols, 32);
+        l.off_row_sums = l.total;
+        l.total += round_up(l.slices * a.rows * l.ld_row_sums * 4, 256);
+    } else if (rows && ld == cols && !addressable(rows, ld) && a.rows * cols * 2 >= kUnpackBytes) {
         l.unpack_rows = true;
         l.ld_rows = round_up(cols, 64);
         l.off_rows = l.total;
@@ -807,17 +880,20 @@ int pack_operands(GroupedArgs& a, const GroupedLayout& l, int sm_count, cudaStre
     uint8_t* ws = (uint8_t*)a.workspace;
     PackedArgs p{};
     uint32_t n = 0, blocks = 0;
-    auto add = [&](const void*& src, uint64_t& ld, uint64_t stride, uint64_t rows, uint64_t total, uint64_t cols, uint64_t off, uint64_t ld_dst) {
-        const uint64_t want = (total * (ld_dst / 8) + 255) / 256, most = (uint64_t)sm_count * 8;
-        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, stride, total, (uint32_t)rows, (uint32_t)cols, (uint32_t)ld_dst, (uint32_t)(want < most ? want : most)};
-        blocks += p.m[n++].blocks;
+    auto add = [&](const void*& src, uint64_t& ld, uint64_t stride, uint64_t rows, uint64_t matrices, uint64_t cols, uint64_t off, uint64_t ld_dst, const int64_t* offsets) {
+        const uint64_t want = (rows * (ld_dst / 8) + 255) / 256, share = (uint64_t)sm_count * 8 / matrices, most = share > 64 ? share : 64;      // there may be rows in one group only
+        p.m[n] = {(const uint16_t*)src, (uint16_t*)(ws + off), ld, stride, (uint32_t)rows, (uint32_t)matrices, (uint32_t)cols, (uint32_t)ld_dst,
+                  (uint32_t)(want < most ? want : most), offsets};
+        blocks += p.m[n].blocks * p.m[n].matrices;
+        ++n;
         src = ws + off;
         ld = ld_dst;
     };
-    if (l.pack_x && (a.y || a.dweight)) add(a.x, a.ld_x, 0, a.rows, a.rows, a.width, l.off_x, l.ld_x);
-    if (l.pack_dy) add(a.dy, a.ld_dy, 0, a.rows, a.rows, a.out, l.off_dy, l.ld_dy);
+    p.rows = (uint32_t)a.rows;
+    if (l.pack_x && (a.y || a.dweight)) add(a.x, a.ld_x, 0, a.rows, 1, a.width, l.off_x, l.ld_x, nullptr);
+    if (l.pack_dy) add(a.dy, a.ld_dy, 0, a.rows, 1, a.out, l.off_dy, l.ld_dy, nullptr);
     if (l.pack_w && (a.y || a.dx)) {
-        add(a.weight, a.ld_weight, a.stride_weight, a.out, a.groups * a.out, a.width, l.off_w, l.ld_w);
+        add(a.weight, a.ld_weight, a.stride_weight, a.out, a.groups, a.width, l.off_w, l.ld_w, a.offsets);
         a.stride_weight = a.out * l.ld_w;
     }
     if (n) SK_OP_CUDA(launch_kernel(true, k_grouped_pack, dim3(blocks), 256, 0, st, p));
@@ -845,38 +921,71 @@ int launch_unpack(const GroupedArgs& a, const void* src, uint64_t ld_src, void* 
     return SK_OK;
 }
 
+// What y and dx are made from and go to.
+struct RowsCall {
+    const void* rows;
+    uint64_t ld_rows;
+    bool transposed;                                 // the matrix is read along its rows
+    void* out;
+    uint64_t ld_out;
+};
+
 template <int CG, int BN>
-int launch_rows(const GroupedArgs& a, const void* matrix_rows, uint64_t ld_rows, bool transposed, void* out, uint64_t ld_out, int fill, const OpDevice& dev,
-                cudaStream_t st) {
+int launch_rows(const GroupedArgs& a, const GroupedLayout& l, const RowsCall& c, const OpDevice& dev, cudaStream_t st) {
     using Plan = RowsPlan<CG, BN>;
     static_assert(Plan::kTableOffset == GemmTile<CG, BN, RowsEpi>::kStages * GemmTile<CG, BN, RowsEpi>::kStageBytes);
     Plan p{};
-    const uint32_t K = (uint32_t)(transposed ? a.out : a.width);
+    const uint32_t K = (uint32_t)(c.transposed ? a.out : a.width);
     const bool bf16 = a.type == SK_BF16;
     p.offsets = a.offsets;
     p.groups = (uint32_t)a.groups;
     p.rows = (uint32_t)a.rows;
-    p.features = (uint32_t)(transposed ? a.width : a.out);
+    p.features = (uint32_t)(c.transposed ? a.width : a.out);
     p.tiles_m = (p.features + 128 * CG - 1) / (128 * CG);
     p.k_stages = (K + kGemmK - 1) / kGemmK;
     p.last_k = (K - (p.k_stages - 1) * kGemmK + 15) / 16 * 16;
     p.k_rows = K < kGemmK ? p.last_k : kGemmK;
-    p.mn = transposed;
+    p.slices = l.slices;
+    p.each = (p.k_stages + l.slices - 1) / l.slices;
+    p.mn = c.transposed;
     p.bf16 = bf16;
-    p.fill = fill;
+    p.fill = a.fill;
     p.waits = dev.waits();
-    const Operand w{a.weight, a.out, a.width, a.ld_weight, a.stride_weight, (uint32_t)a.groups, transposed};
-    const Operand x{matrix_rows, a.rows, K, ld_rows, 0, 1, false};
-    bool ok = encode_operand(&p.matrix, w, bf16, transposed ? p.k_rows : 128);
+    const Operand w{a.weight, a.out, a.width, a.ld_weight, a.stride_weight, (uint32_t)a.groups, c.transposed};
+    const Operand x{c.rows, a.rows, K, c.ld_rows, 0, 1, false};
+    bool ok = encode_operand(&p.matrix, w, bf16, c.transposed ? p.k_rows : 128);
     for (int q = 0; q < 4; ++q) ok = ok && encode_operand(&p.rows_map[q], x, bf16, 128 >> q);
     if (!ok) return set_error(SK_ECUDA, "%s: the tensors cannot be described to the copy engine", __func__);
     // rows over BN of each segment, at most one tile more in each
-    const uint64_t live = (a.groups < a.rows ? a.groups : a.rows) + (fill ? 2 : 0), most = (a.rows / BN + live) * p.tiles_m, slots = (uint64_t)dev.sm_count / CG;
-    RowsEpi::Args ea{{}, (uint16_t*)out, ld_out, bf16, row_alignment(out, ld_out, a.type), addressable(out, ld_out)};
-    if (ea.by_box && !encode_out(&ea.map, out, 1, a.rows, p.features, ld_out, a.rows * ld_out, a.type, 16))
+    const uint64_t live = (a.groups < a.rows ? a.groups : a.rows) + (a.fill ? 2 : 0), most = (a.rows / BN + live) * p.tiles_m * l.slices;
+    const uint64_t slots = (uint64_t)dev.sm_count / CG;
+    const uint32_t units = (uint32_t)(most < slots ? most : slots);
+    if constexpr (CG == 1) {
+        if (l.slices > 1) {
+            float* sums = (float*)((uint8_t*)a.workspace + l.off_row_sums);
+            const SumsEpi::Args ea{sums, l.ld_row_sums, a.rows * l.ld_row_sums};
+            SK_OP_CUDA((launch_plan<CG, BN, Plan, SumsEpi>(true, p, ea, units, st)));
+            SK_OP_CUDA(launch_kernel(true, k_grouped_sum, dim3((p.features + 255) / 256, (uint32_t)(a.rows < 4096 ? a.rows : 4096)), 256, 0, st, (const float*)sums, ea.ld,
+                                     ea.stride, l.slices, a.offsets, p.groups, p.rows, p.features, (uint16_t*)c.out, c.ld_out, (int)bf16, a.fill));
+            return SK_OK;
+        }
+    }
+    RowsEpi::Args ea{{}, (uint16_t*)c.out, c.ld_out, bf16, row_alignment(c.out, c.ld_out, a.type), addressable(c.out, c.ld_out)};
+    if (ea.by_box && !encode_out(&ea.map, c.out, 1, a.rows, p.features, c.ld_out, a.rows * c.ld_out, a.type, 16))
         return set_error(SK_ECUDA, "%s: the output cannot be described to the copy engine", __func__);
-    SK_OP_CUDA((launch_plan<CG, BN, Plan, RowsEpi>(true, p, ea, (uint32_t)(most < slots ? most : slots), st)));
+    SK_OP_CUDA((launch_plan<CG, BN, Plan, RowsEpi>(true, p, ea, units, st)));
     return SK_OK;
+}
+// y or dx, to where the layout says
+int launch_rows_any(const GroupedArgs& a, const GroupedLayout& l, bool backward, const OpDevice& dev, cudaStream_t st) {
+    RowsCall c{a.x, a.ld_x, false, a.y, a.ld_y};
+    if (backward) c = {a.dy, a.ld_dy, true, a.dx, a.ld_dx};
+    if (l.unpack_rows) {
+        c.out = (uint8_t*)a.workspace + l.off_rows;
+        c.ld_out = l.ld_rows;
+    }
+    const uint64_t features = backward ? a.width : a.out, k_stages = ((backward ? a.out : a.width) + kGemmK - 1) / kGemmK;
+    return l.slices == 1 && wide_rows(a, features, k_stages, dev.sm_count) ? launch_rows<2, 256>(a, l, c, dev, st) : launch_rows<1, 128>(a, l, c, dev, st);
 }
 
 template <int CG, int BN, bool PARTS>
@@ -900,7 +1009,7 @@ int launch_matrices(const GroupedArgs& a, const GroupedLayout& l, const OpDevice
     for (int q = 0; q < 7; ++q) ok = ok && encode_operand(&p.a[q], dy, bf16, 64 >> q) && encode_operand(&p.b[q], x, bf16, 64 >> q);
     if (!ok) return set_error(SK_ECUDA, "%s: the tensors cannot be described to the copy engine", __func__);
     p.most_slices = l.most_slices;
-    p.beside = a.dx != nullptr;
+    p.beside = a.dx && l.slices == 1;                // the kernel before is the product itself, which releases its successors
     p.slices = (uint32_t*)((uint8_t*)a.workspace + l.off_slices);
     typename MatrixEpi<PARTS>::Args ea{{}, a.dweight, a.ld_dweight, a.groups > 1 ? a.stride_dweight : a.out * a.ld_dweight, a.dweight_type, 0, 0,
                                        (float*)((uint8_t*)a.workspace + l.off_sums), l.ld_sums, nullptr, 0};
@@ -936,23 +1045,17 @@ uint64_t grouped_workspace(const GroupedArgs& a, bool backward) { return layout_
 int launch_grouped(GroupedArgs a, const OpDevice& dev, cudaStream_t st) {
     const GroupedLayout l = layout_of(a, false);
     if (int rc = pack_operands(a, l, dev.sm_count, st)) return rc;
-    auto launch = wide_rows(a, a.out, (a.width + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_rows<2, 256> : launch_rows<1, 128>;
-    if (!l.unpack_rows) return launch(a, a.x, a.ld_x, false, a.y, a.ld_y, a.fill, dev, st);
-    void* rows = (uint8_t*)a.workspace + l.off_rows;
-    if (int rc = launch(a, a.x, a.ld_x, false, rows, l.ld_rows, a.fill, dev, st)) return rc;
-    return launch_unpack(a, rows, l.ld_rows, a.y, a.rows, a.out, a.type, false, dev.sm_count, st);
+    if (int rc = launch_rows_any(a, l, false, dev, st)) return rc;
+    return l.unpack_rows ? launch_unpack(a, (uint8_t*)a.workspace + l.off_rows, l.ld_rows, a.y, a.rows, a.out, a.type, false, dev.sm_count, st) : SK_OK;
 }
 
 int launch_grouped_backward(GroupedArgs a, const OpDevice& dev, cudaStream_t st) {
     const GroupedLayout l = layout_of(a, true);
     if (int rc = pack_operands(a, l, dev.sm_count, st)) return rc;
-    if (a.dx) {
-        auto launch = wide_rows(a, a.width, (a.out + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_rows<2, 256> : launch_rows<1, 128>;
-        void* rows = l.unpack_rows ? (uint8_t*)a.workspace + l.off_rows : a.dx;
-        if (int rc = launch(a, a.dy, a.ld_dy, true, rows, l.unpack_rows ? l.ld_rows : a.ld_dx, a.fill, dev, st)) return rc;
-    }
+    if (a.dx)
+        if (int rc = launch_rows_any(a, l, true, dev, st)) return rc;
     auto unpack_dx = [&] {                           // behind both products: the second one begins while the first still runs
-        return l.unpack_rows ? launch_unpack(a, (uint8_t*)a.workspace + l.off_rows, l.ld_rows, a.dx, a.rows, a.width, a.type, false, dev.sm_count, st) : SK_OK;
+        return a.dx && l.unpack_rows ? launch_unpack(a, (uint8_t*)a.workspace + l.off_rows, l.ld_rows, a.dx, a.rows, a.width, a.type, false, dev.sm_count, st) : SK_OK;
     };
     if (!a.dweight) return unpack_dx();
     // The accumulators' truncation grows with the rows added up: 16-bit gradients of fp16 and 32-bit ones show it, bf16's rounding is coarser.

@@ -184,6 +184,23 @@ def test_long_groups_of_small_matrices(ops, sizes, width, out, dtype):
     check(ops, e, e[-1] + 70, width, out, dtype, dweight_type=torch.float32)
 
 
+# few rows and long sums: K in slices
+@pytest.mark.parametrize("dtype", HALF, ids=str)
+@pytest.mark.parametrize("sizes", [[1], [5, 0, 2], [0, 17, 33, 0], [128, 1], [300]], ids=str)
+@pytest.mark.parametrize("width,out", [(4096, 200), (200, 4096), (3413, 77), (77, 3413), (2050, 1024), (1087, 1025)])
+def test_few_rows_and_long_sums(ops, sizes, width, out, dtype):
+    e = ends(sizes, 3)
+    rows = e[-1] + 4
+    x, dy = randn(1, rows, width, dtype=dtype), randn(3, rows, out, dtype=dtype)
+    y, dx, _ = check(ops, e, rows, width, out, dtype, x=x, dy=dy)
+    w, off = randn(2, len(sizes), out, width, dtype=dtype), offsets_of(e)
+    oy, ox = torch.full_like(y, 7.0), torch.full_like(dx, 5.0)
+    ops.grouped_linear(x, w, off, out=oy)
+    ops.grouped_linear_backward(dy, x, w, off, dx=ox, dweight=False)
+    for o, t, v in ((oy, y, 7), (ox, dx, 5)):
+        assert torch.equal(o[e[0]:e[-1]], t[e[0]:e[-1]]) and bool((o[:e[0]] == v).all()) and bool((o[e[-1]:] == v).all())
+
+
 # outputs of some megabytes whose rows the copy engine cannot write, or that begin off its boundaries
 @pytest.mark.parametrize("dtype", HALF, ids=str)
 @pytest.mark.parametrize("width,out", [(1001, 1333), (1002, 1334), (1004, 1340), (2049, 515), (75, 3001), (1400, 1416)])
