@@ -791,7 +791,8 @@ struct GroupedLayout {
     bool unpack_rows, unpack_matrices;               // y or dx, dW: through the workspace, where rows are whole lines
     uint64_t ld_rows, ld_matrices, off_rows, off_matrices;
 };
-// An output goes through the workspace if its rows cannot be written by the copy engine, if it is one run of values, and if it is large enough for another launch.
+// An output goes through the workspace if it is one run of values, large enough for another launch, and its rows cannot be written by the copy engine (dW; 14 rows of 15 groups
+// of 2822 x 832: 74 us from the tiles, 46 so) or not even in words (y and dx; 12928 rows of 2073: 68 and 58, but of 1954 61 and 65).
 constexpr uint64_t kUnpackBytes = 4 << 20;
 constexpr uint32_t kPlanSms = 148;                   // the slices, and with them the workspace, are planned for a B200
 // How many slices all groups of dW may be cut into, 0: K is not split. Few groups of few tiles, rows enough to be worth another launch (4096 are some 19 us of one
@@ -866,7 +867,7 @@ GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
         l.ld_row_sums = round_up(cols, 32);
         l.off_row_sums = l.total;
         l.total += round_up(l.slices * a.rows * l.ld_row_sums * 4, 256);
-    } else if (rows && ld == cols && !addressable(rows, ld) && a.rows * cols * 2 >= kUnpackBytes) {
+    } else if (rows && ld == cols && row_alignment(rows, ld, SK_BF16) < 4 && a.rows * cols * 2 >= kUnpackBytes) {
         l.unpack_rows = true;
         l.ld_rows = round_up(cols, 64);
         l.off_rows = l.total;
