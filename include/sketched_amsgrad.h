@@ -344,7 +344,9 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
  * x: rows x width, weight: groups matrices of out x width, y: rows x out, all of `type` (SK_BF16 or SK_F16); stride_weight: elements from one matrix
  * to the next.  offsets: groups + 1 int64 on the DEVICE, not decreasing, within 0..rows (what is not is taken as the nearest that is, never as an
  * address).  Rows of no group (before offsets[0], from offsets[groups] on): zero if fill, else left as they were.
- * Sums are the tensor cores' 32-bit ones.  1 <= groups <= 2048; rows <= 2^30; 1 <= width, out <= 2^20.  y may not be x or weight. */
+ * Sums are the tensor cores' 32-bit ones, which truncate (one-sign sums of 4096 products are 1e-5 to 5e-5 too small).  1 <= groups <= 2048;
+ * rows <= 2^30; 1 <= width, out <= 2^20.  y may not be x or weight.  The workspace holds copies of operands whose rows are not 16-byte aligned, a
+ * large output whose rows are not 4-byte aligned, sums of slices of K; none of them for aligned rows of many tiles. */
 uint64_t sk_grouped_linear_workspace(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight,
                                      uint64_t rows, uint64_t groups, uint64_t width, uint64_t out, const void* y, uint64_t ld_y);
 int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight, int type, uint64_t rows,
