@@ -299,7 +299,7 @@ struct PolicyArgs {
     float* dnll;
     float4* workspace;
 };
-int launch_policy(const PolicyArgs& a, cudaStream_t st);
+int launch_policy(PolicyArgs a, cudaStream_t st);
 int launch_policy_backward(const PolicyArgs& a, cudaStream_t st);
 uint64_t policy_workspace(uint64_t tokens, uint64_t sequences);
 

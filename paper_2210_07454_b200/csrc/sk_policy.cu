@@ -186,9 +186,8 @@ __device__ T block_sum(T s) {
     return r;
 }
 
-// workspace: chunks' sums (of all their tokens, or of their first token's sequence), then for each sequence the sum where it begins
-__device__ void join(const PolicyArgs& a, uint32_t chunks) {
-    const float4 *heads = a.workspace, *starts = a.workspace + chunks;
+// heads: chunks' sums (of all their tokens, or of their first token's sequence); starts: for each sequence the sum where it begins
+__device__ void join(const PolicyArgs& a, uint32_t chunks, const float4* heads, const float4* starts) {
     if (!a.average_sequences) {
         Sums s{};
         for (uint32_t c = threadIdx.x; c < chunks; c += blockDim.x) add(s, heads[c]);
@@ -245,8 +244,11 @@ __device__ void join(const PolicyArgs& a, uint32_t chunks) {
     }
 }
 
+// One chunk of few sequences keeps its sums to itself and needs no workspace.
+constexpr uint32_t kOwnSums = 64;
 __global__ void __launch_bounds__(kPolicyThreads, 4) k_policy(const __grid_constant__ PolicyArgs a) {
-    __shared__ float4 of_token[kChunk];
+    __shared__ float4 of_token[kChunk], own[1 + kOwnSums];
+    float4* const sums = a.workspace ? a.workspace : own;
     chain_acquire();
     const uint64_t c0 = (uint64_t)blockIdx.x * kChunk, c1 = min(c0 + kChunk, a.tokens);
     Tokens<kPerThread> t(a, c0, c1);
@@ -272,7 +274,7 @@ __global__ void __launch_bounds__(kPolicyThreads, 4) k_policy(const __grid_const
     const uint32_t chunks = gridDim.x;
     if (!a.average_sequences) {
         s = block_sum(s);
-        if (threadIdx.x == 0) a.workspace[blockIdx.x] = s;
+        if (threadIdx.x == 0) sums[blockIdx.x] = s;
     } else {
         __syncthreads();
         const uint32_t warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -295,18 +297,18 @@ __global__ void __launch_bounds__(kPolicyThreads, 4) k_policy(const __grid_const
                 float4 p = make_float4(0, 0, 0, 0);
                 for (uint32_t i = lane; i < n; i += 32) add(p, of_token[f + i]);
                 warp_sum(p);
-                if ((int)lane == l) a.workspace[begins_here ? chunks + q : blockIdx.x] = p;
+                if ((int)lane == l) sums[begins_here ? chunks + q : blockIdx.x] = p;
             }
         }
     }
     if (chunks > 1) return;
     __syncthreads();
-    join(a, 1);
+    join(a, 1, sums, sums + 1);
 }
 
 __global__ void __launch_bounds__(kPolicyJoin) k_policy_join(const __grid_constant__ PolicyArgs a, uint32_t chunks) {
     chain_acquire();
-    join(a, chunks);
+    join(a, chunks, a.workspace, a.workspace + chunks);
 }
 
 constexpr uint32_t kBackEach = 4;
@@ -341,9 +343,12 @@ uint64_t chunks_of(uint64_t tokens) { return (tokens + kChunk - 1) / kChunk; }
 
 }  // namespace
 
-uint64_t policy_workspace(uint64_t tokens, uint64_t sequences) { return (chunks_of(tokens) + sequences) * sizeof(float4); }
+uint64_t policy_workspace(uint64_t tokens, uint64_t sequences) {
+    return tokens <= kChunk && sequences <= kOwnSums ? 0 : (chunks_of(tokens) + sequences) * sizeof(float4);
+}
 
-int launch_policy(const PolicyArgs& a, cudaStream_t st) {
+int launch_policy(PolicyArgs a, cudaStream_t st) {
+    if (!policy_workspace(a.tokens, a.sequences)) a.workspace = nullptr;
     const uint32_t chunks = (uint32_t)chunks_of(a.tokens);
     SK_OP_CUDA(launch_kernel(true, k_policy, dim3(chunks), kPolicyThreads, 0, st, a));
     // a thread a sequence; sums over the chunks need few

@@ -132,7 +132,9 @@ def _on(stream, call, *given):
 def _run(device, fn, *args):
     """Calls into the library with the tensors' device current."""
     if _current_device() == device:
-        _check(fn(*args))
+        rc = fn(*args)
+        if rc < 0:
+            _check(rc)
     else:
         with torch.cuda.device(device):
             _check(fn(*args))
@@ -536,18 +538,22 @@ def dropout(x, p, seed, residual=None, out=None, stream=None):
     if stream is not None:
         return _on(stream, lambda: dropout(x, p, seed, residual, out), x, seed, residual, out)
     code = _tensor(x, "x", _TYPES)
-    if not x.dim():
+    shape = x.shape
+    if not shape:
         raise SkError("x must have at least 1 dimension")
-    device, cols = x.get_device(), x.shape[-1]
-    rows, ld = _rows(x, "x")
+    device, cols, whole = x.get_device(), shape[-1], x.is_contiguous()
+    rows, ld = (x.numel() // cols if cols else 0, cols) if whole else _rows(x, "x")
     pr, ld_r = None, cols
     if residual is not None:
         if _tensor(residual, "residual", _TYPES, device) != code:
             raise SkError(f"residual has type {residual.dtype}, x {x.dtype}")
-        _same_shape(residual, x, "residual")
-        pr, ld_r = residual.data_ptr(), _rows(residual, "residual")[1]
+        if residual.shape != shape:
+            _same_shape(residual, x, "residual")
+        pr = residual.data_ptr()
+        if not residual.is_contiguous():
+            ld_r = _rows(residual, "residual")[1]
     if out is None:
-        y, ld_y = _new_like(x, x.dtype, device), cols
+        y, ld_y = (_new_on(device)(tuple(shape), x.stride(), x.dtype) if whole else _new_like(x, x.dtype, device)), cols
     else:
         if _tensor(out, "out", _TYPES, device) != code:
             raise SkError(f"out has type {out.dtype}, x {x.dtype}")

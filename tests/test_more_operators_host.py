@@ -105,5 +105,6 @@ def test_policy_loss_checks(L):
                          (dict(high=math.nan), b"clip"), (dict(kl=math.inf), b"kl"), (dict(ref=None), b"reference"), (dict(nll=P + 2), b"aligned"),
                          (dict(t=P + 4), b"aligned"), (dict(off=P + 4), b"aligned")):
             assert refused(L, f(**kw), word), kw
-    assert refused(L, call(result=None), b"null") and refused(L, call(), b"workspace") and refused(L, back(dnll=None), b"null")
-    assert L.sk_policy_loss_workspace(0, 3) == 0 and L.sk_policy_loss_workspace(10, 3) >= 16 * 4
+    assert refused(L, call(result=None), b"null") and refused(L, call(n=5000), b"workspace") and refused(L, back(dnll=None), b"null")
+    assert L.sk_policy_loss_workspace(0, 3) == L.sk_policy_loss_workspace(10, 3) == 0 and L.sk_policy_loss_workspace(10, 3000) >= 16 * 3000
+    assert L.sk_policy_loss_workspace(5000, 3) >= 16 * 6
