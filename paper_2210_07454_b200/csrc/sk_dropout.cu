@@ -42,9 +42,9 @@ __device__ __forceinline__ void apply(const DropoutArgs& a, uint64_t key, uint64
     }
 }
 
-// One run of values, 16-byte aligned: kEach accesses to a thread on their way at once.
+// Values in whole 16-byte accesses: one run of them, or (ROWS) rows of a whole number of accesses, any number of accesses apart. kEach of them to a thread on their way at once.
 constexpr uint32_t kDropThreads = 256, kEach = 4;
-template <typename T, bool RES>
+template <typename T, bool RES, bool ROWS>
 __global__ void __launch_bounds__(kDropThreads) k_dropout_flat(const __grid_constant__ DropoutArgs a, uint64_t n) {
     constexpr uint32_t N = Vec<T>::kN;
     chain_acquire();
@@ -52,12 +52,19 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_flat(const __grid_cons
     const uint4 *x = (const uint4*)a.x, *res = (const uint4*)a.residual;
     uint4* y = (uint4*)a.y;
     uint4 vx[kEach], vr[kEach];
+    uint64_t row[ROWS ? kEach : 1], col[ROWS ? kEach : 1];
+    auto at = [&](uint32_t e, uint64_t v, uint64_t ld) { return ROWS ? row[ROWS ? e : 0] * (ld / N) + col[ROWS ? e : 0] : v; };
 #pragma unroll
     for (uint32_t e = 0; e < kEach; ++e) {
         const uint64_t v = v0 + e * kDropThreads;
         if (v < vectors) {
-            vx[e] = x[v];
-            if (RES) vr[e] = res[v];
+            if constexpr (ROWS) {
+                const uint64_t each = a.cols / N;
+                row[e] = vectors >> 32 ? v / each : (uint32_t)v / (uint32_t)each;
+                col[e] = v - row[e] * each;
+            }
+            vx[e] = x[at(e, v, a.ld_x)];
+            if (RES) vr[e] = res[at(e, v, a.ld_residual)];
         }
     }
 #pragma unroll
@@ -66,9 +73,10 @@ __global__ void __launch_bounds__(kDropThreads) k_dropout_flat(const __grid_cons
         if (v < vectors) {
             uint4 out;
             apply<T, RES>(a, key, v * N, vx[e], vr[e], out);
-            y[v] = out;
+            y[at(e, v, a.ld_y)] = out;
         }
     }
+    if (ROWS) return;
     const uint64_t i = vectors * N + threadIdx.x;                // what is left of a last vector
     if (blockIdx.x == 0 && i < n) {
         const float r = RES ? to_float(((const T*)a.residual)[i]) : 0.0f;
@@ -108,12 +116,12 @@ int launch(const DropoutArgs& a, int sm_count, cudaStream_t st) {
     const uint64_t n = a.rows * a.cols;
     const bool dense = a.rows == 1 || (a.ld_x == a.cols && a.ld_y == a.cols && (!RES || a.ld_residual == a.cols));
     const bool aligned = ((uintptr_t)a.x | (uintptr_t)a.y | (RES ? (uintptr_t)a.residual : 0)) % 16 == 0;
-    if (dense && aligned) {
-        const uint64_t vectors = n / Vec<T>::kN, each = kDropThreads * kEach, blocks = (vectors + each - 1) / each;
-        if (blocks < (1ull << 31)) {
-            SK_OP_CUDA(launch_kernel(true, k_dropout_flat<T, RES>, dim3(blocks ? (uint32_t)blocks : 1), kDropThreads, 0, st, a, n));
-            return SK_OK;
-        }
+    const bool whole = (a.cols | a.ld_x | a.ld_y | (RES ? a.ld_residual : 0)) % Vec<T>::kN == 0;
+    const uint64_t vectors = n / Vec<T>::kN, vectors_each = kDropThreads * kEach, blocks = (vectors + vectors_each - 1) / vectors_each;
+    if (aligned && (dense || whole) && blocks < (1ull << 31)) {
+        auto kernel = dense ? k_dropout_flat<T, RES, false> : k_dropout_flat<T, RES, true>;
+        SK_OP_CUDA(launch_kernel(true, kernel, dim3(blocks ? (uint32_t)blocks : 1), kDropThreads, 0, st, a, n));
+        return SK_OK;
     }
     const uint64_t want = (n + 4 * kDropThreads - 1) / (4 * kDropThreads), most = (uint64_t)sm_count * 32;
     SK_OP_CUDA(launch_kernel(true, k_dropout_rows<T, RES>, dim3((uint32_t)(want < most ? want : most)), kDropThreads, 0, st, a, n));

@@ -708,7 +708,8 @@ cudaError_t launch_products(bool chain, const Operand& a, const Operand& b, Gemm
 }
 
 // Which tile for a product on its own: pairs of blocks on 256 x 256, or single blocks on 128 x 128.  Both take about 620 cycles a stage
-// at an SM, because 32 KB of operands a stage come from L2 at 50 bytes a cycle: measured 617 (pair; its products alone take 512) and 636.  The
+// at an SM, because 32 KB of operands a stage come from L2 at 50 bytes a cycle: measured 617 (pair; its products alone take 512) and 636
+// (570 for the pair since the feeding threads are elected; the choice keeps the figures it was made with).  The
 // pair does twice the work per SM in that time; the small tile ends sooner (its epilogue and start take about 7000 cycles, the pair's
 // 12,000, measured with K = 64) and spreads a small product over more SMs.  The one whose last wave ends first wins.
 inline bool wide_tiles(uint64_t M, uint64_t N, uint64_t stages, int sm_count) {

@@ -4,7 +4,7 @@
 // all warps are made into the places at which each warp's assignments of each expert begin, and the warp walks its run again and deals
 // the places out in order.  Whole numbers throughout: the same result every time.
 //
-// One block does it all for a few thousand assignments.  For more, a first launch counts by blocks, and in the second every block adds up the counts
+// One block does it all for up to 2048 assignments.  For more, a first launch counts by blocks, and in the second every block adds up the counts
 // of the blocks before it (from L2: a table of at most one row for each SM) before it does the same.  Bound by latency: 24 bytes an assignment
 // are little, the chain load - count - barrier - scan - barrier - deal is what takes the time.
 #include "sk_chain.cuh"

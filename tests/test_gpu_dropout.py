@@ -84,7 +84,7 @@ def test_what_is_dropped_may_hold_anything(ops, dtype):
 
 # row lengths and distances that are and are not whole accesses; the mask goes by the value's number, not by its address
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
-@pytest.mark.parametrize("cols,pad,offset", [(64, 8, 0), (64, 8, 1), (65, 0, 1), (40, 3, 0), (7, 1, 2), (1, 4, 3), (1000, 24, 8)])
+@pytest.mark.parametrize("cols,pad,offset", [(64, 8, 0), (64, 16, 8), (64, 4, 4), (4096, 4096, 0), (64, 8, 1), (65, 0, 1), (40, 3, 0), (7, 1, 2), (1, 4, 3), (1000, 24, 8)])
 def test_strides(ops, cols, pad, offset, dtype):
     rows = 37
 
