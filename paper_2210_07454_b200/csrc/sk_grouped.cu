@@ -350,8 +350,10 @@ struct MatrixPlan {
         __shared__ Table t;
         return t;
     }
+    // from L2: a kernel that begins beside the one before it has not passed the wait at which a first-level cache is sure to hold nothing old
+    __device__ __forceinline__ uint32_t border(uint32_t g) const { return bounded((int64_t)__ldcg((const long long*)offsets + g), rows); }
     __device__ __forceinline__ uint32_t length(uint32_t g) const {
-        const uint32_t from = bounded(offsets[g], rows), to = bounded(offsets[g + 1], rows);
+        const uint32_t from = border(g), to = border(g + 1);
         return to > from ? to - from : 0;
     }
     __device__ void prepare(void* memory) const {
@@ -431,7 +433,7 @@ struct MatrixPlan {
             count = order.first[low + 1] - order.first[low];
         }
         if (g >= groups) return false;
-        const uint32_t from = bounded(offsets[g], rows), rest = length(g), stages = (rest + kGemmK - 1) / kGemmK, each = (stages + count - 1) / count;
+        const uint32_t from = border(g), rest = length(g), stages = (rest + kGemmK - 1) / kGemmK, each = (stages + count - 1) / count;
         const uint32_t valid = min(rest - slice * each * kGemmK, each * kGemmK);
         j.M = M;
         j.N = N;

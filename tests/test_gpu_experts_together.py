@@ -136,6 +136,36 @@ def test_in_a_graph(ops, sizes):
     ops.sync()
 
 
+@pytest.mark.parametrize("tokens,groups,width,out", [(40, 6, 64, 256), (3000, 12, 136, 520), (6000, 3, 256, 128)])
+def test_the_second_product_beside_the_first(ops, tokens, groups, width, out):
+    """The product that gives dweight begins while the one for dx still runs; the groups change from replay to replay in the same memory. It gives the bits that it gives alone."""
+    g = torch.Generator(device="cuda").manual_seed(tokens)
+    experts = torch.zeros(tokens, dtype=torch.int64, device="cuda")
+    x, dy = (torch.zeros(tokens, n, dtype=torch.bfloat16, device="cuda") for n in (width, out))
+    w = torch.randn(groups, out, width, generator=g, device="cuda").bfloat16()
+
+    def step():
+        order, _, ends = ops.sort_by_expert(experts, groups)
+        return (ends, *ops.grouped_linear_backward(dy, x, w, ends))
+
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ends, dx, dw = step()
+    for _ in range(40):
+        experts.copy_(torch.randint(-1, groups, (tokens,), generator=g, device="cuda"))
+        x.copy_(torch.randn(tokens, width, generator=g, device="cuda"))
+        dy.copy_(torch.randn(tokens, out, generator=g, device="cuda"))
+        graph.replay()
+        got = dx.clone(), dw.clone()
+        torch.cuda.synchronize()
+        assert torch.equal(ops.grouped_linear_backward(dy, x, w, ends, dweight=False)[0], got[0])
+        torch.cuda.synchronize()
+        assert torch.equal(ops.grouped_linear_backward(dy, x, w, ends, dx=False)[1], got[1])
+    ops.sync()
+
+
 def test_two_graphs_replayed_at_once(ops):
     """Two captures of the same calls, replayed in two streams: nothing of one is the other's."""
     sets = [inputs(s, tokens=20000, width=64, out=48) for s in (1, 2)]
