@@ -399,7 +399,8 @@ int sk_policy_loss(const float* nll, const float* old_nll, const float* advantag
                    double kl, int average_sequences, float* result, float* norm, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* Its gradient, with the norm of the forward pass: dnll = dloss norm ([not clipped] A r + kl (exp(e) - 1)), 0 for tokens that take no part: what
- * sk_linear_cross_entropy_backward takes as dloss.  dloss: one fp32 on the DEVICE, or NULL (1).  dnll may be any of the tokens' fp32 inputs. */
+ * sk_linear_cross_entropy_backward takes as dloss.  dloss: one fp32 on the DEVICE, or NULL (1).  dnll may be any of the tokens' fp32 inputs,
+ * but not norm, dloss or the sequences' advantages. */
 int sk_policy_loss_backward(const float* dloss, const float* nll, const float* old_nll, const float* advantages, int advantage_of_sequences,
                             const int64_t* targets, const int64_t* offsets, uint64_t sequences, const float* reference_nll, uint64_t tokens,
                             double clip_low, double clip_high, double kl, const float* norm, float* dnll, void* stream);

@@ -445,6 +445,8 @@ int sk_policy_loss_backward(const float* dloss, const float* nll, const float* o
     if (int rc = policy_checked(who, a, clip_low, clip_high)) return rc;
     if (!tokens) return SK_OK;
     if (!norm || !dnll) return set_error(SK_EINVAL, "%s: null argument", who);
+    if (dnll == norm || dnll == dloss || (advantage_of_sequences && dnll == advantages))         // read by other tokens' threads too
+        return set_error(SK_EINVAL, "%s: the gradient can be written over what has one value a token only", who);
     return launch_policy_backward(a, (cudaStream_t)stream);
 }
 

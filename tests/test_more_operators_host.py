@@ -108,3 +108,11 @@ def test_policy_loss_checks(L):
     assert refused(L, call(result=None), b"null") and refused(L, call(n=5000), b"workspace") and refused(L, back(dnll=None), b"null")
     assert L.sk_policy_loss_workspace(0, 3) == L.sk_policy_loss_workspace(10, 3) == 0 and L.sk_policy_loss_workspace(10, 3000) >= 16 * 3000
     assert L.sk_policy_loss_workspace(5000, 3) >= 16 * 6
+
+
+def test_policy_gradient_over_what_other_tokens_read(L):
+    def back(of, dnll, dloss=None, a=P):
+        return L.sk_policy_loss_backward(dloss, P, P, a, of, None, P, 2, None, 10, 0.2, 0.2, 0.0, Q, dnll, None)
+
+    for kw in (dict(of=0, dnll=Q), dict(of=1, dnll=Q), dict(of=0, dnll=R, dloss=R), dict(of=1, dnll=R, a=R)):
+        assert refused(L, back(**kw), b"one value a token"), kw
