@@ -846,7 +846,7 @@ GroupedLayout layout_of(const GroupedArgs& a, bool backward) {
     l.off_w = take(l.pack_w, a.groups * a.out, l.ld_w);
     if (backward) {
         l.wide = wide_matrices(a);
-        l.most_slices = (uint32_t)slices_of(a, l.wide);
+        l.most_slices = a.dweight ? (uint32_t)slices_of(a, l.wide) : 0;
         if (l.most_slices) {
             l.ld_sums = round_up(a.width, 32);
             l.off_slices = l.total;

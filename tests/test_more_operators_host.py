@@ -116,3 +116,11 @@ def test_policy_gradient_over_what_other_tokens_read(L):
 
     for kw in (dict(of=0, dnll=Q), dict(of=1, dnll=Q), dict(of=0, dnll=R, dloss=R), dict(of=1, dnll=R, a=R)):
         assert refused(L, back(**kw), b"one value a token"), kw
+
+
+def test_workspace_of_one_gradient(L):
+    """The sums of dweight's slices are asked for with dweight only."""
+    def need(dx, dw, rows=30000, width=64, out=200):
+        return L.sk_grouped_linear_backward_workspace(P, out, P, width, Q, width, out * width, rows, 2, width, out, dx, width, dw, width, out * width, 1)
+
+    assert need(R, None) == 0 < need(None, 2 * R) == need(R, 2 * R)
