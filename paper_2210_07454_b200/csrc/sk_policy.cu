@@ -22,9 +22,8 @@ namespace {
 constexpr uint32_t kPolicyThreads = 256, kPerThread = 8, kChunk = kPolicyThreads * kPerThread;
 constexpr uint32_t kPolicyJoin = 1024;               // threads of the second launch, at most
 
-// exp(e) - e - 1. Below 1 the series, in which nothing cancels (the next term is 2e-9 of the sum); beyond, exp, whose error is at most three times as large
-// relative to the difference. exp(e) - 1 is this plus e.
-__device__ __forceinline__ float k_term(float e) {
+// exp(e) - e - 1 for |e| < 1, by its series, in which nothing cancels: the next term is 3e-9 of the sum at 1, 6e-9 at -1.
+__device__ __forceinline__ float k_series(float e) {
     float s = 1.0f / 39916800;
     s = fmaf(s, e, 1.0f / 3628800);
     s = fmaf(s, e, 1.0f / 362880);
@@ -35,10 +34,12 @@ __device__ __forceinline__ float k_term(float e) {
     s = fmaf(s, e, 1.0f / 24);
     s = fmaf(s, e, 1.0f / 6);
     s = fmaf(s, e, 0.5f);
-    s *= e * e;
-    if (!(fabsf(e) < 1.0f)) s = expf(e) - e - 1.0f;
-    return s;
+    return s * (e * e);
 }
+// exp(e) - e - 1 and its derivative exp(e) - 1. From 1 on by exp, whose error is at most 3.8 and 1.6 times as large relative to the difference (at 1). The derivative is not
+// formed from the value there: e, however large, would be subtracted and added again (-1 became 0 for e below -2^24, NaN for -inf).
+__device__ __forceinline__ float k_term(float e) { return fabsf(e) < 1.0f ? k_series(e) : expf(e) - e - 1.0f; }
+__device__ __forceinline__ float k_slope(float e) { return fabsf(e) < 1.0f ? k_series(e) + e : expf(e) - 1.0f; }
 
 struct Token { float ratio, advantage; bool clipped; };
 // The difference is rounded once, like the argument of exp; it says by itself what is clipped unless it lies within its rounding of the border.
@@ -330,10 +331,7 @@ __global__ void __launch_bounds__(kPolicyThreads) k_policy_backward(const __grid
         if (t.live >> i & 1) {
             const Token p = token_of(a, t.old_nll[i], t.nll[i], t.advantage[i]);
             g = p.clipped ? 0.0f : p.advantage * p.ratio;
-            if (a.reference && a.kl != 0) {
-                const float e = t.nll[i] - t.reference[i];
-                g += a.kl * (k_term(e) + e);
-            }
+            if (a.reference && a.kl != 0) g += a.kl * k_slope(t.nll[i] - t.reference[i]);
             g *= dloss * norm[i];
         }
         if (at < c1) a.dnll[at] = g;
