@@ -385,7 +385,8 @@ int sk_dropout(const void* x, uint64_t ld_x, const void* residual, uint64_t ld_r
 
 /* The clipped policy loss with a KL term, over the losses that sk_linear_cross_entropy gives (nll: of the policy that is trained, old_nll: of
  * the one that drew the tokens, reference_nll: of one it is to stay close to; NULL = none).  Per token, with r = exp(old_nll - nll):
- *   s = A min(r, 1 + clip_high) for A >= 0, A max(r, 1 - clip_low) for A < 0;  e = nll - reference_nll;  k = exp(e) - e - 1;
+ *   s = A min(r, 1 + clip_high) for A >= 0, A max(r, 1 - clip_low) for A < 0 (0 for A = 0, be r infinite);
+ *   e = nll - reference_nll;  k = exp(e) - e - 1;
  *   token loss = -s + kl k.
  * tokens fp32 each; advantages A: one for each token or, if advantage_of_sequences, for each sequence.  Tokens with a negative target take no
  * part (targets may be NULL: all do), whatever their other values are.  offsets: sequences + 1 int64 on the DEVICE, not decreasing; sequence q is

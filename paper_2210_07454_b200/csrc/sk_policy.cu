@@ -7,7 +7,7 @@
 //   d loss / d nll = norm ([not clipped] A r + kl (exp e - 1))
 //
 // What is clipped is decided as on d in 64 bits, where the difference of two 32-bit numbers is exact enough, so that the loss and its gradient, which are
-// two calls, and anyone who computes the formula decide alike.  A min(r, ...) instead of min(A r, ...): an infinite r with A = 0 is 0.
+// two calls, and anyone who computes the formula decide alike.  A = 0 gives 0 however far r or its bound is, beyond 32 bits too.
 //
 // Tokens are taken in chunks of kChunk by a block each.  A chunk adds up what it has of each sequence; a sequence that goes over several chunks has
 // one sum where it begins (unless that is a chunk's first token) and one for each chunk whose first token is its own.  A second launch joins
@@ -57,6 +57,9 @@ __device__ __forceinline__ Token token_of(const PolicyArgs& a, float old_nll, fl
     }
     return v;
 }
+
+// advantage times the ratio or its bound: nothing of what has overflowed
+__device__ __forceinline__ float weighted(float advantage, float by) { return advantage == 0 && isinf(by) ? 0.0f : advantage * by; }
 
 // The number of sequences that begin at or before token t, less one: the token's own (or, behind the last one's end, the number of sequences; before
 // the first, -1).  By a whole warp: 32 probes at a time.
@@ -262,7 +265,7 @@ __global__ void __launch_bounds__(kPolicyThreads, 4) k_policy(const __grid_const
         float4 v = make_float4(0, 0, 0, 0);
         if (t.live >> i & 1) {
             const Token p = token_of(a, t.old_nll[i], t.nll[i], t.advantage[i]);
-            v.x = -p.advantage * (p.clipped ? (p.advantage >= 0 ? a.high : a.low) : p.ratio);
+            v.x = -weighted(p.advantage, p.clipped ? (p.advantage >= 0 ? a.high : a.low) : p.ratio);
             if (a.reference) {
                 v.y = k_term(t.nll[i] - t.reference[i]);
                 if (a.kl != 0) v.x += a.kl * v.y;
@@ -330,7 +333,7 @@ __global__ void __launch_bounds__(kPolicyThreads) k_policy_backward(const __grid
         float g = 0;
         if (t.live >> i & 1) {
             const Token p = token_of(a, t.old_nll[i], t.nll[i], t.advantage[i]);
-            g = p.clipped ? 0.0f : p.advantage * p.ratio;
+            g = p.clipped ? 0.0f : weighted(p.advantage, p.ratio);
             if (a.reference && a.kl != 0) g += a.kl * k_slope(t.nll[i] - t.reference[i]);
             g *= dloss * norm[i];
         }

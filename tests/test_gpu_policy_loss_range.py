@@ -59,3 +59,39 @@ def test_gradient_of_a_token_that_the_reference_excludes_beside_others(ops):
         assert abs(float(got[t]) - value) <= 16 * E * size
     got[[7, 2500]] = want[[7, 2500]]
     assert torch.equal(got, want)
+
+
+# ratios that overflow, by themselves or as a difference of infinite losses, under bounds that do and do not reach them
+@pytest.mark.parametrize("clip", [(0.2, 0.2), (1.0, math.inf), (0.2, 3e38), (0.2, 1e60), (0.0, 0.0)], ids=str)
+@pytest.mark.parametrize("of", ["tokens", "sequences"])
+@pytest.mark.parametrize("zero", [0.0, -0.0])
+def test_an_advantage_of_zero_is_zero_whatever_the_ratio(ops, zero, of, clip):
+    for old in (89.0, 200.0, 3e38, math.inf):
+        nll, a = vector(0.0), vector(zero)
+        offsets = torch.tensor([0, 1], device="cuda")
+        result, norm = ops.policy_loss(nll, vector(old), a, offsets=offsets, clip=clip, advantage_of=of)
+        assert result[0] == 0 and norm.tolist() == [1.0]
+        assert float(result[2]) == (old > math.log1p(clip[1]))
+        assert ops.policy_loss_backward(None, nll, vector(old), a, norm, offsets=offsets, clip=clip, advantage_of=of).tolist() == [0.0]
+
+
+def test_advantages_of_zero_beside_others(ops):
+    """A group of answers of one reward, advantages of zero, next to one with advantages: only the latter counts."""
+    g = torch.Generator(device="cuda").manual_seed(2)
+    nll = torch.rand(4000, generator=g, device="cuda")
+    old = nll + 0.1
+    offsets, a = torch.tensor([0, 1500, 4000], device="cuda"), vector(0.0, 1.5)
+    args = dict(offsets=offsets, clip=(1.0, math.inf), advantage_of="sequences")
+    want, norm = ops.policy_loss(nll, old, a, average="sequences", **args)
+    grad = ops.policy_loss_backward(None, nll, old, a, norm, **args)
+    old[:1500] += 200.0
+    got, norm = ops.policy_loss(nll, old, a, average="sequences", **args)
+    assert torch.equal(got, want)
+    assert torch.equal(ops.policy_loss_backward(None, nll, old, a, norm, **args), grad) and not grad[:1500].any()
+
+
+def test_a_ratio_that_is_no_number_stays_one(ops):
+    for nll, old in ((math.nan, 1.0), (1.0, math.nan), (math.inf, math.inf)):
+        result, norm = ops.policy_loss(vector(nll), vector(old), vector(0.0))
+        assert math.isnan(float(result[0]))
+        assert math.isnan(ops.policy_loss_backward(None, vector(nll), vector(old), vector(0.0), norm).item())
