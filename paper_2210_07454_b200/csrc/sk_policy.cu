@@ -37,8 +37,9 @@ __device__ __forceinline__ float k_series(float e) {
     return s * (e * e);
 }
 // exp(e) - e - 1 and its derivative exp(e) - 1. From 1 on by exp, whose error is at most 3.8 and 1.6 times as large relative to the difference (at 1). The derivative is not
-// formed from the value there: e, however large, would be subtracted and added again (-1 became 0 for e below -2^24, NaN for -inf).
-__device__ __forceinline__ float k_term(float e) { return fabsf(e) < 1.0f ? k_series(e) : expf(e) - e - 1.0f; }
+// formed from the value there: e, however large, would be subtracted and added again (-1 became 0 for e below -2^24, NaN for -inf). Beside exp(128), which overflows, e does
+// not matter, and an infinite one would give inf - inf.
+__device__ __forceinline__ float k_term(float e) { return fabsf(e) < 1.0f ? k_series(e) : expf(e) - fminf(e, 128.0f) - 1.0f; }
 __device__ __forceinline__ float k_slope(float e) { return fabsf(e) < 1.0f ? k_series(e) + e : expf(e) - 1.0f; }
 
 struct Token { float ratio, advantage; bool clipped; };

@@ -95,3 +95,18 @@ def test_a_ratio_that_is_no_number_stays_one(ops):
         result, norm = ops.policy_loss(vector(nll), vector(old), vector(0.0))
         assert math.isnan(float(result[0]))
         assert math.isnan(ops.policy_loss_backward(None, vector(nll), vector(old), vector(0.0), norm).item())
+
+
+def test_divergence_over_its_whole_range(ops):
+    """exp(e) - e - 1, infinite at both ends (a token that the policy or that the reference excludes). exp is 3.8 times as far off relative to the
+    difference at most, 15.2 E; the difference's two roundings."""
+    for v in torch.tensor(FAR + NEAR).float().tolist() + [-math.inf, math.inf]:
+        zero = vector(0.0)
+        for nll, ref in ((zero, vector(-v)), (vector(v), zero)):
+            result, _ = ops.policy_loss(nll, nll, zero, reference_nll=ref, kl=0.5) if math.isfinite(v) else ops.policy_loss(nll, zero, zero, reference_nll=ref, kl=0.5)
+            want = math.inf if v > 700 or math.isinf(v) else math.expm1(v) - v if abs(v) > 1e-3 else v * v / 2 * (1 + v / 3 * (1 + v / 4))
+            if want > 3.4e38:
+                assert float(result[1]) == math.inf and float(result[0]) == math.inf, (v, result)
+            else:
+                assert abs(float(result[1]) - want) <= 20 * E * want, (v, result)
+                assert abs(float(result[0]) - 0.5 * want) <= 22 * E * 0.5 * want, (v, result)
