@@ -14,7 +14,7 @@
 namespace sk {
 namespace {
 
-constexpr uint32_t kSortThreads = 1024;
+constexpr uint32_t kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr uint32_t kOneBlock = 2048;                 // assignments that one block sorts by itself
 constexpr uint32_t kSortChunk = 1024;                // and that a block of many takes at least
 
@@ -91,7 +91,7 @@ __device__ __forceinline__ uint32_t warp_scan(uint32_t v) {
 
 __global__ void __launch_bounds__(kSortThreads) k_sort(const __grid_constant__ Sort s) {
     extern __shared__ __align__(16) uint32_t memory[];
-    __shared__ uint32_t sums[kSortThreads / 32];
+    __shared__ uint32_t sums[kSortWarps];
     const uint32_t keys = s.a.groups + 1, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     // counts in all blocks, in the blocks before this one; by warps
     uint32_t *total = memory, *before = total + s.row, *table = before + s.row;
@@ -158,7 +158,7 @@ __global__ void __launch_bounds__(kSortThreads) k_sort(const __grid_constant__ S
             before[g] += start;
             if (blockIdx.x == 0) s.a.offsets[g] = start;         // of those that belong to no expert: where those of the last one end
         }
-        carry += sums[kSortThreads / 32 - 1];
+        carry += sums[kSortWarps - 1];
         __syncthreads();
     }
     if (warp >= s.warps) return;
@@ -187,14 +187,15 @@ uint64_t sort_workspace(uint64_t n, uint32_t groups, int sm_count) {
 }
 
 int launch_sort(const SortArgs& a, int sm_count, cudaStream_t st) {
-    Sort s{a, blocks_of(a.n, sm_count), 0, kSortThreads / 32, row_of(a.groups), a.groups + 1, 0};
+    Sort s{a, blocks_of(a.n, sm_count), 0, kSortWarps, row_of(a.groups), a.groups + 1, 0};
     while (a.groups >> s.bits) ++s.bits;
     s.chunk = (uint32_t)((a.n + s.blocks - 1) / s.blocks);
     s.blocks = (uint32_t)((a.n + s.chunk - 1) / s.chunk);
     const uint64_t most = 200 << 10;                 // bytes of shared memory
     while ((2ull * s.row + s.warps * s.pitch) * 4 > most) s.warps /= 2;
     const uint32_t smem = (2 * s.row + s.warps * s.pitch) * 4;
-    if (smem > 48 << 10) SK_OP_CUDA(cudaFuncSetAttribute(k_sort, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most));
+    // the limit without leave is that of the tables and the kernel's own variables together (360 experts are over it by those alone)
+    if (smem + kSortWarps * 4 > 48 << 10) SK_OP_CUDA(cudaFuncSetAttribute(k_sort, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)most));
     if (s.blocks > 1) SK_OP_CUDA(launch_kernel(true, k_sort_count, dim3(s.blocks), kSortThreads, s.row * 4, st, s));
     SK_OP_CUDA(launch_kernel(true, k_sort, dim3(s.blocks), kSortThreads, smem, st, s));
     return SK_OK;
