@@ -355,8 +355,9 @@ int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t
 
 /* Its gradients: dx_i = W_g^T dy_i (rows of no group: as for y), dweight_g = sum over the rows of group g of dy_i x_i^T (zero for an empty group).
  * dy: rows x out, dx: rows x width, of `type`; dweight: groups matrices of out x width, of `type` or SK_F32, stride_dweight apart (it may be a
- * slice of the gradient array of sk_step); dx and dweight may be NULL.  For SK_F32 and fp16 dweight is added up in parts of 1024 rows with rounding
- * between them; for bf16 in the tensor cores' accumulators alone, whose truncation stays below its rounding.  No output may be an input. */
+ * slice of the gradient array of sk_step); dx and dweight may be NULL.  For SK_F32 and fp16, and for bf16 from more than 131072 rows, dweight is
+ * added up in parts of 1024 rows with rounding between them; for bf16 from fewer in the tensor cores' accumulators alone, whose truncation (up to
+ * 8e-4 of a sum of one sign) stays below its rounding.  No output may be an input. */
 uint64_t sk_grouped_linear_backward_workspace(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight,
                                               uint64_t ld_weight, uint64_t stride_weight, uint64_t rows, uint64_t groups, uint64_t width,
                                               uint64_t out, const void* dx, uint64_t ld_dx, const void* dweight, uint64_t ld_dweight,

@@ -329,6 +329,10 @@ __global__ void __launch_bounds__(256) k_grouped_sum(const float* sums, uint64_t
     }
 }
 
+// What the tensor cores truncate grows with the length of a sum: some 6e-9 of a sum of one sign for each of its products, 6.5e-3 of 1048576, where bf16's half step is 3.9e-3. For
+// dW from more rows than this (a fifth of that half step, if they are one group's) sums are taken in parts: 131072 rows of 768 x 2048 296 -> 298 us in 32 groups, 400 -> 421 in 256.
+constexpr uint64_t kLongRows = 131072;
+
 // dW by tiles of 128 CG x BN of every matrix, the longest groups first; units take them up and down in turn, so that what one has too much in one round
 // it has too little in the next (in the groups' own order, 32 groups of 16384 rows kept one pair of blocks busy for 82,000 cycles and another for 55,000).
 // Where there are few tiles, K is split: the longest slice is made as short as it can be with as many slices as there are units, or twice as many. A group
@@ -1061,8 +1065,8 @@ int launch_grouped_backward(GroupedArgs a, const OpDevice& dev, cudaStream_t st)
         return a.dx && l.unpack_rows ? launch_unpack(a, (uint8_t*)a.workspace + l.off_rows, l.ld_rows, a.dx, a.rows, a.width, a.type, false, dev.sm_count, st) : SK_OK;
     };
     if (!a.dweight) return unpack_dx();
-    // The accumulators' truncation grows with the rows added up: 16-bit gradients of fp16 and 32-bit ones show it, bf16's rounding is coarser.
-    const bool parts = a.dweight_type == SK_F32 || a.type == SK_F16;
+    // The accumulators' truncation grows with the rows added up: 16-bit gradients of fp16 and 32-bit ones show it, bf16's coarser rounding that of long groups only.
+    const bool parts = a.dweight_type == SK_F32 || a.type == SK_F16 || a.rows > kLongRows;
     auto launch = parts ? (l.wide ? launch_matrices<2, 256, true> : launch_matrices<1, 128, true>)
                         : (l.wide ? launch_matrices<2, 256, false> : launch_matrices<1, 128, false>);
     if (int rc = launch(a, l, dev, st)) return rc;
