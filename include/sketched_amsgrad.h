@@ -344,7 +344,9 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
  * x: rows x width, weight: groups matrices of out x width, y: rows x out, all of `type` (SK_BF16 or SK_F16); stride_weight: elements from one matrix
  * to the next.  offsets: groups + 1 int64 on the DEVICE, not decreasing, within 0..rows (what is not is taken as the nearest that is, never as an
  * address).  Rows of no group (before offsets[0], from offsets[groups] on): zero if fill, else left as they were.
- * Sums are the tensor cores' 32-bit ones, which truncate (one-sign sums of 4096 products are 1e-5 to 5e-5 too small).  1 <= groups <= 2048;
+ * Sums are the tensor cores' 32-bit ones, which truncate: a sum of one sign of K products comes out too small by some 6.5e-9 K of itself (1e-5 to 5e-5
+ * for 4096).  Up to K = 131072 (bf16) and 32768 (fp16) that stays below half of the outputs' half step, 2^-8 and 2^-11; longer sums are taken in
+ * parts of 1024 products with rounding between them.  1 <= groups <= 2048;
  * rows <= 2^30; 1 <= width, out <= 2^20.  y may not be x or weight.  The workspace holds copies of operands whose rows are not 16-byte aligned, a
  * large output whose rows are not 4-byte aligned, sums of slices of K; none of them for aligned rows of many tiles. */
 uint64_t sk_grouped_linear_workspace(const void* x, uint64_t ld_x, const void* weight, uint64_t ld_weight, uint64_t stride_weight,
@@ -357,7 +359,7 @@ int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t
  * dy: rows x out, dx: rows x width, of `type`; dweight: groups matrices of out x width, of `type` or SK_F32, stride_dweight apart (it may be a
  * slice of the gradient array of sk_step); dx and dweight may be NULL.  For SK_F32 and fp16, and for bf16 from more than 131072 rows, dweight is
  * added up in parts of 1024 rows with rounding between them; for bf16 from fewer in the tensor cores' accumulators alone, whose truncation (up to
- * 8e-4 of a sum of one sign) stays below its rounding.  No output may be an input. */
+ * 9e-4 of a sum of one sign) stays below its rounding.  No output may be an input. */
 uint64_t sk_grouped_linear_backward_workspace(const void* dy, uint64_t ld_dy, const void* x, uint64_t ld_x, const void* weight,
                                               uint64_t ld_weight, uint64_t stride_weight, uint64_t rows, uint64_t groups, uint64_t width,
                                               uint64_t out, const void* dx, uint64_t ld_dx, const void* dweight, uint64_t ld_dweight,

@@ -27,6 +27,13 @@ namespace {
 constexpr uint32_t kSegments = kMaxGroups + 2;       // the groups, the rows before the first and behind the last
 constexpr uint32_t kTableWords = 2 * (kSegments + 1);
 
+// What the tensor cores truncate grows with the length of a sum: 6.5e-9 of a sum of one sign for each of its products (32768 to 1048576 of them), so that it would pass the half step
+// of an fp16 output (4.9e-4) beyond 75000, of a bf16 one (3.9e-3) beyond 600000. Sums longer than these, where it is less than half of that, are taken in parts of kPartStages
+// stages, which the epilogue adds up with rounding; for dW it goes by all rows together, and those of fp16 and fp32 are always in parts. 4096 rows of 4 groups of 32832 x 4096 fp16
+// 870 -> 1050 us so, 2048 of 2 of 131136 x 2048 bf16 755 -> 1005 (in tiles of single blocks); dW of 131073 rows, 768 x 2048, 296 -> 298 in 32 groups, 400 -> 421 in 256.
+constexpr uint32_t kPartStages = 16;
+constexpr uint64_t long_sum(bool bf16) { return bf16 ? 131072 : 32768; }
+
 // The group boundaries as the kernels take them: never decreasing, never outside 0..rows, whatever the offsets hold.
 __device__ __forceinline__ uint32_t bounded(int64_t v, uint32_t rows) { return v < 0 ? 0 : v > (int64_t)rows ? rows : (uint32_t)v; }
 
@@ -230,7 +237,7 @@ struct RowsPlan {
         j.a_mn = mn;
         j.b_mn = 0;
         j.bf16 = bf16;
-        j.part = j.k_stages;
+        j.part = kPartStages;
         return true;
     }
     __device__ __forceinline__ const uint32_t* table() const {
@@ -282,32 +289,46 @@ struct RowsPlan {
     __device__ __forceinline__ const CUtensorMap* descriptor(uint32_t i) const { return i == 0 ? &matrix : i < 5 ? &rows_map[i - 1] : nullptr; }
 };
 
-// Where there are few tiles and K is long, it is split: slices' sums in 32 bits, rows and columns as in the output, joined by k_grouped_sum. A lane holds an output
-// column, so that a warp writes 32 neighbouring ones of a row.
-struct SumsEpi {
+// The tile written by the lanes, which hold an output column each, so that a warp writes 32 neighbouring ones of a row. Where there are few tiles and K is long, it is split:
+// slices' sums in 32 bits, rows and columns as in the output, joined by k_grouped_sum. FINAL: the output itself, of sums that are taken in parts (PARTS, see long_sum), whose
+// epilogue is nothing beside their length.
+template <bool PARTS, bool FINAL>
+struct LanesEpi {
     static constexpr int kWarps = RowsEpi::kWarps, kWords = RowsEpi::kWords;
-    static constexpr bool kParts = false, kInterleaved = true;
-    struct Args { float* sums; uint64_t ld, stride; };           // stride: from slice to slice
+    static constexpr bool kParts = PARTS, kInterleaved = !PARTS;
+    using Out = std::conditional_t<FINAL, uint16_t, float>;
+    struct Args { Out* out; uint64_t ld, stride; uint32_t bf16; };           // stride: from slice to slice
     const Args& a;
     const RaggedJob& t;
     uint32_t feature;
-    __device__ SumsEpi(const Args& a_, const RaggedJob& t_, uint32_t row, uint32_t, uint32_t) : a(a_), t(t_), feature(row) {}
+    __device__ LanesEpi(const Args& a_, const RaggedJob& t_, uint32_t row, uint32_t, uint32_t) : a(a_), t(t_), feature(row) {}
     template <class Plan> __device__ bool begin(const Plan&, uint32_t) { return true; }
     __device__ static void finish() {}
-    __device__ static uint32_t column(const RaggedJob& t, uint32_t part, uint32_t c, uint32_t cols, uint32_t bn) { return RowsEpi::column(t, part, c, cols, bn); }
+    __device__ static uint32_t column(const RaggedJob& t, uint32_t part, uint32_t c, uint32_t cols, uint32_t bn) {
+        return PARTS ? part * cols + c : RowsEpi::column(t, part, c, cols, bn);
+    }
     __device__ static void load(uint32_t addr, float (&v)[32]) { tmem_load32(addr, v); }
     __device__ void chunk(uint32_t col, float (&v)[32], bool) {
-        float* o = a.sums + t.slice * a.stride + (uint64_t)(t.first + col) * a.ld + feature;
+        Out* o = a.out + (FINAL ? 0 : t.slice * a.stride) + (uint64_t)(t.first + col) * a.ld + feature;
         const uint32_t rows = t.N - col;
         if (feature < t.M) {
 #pragma unroll
             for (uint32_t i = 0; i < 32; ++i)
-                if (i < rows) o[i * a.ld] = v[i];
+                if (i < rows) {
+                    if constexpr (FINAL) o[i * a.ld] = (uint16_t)pack16(v[i], 0.0f, a.bf16);
+                    else o[i * a.ld] = v[i];
+                }
         }
         __syncwarp();
     }
     __device__ void end() {}
-    __device__ void nothing(uint32_t, uint32_t, uint32_t, uint32_t) {}           // rows of no group: left to what joins the slices
+    __device__ void nothing(uint32_t part, uint32_t cols, uint32_t bn, uint32_t) {           // rows of no group: slices leave them to what joins them
+        if constexpr (FINAL) {
+            float v[32] = {};
+#pragma unroll 1
+            for (uint32_t c = 0; c < cols && column(t, part, c, cols, bn) < t.N; c += 32) chunk(column(t, part, c, cols, bn), v, false);
+        }
+    }
 };
 // The slices in order, a thread a value. Rows of no group become zero with fill, else stay.
 __global__ void __launch_bounds__(256) k_grouped_sum(const float* sums, uint64_t ld_sums, uint64_t stride, uint32_t slices, const int64_t* offsets, uint32_t groups,
@@ -329,10 +350,6 @@ __global__ void __launch_bounds__(256) k_grouped_sum(const float* sums, uint64_t
     }
 }
 
-// What the tensor cores truncate grows with the length of a sum: some 6e-9 of a sum of one sign for each of its products, 6.5e-3 of 1048576, where bf16's half step is 3.9e-3. For
-// dW from more rows than this (a fifth of that half step, if they are one group's) sums are taken in parts: 131072 rows of 768 x 2048 296 -> 298 us in 32 groups, 400 -> 421 in 256.
-constexpr uint64_t kLongRows = 131072;
-
 // dW by tiles of 128 CG x BN of every matrix, the longest groups first; units take them up and down in turn, so that what one has too much in one round
 // it has too little in the next (in the groups' own order, 32 groups of 16384 rows kept one pair of blocks busy for 82,000 cycles and another for 55,000).
 // Where there are few tiles, K is split: the longest slice is made as short as it can be with as many slices as there are units, or twice as many. A group
@@ -343,7 +360,7 @@ template <int CG, int BN>
 struct MatrixPlan {
     CUtensorMap a[7], b[7];                          // dy and x, boxes of 64, 32, ... 1 rows
     const int64_t* offsets;
-    uint32_t groups, rows, M, N, tiles_m, tiles_n, bf16, part;
+    uint32_t groups, rows, M, N, tiles_m, tiles_n, bf16;
     uint32_t most_slices;                            // of all groups together; 0: none is split
     uint32_t beside;                                 // it may run beside the kernel before it, the product that gives dx
     uint32_t* slices;                                // for each group their number, and that of the first one's sums
@@ -453,7 +470,7 @@ struct MatrixPlan {
         j.k_rows = kGemmK;
         j.a_mn = j.b_mn = 1;
         j.bf16 = bf16;
-        j.part = part;
+        j.part = kPartStages;
         return true;
     }
     struct Feed {
@@ -968,12 +985,18 @@ int launch_rows(const GroupedArgs& a, const GroupedLayout& l, const RowsCall& c,
     const uint64_t slots = (uint64_t)dev.sm_count / CG;
     const uint32_t units = (uint32_t)(most < slots ? most : slots);
     if constexpr (CG == 1) {
+        const bool parts = K > long_sum(bf16);
         if (l.slices > 1) {
             float* sums = (float*)((uint8_t*)a.workspace + l.off_row_sums);
-            const SumsEpi::Args ea{sums, l.ld_row_sums, a.rows * l.ld_row_sums};
-            SK_OP_CUDA((launch_plan<CG, BN, Plan, SumsEpi>(true, p, ea, units, st)));
-            SK_OP_CUDA(launch_kernel(true, k_grouped_sum, dim3((p.features + 255) / 256, (uint32_t)(a.rows < 4096 ? a.rows : 4096)), 256, 0, st, (const float*)sums, ea.ld,
-                                     ea.stride, l.slices, a.offsets, p.groups, p.rows, p.features, (uint16_t*)c.out, c.ld_out, (int)bf16, a.fill));
+            const uint64_t stride = a.rows * l.ld_row_sums;
+            if (parts) SK_OP_CUDA((launch_plan<CG, BN, Plan, LanesEpi<true, false>>(true, p, {sums, l.ld_row_sums, stride, bf16}, units, st)));
+            else SK_OP_CUDA((launch_plan<CG, BN, Plan, LanesEpi<false, false>>(true, p, {sums, l.ld_row_sums, stride, bf16}, units, st)));
+            SK_OP_CUDA(launch_kernel(true, k_grouped_sum, dim3((p.features + 255) / 256, (uint32_t)(a.rows < 4096 ? a.rows : 4096)), 256, 0, st, (const float*)sums, l.ld_row_sums,
+                                     stride, l.slices, a.offsets, p.groups, p.rows, p.features, (uint16_t*)c.out, c.ld_out, (int)bf16, a.fill));
+            return SK_OK;
+        }
+        if (parts) {
+            SK_OP_CUDA((launch_plan<CG, BN, Plan, LanesEpi<true, true>>(true, p, {(uint16_t*)c.out, c.ld_out, 0, bf16}, units, st)));
             return SK_OK;
         }
     }
@@ -991,8 +1014,8 @@ int launch_rows_any(const GroupedArgs& a, const GroupedLayout& l, bool backward,
         c.out = (uint8_t*)a.workspace + l.off_rows;
         c.ld_out = l.ld_rows;
     }
-    const uint64_t features = backward ? a.width : a.out, k_stages = ((backward ? a.out : a.width) + kGemmK - 1) / kGemmK;
-    return l.slices == 1 && wide_rows(a, features, k_stages, dev.sm_count) ? launch_rows<2, 256>(a, l, c, dev, st) : launch_rows<1, 128>(a, l, c, dev, st);
+    const uint64_t features = backward ? a.width : a.out, K = backward ? a.out : a.width;
+    return l.slices == 1 && K <= long_sum(a.type == SK_BF16) && wide_rows(a, features, (K + kGemmK - 1) / kGemmK, dev.sm_count) ? launch_rows<2, 256>(a, l, c, dev, st) : launch_rows<1, 128>(a, l, c, dev, st);
 }
 
 template <int CG, int BN, bool PARTS>
@@ -1009,7 +1032,6 @@ int launch_matrices(const GroupedArgs& a, const GroupedLayout& l, const OpDevice
     p.tiles_m = (p.M + 128 * CG - 1) / (128 * CG);
     p.tiles_n = (p.N + BN - 1) / BN;
     p.bf16 = bf16;
-    p.part = 16;
     p.waits = dev.waits();
     const Operand dy{a.dy, a.rows, a.out, a.ld_dy, 0, 1, true}, x{a.x, a.rows, a.width, a.ld_x, 0, 1, true};
     bool ok = true;
@@ -1066,7 +1088,7 @@ int launch_grouped_backward(GroupedArgs a, const OpDevice& dev, cudaStream_t st)
     };
     if (!a.dweight) return unpack_dx();
     // The accumulators' truncation grows with the rows added up: 16-bit gradients of fp16 and 32-bit ones show it, bf16's coarser rounding that of long groups only.
-    const bool parts = a.dweight_type == SK_F32 || a.type == SK_F16 || a.rows > kLongRows;
+    const bool parts = a.dweight_type == SK_F32 || a.type == SK_F16 || a.rows > long_sum(true);
     auto launch = parts ? (l.wide ? launch_matrices<2, 256, true> : launch_matrices<1, 128, true>)
                         : (l.wide ? launch_matrices<2, 256, false> : launch_matrices<1, 128, false>);
     if (int rc = launch(a, l, dev, st)) return rc;
