@@ -342,8 +342,8 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
 /* The products of a layer of experts.  Group g is the rows offsets[g] .. offsets[g + 1] - 1 of x (a group may be empty), matrix g is weight's g-th:
  *   y_i = W_g x_i  for the rows i of group g.
  * x: rows x width, weight: groups matrices of out x width, y: rows x out, all of `type` (SK_BF16 or SK_F16); stride_weight: elements from one matrix
- * to the next.  offsets: groups + 1 int64 on the DEVICE, not decreasing, within 0..rows (what is not is taken as the nearest that is, never as an
- * address).  Rows of no group (before offsets[0], from offsets[groups] on): zero if fill, else left as they were.
+ * to the next.  offsets: groups + 1 int64 on the DEVICE, not decreasing; what lies outside 0..rows is taken as the nearest that does not.  (Which
+ * rows are whose if they do decrease is left open, and not the same for y, dx and dweight; no address comes of them.)  Rows of no group (before offsets[0], from offsets[groups] on): zero if fill, else left as they were.
  * Sums are the tensor cores' 32-bit ones, which truncate: a sum of one sign of K products comes out too small by some 6.5e-9 K of itself (1e-5 to 5e-5
  * for 4096).  Up to K = 131072 (bf16) and 32768 (fp16) that stays below half of the outputs' half step, 2^-8 and 2^-11; longer sums are taken in
  * parts of 1024 products with rounding between them.  1 <= groups <= 2048;

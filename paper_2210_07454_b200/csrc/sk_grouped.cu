@@ -34,7 +34,8 @@ constexpr uint32_t kTableWords = 2 * (kSegments + 1);
 constexpr uint32_t kPartStages = 16;
 constexpr uint64_t long_sum(bool bf16) { return bf16 ? 131072 : 32768; }
 
-// The group boundaries as the kernels take them: never decreasing, never outside 0..rows, whatever the offsets hold.
+// A boundary of a group as the kernels take it: never outside 0..rows, whatever the offsets hold. (Offsets that decrease: the plans differ in what they make of them, nothing is read or
+// written outside the tensors.)
 __device__ __forceinline__ uint32_t bounded(int64_t v, uint32_t rows) { return v < 0 ? 0 : v > (int64_t)rows ? rows : (uint32_t)v; }
 
 // 16 rows of 64 bytes in shared memory (64-byte swizzle) to rows that begin anywhere: every row's aligned words, two rows at a time, then the values before

@@ -451,8 +451,8 @@ def _grouped(x, weight, offsets):
 
 def grouped_linear(x, weight, offsets, out=None, stream=None):
     """y[i] = weight[g] x[i] for the rows i of every group g: offsets[g] <= i < offsets[g + 1].  x: (rows, width), weight: (groups, out, width), both
-    bf16 or both fp16; offsets: (groups + 1,) int64 on the same device (see ``sort_by_expert``), which the host never reads.  Returns (rows, out) of
-    x's type.  Rows of no group are zero, or left as they were in an ``out`` that is given."""
+    bf16 or both fp16; offsets: (groups + 1,) int64 on the same device (see ``sort_by_expert``), not decreasing, which the host never reads.  Returns
+    (rows, out) of x's type.  Rows of no group are zero, or left as they were in an ``out`` that is given."""
     if stream is not None:
         return _on(stream, lambda: grouped_linear(x, weight, offsets, out), x, weight, offsets, out)
     device, code, rows, groups, width, n, ld_x, ld_w, s_w, po = _grouped(x, weight, offsets)
