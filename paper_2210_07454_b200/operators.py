@@ -525,9 +525,12 @@ def _seed(seed, device):
         _vector(seed, "seed", 1, _INT64, device)
         return 0, seed.data_ptr()
     try:
-        return int(seed) & 0xFFFFFFFFFFFFFFFF, None
-    except (TypeError, ValueError):
-        raise SkError("seed must be a whole number or a CUDA tensor of one int64") from None
+        value = int(seed)
+        if value == seed:                            # nothing that had to be rounded
+            return value & 0xFFFFFFFFFFFFFFFF, None
+    except (TypeError, ValueError, OverflowError):
+        pass
+    raise SkError("seed must be a whole number or a CUDA tensor of one int64")
 
 
 def dropout(x, p, seed, residual=None, out=None, stream=None):
