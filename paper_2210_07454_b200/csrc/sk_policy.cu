@@ -40,10 +40,15 @@ __device__ __forceinline__ float k_series(float e) {
 // formed from the value there: e, however large, would be subtracted and added again (-1 became 0 for e below -2^24, NaN for -inf). Beside exp(128), which overflows, e does
 // not matter, and an infinite one would give inf - inf.
 __device__ __forceinline__ float k_term(float e) { return fabsf(e) < 1.0f ? k_series(e) : expf(e) - fminf(e, 128.0f) - 1.0f; }
-__device__ __forceinline__ float k_slope(float e) { return fabsf(e) < 1.0f ? k_series(e) + e : expf(e) - 1.0f; }
+__device__ __forceinline__ float k_slope(float e) {
+    float s = k_series(e) + e;
+    if (!(fabsf(e) < 1.0f)) s = expf(e) - 1.0f;
+    return s;
+}
 
-struct Token { float ratio, advantage; bool clipped; };
-// The difference is rounded once, like the argument of exp; it says by itself what is clipped unless it lies within its rounding of the border.
+struct Token { float ratio, held, advantage; bool clipped; };        // held: the bound that takes the ratio's place
+// The difference is rounded once, like the argument of exp; it says by itself what is clipped unless it lies within its rounding of the border. Ratios that may overflow, as rare,
+// take the same branch: of an advantage of zero they leave nothing. (Asked for each product by itself, that took the gradient of 1000003 tokens from 8.1 to 8.6 us.)
 __device__ __forceinline__ Token token_of(const PolicyArgs& a, float old_nll, float nll, float advantage) {
     const float d = old_nll - nll;
     Token v;
@@ -52,15 +57,14 @@ __device__ __forceinline__ Token token_of(const PolicyArgs& a, float old_nll, fl
     const bool up = advantage >= 0;
     const float border = up ? a.border_high : a.border_low;
     v.clipped = up ? d > border : d < border;
-    if (fabsf(d - border) <= 0x1p-21f * fabsf(border)) {
+    v.held = up ? a.high : a.low;
+    if (fabsf(d - border) <= 0x1p-21f * fabsf(border) || d > 88.0f) {
         const double exact = (double)old_nll - (double)nll;
         v.clipped = up ? exact > a.log_high : exact < a.log_low;
+        if (advantage == 0 && d > 88.0f) v.ratio = v.held = 0.0f;
     }
     return v;
 }
-
-// advantage times the ratio or its bound: nothing of what has overflowed
-__device__ __forceinline__ float weighted(float advantage, float by) { return advantage == 0 && isinf(by) ? 0.0f : advantage * by; }
 
 // The number of sequences that begin at or before token t, less one: the token's own (or, behind the last one's end, the number of sequences; before
 // the first, -1).  By a whole warp: 32 probes at a time.
@@ -266,7 +270,7 @@ __global__ void __launch_bounds__(kPolicyThreads, 4) k_policy(const __grid_const
         float4 v = make_float4(0, 0, 0, 0);
         if (t.live >> i & 1) {
             const Token p = token_of(a, t.old_nll[i], t.nll[i], t.advantage[i]);
-            v.x = -weighted(p.advantage, p.clipped ? (p.advantage >= 0 ? a.high : a.low) : p.ratio);
+            v.x = -p.advantage * (p.clipped ? p.held : p.ratio);
             if (a.reference) {
                 v.y = k_term(t.nll[i] - t.reference[i]);
                 if (a.kl != 0) v.x += a.kl * v.y;
@@ -334,7 +338,7 @@ __global__ void __launch_bounds__(kPolicyThreads) k_policy_backward(const __grid
         float g = 0;
         if (t.live >> i & 1) {
             const Token p = token_of(a, t.old_nll[i], t.nll[i], t.advantage[i]);
-            g = p.clipped ? 0.0f : weighted(p.advantage, p.ratio);
+            g = p.clipped ? 0.0f : p.advantage * p.ratio;
             if (a.reference && a.kl != 0) g += a.kl * k_slope(t.nll[i] - t.reference[i]);
             g *= dloss * norm[i];
         }
