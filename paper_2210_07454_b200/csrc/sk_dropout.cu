@@ -6,7 +6,7 @@
 // One draw serves four values, so that the generator (some twenty integer instructions) stays behind the memory traffic: with 32 bits a value it would take
 // about as long as reading and writing 16-bit values does.  What is lost is the resolution of p, 2^-16; the factor is that of the rounded p, so
 // that the mean is kept exactly.  Bound by HBM: every value is read once and written once. 32768 x 4096 bf16 with a residual (805 MB) 116 us, 6.9 TB/s; rows twice as far apart at the
-// same rate; rows off the 16-byte boundary 2.3 TB/s (bf16) and 4.9 (fp32), a draw's values to a thread.
+// same rate; rows off the 16-byte boundary 2.4 TB/s (bf16) and 4.9 (fp32): a draw's values to a thread, by single accesses.
 #include "sk_chain.cuh"
 #include "sk_operators.h"
 

@@ -10,12 +10,13 @@
 // blocks: 32), and only those rows are copied. (With rows of x as the first operand a group of 300 rows takes two tiles of 256, of which 41 % are
 // nobody's.) A group's rows are shared out evenly among its tiles. The tile comes out transposed and is turned round on its way through shared
 // memory. Every block makes the list of tiles for itself, from the offsets, in shared memory.
-// 16384 x 768 x 2048 in one group 38 us (1.36 PFLOP/s), in 32 groups of 102 to 1684 rows 48; 16 groups of 4096 x 2048 197 (1.4); 64 rows of 64
-// experts of 2048 x 2048 48, reading 537 MB.
+// 16384 x 768 x 2048 in one group 38 us (1.36 PFLOP/s), in 32 groups of 102 to 1684 rows 48; 16 groups of 4096 x 2048 197 (1.4); a row for each of 64
+// experts of 2048 x 2048 83, reading 537 MB (6.5 TB/s); 64 rows drawn for 34 of them 48 (285 MB).
 //
 // dW: a tile of W_g, K the group's rows. The last stage of a group is copied in boxes of 32, 16, ... 1 rows, and what is missing to the 16
 // rows of a matrix instruction comes as zeros from behind the last row of the matrix: rows of the next group, which may hold
-// anything, never reach shared memory. 32 groups as above 52 us; 64 matrices of 2048 x 2048 from a row each 118, writing 537 MB.
+// anything, never reach shared memory. 32 groups as above 53 us, in 32 bits 65; 64 matrices of 2048 x 2048 from a row each 139, writing 537 MB
+// (3.9 TB/s), of which 34 have a row 123.
 //
 // Rows that TMA cannot address (a base off the 16-byte boundary, or rows no multiple of 16 bytes apart) are copied first.
 #include "sk_gemm.cuh"

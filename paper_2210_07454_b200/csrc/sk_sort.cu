@@ -6,7 +6,7 @@
 //
 // One block does it all for up to 2048 assignments.  For more, a first launch counts by blocks, and in the second every block adds up the counts
 // of the blocks before it (from L2: a table of at most one row for each SM) before it does the same.  Bound by latency: 24 bytes an assignment
-// are little, the chain load - count - barrier - scan - barrier - deal is what takes the time. 16 assignments 3.4 us, 8192 of 64 experts 7, 262144 of 8 / 256 / 512 experts 7.7 / 11.5 /
+// are little, the chain load - count - barrier - scan - barrier - deal is what takes the time. 16 assignments 3.4 us, 8192 of 64 experts 6.6, 262144 of 8 / 256 / 512 experts 7.6 / 11.6 /
 // 15.3 (the blocks' counts, read by every block, grow with the experts).
 #include "sk_chain.cuh"
 #include "sk_operators.h"
@@ -29,7 +29,7 @@ __device__ __forceinline__ uint32_t expert_of(const SortArgs& a, uint64_t i) {
 }
 
 // The lanes of `there` with the same expert as this one's, a bit of its number at a time.  (The match instruction takes longer the more different values
-// there are: 8192 assignments to 64 experts took 17.7 us with it, 15.4 so.)
+// there are: 262144 assignments to 8, 256, 512 experts take 7.1, 12.3, 15.7 us with it.)
 __device__ __forceinline__ uint32_t same_expert(uint32_t there, uint32_t e, uint32_t bits) {
     uint32_t same = there;
     for (uint32_t b = 0; b < bits; ++b) {
