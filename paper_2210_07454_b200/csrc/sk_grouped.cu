@@ -803,6 +803,10 @@ __global__ void __launch_bounds__(256) k_grouped_unpack(const __grid_constant__ 
 }
 
 bool addressable(const void* p, uint64_t ld) { return (uintptr_t)p % 16 == 0 && ld % 8 == 0; }
+// The copy engine writes whole pieces of 16 bytes: behind a row that ends inside one it puts zeros. What lies there is not the output's, unless the rows are the workspace's own.
+bool by_boxes(const void* p, uint64_t ld_bytes, uint64_t stride_bytes, uint64_t row_bytes, bool own) {
+    return ((uintptr_t)p | ld_bytes | stride_bytes) % 16 == 0 && (own || row_bytes % 16 == 0);
+}
 
 // Copies that a call needs, and where they lie in the workspace.
 struct GroupedLayout {
@@ -1002,7 +1006,7 @@ int launch_rows(const GroupedArgs& a, const GroupedLayout& l, const RowsCall& c,
             return SK_OK;
         }
     }
-    RowsEpi::Args ea{{}, (uint16_t*)c.out, c.ld_out, bf16, row_alignment(c.out, c.ld_out, a.type), addressable(c.out, c.ld_out)};
+    RowsEpi::Args ea{{}, (uint16_t*)c.out, c.ld_out, bf16, row_alignment(c.out, c.ld_out, a.type), by_boxes(c.out, c.ld_out * 2, 0, p.features * 2, l.unpack_rows)};
     if (ea.by_box && !encode_out(&ea.map, c.out, 1, a.rows, p.features, c.ld_out, a.rows * c.ld_out, a.type, 16))
         return set_error(SK_ECUDA, "%s: the output cannot be described to the copy engine", __func__);
     SK_OP_CUDA((launch_plan<CG, BN, Plan, RowsEpi>(true, p, ea, units, st)));
@@ -1054,7 +1058,7 @@ int launch_matrices(const GroupedArgs& a, const GroupedLayout& l, const OpDevice
         ea.ld = l.ld_matrices;
         ea.stride = a.out * l.ld_matrices;
     }
-    ea.by_box = ((uintptr_t)ea.out | ea.ld * size | ea.stride * size) % 16 == 0;
+    ea.by_box = by_boxes(ea.out, ea.ld * size, ea.stride * size, a.width * size, l.unpack_matrices);
     if (ea.by_box && !encode_out(&ea.map, ea.out, a.groups, a.out, a.width, ea.ld, ea.stride, ea.type, 32))
         return set_error(SK_ECUDA, "%s: the output cannot be described to the copy engine", __func__);
     const uint32_t by_row = row_alignment(ea.out, ea.ld, ea.type), by_matrix = row_alignment(ea.out, ea.stride, ea.type);
