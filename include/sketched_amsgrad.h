@@ -413,9 +413,10 @@ int sk_policy_loss_backward(const float* dloss, const float* nll, const float* o
  * last report (SK_EDEVICE with a message: such a kernel's outputs are invalid).  Each is reported once. */
 int sk_operators_sync(void* stream);
 
-/* Test hook: the products of the calling thread's next sk_orthogonalize, if they are the tiles of one cooperative launch, wait for more
- * signals than are given, and every wait inside that kernel runs out after limit_ms (1..1000) milliseconds.  The kernel ends by
- * itself, with out unspecified, and the next sk_operators_sync reports it. */
+/* Test hook for the calling thread's next sk_orthogonalize, sk_grouped_linear or sk_grouped_linear_backward: its products, for the first if they are
+ * the tiles of one cooperative launch, wait for signals that are not given (for the others for operands that are not copied), and every
+ * wait inside those kernels runs out after limit_ms (1..1000) milliseconds.  They end by themselves, with the outputs unspecified, and the next
+ * sk_operators_sync reports it. */
 int sk_test_operators_wait(uint32_t limit_ms);
 
 const char* sk_last_error(void);

@@ -373,8 +373,10 @@ k_gemm(const __grid_constant__ Plan plan, const __grid_constant__ typename Epi::
 
     // The two single threads that feed the tensor cores have a stage's time, some 600 cycles, for each trip of their loops: what is constant
     // over a tile is in registers, and the ring's slot and its parity go round without divisions.
+    bool feeds = true;                                           // no copies: the waits for them, and for what would come of them, run out
+    if constexpr (Plan::kRagged) feeds = !plan.withheld;
     if (warp == 0) {
-        if (elect_one()) {
+        if (feeds && elect_one()) {
             uint32_t s = 0, parity = 1;                          // a fresh barrier counts as having completed its previous phase
             bool ok = true, any = false;
             for (uint32_t i = 0; ok && plan.job(unit, units, i, t); ++i) {

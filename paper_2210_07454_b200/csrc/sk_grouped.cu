@@ -166,6 +166,7 @@ struct RowsPlan {
     uint32_t beside;                                 // no
     uint32_t slices, each;                           // of K, and their stages
     uint32_t mn, k_rows, bf16, fill;                 // mn: the matrix is read along its rows; fill: rows of no group become zero
+    uint32_t withheld;                               // see k_gemm
     Waits waits;
     static constexpr bool kCooperative = false, kEmpty = false, kThree = false, kRagged = true;
     static constexpr uint32_t kStep = 16 * CG;       // of a tile's rows: a block's own are whole groups of eight, as the swizzle has them, and more
@@ -366,6 +367,7 @@ struct MatrixPlan {
     uint32_t most_slices;                            // of all groups together; 0: none is split
     uint32_t beside;                                 // it may run beside the kernel before it, the product that gives dx
     uint32_t* slices;                                // for each group their number, and that of the first one's sums
+    uint32_t withheld;                               // see k_gemm
     Waits waits;
     static constexpr bool kCooperative = false, kEmpty = false, kThree = false, kRagged = true;
     struct Table { uint16_t order[kSorted], first[kSorted + 1]; };       // groups by length, slices before each
@@ -980,7 +982,8 @@ int launch_rows(const GroupedArgs& a, const GroupedLayout& l, const RowsCall& c,
     p.mn = c.transposed;
     p.bf16 = bf16;
     p.fill = a.fill;
-    p.waits = dev.waits();
+    p.waits = a.waits(dev);
+    p.withheld = a.withhold_ms != 0;
     const Operand w{a.weight, a.out, a.width, a.ld_weight, a.stride_weight, (uint32_t)a.groups, c.transposed};
     const Operand x{c.rows, a.rows, K, c.ld_rows, 0, 1, false};
     bool ok = encode_operand(&p.matrix, w, bf16, c.transposed ? p.k_rows : 128);
@@ -1038,7 +1041,8 @@ int launch_matrices(const GroupedArgs& a, const GroupedLayout& l, const OpDevice
     p.tiles_m = (p.M + 128 * CG - 1) / (128 * CG);
     p.tiles_n = (p.N + BN - 1) / BN;
     p.bf16 = bf16;
-    p.waits = dev.waits();
+    p.waits = a.waits(dev);
+    p.withheld = a.withhold_ms != 0;
     const Operand dy{a.dy, a.rows, a.out, a.ld_dy, 0, 1, true}, x{a.x, a.rows, a.width, a.ld_x, 0, 1, true};
     bool ok = true;
     for (int q = 0; q < 7; ++q) ok = ok && encode_operand(&p.a[q], dy, bf16, 64 >> q) && encode_operand(&p.b[q], x, bf16, 64 >> q);

@@ -72,6 +72,11 @@ int check_workspace(const char* who, const void* ws, uint64_t have, uint64_t nee
     return SK_OK;
 }
 constexpr uint64_t kMaxExtent = 1ull << 31;
+uint32_t take_withhold_ms() {
+    const uint32_t ms = t_withhold_ms;
+    t_withhold_ms = 0;
+    return ms;
+}
 }  // namespace
 }  // namespace sk
 
@@ -250,9 +255,7 @@ int sk_orthogonalize(const void* update, uint64_t ld_update, uint64_t stride_upd
     if (int rc = check_workspace(who, workspace, workspace_bytes, orthogonalize_workspace(a))) return rc;
     OpDevice dev;
     if (int rc = op_device(&dev)) return rc;
-    const uint32_t withhold_ms = t_withhold_ms;
-    t_withhold_ms = 0;
-    return launch_orthogonalize(a, dev, withhold_ms, (cudaStream_t)stream);
+    return launch_orthogonalize(a, dev, take_withhold_ms(), (cudaStream_t)stream);
 }
 
 static int grouped_checked(const char* who, const GroupedArgs& a, bool backward) {
@@ -297,6 +300,7 @@ int sk_grouped_linear(const void* x, uint64_t ld_x, const void* weight, uint64_t
     if (int rc = check_workspace(who, workspace, workspace_bytes, grouped_workspace(a, false))) return rc;
     OpDevice dev;
     if (int rc = op_device(&dev)) return rc;
+    a.withhold_ms = take_withhold_ms();
     return launch_grouped(a, dev, (cudaStream_t)stream);
 }
 
@@ -340,6 +344,7 @@ int sk_grouped_linear_backward(const void* dy, uint64_t ld_dy, const void* x, ui
     if (int rc = check_workspace(who, workspace, workspace_bytes, grouped_workspace(a, true))) return rc;
     OpDevice dev;
     if (int rc = op_device(&dev)) return rc;
+    a.withhold_ms = take_withhold_ms();
     return launch_grouped_backward(a, dev, (cudaStream_t)stream);
 }
 

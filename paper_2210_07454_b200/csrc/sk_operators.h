@@ -258,6 +258,8 @@ struct GroupedArgs {
     uint64_t ld_dy, ld_dx, ld_dweight, stride_dweight;
     int dweight_type;
     void* workspace;
+    uint32_t withhold_ms;            // not zero in tests, see sk_test_operators_wait
+    Waits waits(const OpDevice& dev) const { return {dev.status, withhold_ms ? withhold_ms : kWaitLimitMs}; }
 };
 int launch_grouped(GroupedArgs a, const OpDevice& dev, cudaStream_t st);
 int launch_grouped_backward(GroupedArgs a, const OpDevice& dev, cudaStream_t st);
