@@ -65,6 +65,6 @@ def test_slices_of_k(ops, sizes, width, out, dtype):
 @pytest.mark.parametrize("dtype", HALF, ids=str)
 @pytest.mark.parametrize("sizes,width,out", [([700, 0, 33, 0, 1, 1500, 0], 1001, 1333), ([513, 511, 90, 1, 0, 64], 512, 768), ([i * 7 % 5 for i in range(2048)], 64, 40),
                                              ([i * 37 % 301 for i in range(300)], 72, 136), ([140_000, 3], 64, 2100), ([0, 200_001, 77] + [1] * 290, 136, 64), ([130], 33000, 600),
-                                             ([40, 90], 140_000, 5000)], ids=lambda v: str(v)[:40])
+                                             ([40, 90], 140_000, 5000), ([900, 0, 333], 33_001, 2101), ([1100], 131_075, 2101)], ids=lambda v: str(v)[:40])
 def test_whole_sums(ops, sizes, width, out, dtype):
     check(ops, sizes, 11, 30, width, out, dtype)
